@@ -280,6 +280,107 @@ spd_status spd_service_attn_merge_append(const spd_shape *shape, const void *q, 
                                          void *cuda_stream);
 
 /*
+ * Scored calls: attention whose scores are not the plain scaled products.  (The paper's prototype runs models with
+ * rotary positions and plain scores; these calls serve models that cap their scores, bias them by distance, or look back
+ * through a sliding window, over the same two partitions.)  Tokens are numbered through the private and then the public
+ * partition, and the query of a decode call is the last of them; with d = (query's position - key's position) >= 0,
+ *     s = sm_scale q.k;   s <- logit_cap tanh(s / logit_cap);   s <- s - alibi_slopes[h] d;   hidden where d >= window.
+ *   logit_cap    : 0 = none, else within [1e-30, 1e30].
+ *   window       : 0 = none, else the query sees itself and the window - 1 tokens before it.  Pages that lie wholly in front
+ *                  of the window are neither listed nor read (their page_indices entries may hold anything), and rows in
+ *                  front of it inside the first page never enter a result, whatever they hold.
+ *   alibi_slopes : device [num_q_heads] fp32, or NULL = no bias.
+ * spd_decode_step_scored is spd_decode_step (fused) with these scores.  spd_partial_attn_scored and
+ * spd_service_attn_merge_scored are its two halves: each sees one partition and is told how many tokens the other one holds
+ * (pub_lens, priv_lens: device [batch]; a negative entry, or a sum beyond 2^31 - 1, raises SPD_ERR_BAD_PAGE for the user).
+ * A partition wholly in front of the window gives the empty partial.  `plan` as for the *_planned calls; a plan also fits
+ * only calls with the same window.  spd_set_bf16_math does not concern these calls (tensor cores always).  Stream order,
+ * errors and workspace as for the plain calls.
+ */
+typedef struct {
+    float        logit_cap;
+    int32_t      window;
+    const float *alibi_slopes;
+} spd_score;
+spd_status spd_partial_attn_scored(const spd_shape *shape, const spd_score *score, const void *q,
+                                   const spd_paged_kv *priv, const int32_t *pub_lens, spd_partial out,
+                                   spd_plan_mode plan, void *ws, size_t ws_bytes, void *cuda_stream);
+spd_status spd_service_attn_merge_scored(const spd_shape *shape, const spd_score *score, const void *q,
+                                         const spd_paged_kv *pub, const int32_t *priv_lens, spd_partial in,
+                                         void *out, spd_dtype out_dtype, spd_plan_mode plan, void *ws,
+                                         size_t ws_bytes, void *cuda_stream);
+spd_status spd_decode_step_scored(const spd_shape *shape, const spd_score *score, const void *q,
+                                  const spd_paged_kv *priv, const spd_paged_kv *pub, void *out,
+                                  spd_dtype out_dtype, spd_plan_mode plan, void *ws, size_t ws_bytes,
+                                  void *cuda_stream);
+
+/*
+ * Rows of new tokens, as a projection leaves them: [total_tokens][heads][head_dim] in the shape's dtype, consecutive
+ * tokens *_stride elements apart (0 = packed, i.e. heads * head_dim; q, k and v may be parts of one wider row).  Strides
+ * and pointers are multiples of 16 bytes.
+ */
+typedef struct {
+    const void *q, *k, *v;
+    int64_t     q_stride, k_stride, v_stride;
+} spd_tokens;
+
+/*
+ * Prompt attention with the scores of the scored calls and interval masks (no counterpart in the paper): row i of a prompt
+ * sees its keys j with lo_i <= j <= hi_i, positions counted within the prompt,
+ *     lo_i = max(0, doc_start_i, i - window + 1),     hi_i = i, or min(prefix_lens[u], length) - 1 where i lies below that.
+ *   prefix_lens : device [batch] or NULL; the first prefix_lens[u] tokens see one another in both directions.
+ *   doc_start   : device [total_tokens] or NULL; the first token that the row may see (packed documents: its document's
+ *                 first token; padding: anything above i).
+ * d is |i - j|.  A row that sees nothing gives zeros.  Keys that a row does not see never enter its result, whatever
+ * their rows of k and v hold.  `tok` as above; tok_indptr [batch+1] (device), its consistency and what happens where it
+ * is not consistent as for spd_prefill_attn; out [total_tokens][num_q_heads][head_dim] in out_dtype, packed.  The prompts'
+ * rows do not go to a cache here: spd_append_kv_rope does that, with or without rotation.  sm_scale > 0, else
+ * SPD_ERR_UNSUPPORTED.
+ */
+spd_status spd_prefill_attn_scored(const spd_shape *shape, const spd_score *score, int64_t total_tokens,
+                                   const spd_tokens *tok, const int32_t *tok_indptr, const int32_t *prefix_lens,
+                                   const int32_t *doc_start, void *out, spd_dtype out_dtype, void *ws,
+                                   size_t ws_bytes, void *cuda_stream);
+
+/*
+ * Append with the position rotation on the way (protocol step 3a for models with rotary positions; also step 2's hand-over
+ * of prompts): the new tokens' q and k rows are rotated, k and v written to the paged cache behind what it holds.
+ *   rotation of a head: pair i of rotary_dim / 2 -- channels (i, i + rotary_dim / 2), or (2 i, 2 i + 1) with interleaved != 0
+ *     -- turns by the angle pos * inv_freq[i] and is multiplied by `scale`; channels from rotary_dim on are copied.
+ *     rotary_dim is a multiple of 16, at most head_dim.  Angles are formed in 64 bits, products in fp32, rounded once.
+ *     num_axes > 1 (image and video prompts: time, height, width): the first sections[0] pairs go by positions[0][token],
+ *     the next sections[1] by positions[1][token], and so on; the sections add up to rotary_dim / 2.
+ *     rope == NULL: no rotation, k and v are appended as they are and q is not touched (ALiBi models).
+ *   tok_indptr [batch+1] (device): user u brings tokens [tok_indptr[u], tok_indptr[u+1]) of the total_tokens rows; it starts
+ *     at 0, is non-decreasing and ends at total_tokens -- otherwise the call raises SPD_ERR_BAD_PAGE for the first user where
+ *     it is not, and writes nothing but new_lens (the old lengths).  NULL: one token per user, total_tokens == batch.
+ *   positions [num_axes][total_tokens] (device, int32) or NULL: then token i of user u has position
+ *     pos_base[u] + seq_lens[u] + i (pos_base NULL = 0; the private lengths, when appending to the public partition).
+ *     Required when num_axes > 1; not together with pos_base.
+ *   q_out [total_tokens][num_q_heads][head_dim], k_out [total_tokens][num_kv_heads][head_dim], packed: the rotated rows; may
+ *     be the (packed) inputs themselves; k_out may be NULL.  They are written for every token of a consistent tok_indptr.
+ *   cache: token i of user u goes to position seq_lens[u] + i of the partition.  new_lens [batch] receives the grown
+ *     lengths; it may be seq_lens itself (in place), another array, or NULL (lengths are the caller's business, e.g. counted
+ *     once for all layers).  A user whose listed pages cannot hold the new tokens, or with a page out of range among
+ *     them, keeps its length and raises SPD_ERR_BAD_PAGE; rows behind its length may have been written.
+ * One kernel in plain stream order.  Two tokens of one call must not land in one slot (shared pages).
+ */
+typedef struct {
+    int32_t      rotary_dim;
+    int32_t      interleaved;
+    int32_t      num_axes;      /* 1 .. 4 */
+    int32_t      sections[4];   /* pairs per axis; only read when num_axes > 1 */
+    float        scale;         /* finite; 1 = a pure rotation */
+    const float *inv_freq;      /* device [rotary_dim / 2] */
+} spd_rope;
+spd_status spd_append_kv_rope(const spd_shape *shape, const spd_rope *rope, int64_t total_tokens,
+                              const spd_tokens *tok, const int32_t *tok_indptr, const int32_t *positions,
+                              const int32_t *pos_base, void *q_out, void *k_out, void *k_pool, void *v_pool,
+                              int32_t num_pages, const int32_t *page_indptr, const int32_t *page_indices,
+                              const int32_t *seq_lens, int32_t *new_lens, void *ws, size_t ws_bytes,
+                              void *cuda_stream);
+
+/*
  * One token step over `num_layers` layers (protocol step 3 for every layer of the model; Fig. 3 steps 2 to
  * 5): for each layer in order, the new token's K and V rows are appended to that layer's public cache and the
  * layer's decode step runs, both inside one launch (spd_decode_step_append).  `layers` is a HOST array;

@@ -27,7 +27,9 @@ EXPORTS = ["spd_workspace_size", "spd_partial_attn", "spd_service_attn_merge", "
            "spd_partial_attn_watch", "spd_decode_step_watch", "spd_set_bf16_math", "spd_merge_partials", "spd_prefill_attn",
            "spd_set_prefill_rows", "spd_token_step", "spd_partial_attn_planned", "spd_service_attn_merge_planned",
            "spd_decode_step_planned", "spd_set_split", "spd_set_programmatic_launch", "spd_debug_read_plan",
-           "spd_debug_sm_moves", "spd_decode_step_append", "spd_watch_alarm", "spd_service_attn_merge_append"]
+           "spd_debug_sm_moves", "spd_decode_step_append", "spd_watch_alarm", "spd_service_attn_merge_append",
+           "spd_partial_attn_scored", "spd_service_attn_merge_scored", "spd_decode_step_scored", "spd_prefill_attn_scored",
+           "spd_append_kv_rope"]
 
 
 class SpdError(RuntimeError):
@@ -60,6 +62,20 @@ class StepBlob(C.Structure):
 
 class Watch(C.Structure):
     _fields_ = [("tok_lo", C.c_void_p), ("tok_hi", C.c_void_p), ("out", C.c_void_p)]
+
+
+class Score(C.Structure):
+    _fields_ = [("logit_cap", C.c_float), ("window", C.c_int32), ("alibi_slopes", C.c_void_p)]
+
+
+class Tokens(C.Structure):
+    _fields_ = [("q", C.c_void_p), ("k", C.c_void_p), ("v", C.c_void_p), ("q_stride", C.c_int64), ("k_stride", C.c_int64),
+                ("v_stride", C.c_int64)]
+
+
+class Rope(C.Structure):
+    _fields_ = [("rotary_dim", C.c_int32), ("interleaved", C.c_int32), ("num_axes", C.c_int32), ("sections", C.c_int32 * 4),
+                ("scale", C.c_float), ("inv_freq", C.c_void_p)]
 
 
 class Partial(C.Structure):
@@ -108,6 +124,16 @@ def lib() -> C.CDLL:
                                              C.c_int, vp, sz, vp]
         L.spd_service_attn_merge_append.argtypes = [C.POINTER(Shape), vp, vp, vp, C.POINTER(PagedKV), Partial, vp, C.c_int, C.c_int,
                                                     vp, sz, vp]
+        L.spd_partial_attn_scored.argtypes = [C.POINTER(Shape), C.POINTER(Score), vp, C.POINTER(PagedKV), vp, Partial, C.c_int,
+                                              vp, sz, vp]
+        L.spd_service_attn_merge_scored.argtypes = [C.POINTER(Shape), C.POINTER(Score), vp, C.POINTER(PagedKV), vp, Partial, vp,
+                                                    C.c_int, C.c_int, vp, sz, vp]
+        L.spd_decode_step_scored.argtypes = [C.POINTER(Shape), C.POINTER(Score), vp, C.POINTER(PagedKV), C.POINTER(PagedKV), vp,
+                                             C.c_int, C.c_int, vp, sz, vp]
+        L.spd_prefill_attn_scored.argtypes = [C.POINTER(Shape), C.POINTER(Score), C.c_int64, C.POINTER(Tokens), vp, vp, vp, vp,
+                                              C.c_int, vp, sz, vp]
+        L.spd_append_kv_rope.argtypes = [C.POINTER(Shape), C.POINTER(Rope), C.c_int64, C.POINTER(Tokens), vp, vp, vp, vp, vp, vp,
+                                         vp, C.c_int32, vp, vp, vp, vp, vp, sz, vp]
         L.spd_watch_alarm.argtypes = [vp, C.c_int32, C.c_int32, vp, C.c_float, vp, vp]
         L.spd_set_split.argtypes = [C.c_int32, C.c_int32]
         L.spd_set_programmatic_launch.argtypes = [C.c_int32]
@@ -447,3 +473,113 @@ def spd_prefill_attn(shape, q, k, v, tok_indptr, part, out, ws, stream=None) -> 
                                   part.page_indptr.data_ptr(), _ptr(part.page_indices), part.seq_lens.data_ptr(),
                                   _ptr(out), _dtype_code(out.dtype), ws.data_ptr(), ws.numel(), _stream_ptr(stream)),
            "spd_prefill_attn")
+
+
+def make_score(logit_cap: float = 0.0, window: int = 0, alibi_slopes: Optional[torch.Tensor] = None) -> Score:
+    """Score options of the *_scored calls; alibi_slopes: float32 [num_q_heads] on the device."""
+    sc = Score(float(logit_cap), int(window), None)
+    if alibi_slopes is not None:
+        assert alibi_slopes.dtype == torch.float32 and alibi_slopes.is_contiguous() and alibi_slopes.is_cuda
+        sc.alibi_slopes = alibi_slopes.data_ptr()
+        sc._keep = alibi_slopes
+    return sc
+
+
+def make_rope(inv_freq: torch.Tensor, interleaved: bool = False, sections=None, scale: float = 1.0) -> Rope:
+    """Rotation of spd_append_kv_rope; inv_freq: float32 [rotary_dim / 2] on the device; sections: pairs per position axis."""
+    assert inv_freq.dtype == torch.float32 and inv_freq.is_contiguous() and inv_freq.is_cuda and inv_freq.dim() == 1
+    rope = Rope(2 * inv_freq.numel(), 1 if interleaved else 0, len(sections) if sections else 1, (C.c_int32 * 4)(*(sections or ())),
+                float(scale), inv_freq.data_ptr())
+    rope._keep = inv_freq
+    return rope
+
+
+def _check_slopes(shape, score) -> None:
+    keep = getattr(score, "_keep", None)
+    assert keep is None or keep.numel() == shape.num_q_heads
+
+
+def _rows(shape, t: torch.Tensor, heads: int, n: int):
+    """(pointer, token stride in elements) of [n, heads, head_dim] rows that may be part of a wider row per token."""
+    assert t.dtype == (torch.float32 if shape.dtype == SPD_F32 else torch.bfloat16)
+    assert tuple(t.shape) == (n, heads, shape.head_dim)
+    if n == 0:
+        return None, 0
+    assert t.stride(2) == 1 and (heads == 1 or t.stride(1) == shape.head_dim)
+    return t.data_ptr(), t.stride(0) if n > 1 else 0
+
+
+def _i32(t: Optional[torch.Tensor], *size) -> Optional[int]:
+    """Pointer of an int32 tensor of the given shape, or None."""
+    if t is None:
+        return None
+    assert t.dtype == torch.int32 and t.is_contiguous() and tuple(t.shape) == size, (t.dtype, tuple(t.shape), size)
+    return t.data_ptr()
+
+
+def spd_partial_attn_scored(shape, score, q, priv, pub_lens, out, ws, plan=SPD_PLAN_PER_CALL, stream=None) -> None:
+    """spd_partial_attn with score options; pub_lens: int32 [batch], tokens in the public partition."""
+    _check_slopes(shape, score)
+    kv = paged_kv(priv)
+    part = Partial(out[0].data_ptr(), out[1].data_ptr(), out[2].data_ptr())
+    _check(lib().spd_partial_attn_scored(C.byref(shape), C.byref(score), q.data_ptr(), C.byref(kv), _i32(pub_lens, shape.batch), part,
+                                         int(plan), ws.data_ptr(), ws.numel(), _stream_ptr(stream)), "spd_partial_attn_scored")
+
+
+def spd_service_attn_merge_scored(shape, score, q, pub, priv_lens, partial_in, out, ws, plan=SPD_PLAN_PER_CALL, stream=None) -> None:
+    """spd_service_attn_merge with score options; priv_lens: int32 [batch], tokens in the private partition."""
+    _check_slopes(shape, score)
+    kv = paged_kv(pub)
+    part = Partial(partial_in[0].data_ptr(), partial_in[1].data_ptr(), partial_in[2].data_ptr())
+    _check(lib().spd_service_attn_merge_scored(C.byref(shape), C.byref(score), q.data_ptr(), C.byref(kv), _i32(priv_lens, shape.batch),
+                                               part, out.data_ptr(), _dtype_code(out.dtype), int(plan), ws.data_ptr(), ws.numel(),
+                                               _stream_ptr(stream)), "spd_service_attn_merge_scored")
+
+
+def spd_decode_step_scored(shape, score, q, priv, pub, out, ws, plan=SPD_PLAN_PER_CALL, stream=None) -> None:
+    """The fused decode step with score options (make_score) over both partitions."""
+    _check_slopes(shape, score)
+    a, b = paged_kv(priv), paged_kv(pub)
+    _check(lib().spd_decode_step_scored(C.byref(shape), C.byref(score), q.data_ptr(), C.byref(a), C.byref(b), out.data_ptr(),
+                                        _dtype_code(out.dtype), int(plan), ws.data_ptr(), ws.numel(), _stream_ptr(stream)),
+           "spd_decode_step_scored")
+
+
+def spd_prefill_attn_scored(shape, score, q, k, v, tok_indptr, out, ws, prefix_lens=None, doc_start=None, stream=None) -> None:
+    """Prompt attention with score options and interval masks: q [T,Hq,D], k, v [T,Hkv,D] (rows may be parts of a wider row per
+    token), tok_indptr int32 [B+1], prefix_lens int32 [B], doc_start int32 [T], out [T,Hq,D] packed."""
+    _check_slopes(shape, score)
+    T = int(q.shape[0])
+    (qp, qs), (kp, ks), (vp, vs) = (_rows(shape, t, h, T) for t, h in ((q, shape.num_q_heads), (k, shape.num_kv_heads), (v, shape.num_kv_heads)))
+    assert out.is_contiguous() and out.numel() == T * shape.num_q_heads * shape.head_dim
+    tok = Tokens(qp, kp, vp, qs, ks, vs)
+    _check(lib().spd_prefill_attn_scored(C.byref(shape), C.byref(score), T, C.byref(tok), _i32(tok_indptr, shape.batch + 1),
+                                         _i32(prefix_lens, shape.batch), _i32(doc_start, T), _ptr(out), _dtype_code(out.dtype),
+                                         ws.data_ptr(), ws.numel(), _stream_ptr(stream)), "spd_prefill_attn_scored")
+
+
+def spd_append_kv_rope(shape, rope, q, k, v, part, ws, q_out=None, k_out=None, tok_indptr=None, positions=None, pos_base=None,
+                       new_lens="in place", stream=None) -> None:
+    """Rotate the new tokens' q and k rows (into q_out, k_out) and append k and v to the partition `part`.
+
+    rope: make_rope(...) or None (no rotation; q and q_out are not used).  tok_indptr int32 [B+1]: tokens per user; None: one
+    token per user.  positions int32 [axes, T] or [T]; pos_base int32 [B].  new_lens: an int32 [B] tensor, None, or by default
+    part.seq_lens itself."""
+    T, B = int(k.shape[0]), shape.batch
+    kp, ks = _rows(shape, k, shape.num_kv_heads, T)
+    vp, vs = _rows(shape, v, shape.num_kv_heads, T)
+    qp, qs = _rows(shape, q, shape.num_q_heads, T) if rope is not None else (None, 0)
+    for o, heads in ((q_out, shape.num_q_heads), (k_out, shape.num_kv_heads)):
+        assert o is None or (o.is_contiguous() and o.dtype == k.dtype and o.numel() == T * heads * shape.head_dim)
+    if positions is not None:
+        positions = positions.view(1, -1) if positions.dim() == 1 else positions
+        assert rope is not None and positions.shape[0] == rope.num_axes
+    tok = Tokens(qp, kp, vp, qs, ks, vs)
+    for t in (part.k_pool, part.v_pool, part.page_indices):
+        assert t.is_contiguous()
+    lens = part.seq_lens if isinstance(new_lens, str) else new_lens
+    _check(lib().spd_append_kv_rope(C.byref(shape), C.byref(rope) if rope is not None else None, T, C.byref(tok), _i32(tok_indptr, B + 1),
+                                    _i32(positions, rope.num_axes, T) if positions is not None else None, _i32(pos_base, B),
+                                    _ptr(q_out), _ptr(k_out), part.k_pool.data_ptr(), part.v_pool.data_ptr(), int(part.k_pool.shape[0]),
+                                    _i32(part.page_indptr, B + 1), _ptr(part.page_indices), _i32(part.seq_lens, B), _i32(lens, B),
+                                    ws.data_ptr(), ws.numel(), _stream_ptr(stream)), "spd_append_kv_rope")

@@ -8,15 +8,15 @@ import sys
 _PKG = os.path.dirname(os.path.abspath(__file__))
 _ROOT = os.path.dirname(_PKG)
 LIB_PATH = os.path.join(_PKG, "libspd.so")
-SOURCES = [os.path.join(_PKG, "csrc", "spd_api.cu")]
-HEADERS = sorted(os.path.join(_PKG, "csrc", f) for f in os.listdir(os.path.join(_PKG, "csrc")) if f.endswith(".cuh")) + \
+SOURCES = [os.path.join(_PKG, "csrc", f) for f in ("spd_api.cu", "spd_scored.cu")]
+HEADERS = sorted(os.path.join(_PKG, "csrc", f) for f in os.listdir(os.path.join(_PKG, "csrc")) if f.endswith((".cuh", ".h"))) + \
           [os.path.join(_ROOT, "include", "spd.h")]
 
 
 def nvcc_command(verbose: bool = False):
     nvcc = os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")
     cmd = [nvcc, "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
-           "-shared", "-Xcompiler", "-fPIC", "-I", os.path.join(_ROOT, "include"), "-o", LIB_PATH] + SOURCES
+           "-t", str(len(SOURCES)), "-shared", "-Xcompiler", "-fPIC", "-I", os.path.join(_ROOT, "include"), "-o", LIB_PATH] + SOURCES
     if verbose:
         cmd[1:1] = ["-Xptxas", "-v"]
     return cmd

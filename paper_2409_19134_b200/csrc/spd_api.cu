@@ -10,7 +10,8 @@
 #include <unordered_map>
 #include <vector>
 
-#include "spd_kernels.cuh"
+#include "spd_host.h"
+#include "spd_launch.cuh"
 #include "spd_prefill.cuh"
 #include "spd_prefill_pair.cuh"
 #include "spd_prefill_fma.cuh"
@@ -145,10 +146,6 @@ spd_status host_step_streams(HostStepStreams *out) {
 #define SPD_TMA_L2_PROMOTION CU_TENSOR_MAP_L2_PROMOTION_L2_256B
 #endif
 
-typedef CUresult (*EncodeTiledFn)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *,
-                                  const cuuint64_t *, const cuuint32_t *, const cuuint32_t *, CUtensorMapInterleave,
-                                  CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
-
 EncodeTiledFn encode_fn() {
     static EncodeTiledFn fn = nullptr;
     static std::once_flag once;
@@ -223,7 +220,15 @@ spd_status check_shape(const spd_shape *s) {
     return SPD_OK;
 }
 
-bool misaligned(const void *p, size_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) != 0; }
+using host::misaligned;
+
+spd_status check_score(const spd_score *sc) {
+    if (!sc) return SPD_ERR_INVALID_ARG;
+    const float cap = sc->logit_cap;      // NaN, infinity and caps whose reciprocal would leave fp32 are refused
+    if (!(cap == 0.f || (cap >= 1e-30f && cap <= 1e30f)) || sc->window < 0) return SPD_ERR_INVALID_ARG;
+    if (misaligned(sc->alibi_slopes, 4)) return SPD_ERR_INVALID_ARG;
+    return SPD_OK;
+}
 
 spd_status check_kv(const spd_shape *s, const spd_paged_kv *kv) {
     if (!kv) return SPD_ERR_INVALID_ARG;
@@ -255,44 +260,6 @@ spd_status make_map(CUtensorMap *map, const spd_shape &s, const void *pool, int6
     return r == CUDA_SUCCESS ? SPD_OK : SPD_ERR_CUDA;
 }
 
-template <class Math>
-spd_status launch_attn(const Params &p_in, const CUtensorMap *maps, int sms, cudaStream_t st, bool pdl) {
-    if (sms > kMaxGrid) return SPD_ERR_UNSUPPORTED;
-    Params p = p_in;
-    p.num_warps = sms * Math::kWarps;   // the plan cuts the tile stream into one share per warp of THIS grid
-    // At least 117 KB, so that an SM never holds two of these CTAs whatever the variant needs: the kernel's
-    // reasoning about which launch can still be running when the next but one starts rests on one CTA per SM.
-    const size_t smem = attn_smem_bytes<Math>(sms) > 117 * 1024 ? attn_smem_bytes<Math>(sms) : 117 * 1024;
-    static std::once_flag once[64];
-    int dev = 0;
-    cudaGetDevice(&dev);
-    cudaError_t attr_err = cudaSuccess;
-    std::call_once(once[dev & 63], [&] {
-        attr_err = cudaFuncSetAttribute(attn_kernel<Math>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                        static_cast<int>(smem));
-    });
-    if (attr_err != cudaSuccess) {
-        fprintf(stderr, "libspd: cudaFuncSetAttribute(dynamic shared memory %zu): %s\n", smem, cudaGetErrorString(attr_err));
-        return SPD_ERR_CUDA;
-    }
-    // Programmatic stream serialisation (pdl): this kernel's read-only preamble may overlap the tail of the
-    // previous kernel on the stream if that kernel allows it (the attention kernel does).
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(sms);
-    cfg.blockDim = dim3(Math::kWarps * 32);
-    cfg.dynamicSmemBytes = smem;
-    cfg.stream = st;
-    cudaLaunchAttribute attr[1];
-    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr[0].val.programmaticStreamSerializationAllowed = 1;
-    cfg.attrs = attr;
-    cfg.numAttrs = pdl ? 1 : 0;
-    const cudaError_t err = cudaLaunchKernelEx(&cfg, attn_kernel<Math>, p, maps[0], maps[1], maps[2], maps[3]);
-    ++g_launches;
-    if (err != cudaSuccess) fprintf(stderr, "libspd: launch of the attention kernel: %s\n", cudaGetErrorString(err));
-    return err == cudaSuccess ? SPD_OK : SPD_ERR_CUDA;
-}
-
 // What one library call boils down to: one launch of the attention kernel.
 struct Job {
     const spd_shape *shape;
@@ -310,14 +277,16 @@ struct Job {
     bool plain_order;              // launch in plain stream order (an input was written by the kernel just before)
     const void *k_new, *v_new;     // optional append of the new token's rows to part[1] inside the launch
     bool wait_first;               // read nothing before the previous kernel on the stream has finished, not even a stored plan
+    const spd_score *score;        // optional: capped scores, distance bias, window
+    const int32_t *peer_lens[2];   // scored: lengths of a partition that the call does not read
     const spd_shape *layout_shape; // shape that lays the workspace out, if not `shape` (a call served in two halves keeps the whole batch's layout)
 };
 
 // The stored plan of a call is tagged with what it was cut for besides the lengths, so that a launch told to load a
 // plan which was never stored (or stored for another shape) reports SPD_ERR_PLAN instead of using it.
-int32_t plan_tag_of(const spd_shape &s, int min_tiles, int uniform) {
+int32_t plan_tag_of(const spd_shape &s, int min_tiles, int uniform, int window) {
     uint32_t h = 0x9e3779b9u;
-    const int32_t v[] = {s.batch, s.num_q_heads, s.num_kv_heads, s.head_dim, static_cast<int32_t>(s.dtype), min_tiles, uniform};
+    const int32_t v[] = {s.batch, s.num_q_heads, s.num_kv_heads, s.head_dim, static_cast<int32_t>(s.dtype), min_tiles, uniform, window};
     for (int32_t x : v) h = (h ^ static_cast<uint32_t>(x)) * 0x01000193u + 0x7f4a7c15u;
     h &= 0x7fffffffu;
     return static_cast<int32_t>(h ? h : 1u);
@@ -357,7 +326,7 @@ spd_status run_job(const Job &job, void *ws, size_t ws_bytes, void *stream) {
     p.uniform = g_uniform_shares.load();
     p.plan = reinterpret_cast<int32_t *>(w + L.plan + slot * kPlanBytes);
     p.plan_mode = job.plan_mode;
-    p.plan_tag = plan_tag_of(s, p.min_tiles, p.uniform);
+    p.plan_tag = plan_tag_of(s, p.min_tiles, p.uniform, job.score ? job.score->window : 0);
     p.epoch = job.epoch;
     p.scratch = reinterpret_cast<float *>(w + L.scratch);
     p.mode = job.mode;
@@ -366,6 +335,14 @@ spd_status run_job(const Job &job, void *ws, size_t ws_bytes, void *stream) {
     p.out = job.out;
     p.out_bf16 = job.out_dtype == SPD_BF16;
     if (job.watch) { p.watch_lo = job.watch->tok_lo; p.watch_hi = job.watch->tok_hi; p.watch_out = job.watch->out; }
+    if (job.score) {
+        p.scored = 1;
+        p.cap = job.score->logit_cap;
+        p.cap_log2 = p.cap > 0.f ? 2.f * kLog2e / p.cap : 0.f;
+        p.window = job.score->window;
+        p.slopes = job.score->alibi_slopes;
+        p.peer_lens[0] = job.peer_lens[0]; p.peer_lens[1] = job.peer_lens[1];
+    }
     if (job.k_new) {
         if (!job.part[1] || !job.v_new || job.part[1]->num_pages <= 0 || misaligned(job.k_new, 16) || misaligned(job.v_new, 16))
             return SPD_ERR_INVALID_ARG;
@@ -412,7 +389,9 @@ spd_status run_job(const Job &job, void *ws, size_t ws_bytes, void *stream) {
     prof_mark(pj, 0, st);
     const int D = s.head_dim;
     const bool pdl = programmatic_launch() && !job.plain_order;
-    if (bf && g_bf16_math.load() == 1) {
+    if (job.score) {
+        rc = launch_attn_scored(p, maps, di.sms, st, pdl, bf, D);
+    } else if (bf && g_bf16_math.load() == 1) {
 #define SPD_SIMT_CASE(DD, GG) if (D == DD && p.geff == GG) rc = launch_attn<MathBF16Simt<DD, GG>>(p, maps, di.sms, st, pdl);
         SPD_SIMT_CASE(64, 1) SPD_SIMT_CASE(64, 2) SPD_SIMT_CASE(64, 4) SPD_SIMT_CASE(64, 8)
         SPD_SIMT_CASE(128, 1) SPD_SIMT_CASE(128, 2) SPD_SIMT_CASE(128, 4) SPD_SIMT_CASE(128, 8)
@@ -440,6 +419,26 @@ spd_partial ws_partial(const spd_shape &s, void *ws, int sms) {
 }
 
 }  // namespace
+
+namespace spd {
+namespace host {
+
+spd_status check_shape(const spd_shape *s) { return ::check_shape(s); }
+spd_status check_score(const spd_score *score) { return ::check_score(score); }
+spd_status device_sms(int *sms) {
+    DeviceInfo di;
+    const spd_status rc = device_info(&di);
+    *sms = di.sms;
+    return rc;
+}
+EncodeTiledFn tensor_map_encoder() { return encode_fn(); }
+int32_t next_call_id() { return next_epoch(); }
+void count_launch() { ++g_launches; }
+size_t flags_offset(int batch) { return ws_head(batch, 0).bad; }
+size_t flags_end(int batch) { return ws_head(batch, 0).tickets; }
+
+}  // namespace host
+}  // namespace spd
 
 extern "C" {
 
@@ -620,6 +619,58 @@ spd_status spd_decode_step_watch(const spd_shape *shape, const void *q, const sp
     job.mode = OUT_FINAL; job.out = out; job.out_dtype = out_dtype;
     job.epoch = next_epoch();
     job.watch = watch;
+    return run_job(job, ws, ws_bytes, cuda_stream);
+}
+
+spd_status spd_partial_attn_scored(const spd_shape *shape, const spd_score *score, const void *q, const spd_paged_kv *priv,
+                                   const int32_t *pub_lens, spd_partial out, spd_plan_mode plan, void *ws, size_t ws_bytes,
+                                   void *cuda_stream) {
+    spd_status rc = check_shape(shape);
+    if (rc != SPD_OK) return rc;
+    if ((rc = check_score(score)) != SPD_OK || (rc = check_plan(plan)) != SPD_OK || (rc = check_kv(shape, priv)) != SPD_OK) return rc;
+    if (!pub_lens || !out.o || !out.m || !out.l || misaligned(out.o, 16)) return SPD_ERR_INVALID_ARG;
+    Job job{};
+    job.shape = shape; job.q = q; job.part[0] = priv;
+    job.mode = OUT_PARTIAL; job.pout = out; job.out_dtype = SPD_F32;
+    job.epoch = next_epoch();
+    job.plan_mode = plan;
+    job.score = score; job.peer_lens[1] = pub_lens;
+    return run_job(job, ws, ws_bytes, cuda_stream);
+}
+
+spd_status spd_service_attn_merge_scored(const spd_shape *shape, const spd_score *score, const void *q, const spd_paged_kv *pub,
+                                         const int32_t *priv_lens, spd_partial in, void *out, spd_dtype out_dtype,
+                                         spd_plan_mode plan, void *ws, size_t ws_bytes, void *cuda_stream) {
+    spd_status rc = check_shape(shape);
+    if (rc != SPD_OK) return rc;
+    if ((rc = check_score(score)) != SPD_OK || (rc = check_plan(plan)) != SPD_OK || (rc = check_kv(shape, pub)) != SPD_OK) return rc;
+    if (!priv_lens || !in.o || !in.m || !in.l || misaligned(in.o, 16)) return SPD_ERR_INVALID_ARG;
+    if (!out || misaligned(out, 16)) return SPD_ERR_INVALID_ARG;
+    if (out_dtype != SPD_F32 && out_dtype != SPD_BF16) return SPD_ERR_UNSUPPORTED;
+    Job job{};
+    job.shape = shape; job.q = q; job.part[1] = pub;
+    job.mode = OUT_FINAL; job.pin = &in; job.out = out; job.out_dtype = out_dtype;
+    job.epoch = next_epoch();
+    job.plan_mode = plan;
+    job.score = score; job.peer_lens[0] = priv_lens;
+    return run_job(job, ws, ws_bytes, cuda_stream);
+}
+
+spd_status spd_decode_step_scored(const spd_shape *shape, const spd_score *score, const void *q, const spd_paged_kv *priv,
+                                  const spd_paged_kv *pub, void *out, spd_dtype out_dtype, spd_plan_mode plan, void *ws,
+                                  size_t ws_bytes, void *cuda_stream) {
+    spd_status rc = check_shape(shape);
+    if (rc != SPD_OK) return rc;
+    if ((rc = check_score(score)) != SPD_OK || (rc = check_plan(plan)) != SPD_OK) return rc;
+    if ((rc = check_kv(shape, priv)) != SPD_OK || (rc = check_kv(shape, pub)) != SPD_OK) return rc;
+    if (!out || misaligned(out, 16)) return SPD_ERR_INVALID_ARG;
+    if (out_dtype != SPD_F32 && out_dtype != SPD_BF16) return SPD_ERR_UNSUPPORTED;
+    Job job{};
+    job.shape = shape; job.q = q; job.part[0] = priv; job.part[1] = pub;
+    job.mode = OUT_FINAL; job.out = out; job.out_dtype = out_dtype;
+    job.epoch = next_epoch();
+    job.plan_mode = plan;
+    job.score = score;
     return run_job(job, ws, ws_bytes, cuda_stream);
 }
 

@@ -101,6 +101,12 @@ struct Params {
     // optional monitor: softmax mass on tokens [watch_lo[u], watch_hi[u]) of the private partition
     const int32_t *watch_lo, *watch_hi;   // [B]
     float *watch_out;                      // [B][Hq]; null = not watching
+    // options of a scored call (kernels with Math::kScored): s <- cap tanh(s / cap) - slope_h d, hidden where d >= window
+    int32_t scored;
+    float cap, cap_log2;                   // 0 = no cap; 2 log2(e) / cap
+    int32_t window;                        // 0 = no window
+    const float *slopes;                   // [Hq]; null = no distance bias
+    const int32_t *peer_lens[2];           // [B] lengths of a partition that the call does not read; null = empty
 };
 
 // ---------------------------------------------------------------------------------------------

@@ -1,0 +1,35 @@
+// What the library's translation units share on the host: argument checks, device facts, launch accounting, the
+// workspace's head and the tensor-map encoder.  Defined in spd_api.cu; not part of the C ABI.
+#pragma once
+
+#include <cuda.h>
+#include <cuda_runtime.h>
+
+#include "spd.h"
+#include "spd_device.cuh"
+
+namespace spd {
+
+typedef CUresult (*EncodeTiledFn)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *,
+                                  const cuuint64_t *, const cuuint32_t *, const cuuint32_t *, CUtensorMapInterleave,
+                                  CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+
+namespace host {
+
+spd_status check_shape(const spd_shape *s);
+spd_status check_score(const spd_score *score);
+spd_status device_sms(int *sms);               // also makes the current device's context current on the calling thread
+EncodeTiledFn tensor_map_encoder();            // null if the driver has none
+int32_t next_call_id();                        // non-zero id of a call (flags in the workspace hold it)
+void count_launch();
+size_t flags_offset(int batch);                // per-user flags in the workspace
+size_t flags_end(int batch);                   // first byte behind them
+
+inline bool misaligned(const void *p, size_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) != 0; }
+
+}  // namespace host
+
+// Launch of the scored attention kernels (spd_scored.cu): bf16 or fp32, by head_dim and group.
+spd_status launch_attn_scored(const Params &p, const CUtensorMap *maps, int sms, cudaStream_t st, bool pdl, bool bf16, int head_dim);
+
+}  // namespace spd

@@ -33,11 +33,34 @@ constexpr float kLog2e = 1.4426950408889634f;
 #endif
 
 // ------------------------------------------------------------------------------------------------
+// Where a scored call's query stands.  Tokens are numbered through the private and then the public partition, a
+// partition that this call does not read contributing its length (peer_lens); the query is the last token.  Keys at a
+// distance of `window` or more from it are hidden, so a partition's first skip tiles hold nothing visible.
+struct ScoredView {
+    int32_t skip0, skip1;     // tiles in front of the window, private and public
+    int32_t rel0, rel1;       // distance from the query to the first token of the first tile that is streamed
+};
+
+__device__ __forceinline__ bool scored_view(const Params &p, int u, ScoredView &v) {
+    const int64_t a = p.part[0].present ? p.part[0].lens[u] : (p.peer_lens[0] ? p.peer_lens[0][u] : 0);
+    const int64_t b = p.part[1].present ? p.part[1].lens[u] : (p.peer_lens[1] ? p.peer_lens[1][u] : 0);
+    const int64_t total = a + b;
+    const bool ok = a >= 0 && b >= 0 && total <= 0x7fffffff;
+    const int64_t first = (ok && p.window > 0 && total > p.window) ? total - p.window : 0;   // first visible position
+    const int64_t f0 = first < a ? first : a, f1 = first > a ? first - a : 0;
+    v.skip0 = static_cast<int32_t>(first < a ? f0 / kPage : (a + kPage - 1) / kPage);
+    v.skip1 = static_cast<int32_t>(f1 / kPage);
+    v.rel0 = static_cast<int32_t>(total - 1 - static_cast<int64_t>(v.skip0) * kPage);
+    v.rel1 = static_cast<int32_t>(total - 1 - a - static_cast<int64_t>(v.skip1) * kPage);
+    return ok;
+}
+
+// ------------------------------------------------------------------------------------------------
 // Validated page-tile counts of one user (private, public).  A pure function of the call's inputs,
 // so every CTA that evaluates it agrees.  A user whose tables are inconsistent owns no tile and
 // gets zeros; with Flag the user is also flagged for this call (a write to the workspace, so only
 // done once the previous kernel on the stream has finished with it).
-template <bool Flag = false>
+template <bool Flag = false, bool Scored = false>
 __device__ __forceinline__ bool user_tiles(const Params &p, int u, int &n0, int &n1) {
     n0 = n1 = 0;
     bool bad = false;
@@ -55,6 +78,12 @@ __device__ __forceinline__ bool user_tiles(const Params &p, int u, int &n0, int 
             const int n = static_cast<int>((len + kPage - 1) / kPage);
             if (s == 0) n0 = n; else n1 = n;
         }
+    }
+    if constexpr (Scored) {       // only the tiles that hold a key inside the window are streamed
+        ScoredView v;
+        bad = !scored_view(p, u, v) || bad;
+        n0 -= min(n0, v.skip0);
+        n1 -= min(n1, v.skip1);
     }
     if (bad) {
         n0 = n1 = 0;
@@ -108,7 +137,8 @@ __device__ __forceinline__ void finalize_store(const Params &p, int u, int h, fl
 #pragma unroll
         for (int i = 0; i < V; ++i) o[i] = w * o[i] + wi * oi[i];
     }
-    const float inv = (L > 0.f && !bad) ? 1.f / L : 0.f;
+    // a scored call lets NaN among the visible keys through; the plain calls give zeros there
+    const float inv = ((L > 0.f || (p.scored && L != L)) && !bad) ? 1.f / L : 0.f;
     if (p.watch_out && lane == 0) p.watch_out[idx] = wself * lw * inv;   // share of the full softmax mass
 #pragma unroll
     for (int i = 0; i < V; ++i) o[i] = (inv == 0.f) ? 0.f : o[i] * inv;
@@ -308,6 +338,21 @@ __device__ __forceinline__ void piece_ticket(const Params &p, const PieceInfo &p
 }
 
 // ------------------------------------------------------------------------------------------------
+// One score of a scored call, `s` scaled already, `d` >= 0 the distance from the query to the key:
+//   cap tanh(s / cap) - slope d, and -inf outside the window.
+// tanh(x) = 1 - 2 / (e^2x + 1).  The fast form's error is about 2^-23 of the cap (the two special-function steps), far
+// below what the 16-bit inputs carry; fp32 calls use tanhf.
+template <bool Exact>
+__device__ __forceinline__ float scored_value(const Params &p, float s, float slope, int d) {
+    if (p.cap > 0.f) {
+        if constexpr (Exact) s = p.cap * tanhf(s / p.cap);
+        else s = p.cap - __fdividef(2.f * p.cap, ex2_approx(s * p.cap_log2) + 1.f);
+    }
+    s = fmaf(-slope, static_cast<float>(d), s);
+    return (p.window > 0 && d >= p.window) ? -INFINITY : s;
+}
+
+// ------------------------------------------------------------------------------------------------
 // bf16 tile math on the tensor cores (mma.sync m16n8k16, fp32 accumulate).
 //   S  = Q K^T   : M = 16 query-head rows (8 used), N = 8 tokens (x2), K = head_dim
 //   O^T = V^T P^T : M = 16 channels (x D/16), N = 8 query heads, K = 16 tokens
@@ -315,9 +360,12 @@ __device__ __forceinline__ void piece_ticket(const Params &p, const PieceInfo &p
 // fragment that the second product wants for P^T, so P never leaves registers.  P is split into a
 // bf16 head and a bf16 remainder (two MMAs) so that rounding P to 8 bits of mantissa does not show
 // in the output.  K and V tiles sit in shared memory as 128-byte-swizzled [half][16 tokens][64].
-template <int D_>
+// Scored: the scores get the options of a scored call (scored_value) and `watch_base` carries the distance from the query
+// to the tile's first token instead.
+template <int D_, bool Scored_ = false>
 struct MathBF16 {
     static constexpr int D = D_;
+    static constexpr bool kScored = Scored_;
     static constexpr int kTileBytes = kPage * D * 2;
     static constexpr int kBoxes = D / 64;          // TMA boxes per tile (64 bf16 = 128 B wide)
     static constexpr int kBoxBytes = kPage * 128;
@@ -335,6 +383,7 @@ struct MathBF16 {
         float m, l;
         float lw;          // part of l that came from the watched token range
         int wlo, whi;      // watched range of the private partition, [wlo, whi); empty = not watching
+        float slope;       // scored call: distance bias of this thread's head
     };
 
     __device__ static __forceinline__ void begin(State &st, const Params &p, int u, int sq, int lane, uint8_t *) {
@@ -357,8 +406,12 @@ struct MathBF16 {
         st.m = -INFINITY;
         st.l = 0.f;
         st.lw = 0.f;
-        st.wlo = p.watch_out ? p.watch_lo[u] : 0;
-        st.whi = p.watch_out ? p.watch_hi[u] : 0;
+        if constexpr (kScored) {
+            st.slope = p.slopes ? p.slopes[live ? h : 0] : 0.f;
+        } else {
+            st.wlo = p.watch_out ? p.watch_lo[u] : 0;
+            st.whi = p.watch_out ? p.watch_hi[u] : 0;
+        }
     }
 
     // watch_base: index within the private partition of the tile's first token (hugely negative for
@@ -379,6 +432,17 @@ struct MathBF16 {
             fence_proxy_async();
             __syncwarp();
         }
+        if constexpr (kScored) {
+            if (p.window > 0 && watch_base >= p.window) {     // leading rows outside the window: zeroed for the same reason
+                const int lead = min(kPage, watch_base - p.window + 1);
+                for (int i = lane; i < lead * 8 * kBoxes; i += 32) {
+                    const int rr = (i >> 3) % lead, rest = (i >> 3) / lead;
+                    *reinterpret_cast<uint4 *>(Vs + rest * kBoxBytes + rr * 128 + (i & 7) * 16) = make_uint4(0, 0, 0, 0);
+                }
+                fence_proxy_async();
+                __syncwarp();
+            }
+        }
         const uint32_t kbase = smem_u32(Ks), vbase = smem_u32(Vs);
         float s[2][4];
 #pragma unroll
@@ -395,6 +459,13 @@ struct MathBF16 {
         const int tk = 2 * (lane & 3);
         float v0 = s[0][0] * p.sm_scale, v1 = s[0][1] * p.sm_scale;
         float v2 = s[1][0] * p.sm_scale, v3 = s[1][1] * p.sm_scale;
+        if constexpr (kScored) {
+            const int d = watch_base - tk;
+            v0 = scored_value<false>(p, v0, st.slope, d);
+            v1 = scored_value<false>(p, v1, st.slope, d - 1);
+            v2 = scored_value<false>(p, v2, st.slope, d - 8);
+            v3 = scored_value<false>(p, v3, st.slope, d - 9);
+        }
         if (tk >= valid) v0 = -INFINITY;
         if (tk + 1 >= valid) v1 = -INFINITY;
         if (tk + 8 >= valid) v2 = -INFINITY;
@@ -408,7 +479,7 @@ struct MathBF16 {
         const float p2 = ex2_approx((v2 - m_new) * kLog2e), p3 = ex2_approx((v3 - m_new) * kLog2e);
         st.l = st.l * alpha + ((p0 + p1) + (p2 + p3));
         st.m = m_new;
-        if (st.whi > st.wlo) {   // warp-uniform
+        if (!kScored && st.whi > st.wlo) {   // warp-uniform
             const int t0 = watch_base + tk;
             float w = (t0 >= st.wlo && t0 < st.whi) ? p0 : 0.f;
             w += (t0 + 1 >= st.wlo && t0 + 1 < st.whi) ? p1 : 0.f;
@@ -465,6 +536,7 @@ struct MathBF16 {
 template <int D_, int GE_>
 struct MathBF16Simt {
     static constexpr int D = D_, GE = GE_;
+    static constexpr bool kScored = false;
     static constexpr int kTileBytes = kPage * D * 2;
     static constexpr int kBoxes = D / 64;
     static constexpr int kBoxBytes = kPage * 128;
@@ -602,9 +674,10 @@ struct MathBF16Simt {
 //            row of K in float4 steps, starting at a chunk rotated by t so that the 8 lanes of a
 //            shared-memory phase hit 8 different bank groups; halves are added with one shuffle.
 //   P V    : probabilities go through a small shared array; each lane owns D/32 channels of O.
-template <int D_, int GE_>
+template <int D_, int GE_, bool Scored_ = false>
 struct MathF32 {
     static constexpr int D = D_, GE = GE_;
+    static constexpr bool kScored = Scored_;
     static constexpr int kTileBytes = kPage * D * 4;
     static constexpr int kBoxes = 1;
     static constexpr int kBoxBytes = kTileBytes;
@@ -619,6 +692,7 @@ struct MathF32 {
         float o[GE][V];
         float m[GE], l[GE], lw[GE];
         int wlo, whi;
+        float slope[GE];   // scored call: distance bias of each head
     };
 
     __device__ static __forceinline__ void begin(State &st, const Params &p, int u, int sq, int lane, uint8_t *extra) {
@@ -636,9 +710,12 @@ struct MathF32 {
             st.m[hh] = -INFINITY;
             st.l[hh] = 0.f;
             st.lw[hh] = 0.f;
+            if constexpr (kScored) st.slope[hh] = p.slopes ? p.slopes[hbase + hh] : 0.f;
         }
-        st.wlo = p.watch_out ? p.watch_lo[u] : 0;
-        st.whi = p.watch_out ? p.watch_hi[u] : 0;
+        if constexpr (!kScored) {
+            st.wlo = p.watch_out ? p.watch_lo[u] : 0;
+            st.whi = p.watch_out ? p.watch_hi[u] : 0;
+        }
     }
 
     __device__ static __forceinline__ void tile(State &st, const Params &p, uint8_t *Ks, uint8_t *Vs, int valid,
@@ -668,7 +745,8 @@ struct MathF32 {
 #pragma unroll
         for (int hh = 0; hh < GE; ++hh) {
             float v = s[hh] + __shfl_xor_sync(0xffffffffu, s[hh], 16);
-            v = (t < valid) ? v * p.sm_scale : -INFINITY;
+            if constexpr (kScored) v = (t < valid) ? scored_value<true>(p, v * p.sm_scale, st.slope[hh], watch_base - t) : -INFINITY;
+            else v = (t < valid) ? v * p.sm_scale : -INFINITY;
             float tmax = v;
 #pragma unroll
             for (int d = 8; d >= 1; d >>= 1) tmax = fmaxf(tmax, __shfl_xor_sync(0xffffffffu, tmax, d));
@@ -676,7 +754,8 @@ struct MathF32 {
             const float alpha = exp2f((st.m[hh] - m_new) * kLog2e);
             const float pr = exp2f((v - m_new) * kLog2e);
             st.l[hh] = st.l[hh] * alpha + (hf == 0 ? pr : 0.f);
-            st.lw[hh] = st.lw[hh] * alpha + ((hf == 0 && watch_base + t >= st.wlo && watch_base + t < st.whi) ? pr : 0.f);
+            if constexpr (!kScored)
+                st.lw[hh] = st.lw[hh] * alpha + ((hf == 0 && watch_base + t >= st.wlo && watch_base + t < st.whi) ? pr : 0.f);
             st.m[hh] = m_new;
 #pragma unroll
             for (int i = 0; i < V; ++i) st.o[hh][i] *= alpha;
@@ -684,7 +763,9 @@ struct MathF32 {
         }
         __syncwarp();
         const float *vcol = reinterpret_cast<const float *>(Vs) + lane * V;
-        for (int tt = 0; tt < valid; ++tt) {   // rows past `valid` are never touched
+        int lead = 0;                          // rows outside the window are never touched either
+        if constexpr (kScored) lead = (p.window > 0 && watch_base >= p.window) ? min(valid, watch_base - p.window + 1) : 0;
+        for (int tt = lead; tt < valid; ++tt) {   // rows past `valid` are never touched
             float vv[V];
             if constexpr (V == 4) { float4 x = *reinterpret_cast<const float4 *>(vcol + tt * D); vv[0] = x.x; vv[1] = x.y; vv[2] = x.z; vv[3] = x.w; }
             else { float2 x = *reinterpret_cast<const float2 *>(vcol + tt * D); vv[0] = x.x; vv[1] = x.y; }
@@ -754,25 +835,28 @@ struct Cursor {
     int len0, len1;        // token counts of the user
     int idx_cur, idx_next; // this lane's page index of the current / next batch of 32 tiles
     int key;               // (partition << 24 | batch) that idx_cur holds, -1 = nothing
+    int rel0, rel1;        // scored call: distance from the query to the first streamed token of each partition
 };
 
 constexpr int kUserCache = 1024;   // users whose validated tile counts a CTA keeps in shared memory
 
 // Tile counts of user u: from the CTA's cache when it holds them (a launch that loaded its plan has no cache:
 // cache == nullptr), else recomputed from the inputs.
+template <bool Scored = false>
 __device__ __forceinline__ void cached_tiles(const Params &p, const int2 *cache, int u, int &n0, int &n1) {
     if (cache != nullptr && u < kUserCache) {
         const int2 v = cache[u];
         n0 = v.x;
         n1 = v.y;
     } else {
-        user_tiles(p, u, n0, n1);
+        user_tiles<false, Scored>(p, u, n0, n1);
     }
 }
 
+template <bool Scored = false>
 __device__ __forceinline__ void cursor_load_user(Cursor &c, const Params &p, const int2 *cache) {
     int n0, n1;
-    cached_tiles(p, cache, c.u, n0, n1);
+    cached_tiles<Scored>(p, cache, c.u, n0, n1);
     c.npp = n0;
     c.np = n0 + n1;
     c.base0 = p.part[0].present ? p.part[0].indptr[c.u] : 0;
@@ -780,6 +864,12 @@ __device__ __forceinline__ void cursor_load_user(Cursor &c, const Params &p, con
     c.len0 = p.part[0].present ? p.part[0].lens[c.u] : 0;
     c.len1 = p.part[1].present ? p.part[1].lens[c.u] + (p.k_new != nullptr ? 1 : 0) : 0;
     c.key = -1;
+    if constexpr (Scored) {      // tables and lengths as seen from the first tile inside the window
+        ScoredView v;
+        scored_view(p, c.u, v);
+        c.base0 += v.skip0; c.len0 -= v.skip0 * kPage; c.rel0 = v.rel0;
+        c.base1 += v.skip1; c.len1 -= v.skip1 * kPage; c.rel1 = v.rel1;
+    }
 }
 
 __device__ __forceinline__ int cursor_fetch_batch(const Cursor &c, const Params &p, int part, int batch, int lane) {
@@ -815,6 +905,7 @@ __global__ void __launch_bounds__(Math::kWarps * 32, 1)
 attn_kernel(const __grid_constant__ Params p, const __grid_constant__ CUtensorMap mk0,
             const __grid_constant__ CUtensorMap mv0, const __grid_constant__ CUtensorMap mk1,
             const __grid_constant__ CUtensorMap mv1) {
+    constexpr bool SC = Math::kScored;
     constexpr int D = Math::D, NS = Math::kStages, TB = Math::kTileBytes, NT = Math::kWarps * 32;
     static_assert(TB % 1024 == 0, "swizzled tiles need 1024-byte aligned bases");
     static_assert(Math::kExtraBytes % 16 == 0, "per-warp extra area holds float4 data");
@@ -878,7 +969,7 @@ attn_kernel(const __grid_constant__ Params p, const __grid_constant__ CUtensorMa
         const int ub = threadIdx.x * C, ue = min(p.B, ub + C);
         for (int u = ub; u < ue; ++u) {
             int n0, n1;
-            user_tiles(p, u, n0, n1);
+            user_tiles<false, SC>(p, u, n0, n1);
             if (u < kUserCache) sh_np[u] = make_int2(n0, n1);
             sum += n0 + n1;
         }
@@ -1003,7 +1094,7 @@ attn_kernel(const __grid_constant__ Params p, const __grid_constant__ CUtensorMa
         }
         int acc = chunk_pfx[lo], n0 = 0, n1 = 0;
         for (u = lo * C;; ++u) {  // ends inside the chunk, because the chunk holds tile x
-            cached_tiles(p, sh_np, u, n0, n1);
+            cached_tiles<SC>(p, sh_np, u, n0, n1);
             if (acc + n0 + n1 > x) break;
             acc += n0 + n1;
         }
@@ -1078,9 +1169,9 @@ attn_kernel(const __grid_constant__ Params p, const __grid_constant__ CUtensorMa
         if (plan_ok)
         for (int u = gwarp; u < p.B; u += p.num_warps) {
             int n0, n1;
-            cached_tiles(p, np_cache, u, n0, n1);
+            cached_tiles<SC>(p, np_cache, u, n0, n1);
             if (n0 + n1 != 0) continue;
-            const bool bad = user_tiles<true>(p, u, n0, n1);
+            const bool bad = user_tiles<true, SC>(p, u, n0, n1);
             for (int sq = 0; sq < p.S; ++sq) {
                 const int hbase = first_head(p, sq);
                 for (int hh = 0; hh < p.geff; ++hh) {
@@ -1102,7 +1193,7 @@ attn_kernel(const __grid_constant__ Params p, const __grid_constant__ CUtensorMa
     __syncwarp();
 
     const int n2 = tb == t0 ? n : t1 - tb;   // tiles streamed before the jump back to t0
-    cursor_load_user(c, p, np_cache);
+    cursor_load_user<SC>(c, p, np_cache);
     int cur_t = tb;            // index in the tile stream of the next tile to issue
 
     const uint64_t stream_policy = l2_evict_first_policy();
@@ -1113,7 +1204,7 @@ attn_kernel(const __grid_constant__ Params p, const __grid_constant__ CUtensorMa
     auto issue = [&](int stage) {
         if (issued == n2 && n2 < n) {      // the trailing piece is out: back to the share's first tile
             c.u = sh_jump[wid][0]; c.sq = sh_jump[wid][1]; c.j = sh_jump[wid][2];
-            cursor_load_user(c, p, np_cache);
+            cursor_load_user<SC>(c, p, np_cache);
             cur_t = t0;
         }
         // page of tile (c.u, c.sq, c.j)
@@ -1139,7 +1230,7 @@ attn_kernel(const __grid_constant__ Params p, const __grid_constant__ CUtensorMa
         if (lane == 0) {
             descs[3 * stage] = make_int4(valid, (first ? 1 : 0) | (last ? 2 : 0) | (newtok ? 4 : 0) | (kind << 8), c.u, c.sq);
             descs[3 * stage + 1] = make_int4(c.np, c.j, cur_t, c.npp);
-            descs[3 * stage + 2] = make_int4(page, 0, 0, 0);
+            descs[3 * stage + 2] = make_int4(page, SC ? (part ? c.rel1 : c.rel0) - jj * kPage : 0, 0, 0);
             const uint32_t bar = smem_u32(&bars[stage]);
             if (valid == 0) {
                 mbar_arrive(bar);
@@ -1170,7 +1261,7 @@ attn_kernel(const __grid_constant__ Params p, const __grid_constant__ CUtensorMa
                         break;
                     }
                     ++c.u;
-                    cursor_load_user(c, p, np_cache);
+                    cursor_load_user<SC>(c, p, np_cache);
                 } while (c.np == 0);
             } else {
                 c.key = -1;   // same user, page table starts over
@@ -1191,9 +1282,10 @@ attn_kernel(const __grid_constant__ Params p, const __grid_constant__ CUtensorMa
         uint8_t *Ks = ring + static_cast<size_t>(stage) * 2 * TB, *Vs = Ks + TB;
         if (d.y & 1) { Math::begin(st, p, d.z, d.w, lane, extra); seg_bad = false; }
         const int4 e = descs[3 * stage + 1];
-        if ((d.y & 4) && d.x > 0) append_row<Math>(p, Ks, Vs, d.z, d.w, d.x - 1, descs[3 * stage + 2].x, lane);
+        if (!SC && (d.y & 4) && d.x > 0) append_row<Math>(p, Ks, Vs, d.z, d.w, d.x - 1, descs[3 * stage + 2].x, lane);
         if (d.x > 0) {
-            Math::tile(st, p, Ks, Vs, d.x, lane, extra, e.y < e.w ? e.y * kPage : -(1 << 30));
+            Math::tile(st, p, Ks, Vs, d.x, lane, extra,
+                       SC ? descs[3 * stage + 2].y : e.y < e.w ? e.y * kPage : -(1 << 30));
         } else {                                   // a page index outside the pool: flag the user, skip the tile
             seg_bad = true;
             if (lane == 0) { p.bad[d.z] = p.epoch; flag_error(p.hdr, 4 /* SPD_ERR_BAD_PAGE */, d.z); }
@@ -1290,7 +1382,7 @@ struct AppendParams {
     int32_t *hdr;
 };
 
-__global__ void __launch_bounds__(128) append_kernel(AppendParams p) {
+static __global__ void __launch_bounds__(128) append_kernel(AppendParams p) {
     const int u = blockIdx.x;
     __shared__ int64_t dst_row;   // byte offset of (page, kv head 0, slot) in a pool, or -1
     if (threadIdx.x == 0) {

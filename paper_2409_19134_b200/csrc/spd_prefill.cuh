@@ -224,7 +224,7 @@ constexpr size_t prefill_smem_bytes() { return kPfQTile + 4 * static_cast<size_t
 
 constexpr int kPfThreads = 192;   // 4 softmax warps + 2 warps with one issuing thread each
 
-__global__ void __launch_bounds__(kPfThreads, 2)
+static __global__ void __launch_bounds__(kPfThreads, 2)
 prefill_kernel(const __grid_constant__ PrefillParams p, const __grid_constant__ CUtensorMap mq,
                const __grid_constant__ CUtensorMap mk, const __grid_constant__ CUtensorMap mv) {
     extern __shared__ __align__(1024) uint8_t base[];
@@ -487,7 +487,7 @@ struct PromptKvParams {
     int32_t *hdr;
 };
 
-__global__ void __launch_bounds__(128) prompt_kv_kernel(PromptKvParams p) {
+static __global__ void __launch_bounds__(128) prompt_kv_kernel(PromptKvParams p) {
     __shared__ int64_t dst_row;
     const int64_t tok = blockIdx.x;
     if (tok == p.T) {                              // the extra block: users without a prompt hold no tokens

@@ -1,0 +1,160 @@
+// Entry points of the scored calls' own kernels: append with rotation, prompt attention with score options, and the
+// launch of the scored decode kernels.
+#include "spd_host.h"
+#include "spd_launch.cuh"
+#include "spd_prefill_scored.cuh"
+#include "spd_rope.cuh"
+
+namespace spd {
+
+spd_status launch_attn_scored(const Params &p, const CUtensorMap *maps, int sms, cudaStream_t st, bool pdl, bool bf16, int head_dim) {
+    spd_status rc = SPD_ERR_UNSUPPORTED;
+    if (bf16) {
+        rc = head_dim == 128 ? launch_attn<MathBF16<128, true>>(p, maps, sms, st, pdl) : launch_attn<MathBF16<64, true>>(p, maps, sms, st, pdl);
+    } else {
+#define SPD_F32_CASE(DD, GG) if (head_dim == DD && p.geff == GG) rc = launch_attn<MathF32<DD, GG, true>>(p, maps, sms, st, pdl);
+        SPD_F32_CASE(64, 1) SPD_F32_CASE(64, 2) SPD_F32_CASE(64, 4) SPD_F32_CASE(64, 8)
+        SPD_F32_CASE(128, 1) SPD_F32_CASE(128, 2) SPD_F32_CASE(128, 4) SPD_F32_CASE(128, 8)
+#undef SPD_F32_CASE
+    }
+    return rc;
+}
+
+}  // namespace spd
+
+namespace {
+
+using namespace spd;
+using host::misaligned;
+
+int elem_size(const spd_shape &s) { return s.dtype == SPD_BF16 ? 2 : 4; }
+
+// Strides of a token's rows in elements (0 = packed); false if they do not fit the rows or their alignment.
+bool row_stride(const spd_shape &s, int heads, int64_t given, int64_t *stride) {
+    const int64_t row = static_cast<int64_t>(heads) * s.head_dim;
+    *stride = given == 0 ? row : given;
+    return *stride >= row && *stride < (1ll << 31) && *stride * elem_size(s) % 16 == 0;
+}
+
+}  // namespace
+
+extern "C" {
+
+spd_status spd_append_kv_rope(const spd_shape *shape, const spd_rope *rope, int64_t total_tokens, const spd_tokens *tok,
+                              const int32_t *tok_indptr, const int32_t *positions, const int32_t *pos_base, void *q_out,
+                              void *k_out, void *k_pool, void *v_pool, int32_t num_pages, const int32_t *page_indptr,
+                              const int32_t *page_indices, const int32_t *seq_lens, int32_t *new_lens, void *ws,
+                              size_t ws_bytes, void *cuda_stream) {
+    spd_status rc = host::check_shape(shape);
+    if (rc != SPD_OK) return rc;
+    const spd_shape &s = *shape;
+    const int64_t T = total_tokens;
+    if (!tok || !page_indptr || !seq_lens || !ws || misaligned(ws, 256)) return SPD_ERR_INVALID_ARG;
+    if (T < 0 || T >= (1ll << 31) || num_pages < 0 || (!tok_indptr && T != s.batch)) return SPD_ERR_INVALID_ARG;
+    if (ws_bytes < host::flags_end(s.batch)) return SPD_ERR_WORKSPACE;
+    if (T > 0 && (!tok->k || !tok->v || !k_pool || !v_pool || num_pages <= 0)) return SPD_ERR_INVALID_ARG;
+    if (misaligned(tok->k, 16) || misaligned(tok->v, 16) || misaligned(k_pool, 128) || misaligned(v_pool, 128)) return SPD_ERR_INVALID_ARG;
+    RopeAppendParams p{};
+    p.B = s.batch; p.Hkv = s.num_kv_heads; p.D = s.head_dim; p.T = T;
+    int64_t qs = 0, ks, vs;
+    if (!row_stride(s, s.num_kv_heads, tok->k_stride, &ks) || !row_stride(s, s.num_kv_heads, tok->v_stride, &vs)) return SPD_ERR_INVALID_ARG;
+    if (rope) {
+        if (rope->rotary_dim <= 0 || rope->rotary_dim > s.head_dim || rope->rotary_dim % 16 != 0) return SPD_ERR_UNSUPPORTED;
+        if (rope->num_axes < 1 || rope->num_axes > 4) return SPD_ERR_UNSUPPORTED;
+        if (!rope->inv_freq || (rope->interleaved != 0 && rope->interleaved != 1)) return SPD_ERR_INVALID_ARG;
+        if (!(rope->scale >= -3e38f && rope->scale <= 3e38f)) return SPD_ERR_INVALID_ARG;
+        if ((rope->num_axes > 1 && !positions) || (positions && pos_base)) return SPD_ERR_INVALID_ARG;
+        if (T > 0 && (!tok->q || !q_out)) return SPD_ERR_INVALID_ARG;
+        if (misaligned(tok->q, 16) || misaligned(q_out, 16) || misaligned(k_out, 16)) return SPD_ERR_INVALID_ARG;
+        if (!row_stride(s, s.num_q_heads, tok->q_stride, &qs)) return SPD_ERR_INVALID_ARG;
+        // in place only where the output's rows are the input's
+        if (q_out == tok->q && qs != static_cast<int64_t>(s.num_q_heads) * s.head_dim) return SPD_ERR_INVALID_ARG;
+        const int pairs = rope->rotary_dim / 2;
+        int at = 0;
+        for (int a = 0; a < 4; ++a) {
+            if (rope->num_axes > 1 && a < rope->num_axes) {
+                if (rope->sections[a] < 0 || rope->sections[a] > pairs) return SPD_ERR_INVALID_ARG;
+                at += rope->sections[a];
+            }
+            p.axis_end[a] = rope->num_axes > 1 ? at : pairs;
+        }
+        if (rope->num_axes > 1 && at != pairs) return SPD_ERR_INVALID_ARG;
+        p.Hq = s.num_q_heads;
+        p.q = static_cast<const uint8_t *>(tok->q);
+        p.q_out = static_cast<uint8_t *>(q_out);
+        p.rot = rope->rotary_dim; p.interleaved = rope->interleaved; p.scale = rope->scale; p.inv_freq = rope->inv_freq;
+        p.positions = positions; p.pos_base = pos_base;
+    } else if (positions || pos_base || q_out) {
+        return SPD_ERR_INVALID_ARG;            // nothing is rotated: these would be ignored silently
+    }
+    if (k_out && misaligned(k_out, 16)) return SPD_ERR_INVALID_ARG;
+    if (k_out && k_out == tok->k && ks != static_cast<int64_t>(s.num_kv_heads) * s.head_dim) return SPD_ERR_INVALID_ARG;
+    const int es = elem_size(s);
+    p.k = static_cast<const uint8_t *>(tok->k); p.v = static_cast<const uint8_t *>(tok->v);
+    p.q_stride = qs * es; p.k_stride = ks * es; p.v_stride = vs * es;
+    p.k_out = static_cast<uint8_t *>(k_out);
+    p.tok_indptr = tok_indptr;
+    p.k_pool = static_cast<uint8_t *>(k_pool); p.v_pool = static_cast<uint8_t *>(v_pool); p.num_pages = num_pages;
+    p.indptr = page_indptr; p.indices = page_indices; p.lens = seq_lens; p.new_lens = new_lens;
+    p.hdr = static_cast<int32_t *>(ws);
+    p.bad = reinterpret_cast<int32_t *>(static_cast<uint8_t *>(ws) + host::flags_offset(s.batch));
+    p.epoch = host::next_call_id();
+    const int g = s.num_q_heads / s.num_kv_heads;
+    p.S = s.num_kv_heads * (g > kHeadsPerItem ? g / kHeadsPerItem : 1);
+    int sms = 0;
+    if ((rc = host::device_sms(&sms)) != SPD_OK) return rc;
+    cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+    if (!tok_indptr) {
+        if (es == 2) append_rope_kernel<__nv_bfloat16, false><<<s.batch, kRopeThreads, 0, st>>>(p);
+        else append_rope_kernel<float, false><<<s.batch, kRopeThreads, 0, st>>>(p);
+    } else {
+        const unsigned grid = T == 0 ? 1u : static_cast<unsigned>((T + kRopeTokens - 1) / kRopeTokens);
+        if (es == 2) append_rope_kernel<__nv_bfloat16, true><<<grid, kRopeThreads, 0, st>>>(p);
+        else append_rope_kernel<float, true><<<grid, kRopeThreads, 0, st>>>(p);
+    }
+    host::count_launch();
+    return cudaGetLastError() == cudaSuccess ? SPD_OK : SPD_ERR_CUDA;
+}
+
+spd_status spd_prefill_attn_scored(const spd_shape *shape, const spd_score *score, int64_t total_tokens, const spd_tokens *tok,
+                                   const int32_t *tok_indptr, const int32_t *prefix_lens, const int32_t *doc_start, void *out,
+                                   spd_dtype out_dtype, void *ws, size_t ws_bytes, void *cuda_stream) {
+    spd_status rc = host::check_shape(shape);
+    if (rc != SPD_OK) return rc;
+    if ((rc = host::check_score(score)) != SPD_OK) return rc;
+    const spd_shape &s = *shape;
+    const int64_t T = total_tokens;
+    if (!(s.sm_scale > 0.f && s.sm_scale <= 1e30f)) return SPD_ERR_UNSUPPORTED;      // row maxima are taken before scaling
+    if (out_dtype != SPD_F32 && out_dtype != SPD_BF16) return SPD_ERR_UNSUPPORTED;
+    if (T < 0 || T >= (1ll << 31) - 1024) return SPD_ERR_INVALID_ARG;
+    if (!tok || !tok_indptr || !ws || misaligned(ws, 256)) return SPD_ERR_INVALID_ARG;
+    if (ws_bytes < HDR_WORDS * 4) return SPD_ERR_WORKSPACE;
+    if (T > 0 && (!tok->q || !tok->k || !tok->v || !out)) return SPD_ERR_INVALID_ARG;
+    if (misaligned(tok->q, 16) || misaligned(tok->k, 16) || misaligned(tok->v, 16) || misaligned(out, 16)) return SPD_ERR_INVALID_ARG;
+    ScoredPrefillParams p{};
+    if (!row_stride(s, s.num_q_heads, tok->q_stride, &p.q_stride) || !row_stride(s, s.num_kv_heads, tok->k_stride, &p.k_stride) ||
+        !row_stride(s, s.num_kv_heads, tok->v_stride, &p.v_stride))
+        return SPD_ERR_INVALID_ARG;
+    int sms = 0;
+    if ((rc = host::device_sms(&sms)) != SPD_OK) return rc;
+    if (T == 0) return SPD_OK;
+    p.B = s.batch; p.Hq = s.num_q_heads; p.Hkv = s.num_kv_heads; p.T = T;
+    p.sm_scale = s.sm_scale; p.tok_indptr = tok_indptr; p.out = out; p.out_bf16 = out_dtype == SPD_BF16;
+    p.hdr = static_cast<int32_t *>(ws);
+    p.q = tok->q; p.k = tok->k; p.v = tok->v;
+    p.cap = score->logit_cap; p.window = score->window; p.slopes = score->alibi_slopes;
+    p.prefix_lens = prefix_lens; p.doc_start = doc_start;
+    cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+    const int64_t max_blocks = (T + kFmaRows - 1) / kFmaRows + s.batch;
+    if (max_blocks >= (1ll << 31)) return SPD_ERR_UNSUPPORTED;
+    const dim3 grid(static_cast<unsigned>(max_blocks), static_cast<unsigned>(s.num_q_heads));
+    const bool bf = s.dtype == SPD_BF16;
+    if (bf && s.head_dim == 128) prefill_scored_fma_kernel<__nv_bfloat16, 128><<<grid, kFmaRows * 32, 0, st>>>(p);
+    else if (bf) prefill_scored_fma_kernel<__nv_bfloat16, 64><<<grid, kFmaRows * 32, 0, st>>>(p);
+    else if (s.head_dim == 128) prefill_scored_fma_kernel<float, 128><<<grid, kFmaRows * 32, 0, st>>>(p);
+    else prefill_scored_fma_kernel<float, 64><<<grid, kFmaRows * 32, 0, st>>>(p);
+    host::count_launch();
+    return cudaGetLastError() == cudaSuccess ? SPD_OK : SPD_ERR_CUDA;
+}
+
+}  // extern "C"
