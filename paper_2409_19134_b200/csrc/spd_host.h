@@ -27,6 +27,16 @@ size_t flags_end(int batch);                   // first byte behind them
 
 inline bool misaligned(const void *p, size_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) != 0; }
 
+
+inline int elem_size(const spd_shape &s) { return s.dtype == SPD_BF16 ? 2 : 4; }
+
+// Strides of a token's rows in elements (0 = packed); false if they do not fit the rows or their alignment.
+inline bool row_stride(const spd_shape &s, int heads, int64_t given, int64_t *stride) {
+    const int64_t row = static_cast<int64_t>(heads) * s.head_dim;
+    *stride = given == 0 ? row : given;
+    return *stride >= row && *stride < (1ll << 31) && *stride * elem_size(s) % 16 == 0;
+}
+
 }  // namespace host
 
 // Launch of the scored attention kernels (spd_scored.cu): bf16 or fp32, by head_dim and group.

@@ -1,0 +1,124 @@
+// Prompt attention with score options and interval masks: argument checks, tensor maps, choice of the kernel.
+#include <cmath>
+#include <cstdio>
+#include <mutex>
+
+#include "spd_host.h"
+#include "spd_prefill_scored.cuh"
+#include "spd_prefill_scored_tc.cuh"
+
+namespace {
+
+using namespace spd;
+using host::misaligned;
+using host::row_stride;
+
+// [T][heads][head_dim] bf16 with a token stride, as a 3-D tensor map; one box = 128 tokens x 64 channels of one head, 128-byte swizzle.
+spd_status make_token_map(CUtensorMap *map, const void *ptr, int64_t T, int heads, int D, int64_t stride) {
+    EncodeTiledFn fn = host::tensor_map_encoder();
+    if (!fn) return SPD_ERR_CUDA;
+    cuuint64_t dims[3] = {static_cast<cuuint64_t>(D), static_cast<cuuint64_t>(heads), static_cast<cuuint64_t>(T)};
+    cuuint64_t strides[2] = {static_cast<cuuint64_t>(D) * 2, static_cast<cuuint64_t>(stride) * 2};
+    cuuint32_t box[3] = {64, 1, kStKeys};
+    cuuint32_t estr[3] = {1, 1, 1};
+    const CUresult r = fn(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void *>(ptr), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                          CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    if (r != CUDA_SUCCESS) fprintf(stderr, "libspd: cuTensorMapEncodeTiled failed with CUresult %d\n", static_cast<int>(r));
+    return r == CUDA_SUCCESS ? SPD_OK : SPD_ERR_CUDA;
+}
+
+template <int D, bool CAP, bool BIAS>
+spd_status launch_prefill_tc(const ScoredTcParams &p, const CUtensorMap &mq, const CUtensorMap &mk, const CUtensorMap &mv, dim3 grid, cudaStream_t st) {
+    static std::once_flag once[64];
+    int dev = 0;
+    cudaGetDevice(&dev);
+    cudaError_t err = cudaSuccess;
+    std::call_once(once[dev & 63], [&] {
+        err = cudaFuncSetAttribute(prefill_scored_tc_kernel<D, CAP, BIAS>, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(st_smem_bytes(D)));
+    });
+    if (err != cudaSuccess) return SPD_ERR_CUDA;
+    prefill_scored_tc_kernel<D, CAP, BIAS><<<grid, kStThreads, st_smem_bytes(D), st>>>(p, mq, mk, mv);
+    host::count_launch();
+    return cudaGetLastError() == cudaSuccess ? SPD_OK : SPD_ERR_CUDA;
+}
+
+// bf16 prompts on the tensor cores.
+spd_status prefill_tc(const spd_shape &s, const ScoredPrefillParams &sp, cudaStream_t st) {
+    ScoredTcParams p{};
+    p.s = sp;
+    const int g = s.num_q_heads / s.num_kv_heads;
+    p.heads_per_cta = g % 2 == 0 ? 2 : 1;
+    p.c2 = s.sm_scale * kLog2e;
+    p.half_at = p.one_at = -1.f;
+    if (sp.cap > 0.f) {
+        const double y1 = static_cast<double>(s.sm_scale) / sp.cap;
+        p.cap2 = sp.cap * kLog2e;
+        p.y1 = static_cast<float>(fmin(y1, 1e30));
+        bool fits = true;             // coefficients that leave fp32's range: the exact form does it
+        for (int i = 0; i < 6; ++i) {
+            const double c = sp.cap * 1.4426950408889634 * pow(y1, 2 * i + 1);
+            if (i < 4) p.p1[i] = static_cast<float>(c * kTanhHalf[i]);
+            p.p2[i] = static_cast<float>(c * kTanhOne[i]);
+            fits = fits && c > 1e-30 && c < 1e30;
+        }
+        if (fits) { p.half_at = 0.5f; p.one_at = 1.f; }
+    }
+    CUtensorMap mq, mk, mv;
+    spd_status rc;
+    if ((rc = make_token_map(&mq, sp.q, sp.T, s.num_q_heads, s.head_dim, sp.q_stride)) != SPD_OK) return rc;
+    if ((rc = make_token_map(&mk, sp.k, sp.T, s.num_kv_heads, s.head_dim, sp.k_stride)) != SPD_OK) return rc;
+    if ((rc = make_token_map(&mv, sp.v, sp.T, s.num_kv_heads, s.head_dim, sp.v_stride)) != SPD_OK) return rc;
+    const int rows = p.heads_per_cta == 2 ? 128 : 256;
+    const dim3 grid(static_cast<unsigned>((sp.T + rows - 1) / rows + s.batch), static_cast<unsigned>(s.num_q_heads / p.heads_per_cta));
+    const bool cap = sp.cap > 0.f, bias = sp.slopes != nullptr;
+#define SPD_TC_CASE(DD, CC, BB) if (s.head_dim == DD && cap == CC && bias == BB) return launch_prefill_tc<DD, CC, BB>(p, mq, mk, mv, grid, st);
+    SPD_TC_CASE(128, false, false) SPD_TC_CASE(128, true, false) SPD_TC_CASE(128, false, true) SPD_TC_CASE(128, true, true)
+    SPD_TC_CASE(64, false, false) SPD_TC_CASE(64, true, false) SPD_TC_CASE(64, false, true) SPD_TC_CASE(64, true, true)
+#undef SPD_TC_CASE
+    return SPD_ERR_UNSUPPORTED;
+}
+
+}  // namespace
+
+extern "C" {
+
+spd_status spd_prefill_attn_scored(const spd_shape *shape, const spd_score *score, int64_t total_tokens, const spd_tokens *tok,
+                                   const int32_t *tok_indptr, const int32_t *prefix_lens, const int32_t *doc_start, void *out,
+                                   spd_dtype out_dtype, void *ws, size_t ws_bytes, void *cuda_stream) {
+    spd_status rc = host::check_shape(shape);
+    if (rc != SPD_OK) return rc;
+    if ((rc = host::check_score(score)) != SPD_OK) return rc;
+    const spd_shape &s = *shape;
+    const int64_t T = total_tokens;
+    if (!(s.sm_scale > 0.f && s.sm_scale <= 1e30f)) return SPD_ERR_UNSUPPORTED;      // row maxima are taken before scaling
+    if (out_dtype != SPD_F32 && out_dtype != SPD_BF16) return SPD_ERR_UNSUPPORTED;
+    if (T < 0 || T >= (1ll << 31) - 1024) return SPD_ERR_INVALID_ARG;
+    if (!tok || !tok_indptr || !ws || misaligned(ws, 256)) return SPD_ERR_INVALID_ARG;
+    if (ws_bytes < HDR_WORDS * 4) return SPD_ERR_WORKSPACE;
+    if (T > 0 && (!tok->q || !tok->k || !tok->v || !out)) return SPD_ERR_INVALID_ARG;
+    if (misaligned(tok->q, 16) || misaligned(tok->k, 16) || misaligned(tok->v, 16) || misaligned(out, 16)) return SPD_ERR_INVALID_ARG;
+    ScoredPrefillParams p{};
+    if (!row_stride(s, s.num_q_heads, tok->q_stride, &p.q_stride) || !row_stride(s, s.num_kv_heads, tok->k_stride, &p.k_stride) ||
+        !row_stride(s, s.num_kv_heads, tok->v_stride, &p.v_stride))
+        return SPD_ERR_INVALID_ARG;
+    int sms = 0;
+    if ((rc = host::device_sms(&sms)) != SPD_OK) return rc;
+    if (T == 0) return SPD_OK;
+    p.B = s.batch; p.Hq = s.num_q_heads; p.Hkv = s.num_kv_heads; p.T = T;
+    p.sm_scale = s.sm_scale; p.tok_indptr = tok_indptr; p.out = out; p.out_bf16 = out_dtype == SPD_BF16;
+    p.hdr = static_cast<int32_t *>(ws);
+    p.q = tok->q; p.k = tok->k; p.v = tok->v;
+    p.cap = score->logit_cap; p.window = score->window; p.slopes = score->alibi_slopes;
+    p.prefix_lens = prefix_lens; p.doc_start = doc_start;
+    cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+    if (s.dtype == SPD_BF16) return prefill_tc(s, p, st);
+    const int64_t max_blocks = (T + kFmaRows - 1) / kFmaRows + s.batch;
+    if (max_blocks >= (1ll << 31)) return SPD_ERR_UNSUPPORTED;
+    const dim3 grid(static_cast<unsigned>(max_blocks), static_cast<unsigned>(s.num_q_heads));
+    if (s.head_dim == 128) prefill_scored_fma_kernel<float, 128><<<grid, kFmaRows * 32, 0, st>>>(p);
+    else prefill_scored_fma_kernel<float, 64><<<grid, kFmaRows * 32, 0, st>>>(p);
+    host::count_launch();
+    return cudaGetLastError() == cudaSuccess ? SPD_OK : SPD_ERR_CUDA;
+}
+
+}  // extern "C"

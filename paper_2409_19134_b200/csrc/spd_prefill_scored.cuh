@@ -36,7 +36,7 @@ __device__ __forceinline__ void scored_check_offsets(const PrefillParams &p) {
 }
 
 // Keys that row i of a prompt of len tokens sees; lo > hi: none.
-__device__ __forceinline__ void scored_interval(const ScoredPrefillParams &p, int first, int len, int prefix, int i, int &lo, int &hi) {
+__device__ __forceinline__ void scored_interval(const ScoredPrefillParams &p, int first, int prefix, int i, int &lo, int &hi) {
     lo = p.doc_start ? max(0, p.doc_start[first + i]) : 0;
     if (p.window > 0) lo = max(lo, i - p.window + 1);      // window <= 2^31 - 1 and i >= 0: no overflow
     hi = i < prefix ? prefix - 1 : i;
@@ -66,7 +66,7 @@ __global__ void __launch_bounds__(kFmaRows * 32) prefill_scored_fma_kernel(const
     int lo = 1, hi = 0;
     if (live) {
         for (int d = lane; d < D; d += 32) Qs[wid * D + d] = fma_widen<T>(q[(first + row) * p.q_stride + h * D + d]);
-        scored_interval(p, first, len, prefix, row, lo, hi);
+        scored_interval(p, first, prefix, row, lo, hi);
     }
     if (lane == 0) { blo[wid] = lo <= hi ? lo : 0x7fffffff; bhi[wid] = lo <= hi ? hi : -1; }
     __syncthreads();

@@ -1,8 +1,6 @@
-// Entry points of the scored calls' own kernels: append with rotation, prompt attention with score options, and the
-// launch of the scored decode kernels.
+// Append with rotation, and the launch of the scored decode kernels.
 #include "spd_host.h"
 #include "spd_launch.cuh"
-#include "spd_prefill_scored.cuh"
 #include "spd_rope.cuh"
 
 namespace spd {
@@ -25,16 +23,9 @@ spd_status launch_attn_scored(const Params &p, const CUtensorMap *maps, int sms,
 namespace {
 
 using namespace spd;
+using host::elem_size;
 using host::misaligned;
-
-int elem_size(const spd_shape &s) { return s.dtype == SPD_BF16 ? 2 : 4; }
-
-// Strides of a token's rows in elements (0 = packed); false if they do not fit the rows or their alignment.
-bool row_stride(const spd_shape &s, int heads, int64_t given, int64_t *stride) {
-    const int64_t row = static_cast<int64_t>(heads) * s.head_dim;
-    *stride = given == 0 ? row : given;
-    return *stride >= row && *stride < (1ll << 31) && *stride * elem_size(s) % 16 == 0;
-}
+using host::row_stride;
 
 }  // namespace
 
@@ -112,47 +103,6 @@ spd_status spd_append_kv_rope(const spd_shape *shape, const spd_rope *rope, int6
         if (es == 2) append_rope_kernel<__nv_bfloat16, true><<<grid, kRopeThreads, 0, st>>>(p);
         else append_rope_kernel<float, true><<<grid, kRopeThreads, 0, st>>>(p);
     }
-    host::count_launch();
-    return cudaGetLastError() == cudaSuccess ? SPD_OK : SPD_ERR_CUDA;
-}
-
-spd_status spd_prefill_attn_scored(const spd_shape *shape, const spd_score *score, int64_t total_tokens, const spd_tokens *tok,
-                                   const int32_t *tok_indptr, const int32_t *prefix_lens, const int32_t *doc_start, void *out,
-                                   spd_dtype out_dtype, void *ws, size_t ws_bytes, void *cuda_stream) {
-    spd_status rc = host::check_shape(shape);
-    if (rc != SPD_OK) return rc;
-    if ((rc = host::check_score(score)) != SPD_OK) return rc;
-    const spd_shape &s = *shape;
-    const int64_t T = total_tokens;
-    if (!(s.sm_scale > 0.f && s.sm_scale <= 1e30f)) return SPD_ERR_UNSUPPORTED;      // row maxima are taken before scaling
-    if (out_dtype != SPD_F32 && out_dtype != SPD_BF16) return SPD_ERR_UNSUPPORTED;
-    if (T < 0 || T >= (1ll << 31) - 1024) return SPD_ERR_INVALID_ARG;
-    if (!tok || !tok_indptr || !ws || misaligned(ws, 256)) return SPD_ERR_INVALID_ARG;
-    if (ws_bytes < HDR_WORDS * 4) return SPD_ERR_WORKSPACE;
-    if (T > 0 && (!tok->q || !tok->k || !tok->v || !out)) return SPD_ERR_INVALID_ARG;
-    if (misaligned(tok->q, 16) || misaligned(tok->k, 16) || misaligned(tok->v, 16) || misaligned(out, 16)) return SPD_ERR_INVALID_ARG;
-    ScoredPrefillParams p{};
-    if (!row_stride(s, s.num_q_heads, tok->q_stride, &p.q_stride) || !row_stride(s, s.num_kv_heads, tok->k_stride, &p.k_stride) ||
-        !row_stride(s, s.num_kv_heads, tok->v_stride, &p.v_stride))
-        return SPD_ERR_INVALID_ARG;
-    int sms = 0;
-    if ((rc = host::device_sms(&sms)) != SPD_OK) return rc;
-    if (T == 0) return SPD_OK;
-    p.B = s.batch; p.Hq = s.num_q_heads; p.Hkv = s.num_kv_heads; p.T = T;
-    p.sm_scale = s.sm_scale; p.tok_indptr = tok_indptr; p.out = out; p.out_bf16 = out_dtype == SPD_BF16;
-    p.hdr = static_cast<int32_t *>(ws);
-    p.q = tok->q; p.k = tok->k; p.v = tok->v;
-    p.cap = score->logit_cap; p.window = score->window; p.slopes = score->alibi_slopes;
-    p.prefix_lens = prefix_lens; p.doc_start = doc_start;
-    cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
-    const int64_t max_blocks = (T + kFmaRows - 1) / kFmaRows + s.batch;
-    if (max_blocks >= (1ll << 31)) return SPD_ERR_UNSUPPORTED;
-    const dim3 grid(static_cast<unsigned>(max_blocks), static_cast<unsigned>(s.num_q_heads));
-    const bool bf = s.dtype == SPD_BF16;
-    if (bf && s.head_dim == 128) prefill_scored_fma_kernel<__nv_bfloat16, 128><<<grid, kFmaRows * 32, 0, st>>>(p);
-    else if (bf) prefill_scored_fma_kernel<__nv_bfloat16, 64><<<grid, kFmaRows * 32, 0, st>>>(p);
-    else if (s.head_dim == 128) prefill_scored_fma_kernel<float, 128><<<grid, kFmaRows * 32, 0, st>>>(p);
-    else prefill_scored_fma_kernel<float, 64><<<grid, kFmaRows * 32, 0, st>>>(p);
     host::count_launch();
     return cudaGetLastError() == cudaSuccess ? SPD_OK : SPD_ERR_CUDA;
 }
