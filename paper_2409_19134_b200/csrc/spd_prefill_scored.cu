@@ -13,13 +13,13 @@ using namespace spd;
 using host::misaligned;
 using host::row_stride;
 
-// [T][heads][head_dim] bf16 with a token stride, as a 3-D tensor map; one box = 128 tokens x 64 channels of one head, 128-byte swizzle.
-spd_status make_token_map(CUtensorMap *map, const void *ptr, int64_t T, int heads, int D, int64_t stride) {
+// [T][heads][head_dim] bf16 with a token stride, as a 3-D tensor map; one box = `rows` tokens x 64 channels of one head, 128-byte swizzle.
+spd_status make_token_map(CUtensorMap *map, const void *ptr, int64_t T, int heads, int D, int64_t stride, int rows) {
     EncodeTiledFn fn = host::tensor_map_encoder();
     if (!fn) return SPD_ERR_CUDA;
     cuuint64_t dims[3] = {static_cast<cuuint64_t>(D), static_cast<cuuint64_t>(heads), static_cast<cuuint64_t>(T)};
     cuuint64_t strides[2] = {static_cast<cuuint64_t>(D) * 2, static_cast<cuuint64_t>(stride) * 2};
-    cuuint32_t box[3] = {64, 1, kStKeys};
+    cuuint32_t box[3] = {64, 1, static_cast<cuuint32_t>(rows)};
     cuuint32_t estr[3] = {1, 1, 1};
     const CUresult r = fn(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void *>(ptr), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
                           CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
@@ -65,9 +65,9 @@ spd_status prefill_tc(const spd_shape &s, const ScoredPrefillParams &sp, cudaStr
     }
     CUtensorMap mq, mk, mv;
     spd_status rc;
-    if ((rc = make_token_map(&mq, sp.q, sp.T, s.num_q_heads, s.head_dim, sp.q_stride)) != SPD_OK) return rc;
-    if ((rc = make_token_map(&mk, sp.k, sp.T, s.num_kv_heads, s.head_dim, sp.k_stride)) != SPD_OK) return rc;
-    if ((rc = make_token_map(&mv, sp.v, sp.T, s.num_kv_heads, s.head_dim, sp.v_stride)) != SPD_OK) return rc;
+    if ((rc = make_token_map(&mq, sp.q, sp.T, s.num_q_heads, s.head_dim, sp.q_stride, 128)) != SPD_OK) return rc;
+    if ((rc = make_token_map(&mk, sp.k, sp.T, s.num_kv_heads, s.head_dim, sp.k_stride, kStKeys)) != SPD_OK) return rc;
+    if ((rc = make_token_map(&mv, sp.v, sp.T, s.num_kv_heads, s.head_dim, sp.v_stride, kStKeys)) != SPD_OK) return rc;
     const int rows = p.heads_per_cta == 2 ? 128 : 256;
     const dim3 grid(static_cast<unsigned>((sp.T + rows - 1) / rows + s.batch), static_cast<unsigned>(s.num_q_heads / p.heads_per_cta));
     const bool cap = sp.cap > 0.f, bias = sp.slopes != nullptr;
