@@ -28,7 +28,7 @@ spd_status make_token_map(CUtensorMap *map, const void *ptr, int64_t T, int head
 }
 
 template <int D, bool CAP, bool BIAS>
-spd_status launch_prefill_tc(const ScoredTcParams &p, const CUtensorMap &mq, const CUtensorMap &mk, const CUtensorMap &mv, dim3 grid, cudaStream_t st) {
+spd_status launch_prefill_tc(const ScoredTcParams &p, const CUtensorMap &mq, const CUtensorMap &mk, const CUtensorMap &mv, unsigned grid, cudaStream_t st) {
     static std::once_flag once[64];
     int dev = 0;
     cudaGetDevice(&dev);
@@ -69,7 +69,11 @@ spd_status prefill_tc(const spd_shape &s, const ScoredPrefillParams &sp, cudaStr
     if ((rc = make_token_map(&mk, sp.k, sp.T, s.num_kv_heads, s.head_dim, sp.k_stride, kStKeys)) != SPD_OK) return rc;
     if ((rc = make_token_map(&mv, sp.v, sp.T, s.num_kv_heads, s.head_dim, sp.v_stride, kStKeys)) != SPD_OK) return rc;
     const int rows = p.heads_per_cta == 2 ? 128 : 256;
-    const dim3 grid(static_cast<unsigned>((sp.T + rows - 1) / rows + s.batch), static_cast<unsigned>(s.num_q_heads / p.heads_per_cta));
+    // at most one CTA per SM; fewer where there are not that many items
+    const int64_t items = ((sp.T + rows - 1) / rows + s.batch) * (s.num_q_heads / p.heads_per_cta);
+    int sms = 0;
+    if ((rc = host::device_sms(&sms)) != SPD_OK) return rc;
+    const unsigned grid = static_cast<unsigned>(items < sms ? items : sms);
     const bool cap = sp.cap > 0.f, bias = sp.slopes != nullptr;
 #define SPD_TC_CASE(DD, CC, BB) if (s.head_dim == DD && cap == CC && bias == BB) return launch_prefill_tc<DD, CC, BB>(p, mq, mk, mv, grid, st);
     SPD_TC_CASE(128, false, false) SPD_TC_CASE(128, true, false) SPD_TC_CASE(128, false, true) SPD_TC_CASE(128, true, true)
