@@ -1,6 +1,7 @@
 // Prompt attention with score options and interval masks: argument checks, tensor maps, choice of the kernel.
 #include <cmath>
 #include <cstdio>
+#include <cstring>
 #include <mutex>
 
 #include "spd_host.h"
@@ -27,7 +28,7 @@ spd_status make_token_map(CUtensorMap *map, const void *ptr, int64_t T, int head
     return r == CUDA_SUCCESS ? SPD_OK : SPD_ERR_CUDA;
 }
 
-template <int D, bool CAP, bool BIAS>
+template <int D, int CAP, bool BIAS>
 spd_status launch_prefill_tc(const ScoredTcParams &p, const CUtensorMap &mq, const CUtensorMap &mk, const CUtensorMap &mv, unsigned grid, cudaStream_t st) {
     static std::once_flag once[64];
     int dev = 0;
@@ -40,6 +41,13 @@ spd_status launch_prefill_tc(const ScoredTcParams &p, const CUtensorMap &mq, con
     prefill_scored_tc_kernel<D, CAP, BIAS><<<grid, kStThreads, st_smem_bytes(D), st>>>(p, mq, mk, mv);
     host::count_launch();
     return cudaGetLastError() == cudaSuccess ? SPD_OK : SPD_ERR_CUDA;
+}
+
+uint64_t twice(double x) {              // an fp32 value in both halves of a two-lane operand
+    const float f = static_cast<float>(x);
+    uint32_t u;
+    memcpy(&u, &f, 4);
+    return (static_cast<uint64_t>(u) << 32) | u;
 }
 
 // bf16 prompts on the tensor cores.
@@ -57,8 +65,8 @@ spd_status prefill_tc(const spd_shape &s, const ScoredPrefillParams &sp, cudaStr
         bool fits = true;             // coefficients that leave fp32's range: the exact form does it
         for (int i = 0; i < 6; ++i) {
             const double c = sp.cap * 1.4426950408889634 * pow(y1, 2 * i + 1);
-            if (i < 4) p.p1[i] = static_cast<float>(c * kTanhHalf[i]);
-            p.p2[i] = static_cast<float>(c * kTanhOne[i]);
+            if (i < 4) p.p1[i] = twice(c * kTanhHalf[i]);
+            p.p2[i] = twice(c * kTanhOne[i]);
             fits = fits && c > 1e-30 && c < 1e30;
         }
         if (fits) { p.half_at = 0.5f; p.one_at = 1.f; }
@@ -74,10 +82,11 @@ spd_status prefill_tc(const spd_shape &s, const ScoredPrefillParams &sp, cudaStr
     int sms = 0;
     if ((rc = host::device_sms(&sms)) != SPD_OK) return rc;
     const unsigned grid = static_cast<unsigned>(items < sms ? items : sms);
-    const bool cap = sp.cap > 0.f, bias = sp.slopes != nullptr;
+    const bool bias = sp.slopes != nullptr;
+    const int cap = sp.cap == 0.f ? 0 : (sp.cap <= kStFixedCap && !bias) ? 1 : 2;
 #define SPD_TC_CASE(DD, CC, BB) if (s.head_dim == DD && cap == CC && bias == BB) return launch_prefill_tc<DD, CC, BB>(p, mq, mk, mv, grid, st);
-    SPD_TC_CASE(128, false, false) SPD_TC_CASE(128, true, false) SPD_TC_CASE(128, false, true) SPD_TC_CASE(128, true, true)
-    SPD_TC_CASE(64, false, false) SPD_TC_CASE(64, true, false) SPD_TC_CASE(64, false, true) SPD_TC_CASE(64, true, true)
+    SPD_TC_CASE(128, 0, false) SPD_TC_CASE(128, 1, false) SPD_TC_CASE(128, 2, false) SPD_TC_CASE(128, 0, true) SPD_TC_CASE(128, 2, true)
+    SPD_TC_CASE(64, 0, false) SPD_TC_CASE(64, 1, false) SPD_TC_CASE(64, 2, false) SPD_TC_CASE(64, 0, true) SPD_TC_CASE(64, 2, true)
 #undef SPD_TC_CASE
     return SPD_ERR_UNSUPPORTED;
 }

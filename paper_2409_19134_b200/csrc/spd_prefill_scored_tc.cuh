@@ -30,9 +30,10 @@
 namespace spd {
 
 constexpr int kStKeys = 80;                         // keys per block
-constexpr int kStThreads = 416;                     // 8 softmax warps, 2 issuing, 1 loading, 1 guarding, 1 planning
+constexpr int kStThreads = 512;                     // 8 softmax warps, 2 issuing, 1 loading, 1 guarding, 1 planning, 3 with nothing to do
 constexpr int kStConsumers = 12;                    // warps that read a plan
 constexpr int kStTmemCols = 512;
+constexpr float kStFixedCap = 64.f;                 // caps up to here: weights relative to 0 (64 log2(e) = 92.3)
 constexpr int kStS0 = 0, kStS1 = 96;                  // S of each tile (fp32, 80 columns)
 constexpr int kStP0 = 176, kStP1 = 216;              // P (bf16 pairs, 40 columns)
 constexpr int kStO0 = 256, kStO1 = 384;              // O (fp32, D columns)
@@ -48,8 +49,8 @@ struct StPlan {
     int32_t valid;                  // 0: the list is done
     int32_t first, len, row0, h0;   // prompt (first token, tokens), first row of the item, first head
     int32_t tiles;                  // tiles with rows of the prompt
-    int32_t key0, nb;               // first key, blocks
-    int32_t ja[2], jb[2];           // blocks that a tile works on, [ja, jb)
+    int32_t kend, nb;               // first key of the last block, blocks; they are worked through from the last to the first
+    int32_t ja[2], jb[2];           // blocks that a tile works on, [ja, jb) in that order
     int32_t fulllo, fullhi;         // keys that every row sees
     int32_t poisoned;               // a V row that is not finite is hidden from some rows and visible to others
     int32_t pad;
@@ -59,7 +60,7 @@ struct StPlan {
 constexpr int kStBarBytes = 320;
 constexpr int kStStage = 4096;      // bytes per softmax warp for its way out: 32 rows x 32 fp32
 constexpr size_t st_smem_bytes(int D) {
-    return 2 * static_cast<size_t>(st_qtile(D)) + 2 * st_slots(D) * static_cast<size_t>(st_tile(D)) + 8 * kStStage + kStBarBytes + 2 * sizeof(StPlan);
+    return 2 * static_cast<size_t>(st_qtile(D)) + 2 * st_slots(D) * static_cast<size_t>(st_tile(D)) + 8 * kStStage + kStBarBytes + 2 * sizeof(StPlan) + 2 * kStKeys * 4;
 }
 
 struct ScoredTcParams {
@@ -69,7 +70,7 @@ struct ScoredTcParams {
     float cap2;                 // cap log2(e)
     float y1;                   // sm_scale / cap: what is inside the tanh per unit of q.k
     float half_at, one_at;      // where the two polynomials below end (1/2 and 1; -1 = not to be used)
-    float p1[4], p2[6];         // cap2 tanh(y1 x) = x P(x^2): coefficients for |y1 x| <= 1/2 and <= 1
+    uint64_t p1[4], p2[6];      // cap2 tanh(y1 x) = x P(x^2): coefficients for |y1 x| <= 1/2 and <= 1, each in both halves
 };
 
 // tanh(y) = y P(y^2) by minimax polynomials (exchange algorithm, absolute error): 1.3e-7 for |y| <= 1/2, 2.4e-7 for |y| <= 1.
@@ -183,7 +184,8 @@ __device__ __noinline__ void st_slow_row(const ScoredTcParams &p, int64_t first,
     }
 }
 
-template <int D, bool CAP, bool BIAS>
+// CAP: 0 = scores are not capped; 1 = capped, with a cap that lets every weight be taken relative to 0; 2 = any cap.
+template <int D, int CAP, bool BIAS>
 __global__ void __launch_bounds__(kStThreads, 1)
 prefill_scored_tc_kernel(const __grid_constant__ ScoredTcParams p, const __grid_constant__ CUtensorMap mq,
                          const __grid_constant__ CUtensorMap mk, const __grid_constant__ CUtensorMap mv) {
@@ -202,6 +204,7 @@ prefill_scored_tc_kernel(const __grid_constant__ ScoredTcParams p, const __grid_
     static_assert(NBARS * 8 + 4 <= kStBarBytes, "barrier block");
     uint32_t &tmem_slot = *reinterpret_cast<uint32_t *>(bars + NBARS);
     StPlan *plans = reinterpret_cast<StPlan *>(stage_all + 8 * kStStage + kStBarBytes);
+    uint8_t *bias_all = reinterpret_cast<uint8_t *>(plans + 2);      // [tile][key of a block]
     const int tid = threadIdx.x, wid = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31;
     const int hpc = p.heads_per_cta, hgroups = p.s.Hq / hpc, gq = p.s.Hq / p.s.Hkv;
     const int rows_item = hpc == 2 ? 128 : 256;
@@ -235,236 +238,9 @@ prefill_scored_tc_kernel(const __grid_constant__ ScoredTcParams p, const __grid_
     auto plan_of = [&](int r) -> StPlan & { wait(&bar_plan[r & 1], r >> 1); __syncwarp(); return plans[r & 1]; };
     auto plan_done = [&](int r) { __syncwarp(); if (lane == 0) mbar_arrive(smem_u32(&bar_planfree[r & 1])); };
 
-    if (wid == 12) {
-        // ---------------- the planning warp
-        // lane l sums the item rows of users [l C, (l + 1) C); users from the first inconsistent one on are left out
-        const int C = (p.s.B + 31) / 32, u0 = lane * C, u1 = min(p.s.B, u0 + C);
-        int sum = 0;
-        bool bad = false;
-#pragma unroll 4
-        for (int u = u0; u < u1; ++u) {
-            const int64_t a = p.s.tok_indptr[u], b = p.s.tok_indptr[u + 1];
-            bad = bad || a < 0 || b < a || b > p.s.T;
-            if (!bad) sum += static_cast<int>((b - a + rows_item - 1) / rows_item);
-        }
-        int inc = sum;
-#pragma unroll
-        for (int d = 1; d < 32; d <<= 1) {
-            const int up = __shfl_up_sync(0xffffffffu, inc, d);
-            if (lane >= d) inc += up;
-        }
-        const unsigned badmask = __ballot_sync(0xffffffffu, bad);
-        const int blocks = __shfl_sync(0xffffffffu, inc, badmask ? __ffs(badmask) - 1 : 31);
-        const int64_t items = static_cast<int64_t>(blocks) * hgroups;
-        for (int r = 0;; ++r) {
-            // dealt out to and fro, so that nobody gets the heaviest of every round
-            const int64_t item = static_cast<int64_t>(r) * gridDim.x + ((r & 1) ? gridDim.x - 1 - blockIdx.x : blockIdx.x);
-            StPlan &pl = plans[r & 1];
-            if (r >= 2) wait(&bar_planfree[r & 1], (r >> 1) - 1);
-            __syncwarp();
-            const bool valid = ok && static_cast<int64_t>(r) * gridDim.x < items;      // a round may have nothing for this CTA: an empty item
-            if (!valid) {
-                if (lane == 0) { pl.valid = 0; mbar_arrive(smem_u32(&bar_plan[r & 1])); }
-                break;
-            }
-            const bool some = item < items;
-            const int blk = some ? static_cast<int>(item / hgroups) : 0, h0 = some ? static_cast<int>(item % hgroups) * hpc : 0;
-            int user = 0, qb = 0, first = 0, len = 0;
-            if (some) {                   // the user whose rows hold block blk; a prompt's blocks count from its end
-                const int src = __ffs(__ballot_sync(0xffffffffu, blk < inc)) - 1;
-                if (lane == src) {
-                    int rem = blk - (inc - sum);
-                    for (user = u0; user < u1; ++user) {
-                        first = p.s.tok_indptr[user];
-                        len = p.s.tok_indptr[user + 1] - first;
-                        const int nb = (len + rows_item - 1) / rows_item;
-                        if (rem < nb) { qb = nb - 1 - rem; break; }
-                        rem -= nb;
-                    }
-                }
-                user = __shfl_sync(0xffffffffu, user, src);
-                qb = __shfl_sync(0xffffffffu, qb, src);
-                first = __shfl_sync(0xffffffffu, first, src);
-                len = __shfl_sync(0xffffffffu, len, src);
-            }
-            const int row0 = qb * rows_item;
-            const int prefix = some && p.s.prefix_lens ? min(len, p.s.prefix_lens[user]) : 0;
-            int tlo[2] = {0x7fffffff, 0x7fffffff}, thi[2] = {-1, -1}, fulllo = -1, fullhi = 0x7fffffff;
-#pragma unroll
-            for (int w = 0; w < 8; ++w) {           // the 32 rows of softmax warp w; two heads have the same rows
-                const int qrow = row0 + (hpc == 2 ? 32 * (w & 3) : 32 * w) + lane;
-                int lo = 0x7fffffff, hi = -1;
-                const bool live = some && qrow < len;
-                if (live) scored_interval(p.s, first, prefix, qrow, lo, hi);
-                const bool sees = lo <= hi;
-                if (!sees) { lo = 0x7fffffff; hi = -1; }
-                pl.span[32 * w + lane] = make_int2(lo, hi);
-                // a live row that sees nothing makes every block one with hidden keys
-                const int a = __reduce_min_sync(0xffffffffu, lo), b = __reduce_max_sync(0xffffffffu, hi);
-                const int c = __reduce_max_sync(0xffffffffu, sees ? lo : (live ? 0x7fffffff : -1));
-                const int d = __reduce_min_sync(0xffffffffu, sees ? hi : (live ? -1 : 0x7fffffff));
-                if (lane == 0) pl.stats[w] = StBlockStats{a, b, c, d};
-                tlo[w >> 2] = min(tlo[w >> 2], a); thi[w >> 2] = max(thi[w >> 2], b);
-                fulllo = max(fulllo, c); fullhi = min(fullhi, d);
-            }
-            if (lane == 0) {
-                const int key0 = min(tlo[0], tlo[1]), key1 = max(thi[0], thi[1]);
-                pl.valid = 1; pl.first = first; pl.len = len; pl.row0 = row0; pl.h0 = h0;
-                pl.tiles = !some ? 0 : (hpc == 2 || row0 + 128 < len) ? 2 : 1;
-                pl.key0 = key0; pl.nb = key1 < 0 ? 0 : (key1 - key0) / KB + 1;
-#pragma unroll
-                for (int x = 0; x < 2; ++x) {
-                    pl.ja[x] = thi[x] < 0 ? 0 : (tlo[x] - key0) / KB;
-                    pl.jb[x] = thi[x] < 0 ? 0 : (thi[x] - key0) / KB + 1;
-                }
-                pl.fulllo = fulllo; pl.fullhi = fullhi; pl.poisoned = 0;
-            }
-            __syncwarp();
-            if (lane == 0) mbar_arrive(smem_u32(&bar_plan[r & 1]));
-        }
-    } else if (wid == 10) {
-        // ---------------- the loading warp (one thread of it); c counts blocks over all items
-        int c = 0, nq = 0;
-        for (int r = 0; ok; ++r) {
-            const StPlan &pl = plan_of(r);
-            if (!ok || !pl.valid) break;
-            const int NB = pl.nb, kvh = pl.h0 / gq, y0 = pl.first + pl.key0;
-            if (lane == 0 && NB > 0) {
-                if (nq > 0) wait1(bar_qfree, nq - 1);
-                if (ok) {
-                    mbar_expect_tx(smem_u32(bar_q), pl.tiles * QTILE);
-                    for (int t = 0; t < pl.tiles; ++t)
-                        for (int x = 0; x < BOXES; ++x)
-                            tma_load_3d(Qs + t * QTILE + x * kStQBox, &mq, 64 * x, hpc == 2 ? pl.h0 + t : pl.h0, pl.first + pl.row0 + (hpc == 2 ? 0 : 128 * t), smem_u32(bar_q));
-                }
-                for (int j = 0; j < NB && ok; ++j, ++c) {
-                    const int slot = c % NS, use = c / NS, y = y0 + j * KB;
-                    if (use > 0) wait1(&bar_kfree[slot], use - 1);
-                    if (!ok) break;
-                    mbar_expect_tx(smem_u32(&bar_k[slot]), TILE);
-                    for (int x = 0; x < BOXES; ++x) tma_load_3d(Ks + slot * TILE + x * kStBox, &mk, 64 * x, kvh, y, smem_u32(&bar_k[slot]));
-                    if (use > 0) wait1(&bar_vfree[slot], use - 1);
-                    if (!ok) break;
-                    mbar_expect_tx(smem_u32(&bar_v[slot]), TILE);
-                    for (int x = 0; x < BOXES; ++x) tma_load_3d(Vs + slot * TILE + x * kStBox, &mv, 64 * x, kvh, y, smem_u32(&bar_v[slot]));
-                }
-            }
-            if (NB > 0) ++nq;
-            ok = __shfl_sync(0xffffffffu, ok, 0);
-            plan_done(r);
-        }
-        if (lane == 0 && !ok) {              // leave nothing in flight behind: a bounded chance for what was asked for last
-            if (nq > 0) mbar_wait(smem_u32(bar_q), (nq - 1) & 1);
-            for (int x = 0; x < NS; ++x) {
-                const int uses = (c - x + NS) / NS;          // blocks that went to slot x, the one that was cut off included
-                if (c >= x && uses > 0) { mbar_wait(smem_u32(&bar_k[x]), (uses - 1) & 1); mbar_wait(smem_u32(&bar_v[x]), (uses - 1) & 1); }
-            }
-        }
-    } else if (wid == 11) {
-        // ---------------- the guard: V rows of blocks with hidden keys
-        int c = 0;
-        for (int r = 0; ok; ++r) {
-            StPlan &pl = plan_of(r);
-            if (!ok || !pl.valid) break;
-            const int NB = pl.nb;
-            for (int j = 0; j < NB && ok; ++j, ++c) {
-                // every block passes through here, so that the guard is never a whole ring ahead of or behind the others
-                const int slot = c % NS, kb = pl.key0 + j * KB;
-                wait(&bar_v[slot], c / NS);
-                __syncwarp();
-                if (pl.fulllo <= kb && kb + KB - 1 <= pl.fullhi) {
-                    if (lane == 0) mbar_arrive(smem_u32(&bar_guard[slot]));
-                    continue;
-                }
-                uint8_t *vt = base + 2 * QTILE + (NS + slot) * TILE;
-                auto odd = [](const uint4 &w) {           // a 16-bit half with all exponent bits set carries into its sign bit
-                    return ((w.x & 0x7f807f80u) + 0x00800080u) | ((w.y & 0x7f807f80u) + 0x00800080u) | ((w.z & 0x7f807f80u) + 0x00800080u) |
-                           ((w.w & 0x7f807f80u) + 0x00800080u);
-                };
-                uint32_t any = 0;
-#pragma unroll 5
-                for (int x = lane; x < TILE / 16; x += 32) any |= odd(*reinterpret_cast<const uint4 *>(vt + x * 16));
-                if (__any_sync(0xffffffffu, (any & 0x80008000u) != 0)) {
-                    for (int row = 0; row < KB; ++row) {        // rare: row by row
-                        uint4 *chunk = reinterpret_cast<uint4 *>(vt + (lane >> 3) * kStBox + row * 128 + (lane & 7) * 16);
-                        const bool mine = lane < 8 * BOXES;
-                        if (!__any_sync(0xffffffffu, mine && (odd(*(mine ? chunk : reinterpret_cast<uint4 *>(vt + row * 128))) & 0x80008000u) != 0)) continue;
-                        const int key = kb + row;
-                        bool seen = false, hidden = false;
-                        for (int x = lane; x < 256; x += 32) {
-                            const int2 sp = pl.span[x];
-                            const bool s = sp.x <= key && key <= sp.y;
-                            seen = seen || s;
-                            hidden = hidden || !s;
-                        }
-                        if (!__any_sync(0xffffffffu, seen)) {
-                            if (mine) *chunk = make_uint4(0, 0, 0, 0);
-                        } else if (__any_sync(0xffffffffu, hidden)) {
-                            pl.poisoned = 1;
-                        }
-                    }
-                    fence_proxy_async();
-                    __syncwarp();
-                }
-                if (lane == 0) mbar_arrive(smem_u32(&bar_guard[slot]));
-            }
-            plan_done(r);
-        }
-    } else if (wid >= 8) {
-        // ---------------- the warp that issues tile x's MMAs: S of block j, then P V of block j - 1; n counts the tile's blocks
-        const int x = wid - 8;
-        const uint32_t ts = tmem + (x ? kStS1 : kStS0), tp = tmem + (x ? kStP1 : kStP0), to = tmem + (x ? kStO1 : kStO0);
-        int c = 0, n = 0, nq = 0;
-        for (int r = 0; ok; ++r) {
-            const StPlan &pl = plan_of(r);
-            if (!ok || !pl.valid) break;
-            const int NB = pl.nb, a = x ? pl.ja[1] : pl.ja[0], b = x ? pl.jb[1] : pl.jb[0];
-            if (NB > 0) wait(bar_q, nq++);
-            for (int j = 0; j <= NB && NB > 0 && ok; ++j) {
-                if (j < NB) {
-                    const int slot = (c + j) % NS;
-                    // a tile that has no use for a block gives it back all the same, once it is there: never a ring ahead
-                    wait(&bar_k[slot], (c + j) / NS);
-                    if (a <= j && j < b) {
-                        const int k = n + j - a;
-                        if (k > 0) wait(&bar_sf[x], k - 1);
-                        __syncwarp();
-                        tc_fence_after();
-#pragma unroll
-                        for (int kk = 0; kk < D / 16; ++kk)       // 16 channels per MMA
-                            st_mma_ss(ts, umma_desc(Qs + x * QTILE + (kk >> 2) * kStQBox + (kk & 3) * 32, 16, 1024),
-                                      umma_desc(Ks + slot * TILE + (kk >> 2) * kStBox + (kk & 3) * 32, 16, 1024), umma_idesc(false, KB), kk > 0 ? 1u : 0u);
-                        st_commit(smem_u32(&bar_s[x]));
-                        st_commit(smem_u32(&bar_kfree[slot]));
-                    } else if (lane == 0) {
-                        mbar_arrive(smem_u32(&bar_kfree[slot]));
-                    }
-                    if (j == NB - 1) st_commit(smem_u32(bar_qfree));      // behind the item's last use of Q (at once where nothing is under way)
-                }
-                if (j > 0) {
-                    const int jj = j - 1, slot = (c + jj) % NS;
-                    wait(&bar_v[slot], (c + jj) / NS);
-                    wait(&bar_guard[slot], (c + jj) / NS);
-                    if (a <= jj && jj < b) {
-                        const int i = jj - a;
-                        wait(&bar_p[x], n + i);           // also: this tile's softmax has read the O of the item before
-                        __syncwarp();
-                        tc_fence_after();
-#pragma unroll
-                        for (int kk = 0; kk < KB / 16; ++kk)      // 16 keys per MMA: 8 columns of P, 2 KB of each 64-channel box of V
-                            st_mma_ts(to, tp + kk * 8, umma_desc(Vs + slot * TILE + kk * 2048, kStBox, 1024), umma_idesc(true, D), (i > 0 || kk > 0) ? 1u : 0u);
-                        st_commit(smem_u32(&bar_o[x]));
-                        st_commit(smem_u32(&bar_vfree[slot]));
-                    } else if (lane == 0) {
-                        mbar_arrive(smem_u32(&bar_vfree[slot]));
-                    }
-                }
-            }
-            c += NB;
-            n += b - a;
-            plan_done(r);
-        }
-    } else {
+    // the launch's 512 x 128 registers, shared out by warpgroup: 256 x 192 + 256 x 64 = 65536
+    if (wid < 8) {
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 192;");
         // ---------------- softmax warps: one query row per thread; n counts the tile's blocks
         const int t = wid >> 2, row = tid & 127;
         const uint32_t lanes = static_cast<uint32_t>((wid & 3) * 32) << 16;
@@ -476,15 +252,26 @@ prefill_scored_tc_kernel(const __grid_constant__ ScoredTcParams p, const __grid_
             if (!ok || !pl.valid) break;
             const StBlockStats w = pl.stats[wid];
             const int2 sp = pl.span[tid];
-            const int lo = sp.x, hi = sp.y, key0 = pl.key0, my_a = t ? pl.ja[1] : pl.ja[0], my_b = t ? pl.jb[1] : pl.jb[0];
+            const int lo = sp.x, hi = sp.y, kend = pl.kend, my_a = t ? pl.ja[1] : pl.ja[0], my_b = t ? pl.jb[1] : pl.jb[0];
             const int h = hpc == 2 ? pl.h0 + t : pl.h0, len = pl.len, trow0 = pl.row0 + (hpc == 2 ? 0 : 128 * t), qrow = trow0 + row;
             const int64_t first = pl.first;
             const bool have = t < pl.tiles;
             float l = 0.f, m = -INFINITY;                  // m: reference point in log2 units of the score
+            int form = 1;                                  // the cap's form that would have served the block before
+            // The bias without the row's own constant: with the scores of a block taken relative to -slope (row - kb), kb its first
+            // key, a key x places in counts slope x for every row, a table per head; the reference m moves into the next
+            // block's frame by a constant.
             float slope2 = 0.f;
-            if constexpr (BIAS) slope2 = p.s.slopes[h] * kLog2e;
+            float *bias = reinterpret_cast<float *>(bias_all) + t * KB;
+            if constexpr (BIAS) {
+                slope2 = p.s.slopes[h] * kLog2e;
+                asm volatile("bar.sync %0, 128;" ::"r"(1 + t) : "memory");      // the tile's warps are done with the item before
+                if (row < KB) bias[row] = slope2 * static_cast<float>(row);
+                asm volatile("bar.sync %0, 128;" ::"r"(1 + t) : "memory");
+            }
             for (int j = my_a; j < my_b && ok; ++j) {
-                const int i = j - my_a, kb = key0 + j * KB;
+                const int i = j - my_a, kb = kend - j * KB;
+                if constexpr (BIAS) m = i > 0 ? m + slope2 * static_cast<float>(KB) : m;
                 wait(&bar_s[t], n + i);
                 __syncwarp();
                 tc_fence_after();
@@ -523,157 +310,131 @@ prefill_scored_tc_kernel(const __grid_constant__ ScoredTcParams p, const __grid_
                     }
                 }
                 auto seen = [&](int x) { return (see[x >> 5] >> (x & 31)) & 1u; };
-                // ---- score options.  Afterwards sv holds the score in log2 units (BIAS), or still q.k with the cap (CAP) or the
-                // scale applied on the way to the exponential.
-                constexpr int L = KB / 4;                   // extrema run in four chains
-                bool poly1 = false, poly2 = false;          // warp-uniform: the cap's polynomials hold for every score here
-                float mx = -INFINITY;
-                if constexpr (CAP) {
-                    if (!masked) {                          // (a masked block takes the exact form: hidden scores may be anything)
-                        float a4[4], b4[4];
+                auto form_of = [&](float big) {              // 1, 2: the polynomial that holds for the whole warp; 0: the exact form
+                    return __all_sync(0xffffffffu, big <= p.half_at) ? 1 : __all_sync(0xffffffffu, big <= p.one_at) ? 2 : 0;
+                };
+                auto poly1 = [&](int x) {                    // capped scores x, x + 1 in log2 units
+                    const uint64_t s2 = pack_f32x2(sv[x], sv[x + 1]), y = mul_f32x2(s2, s2);
+                    uint64_t q = fma_f32x2(y, p.p1[3], p.p1[2]);
+                    q = fma_f32x2(q, y, p.p1[1]);
+                    q = fma_f32x2(q, y, p.p1[0]);
+                    return mul_f32x2(q, s2);
+                };
+                auto poly2 = [&](int x) {
+                    const uint64_t s2 = pack_f32x2(sv[x], sv[x + 1]), y = mul_f32x2(s2, s2);
+                    uint64_t q = fma_f32x2(y, p.p2[5], p.p2[4]);
+                    q = fma_f32x2(q, y, p.p2[3]);
+                    q = fma_f32x2(q, y, p.p2[2]);
+                    q = fma_f32x2(q, y, p.p2[1]);
+                    q = fma_f32x2(q, y, p.p2[0]);
+                    return mul_f32x2(q, s2);
+                };
+                auto exact = [&](int x) { return pack_f32x2(st_cap(p, sv[x]), st_cap(p, sv[x + 1])); };
+                auto in_place = [&](auto &&f) {
 #pragma unroll
-                        for (int c = 0; c < 4; ++c) {
-                            a4[c] = fmax3(sv[L * c], sv[L * c + 1], sv[L * c + 2]);
-                            b4[c] = fmax3_abs(sv[L * c], sv[L * c + 1], sv[L * c + 2]);
+                    for (int x = 0; x < KB; x += 2) unpack_f32x2(f(x), sv[x], sv[x + 1]);
+                };
+                // ---- score options in place.  Where any apply (kLog2) sv then holds scores in log2 units; q.k else.
+                constexpr bool kLog2 = CAP == 2 || BIAS;
+                if constexpr (CAP == 2) {
+                    float big[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-                            for (int x = 3; x < L - 1; x += 2) {
-                                a4[c] = fmax3(a4[c], sv[L * c + x], sv[L * c + x + 1]);
-                                b4[c] = fmax3_abs(b4[c], sv[L * c + x], sv[L * c + x + 1]);
-                            }
-                        }
-                        mx = fmaxf(fmax3(a4[0], a4[1], a4[2]), fmax3(a4[3], sv[L - 1], sv[2 * L - 1]));
-                        mx = fmax3(mx, sv[3 * L - 1], sv[4 * L - 1]);
-                        float big = fmax3_abs(fmax3_abs(b4[0], b4[1], b4[2]), b4[3], sv[L - 1]);
-                        big = fmax3_abs(fmax3_abs(big, sv[2 * L - 1], sv[3 * L - 1]), sv[4 * L - 1], 0.f) * p.y1;
-                        poly1 = __all_sync(0xffffffffu, big <= p.half_at);
-                        poly2 = !poly1 && __all_sync(0xffffffffu, big <= p.one_at);
-                    }
+                    for (int x = 0; x < KB; x += 2) big[(x >> 1) & 3] = fmax3_abs(big[(x >> 1) & 3], sv[x], sv[x + 1]);
+                    const int form = masked ? 0 : form_of(fmaxf(fmaxf(big[0], big[1]), fmaxf(big[2], big[3])) * p.y1);   // hidden scores may be anything
+                    if (form == 1) in_place(poly1);
+                    else if (form == 2) in_place(poly2);
+                    else in_place(exact);
                 }
                 if constexpr (BIAS) {
-                    if constexpr (CAP) {
-                        if (poly1 || poly2) {
-#pragma unroll
-                            for (int x = 0; x < KB; x += 2) {
-                                const uint64_t s2 = pack_f32x2(sv[x], sv[x + 1]), y = mul_f32x2(s2, s2);
-                                uint64_t q;
-                                if (poly1) {
-                                    q = fma_f32x2(y, pack_f32x2(p.p1[3], p.p1[3]), pack_f32x2(p.p1[2], p.p1[2]));
-                                    q = fma_f32x2(q, y, pack_f32x2(p.p1[1], p.p1[1]));
-                                    q = fma_f32x2(q, y, pack_f32x2(p.p1[0], p.p1[0]));
-                                } else {
-                                    q = fma_f32x2(y, pack_f32x2(p.p2[5], p.p2[5]), pack_f32x2(p.p2[4], p.p2[4]));
-                                    q = fma_f32x2(q, y, pack_f32x2(p.p2[3], p.p2[3]));
-                                    q = fma_f32x2(q, y, pack_f32x2(p.p2[2], p.p2[2]));
-                                    q = fma_f32x2(q, y, pack_f32x2(p.p2[1], p.p2[1]));
-                                    q = fma_f32x2(q, y, pack_f32x2(p.p2[0], p.p2[0]));
-                                }
-                                unpack_f32x2(mul_f32x2(q, s2), sv[x], sv[x + 1]);
-                            }
-                        } else {
-#pragma unroll
-                            for (int x = 0; x < KB; ++x) sv[x] = st_cap(p, sv[x]);
-                        }
-                    }
                     const float scale = CAP ? 1.f : p.c2;
-                    if (kb + KB - 1 <= trow0 || kb >= trow0 + 127) {      // the block lies on one side of the tile's rows
-                        const float st = kb >= trow0 + 127 ? -slope2 : slope2, b0 = -slope2 * fabsf(static_cast<float>(qrow - kb));
+                    if (kb + KB - 1 <= trow0) {                       // the block lies behind all of the tile's rows
+                        const uint64_t sc2 = pack_f32x2(scale, scale);
 #pragma unroll
-                        for (int x = 0; x < KB; ++x) sv[x] = fmaf(st, static_cast<float>(x), CAP ? sv[x] + b0 : fmaf(sv[x], scale, b0));
-                    } else {
-                        const float off = static_cast<float>(kb - qrow);
+                        for (int x = 0; x < KB; x += 4) {
+                            const ulonglong2 b4 = *reinterpret_cast<const ulonglong2 *>(bias + x);
+                            unpack_f32x2(fma_f32x2(pack_f32x2(sv[x], sv[x + 1]), sc2, b4.x), sv[x], sv[x + 1]);
+                            unpack_f32x2(fma_f32x2(pack_f32x2(sv[x + 2], sv[x + 3]), sc2, b4.y), sv[x + 2], sv[x + 3]);
+                        }
+                    } else {                                           // a key ahead of the row counts -slope (x + 2 (kb - row))
+                        const float off = static_cast<float>(kb - qrow), off2 = 2.f * off;
 #pragma unroll
-                        for (int x = 0; x < KB; ++x) sv[x] = fmaf(sv[x], scale, -slope2 * fabsf(static_cast<float>(x) + off));
+                        for (int x = 0; x < KB; ++x) {
+                            const float fx = static_cast<float>(x);
+                            sv[x] = fmaf(slope2, fx + off <= 0.f ? fx : -(fx + off2), sv[x] * scale);
+                        }
                     }
                 }
                 if (masked) {
+                    if constexpr (CAP == 1) in_place(exact);
 #pragma unroll
                     for (int x = 0; x < KB; ++x) sv[x] = seen(x) ? sv[x] : -INFINITY;
                 }
-                if (!CAP || BIAS || masked) {
-                    float r4[4];                             // four chains of three-input maxima
-#pragma unroll
-                    for (int c = 0; c < 4; ++c) {
-                        r4[c] = fmax3(sv[L * c], sv[L * c + 1], sv[L * c + 2]);
-#pragma unroll
-                        for (int x = 3; x < L - 1; x += 2) r4[c] = fmax3(r4[c], sv[L * c + x], sv[L * c + x + 1]);
-                        r4[c] = fmaxf(r4[c], sv[L * c + L - 1]);
-                    }
-                    mx = fmaxf(fmax3(r4[0], r4[1], r4[2]), r4[3]);
-                }
-                // the reference moves only when the block's maximum lies more than kPfSlack above it, so that O is hardly
-                // ever rescaled; a row that has seen nothing yet keeps -inf
-                float xmax;
-                if constexpr (BIAS) xmax = mx;
-                else if constexpr (CAP) {
-                    if (poly1) {             // the polynomial that the weights below use
-                        const float y = mx * mx;
-                        xmax = mx * fmaf(fmaf(fmaf(p.p1[3], y, p.p1[2]), y, p.p1[1]), y, p.p1[0]);
-                    } else xmax = mx == -INFINITY ? -INFINITY : st_cap(p, mx);
-                }
-                else xmax = mx * p.c2;
-                const float m_new = (xmax > m + kPfSlack) ? xmax : m;
-                const float ref = m_new == -INFINITY ? 0.f : m_new;
-                const float alpha = m == -INFINITY ? 1.f : ex2_approx(m - m_new);
-                l *= alpha;
-                m = m_new;
+                // ---- weights 2^(score - reference), their sum, and P
                 bool o_ready = n + i == 0;                       // O has taken the block before in
-                if (i > 0 && !__all_sync(0xffffffffu, alpha == 1.f)) {
-                    wait(&bar_o[t], n + i - 1);
-                    o_ready = true;
-                    tc_fence_after();
-#pragma unroll 1
-                    for (int c = 0; c < D / 32; ++c) {
-                        float ov[32];
-                        tmem_ld32(t_o + c * 32, ov);
-#pragma unroll
-                        for (int x = 0; x < 32; ++x) ov[x] *= alpha;
-                        tmem_st32(t_o + c * 32, ov);
-                    }
-                }
-                const uint64_t mx2 = pack_f32x2(-ref, -ref);
-                uint64_t lsum2 = 0;                          // two partial row sums, (+0, +0)
+                uint64_t lsum2 = 0;                              // two partial row sums, (+0, +0)
                 uint32_t pk[KB / 2];
-                {
-                    auto weights = [&](auto &&arg) {         // arg(x): scores x, x + 1 in log2 units, relative to the reference
+                // arg(x): scores x, x + 1 in log2 units, relative to the reference; extremum: runs alongside, in four chains
+                float r4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+                auto weights = [&](auto &&arg, auto &&extremum) {
+                    lsum2 = 0;
 #pragma unroll
-                        for (int y = 0; y < KB / 2; ++y) {
-                            float a0, a1;
-                            unpack_f32x2(arg(2 * y), a0, a1);
-                            const float p0 = ex2_approx(a0), p1 = ex2_approx(a1);
-                            lsum2 = add_f32x2(lsum2, pack_f32x2(p0, p1));
-                            pk[y] = pack_bf16(p0, p1);
-                        }
-                    };
-                    if constexpr (BIAS) {
-                        weights([&](int x) { return add_f32x2(pack_f32x2(sv[x], sv[x + 1]), mx2); });
-                    } else if constexpr (!CAP) {
-                        const uint64_t c22 = pack_f32x2(p.c2, p.c2);
-                        weights([&](int x) { return fma_f32x2(pack_f32x2(sv[x], sv[x + 1]), c22, mx2); });
-                    } else if (poly1) {
-                        weights([&](int x) {
-                            const uint64_t s2 = pack_f32x2(sv[x], sv[x + 1]), y = mul_f32x2(s2, s2);
-                            uint64_t q = fma_f32x2(y, pack_f32x2(p.p1[3], p.p1[3]), pack_f32x2(p.p1[2], p.p1[2]));
-                            q = fma_f32x2(q, y, pack_f32x2(p.p1[1], p.p1[1]));
-                            q = fma_f32x2(q, y, pack_f32x2(p.p1[0], p.p1[0]));
-                            return fma_f32x2(q, s2, mx2);
-                        });
-                    } else if (poly2) {
-                        weights([&](int x) {
-                            const uint64_t s2 = pack_f32x2(sv[x], sv[x + 1]), y = mul_f32x2(s2, s2);
-                            uint64_t q = fma_f32x2(y, pack_f32x2(p.p2[5], p.p2[5]), pack_f32x2(p.p2[4], p.p2[4]));
-                            q = fma_f32x2(q, y, pack_f32x2(p.p2[3], p.p2[3]));
-                            q = fma_f32x2(q, y, pack_f32x2(p.p2[2], p.p2[2]));
-                            q = fma_f32x2(q, y, pack_f32x2(p.p2[1], p.p2[1]));
-                            q = fma_f32x2(q, y, pack_f32x2(p.p2[0], p.p2[0]));
-                            return fma_f32x2(q, s2, mx2);
-                        });
-                    } else {
-                        weights([&](int x) {
-                            const float a0 = sv[x] == -INFINITY ? -INFINITY : st_cap(p, sv[x]) - ref;
-                            const float a1 = sv[x + 1] == -INFINITY ? -INFINITY : st_cap(p, sv[x + 1]) - ref;
-                            return pack_f32x2(a0, a1);
-                        });
+                    for (int y = 0; y < KB / 2; ++y) {
+                        float a0, a1;
+                        extremum(r4[y & 3], sv[2 * y], sv[2 * y + 1]);
+                        unpack_f32x2(arg(2 * y), a0, a1);
+                        const float p0 = ex2_approx(a0), p1 = ex2_approx(a1);
+                        lsum2 = add_f32x2(lsum2, pack_f32x2(p0, p1));
+                        pk[y] = pack_bf16(p0, p1);
                     }
+                };
+                auto nothing = [](float &, float, float) {};
+                if constexpr (CAP == 1) {
+                    // Capped scores lie within +-cap2 <= 92 log2 units: relative to 0, weights, sums over 2^24 keys and O stay within
+                    // fp32, so no maximum is needed.  The form that suits the block before is tried first; whether it holds here
+                    // is found out alongside.
+                    if (masked) {
+                        weights([&](int x) { return pack_f32x2(sv[x], sv[x + 1]); }, nothing);
+                    } else {
+                        auto largest = [](float &r, float a, float b) { r = fmax3_abs(r, a, b); };
+                        r4[0] = r4[1] = r4[2] = r4[3] = 0.f;
+                        if (form == 1) weights(poly1, largest);
+                        else if (form == 2) weights(poly2, largest);
+                        else weights(exact, largest);
+                        const int holds = form_of(fmaxf(fmaxf(r4[0], r4[1]), fmaxf(r4[2], r4[3])) * p.y1);
+                        if (form == 1 && holds == 2) weights(poly2, nothing);
+                        else if (form != 0 && holds == 0) weights(exact, nothing);
+                        form = holds;
+                    }
+                } else {
+                    // The reference is the greatest score so far, or less by up to kPfSlack, so that O is hardly ever rescaled;
+                    // a row that has seen nothing keeps -inf.  (Taking the weights relative to the block before's reference, with
+                    // the maximum found alongside and the weights taken again where that was too low, was 7 % slower.)
+#pragma unroll
+                    for (int x = 0; x < KB; x += 2) r4[(x >> 1) & 3] = fmax3(r4[(x >> 1) & 3], sv[x], sv[x + 1]);
+                    const float mx = fmaxf(fmaxf(r4[0], r4[1]), fmaxf(r4[2], r4[3])), xmax = kLog2 ? mx : mx * p.c2;
+                    if (__any_sync(0xffffffffu, xmax > m + kPfSlack)) {
+                        const float m_new = (xmax > m + kPfSlack) ? xmax : m;
+                        const float alpha = m == -INFINITY ? 1.f : ex2_approx(m - m_new);
+                        l *= alpha;
+                        m = m_new;
+                        if (i > 0 && !__all_sync(0xffffffffu, alpha == 1.f)) {
+                            wait(&bar_o[t], n + i - 1);
+                            o_ready = true;
+                            tc_fence_after();
+#pragma unroll 1
+                            for (int c = 0; c < D / 32; ++c) {
+                                float ov[32];
+                                tmem_ld32(t_o + c * 32, ov);
+#pragma unroll
+                                for (int x = 0; x < 32; ++x) ov[x] *= alpha;
+                                tmem_st32(t_o + c * 32, ov);
+                            }
+                        }
+                    }
+                    const float ref = m == -INFINITY ? 0.f : m;
+                    const uint64_t mx2 = pack_f32x2(-ref, -ref), c22 = pack_f32x2(p.c2, p.c2);
+                    if constexpr (kLog2) weights([&](int x) { return add_f32x2(pack_f32x2(sv[x], sv[x + 1]), mx2); }, nothing);
+                    else weights([&](int x) { return fma_f32x2(pack_f32x2(sv[x], sv[x + 1]), c22, mx2); }, nothing);
                 }
                 if (!o_ready) wait(&bar_o[t], n + i - 1);      // P of the block before has been read
                 tc_fence_after();
@@ -751,6 +512,239 @@ prefill_scored_tc_kernel(const __grid_constant__ ScoredTcParams p, const __grid_
             tc_fence_before();                               // O is read: ordered before this warp's next arrival
             plan_done(r);
         }
+    } else {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
+    if (wid == 12) {
+        // ---------------- the planning warp
+        // lane l sums the item rows of users [l C, (l + 1) C); users from the first inconsistent one on are left out
+        const int C = (p.s.B + 31) / 32, u0 = lane * C, u1 = min(p.s.B, u0 + C);
+        int sum = 0;
+        bool bad = false;
+#pragma unroll 4
+        for (int u = u0; u < u1; ++u) {
+            const int64_t a = p.s.tok_indptr[u], b = p.s.tok_indptr[u + 1];
+            bad = bad || a < 0 || b < a || b > p.s.T;
+            if (!bad) sum += static_cast<int>((b - a + rows_item - 1) / rows_item);
+        }
+        int inc = sum;
+#pragma unroll
+        for (int d = 1; d < 32; d <<= 1) {
+            const int up = __shfl_up_sync(0xffffffffu, inc, d);
+            if (lane >= d) inc += up;
+        }
+        const unsigned badmask = __ballot_sync(0xffffffffu, bad);
+        const int blocks = __shfl_sync(0xffffffffu, inc, badmask ? __ffs(badmask) - 1 : 31);
+        const int64_t items = static_cast<int64_t>(blocks) * hgroups;
+        for (int r = 0;; ++r) {
+            // dealt out to and fro, so that nobody gets the heaviest of every round
+            const int64_t item = static_cast<int64_t>(r) * gridDim.x + ((r & 1) ? gridDim.x - 1 - blockIdx.x : blockIdx.x);
+            StPlan &pl = plans[r & 1];
+            if (r >= 2) wait(&bar_planfree[r & 1], (r >> 1) - 1);
+            __syncwarp();
+            const bool valid = ok && static_cast<int64_t>(r) * gridDim.x < items;      // a round may have nothing for this CTA: an empty item
+            if (!valid) {
+                if (lane == 0) { pl.valid = 0; mbar_arrive(smem_u32(&bar_plan[r & 1])); }
+                break;
+            }
+            const bool some = item < items;
+            const int blk = some ? static_cast<int>(item / hgroups) : 0, h0 = some ? static_cast<int>(item % hgroups) * hpc : 0;
+            int user = 0, qb = 0, first = 0, len = 0;
+            if (some) {                   // the user whose rows hold block blk; a prompt's blocks count from its end
+                const int src = __ffs(__ballot_sync(0xffffffffu, blk < inc)) - 1;
+                if (lane == src) {
+                    int rem = blk - (inc - sum);
+                    for (user = u0; user < u1; ++user) {
+                        first = p.s.tok_indptr[user];
+                        len = p.s.tok_indptr[user + 1] - first;
+                        const int nb = (len + rows_item - 1) / rows_item;
+                        if (rem < nb) { qb = nb - 1 - rem; break; }
+                        rem -= nb;
+                    }
+                }
+                user = __shfl_sync(0xffffffffu, user, src);
+                qb = __shfl_sync(0xffffffffu, qb, src);
+                first = __shfl_sync(0xffffffffu, first, src);
+                len = __shfl_sync(0xffffffffu, len, src);
+            }
+            const int row0 = qb * rows_item;
+            const int prefix = some && p.s.prefix_lens ? min(len, p.s.prefix_lens[user]) : 0;
+            int tlo[2] = {0x7fffffff, 0x7fffffff}, thi[2] = {-1, -1}, fulllo = -1, fullhi = 0x7fffffff;
+#pragma unroll
+            for (int w = 0; w < 8; ++w) {           // the 32 rows of softmax warp w; two heads have the same rows
+                const int qrow = row0 + (hpc == 2 ? 32 * (w & 3) : 32 * w) + lane;
+                int lo = 0x7fffffff, hi = -1;
+                const bool live = some && qrow < len;
+                if (live) scored_interval(p.s, first, prefix, qrow, lo, hi);
+                const bool sees = lo <= hi;
+                if (!sees) { lo = 0x7fffffff; hi = -1; }
+                pl.span[32 * w + lane] = make_int2(lo, hi);
+                // a live row that sees nothing makes every block one with hidden keys
+                const int a = __reduce_min_sync(0xffffffffu, lo), b = __reduce_max_sync(0xffffffffu, hi);
+                const int c = __reduce_max_sync(0xffffffffu, sees ? lo : (live ? 0x7fffffff : -1));
+                const int d = __reduce_min_sync(0xffffffffu, sees ? hi : (live ? -1 : 0x7fffffff));
+                if (lane == 0) pl.stats[w] = StBlockStats{a, b, c, d};
+                tlo[w >> 2] = min(tlo[w >> 2], a); thi[w >> 2] = max(thi[w >> 2], b);
+                fulllo = max(fulllo, c); fullhi = min(fullhi, d);
+            }
+            if (lane == 0) {
+                const int key0 = min(tlo[0], tlo[1]), key1 = max(thi[0], thi[1]);
+                pl.valid = 1; pl.first = first; pl.len = len; pl.row0 = row0; pl.h0 = h0;
+                pl.tiles = !some ? 0 : (hpc == 2 || row0 + 128 < len) ? 2 : 1;
+                const int nb = key1 < 0 ? 0 : (key1 - key0) / KB + 1;
+                pl.nb = nb; pl.kend = key1 < 0 ? 0 : key0 + (nb - 1) * KB;
+#pragma unroll
+                for (int x = 0; x < 2; ++x) {
+                    pl.ja[x] = thi[x] < 0 ? 0 : nb - 1 - (thi[x] - key0) / KB;
+                    pl.jb[x] = thi[x] < 0 ? 0 : nb - (tlo[x] - key0) / KB;
+                }
+                pl.fulllo = fulllo; pl.fullhi = fullhi; pl.poisoned = 0;
+            }
+            __syncwarp();
+            if (lane == 0) mbar_arrive(smem_u32(&bar_plan[r & 1]));
+        }
+    } else if (wid == 10) {
+        // ---------------- the loading warp (one thread of it); c counts blocks over all items
+        int c = 0, nq = 0;
+        for (int r = 0; ok; ++r) {
+            const StPlan &pl = plan_of(r);
+            if (!ok || !pl.valid) break;
+            const int NB = pl.nb, kvh = pl.h0 / gq, y0 = pl.first + pl.kend;
+            if (lane == 0 && NB > 0) {
+                if (nq > 0) wait1(bar_qfree, nq - 1);
+                if (ok) {
+                    mbar_expect_tx(smem_u32(bar_q), pl.tiles * QTILE);
+                    for (int t = 0; t < pl.tiles; ++t)
+                        for (int x = 0; x < BOXES; ++x)
+                            tma_load_3d(Qs + t * QTILE + x * kStQBox, &mq, 64 * x, hpc == 2 ? pl.h0 + t : pl.h0, pl.first + pl.row0 + (hpc == 2 ? 0 : 128 * t), smem_u32(bar_q));
+                }
+                for (int j = 0; j < NB && ok; ++j, ++c) {
+                    const int slot = c % NS, use = c / NS, y = y0 - j * KB;
+                    if (use > 0) wait1(&bar_kfree[slot], use - 1);
+                    if (!ok) break;
+                    mbar_expect_tx(smem_u32(&bar_k[slot]), TILE);
+                    for (int x = 0; x < BOXES; ++x) tma_load_3d(Ks + slot * TILE + x * kStBox, &mk, 64 * x, kvh, y, smem_u32(&bar_k[slot]));
+                    if (use > 0) wait1(&bar_vfree[slot], use - 1);
+                    if (!ok) break;
+                    mbar_expect_tx(smem_u32(&bar_v[slot]), TILE);
+                    for (int x = 0; x < BOXES; ++x) tma_load_3d(Vs + slot * TILE + x * kStBox, &mv, 64 * x, kvh, y, smem_u32(&bar_v[slot]));
+                }
+            }
+            if (NB > 0) ++nq;
+            ok = __shfl_sync(0xffffffffu, ok, 0);
+            plan_done(r);
+        }
+        if (lane == 0 && !ok) {              // leave nothing in flight behind: a bounded chance for what was asked for last
+            if (nq > 0) mbar_wait(smem_u32(bar_q), (nq - 1) & 1);
+            for (int x = 0; x < NS; ++x) {
+                const int uses = (c - x + NS) / NS;          // blocks that went to slot x, the one that was cut off included
+                if (c >= x && uses > 0) { mbar_wait(smem_u32(&bar_k[x]), (uses - 1) & 1); mbar_wait(smem_u32(&bar_v[x]), (uses - 1) & 1); }
+            }
+        }
+    } else if (wid == 11) {
+        // ---------------- the guard: V rows of blocks with hidden keys
+        int c = 0;
+        for (int r = 0; ok; ++r) {
+            StPlan &pl = plan_of(r);
+            if (!ok || !pl.valid) break;
+            const int NB = pl.nb;
+            for (int j = 0; j < NB && ok; ++j, ++c) {
+                // every block passes through here, so that the guard is never a whole ring ahead of or behind the others
+                const int slot = c % NS, kb = pl.kend - j * KB;
+                wait(&bar_v[slot], c / NS);
+                __syncwarp();
+                if (pl.fulllo <= kb && kb + KB - 1 <= pl.fullhi) {
+                    if (lane == 0) mbar_arrive(smem_u32(&bar_guard[slot]));
+                    continue;
+                }
+                uint8_t *vt = base + 2 * QTILE + (NS + slot) * TILE;
+                auto odd = [](const uint4 &w) {           // a 16-bit half with all exponent bits set carries into its sign bit
+                    return ((w.x & 0x7f807f80u) + 0x00800080u) | ((w.y & 0x7f807f80u) + 0x00800080u) | ((w.z & 0x7f807f80u) + 0x00800080u) |
+                           ((w.w & 0x7f807f80u) + 0x00800080u);
+                };
+                uint32_t any = 0;
+#pragma unroll 5
+                for (int x = lane; x < TILE / 16; x += 32) any |= odd(*reinterpret_cast<const uint4 *>(vt + x * 16));
+                if (__any_sync(0xffffffffu, (any & 0x80008000u) != 0)) {
+                    for (int row = 0; row < KB; ++row) {        // rare: row by row
+                        uint4 *chunk = reinterpret_cast<uint4 *>(vt + (lane >> 3) * kStBox + row * 128 + (lane & 7) * 16);
+                        const bool mine = lane < 8 * BOXES;
+                        if (!__any_sync(0xffffffffu, mine && (odd(*(mine ? chunk : reinterpret_cast<uint4 *>(vt + row * 128))) & 0x80008000u) != 0)) continue;
+                        const int key = kb + row;
+                        bool seen = false, hidden = false;
+                        for (int x = lane; x < 256; x += 32) {
+                            const int2 sp = pl.span[x];
+                            const bool s = sp.x <= key && key <= sp.y;
+                            seen = seen || s;
+                            hidden = hidden || !s;
+                        }
+                        if (!__any_sync(0xffffffffu, seen)) {
+                            if (mine) *chunk = make_uint4(0, 0, 0, 0);
+                        } else if (__any_sync(0xffffffffu, hidden)) {
+                            pl.poisoned = 1;
+                        }
+                    }
+                    fence_proxy_async();
+                    __syncwarp();
+                }
+                if (lane == 0) mbar_arrive(smem_u32(&bar_guard[slot]));
+            }
+            plan_done(r);
+        }
+    } else if (wid < 10) {
+        // ---------------- the warp that issues tile x's MMAs: S of block j, then P V of block j - 1; n counts the tile's blocks
+        const int x = wid - 8;
+        const uint32_t ts = tmem + (x ? kStS1 : kStS0), tp = tmem + (x ? kStP1 : kStP0), to = tmem + (x ? kStO1 : kStO0);
+        int c = 0, n = 0, nq = 0;
+        for (int r = 0; ok; ++r) {
+            const StPlan &pl = plan_of(r);
+            if (!ok || !pl.valid) break;
+            const int NB = pl.nb, a = x ? pl.ja[1] : pl.ja[0], b = x ? pl.jb[1] : pl.jb[0];
+            if (NB > 0) wait(bar_q, nq++);
+            for (int j = 0; j <= NB && NB > 0 && ok; ++j) {
+                if (j < NB) {
+                    const int slot = (c + j) % NS;
+                    // a tile that has no use for a block gives it back all the same, once it is there: never a ring ahead
+                    wait(&bar_k[slot], (c + j) / NS);
+                    if (a <= j && j < b) {
+                        const int k = n + j - a;
+                        if (k > 0) wait(&bar_sf[x], k - 1);
+                        __syncwarp();
+                        tc_fence_after();
+#pragma unroll
+                        for (int kk = 0; kk < D / 16; ++kk)       // 16 channels per MMA
+                            st_mma_ss(ts, umma_desc(Qs + x * QTILE + (kk >> 2) * kStQBox + (kk & 3) * 32, 16, 1024),
+                                      umma_desc(Ks + slot * TILE + (kk >> 2) * kStBox + (kk & 3) * 32, 16, 1024), umma_idesc(false, KB), kk > 0 ? 1u : 0u);
+                        st_commit(smem_u32(&bar_s[x]));
+                        st_commit(smem_u32(&bar_kfree[slot]));
+                    } else if (lane == 0) {
+                        mbar_arrive(smem_u32(&bar_kfree[slot]));
+                    }
+                    if (j == NB - 1) st_commit(smem_u32(bar_qfree));      // behind the item's last use of Q (at once where nothing is under way)
+                }
+                if (j > 0) {
+                    const int jj = j - 1, slot = (c + jj) % NS;
+                    wait(&bar_v[slot], (c + jj) / NS);
+                    wait(&bar_guard[slot], (c + jj) / NS);
+                    if (a <= jj && jj < b) {
+                        const int i = jj - a;
+                        wait(&bar_p[x], n + i);           // also: this tile's softmax has read the O of the item before
+                        __syncwarp();
+                        tc_fence_after();
+#pragma unroll
+                        for (int kk = 0; kk < KB / 16; ++kk)      // 16 keys per MMA: 8 columns of P, 2 KB of each 64-channel box of V
+                            st_mma_ts(to, tp + kk * 8, umma_desc(Vs + slot * TILE + kk * 2048, kStBox, 1024), umma_idesc(true, D), (i > 0 || kk > 0) ? 1u : 0u);
+                        st_commit(smem_u32(&bar_o[x]));
+                        st_commit(smem_u32(&bar_vfree[slot]));
+                    } else if (lane == 0) {
+                        mbar_arrive(smem_u32(&bar_vfree[slot]));
+                    }
+                }
+            }
+            c += NB;
+            n += b - a;
+            plan_done(r);
+        }
+    }
     }
     tc_fence_before();
     const bool gave_up = !__syncthreads_and(ok);
