@@ -2,15 +2,61 @@
 #include "spd_host.h"
 #include "spd_launch.cuh"
 #include "spd_rope.cuh"
+#include "spd_short.cuh"
 
 namespace spd {
+
+// How many CTAs of one cluster share a sequence, or 0 where the call is not a short one.  The host does not know the lengths; a
+// window, or the pools' size, bounds the tiles of a sequence.  Every cluster must find a place at once (one CTA per SM), a
+// warp's tiles stay few, and a caller who set the cut or asked for a stored plan gets the persistent kernel.
+template <class Math>
+static int short_cluster(const Params &p, int sms) {
+    if (p.plan_mode != PLAN_DERIVE || p.min_tiles != kMinTilesPerWarp || p.uniform) return 0;
+    const int64_t seqs = static_cast<int64_t>(p.B) * p.S;
+    int64_t tiles = static_cast<int64_t>(p.part[0].num_pages) + p.part[1].num_pages;
+    if (p.window > 0 && p.window / kPage + 3 < tiles) tiles = p.window / kPage + 3;      // ragged at both ends and where the partitions meet
+    int c = 1;
+    while (2 * c <= kShortMaxCluster && 2 * c * seqs <= sms && tiles > c * Math::kWarps) c *= 2;
+    return c * seqs <= sms && tiles <= static_cast<int64_t>(c) * Math::kWarps * kShortTiles ? c : 0;
+}
+
+template <class Math>
+static spd_status launch_scored(const Params &p, const CUtensorMap *maps, int sms, cudaStream_t st, bool pdl) {
+    const int cluster = short_cluster<Math>(p, sms);
+    if (cluster == 0) return launch_attn<Math>(p, maps, sms, st, pdl);
+    static std::once_flag once[64];
+    int dev = 0;
+    cudaGetDevice(&dev);
+    cudaError_t err = cudaSuccess;
+    std::call_once(once[dev & 63], [&] {
+        err = cudaFuncSetAttribute(attn_short_kernel<Math>, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(short_smem_bytes<Math>()));
+    });
+    if (err != cudaSuccess) return SPD_ERR_CUDA;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(static_cast<unsigned>(p.B * p.S * cluster));
+    cfg.blockDim = dim3(Math::kWarps * 32);
+    cfg.dynamicSmemBytes = short_smem_bytes<Math>();
+    cfg.stream = st;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = static_cast<unsigned>(cluster);
+    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+    attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[1].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = pdl ? 2 : 1;
+    err = cudaLaunchKernelEx(&cfg, attn_short_kernel<Math>, p, maps[0], maps[1], maps[2], maps[3], cluster);
+    host::count_launch();
+    if (err != cudaSuccess) fprintf(stderr, "libspd: launch of the short attention kernel: %s\n", cudaGetErrorString(err));
+    return err == cudaSuccess ? SPD_OK : SPD_ERR_CUDA;
+}
 
 spd_status launch_attn_scored(const Params &p, const CUtensorMap *maps, int sms, cudaStream_t st, bool pdl, bool bf16, int head_dim) {
     spd_status rc = SPD_ERR_UNSUPPORTED;
     if (bf16) {
-        rc = head_dim == 128 ? launch_attn<MathBF16<128, true>>(p, maps, sms, st, pdl) : launch_attn<MathBF16<64, true>>(p, maps, sms, st, pdl);
+        rc = head_dim == 128 ? launch_scored<MathBF16<128, true>>(p, maps, sms, st, pdl) : launch_scored<MathBF16<64, true>>(p, maps, sms, st, pdl);
     } else {
-#define SPD_F32_CASE(DD, GG) if (head_dim == DD && p.geff == GG) rc = launch_attn<MathF32<DD, GG, true>>(p, maps, sms, st, pdl);
+#define SPD_F32_CASE(DD, GG) if (head_dim == DD && p.geff == GG) rc = launch_scored<MathF32<DD, GG, true>>(p, maps, sms, st, pdl);
         SPD_F32_CASE(64, 1) SPD_F32_CASE(64, 2) SPD_F32_CASE(64, 4) SPD_F32_CASE(64, 8)
         SPD_F32_CASE(128, 1) SPD_F32_CASE(128, 2) SPD_F32_CASE(128, 4) SPD_F32_CASE(128, 8)
 #undef SPD_F32_CASE

@@ -10,6 +10,14 @@ from tests import scored_reference as ref
 pytestmark = pytest.mark.gpu
 
 
+@pytest.fixture(params=["short", "persistent"])
+def kernel(request):
+    """Small calls go to the cluster kernel; asking for a cut of its own (here: at least 3 tiles per share) keeps the persistent one."""
+    spd.spd_set_split(3 if request.param == "persistent" else 0, False)
+    yield request.param
+    spd.spd_set_split(0, False)
+
+
 def slopes_of(hq):
     return (2.0 ** (-8.0 * torch.arange(1, hq + 1, dtype=torch.float64) / hq)).float()
 
@@ -42,7 +50,7 @@ SHAPES = [("bf16", 128, 8, 1), ("bf16", 128, 4, 4), ("bf16", 64, 4, 2), ("bf16",
 @pytest.mark.parametrize("dtype,d,hq,hkv", SHAPES)
 @pytest.mark.parametrize("cap,window,alibi", [(0.0, 0, False), (20.0, 0, False), (0.0, 0, True), (0.0, 1, False), (0.0, 17, True), (5.0, 33, True),
                                               (50.0, 300, False), (0.0, 100000, False)])
-def test_fused_and_halves(dtype, d, hq, hkv, cap, window, alibi):
+def test_fused_and_halves(kernel, dtype, d, hq, hkv, cap, window, alibi):
     w = workload(*LENGTHS, hq, hkv, d, dtype, seed=d + hq, qscale=3.0)
     g, shape, score, sl, ws = setup(w, cap, window, alibi)
     want, _, _, _, tol = ref.decode(w, cap, window, sl)
@@ -108,7 +116,7 @@ def test_what_lies_in_front_of_the_window_is_never_used(dtype, window):
                 if base + min(m, 16 * pgi + 16) <= first:
                     part.page_indices[lo + pgi] = -1 if pgi % 2 else part.num_pages + 5
     g, shape, score, _, ws = setup(w, 0.0, window, False)
-    for share in (0, 1):
+    for share in (0, 1, 3):               # 0: the cluster kernel
         try:
             spd.spd_set_split(share, False)
             out = torch.full((w.batch, 8, 128), float("nan"), device="cuda")
@@ -120,7 +128,7 @@ def test_what_lies_in_front_of_the_window_is_never_used(dtype, window):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
-def test_nan_inside_the_window_is_not_hidden(dtype):
+def test_nan_inside_the_window_is_not_hidden(kernel, dtype):
     w = workload([300, 40], [10, 40], 4, 2, 64, dtype, seed=31)
     want, _, _, _, tol = ref.decode(w, 0.0, 64)
     pg = int(w.priv.page_indices[int(w.priv.page_indptr[0]) + 290 // 16])
@@ -165,7 +173,7 @@ def test_stored_plan_belongs_to_its_window():
     assert spd.spd_query_device_status(ws)[0] == 7
 
 
-def test_bad_pages_and_lengths_are_contained():
+def test_bad_pages_and_lengths_are_contained(kernel):
     w = workload([200, 100, 90, 300], [20, 30, 5, 8], 8, 2, 128, "bf16", seed=23)
     want, _, _, _, tol = ref.decode(w, 0.0, 128)
     w.priv.page_indices[int(w.priv.page_indptr[0]) + 7] = w.priv.num_pages        # tokens 112 .. 127 of user 0: inside its window
@@ -184,7 +192,7 @@ def test_bad_pages_and_lengths_are_contained():
     assert bool((part[1][2] == -float("inf")).all()) and bool((part[2][2] == 0).all())
 
 
-def test_captured_and_replayed_on_another_stream():
+def test_captured_and_replayed_on_another_stream(kernel):
     w = workload([700, 80, 0], [40, 9, 33], 8, 2, 128, "bf16", seed=24)
     g, shape, score, sl, ws = setup(w, 10.0, 200, True)
     want, _, _, _, tol = ref.decode(w, 10.0, 200, sl)
@@ -201,3 +209,36 @@ def test_captured_and_replayed_on_another_stream():
         torch.cuda.synchronize()
         close(out, want, tol, "replay")
     assert spd.spd_query_device_status(ws) == (spd.SPD_OK, -1)
+
+
+@pytest.mark.parametrize("dtype,d,hq,hkv", [("bf16", 128, 8, 1), ("bf16", 64, 4, 4), ("f32", 64, 8, 2), ("f32", 128, 16, 1)])
+def test_clusters_of_every_size(dtype, d, hq, hkv):
+    """One user to so many that a sequence gets a single CTA; users with nothing cached, with one token, and with the longest sequence."""
+    for B in (1, 2, 5, 18, 37):
+        lin = [(37 * u * u + 900 * (u == 0)) % 1200 for u in range(B)]
+        lout = [(11 * u) % 40 for u in range(B)]
+        w = workload(lin, lout, hq, hkv, d, dtype, seed=B)
+        g, shape, score, sl, ws = setup(w, 15.0, 0, True)
+        want, _, _, _, tol = ref.decode(w, 15.0, 0, sl)
+        out = torch.full((B, hq, d), float("nan"), device="cuda")
+        spd.spd_decode_step_scored(shape, score, g.q, g.priv, g.pub, out, ws)
+        assert spd.spd_query_device_status(ws) == (spd.SPD_OK, -1)
+        close(out, want, tol, f"{B} users")
+
+
+def test_two_streams_side_by_side():
+    """Two batches with a workspace each, called in turn on two streams; every result is right."""
+    jobs = []
+    for s in range(2):
+        w = workload([300 + 50 * s, 40, 90], [5, 60, 0], 8, 2, 128, "bf16", seed=40 + s)
+        g, shape, score, sl, ws = setup(w, 0.0, 128, True)
+        want, _, _, _, tol = ref.decode(w, 0.0, 128, sl)
+        jobs.append((g, shape, score, ws, torch.empty((3, 8, 128), device="cuda"), torch.cuda.Stream(), want, tol))
+    torch.cuda.synchronize()
+    for _ in range(20):
+        for g, shape, score, ws, out, st, _, _ in jobs:
+            spd.spd_decode_step_scored(shape, score, g.q, g.priv, g.pub, out, ws, stream=st)
+    torch.cuda.synchronize()
+    for _, _, _, ws, out, st, want, tol in jobs:
+        close(out, want, tol, "side by side")
+        assert spd.spd_query_device_status(ws, st) == (spd.SPD_OK, -1)
