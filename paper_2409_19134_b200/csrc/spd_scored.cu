@@ -6,32 +6,54 @@
 
 namespace spd {
 
-// How many CTAs of one cluster share a sequence, or 0 where the call is not a short one.  The host does not know the lengths; a
-// window, or the pools' size, bounds the tiles of a sequence.  Every cluster must find a place at once (one CTA per SM), a
-// warp's tiles stay few, and a caller who set the cut or asked for a stored plan gets the persistent kernel.
+// Clusters of 1, 2, 4, 8 CTAs of the short kernel that the current device holds at once (a cluster lies within one group of
+// SMs, so not every SM can be used by large ones).  Looked up once per device; also raises the kernel's shared-memory limit.
 template <class Math>
-static int short_cluster(const Params &p, int sms) {
+static const int *short_capacity() {
+    static std::once_flag once[64];
+    static int fit[64][4];
+    int dev = 0;
+    cudaGetDevice(&dev);
+    dev &= 63;
+    std::call_once(once[dev], [&] {
+        if (cudaFuncSetAttribute(attn_short_kernel<Math>, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(short_smem_bytes<Math>())) != cudaSuccess)
+            return;                                        // nothing fits: the persistent kernel serves the calls
+        for (int i = 0; i < 4; ++i) {
+            cudaLaunchConfig_t cfg = {};
+            cfg.gridDim = dim3(1u << i);
+            cfg.blockDim = dim3(Math::kWarps * 32);
+            cfg.dynamicSmemBytes = short_smem_bytes<Math>();
+            cudaLaunchAttribute attr[1];
+            attr[0].id = cudaLaunchAttributeClusterDimension;
+            attr[0].val.clusterDim.x = 1u << i;
+            attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+            cfg.attrs = attr;
+            cfg.numAttrs = 1;
+            if (cudaOccupancyMaxActiveClusters(&fit[dev][i], attn_short_kernel<Math>, &cfg) != cudaSuccess) { fit[dev][i] = 0; cudaGetLastError(); }
+        }
+    });
+    return fit[dev];
+}
+
+// How many CTAs of one cluster share a sequence, or 0 where the call is not a short one.  The host does not know the lengths; a
+// window, or the pools' size, bounds the tiles of a sequence.  A caller who set the cut or asked for a stored plan gets the
+// persistent kernel.
+template <class Math>
+static int short_cluster(const Params &p) {
     if (p.plan_mode != PLAN_DERIVE || p.min_tiles != kMinTilesPerWarp || p.uniform) return 0;
     const int64_t seqs = static_cast<int64_t>(p.B) * p.S;
     int64_t tiles = static_cast<int64_t>(p.part[0].num_pages) + p.part[1].num_pages;
     if (p.window > 0 && p.window / kPage + 3 < tiles) tiles = p.window / kPage + 3;      // ragged at both ends and where the partitions meet
-    int c = 1;
-    while (2 * c <= kShortMaxCluster && 2 * c * seqs <= sms && tiles > c * Math::kWarps) c *= 2;
-    return c * seqs <= sms && tiles <= static_cast<int64_t>(c) * Math::kWarps * kShortTiles ? c : 0;
+    const int *fit = short_capacity<Math>();
+    int i = 0;
+    while (i < 3 && seqs <= fit[i + 1] && tiles > (Math::kWarps << i)) ++i;
+    return seqs <= fit[i] && tiles <= (static_cast<int64_t>(Math::kWarps) << i) * kShortTiles ? 1 << i : 0;
 }
 
 template <class Math>
 static spd_status launch_scored(const Params &p, const CUtensorMap *maps, int sms, cudaStream_t st, bool pdl) {
-    const int cluster = short_cluster<Math>(p, sms);
+    const int cluster = short_cluster<Math>(p);
     if (cluster == 0) return launch_attn<Math>(p, maps, sms, st, pdl);
-    static std::once_flag once[64];
-    int dev = 0;
-    cudaGetDevice(&dev);
-    cudaError_t err = cudaSuccess;
-    std::call_once(once[dev & 63], [&] {
-        err = cudaFuncSetAttribute(attn_short_kernel<Math>, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(short_smem_bytes<Math>()));
-    });
-    if (err != cudaSuccess) return SPD_ERR_CUDA;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(static_cast<unsigned>(p.B * p.S * cluster));
     cfg.blockDim = dim3(Math::kWarps * 32);
@@ -45,7 +67,7 @@ static spd_status launch_scored(const Params &p, const CUtensorMap *maps, int sm
     attr[1].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr;
     cfg.numAttrs = pdl ? 2 : 1;
-    err = cudaLaunchKernelEx(&cfg, attn_short_kernel<Math>, p, maps[0], maps[1], maps[2], maps[3], cluster);
+    const cudaError_t err = cudaLaunchKernelEx(&cfg, attn_short_kernel<Math>, p, maps[0], maps[1], maps[2], maps[3], cluster);
     host::count_launch();
     if (err != cudaSuccess) fprintf(stderr, "libspd: launch of the short attention kernel: %s\n", cudaGetErrorString(err));
     return err == cudaSuccess ? SPD_OK : SPD_ERR_CUDA;
