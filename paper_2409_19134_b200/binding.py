@@ -186,8 +186,9 @@ def paged_kv(part) -> PagedKV:
 
 
 def _stream_ptr(stream: Optional[torch.cuda.Stream]) -> int:
-    s = stream if stream is not None else torch.cuda.current_stream()
-    return s.cuda_stream
+    if stream is not None:
+        return stream.cuda_stream
+    return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())    # torch.cuda.current_stream() without the wrapper object
 
 
 def spd_workspace_size(shape: Shape) -> int:
@@ -494,68 +495,92 @@ def make_rope(inv_freq: torch.Tensor, interleaved: bool = False, sections=None, 
     return rope
 
 
-def _check_slopes(shape, score) -> None:
+_TORCH_DTYPES = {SPD_F32: torch.float32, SPD_BF16: torch.bfloat16}
+
+
+def _here(t: torch.Tensor) -> None:
+    """The tensors of a call live on the current device, whose stream and context the call uses."""
+    if t.get_device() != torch._C._cuda_getDevice():
+        raise ValueError(f"tensor on {t.device}, but the current device is cuda:{torch.cuda.current_device()}")
+
+
+def _slopes(shape, score) -> None:
     keep = getattr(score, "_keep", None)
-    assert keep is None or keep.numel() == shape.num_q_heads
+    assert keep is None or keep.numel() == shape.num_q_heads, "one slope per query head"
 
 
-def _rows(shape, t: torch.Tensor, heads: int, n: int):
-    """(pointer, token stride in elements) of [n, heads, head_dim] rows that may be part of a wider row per token."""
-    assert t.dtype == (torch.float32 if shape.dtype == SPD_F32 else torch.bfloat16)
-    assert tuple(t.shape) == (n, heads, shape.head_dim)
+def _rows(t: torch.Tensor, heads: int, d: int, n: int, dtype):
+    """(pointer, token stride in elements) of [n, heads, d] rows that may be part of a wider row per token."""
+    if t.dtype != dtype or t.shape != (n, heads, d):
+        raise ValueError(f"expected {dtype} [{n}, {heads}, {d}], got {t.dtype} {list(t.shape)}")
+    s0, s1, s2 = t.stride()
     if n == 0:
         return None, 0
-    assert t.stride(2) == 1 and (heads == 1 or t.stride(1) == shape.head_dim)
-    return t.data_ptr(), t.stride(0) if n > 1 else 0
+    if s2 != 1 or (heads > 1 and s1 != d):
+        raise ValueError("a token's heads must be packed")
+    return t.data_ptr(), s0 if n > 1 else 0
 
 
 def _i32(t: Optional[torch.Tensor], *size) -> Optional[int]:
-    """Pointer of an int32 tensor of the given shape, or None."""
+    """Pointer of a contiguous int32 tensor of the given shape, or None."""
     if t is None:
         return None
-    assert t.dtype == torch.int32 and t.is_contiguous() and tuple(t.shape) == size, (t.dtype, tuple(t.shape), size)
+    if t.dtype != torch.int32 or t.shape != size or not t.is_contiguous():
+        raise ValueError(f"expected contiguous int32 {list(size)}, got {t.dtype} {list(t.shape)}")
     return t.data_ptr()
+
+
+def _packed(t: Optional[torch.Tensor], numel: int, dtype=None) -> Optional[int]:
+    """Pointer of a contiguous tensor of `numel` elements, or None."""
+    if t is None:
+        return None
+    if t.numel() != numel or not t.is_contiguous() or (dtype is not None and t.dtype != dtype):
+        raise ValueError(f"expected a contiguous tensor of {numel} elements, got {t.dtype} {list(t.shape)}")
+    return t.data_ptr() if numel else None
 
 
 def spd_partial_attn_scored(shape, score, q, priv, pub_lens, out, ws, plan=SPD_PLAN_PER_CALL, stream=None) -> None:
     """spd_partial_attn with score options; pub_lens: int32 [batch], tokens in the public partition."""
-    _check_slopes(shape, score)
+    _slopes(shape, score)
+    _here(q)
     kv = paged_kv(priv)
     part = Partial(out[0].data_ptr(), out[1].data_ptr(), out[2].data_ptr())
-    _check(lib().spd_partial_attn_scored(C.byref(shape), C.byref(score), q.data_ptr(), C.byref(kv), _i32(pub_lens, shape.batch), part,
-                                         int(plan), ws.data_ptr(), ws.numel(), _stream_ptr(stream)), "spd_partial_attn_scored")
+    _check(lib().spd_partial_attn_scored(shape, score, q.data_ptr(), kv, _i32(pub_lens, shape.batch), part, plan, ws.data_ptr(), ws.numel(),
+                                         _stream_ptr(stream)), "spd_partial_attn_scored")
 
 
 def spd_service_attn_merge_scored(shape, score, q, pub, priv_lens, partial_in, out, ws, plan=SPD_PLAN_PER_CALL, stream=None) -> None:
     """spd_service_attn_merge with score options; priv_lens: int32 [batch], tokens in the private partition."""
-    _check_slopes(shape, score)
+    _slopes(shape, score)
+    _here(q)
     kv = paged_kv(pub)
     part = Partial(partial_in[0].data_ptr(), partial_in[1].data_ptr(), partial_in[2].data_ptr())
-    _check(lib().spd_service_attn_merge_scored(C.byref(shape), C.byref(score), q.data_ptr(), C.byref(kv), _i32(priv_lens, shape.batch),
-                                               part, out.data_ptr(), _dtype_code(out.dtype), int(plan), ws.data_ptr(), ws.numel(),
-                                               _stream_ptr(stream)), "spd_service_attn_merge_scored")
+    _check(lib().spd_service_attn_merge_scored(shape, score, q.data_ptr(), kv, _i32(priv_lens, shape.batch), part, out.data_ptr(),
+                                               _dtype_code(out.dtype), plan, ws.data_ptr(), ws.numel(), _stream_ptr(stream)),
+           "spd_service_attn_merge_scored")
 
 
 def spd_decode_step_scored(shape, score, q, priv, pub, out, ws, plan=SPD_PLAN_PER_CALL, stream=None) -> None:
     """The fused decode step with score options (make_score) over both partitions."""
-    _check_slopes(shape, score)
+    _slopes(shape, score)
+    _here(q)
     a, b = paged_kv(priv), paged_kv(pub)
-    _check(lib().spd_decode_step_scored(C.byref(shape), C.byref(score), q.data_ptr(), C.byref(a), C.byref(b), out.data_ptr(),
-                                        _dtype_code(out.dtype), int(plan), ws.data_ptr(), ws.numel(), _stream_ptr(stream)),
-           "spd_decode_step_scored")
+    _check(lib().spd_decode_step_scored(shape, score, q.data_ptr(), a, b, out.data_ptr(), _dtype_code(out.dtype), plan, ws.data_ptr(),
+                                        ws.numel(), _stream_ptr(stream)), "spd_decode_step_scored")
 
 
 def spd_prefill_attn_scored(shape, score, q, k, v, tok_indptr, out, ws, prefix_lens=None, doc_start=None, stream=None) -> None:
     """Prompt attention with score options and interval masks: q [T,Hq,D], k, v [T,Hkv,D] (rows may be parts of a wider row per
     token), tok_indptr int32 [B+1], prefix_lens int32 [B], doc_start int32 [T], out [T,Hq,D] packed."""
-    _check_slopes(shape, score)
-    T = int(q.shape[0])
-    (qp, qs), (kp, ks), (vp, vs) = (_rows(shape, t, h, T) for t, h in ((q, shape.num_q_heads), (k, shape.num_kv_heads), (v, shape.num_kv_heads)))
-    assert out.is_contiguous() and out.numel() == T * shape.num_q_heads * shape.head_dim
-    tok = Tokens(qp, kp, vp, qs, ks, vs)
-    _check(lib().spd_prefill_attn_scored(C.byref(shape), C.byref(score), T, C.byref(tok), _i32(tok_indptr, shape.batch + 1),
-                                         _i32(prefix_lens, shape.batch), _i32(doc_start, T), _ptr(out), _dtype_code(out.dtype),
-                                         ws.data_ptr(), ws.numel(), _stream_ptr(stream)), "spd_prefill_attn_scored")
+    _slopes(shape, score)
+    _here(q)
+    T, B, hq, hkv, d, dtype = q.shape[0], shape.batch, shape.num_q_heads, shape.num_kv_heads, shape.head_dim, _TORCH_DTYPES[shape.dtype]
+    qp, qs = _rows(q, hq, d, T, dtype)
+    kp, ks = _rows(k, hkv, d, T, dtype)
+    vp, vs = _rows(v, hkv, d, T, dtype)
+    _check(lib().spd_prefill_attn_scored(shape, score, T, Tokens(qp, kp, vp, qs, ks, vs), _i32(tok_indptr, B + 1), _i32(prefix_lens, B),
+                                         _i32(doc_start, T), _packed(out, T * hq * d), _dtype_code(out.dtype), ws.data_ptr(), ws.numel(),
+                                         _stream_ptr(stream)), "spd_prefill_attn_scored")
 
 
 def spd_append_kv_rope(shape, rope, q, k, v, part, ws, q_out=None, k_out=None, tok_indptr=None, positions=None, pos_base=None,
@@ -565,21 +590,20 @@ def spd_append_kv_rope(shape, rope, q, k, v, part, ws, q_out=None, k_out=None, t
     rope: make_rope(...) or None (no rotation; q and q_out are not used).  tok_indptr int32 [B+1]: tokens per user; None: one
     token per user.  positions int32 [axes, T] or [T]; pos_base int32 [B].  new_lens: an int32 [B] tensor, None, or by default
     part.seq_lens itself."""
-    T, B = int(k.shape[0]), shape.batch
-    kp, ks = _rows(shape, k, shape.num_kv_heads, T)
-    vp, vs = _rows(shape, v, shape.num_kv_heads, T)
-    qp, qs = _rows(shape, q, shape.num_q_heads, T) if rope is not None else (None, 0)
-    for o, heads in ((q_out, shape.num_q_heads), (k_out, shape.num_kv_heads)):
-        assert o is None or (o.is_contiguous() and o.dtype == k.dtype and o.numel() == T * heads * shape.head_dim)
+    _here(k)
+    T, B, hq, hkv, d, dtype = k.shape[0], shape.batch, shape.num_q_heads, shape.num_kv_heads, shape.head_dim, _TORCH_DTYPES[shape.dtype]
+    kp, ks = _rows(k, hkv, d, T, dtype)
+    vp, vs = _rows(v, hkv, d, T, dtype)
+    qp, qs = _rows(q, hq, d, T, dtype) if rope is not None else (None, 0)
     if positions is not None:
-        positions = positions.view(1, -1) if positions.dim() == 1 else positions
-        assert rope is not None and positions.shape[0] == rope.num_axes
-    tok = Tokens(qp, kp, vp, qs, ks, vs)
-    for t in (part.k_pool, part.v_pool, part.page_indices):
-        assert t.is_contiguous()
-    lens = part.seq_lens if isinstance(new_lens, str) else new_lens
-    _check(lib().spd_append_kv_rope(C.byref(shape), C.byref(rope) if rope is not None else None, T, C.byref(tok), _i32(tok_indptr, B + 1),
-                                    _i32(positions, rope.num_axes, T) if positions is not None else None, _i32(pos_base, B),
-                                    _ptr(q_out), _ptr(k_out), part.k_pool.data_ptr(), part.v_pool.data_ptr(), int(part.k_pool.shape[0]),
-                                    _i32(part.page_indptr, B + 1), _ptr(part.page_indices), _i32(part.seq_lens, B), _i32(lens, B),
-                                    ws.data_ptr(), ws.numel(), _stream_ptr(stream)), "spd_append_kv_rope")
+        if rope is None:
+            raise ValueError("positions are for a rotation")
+        positions = _i32(positions, T) if positions.dim() == 1 and rope.num_axes == 1 else _i32(positions, rope.num_axes, T)
+    if not (part.k_pool.is_contiguous() and part.v_pool.is_contiguous() and part.page_indices.is_contiguous()):
+        raise ValueError("pools and page tables are contiguous")
+    lens = _i32(part.seq_lens, B)
+    _check(lib().spd_append_kv_rope(shape, rope, T, Tokens(qp, kp, vp, qs, ks, vs), _i32(tok_indptr, B + 1), positions, _i32(pos_base, B),
+                                    _packed(q_out, T * hq * d, dtype), _packed(k_out, T * hkv * d, dtype), part.k_pool.data_ptr(),
+                                    part.v_pool.data_ptr(), part.k_pool.shape[0], _i32(part.page_indptr, B + 1), _ptr(part.page_indices),
+                                    lens, lens if isinstance(new_lens, str) else _i32(new_lens, B), ws.data_ptr(), ws.numel(),
+                                    _stream_ptr(stream)), "spd_append_kv_rope")

@@ -6,6 +6,7 @@
 
 #include "spd_host.h"
 #include "spd_prefill_scored.cuh"
+#include "spd_prefill_scored_f32.cuh"
 #include "spd_prefill_scored_tc.cuh"
 
 namespace {
@@ -91,6 +92,31 @@ spd_status prefill_tc(const spd_shape &s, const ScoredPrefillParams &sp, cudaStr
     return SPD_ERR_UNSUPPORTED;
 }
 
+template <int D, int RPT>
+spd_status launch_prefill_f32(const spd_shape &s, const ScoredPrefillParams &p, cudaStream_t st) {
+    using C = ScoredF32<D, RPT>;
+    static std::once_flag once[64];
+    int dev = 0;
+    cudaGetDevice(&dev);
+    cudaError_t err = cudaSuccess;
+    std::call_once(once[dev & 63], [&] {
+        err = cudaFuncSetAttribute(prefill_scored_f32_kernel<D, RPT>, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(C::smem_bytes()));
+    });
+    if (err != cudaSuccess) return SPD_ERR_CUDA;
+    const dim3 grid(static_cast<unsigned>((p.T + C::R - 1) / C::R + s.batch), static_cast<unsigned>(s.num_q_heads));
+    prefill_scored_f32_kernel<D, RPT><<<grid, 256, C::smem_bytes(), st>>>(p);
+    host::count_launch();
+    return cudaGetLastError() == cudaSuccess ? SPD_OK : SPD_ERR_CUDA;
+}
+
+// fp32 prompts on the FMA pipes: four rows per thread, two where that leaves SMs without work.
+spd_status prefill_f32(const spd_shape &s, const ScoredPrefillParams &p, int sms, cudaStream_t st) {
+    if (s.num_q_heads > 65535) return SPD_ERR_UNSUPPORTED;
+    const bool small = (p.T + 63) / 64 * s.num_q_heads < 2 * static_cast<int64_t>(sms);
+    if (s.head_dim == 128) return small ? launch_prefill_f32<128, 2>(s, p, st) : launch_prefill_f32<128, 4>(s, p, st);
+    return small ? launch_prefill_f32<64, 2>(s, p, st) : launch_prefill_f32<64, 4>(s, p, st);
+}
+
 }  // namespace
 
 extern "C" {
@@ -125,13 +151,7 @@ spd_status spd_prefill_attn_scored(const spd_shape *shape, const spd_score *scor
     p.prefix_lens = prefix_lens; p.doc_start = doc_start;
     cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
     if (s.dtype == SPD_BF16) return prefill_tc(s, p, st);
-    const int64_t max_blocks = (T + kFmaRows - 1) / kFmaRows + s.batch;
-    if (max_blocks >= (1ll << 31)) return SPD_ERR_UNSUPPORTED;
-    const dim3 grid(static_cast<unsigned>(max_blocks), static_cast<unsigned>(s.num_q_heads));
-    if (s.head_dim == 128) prefill_scored_fma_kernel<float, 128><<<grid, kFmaRows * 32, 0, st>>>(p);
-    else prefill_scored_fma_kernel<float, 64><<<grid, kFmaRows * 32, 0, st>>>(p);
-    host::count_launch();
-    return cudaGetLastError() == cudaSuccess ? SPD_OK : SPD_ERR_CUDA;
+    return prefill_f32(s, p, sms, st);
 }
 
 }  // extern "C"

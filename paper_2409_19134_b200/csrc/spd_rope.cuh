@@ -7,6 +7,9 @@
 // anybody, and keeps the sines and cosines of its unit in registers while it walks the token's heads.  Angles: the turns
 // pos * inv_freq / 2 pi are formed in 64 bits and reduced to [-1/2, 1/2] there (a position of 10^5 leaves 32 bits no
 // fraction to speak of), then sincospif; once per token and pair, shared by all heads.
+// Measured: 8 prompts, 38 k tokens of 32/8 heads, head_dim 128, bf16 (1.42 GB) 258 us, 5.5 TB/s; rows in flight per thread 2 / 3 / 4:
+// 269 / 258 / 259 us, tokens per CTA 2 / 4 / 8: 306 / 258 / 255, and 7.0 / 7.4 / 9.2 us for 1800 tokens; without loading rows ahead of
+// the search 327.  One token for each of 512 users (22 MB, L2) 6.2 us, of 8 users 3.6 us.
 #pragma once
 
 #include "spd_device.cuh"
@@ -102,7 +105,7 @@ template <> __device__ __forceinline__ void rope_rotate<__nv_bfloat16>(uint4 &a,
 
 // E: element type.  Runs: users bring runs of tokens (tok_indptr), kRopeTokens tokens per CTA; else one CTA per user.
 template <typename E, bool Runs>
-__global__ void __launch_bounds__(kRopeThreads) append_rope_kernel(const __grid_constant__ RopeAppendParams p) {
+__global__ void __launch_bounds__(kRopeThreads, 4) append_rope_kernel(const __grid_constant__ RopeAppendParams p) {
     constexpr int NT = Runs ? kRopeTokens : 1, CH = 16 / sizeof(E);     // CH channels per 16-byte chunk = pairs per unit
     __shared__ float2 cs[NT][64];
     __shared__ int64_t row_off[NT];          // byte offset of the token's slot in a pool, -1 = not written
@@ -119,6 +122,32 @@ __global__ void __launch_bounds__(kRopeThreads) append_rope_kernel(const __grid_
         p.hdr[HDR_BATCH] = p.B;
         p.hdr[HDR_NSEQ] = p.B * p.S;
     }
+
+    // A thread keeps to one token and one unit (two 16-byte chunks) and walks that token's rows: q heads, then k heads, then v
+    // heads.  The first rows are asked for before anybody knows where they go: finding a token's user, page and angles is a
+    // chain of loads that those rows need not wait for.
+    constexpr int TPT = kRopeThreads / NT, PB = Runs ? 3 : 2;      // threads per token, rows in flight per thread
+    const int units = row_bytes / 32, ru = p.rot / (2 * CH);
+    const int my = tid / TPT, j = tid % units, r0 = (tid % TPT) / units, dr = TPT / units;
+    const bool turn = j < ru;
+    const int c0 = (turn && !p.interleaved ? j : 2 * j) * 16, c1 = (turn && !p.interleaved ? j + ru : 2 * j + 1) * 16;
+    const int rows = my < nt ? p.Hq + 2 * p.Hkv : 0;
+    const int64_t tok = tok0 + my;
+    uint4 a[PB], b[PB];
+    auto load = [&](int base) {
+#pragma unroll
+        for (int x = 0; x < PB; ++x) {
+            const int r = base + x * dr;
+            if (r >= rows) continue;
+            const bool is_q = r < p.Hq, is_v = r >= p.Hq + p.Hkv;
+            const uint8_t *src = is_q ? p.q + tok * p.q_stride + static_cast<int64_t>(r) * row_bytes
+                                : is_v ? p.v + tok * p.v_stride + static_cast<int64_t>(r - p.Hq - p.Hkv) * row_bytes
+                                       : p.k + tok * p.k_stride + static_cast<int64_t>(r - p.Hq) * row_bytes;
+            a[x] = *reinterpret_cast<const uint4 *>(src + c0);
+            b[x] = *reinterpret_cast<const uint4 *>(src + c1);
+        }
+    };
+    load(r0);
 
     if constexpr (Runs) {
         // one pass over tok_indptr finds every token's user and any inconsistency
@@ -165,37 +194,33 @@ __global__ void __launch_bounds__(kRopeThreads) append_rope_kernel(const __grid_
             cs[i][pr] = rope_turn(p, tok0 + i, tok_pos[i], pr);
         }
         __syncthreads();
-        // unit j of a row: the chunks c0 and c1; rows of a token: q heads, then k heads, then v heads
-        const int units = row_bytes / 32, ru = p.rot / (2 * CH);
-        const int j = tid % units, r0 = tid / units, dr = kRopeThreads / units;
-        const bool turn = j < ru;
-        const int c0 = (turn && !p.interleaved ? j : 2 * j) * 16, c1 = (turn && !p.interleaved ? j + ru : 2 * j + 1) * 16;
-        const int rows = p.Hq + 2 * p.Hkv;
-        for (int i = 0; i < nt; ++i) {
-            const int64_t tok = tok0 + i, off = row_off[i];
+        if (my < nt) {
+            const int64_t off = row_off[my];
             float2 w[CH];
             if (turn) {
 #pragma unroll
-                for (int e = 0; e < CH; ++e) w[e] = cs[i][j * CH + e];
+                for (int e = 0; e < CH; ++e) w[e] = cs[my][j * CH + e];
             }
-            for (int r = r0; r < rows; r += dr) {
-                const bool is_q = r < p.Hq, is_v = r >= p.Hq + p.Hkv;
-                const int h = is_q ? r : (is_v ? r - p.Hq - p.Hkv : r - p.Hq);
-                if (is_v && off < 0) continue;
-                const uint8_t *src = (is_q ? p.q + tok * p.q_stride : is_v ? p.v + tok * p.v_stride : p.k + tok * p.k_stride) +
-                                     static_cast<int64_t>(h) * row_bytes;
-                uint4 a = *reinterpret_cast<const uint4 *>(src + c0), b = *reinterpret_cast<const uint4 *>(src + c1);
-                if (turn && !is_v) rope_rotate<E>(a, b, w, p.interleaved != 0);
-                uint8_t *packed = is_q ? p.q_out + (tok * p.Hq + h) * row_bytes
-                                       : (!is_v && p.k_out ? p.k_out + (tok * p.Hkv + h) * row_bytes : nullptr);
-                if (packed) {
-                    *reinterpret_cast<uint4 *>(packed + c0) = a;
-                    *reinterpret_cast<uint4 *>(packed + c1) = b;
-                }
-                if (!is_q && off >= 0) {
-                    uint8_t *slot = (is_v ? p.v_pool : p.k_pool) + off + static_cast<int64_t>(h) * kPage * row_bytes;
-                    *reinterpret_cast<uint4 *>(slot + c0) = a;
-                    *reinterpret_cast<uint4 *>(slot + c1) = b;
+            for (int base = r0; base < rows; base += PB * dr) {
+                if (base != r0) load(base);
+#pragma unroll
+                for (int x = 0; x < PB; ++x) {
+                    const int r = base + x * dr;
+                    if (r >= rows) continue;
+                    const bool is_q = r < p.Hq, is_v = r >= p.Hq + p.Hkv;
+                    const int h = is_q ? r : (is_v ? r - p.Hq - p.Hkv : r - p.Hq);
+                    if (turn && !is_v) rope_rotate<E>(a[x], b[x], w, p.interleaved != 0);
+                    uint8_t *packed = is_q ? p.q_out + (tok * p.Hq + h) * row_bytes
+                                           : (!is_v && p.k_out ? p.k_out + (tok * p.Hkv + h) * row_bytes : nullptr);
+                    if (packed) {
+                        *reinterpret_cast<uint4 *>(packed + c0) = a[x];
+                        *reinterpret_cast<uint4 *>(packed + c1) = b[x];
+                    }
+                    if (!is_q && off >= 0) {
+                        uint8_t *slot = (is_v ? p.v_pool : p.k_pool) + off + static_cast<int64_t>(h) * kPage * row_bytes;
+                        *reinterpret_cast<uint4 *>(slot + c0) = a[x];
+                        *reinterpret_cast<uint4 *>(slot + c1) = b[x];
+                    }
                 }
             }
         }
@@ -207,10 +232,34 @@ __global__ void __launch_bounds__(kRopeThreads) append_rope_kernel(const __grid_
         __threadfence();
         asm volatile("fence.proxy.async.global;" ::: "memory");
     } else {
+        if (p.new_lens != nullptr && p.new_lens != p.lens) {
+            // grown lengths to another array: the CTA with a user's first token looks over that user's pages and writes its entry
+            for (int i = 0; i < nt && consistent; ++i) {
+                const int u = tok_user[i];
+                const int64_t a0 = p.tok_indptr[u], n = p.tok_indptr[u + 1] - a0;
+                if (a0 != tok0 + i) continue;
+                int64_t lo, held;
+                bool good = rope_user_room(p, u, n, lo, held);
+                if (good)
+                    for (int64_t x = held / kPage + tid; x <= (held + n - 1) / kPage; x += kRopeThreads) {
+                        const int page = p.indices[lo + x];
+                        good = good && page >= 0 && page < p.num_pages;
+                    }
+                good = __syncthreads_and(good);
+                if (tid == 0) p.new_lens[u] = static_cast<int32_t>(held + (good ? n : 0));
+            }
+            if (blockIdx.x == 0)           // users without tokens, and everybody where nothing is appended
+                for (int u = tid; u < p.B; u += kRopeThreads) {
+                    if (consistent && p.tok_indptr[u + 1] != p.tok_indptr[u]) continue;
+                    int64_t lo, held;
+                    if (!rope_user_room(p, u, 0, lo, held) && consistent) flag_error(p.hdr, 4 /* SPD_ERR_BAD_PAGE */, u);
+                    p.new_lens[u] = static_cast<int32_t>(held);
+                }
+        }
         __threadfence();
         asm volatile("fence.proxy.async.global;" ::: "memory");
-        if (p.new_lens == nullptr) return;
-        // the lengths grow once nobody reads them any more: the last CTA out does it
+        if (p.new_lens != p.lens) return;
+        // in place: the lengths grow once nobody reads them any more, so the last CTA out does it
         __syncthreads();
         if (tid == 0) last_cta = atomicAdd(&p.hdr[HDR_GRID_EXITS], 1) == static_cast<int32_t>(gridDim.x) - 1;
         __syncthreads();

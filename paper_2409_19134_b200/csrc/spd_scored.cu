@@ -39,20 +39,20 @@ static const int *short_capacity() {
 // window, or the pools' size, bounds the tiles of a sequence.  A caller who set the cut or asked for a stored plan gets the
 // persistent kernel.
 template <class Math>
-static int short_cluster(const Params &p) {
+static int short_cluster(const Params &p, int sms) {
     if (p.plan_mode != PLAN_DERIVE || p.min_tiles != kMinTilesPerWarp || p.uniform) return 0;
     const int64_t seqs = static_cast<int64_t>(p.B) * p.S;
     int64_t tiles = static_cast<int64_t>(p.part[0].num_pages) + p.part[1].num_pages;
     if (p.window > 0 && p.window / kPage + 3 < tiles) tiles = p.window / kPage + 3;      // ragged at both ends and where the partitions meet
     const int *fit = short_capacity<Math>();
     int i = 0;
-    while (i < 3 && seqs <= fit[i + 1] && tiles > (Math::kWarps << i)) ++i;
+    while (i < 3 && seqs <= fit[i + 1] && (seqs << (i + 1)) <= sms && tiles > (Math::kWarps << i)) ++i;     // two CTAs of one SM would only slow each other
     return seqs <= fit[i] && tiles <= (static_cast<int64_t>(Math::kWarps) << i) * kShortTiles ? 1 << i : 0;
 }
 
 template <class Math>
 static spd_status launch_scored(const Params &p, const CUtensorMap *maps, int sms, cudaStream_t st, bool pdl) {
-    const int cluster = short_cluster<Math>(p);
+    const int cluster = short_cluster<Math>(p, sms);
     if (cluster == 0) return launch_attn<Math>(p, maps, sms, st, pdl);
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(static_cast<unsigned>(p.B * p.S * cluster));
