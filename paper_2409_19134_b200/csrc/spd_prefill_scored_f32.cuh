@@ -20,7 +20,7 @@ struct ScoredF32 {
 };
 
 template <int D, int RPT>
-__global__ void __launch_bounds__(256) prefill_scored_f32_kernel(const __grid_constant__ ScoredPrefillParams p) {
+__global__ void __launch_bounds__(256, 2) prefill_scored_f32_kernel(const __grid_constant__ ScoredPrefillParams p) {
     using C = ScoredF32<D, RPT>;
     constexpr int R = C::R, KB = C::KB, KPT = C::KPT, CPT = C::CPT, QP = C::QP, PP = C::PP, LD = KB * D / 4 / 256;   // float4 loads per thread and tile
     extern __shared__ __align__(16) float sm[];
