@@ -26,6 +26,8 @@ enum HdrWord {
     HDR_SM_LAUNCHES = 4,   // attention launches that compared their CTAs' SMs with the previous launch's
     HDR_SM_MOVES = 5,      // CTAs of those launches that found themselves on another SM than last time
     HDR_GRID_EXITS = 6,    // CTAs of the running launch that have finished (only counted by launches that append); zero between calls
+    HDR_NEXT_ITEM = 8,     // scored prompt attention: items handed out so far; zero between calls
+    HDR_ITEM_EXITS = 9,    // ... and CTAs that found no more; zero between calls
     HDR_WORDS = 64
 };
 

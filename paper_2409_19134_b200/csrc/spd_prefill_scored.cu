@@ -15,22 +15,24 @@ using namespace spd;
 using host::misaligned;
 using host::row_stride;
 
-// [T][heads][head_dim] bf16 with a token stride, as a 3-D tensor map; one box = `rows` tokens x 64 channels of one head, 128-byte swizzle.
-spd_status make_token_map(CUtensorMap *map, const void *ptr, int64_t T, int heads, int D, int64_t stride, int rows) {
+// [T][heads][head_dim] bf16 (the output may be fp32) with a token stride, as a 3-D tensor map; one box = `rows` tokens x 128 bytes of
+// one head, 128-byte swizzle.
+spd_status make_token_map(CUtensorMap *map, const void *ptr, int64_t T, int heads, int D, int64_t stride, int rows, bool f32 = false) {
     EncodeTiledFn fn = host::tensor_map_encoder();
     if (!fn) return SPD_ERR_CUDA;
     cuuint64_t dims[3] = {static_cast<cuuint64_t>(D), static_cast<cuuint64_t>(heads), static_cast<cuuint64_t>(T)};
-    cuuint64_t strides[2] = {static_cast<cuuint64_t>(D) * 2, static_cast<cuuint64_t>(stride) * 2};
-    cuuint32_t box[3] = {64, 1, static_cast<cuuint32_t>(rows)};
+    const cuuint64_t es = f32 ? 4 : 2;
+    cuuint64_t strides[2] = {static_cast<cuuint64_t>(D) * es, static_cast<cuuint64_t>(stride) * es};
+    cuuint32_t box[3] = {f32 ? 32u : 64u, 1, static_cast<cuuint32_t>(rows)};
     cuuint32_t estr[3] = {1, 1, 1};
-    const CUresult r = fn(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void *>(ptr), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+    const CUresult r = fn(map, f32 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void *>(ptr), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
                           CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
     if (r != CUDA_SUCCESS) fprintf(stderr, "libspd: cuTensorMapEncodeTiled failed with CUresult %d\n", static_cast<int>(r));
     return r == CUDA_SUCCESS ? SPD_OK : SPD_ERR_CUDA;
 }
 
 template <int D, int CAP, bool BIAS>
-spd_status launch_prefill_tc(const ScoredTcParams &p, const CUtensorMap &mq, const CUtensorMap &mk, const CUtensorMap &mv, unsigned grid, cudaStream_t st) {
+spd_status launch_prefill_tc(const ScoredTcParams &p, const CUtensorMap &mq, const CUtensorMap &mk, const CUtensorMap &mv, const CUtensorMap &mo, unsigned grid, cudaStream_t st) {
     static std::once_flag once[64];
     int dev = 0;
     cudaGetDevice(&dev);
@@ -39,7 +41,7 @@ spd_status launch_prefill_tc(const ScoredTcParams &p, const CUtensorMap &mq, con
         err = cudaFuncSetAttribute(prefill_scored_tc_kernel<D, CAP, BIAS>, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(st_smem_bytes(D)));
     });
     if (err != cudaSuccess) return SPD_ERR_CUDA;
-    prefill_scored_tc_kernel<D, CAP, BIAS><<<grid, kStThreads, st_smem_bytes(D), st>>>(p, mq, mk, mv);
+    prefill_scored_tc_kernel<D, CAP, BIAS><<<grid, kStThreads, st_smem_bytes(D), st>>>(p, mq, mk, mv, mo);
     host::count_launch();
     return cudaGetLastError() == cudaSuccess ? SPD_OK : SPD_ERR_CUDA;
 }
@@ -72,11 +74,13 @@ spd_status prefill_tc(const spd_shape &s, const ScoredPrefillParams &sp, cudaStr
         }
         if (fits) { p.half_at = 0.5f; p.one_at = 1.f; }
     }
-    CUtensorMap mq, mk, mv;
+    CUtensorMap mq, mk, mv, mo;
     spd_status rc;
     if ((rc = make_token_map(&mq, sp.q, sp.T, s.num_q_heads, s.head_dim, sp.q_stride, 128)) != SPD_OK) return rc;
     if ((rc = make_token_map(&mk, sp.k, sp.T, s.num_kv_heads, s.head_dim, sp.k_stride, kStKeys)) != SPD_OK) return rc;
     if ((rc = make_token_map(&mv, sp.v, sp.T, s.num_kv_heads, s.head_dim, sp.v_stride, kStKeys)) != SPD_OK) return rc;
+    if ((rc = make_token_map(&mo, sp.out, sp.T, s.num_q_heads, s.head_dim, static_cast<int64_t>(s.num_q_heads) * s.head_dim, 32, !sp.out_bf16)) != SPD_OK)
+        return rc;
     const int rows = p.heads_per_cta == 2 ? 128 : 256;
     // at most one CTA per SM; fewer where there are not that many items
     const int64_t items = ((sp.T + rows - 1) / rows + s.batch) * (s.num_q_heads / p.heads_per_cta);
@@ -85,7 +89,7 @@ spd_status prefill_tc(const spd_shape &s, const ScoredPrefillParams &sp, cudaStr
     const unsigned grid = static_cast<unsigned>(items < sms ? items : sms);
     const bool bias = sp.slopes != nullptr;
     const int cap = sp.cap == 0.f ? 0 : (sp.cap <= kStFixedCap && !bias) ? 1 : 2;
-#define SPD_TC_CASE(DD, CC, BB) if (s.head_dim == DD && cap == CC && bias == BB) return launch_prefill_tc<DD, CC, BB>(p, mq, mk, mv, grid, st);
+#define SPD_TC_CASE(DD, CC, BB) if (s.head_dim == DD && cap == CC && bias == BB) return launch_prefill_tc<DD, CC, BB>(p, mq, mk, mv, mo, grid, st);
     SPD_TC_CASE(128, 0, false) SPD_TC_CASE(128, 1, false) SPD_TC_CASE(128, 2, false) SPD_TC_CASE(128, 0, true) SPD_TC_CASE(128, 2, true)
     SPD_TC_CASE(64, 0, false) SPD_TC_CASE(64, 1, false) SPD_TC_CASE(64, 2, false) SPD_TC_CASE(64, 0, true) SPD_TC_CASE(64, 2, true)
 #undef SPD_TC_CASE

@@ -3,7 +3,7 @@
 // One CTA per SM works through a list of items, each two 128-row query tiles over shared K/V blocks of 80 keys: two query
 // heads of one KV head over the same rows where the group is even (both tiles then need the same keys, and a short prompt
 // still fills two tiles), else two consecutive row blocks of one head.  Items are numbered heaviest first within a prompt and
-// dealt out to and fro; a planning warp works out the next item while this one runs, and its Q, K and V are on the way before
+// drawn from a counter; a planning warp works out the next item while this one runs, and its Q, K and V are on the way before
 // this one's output is written (a CTA per item spent 8 to 10 us starting and ending).  Per tile t:
 //     S_t = Q_t K^T        128 x 80 x D, fp32 in TMEM
 //     softmax              one row per thread: S_t into registers (S_t is free again at once), score options, mask,
@@ -53,7 +53,7 @@ struct StPlan {
     int32_t ja[2], jb[2];           // blocks that a tile works on, [ja, jb) in that order
     int32_t fulllo, fullhi;         // keys that every row sees
     int32_t poisoned;               // a V row that is not finite is hidden from some rows and visible to others
-    int32_t pad;
+    int32_t ahead;                  // some row sees keys ahead of it (a prefix)
     StBlockStats stats[8];          // per softmax warp
     int2 span[256];                 // [tile][row]: first and last key the row sees
 };
@@ -128,6 +128,16 @@ __device__ __forceinline__ float fmax3_abs(float a, float b, float c) {
     return r;
 }
 
+// One box from shared memory to the output (every row of it belongs to the prompt), and the waits for such stores: until the
+// staging area has been read, and until they are done.
+__device__ __forceinline__ void tma_store_3d(const CUtensorMap *map, uint32_t src, int x, int y, int z) {
+    asm volatile("cp.async.bulk.tensor.3d.global.shared::cta.bulk_group [%0, {%2, %3, %4}], [%1];"
+                 ::"l"(reinterpret_cast<uint64_t>(map)), "r"(src), "r"(x), "r"(y), "r"(z) : "memory");
+    asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+}
+__device__ __forceinline__ void tma_store_wait_read() { asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory"); }
+__device__ __forceinline__ void tma_store_wait() { asm volatile("cp.async.bulk.wait_group 0;" ::: "memory"); }
+
 // The MMAs and the commit of a converged warp, issued by its elected lane (always the same one, so their order holds).
 __device__ __forceinline__ void st_mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
     asm volatile("{\n\t.reg .pred p, e;\n\telect.sync _|e, 0xffffffff;\n\tsetp.ne.b32 p, %4, 0;\n\t"
@@ -188,7 +198,8 @@ __device__ __noinline__ void st_slow_row(const ScoredTcParams &p, int64_t first,
 template <int D, int CAP, bool BIAS>
 __global__ void __launch_bounds__(kStThreads, 1)
 prefill_scored_tc_kernel(const __grid_constant__ ScoredTcParams p, const __grid_constant__ CUtensorMap mq,
-                         const __grid_constant__ CUtensorMap mk, const __grid_constant__ CUtensorMap mv) {
+                         const __grid_constant__ CUtensorMap mk, const __grid_constant__ CUtensorMap mv,
+                         const __grid_constant__ CUtensorMap mo) {
     constexpr int QTILE = st_qtile(D), TILE = st_tile(D), NS = st_slots(D), BOXES = D / 64, KB = kStKeys;
     extern __shared__ __align__(1024) uint8_t base[];
     const uint32_t Qs = smem_u32(base), Ks = Qs + 2 * QTILE, Vs = Ks + NS * TILE;
@@ -211,7 +222,7 @@ prefill_scored_tc_kernel(const __grid_constant__ ScoredTcParams p, const __grid_
 
     if (blockIdx.x == 0) scored_check_offsets(p.s);
     if (tid == 320) {
-        prefetch_tensormap(&mq); prefetch_tensormap(&mk); prefetch_tensormap(&mv);
+        prefetch_tensormap(&mq); prefetch_tensormap(&mk); prefetch_tensormap(&mv); prefetch_tensormap(&mo);
         for (int b = 0; b < NBARS; ++b) {
             // Q and ring slots free: one per tile; S in registers, P written: one per softmax warp of the tile; plan read: one per warp
             const int n = b == 1 || (b >= 14 + 2 * NS && b < 14 + 4 * NS) ? 2 : (b >= 4 && b < 8) ? 4 : (b >= 12 && b < 14) ? kStConsumers : 1;
@@ -255,7 +266,7 @@ prefill_scored_tc_kernel(const __grid_constant__ ScoredTcParams p, const __grid_
             const int lo = sp.x, hi = sp.y, kend = pl.kend, my_a = t ? pl.ja[1] : pl.ja[0], my_b = t ? pl.jb[1] : pl.jb[0];
             const int h = hpc == 2 ? pl.h0 + t : pl.h0, len = pl.len, trow0 = pl.row0 + (hpc == 2 ? 0 : 128 * t), qrow = trow0 + row;
             const int64_t first = pl.first;
-            const bool have = t < pl.tiles;
+            const bool have = t < pl.tiles, ahead = pl.ahead != 0;
             float l = 0.f, m = -INFINITY;                  // m: reference point in log2 units of the score
             int form = 1;                                  // the cap's form that would have served the block before
             // The bias without the row's own constant: with the scores of a block taken relative to -slope (row - kb), kb its first
@@ -347,7 +358,7 @@ prefill_scored_tc_kernel(const __grid_constant__ ScoredTcParams p, const __grid_
                 }
                 if constexpr (BIAS) {
                     const float scale = CAP ? 1.f : p.c2;
-                    if (kb + KB - 1 <= trow0) {                       // the block lies behind all of the tile's rows
+                    if (kb + KB - 1 <= trow0 || !ahead) {             // no key ahead of its row, but hidden ones
                         const uint64_t sc2 = pack_f32x2(scale, scale);
 #pragma unroll
                         for (int x = 0; x < KB; x += 4) {
@@ -461,57 +472,64 @@ prefill_scored_tc_kernel(const __grid_constant__ ScoredTcParams p, const __grid_
                     if (rr < len) st_slow_row<D>(p, first, rr, h, s2.x, s2.y, lane);
                 }
             } else if (ok && have) {
-                // ---- normalise this thread's row, 32 channels at a time, through the warp's own staging area (16-byte chunks
-                //      XOR-swizzled by the row against bank conflicts), and store whole lines; rows past the prompt's end are not
-                //      stored.  A row that saw nothing (l = 0) gives zeros.
+                // ---- normalise this thread's row, 128 bytes of output at a time, into the warp's staging area (128-byte rows, 16-byte
+                //      chunks XOR-swizzled by the row, as the tensor map wants it and free of bank conflicts); a warp whose 32 rows
+                //      all belong to the prompt stores the box by TMA, another one row by row.  (Stores by the threads took 2500
+                //      of 3900 cycles here.)  A row that saw nothing (l = 0) gives zeros.
                 const float inv = l == 0.f ? 0.f : 1.f / l;
                 uint8_t *stage = stage_all + wid * kStStage;
                 const int rows_live = len - trow0 - (wid & 3) * 32;             // rows of this warp that belong to the prompt
                 const int64_t tok0 = first + trow0 + (wid & 3) * 32;
-                uint8_t *dst = reinterpret_cast<uint8_t *>(p.s.out);
                 const bool b16 = p.s.out_bf16 != 0;
+                const int width = b16 ? 64 : 32;                                 // channels in 128 bytes
 #pragma unroll 1
-                for (int c = 0; c < D / 32; ++c) {
+                for (int c = 0; c < D && rows_live > 0; c += width) {
+                    if (lane == 0) tma_store_wait_read();                        // the box before has left the staging area
+                    __syncwarp();
+                    uint8_t *mine = stage + lane * 128;
                     float ov[32];
-                    tmem_ld32(t_o + c * 32, ov);
+                    tmem_ld32(t_o + c, ov);
 #pragma unroll
                     for (int x = 0; x < 32; ++x) ov[x] = inv == 0.f ? 0.f : ov[x] * inv;
                     if (b16) {
 #pragma unroll
                         for (int q4 = 0; q4 < 4; ++q4)
-                            *reinterpret_cast<uint4 *>(stage + lane * 64 + ((q4 ^ ((lane >> 1) & 3)) << 4)) =
+                            *reinterpret_cast<uint4 *>(mine + ((q4 ^ (lane & 7)) << 4)) =
+                                make_uint4(pack_bf16(ov[8 * q4], ov[8 * q4 + 1]), pack_bf16(ov[8 * q4 + 2], ov[8 * q4 + 3]),
+                                           pack_bf16(ov[8 * q4 + 4], ov[8 * q4 + 5]), pack_bf16(ov[8 * q4 + 6], ov[8 * q4 + 7]));
+                        tmem_ld32(t_o + c + 32, ov);
+#pragma unroll
+                        for (int x = 0; x < 32; ++x) ov[x] = inv == 0.f ? 0.f : ov[x] * inv;
+#pragma unroll
+                        for (int q4 = 0; q4 < 4; ++q4)
+                            *reinterpret_cast<uint4 *>(mine + (((q4 + 4) ^ (lane & 7)) << 4)) =
                                 make_uint4(pack_bf16(ov[8 * q4], ov[8 * q4 + 1]), pack_bf16(ov[8 * q4 + 2], ov[8 * q4 + 3]),
                                            pack_bf16(ov[8 * q4 + 4], ov[8 * q4 + 5]), pack_bf16(ov[8 * q4 + 6], ov[8 * q4 + 7]));
                     } else {
 #pragma unroll
                         for (int q4 = 0; q4 < 8; ++q4)
-                            *reinterpret_cast<float4 *>(stage + lane * 128 + ((q4 ^ (lane & 7)) << 4)) =
+                            *reinterpret_cast<float4 *>(mine + ((q4 ^ (lane & 7)) << 4)) =
                                 make_float4(ov[4 * q4], ov[4 * q4 + 1], ov[4 * q4 + 2], ov[4 * q4 + 3]);
                     }
-                    __syncwarp();
-                    if (b16) {
-#pragma unroll
-                        for (int x = 0; x < 4; ++x) {        // 8 rows of 64 bytes each
-                            const int rr = 8 * x + (lane >> 2), ch = lane & 3;
-                            if (rr < rows_live)
-                                *reinterpret_cast<uint4 *>(dst + (((tok0 + rr) * p.s.Hq + h) * D + c * 32) * 2 + ch * 16) =
-                                    *reinterpret_cast<const uint4 *>(stage + rr * 64 + ((ch ^ ((rr >> 1) & 3)) << 4));
-                        }
+                    if (rows_live >= 32) {
+                        fence_proxy_async();
+                        __syncwarp();
+                        if (lane == 0) tma_store_3d(&mo, smem_u32(stage), c, h, static_cast<int>(tok0));
                     } else {
-#pragma unroll
-                        for (int x = 0; x < 8; ++x) {        // 4 rows of 128 bytes each
-                            const int rr = 4 * x + (lane >> 3), ch = lane & 7;
-                            if (rr < rows_live)
-                                *reinterpret_cast<uint4 *>(dst + (((tok0 + rr) * p.s.Hq + h) * D + c * 32) * 4 + ch * 16) =
-                                    *reinterpret_cast<const uint4 *>(stage + rr * 128 + ((ch ^ (rr & 7)) << 4));
-                        }
+                        __syncwarp();
+                        uint8_t *dst = reinterpret_cast<uint8_t *>(p.s.out);
+                        const int es = b16 ? 2 : 4;
+                        for (int x = lane; x < rows_live * 8; x += 32)
+                            *reinterpret_cast<uint4 *>(dst + (((tok0 + (x >> 3)) * p.s.Hq + h) * D + c) * es + (x & 7) * 16) =
+                                *reinterpret_cast<const uint4 *>(stage + (x >> 3) * 128 + (((x & 7) ^ ((x >> 3) & 7)) << 4));
+                        __syncwarp();
                     }
-                    __syncwarp();
                 }
             }
             tc_fence_before();                               // O is read: ordered before this warp's next arrival
             plan_done(r);
         }
+        if (lane == 0) tma_store_wait();             // before the CTA's shared memory goes
     } else {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
     if (wid == 12) {
@@ -535,21 +553,31 @@ prefill_scored_tc_kernel(const __grid_constant__ ScoredTcParams p, const __grid_
         const unsigned badmask = __ballot_sync(0xffffffffu, bad);
         const int blocks = __shfl_sync(0xffffffffu, inc, badmask ? __ffs(badmask) - 1 : 31);
         const int64_t items = static_cast<int64_t>(blocks) * hgroups;
+        // The first item of a CTA is its index, the next ones are drawn from a counter (items differ in length, by masks and
+        // from prompt to prompt); the last CTA to draw past the end puts the counters back to zero for the next call.
+        int64_t item = blockIdx.x;
         for (int r = 0;; ++r) {
-            // dealt out to and fro, so that nobody gets the heaviest of every round
-            const int64_t item = static_cast<int64_t>(r) * gridDim.x + ((r & 1) ? gridDim.x - 1 - blockIdx.x : blockIdx.x);
             StPlan &pl = plans[r & 1];
             if (r >= 2) wait(&bar_planfree[r & 1], (r >> 1) - 1);
             __syncwarp();
-            const bool valid = ok && static_cast<int64_t>(r) * gridDim.x < items;      // a round may have nothing for this CTA: an empty item
-            if (!valid) {
-                if (lane == 0) { pl.valid = 0; mbar_arrive(smem_u32(&bar_plan[r & 1])); }
+            const bool some = ok && item < items;
+            if (!some) {
+                if (lane == 0) {
+                    pl.valid = 0;
+                    mbar_arrive(smem_u32(&bar_plan[r & 1]));
+                    __threadfence();
+                    if (atomicAdd(&p.s.hdr[HDR_ITEM_EXITS], 1) == static_cast<int32_t>(gridDim.x) - 1) {
+                        p.s.hdr[HDR_NEXT_ITEM] = 0;
+                        p.s.hdr[HDR_ITEM_EXITS] = 0;
+                    }
+                }
                 break;
             }
-            const bool some = item < items;
-            const int blk = some ? static_cast<int>(item / hgroups) : 0, h0 = some ? static_cast<int>(item % hgroups) * hpc : 0;
+            int next = 0;
+            if (lane == 0) next = atomicAdd(&p.s.hdr[HDR_NEXT_ITEM], 1);
+            const int blk = static_cast<int>(item / hgroups), h0 = static_cast<int>(item % hgroups) * hpc;
             int user = 0, qb = 0, first = 0, len = 0;
-            if (some) {                   // the user whose rows hold block blk; a prompt's blocks count from its end
+            {                             // the user whose rows hold block blk; a prompt's blocks count from its end
                 const int src = __ffs(__ballot_sync(0xffffffffu, blk < inc)) - 1;
                 if (lane == src) {
                     int rem = blk - (inc - sum);
@@ -567,13 +595,13 @@ prefill_scored_tc_kernel(const __grid_constant__ ScoredTcParams p, const __grid_
                 len = __shfl_sync(0xffffffffu, len, src);
             }
             const int row0 = qb * rows_item;
-            const int prefix = some && p.s.prefix_lens ? min(len, p.s.prefix_lens[user]) : 0;
+            const int prefix = p.s.prefix_lens ? min(len, p.s.prefix_lens[user]) : 0;
             int tlo[2] = {0x7fffffff, 0x7fffffff}, thi[2] = {-1, -1}, fulllo = -1, fullhi = 0x7fffffff;
 #pragma unroll
             for (int w = 0; w < 8; ++w) {           // the 32 rows of softmax warp w; two heads have the same rows
                 const int qrow = row0 + (hpc == 2 ? 32 * (w & 3) : 32 * w) + lane;
                 int lo = 0x7fffffff, hi = -1;
-                const bool live = some && qrow < len;
+                const bool live = qrow < len;
                 if (live) scored_interval(p.s, first, prefix, qrow, lo, hi);
                 const bool sees = lo <= hi;
                 if (!sees) { lo = 0x7fffffff; hi = -1; }
@@ -589,7 +617,7 @@ prefill_scored_tc_kernel(const __grid_constant__ ScoredTcParams p, const __grid_
             if (lane == 0) {
                 const int key0 = min(tlo[0], tlo[1]), key1 = max(thi[0], thi[1]);
                 pl.valid = 1; pl.first = first; pl.len = len; pl.row0 = row0; pl.h0 = h0;
-                pl.tiles = !some ? 0 : (hpc == 2 || row0 + 128 < len) ? 2 : 1;
+                pl.tiles = (hpc == 2 || row0 + 128 < len) ? 2 : 1;
                 const int nb = key1 < 0 ? 0 : (key1 - key0) / KB + 1;
                 pl.nb = nb; pl.kend = key1 < 0 ? 0 : key0 + (nb - 1) * KB;
 #pragma unroll
@@ -598,9 +626,11 @@ prefill_scored_tc_kernel(const __grid_constant__ ScoredTcParams p, const __grid_
                     pl.jb[x] = thi[x] < 0 ? 0 : nb - (tlo[x] - key0) / KB;
                 }
                 pl.fulllo = fulllo; pl.fullhi = fullhi; pl.poisoned = 0;
+                pl.ahead = prefix > row0 + 1;
             }
             __syncwarp();
             if (lane == 0) mbar_arrive(smem_u32(&bar_plan[r & 1]));
+            item = static_cast<int64_t>(gridDim.x) + __shfl_sync(0xffffffffu, next, 0);
         }
     } else if (wid == 10) {
         // ---------------- the loading warp (one thread of it); c counts blocks over all items
