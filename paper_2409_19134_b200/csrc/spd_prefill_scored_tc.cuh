@@ -17,8 +17,8 @@
 //
 // Masks are intervals [lo, hi] per row.  A CTA walks the blocks between the least lo and the greatest hi of its rows; a warp
 // of the softmax masks only the blocks that its own 32 rows do not see whole, and skips those that they do not see at all.
-// A hidden key's weight is 0, but 0 * NaN is NaN: the guard warp looks through the V rows of every block that some row does
-// not see whole, clears rows that no row of the CTA sees, and where a row that is not finite is hidden from some rows and
+// A hidden key's weight is 0, but 0 * NaN is NaN: guard warps look through the V rows of every block that some row does not see
+// whole, clear rows that no row of the CTA sees, and where a row that is not finite is hidden from some rows and
 // visible to others, the CTA's rows are done again one by one, hidden keys left out.
 //
 // Bound: the exponential unit (2 x 128 x 80 exponentials a block of two tiles at 16 a cycle: 1280 cycles) and the tensor core
@@ -30,8 +30,8 @@
 namespace spd {
 
 constexpr int kStKeys = 80;                         // keys per block
-constexpr int kStThreads = 512;                     // 8 softmax warps, 2 issuing, 1 loading, 1 guarding, 1 planning, 3 with nothing to do
-constexpr int kStConsumers = 12;                    // warps that read a plan
+constexpr int kStThreads = 512;                     // 8 softmax warps, 2 issuing, 1 loading, 1 planning, 4 guarding
+constexpr int kStConsumers = 15;                    // warps that read a plan
 constexpr int kStTmemCols = 512;
 constexpr float kStFixedCap = 64.f;                 // caps up to here: weights relative to 0 (64 log2(e) = 92.3)
 constexpr int kStS0 = 0, kStS1 = 96;                  // S of each tile (fp32, 80 columns)
@@ -210,7 +210,7 @@ prefill_scored_tc_kernel(const __grid_constant__ ScoredTcParams p, const __grid_
     uint64_t *bar_p = bars + 6, *bar_o = bars + 8;                 // per tile: P written; O has taken the block in (P is free)
     uint64_t *bar_plan = bars + 10, *bar_planfree = bars + 12;     // per plan buffer
     uint64_t *bar_k = bars + 14, *bar_v = bar_k + NS, *bar_kfree = bar_v + NS, *bar_vfree = bar_kfree + NS;
-    uint64_t *bar_guard = bar_vfree + NS;                          // per V slot: the guard is done with the block
+    uint64_t *bar_guard = bar_vfree + NS;                          // per V slot: the guards are done with the block
     constexpr int NBARS = 14 + 5 * NS;
     static_assert(NBARS * 8 + 4 <= kStBarBytes, "barrier block");
     uint32_t &tmem_slot = *reinterpret_cast<uint32_t *>(bars + NBARS);
@@ -224,8 +224,9 @@ prefill_scored_tc_kernel(const __grid_constant__ ScoredTcParams p, const __grid_
     if (tid == 320) {
         prefetch_tensormap(&mq); prefetch_tensormap(&mk); prefetch_tensormap(&mv); prefetch_tensormap(&mo);
         for (int b = 0; b < NBARS; ++b) {
-            // Q and ring slots free: one per tile; S in registers, P written: one per softmax warp of the tile; plan read: one per warp
-            const int n = b == 1 || (b >= 14 + 2 * NS && b < 14 + 4 * NS) ? 2 : (b >= 4 && b < 8) ? 4 : (b >= 12 && b < 14) ? kStConsumers : 1;
+            // Q and ring slots free: one per tile; S in registers, P written: one per softmax warp of the tile;
+            // V looked through: one per guard; plan read: one per warp
+            const int n = b == 1 || (b >= 14 + 2 * NS && b < 14 + 4 * NS) ? 2 : ((b >= 4 && b < 8) || b >= 14 + 4 * NS) ? 4 : (b >= 12 && b < 14) ? kStConsumers : 1;
             mbar_init(smem_u32(&bars[b]), n);
         }
         fence_mbar_init();
@@ -670,15 +671,17 @@ prefill_scored_tc_kernel(const __grid_constant__ ScoredTcParams p, const __grid_
                 if (c >= x && uses > 0) { mbar_wait(smem_u32(&bar_k[x]), (uses - 1) & 1); mbar_wait(smem_u32(&bar_v[x]), (uses - 1) & 1); }
             }
         }
-    } else if (wid == 11) {
-        // ---------------- the guard: V rows of blocks with hidden keys
+    } else if (wid == 11 || wid >= 13) {
+        // ---------------- the guards: V rows of blocks with hidden keys, a quarter of the rows each
+        constexpr int GR = KB / 4;
+        const int g0 = (wid == 11 ? 0 : wid - 12) * GR;
         int c = 0;
         for (int r = 0; ok; ++r) {
             StPlan &pl = plan_of(r);
             if (!ok || !pl.valid) break;
             const int NB = pl.nb;
             for (int j = 0; j < NB && ok; ++j, ++c) {
-                // every block passes through here, so that the guard is never a whole ring ahead of or behind the others
+                // every block passes through here, so that no guard is ever a whole ring ahead of or behind the others
                 const int slot = c % NS, kb = pl.kend - j * KB;
                 wait(&bar_v[slot], c / NS);
                 __syncwarp();
@@ -692,10 +695,11 @@ prefill_scored_tc_kernel(const __grid_constant__ ScoredTcParams p, const __grid_
                            ((w.w & 0x7f807f80u) + 0x00800080u);
                 };
                 uint32_t any = 0;
-#pragma unroll 5
-                for (int x = lane; x < TILE / 16; x += 32) any |= odd(*reinterpret_cast<const uint4 *>(vt + x * 16));
+#pragma unroll
+                for (int x = lane; x < BOXES * GR * 8; x += 32)
+                    any |= odd(*reinterpret_cast<const uint4 *>(vt + (x / (GR * 8)) * kStBox + g0 * 128 + (x % (GR * 8)) * 16));
                 if (__any_sync(0xffffffffu, (any & 0x80008000u) != 0)) {
-                    for (int row = 0; row < KB; ++row) {        // rare: row by row
+                    for (int row = g0; row < g0 + GR; ++row) {        // rare: row by row
                         uint4 *chunk = reinterpret_cast<uint4 *>(vt + (lane >> 3) * kStBox + row * 128 + (lane & 7) * 16);
                         const bool mine = lane < 8 * BOXES;
                         if (!__any_sync(0xffffffffu, mine && (odd(*(mine ? chunk : reinterpret_cast<uint4 *>(vt + row * 128))) & 0x80008000u) != 0)) continue;
