@@ -294,8 +294,11 @@ spd_status spd_service_attn_merge_append(const spd_shape *shape, const void *q, 
  * spd_service_attn_merge_scored are its two halves: each sees one partition and is told how many tokens the other one holds
  * (pub_lens, priv_lens: device [batch]; a negative entry, or a sum beyond 2^31 - 1, raises SPD_ERR_BAD_PAGE for the user).
  * A partition wholly in front of the window gives the empty partial.  `plan` as for the *_planned calls; a plan also fits
- * only calls with the same window.  spd_set_bf16_math does not concern these calls (tensor cores always).  Stream order,
- * errors and workspace as for the plain calls.
+ * only calls with the same window.  spd_set_bf16_math does not concern these calls (tensor cores always).  Stream order
+ * (the other half's lengths are read ahead of the previous kernel like one's own), errors and workspace as for the plain calls.
+ * A visible key whose row of k is NaN makes the outputs concerned NaN (the plain calls give zeros there).  Calls with few and
+ * short sequences -- by the window, or by the pools' pages -- take a kernel of their own (a cluster of CTAs per sequence) unless
+ * spd_set_split asks for a cut or `plan` is not SPD_PLAN_PER_CALL.
  */
 typedef struct {
     float        logit_cap;
@@ -335,7 +338,9 @@ typedef struct {
  * their rows of k and v hold.  `tok` as above; tok_indptr [batch+1] (device), its consistency and what happens where it
  * is not consistent as for spd_prefill_attn; out [total_tokens][num_q_heads][head_dim] in out_dtype, packed.  The prompts'
  * rows do not go to a cache here: spd_append_kv_rope does that, with or without rotation.  sm_scale > 0, else
- * SPD_ERR_UNSUPPORTED.
+ * SPD_ERR_UNSUPPORTED.  One kernel in plain stream order; it counts its work in words of `ws`, so calls that share a
+ * workspace must be ordered.  BF16 runs on the tensor cores (weights rounded to bf16 once, as in spd_prefill_attn), FP32 on
+ * the FMA pipes in fp32 throughout.
  */
 spd_status spd_prefill_attn_scored(const spd_shape *shape, const spd_score *score, int64_t total_tokens,
                                    const spd_tokens *tok, const int32_t *tok_indptr, const int32_t *prefix_lens,
@@ -363,7 +368,8 @@ spd_status spd_prefill_attn_scored(const spd_shape *shape, const spd_score *scor
  *     lengths; it may be seq_lens itself (in place), another array, or NULL (lengths are the caller's business, e.g. counted
  *     once for all layers).  A user whose listed pages cannot hold the new tokens, or with a page out of range among
  *     them, keeps its length and raises SPD_ERR_BAD_PAGE; rows behind its length may have been written.
- * One kernel in plain stream order.  Two tokens of one call must not land in one slot (shared pages).
+ * One kernel in plain stream order.  Two tokens of one call must not land in one slot (shared pages).  new_lens must not be
+ * pos_base.
  */
 typedef struct {
     int32_t      rotary_dim;

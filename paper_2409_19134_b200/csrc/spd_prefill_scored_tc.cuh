@@ -13,7 +13,7 @@
 // softmax, which bounds the loop, never waits for the tensor core: with P over S and 128 keys per block it waited 1300 of
 // 3300 cycles.  80 keys is what tensor memory holds that way at head_dim 128 (S 2 x 80, P 2 x 40, O 2 x 128 of 512 columns).
 // A warp per tile issues that tile's MMAs (an MMA with both operands in shared memory is paced by the 128 bytes a cycle of
-// those: 48 cycles for N = 64, 64 for N = 128, by measurement), another loads, one guards and plans.
+// those: 48 cycles for N = 64, 64 for N = 128, by measurement), another loads, one plans, four guard.
 //
 // Masks are intervals [lo, hi] per row.  A CTA walks the blocks between the least lo and the greatest hi of its rows; a warp
 // of the softmax masks only the blocks that its own 32 rows do not see whole, and skips those that they do not see at all.
@@ -22,7 +22,12 @@
 // visible to others, the CTA's rows are done again one by one, hidden keys left out.
 //
 // Bound: the exponential unit (2 x 128 x 80 exponentials a block of two tiles at 16 a cycle: 1280 cycles) and the tensor core
-// (about 1470) alike, with the FMA pipe close behind when scores are capped.
+// (about 1470) alike, of about 2000 that a block takes; with capped scores the FMA pipe too (2700), and over seconds the power
+// limit (8192 tokens, 32/8 heads: 446 us in the first 100 calls, 514 at 1590 MHz and 990 W after three seconds).  Measured in bursts,
+// head_dim 128, bf16: 8192 tokens x 32/8 heads plain 447 us (1230 TFLOP/s of visible pairs), capped 580 (948), distance bias 545
+// (1008); 8 prompts of 2 to 8 k tokens 1.85 ms (1260); 3 prompts with prefix and window 124 us (915).
+// Slower here: the tiles' exponentials in turns by named barriers (20 %), two threads per row (instruction issue, 15 %), the next
+// block's scores prepared in registers under this block's exponentials (60 %; the compiler serialises them).
 #pragma once
 
 #include "spd_prefill_scored.cuh"

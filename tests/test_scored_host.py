@@ -67,9 +67,9 @@ def test_append_arguments_are_checked(lib):
     good = dict(rotary_dim=64, interleaved=0, num_axes=1, sections=(C.c_int32 * 4)(), scale=1.0, inv_freq=P)
 
     def call(rope=good, n=2, tok=spd.Tokens(P, P, P, 0, 0, 0), ip=None, pos=None, base=None, q_out=P + 4096, k_out=None, kp=P, pages=4, indptr=P,
-             lens=P, ws=P, size=1 << 30, shape=SHAPE):
+             lens=P, ws=P, size=1 << 30, shape=SHAPE, new_lens=None):
         r = spd.Rope(**rope) if rope is not None else None
-        return lib.spd_append_kv_rope(shape, r, n, tok, ip, pos, base, q_out, k_out, kp, P, pages, indptr, P, lens, None, ws, size, None)
+        return lib.spd_append_kv_rope(shape, r, n, tok, ip, pos, base, q_out, k_out, kp, P, pages, indptr, P, lens, new_lens, ws, size, None)
     for bad in (dict(n=3), dict(n=-1, ip=P), dict(tok=None), dict(tok=spd.Tokens(P, None, P, 0, 0, 0)), dict(tok=spd.Tokens(None, P, P, 0, 0, 0)),
                 dict(q_out=None), dict(kp=None), dict(kp=P + 64), dict(pages=0), dict(indptr=None), dict(lens=None), dict(ws=None),
                 dict(pos=P, base=P), dict(rope=dict(good, num_axes=3)), dict(rope=dict(good, inv_freq=None)), dict(rope=dict(good, interleaved=2)),
@@ -78,6 +78,7 @@ def test_append_arguments_are_checked(lib):
                 dict(rope=dict(good, num_axes=2, sections=(C.c_int32 * 4)(40, -8, 0, 0)), pos=P),
                 dict(tok=spd.Tokens(P, P, P, 8 * 64 + 8, 0, 0), q_out=P),            # in place over strided rows
                 dict(tok=spd.Tokens(P, P, P, 0, 2 * 64 + 8, 0), k_out=P),
+                dict(base=P + 256, new_lens=P + 256),                                  # lengths written over the positions' base
                 dict(rope=None), dict(rope=None, q_out=None, pos=P), dict(k_out=P + 4)):
         assert call(**bad) == INVALID, bad
     for bad in (dict(rope=dict(good, rotary_dim=80)), dict(rope=dict(good, rotary_dim=24)), dict(rope=dict(good, rotary_dim=0)),
