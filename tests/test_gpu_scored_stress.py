@@ -1,0 +1,156 @@
+"""Scored calls at drawn shapes, at the ends of their ranges, and side by side."""
+import random
+
+import numpy as np
+import pytest
+import torch
+
+from paper_2409_19134_b200 import binding as spd
+from paper_2409_19134_b200 import workloads as wl
+from tests import scored_reference as ref
+from tests.test_gpu_decode_scored import close, setup, slopes_of, workload
+from tests.test_gpu_prefill_scored import DT, P_WEIGHT, documents, prompts, run
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.mark.parametrize("seed", range(24))
+def test_prompts_of_drawn_shapes(seed):
+    r = random.Random(seed)
+    dtype, d, hkv = r.choice(["bf16", "bf16", "f32"]), r.choice([64, 128]), r.choice([1, 2, 3])
+    hq = hkv * r.choice([1, 2, 4, 8, 16])
+    lens = [r.choice([0, 1, 2, 79, 80, 81, 127, 128, 129, r.randrange(1, 400)]) for _ in range(r.choice([1, 2, 7, 40]))]
+    if sum(lens) == 0:
+        lens[0] = 5
+    cap, window = r.choice([0.0, 0.0, 2.0, 30.0, 90.0]), r.choice([0, 0, 1, 80, r.randrange(1, 300)])
+    q, k, v, ip = prompts(lens, hq, hkv, d, dtype, seed, qscale=3.0 if cap else 1.0, wide=r.random() < 0.5)
+    sl = slopes_of(hq) * r.choice([1.0, 4.0, -0.05]) if r.random() < 0.4 else None
+    prefix = torch.tensor([r.randrange(-1, n + 2) for n in lens], dtype=torch.int32) if r.random() < 0.4 else None
+    doc = documents(lens, seed, longest=r.choice([5, 90, 300])) if r.random() < 0.4 else None
+    T = sum(lens)
+    rows = set(r.sample(range(T), min(T, 60))) | {0, T - 1}
+    want, tol = ref.prefill(q, k, v, lens, d ** -0.5, cap, window, sl, None if prefix is None else prefix.clamp(min=0), doc, P_WEIGHT[dtype], rows)
+    out, status = run(q, k, v, ip, d, cap, window, sl, prefix, doc, r.choice([torch.float32, torch.bfloat16]))
+    assert status == (spd.SPD_OK, -1) and bool(torch.isfinite(out.float()).all())
+    at = sorted(rows)
+    close(out[at], want[at], tol[at], (seed, lens))
+
+
+@pytest.mark.parametrize("seed", range(16))
+def test_decode_of_drawn_shapes(seed):
+    r = random.Random(100 + seed)
+    dtype, d, hkv = r.choice(["bf16", "bf16", "f32"]), r.choice([64, 128]), r.choice([1, 2, 3])
+    hq = hkv * r.choice([1, 2, 4, 8, 16])
+    B = r.choice([1, 3, 20])
+    most = r.choice([5, 40, 700, 3000])
+    lin, lout = [r.randrange(0, most) for _ in range(B)], [r.randrange(0, 50) for _ in range(B)]
+    cap, window, alibi = r.choice([0.0, 4.0, 70.0]), r.choice([0, 0, 1, 33, r.randrange(1, 2000)]), r.random() < 0.5
+    w = workload(lin, lout, hq, hkv, d, dtype, seed, qscale=2.0)
+    g, shape, score, sl, ws = setup(w, cap, window, alibi)
+    want, _, _, _, tol = ref.decode(w, cap, window, sl)
+    out = torch.full((B, hq, d), float("nan"), device="cuda")
+    for knob in (0, 2):
+        try:
+            spd.spd_set_split(knob, False)
+            spd.spd_decode_step_scored(shape, score, g.q, g.priv, g.pub, out, ws)
+        finally:
+            spd.spd_set_split(0, False)
+        assert spd.spd_query_device_status(ws) == (spd.SPD_OK, -1)
+        close(out, want, tol, (seed, knob))
+
+
+def test_no_prompt_tokens_and_one_prompt_token():
+    shape = spd.make_shape(2, 4, 2, 128, torch.bfloat16, 0.1)
+    ws, ip = spd.alloc_workspace(shape), torch.zeros(3, dtype=torch.int32, device="cuda")
+    e = lambda h: torch.empty((0, h, 128), dtype=torch.bfloat16, device="cuda")  # noqa: E731
+    spd.spd_prefill_attn_scored(shape, spd.make_score(), e(4), e(2), e(2), ip, e(4), ws)
+    assert spd.spd_query_device_status(ws) == (spd.SPD_OK, -1)
+    q, k, v, ip = prompts([0, 1], 4, 2, 128, "bf16", 3)
+    out, status = run(q, k, v, ip, 128)
+    assert status == (spd.SPD_OK, -1)
+    assert torch.equal(out.cpu(), v.float().repeat_interleave(2, dim=1))       # one key: its weight is exactly 1
+
+
+def test_rows_behind_the_last_prompt_are_left_alone():
+    q, k, v, ip = prompts([50, 70], 2, 1, 128, "bf16", 4)
+    shape = spd.make_shape(2, 2, 1, 128, torch.bfloat16, 128 ** -0.5)
+    ws = spd.alloc_workspace(shape)
+    pad = torch.full((300, 2, 128), 7.0, dtype=torch.bfloat16, device="cuda")
+    out = pad[:120]
+    spd.spd_prefill_attn_scored(shape, spd.make_score(), q.cuda(), k.cuda(), v.cuda(), ip.cuda(), out, ws)
+    assert spd.spd_query_device_status(ws) == (spd.SPD_OK, -1)
+    assert bool((pad[120:] == 7.0).all()) and not bool((out == 7.0).all(dim=-1).any())
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_pools_beyond_32_bit_offsets(dtype):
+    """Pages near the end of a pool of more than 4 GiB: appended to, then read."""
+    B, hq, hkv, d = 2, 8, 8, 128
+    es = 2 if dtype == "bf16" else 4
+    pages = (9 << 29) // (hkv * 16 * d * es) + 8                       # 4.5 GiB each for K and V
+    kp, vp = (torch.zeros((pages, hkv, 16, d), dtype=DT[dtype], device="cuda") for _ in range(2))
+    i32 = lambda *x: torch.tensor(x, dtype=torch.int32, device="cuda")  # noqa: E731
+    part = wl.PagedKV(kp, vp, i32(0, 2, 4), i32(pages - 1, 3, pages - 4, pages - 2), i32(0, 0))
+    small = wl.PagedKV(kp[:1].clone(), vp[:1].clone(), i32(0, 1, 1), i32(0), i32(0, 0))
+    gen = torch.Generator().manual_seed(1)
+    lens = [20, 31]
+    k, v = (torch.randn((51, hkv, d), generator=gen).to(DT[dtype]) for _ in range(2))
+    q = torch.randn((B, hq, d), generator=gen).to(DT[dtype])
+    shape = spd.make_shape(B, hq, hkv, d, DT[dtype], d ** -0.5)
+    ws, score = spd.alloc_workspace(shape), spd.make_score(20.0)
+    spd.spd_append_kv_rope(shape, None, None, k.cuda(), v.cuda(), part, ws, tok_indptr=i32(0, 20, 51))
+    assert part.seq_lens.tolist() == lens
+    assert torch.equal(kp[pages - 2, :, 14].cpu(), k[50]) and torch.equal(vp[pages - 1, :, 15].cpu(), v[15])
+    out = torch.empty((B, hq, d), device="cuda")
+    spd.spd_decode_step_scored(shape, score, q.cuda(), part, small, out, ws)
+    assert spd.spd_query_device_status(ws) == (spd.SPD_OK, -1)
+    t0 = 0
+    for u, n in enumerate(lens):
+        for h in range(hq):
+            want, _, _, _, S = ref.attend(q[u, h], k[t0:t0 + n, h], v[t0:t0 + n, h], torch.ones(n, dtype=torch.bool), d ** -0.5, 20.0)
+            tol = ref.bound(float(v.abs().max()), d, S, n, 20.0, 0.0, 2.0 ** -16 if dtype == "bf16" else 0.0)
+            assert float((out[u, h].cpu().double() - want).abs().max()) <= tol
+        t0 += n
+
+
+def test_two_prompt_calls_side_by_side():
+    """Two batches on two streams, a workspace each, again and again: the work counters do not meet."""
+    jobs = []
+    for s in range(2):
+        lens = [300 + 100 * s, 77, 513]
+        q, k, v, ip = prompts(lens, 8, 2, 128, "bf16", 50 + s)
+        rows = set(range(0, sum(lens), 97))
+        want, tol = ref.prefill(q, k, v, lens, 128 ** -0.5, cap=25.0, window=200, weight=2.0 ** -8, rows=rows)
+        shape = spd.make_shape(3, 8, 2, 128, torch.bfloat16, 128 ** -0.5)
+        jobs.append(([t.cuda() for t in (q, k, v, ip)], shape, spd.alloc_workspace(shape), torch.empty_like(q, dtype=torch.float32, device="cuda"),
+                     torch.cuda.Stream(), sorted(rows), want, tol))
+    torch.cuda.synchronize()
+    score = spd.make_score(25.0, 200)
+    for _ in range(25):
+        for a, shape, ws, out, st, _, _, _ in jobs:
+            spd.spd_prefill_attn_scored(shape, score, *a, out, ws, stream=st)
+    torch.cuda.synchronize()
+    for _, _, ws, out, st, rows, want, tol in jobs:
+        assert spd.spd_query_device_status(ws, st) == (spd.SPD_OK, -1)
+        close(out[rows], want[rows], tol[rows], "side by side")
+
+
+def test_same_call_gives_the_same_bits():
+    """Prompt attention hands its items out in whatever order the CTAs come; no result depends on it."""
+    q, k, v, ip = prompts([700, 33, 260], 8, 4, 128, "bf16", 60)
+    first, _ = run(q, k, v, ip, 128, cap=30.0, window=150, slopes=slopes_of(8))
+    for _ in range(5):
+        again, _ = run(q, k, v, ip, 128, cap=30.0, window=150, slopes=slopes_of(8))
+        assert torch.equal(first, again)
+
+
+def test_another_device_than_the_current_one_is_refused():
+    q, k, v, ip = prompts([4], 2, 1, 64, "f32", 1)
+    shape = spd.make_shape(1, 2, 1, 64, torch.float32, 0.1)
+    ws = spd.alloc_workspace(shape)
+    with pytest.raises(ValueError):
+        spd.spd_prefill_attn_scored(shape, spd.make_score(), q, k, v, ip, q.clone(), ws)      # host tensors
+    with pytest.raises(ValueError):
+        spd.spd_prefill_attn_scored(shape, spd.make_score(), q.cuda().double(), k.cuda(), v.cuda(), ip.cuda(), q.cuda(), ws)
+    with pytest.raises(ValueError):
+        spd.spd_prefill_attn_scored(shape, spd.make_score(), q.cuda(), k.cuda(), v.cuda(), ip.cuda().long(), q.cuda(), ws)
