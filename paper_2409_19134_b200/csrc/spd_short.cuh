@@ -72,7 +72,6 @@ attn_short_kernel(const __grid_constant__ Params p, const __grid_constant__ CUte
     constexpr int D = Math::D, NS = Math::kStages, TB = Math::kTileBytes, NW = Math::kWarps, V = D / 32, PITCH = D + 4;
     static_assert(2 * TB >= (kHeadsPerItem * PITCH + 3 * kHeadsPerItem) * 4, "a stage must hold the epilogue staging");
     extern __shared__ uint8_t smem_raw[];
-    __shared__ int32_t cta_bad;
     uint8_t *base = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
     const int wid = threadIdx.x >> 5, lane = threadIdx.x & 31;
     uint8_t *ring = base + static_cast<size_t>(wid) * NS * 2 * TB;
@@ -81,12 +80,10 @@ attn_short_kernel(const __grid_constant__ Params p, const __grid_constant__ CUte
     uint8_t *extra = tail + short_extra_offset<Math>() + static_cast<size_t>(wid) * Math::kExtraBytes;
     float *result = reinterpret_cast<float *>(tail + short_result_offset<Math>());     // O[8][D], m[8], l[8], bad page seen
 
-    griddep_launch_dependents();
     if (wid == 0 && lane < 4 && (p.part[0].num_pages > 0 || p.part[1].num_pages > 0))
         prefetch_tensormap(lane == 0 ? &mk0 : lane == 1 ? &mv0 : lane == 2 ? &mk1 : &mv1);
     const int seq = blockIdx.x / cluster, rank = blockIdx.x - seq * cluster;
     const int u = seq / p.S, sq = seq - u * p.S, kvh = sq / p.hgroups;
-    if (threadIdx.x == 0) cta_bad = 0;
     if (lane == 0) {
         for (int s = 0; s < NS; ++s) mbar_init(smem_u32(&bars[s]), 1);
         fence_mbar_init();
@@ -141,6 +138,10 @@ attn_short_kernel(const __grid_constant__ Params p, const __grid_constant__ CUte
 
     // Up to here only the call's inputs were read (see the persistent kernel); q, the workspace and the outputs from here on.
     griddep_wait();
+    // The next kernel may start its preamble only now that the kernel before this one has gone: the persistent kernel reads the
+    // rate table and a stored plan there, which the launch before the previous one may still be writing otherwise -- this
+    // grid may be small and can be resident as a whole beside it.
+    griddep_launch_dependents();
     if (blockIdx.x == 0 && threadIdx.x == 0) {
         p.hdr[HDR_BATCH] = p.B;
         p.hdr[HDR_NSEQ] = p.B * p.S;
@@ -167,20 +168,19 @@ attn_short_kernel(const __grid_constant__ Params p, const __grid_constant__ CUte
         if (lane == 0) flag_error(p.hdr, 6 /* SPD_ERR_TIMEOUT */, -1);
         for (int s = 0; s < NS; ++s) mbar_wait(smem_u32(&bars[s]), ((n - 1) / NS) & 1);    // a bounded chance for copies in flight
     }
-    if (bad && lane == 0) cta_bad = 1;
     // ---- the warp's piece into its first stage (every copy into it has been consumed), then the CTA's pieces into one
     __syncwarp();
     float *So = reinterpret_cast<float *>(ring), *Sm = So + kHeadsPerItem * PITCH;
     Math::finish(st, So, Sm, Sm + kHeadsPerItem, lane);
-    __syncthreads();
+    const bool cta_bad = __syncthreads_or(bad) != 0;
     const int hbase = first_head(p, sq);
     bool user_bad = false;                 // inconsistent tables: flagged, zeros
     if (c.np == 0) {
         int n0, n1;
         user_bad = (rank == 0 && threadIdx.x == 0) ? user_tiles<true, true>(p, u, n0, n1) : user_tiles<false, true>(p, u, n0, n1);
     }
-    const bool b1 = user_bad || cta_bad != 0;
-    if (cluster == 1 && cta_bad != 0 && threadIdx.x == 0) { p.bad[u] = p.epoch; flag_error(p.hdr, 4 /* SPD_ERR_BAD_PAGE */, u); }
+    const bool b1 = user_bad || cta_bad;
+    if (cluster == 1 && cta_bad && threadIdx.x == 0) { p.bad[u] = p.epoch; flag_error(p.hdr, 4 /* SPD_ERR_BAD_PAGE */, u); }
     for (int hh = wid; hh < p.geff; hh += NW) {
         ShortJoin<V> a;
         for (int x = 0; x < NW; ++x) {
@@ -199,7 +199,7 @@ attn_short_kernel(const __grid_constant__ Params p, const __grid_constant__ CUte
         }
     }
     if (cluster == 1) return;
-    if (threadIdx.x == 0) result[kHeadsPerItem * (D + 2)] = cta_bad != 0 ? 1.f : 0.f;
+    if (threadIdx.x == 0) result[kHeadsPerItem * (D + 2)] = cta_bad ? 1.f : 0.f;
     cluster_sync_all();
     // ---- across the cluster: CTA r finishes heads r, r + cluster, ...
     bool any_bad = user_bad;

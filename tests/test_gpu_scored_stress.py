@@ -154,3 +154,26 @@ def test_another_device_than_the_current_one_is_refused():
         spd.spd_prefill_attn_scored(shape, spd.make_score(), q.cuda().double(), k.cuda(), v.cuda(), ip.cuda(), q.cuda(), ws)
     with pytest.raises(ValueError):
         spd.spd_prefill_attn_scored(shape, spd.make_score(), q.cuda(), k.cuda(), v.cuda(), ip.cuda().long(), q.cuda(), ws)
+
+
+@pytest.mark.parametrize("dtype,d", [("bf16", 64), ("bf16", 128), ("f32", 64)])
+def test_short_and_long_calls_in_turns(dtype, d):
+    """Calls of the cluster kernel between calls of the persistent one that store, derive and reuse their cut, back to back on one
+    stream and workspace: whatever is still running when the next one starts, nobody reads what is being written."""
+    w = workload([900, 3, 2500, 0, 64, 1200], [30, 0, 77, 5, 1, 400], 8, 4, d, dtype, 11)
+    g, shape, _, _, ws = setup(w, 0.0, 0, False)
+    plain, near = spd.make_score(), spd.make_score(30.0, 40)
+    outs = {}
+    for name, score, args in (("plain", plain, (0.0, 0)), ("near", near, (30.0, 40))):
+        outs[name] = ref.decode(w, *args, None)
+    turns = [("plain", spd.SPD_PLAN_STORE), ("near", spd.SPD_PLAN_PER_CALL), ("plain", spd.SPD_PLAN_STORE), ("plain", spd.SPD_PLAN_REUSE),
+             ("near", spd.SPD_PLAN_STORE), ("plain", spd.SPD_PLAN_STORE), ("near", spd.SPD_PLAN_PER_CALL), ("near", spd.SPD_PLAN_PER_CALL)] * 8
+    calls = [(kind, plan, torch.full((w.batch, 8, d), float("nan"), device="cuda")) for kind, plan in turns]
+    st = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    for kind, plan, out in calls:
+        spd.spd_decode_step_scored(shape, plain if kind == "plain" else near, g.q, g.priv, g.pub, out, ws, plan=plan, stream=st)
+    assert spd.spd_query_device_status(ws, st) == (spd.SPD_OK, -1)
+    for kind, _, out in calls:
+        want, _, _, _, tol = outs[kind]
+        close(out, want, tol, kind)
