@@ -177,3 +177,29 @@ def test_short_and_long_calls_in_turns(dtype, d):
     for kind, _, out in calls:
         want, _, _, _, tol = outs[kind]
         close(out, want, tol, kind)
+
+
+def test_scored_call_behind_an_appending_launch():
+    """The lengths that an appending launch writes as its last act are the ones that the scored call behind it reads."""
+    w = workload([300, 4, 90], [15, 0, 31], 8, 2, 128, "bf16", 12)
+    g, shape, score, _, ws = setup(w, 20.0, 64, False)
+    gen = torch.Generator().manual_seed(2)
+    st = torch.cuda.Stream()
+    k_new, v_new = (torch.randn((10, 3, 2, 128), generator=gen).bfloat16().cuda() for _ in range(2))
+    big = wl.make_paged_kv(np.array([64, 64, 64]), 2, 128, torch.bfloat16, np.random.default_rng(3), gen, "cpu", poison=False)
+    n0 = torch.tensor([15, 0, 31], dtype=torch.int32)
+    big.seq_lens.copy_(n0)
+    pub = big.to("cuda")
+    outs = [torch.empty((3, 8, 128), device="cuda") for _ in range(10)]
+    other = torch.empty_like(outs[0])
+    torch.cuda.synchronize()
+    for s in range(10):
+        spd.spd_decode_step_append(shape, g.q, k_new[s], v_new[s], g.priv, pub, other, ws, stream=st)
+        spd.spd_decode_step_scored(shape, score, g.q, g.priv, pub, outs[s], ws, stream=st)
+    assert spd.spd_query_device_status(ws, st) == (spd.SPD_OK, -1)
+    grown = pub.to("cpu")
+    for s in range(10):
+        grown.seq_lens.copy_(n0 + s + 1)
+        x = wl.Workload("grown", 3, 8, 2, 128, 16, torch.bfloat16, w.sm_scale, w.q, w.priv, grown)
+        want, _, _, _, tol = ref.decode(x, 20.0, 64, None)
+        close(outs[s], want, tol, s)
