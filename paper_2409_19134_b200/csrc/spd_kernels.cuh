@@ -340,13 +340,18 @@ __device__ __forceinline__ void piece_ticket(const Params &p, const PieceInfo &p
 // ------------------------------------------------------------------------------------------------
 // One score of a scored call, `s` scaled already, `d` >= 0 the distance from the query to the key:
 //   cap tanh(s / cap) - slope d, and -inf outside the window.
-// tanh(x) = 1 - 2 / (e^2x + 1).  The fast form's error is about 2^-23 of the cap (the two special-function steps), far
-// below what the 16-bit inputs carry; fp32 calls use tanhf.
+// tanh(x) = 1 - 2 / (e^2x + 1), off by about 2^-23 of the cap (the two special-function steps); below 1/16 of the cap, where
+// that would grow against the score, x - x^3 / 3, off by 2e-6 of the score -- both far below what the 16-bit inputs carry.  fp32 calls use tanhf.
 template <bool Exact>
 __device__ __forceinline__ float scored_value(const Params &p, float s, float slope, int d) {
     if (p.cap > 0.f) {
-        if constexpr (Exact) s = p.cap * tanhf(s / p.cap);
-        else s = p.cap - __fdividef(2.f * p.cap, ex2_approx(s * p.cap_log2) + 1.f);
+        if constexpr (Exact) {
+            s = p.cap * tanhf(s / p.cap);
+        } else {
+            const float z = s * p.cap_log2;                  // 2 log2(e) s / cap
+            const float cubic = fmaf(s * -0.040037751f, z * z, s), full = p.cap - __fdividef(2.f * p.cap, ex2_approx(z) + 1.f);
+            s = fabsf(z) < 0.18033688f ? cubic : full;       // 1 / (12 log2(e)^2) and 2 log2(e) / 16
+        }
     }
     s = fmaf(-slope, static_cast<float>(d), s);
     return (p.window > 0 && d >= p.window) ? -INFINITY : s;

@@ -61,18 +61,23 @@ spd_status prefill_tc(const spd_shape &s, const ScoredPrefillParams &sp, cudaStr
     p.heads_per_cta = g % 2 == 0 ? 2 : 1;
     p.c2 = s.sm_scale * kLog2e;
     p.half_at = p.one_at = -1.f;
+    const bool bias = sp.slopes != nullptr;
+    const int cap = sp.cap == 0.f ? 0 : (sp.cap <= kStFixedCap && !bias) ? 1 : 2;
     if (sp.cap > 0.f) {
         const double y1 = static_cast<double>(s.sm_scale) / sp.cap;
         p.cap2 = sp.cap * kLog2e;
         p.y1 = static_cast<float>(fmin(y1, 1e30));
-        bool fits = true;             // coefficients that leave fp32's range: the exact form does it
+        // Scaled coefficients (CAP 1) that leave fp32's normal range: the exact form does it.
+        bool fits1 = true, fits2 = true;
+        auto normal = [](double c) { return fabs(c) > 1e-37 && fabs(c) < 1e37; };
         for (int i = 0; i < 6; ++i) {
-            const double c = sp.cap * 1.4426950408889634 * pow(y1, 2 * i + 1);
-            if (i < 4) p.p1[i] = twice(c * kTanhHalf[i]);
+            const double c = cap == 1 ? sp.cap * 1.4426950408889634 * pow(y1, 2 * i + 1) : 1.0;
+            if (i < 4) { p.p1[i] = twice(c * kTanhHalf[i]); fits1 = fits1 && normal(c * kTanhHalf[i]); }
             p.p2[i] = twice(c * kTanhOne[i]);
-            fits = fits && c > 1e-30 && c < 1e30;
+            fits2 = fits2 && normal(c * kTanhOne[i]);
         }
-        if (fits) { p.half_at = 0.5f; p.one_at = 1.f; }
+        if (fits1) p.half_at = 0.5f;
+        if (fits2) p.one_at = 1.f;
     }
     CUtensorMap mq, mk, mv, mo;
     spd_status rc;
@@ -87,8 +92,6 @@ spd_status prefill_tc(const spd_shape &s, const ScoredPrefillParams &sp, cudaStr
     int sms = 0;
     if ((rc = host::device_sms(&sms)) != SPD_OK) return rc;
     const unsigned grid = static_cast<unsigned>(items < sms ? items : sms);
-    const bool bias = sp.slopes != nullptr;
-    const int cap = sp.cap == 0.f ? 0 : (sp.cap <= kStFixedCap && !bias) ? 1 : 2;
 #define SPD_TC_CASE(DD, CC, BB) if (s.head_dim == DD && cap == CC && bias == BB) return launch_prefill_tc<DD, CC, BB>(p, mq, mk, mv, mo, grid, st);
     SPD_TC_CASE(128, 0, false) SPD_TC_CASE(128, 1, false) SPD_TC_CASE(128, 2, false) SPD_TC_CASE(128, 0, true) SPD_TC_CASE(128, 2, true)
     SPD_TC_CASE(64, 0, false) SPD_TC_CASE(64, 1, false) SPD_TC_CASE(64, 2, false) SPD_TC_CASE(64, 0, true) SPD_TC_CASE(64, 2, true)

@@ -38,7 +38,7 @@ constexpr int kStKeys = 80;                         // keys per block
 constexpr int kStThreads = 512;                     // 8 softmax warps, 2 issuing, 1 loading, 1 planning, 4 guarding
 constexpr int kStConsumers = 15;                    // warps that read a plan
 constexpr int kStTmemCols = 512;
-constexpr float kStFixedCap = 64.f;                 // caps up to here: weights relative to 0 (64 log2(e) = 92.3)
+constexpr float kStFixedCap = 50.f;                 // caps up to here: weights relative to 0 (50 log2(e) = 72.2)
 constexpr int kStS0 = 0, kStS1 = 96;                  // S of each tile (fp32, 80 columns)
 constexpr int kStP0 = 176, kStP1 = 216;              // P (bf16 pairs, 40 columns)
 constexpr int kStO0 = 256, kStO1 = 384;              // O (fp32, D columns)
@@ -75,7 +75,8 @@ struct ScoredTcParams {
     float cap2;                 // cap log2(e)
     float y1;                   // sm_scale / cap: what is inside the tanh per unit of q.k
     float half_at, one_at;      // where the two polynomials below end (1/2 and 1; -1 = not to be used)
-    uint64_t p1[4], p2[6];      // cap2 tanh(y1 x) = x P(x^2): coefficients for |y1 x| <= 1/2 and <= 1, each in both halves
+    uint64_t p1[4], p2[6];      // coefficients for |y1 x| <= 1/2 and <= 1, each in both halves.  CAP 1: of cap2 tanh(y1 x) = x P(x^2);
+                                // CAP 2: of tanh(y) = y P(y^2), whatever the cap, for scores that were multiplied by y1
 };
 
 // tanh(y) = y P(y^2) by minimax polynomials (exchange algorithm, absolute error): 1.3e-7 for |y| <= 1/2, 2.4e-7 for |y| <= 1.
@@ -157,7 +158,8 @@ __device__ __forceinline__ void st_commit(uint32_t bar) {
                  "@e tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n\t}" ::"r"(bar) : "memory");
 }
 
-// cap2 tanh(y1 x) with the special-function unit: 1 - 2 / (e^2y + 1).
+// cap2 tanh(y1 x) with the special-function unit: 1 - 2 / (e^2y + 1).  Off by 2^-22 of the cap, so for caps that no score comes
+// near the polynomials are not only faster (they are off by 2.3e-6 of the score).
 __device__ __forceinline__ float st_cap(const ScoredTcParams &p, float x) {
     return p.cap2 - __fdividef(2.f * p.cap2, ex2_approx(x * (2.f * kLog2e) * p.y1) + 1.f);
 }
@@ -355,11 +357,20 @@ prefill_scored_tc_kernel(const __grid_constant__ ScoredTcParams p, const __grid_
                 constexpr bool kLog2 = CAP == 2 || BIAS;
                 if constexpr (CAP == 2) {
                     float big[4] = {0.f, 0.f, 0.f, 0.f};
+                    if (masked) {                                  // hidden scores may be anything
+#pragma unroll
+                        for (int x = 0; x < KB; ++x) sv[x] = seen(x) ? sv[x] : 0.f;
+                    }
 #pragma unroll
                     for (int x = 0; x < KB; x += 2) big[(x >> 1) & 3] = fmax3_abs(big[(x >> 1) & 3], sv[x], sv[x + 1]);
-                    const int form = masked ? 0 : form_of(fmaxf(fmaxf(big[0], big[1]), fmaxf(big[2], big[3])) * p.y1);   // hidden scores may be anything
-                    if (form == 1) in_place(poly1);
-                    else if (form == 2) in_place(poly2);
+                    const int form = form_of(fmaxf(fmaxf(big[0], big[1]), fmaxf(big[2], big[3])) * p.y1);
+                    const uint64_t y12 = pack_f32x2(p.y1, p.y1), cap22 = pack_f32x2(p.cap2, p.cap2);
+                    auto scaled = [&](auto &&poly) {
+                        in_place([&](int x) { return mul_f32x2(pack_f32x2(sv[x], sv[x + 1]), y12); });
+                        in_place([&](int x) { return mul_f32x2(poly(x), cap22); });
+                    };
+                    if (form == 1) scaled(poly1);
+                    else if (form == 2) scaled(poly2);
                     else in_place(exact);
                 }
                 if constexpr (BIAS) {
@@ -406,8 +417,8 @@ prefill_scored_tc_kernel(const __grid_constant__ ScoredTcParams p, const __grid_
                 };
                 auto nothing = [](float &, float, float) {};
                 if constexpr (CAP == 1) {
-                    // Capped scores lie within +-cap2 <= 92 log2 units: relative to 0, weights, sums over 2^24 keys and O stay within
-                    // fp32, so no maximum is needed.  The form that suits the block before is tried first; whether it holds here
+                    // Capped scores lie within +-cap2 <= 72 log2 units: relative to 0, weights, sums over 2^24 keys and O (|v| < 2^31)
+                    // stay within fp32, so no maximum is needed.  The form that suits the block before is tried first; whether it holds here
                     // is found out alongside.
                     if (masked) {
                         weights([&](int x) { return pack_f32x2(sv[x], sv[x + 1]); }, nothing);

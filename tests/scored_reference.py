@@ -4,7 +4,7 @@ rotation, with the error bounds that the tests use.  Test-side only: nothing her
 Error bounds.  An output is sum_j p_j v_j / sum_j p_j; a relative error of at most e on every weight p_j moves it by at most
 2 e max|v|.  A weight's relative error is the absolute error of its score (exp' = exp) plus what its own evaluation costs:
   score   D 2^-24 S          D products summed in fp32, S = scale * sum_d |q_d k_d|
-          2^-21 cap          the cap's special-function steps (relative to the cap)
+          2^-21 cap          the cap's special-function steps (relative to the cap; cap_error in its place where a test knows better)
           2^-23 slope dist   product and sum of the distance bias
   weight  2^-21              exponential (2 ulp) and the change of the running maximum
 Rounding the weights to bf16 for the product with V touches the numerator alone and counts once: 2^-8 (prompt attention on the
@@ -49,7 +49,7 @@ def attend(q, k, v, seen, scale, cap=0.0, slope=0.0, dist=None):
     return O / l, O, m, l, float(scale * (k.abs() @ q.abs()).max())
 
 
-def decode(w, cap=0.0, window=0, slopes=None, parts=(True, True)):
+def decode(w, cap=0.0, window=0, slopes=None, parts=(True, True), cap_error=None):
     """Every user and head of a workload (CPU tensors): (out, O, m, l, tol) over the partitions in `parts`, positions counted over both."""
     from paper_2409_19134_b200 import workloads as wl
     B, Hq, Hkv, D = w.batch, w.num_q_heads, w.num_kv_heads, w.head_dim
@@ -71,7 +71,7 @@ def decode(w, cap=0.0, window=0, slopes=None, parts=(True, True)):
                 sl = float(slopes[j]) if slopes is not None else 0.0
                 out[u, j], O[u, j], m[u, j], l[u, j], S = attend(w.q[u, j], k, v, seen, w.sm_scale, cap, sl, dist)
                 bias = abs(sl) * float(dist[seen].max()) if bool(seen.any()) else 0.0
-                tol[u, j] = bound(vmax, D, S, int(seen.sum()), cap, bias, 0.0 if w.dtype == torch.float32 else 2.0 ** -16)
+                tol[u, j] = bound(vmax, D, S, int(seen.sum()), cap if cap_error is None else cap_error, bias, 0.0 if w.dtype == torch.float32 else 2.0 ** -16)
     return out, O, m, l, tol
 
 
@@ -86,7 +86,7 @@ def intervals(n, window=0, prefix=0, doc=None):
     return lo, torch.where(i < prefix, torch.full_like(i, prefix - 1), i)
 
 
-def prefill(q, k, v, lens, scale, cap=0.0, window=0, slopes=None, prefix=None, doc=None, weight=0.0, rows=None):
+def prefill(q, k, v, lens, scale, cap=0.0, window=0, slopes=None, prefix=None, doc=None, weight=0.0, rows=None, cap_error=None):
     """Packed prompts on the CPU -> (out [T,Hq,D], tol [T,Hq]) in float64; rows: only these packed rows (others stay 0)."""
     T, Hq, D = q.shape
     g = Hq // k.shape[1]
@@ -105,7 +105,7 @@ def prefill(q, k, v, lens, scale, cap=0.0, window=0, slopes=None, prefix=None, d
                 kk, vv = k[t0:t0 + n, h // g], v[t0:t0 + n, h // g]
                 out[t0 + i, h], _, _, _, S = attend(q[t0 + i, h], kk, vv, seen, scale, cap, sl, dist)
                 if bool(seen.any()):
-                    tol[t0 + i, h] = bound(float(vv[seen].abs().max()), D, S, int(seen.sum()), cap, abs(sl) * float(dist[seen].max()), weight)
+                    tol[t0 + i, h] = bound(float(vv[seen].abs().max()), D, S, int(seen.sum()), cap if cap_error is None else cap_error, abs(sl) * float(dist[seen].max()), weight)
         t0 += n
     return out, tol
 

@@ -156,6 +156,38 @@ def test_another_device_than_the_current_one_is_refused():
         spd.spd_prefill_attn_scored(shape, spd.make_score(), q.cuda(), k.cuda(), v.cuda(), ip.cuda().long(), q.cuda(), ws)
 
 
+@pytest.mark.parametrize("cap,scale", [(50.0, 1 / 16), (51.0, 64 ** -0.5), (100.0, 64 ** -0.5), (1000.0, 64 ** -0.5), (50.0, 1e-4), (0.01, 1.0), (1e-3, 3.0),
+                                       (1e30, 0.1), (1e-30, 0.1)])
+@pytest.mark.parametrize("alibi", [False, True])
+def test_caps_over_their_range(cap, scale, alibi):
+    """Every size of cap over scores from far below it to far above."""
+    lens, hq, hkv, d = [170, 90], 4, 2, 64
+    q, k, v, ip = prompts(lens, hq, hkv, d, "bf16", 70)
+    q *= torch.logspace(-2, 1.5, q.shape[0])[torch.randperm(q.shape[0], generator=torch.Generator().manual_seed(1))][:, None, None].bfloat16()
+    sl = slopes_of(hq) if alibi else None
+    # Where the cap is far above the scores its error is 2.3e-6 = 2^-18.7 < 6 x 2^-21 of the greatest score (the polynomials'; the
+    # other form only serves blocks in which some score reaches the cap) and not 2^-21 of the cap.
+    top = scale * max(float((q[t0:t0 + n].double().flatten(0, 1) @ k[t0:t0 + n].double().flatten(0, 1).T).abs().max()) for t0, n in ((0, 170), (170, 90)))
+    eff = min(cap, 6 * top)
+    want, tol = ref.prefill(q, k, v, lens, scale, cap, 0, sl, weight=P_WEIGHT["bf16"], cap_error=eff)
+    shape = spd.make_shape(2, hq, hkv, d, torch.bfloat16, scale)
+    ws, out = spd.alloc_workspace(shape), torch.empty(q.shape, device="cuda")
+    spd.spd_prefill_attn_scored(shape, spd.make_score(cap, 0, None if sl is None else sl.cuda()), q.cuda(), k.cuda(), v.cuda(), ip.cuda(), out, ws)
+    assert spd.spd_query_device_status(ws) == (spd.SPD_OK, -1)
+    close(out, want, tol, (cap, scale))
+    # the same rows as generated tokens: the last token of each prompt over its keys
+    w = workload(lens, [0, 0], hq, hkv, d, "bf16", 71, qscale=4.0)
+    w.sm_scale = scale
+    g, shape, score, sl, ws = setup(w, cap, 0, alibi)
+    # the cubic is off by 2 / 15 / 16^4 = 2.1e-6 of the score, the full form by 2^-22 of the cap <= 16 scores: 8 x 2^-21 of the greatest
+    top = scale * float(w.q.double().abs().sum(-1).max()) * 8.0            # |q.k| <= |q|_1 max|k|, and no k exceeds 8
+    want, _, _, _, tol = ref.decode(w, cap, 0, sl, cap_error=min(cap, 8 * top))
+    out = torch.empty((2, hq, d), device="cuda")
+    spd.spd_decode_step_scored(shape, score, g.q, g.priv, g.pub, out, ws)
+    assert spd.spd_query_device_status(ws) == (spd.SPD_OK, -1)
+    close(out, want, tol, ("decode", cap, scale))
+
+
 @pytest.mark.parametrize("dtype,d", [("bf16", 64), ("bf16", 128), ("f32", 64)])
 def test_short_and_long_calls_in_turns(dtype, d):
     """Calls of the cluster kernel between calls of the persistent one that store, derive and reuse their cut, back to back on one
