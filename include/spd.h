@@ -371,7 +371,7 @@ spd_status spd_prefill_attn_scored(const spd_shape *shape, const spd_score *scor
  *     once for all layers).  A user whose listed pages cannot hold the new tokens, or with a page out of range among
  *     them, keeps its length and raises SPD_ERR_BAD_PAGE; rows behind its length may have been written.
  * One kernel in plain stream order.  Two tokens of one call must not land in one slot (shared pages).  new_lens must not be
- * pos_base.
+ * pos_base, nor positions where tok_indptr is given and new_lens is not seq_lens.
  */
 typedef struct {
     int32_t      rotary_dim;

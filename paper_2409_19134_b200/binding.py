@@ -73,8 +73,11 @@ class Tokens(C.Structure):
                 ("v_stride", C.c_int64)]
 
 
+_Sections = C.c_int32 * 4
+
+
 class Rope(C.Structure):
-    _fields_ = [("rotary_dim", C.c_int32), ("interleaved", C.c_int32), ("num_axes", C.c_int32), ("sections", C.c_int32 * 4),
+    _fields_ = [("rotary_dim", C.c_int32), ("interleaved", C.c_int32), ("num_axes", C.c_int32), ("sections", _Sections),
                 ("scale", C.c_float), ("inv_freq", C.c_void_p)]
 
 
@@ -175,14 +178,17 @@ def _ptr(t: Optional[torch.Tensor]) -> Optional[int]:
     return None if t is None or t.numel() == 0 else t.data_ptr()
 
 
+_I32 = torch.int32
+
+
 def paged_kv(part) -> PagedKV:
     """Marshal an object with k_pool, v_pool, page_indptr, page_indices, seq_lens tensors."""
-    for t in (part.k_pool, part.v_pool, part.page_indptr, part.page_indices, part.seq_lens):
-        assert t.is_contiguous()
-    assert part.page_indptr.dtype == torch.int32 and part.page_indices.dtype == torch.int32
-    assert part.seq_lens.dtype == torch.int32
-    return PagedKV(_ptr(part.k_pool), _ptr(part.v_pool), int(part.k_pool.shape[0]),
-                   part.page_indptr.data_ptr(), _ptr(part.page_indices), part.seq_lens.data_ptr())
+    kp, vp, indptr, indices, lens = part.k_pool, part.v_pool, part.page_indptr, part.page_indices, part.seq_lens
+    assert (kp.is_contiguous() and vp.is_contiguous() and indptr.is_contiguous() and indices.is_contiguous() and lens.is_contiguous() and
+            indptr.dtype is _I32 and indices.dtype is _I32 and lens.dtype is _I32)
+    pages = kp.shape[0]
+    return PagedKV(kp.data_ptr() if pages else _ptr(kp), vp.data_ptr() if pages else _ptr(vp), pages,
+                   indptr.data_ptr(), _ptr(indices), lens.data_ptr())
 
 
 def _stream_ptr(stream: Optional[torch.cuda.Stream]) -> int:
@@ -478,6 +484,8 @@ def spd_prefill_attn(shape, q, k, v, tok_indptr, part, out, ws, stream=None) -> 
 
 def make_score(logit_cap: float = 0.0, window: int = 0, alibi_slopes: Optional[torch.Tensor] = None) -> Score:
     """Score options of the *_scored calls; alibi_slopes: float32 [num_q_heads] on the device."""
+    if not -2**31 <= window < 2**31:
+        raise ValueError("the window is a 32-bit number")
     sc = Score(float(logit_cap), int(window), None)
     if alibi_slopes is not None:
         assert alibi_slopes.dtype == torch.float32 and alibi_slopes.is_contiguous() and alibi_slopes.is_cuda
@@ -489,7 +497,7 @@ def make_score(logit_cap: float = 0.0, window: int = 0, alibi_slopes: Optional[t
 def make_rope(inv_freq: torch.Tensor, interleaved: bool = False, sections=None, scale: float = 1.0) -> Rope:
     """Rotation of spd_append_kv_rope; inv_freq: float32 [rotary_dim / 2] on the device; sections: pairs per position axis."""
     assert inv_freq.dtype == torch.float32 and inv_freq.is_contiguous() and inv_freq.is_cuda and inv_freq.dim() == 1
-    rope = Rope(2 * inv_freq.numel(), 1 if interleaved else 0, len(sections) if sections else 1, (C.c_int32 * 4)(*(sections or ())),
+    rope = Rope(2 * inv_freq.numel(), 1 if interleaved else 0, len(sections) if sections else 1, _Sections(*(sections or ())),
                 float(scale), inv_freq.data_ptr())
     rope._keep = inv_freq
     return rope
@@ -500,8 +508,12 @@ _TORCH_DTYPES = {SPD_F32: torch.float32, SPD_BF16: torch.bfloat16}
 
 def _here(t: torch.Tensor) -> None:
     """The tensors of a call live on the current device, whose stream and context the call uses."""
-    if t.get_device() != torch._C._cuda_getDevice():
-        raise ValueError(f"tensor on {t.device}, but the current device is cuda:{torch.cuda.current_device()}")
+    if not t.is_cuda or t.get_device() != torch._C._cuda_getDevice():
+        raise ValueError(f"tensor on {t.device}, which is not the current CUDA device")
+
+
+def _host(t: torch.Tensor) -> ValueError:
+    return ValueError(f"expected a tensor on the current CUDA device, got one on {t.device}")
 
 
 def _slopes(shape, score) -> None:
@@ -511,13 +523,19 @@ def _slopes(shape, score) -> None:
 
 def _rows(t: torch.Tensor, heads: int, d: int, n: int, dtype):
     """(pointer, token stride in elements) of [n, heads, d] rows that may be part of a wider row per token."""
-    if t.dtype != dtype or t.shape != (n, heads, d):
+    if t.dtype is not dtype or t.shape != (n, heads, d):
         raise ValueError(f"expected {dtype} [{n}, {heads}, {d}], got {t.dtype} {list(t.shape)}")
-    s0, s1, s2 = t.stride()
     if n == 0:
         return None, 0
+    if not t.is_cuda:
+        raise _host(t)
+    if t.is_contiguous():
+        return t.data_ptr(), 0
+    s0, s1, s2 = t.stride()
     if s2 != 1 or (heads > 1 and s1 != d):
         raise ValueError("a token's heads must be packed")
+    if n > 1 and s0 < heads * d:            # an expanded tensor's 0 would read as packed
+        raise ValueError("tokens must not overlap")
     return t.data_ptr(), s0 if n > 1 else 0
 
 
@@ -525,8 +543,10 @@ def _i32(t: Optional[torch.Tensor], *size) -> Optional[int]:
     """Pointer of a contiguous int32 tensor of the given shape, or None."""
     if t is None:
         return None
-    if t.dtype != torch.int32 or t.shape != size or not t.is_contiguous():
+    if t.dtype is not torch.int32 or t.shape != size or not t.is_contiguous():
         raise ValueError(f"expected contiguous int32 {list(size)}, got {t.dtype} {list(t.shape)}")
+    if not t.is_cuda:
+        raise _host(t)
     return t.data_ptr()
 
 
@@ -534,15 +554,26 @@ def _packed(t: Optional[torch.Tensor], numel: int, dtype=None) -> Optional[int]:
     """Pointer of a contiguous tensor of `numel` elements, or None."""
     if t is None:
         return None
-    if t.numel() != numel or not t.is_contiguous() or (dtype is not None and t.dtype != dtype):
+    if t.numel() != numel or not t.is_contiguous() or (dtype is not None and t.dtype is not dtype):
         raise ValueError(f"expected a contiguous tensor of {numel} elements, got {t.dtype} {list(t.shape)}")
+    if not t.is_cuda:
+        raise _host(t)
     return t.data_ptr() if numel else None
+
+
+def _query(shape, q, *parts) -> None:
+    """One packed query row per user and head; the partitions where it is."""
+    _here(q)
+    _packed(q, shape.batch * shape.num_q_heads * shape.head_dim, _TORCH_DTYPES[shape.dtype])
+    for part in parts:
+        if not part.seq_lens.is_cuda:
+            raise _host(part.seq_lens)
 
 
 def spd_partial_attn_scored(shape, score, q, priv, pub_lens, out, ws, plan=SPD_PLAN_PER_CALL, stream=None) -> None:
     """spd_partial_attn with score options; pub_lens: int32 [batch], tokens in the public partition."""
     _slopes(shape, score)
-    _here(q)
+    _query(shape, q, priv)
     kv = paged_kv(priv)
     part = Partial(out[0].data_ptr(), out[1].data_ptr(), out[2].data_ptr())
     _check(lib().spd_partial_attn_scored(shape, score, q.data_ptr(), kv, _i32(pub_lens, shape.batch), part, plan, ws.data_ptr(), ws.numel(),
@@ -552,7 +583,8 @@ def spd_partial_attn_scored(shape, score, q, priv, pub_lens, out, ws, plan=SPD_P
 def spd_service_attn_merge_scored(shape, score, q, pub, priv_lens, partial_in, out, ws, plan=SPD_PLAN_PER_CALL, stream=None) -> None:
     """spd_service_attn_merge with score options; priv_lens: int32 [batch], tokens in the private partition."""
     _slopes(shape, score)
-    _here(q)
+    _query(shape, q, pub)
+    _packed(out, q.numel())
     kv = paged_kv(pub)
     part = Partial(partial_in[0].data_ptr(), partial_in[1].data_ptr(), partial_in[2].data_ptr())
     _check(lib().spd_service_attn_merge_scored(shape, score, q.data_ptr(), kv, _i32(priv_lens, shape.batch), part, out.data_ptr(),
@@ -563,7 +595,8 @@ def spd_service_attn_merge_scored(shape, score, q, pub, priv_lens, partial_in, o
 def spd_decode_step_scored(shape, score, q, priv, pub, out, ws, plan=SPD_PLAN_PER_CALL, stream=None) -> None:
     """The fused decode step with score options (make_score) over both partitions."""
     _slopes(shape, score)
-    _here(q)
+    _query(shape, q, priv, pub)
+    _packed(out, q.numel())
     a, b = paged_kv(priv), paged_kv(pub)
     _check(lib().spd_decode_step_scored(shape, score, q.data_ptr(), a, b, out.data_ptr(), _dtype_code(out.dtype), plan, ws.data_ptr(),
                                         ws.numel(), _stream_ptr(stream)), "spd_decode_step_scored")
@@ -599,11 +632,15 @@ def spd_append_kv_rope(shape, rope, q, k, v, part, ws, q_out=None, k_out=None, t
         if rope is None:
             raise ValueError("positions are for a rotation")
         positions = _i32(positions, T) if positions.dim() == 1 and rope.num_axes == 1 else _i32(positions, rope.num_axes, T)
-    if not (part.k_pool.is_contiguous() and part.v_pool.is_contiguous() and part.page_indices.is_contiguous()):
-        raise ValueError("pools and page tables are contiguous")
+    pages, indices = part.k_pool.shape[0], part.page_indices
+    for pool in (part.k_pool, part.v_pool):
+        if pool.dtype is not dtype or pool.numel() != pages * hkv * 16 * d or not pool.is_contiguous() or not pool.is_cuda:
+            raise ValueError(f"expected contiguous {dtype} pools [{pages}, {hkv}, 16, {d}] on the device, got {pool.dtype} {list(pool.shape)} on {pool.device}")
+    if indices.dtype is not torch.int32 or not indices.is_contiguous() or not indices.is_cuda:
+        raise ValueError("page indices are contiguous int32 on the device")
     lens = _i32(part.seq_lens, B)
     _check(lib().spd_append_kv_rope(shape, rope, T, Tokens(qp, kp, vp, qs, ks, vs), _i32(tok_indptr, B + 1), positions, _i32(pos_base, B),
                                     _packed(q_out, T * hq * d, dtype), _packed(k_out, T * hkv * d, dtype), part.k_pool.data_ptr(),
-                                    part.v_pool.data_ptr(), part.k_pool.shape[0], _i32(part.page_indptr, B + 1), _ptr(part.page_indices),
+                                    part.v_pool.data_ptr(), pages, _i32(part.page_indptr, B + 1), _ptr(indices),
                                     lens, lens if isinstance(new_lens, str) else _i32(new_lens, B), ws.data_ptr(), ws.numel(),
                                     _stream_ptr(stream)), "spd_append_kv_rope")

@@ -125,6 +125,7 @@ spd_status spd_append_kv_rope(const spd_shape *shape, const spd_rope *rope, int6
         if ((rope->num_axes > 1 && !positions) || (positions && pos_base)) return SPD_ERR_INVALID_ARG;
         // other CTAs may still read a user's position while its grown length is written
         if (pos_base && pos_base == new_lens) return SPD_ERR_INVALID_ARG;
+        if (tok_indptr && positions && positions == new_lens && new_lens != seq_lens) return SPD_ERR_INVALID_ARG;
         if (T > 0 && (!tok->q || !q_out)) return SPD_ERR_INVALID_ARG;
         if (misaligned(tok->q, 16) || misaligned(q_out, 16) || misaligned(k_out, 16)) return SPD_ERR_INVALID_ARG;
         if (!row_stride(s, s.num_q_heads, tok->q_stride, &qs)) return SPD_ERR_INVALID_ARG;

@@ -154,6 +154,20 @@ def test_another_device_than_the_current_one_is_refused():
         spd.spd_prefill_attn_scored(shape, spd.make_score(), q.cuda().double(), k.cuda(), v.cuda(), ip.cuda(), q.cuda(), ws)
     with pytest.raises(ValueError):
         spd.spd_prefill_attn_scored(shape, spd.make_score(), q.cuda(), k.cuda(), v.cuda(), ip.cuda().long(), q.cuda(), ws)
+    with pytest.raises(ValueError):
+        spd.spd_prefill_attn_scored(shape, spd.make_score(), q.cuda(), k.cuda(), v.cuda(), ip, q.cuda(), ws)      # offsets on the host
+    with pytest.raises(ValueError):
+        spd.spd_prefill_attn_scored(shape, spd.make_score(), q.cuda(), k.cuda()[:1].expand(4, 1, 64), v.cuda(), ip.cuda(), q.cuda(), ws)
+    for rows in (torch.zeros(320).cuda().as_strided((4, 2, 64), (64, 64, 1)), torch.zeros(4, 64, 2).cuda().transpose(1, 2)):      # overlapping, not packed
+        with pytest.raises(ValueError):
+            spd.spd_prefill_attn_scored(shape, spd.make_score(), rows, k.cuda(), v.cuda(), ip.cuda(), q.cuda(), ws)
+    w = workload([5], [3], 2, 1, 64, "f32", 1)
+    g, shape, score, _, ws = setup(w, 0.0, 0, False)
+    out = torch.empty((1, 2, 64), device="cuda")
+    for bad in (dict(q=w.q), dict(q=g.q.double()), dict(q=g.q[:, :1]), dict(priv=w.priv), dict(pub=w.pub), dict(out=out.cpu()), dict(out=out[:, :1])):
+        a = dict(dict(q=g.q, priv=g.priv, pub=g.pub, out=out), **bad)
+        with pytest.raises(ValueError):
+            spd.spd_decode_step_scored(shape, score, a["q"], a["priv"], a["pub"], a["out"], ws)
 
 
 @pytest.mark.parametrize("cap,scale", [(50.0, 1 / 16), (51.0, 64 ** -0.5), (100.0, 64 ** -0.5), (1000.0, 64 ** -0.5), (50.0, 1e-4), (0.01, 1.0), (1e-3, 3.0),

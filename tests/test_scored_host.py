@@ -79,6 +79,7 @@ def test_append_arguments_are_checked(lib):
                 dict(tok=spd.Tokens(P, P, P, 8 * 64 + 8, 0, 0), q_out=P),            # in place over strided rows
                 dict(tok=spd.Tokens(P, P, P, 0, 2 * 64 + 8, 0), k_out=P),
                 dict(base=P + 256, new_lens=P + 256),                                  # lengths written over the positions' base
+                dict(ip=P, pos=P + 512, new_lens=P + 512),                             # ... over positions that others still read
                 dict(rope=None), dict(rope=None, q_out=None, pos=P), dict(k_out=P + 4)):
         assert call(**bad) == INVALID, bad
     for bad in (dict(rope=dict(good, rotary_dim=80)), dict(rope=dict(good, rotary_dim=24)), dict(rope=dict(good, rotary_dim=0)),
@@ -98,3 +99,14 @@ def test_reference_forms_agree_with_torch():
     s = 2.0 * torch.tanh(0.25 * q[4:, 1].double() @ k[4:, 0].double().T / 2.0) - 0.25 * (i[:, None] - i).abs()
     s = s.masked_fill((i < lo[:, None]) | (i > hi[:, None]), -torch.inf)
     assert torch.allclose(out[4:, 1], torch.softmax(s, -1) @ v[4:, 0].double())
+
+
+def test_python_wrappers_refuse_what_the_structs_would_bend():
+    """A window beyond 32 bits would wrap; addresses of host tensors would fault."""
+    for window in (1 << 31, 1 << 32, -(1 << 32)):
+        with pytest.raises(ValueError):
+            spd.make_score(window=window)
+    for call in (lambda: spd._rows(torch.zeros(5, 2, 64), 2, 64, 5, torch.float32), lambda: spd._i32(torch.zeros(3, dtype=torch.int32), 3),
+                 lambda: spd._packed(torch.zeros(8), 8)):
+        with pytest.raises(ValueError):
+            call()
