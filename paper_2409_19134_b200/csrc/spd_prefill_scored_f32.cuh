@@ -2,12 +2,13 @@
 //
 // A CTA owns 16 RPT query rows of one (user, head) and walks key blocks through shared memory; 256 threads as 16 x 16, a thread
 // holding RPT rows x KB / 16 keys of S and RPT rows x D / 16 channels of O in registers, so that an operand read from shared
-// memory serves several FMAs (per warp and 4 channels, RPT = 4: 12 wavefronts of shared memory for 64 FMA instructions).  The 16
+// memory serves several FMAs (shared memory brings a warp 4 bytes per lane and cycle, the same address or not: 32 cycles for 64 FMA
+// instructions per warp and 4 channels at RPT = 4, half the FMA rate at most).  The 16
 // threads of a row group sit in half a warp: row maxima and sums by shuffles, P through shared memory without a CTA
 // barrier.  The next block is fetched into registers under this one's arithmetic.  Bound by shared-memory reads and issue
 // together (75 % and 67 % of their peaks on long prompts: 4096 tokens, 16/4 heads, 26 TFLOP/s); small launches take RPT = 2 for twice
 // the CTAs (4 prompts of 256 tokens, 8 heads, head_dim 64: 30 us).  8 x 4 tiles by 64 or 128 threads with asynchronous copies
-// were no faster (35 us, 25 TFLOP/s).
+// were no faster (35 us, 25 TFLOP/s), nor were FMAs two at a time (30.8 us, 26.1 TFLOP/s): instructions are not what it waits for.
 #pragma once
 
 #include "spd_prefill_scored.cuh"
