@@ -59,14 +59,17 @@ struct StPlan {
     int32_t fulllo, fullhi;         // keys that every row sees
     int32_t poisoned;               // a V row that is not finite is hidden from some rows and visible to others
     int32_t ahead;                  // some row sees keys ahead of it (a prefix)
+    float slope2[2];                // distance bias of each tile's head, log2 units
+    alignas(16) float bias[2][kStKeys];     // ... of the keys of a block: slope x
     StBlockStats stats[8];          // per softmax warp
     int2 span[256];                 // [tile][row]: first and last key the row sees
 };
 constexpr int kStBarBytes = 320;
 constexpr int kStStage = 4096;      // bytes per softmax warp for its way out: 32 rows x 32 fp32
 constexpr size_t st_smem_bytes(int D) {
-    return 2 * static_cast<size_t>(st_qtile(D)) + 2 * st_slots(D) * static_cast<size_t>(st_tile(D)) + 8 * kStStage + kStBarBytes + 2 * sizeof(StPlan) + 2 * kStKeys * 4;
+    return 2 * static_cast<size_t>(st_qtile(D)) + 2 * st_slots(D) * static_cast<size_t>(st_tile(D)) + 8 * kStStage + kStBarBytes + 2 * sizeof(StPlan);
 }
+static_assert(st_smem_bytes(128) <= 232448, "shared memory of an SM");
 
 struct ScoredTcParams {
     ScoredPrefillParams s;
@@ -222,7 +225,6 @@ prefill_scored_tc_kernel(const __grid_constant__ ScoredTcParams p, const __grid_
     static_assert(NBARS * 8 + 4 <= kStBarBytes, "barrier block");
     uint32_t &tmem_slot = *reinterpret_cast<uint32_t *>(bars + NBARS);
     StPlan *plans = reinterpret_cast<StPlan *>(stage_all + 8 * kStStage + kStBarBytes);
-    uint8_t *bias_all = reinterpret_cast<uint8_t *>(plans + 2);      // [tile][key of a block]
     const int tid = threadIdx.x, wid = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31;
     const int hpc = p.heads_per_cta, hgroups = p.s.Hq / hpc, gq = p.s.Hq / p.s.Hkv;
     const int rows_item = hpc == 2 ? 128 : 256;
@@ -278,16 +280,9 @@ prefill_scored_tc_kernel(const __grid_constant__ ScoredTcParams p, const __grid_
             float l = 0.f, m = -INFINITY;                  // m: reference point in log2 units of the score
             int form = 1;                                  // the cap's form that would have served the block before
             // The bias without the row's own constant: with the scores of a block taken relative to -slope (row - kb), kb its first
-            // key, a key x places in counts slope x for every row, a table per head; the reference m moves into the next
-            // block's frame by a constant.
-            float slope2 = 0.f;
-            float *bias = reinterpret_cast<float *>(bias_all) + t * KB;
-            if constexpr (BIAS) {
-                slope2 = p.s.slopes[h] * kLog2e;
-                asm volatile("bar.sync %0, 128;" ::"r"(1 + t) : "memory");      // the tile's warps are done with the item before
-                if (row < KB) bias[row] = slope2 * static_cast<float>(row);
-                asm volatile("bar.sync %0, 128;" ::"r"(1 + t) : "memory");
-            }
+            // key, a key x places in counts slope x for every row, a table per head in the plan; the reference m moves into the
+            // next block's frame by a constant.
+            const float slope2 = BIAS ? pl.slope2[t] : 0.f, *bias = pl.bias[t];
             for (int j = my_a; j < my_b && ok; ++j) {
                 const int i = j - my_a, kb = kend - j * KB;
                 if constexpr (BIAS) m = i > 0 ? m + slope2 * static_cast<float>(KB) : m;
@@ -593,6 +588,8 @@ prefill_scored_tc_kernel(const __grid_constant__ ScoredTcParams p, const __grid_
             int next = 0;
             if (lane == 0) next = atomicAdd(&p.s.hdr[HDR_NEXT_ITEM], 1);
             const int blk = static_cast<int>(item / hgroups), h0 = static_cast<int>(item % hgroups) * hpc;
+            float slope2[2] = {0.f, 0.f};
+            if constexpr (BIAS) { slope2[0] = p.s.slopes[h0] * kLog2e; slope2[1] = p.s.slopes[h0 + hpc - 1] * kLog2e; }
             int user = 0, qb = 0, first = 0, len = 0;
             {                             // the user whose rows hold block blk; a prompt's blocks count from its end
                 const int src = __ffs(__ballot_sync(0xffffffffu, blk < inc)) - 1;
@@ -630,6 +627,13 @@ prefill_scored_tc_kernel(const __grid_constant__ ScoredTcParams p, const __grid_
                 if (lane == 0) pl.stats[w] = StBlockStats{a, b, c, d};
                 tlo[w >> 2] = min(tlo[w >> 2], a); thi[w >> 2] = max(thi[w >> 2], b);
                 fulllo = max(fulllo, c); fullhi = min(fullhi, d);
+            }
+            if constexpr (BIAS) {
+#pragma unroll
+                for (int t = 0; t < 2; ++t) {
+                    if (lane == 0) pl.slope2[t] = slope2[t];
+                    for (int x = lane; x < KB; x += 32) pl.bias[t][x] = slope2[t] * static_cast<float>(x);
+                }
             }
             if (lane == 0) {
                 const int key0 = min(tlo[0], tlo[1]), key1 = max(thi[0], thi[1]);
