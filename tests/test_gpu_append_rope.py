@@ -228,3 +228,49 @@ def test_side_stream_and_graph_replay(ragged):
         assert torch.equal(g.k_pool.cpu(), kp) and torch.equal(g.v_pool.cpu(), vp) and torch.equal(g.seq_lens.cpu(), lens)
         now = wl.PagedKV(kp, vp, part.page_indptr, part.page_indices, lens)
     assert spd.spd_query_device_status(ws, st) == (spd.SPD_OK, -1)
+
+
+def test_a_replayed_call_judges_its_users_afresh():
+    """Runs appended in place from a graph: a user refused for a bad page in one replay is served in the next once its table is mended."""
+    q, k, v, part, ip = make(3, 4, 2, 64, "bf16", [20, 20, 5], [3, 10, 0], seed=31)
+    g, shape = part.to("cuda"), spd.make_shape(3, 4, 2, 64, torch.bfloat16, 0.1)
+    ws, st, kg, vg, ipg = spd.alloc_workspace(shape), torch.cuda.Stream(), k.cuda(), v.cuda(), ip.cuda()
+    at = int(part.page_indptr[1]) + 1
+    g.page_indices[at] = -7
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=st):
+        spd.spd_append_kv_rope(shape, None, None, kg, vg, g, ws, tok_indptr=ipg, stream=st)
+    with torch.cuda.stream(st):
+        graph.replay()
+    torch.cuda.synchronize()
+    assert g.seq_lens.tolist() == [23, 10, 5]
+    g.page_indices[at] = part.page_indices[at]
+    g.seq_lens.copy_(part.seq_lens)
+    torch.cuda.synchronize()
+    with torch.cuda.stream(st):
+        graph.replay()
+    torch.cuda.synchronize()
+    kp, vp, lens = expect(part, ip, k, v)
+    assert g.seq_lens.tolist() == lens.tolist() == [23, 30, 5]
+    assert torch.equal(g.k_pool.cpu(), kp) and torch.equal(g.v_pool.cpu(), vp)
+    assert spd.spd_query_device_status(ws) == (4, 1)              # the first replay's, still to be read
+
+
+def test_positions_may_be_the_lengths_themselves():
+    """One token per user at the position its cache ends at: positions, seq_lens and new_lens one array, with and without offsets."""
+    for ragged in (False, True):
+        q, k, v, part, ip = make(5, 4, 2, 128, "bf16", [1] * 5, [0, 17, 3, 90, 1000], seed=32)
+        g, shape = part.to("cuda"), spd.make_shape(5, 4, 2, 128, torch.bfloat16, 0.1)
+        inv = (10000.0 ** (-torch.arange(64, dtype=torch.float64) / 64)).float()
+        ws, qo = spd.alloc_workspace(shape), torch.empty_like(q, device="cuda")
+        spd.spd_append_kv_rope(shape, spd.make_rope(inv.cuda()), q.cuda(), k.cuda(), v.cuda(), g, ws, q_out=qo,
+                               tok_indptr=ip.cuda() if ragged else None, positions=g.seq_lens)
+        assert g.seq_lens.tolist() == [1, 18, 4, 91, 1001] and spd.spd_query_device_status(ws) == (spd.SPD_OK, -1)
+        want = ref.rotate(q, part.seq_lens.double()[:, None].expand(-1, 64), inv, False)
+        assert bool(((qo.cpu().double() - want).abs() <= ref.rotate_bound(q, inv, False, torch.bfloat16, want)).all())
+        if ragged:
+            with pytest.raises(spd.SpdError):
+                other = g.seq_lens.clone()
+                spd.spd_append_kv_rope(shape, spd.make_rope(inv.cuda()), q.cuda(), k.cuda(), v.cuda(), g, ws, q_out=qo, tok_indptr=ip.cuda(),
+                                       positions=other, new_lens=other)
