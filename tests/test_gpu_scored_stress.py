@@ -249,3 +249,54 @@ def test_scored_call_behind_an_appending_launch():
         x = wl.Workload("grown", 3, 8, 2, 128, 16, torch.bfloat16, w.sm_scale, w.q, w.priv, grown)
         want, _, _, _, tol = ref.decode(x, 20.0, 64, None)
         close(outs[s], want, tol, s)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_more_users_than_a_cta_caches(dtype):
+    B, hq, hkv, d = 1500, 2, 1, 64
+    r = random.Random(5)
+    lin, lout = [r.choice([0, 1, 15, 16, 40, 90]) for _ in range(B)], [r.choice([0, 1, 17, 33]) for _ in range(B)]
+    w = workload(lin, lout, hq, hkv, d, dtype, 21)
+    g, shape, score, sl, ws = setup(w, 20.0, 30, True)
+    want, _, _, _, tol = ref.decode(w, 20.0, 30, sl)
+    out = torch.full((B, hq, d), float("nan"), device="cuda")
+    spd.spd_decode_step_scored(shape, score, g.q, g.priv, g.pub, out, ws)
+    assert spd.spd_query_device_status(ws) == (spd.SPD_OK, -1)
+    close(out, want, tol, "many users")
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_many_tiny_prompts(dtype):
+    r = random.Random(6)
+    lens = [r.choice([0, 0, 1, 2, 3, 5]) for _ in range(900)]
+    q, k, v, ip = prompts(lens, 2, 1, 64, dtype, 22)
+    want, tol = ref.prefill(q, k, v, lens, 64 ** -0.5, 0.0, 2, None, weight=P_WEIGHT[dtype])
+    out, status = run(q, k, v, ip, 64, window=2)
+    assert status == (spd.SPD_OK, -1)
+    close(out, want, tol, "tiny prompts")
+
+
+@pytest.mark.parametrize("dtype,cap,alibi", [("bf16", 0.0, True), ("bf16", 30.0, False), ("f32", 0.0, True)])
+def test_one_very_long_prompt(dtype, cap, alibi):
+    n, hq, hkv, d = 70001, 2, 1, 64
+    q, k, v, ip = prompts([n], hq, hkv, d, dtype, 23)
+    sl = slopes_of(hq) / 64 if alibi else None                     # down to 2^-14: the bias reaches over the whole prompt
+    rows = {0, 1, 79, 80, 4095, 32768, 65535, 65536, 69999, n - 1}
+    want, tol = ref.prefill(q, k, v, [n], d ** -0.5, cap, 0, sl, weight=P_WEIGHT[dtype], rows=rows)
+    out, status = run(q, k, v, ip, d, cap=cap, slopes=sl)
+    assert status == (spd.SPD_OK, -1)
+    at = sorted(rows)
+    close(out[at], want[at], tol[at], "long prompt")
+
+
+@pytest.mark.parametrize("dtype,cap,window,alibi", [("bf16", 0.0, 0, True), ("bf16", 50.0, 200000, False), ("f32", 20.0, 0, True)])
+def test_one_very_long_cache(dtype, cap, window, alibi):
+    w = workload([300007, 5], [13, 100], 4, 1, 64, dtype, 24)
+    g, shape, score, _, ws = setup(w, cap, window, False)
+    sl = slopes_of(4) / 4096 if alibi else None
+    score = spd.make_score(cap, window, None if sl is None else sl.cuda())
+    want, _, _, _, tol = ref.decode(w, cap, window, sl)
+    out = torch.full((2, 4, 64), float("nan"), device="cuda")
+    spd.spd_decode_step_scored(shape, score, g.q, g.priv, g.pub, out, ws)
+    assert spd.spd_query_device_status(ws) == (spd.SPD_OK, -1)
+    close(out, want, tol, "long cache")
