@@ -439,7 +439,7 @@ EncodeTiledFn tensor_map_encoder() { return encode_fn(); }
 int32_t next_call_id() { return next_epoch(); }
 void count_launch() { ++g_launches; }
 size_t flags_offset(int batch) { return ws_head(batch, 0).bad; }
-size_t flags_end(int batch) { return ws_head(batch, 0).tickets; }
+size_t cleared_end(int batch, int seqs) { return ws_head(batch, seqs).end; }
 
 }  // namespace host
 }  // namespace spd

@@ -23,7 +23,7 @@ EncodeTiledFn tensor_map_encoder();            // null if the driver has none
 int32_t next_call_id();                        // non-zero id of a call (flags in the workspace hold it)
 void count_launch();
 size_t flags_offset(int batch);                // per-user flags in the workspace
-size_t flags_end(int batch);                   // first byte behind them
+size_t cleared_end(int batch, int seqs);       // first byte behind what a status query clears after a call over so many sequences
 
 inline bool misaligned(const void *p, size_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) != 0; }
 

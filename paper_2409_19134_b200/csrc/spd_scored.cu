@@ -110,7 +110,8 @@ spd_status spd_append_kv_rope(const spd_shape *shape, const spd_rope *rope, int6
     const int64_t T = total_tokens;
     if (!tok || !page_indptr || !seq_lens || !ws || misaligned(ws, 256)) return SPD_ERR_INVALID_ARG;
     if (T < 0 || T >= (1ll << 31) || num_pages < 0 || (!tok_indptr && T != s.batch)) return SPD_ERR_INVALID_ARG;
-    if (ws_bytes < host::flags_end(s.batch)) return SPD_ERR_WORKSPACE;
+    const int g = s.num_q_heads / s.num_kv_heads, seqs = s.num_kv_heads * (g > kHeadsPerItem ? g / kHeadsPerItem : 1);
+    if (ws_bytes < host::cleared_end(s.batch, s.batch * seqs)) return SPD_ERR_WORKSPACE;
     if (T > 0 && (!tok->k || !tok->v || !k_pool || !v_pool || num_pages <= 0)) return SPD_ERR_INVALID_ARG;
     if (misaligned(tok->k, 16) || misaligned(tok->v, 16) || misaligned(k_pool, 128) || misaligned(v_pool, 128)) return SPD_ERR_INVALID_ARG;
     RopeAppendParams p{};
@@ -161,8 +162,7 @@ spd_status spd_append_kv_rope(const spd_shape *shape, const spd_rope *rope, int6
     p.hdr = static_cast<int32_t *>(ws);
     p.bad = reinterpret_cast<int32_t *>(static_cast<uint8_t *>(ws) + host::flags_offset(s.batch));
     p.epoch = host::next_call_id();
-    const int g = s.num_q_heads / s.num_kv_heads;
-    p.S = s.num_kv_heads * (g > kHeadsPerItem ? g / kHeadsPerItem : 1);
+    p.S = seqs;
     int sms = 0;
     if ((rc = host::device_sms(&sms)) != SPD_OK) return rc;
     cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);

@@ -86,6 +86,12 @@ def test_append_arguments_are_checked(lib):
                 dict(rope=dict(good, num_axes=5), pos=P), dict(rope=dict(good, num_axes=0))):
         assert call(**bad) == UNSUPPORTED, bad
     assert call(size=1024) == WORKSPACE
+    # a workspace that ends where the status query would still clear (flags of 2 users, then tickets of 4 sequences) is too small
+    sizes = [n for n in range(0, 1 << 20, 256) if call(size=n, rope=dict(good, rotary_dim=64), k_out=P + 4) == WORKSPACE]
+    assert call(size=sizes[-1] + 256, k_out=P + 4) == INVALID
+    small, large = spd.make_shape(2, 2, 2, 64, torch.bfloat16, 0.125), spd.make_shape(2, 512, 512, 64, torch.bfloat16, 0.125)
+    assert call(size=sizes[-1] + 256, shape=small, k_out=P + 4) == INVALID
+    assert call(size=sizes[-1] + 256, shape=large, k_out=P + 4) == WORKSPACE
 
 
 def test_reference_forms_agree_with_torch():
