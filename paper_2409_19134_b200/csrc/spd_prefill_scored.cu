@@ -99,29 +99,33 @@ spd_status prefill_tc(const spd_shape &s, const ScoredPrefillParams &sp, cudaStr
     return SPD_ERR_UNSUPPORTED;
 }
 
-template <int D, int RPT>
+template <int D, int RPT, int G>
 spd_status launch_prefill_f32(const spd_shape &s, const ScoredPrefillParams &p, cudaStream_t st) {
-    using C = ScoredF32<D, RPT>;
+    using C = ScoredF32<D, RPT, G>;
     static std::once_flag once[64];
     int dev = 0;
     cudaGetDevice(&dev);
     cudaError_t err = cudaSuccess;
     std::call_once(once[dev & 63], [&] {
-        err = cudaFuncSetAttribute(prefill_scored_f32_kernel<D, RPT>, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(C::smem_bytes()));
+        err = cudaFuncSetAttribute(prefill_scored_f32_kernel<D, RPT, G>, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(C::smem_bytes()));
     });
     if (err != cudaSuccess) return SPD_ERR_CUDA;
     const dim3 grid(static_cast<unsigned>((p.T + C::R - 1) / C::R + s.batch), static_cast<unsigned>(s.num_q_heads));
-    prefill_scored_f32_kernel<D, RPT><<<grid, 256, C::smem_bytes(), st>>>(p);
+    prefill_scored_f32_kernel<D, RPT, G><<<grid, 256 * G, C::smem_bytes(), st>>>(p);
     host::count_launch();
     return cudaGetLastError() == cudaSuccess ? SPD_OK : SPD_ERR_CUDA;
 }
 
-// fp32 prompts on the FMA pipes: four rows per thread, two where that leaves SMs without work.
+// fp32 prompts on the FMA pipes: four rows per thread, two where that leaves SMs without work or prompts do not fill 64 rows; two
+// groups of threads per tile where the keys of a row, not the number of tiles, are what an SM's work consists of.  us, two rows / four /
+// four and two groups, 8 heads of 64: 2 x 256 tokens 19.1 / 26.2 / 24.4, 200 x 20 53 / 70 / 107, 4 x 256 30.2 / 41.2 / 25.1, 2 x 1000
+// 149 / 152 / 129, 4 x 1000 255 / 217 / 205, 16 x 1000 846 / 634 / 683, 64 x 256 271 / 208 / 256.
 spd_status prefill_f32(const spd_shape &s, const ScoredPrefillParams &p, int sms, cudaStream_t st) {
     if (s.num_q_heads > 65535) return SPD_ERR_UNSUPPORTED;
-    const bool small = (p.T + 63) / 64 * s.num_q_heads < 2 * static_cast<int64_t>(sms);
-    if (s.head_dim == 128) return small ? launch_prefill_f32<128, 2>(s, p, st) : launch_prefill_f32<128, 4>(s, p, st);
-    return small ? launch_prefill_f32<64, 2>(s, p, st) : launch_prefill_f32<64, 4>(s, p, st);
+    const int64_t tiles = (p.T + 63) / 64 * s.num_q_heads, mean = p.T / s.batch;
+    if (2 * tiles <= sms || mean <= 32) return s.head_dim == 128 ? launch_prefill_f32<128, 2, 1>(s, p, st) : launch_prefill_f32<64, 2, 1>(s, p, st);
+    if (tiles * 128 < sms * mean) return s.head_dim == 128 ? launch_prefill_f32<128, 4, 2>(s, p, st) : launch_prefill_f32<64, 4, 2>(s, p, st);
+    return s.head_dim == 128 ? launch_prefill_f32<128, 4, 1>(s, p, st) : launch_prefill_f32<64, 4, 1>(s, p, st);
 }
 
 }  // namespace

@@ -6,30 +6,52 @@
 // instructions per warp and 4 channels at RPT = 4, half the FMA rate at most).  The 16
 // threads of a row group sit in half a warp: row maxima and sums by shuffles, P through shared memory without a CTA
 // barrier.  The next block is fetched into registers under this one's arithmetic.  Bound by shared-memory reads and issue
-// together (75 % and 67 % of their peaks on long prompts: 4096 tokens, 16/4 heads, 26 TFLOP/s); small launches take RPT = 2 for twice
-// the CTAs (4 prompts of 256 tokens, 8 heads, head_dim 64: 30 us).  8 x 4 tiles by 64 or 128 threads with asynchronous copies
-// were no faster (35 us, 25 TFLOP/s), nor were FMAs two at a time (30.8 us, 26.1 TFLOP/s): instructions are not what it waits for.
+// together (75 % and 67 % of their peaks on long prompts: 4096 tokens, 16/4 heads, 27.5 TFLOP/s).  Small launches take RPT = 2 for twice
+// the CTAs, or G = 2: two groups of 256 threads share a tile's rows, take its key blocks in turns and join at the end, which halves
+// the chain of blocks (4 prompts of 256 tokens, 8 heads, head_dim 64: 25 us; 30 with RPT = 2, 41 with RPT = 4 alone, 31 with both).
+// 8 x 4 tiles by 64 or 128 threads with asynchronous copies were no faster (35 us, 25 TFLOP/s), nor were FMAs two at a time
+// (30.8 us, 26.1 TFLOP/s): instructions are not what it waits for.
 #pragma once
 
 #include "spd_prefill_scored.cuh"
 
 namespace spd {
 
-template <int D, int RPT>
+// G: groups of 256 threads that share the rows and take key blocks in turns.
+template <int D, int RPT, int G>
 struct ScoredF32 {
     static constexpr int R = 16 * RPT, KB = 4096 / D, KPT = KB / 16, CPT = D / 16, QP = D + 4, PP = KB + 4;
-    static constexpr int kFloats = R * QP + KB * QP + KB * D + R * PP;
+    static constexpr int kGroupFloats = KB * QP + KB * D + R * PP, kFloats = R * QP + G * kGroupFloats;
+    static_assert(kGroupFloats >= R * D + 2 * R, "a group's tiles hold its result for the join");
     static constexpr size_t smem_bytes() { return kFloats * 4 + 2 * R * 4; }
 };
 
-template <int D, int RPT>
-__global__ void __launch_bounds__(256, 2) prefill_scored_f32_kernel(const __grid_constant__ ScoredPrefillParams p) {
-    using C = ScoredF32<D, RPT>;
+template <int G>
+__device__ __forceinline__ void f32_group_sync(int grp) {
+    if constexpr (G == 1) __syncthreads();
+    else asm volatile("bar.sync %0, 256;" ::"r"(1 + grp) : "memory");
+}
+template <int G>
+__device__ __forceinline__ bool f32_group_any(int grp, bool x) {
+    if constexpr (G == 1) {
+        return __syncthreads_or(x);
+    } else {
+        uint32_t r;
+        asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %1, 0;\n\tbar.red.or.pred q, %2, 256, p;\n\tselp.u32 %0, 1, 0, q;\n\t}"
+                     : "=r"(r) : "r"(static_cast<uint32_t>(x)), "r"(1 + grp) : "memory");
+        return r != 0;
+    }
+}
+
+template <int D, int RPT, int G>
+__global__ void __launch_bounds__(256 * G, 2 / G) prefill_scored_f32_kernel(const __grid_constant__ ScoredPrefillParams p) {
+    using C = ScoredF32<D, RPT, G>;
     constexpr int R = C::R, KB = C::KB, KPT = C::KPT, CPT = C::CPT, QP = C::QP, PP = C::PP, LD = KB * D / 4 / 256;   // float4 loads per thread and tile
     extern __shared__ __align__(16) float sm[];
-    float *Qs = sm, *Ks = Qs + R * QP, *Vs = Ks + KB * QP, *Ps = Vs + KB * D;
-    int32_t *rlo = reinterpret_cast<int32_t *>(Ps + R * PP), *rhi = rlo + R;
-    const int tid = threadIdx.x, lane = tid & 31, tx = tid & 15, ty = tid >> 4;
+    const int grp = G == 1 ? 0 : threadIdx.x >> 8;
+    float *Qs = sm, *Ks = Qs + R * QP + grp * C::kGroupFloats, *Vs = Ks + KB * QP, *Ps = Vs + KB * D;
+    int32_t *rlo = reinterpret_cast<int32_t *>(sm + C::kFloats), *rhi = rlo + R;
+    const int tid = threadIdx.x & 255, lane = tid & 31, tx = tid & 15, ty = tid >> 4;
     const int h = blockIdx.y, kvh = h / (p.Hq / p.Hkv);
     if (blockIdx.x == 0 && blockIdx.y == 0) scored_check_offsets(p);
     int qb, first, len;
@@ -37,16 +59,15 @@ __global__ void __launch_bounds__(256, 2) prefill_scored_f32_kernel(const __grid
     if (qb < 0) return;                              // uniform over the CTA
     const int prefix = scored_prefix(p, first, len, lane), row0 = qb * R;
     const float *q = static_cast<const float *>(p.q), *k = static_cast<const float *>(p.k), *v = static_cast<const float *>(p.v);
-    for (int x = tid; x < R * D / 4; x += 256) {
+    for (int x = threadIdx.x; x < R * D / 4; x += 256 * G) {
         const int r = x / (D / 4), c = x % (D / 4);
         const float4 val = row0 + r < len ? *reinterpret_cast<const float4 *>(q + (first + row0 + r) * p.q_stride + h * D + 4 * c) : make_float4(0.f, 0.f, 0.f, 0.f);
         *reinterpret_cast<float4 *>(Qs + r * QP + 4 * c) = val;
     }
     int lo = 0x7fffffff, hi = -1;                    // a thread below R looks after row tid
     if (tid < R && row0 + tid < len) scored_interval(p, first, prefix, row0 + tid, lo, hi);
-    const bool live = tid < R && row0 + tid < len;
     if (lo > hi) { lo = 0x7fffffff; hi = -1; }
-    if (tid < R) { rlo[tid] = lo; rhi[tid] = hi; }
+    if (threadIdx.x < R) { rlo[tid] = lo; rhi[tid] = hi; }
     __syncthreads();
     // keys that any row sees, and that every live row sees
     int key0 = 0x7fffffff, key1 = -1, full0 = -1, full1 = 0x7fffffff;
@@ -56,7 +77,6 @@ __global__ void __launch_bounds__(256, 2) prefill_scored_f32_kernel(const __grid
     }
     key0 = __reduce_min_sync(0xffffffffu, key0); key1 = __reduce_max_sync(0xffffffffu, key1);
     full0 = __reduce_max_sync(0xffffffffu, full0); full1 = __reduce_min_sync(0xffffffffu, full1);
-    (void)live;
     const float slope = p.slopes ? p.slopes[h] : 0.f;
     int mylo[RPT], myhi[RPT];
     float m[RPT], l[RPT], o[RPT][CPT];
@@ -77,10 +97,11 @@ __global__ void __launch_bounds__(256, 2) prefill_scored_f32_kernel(const __grid
             vn[x] = in ? *reinterpret_cast<const float4 *>(v + (first + kb + key) * p.v_stride + kvh * D + 4 * c) : make_float4(0.f, 0.f, 0.f, 0.f);
         }
     };
-    if (key1 >= 0) fetch(key0);
-    for (int kb = key0; kb <= key1; kb += KB) {
+    const int start = key1 < 0 ? 0 : key0 + grp * KB;
+    if (start <= key1) fetch(start);
+    for (int kb = start; kb <= key1; kb += G * KB) {
         const bool hidden = !(full0 <= kb && kb + KB - 1 <= full1);     // some row does not see all of this block
-        __syncthreads();                             // the previous block's readers are done
+        f32_group_sync<G>(grp);                      // the previous block's readers are done
         bool odd = false;
 #pragma unroll
         for (int x = 0; x < LD; ++x) {
@@ -90,8 +111,8 @@ __global__ void __launch_bounds__(256, 2) prefill_scored_f32_kernel(const __grid
             odd = odd || !(isfinite(vn[x].x) && isfinite(vn[x].y) && isfinite(vn[x].z) && isfinite(vn[x].w));
         }
         // 0 * NaN is NaN: where a hidden key's V row may not be finite, hidden keys are left out one by one
-        const bool careful = __syncthreads_or(odd) && hidden;
-        if (kb + KB <= key1) fetch(kb + KB);
+        const bool careful = f32_group_any<G>(grp, odd) && hidden;
+        if (kb + G * KB <= key1) fetch(kb + G * KB);
         float s[RPT][KPT];
 #pragma unroll
         for (int r = 0; r < RPT; ++r)
@@ -178,6 +199,32 @@ __global__ void __launch_bounds__(256, 2) prefill_scored_f32_kernel(const __grid
                 }
         }
         __syncwarp();
+    }
+    if constexpr (G == 2) {                          // the second group's result into its tiles, and joined by the first
+        __syncthreads();
+        float *po = sm + R * QP + C::kGroupFloats, *pm = po + R * D, *pl = pm + R;
+#pragma unroll
+        for (int r = 0; r < RPT; ++r) {
+            const int row = ty * RPT + r;
+            if (grp == 1) {
+#pragma unroll
+                for (int c = 0; c < CPT; ++c) po[row * D + 16 * (c & ~3) + 4 * tx + (c & 3)] = o[r][c];
+                if (tx == 0) { pm[row] = m[r]; pl[row] = l[r]; }
+            }
+        }
+        __syncthreads();
+        if (grp == 1) return;
+#pragma unroll
+        for (int r = 0; r < RPT; ++r) {
+            const int row = ty * RPT + r;
+            const float m1 = pm[row], l1 = pl[row], M = fmaxf(m[r], m1);
+            // a side that saw nothing weighs nothing; one whose scores were all NaN has no maximum either, but a sum that is NaN
+            const float a0 = m[r] == -INFINITY ? (l[r] != l[r] ? 1.f : 0.f) : expf(m[r] - M);
+            const float a1 = m1 == -INFINITY ? (l1 != l1 ? 1.f : 0.f) : expf(m1 - M);
+            l[r] = l[r] * a0 + l1 * a1;
+#pragma unroll
+            for (int c = 0; c < CPT; ++c) o[r][c] = o[r][c] * a0 + po[row * D + 16 * (c & ~3) + 4 * tx + (c & 3)] * a1;
+        }
     }
 #pragma unroll
     for (int r = 0; r < RPT; ++r) {

@@ -300,3 +300,33 @@ def test_one_very_long_cache(dtype, cap, window, alibi):
     spd.spd_decode_step_scored(shape, score, g.q, g.priv, g.pub, out, ws)
     assert spd.spd_query_device_status(ws) == (spd.SPD_OK, -1)
     close(out, want, tol, "long cache")
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("lens,hq,hkv", [([300, 129, 0, 200, 257], 8, 2), ([70] * 40, 4, 4), ([9, 31, 1, 0, 25] * 12, 8, 8)])
+def test_fp32_tiles_of_every_kind(lens, hq, hkv, d):
+    """The three shapes of the fp32 kernel: two groups of threads per tile, one group, and half tiles; what is hidden is spoiled, and a
+    visible key that is NaN spoils exactly the rows that see it."""
+    T = sum(lens)
+    q, k, v, ip = prompts(lens, hq, hkv, d, "f32", 80)
+    doc = documents(lens, 81, longest=90)
+    prefix = torch.tensor([n // 3 for n in lens], dtype=torch.int32)
+    rows = set(random.Random(1).sample(range(T), min(T, 150)))
+    for kw in (dict(cap=15.0, slopes=slopes_of(hq)), dict(window=70, prefix=prefix), dict(doc=doc)):
+        want, tol = ref.prefill(q, k, v, lens, d ** -0.5, kw.get("cap", 0.0), kw.get("window", 0), kw.get("slopes"), kw.get("prefix"), kw.get("doc"), rows=rows)
+        out, status = run(q, k, v, ip, d, kw.get("cap", 0.0), kw.get("window", 0), kw.get("slopes"), kw.get("prefix"), kw.get("doc"))
+        assert status == (spd.SPD_OK, -1)
+        at = sorted(rows)
+        close(out[at], want[at], tol[at], kw.keys())
+    # one spoiled key in the longest prompt: causal rows in front of it are as before, rows from it on are NaN
+    clean, _ = run(q, k, v, ip, d)
+    u = max(range(len(lens)), key=lambda i: lens[i])
+    t0, bad = int(ip[u]), lens[u] // 2
+    for spoil in ("k", "v"):
+        k2, v2 = k.clone(), v.clone()
+        (k2 if spoil == "k" else v2)[t0 + bad] = float("nan")
+        out, _ = run(q, k2, v2, ip, d)
+        hit = torch.zeros(T, dtype=torch.bool)
+        hit[t0 + bad:t0 + lens[u]] = True
+        assert bool(out[hit.cuda()].isnan().all()), spoil
+        assert torch.equal(out[~hit.cuda()], clean[~hit.cuda()]), spoil
