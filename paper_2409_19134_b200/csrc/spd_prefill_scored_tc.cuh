@@ -27,7 +27,8 @@
 // head_dim 128, bf16: 8192 tokens x 32/8 heads plain 447 us (1230 TFLOP/s of visible pairs), capped 580 (948), distance bias 545
 // (1008); 8 prompts of 2 to 8 k tokens 1.85 ms (1260); 3 prompts with prefix and window 124 us (915).
 // Slower here: the tiles' exponentials in turns by named barriers (20 %), two threads per row (instruction issue, 15 %), the next
-// block's scores prepared in registers under this block's exponentials (60 %; the compiler serialises them).
+// block's scores prepared in registers under this block's exponentials (60 %; the compiler serialises them), barriers of its own for
+// each tile's Q, which lets the tiles drift apart (4 % with caps).
 #pragma once
 
 #include "spd_prefill_scored.cuh"

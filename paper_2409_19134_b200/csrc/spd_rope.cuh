@@ -270,7 +270,7 @@ __global__ void __launch_bounds__(kRopeThreads, 4) append_rope_kernel(const __gr
             const int64_t n = consistent ? p.tok_indptr[u + 1] - p.tok_indptr[u] : 0;
             int64_t lo, held;
             const bool flagged = __ldcg(p.bad + u) == p.epoch, ok = rope_user_room(p, u, n, lo, held) && !flagged;
-            if (flagged) p.bad[u] = 0;         // a captured call keeps its id: the next replay judges afresh
+            if (flagged) p.bad[u] = 0;         // a captured call keeps its id: the next replay starts without it
             if (!ok && n == 0 && consistent) flag_error(p.hdr, 4 /* SPD_ERR_BAD_PAGE */, u);    // an inconsistent table
             p.new_lens[u] = static_cast<int32_t>(held + (ok ? n : 0));
         }

@@ -230,7 +230,7 @@ def test_side_stream_and_graph_replay(ragged):
     assert spd.spd_query_device_status(ws, st) == (spd.SPD_OK, -1)
 
 
-def test_a_replayed_call_judges_its_users_afresh():
+def test_a_replayed_call_starts_without_old_flags():
     """Runs appended in place from a graph: a user refused for a bad page in one replay is served in the next once its table is mended."""
     q, k, v, part, ip = make(3, 4, 2, 64, "bf16", [20, 20, 5], [3, 10, 0], seed=31)
     g, shape = part.to("cuda"), spd.make_shape(3, 4, 2, 64, torch.bfloat16, 0.1)
