@@ -488,7 +488,8 @@ def make_score(logit_cap: float = 0.0, window: int = 0, alibi_slopes: Optional[t
         raise ValueError("the window is a 32-bit number")
     sc = Score(float(logit_cap), int(window), None)
     if alibi_slopes is not None:
-        assert alibi_slopes.dtype == torch.float32 and alibi_slopes.is_contiguous() and alibi_slopes.is_cuda
+        if alibi_slopes.dtype is not torch.float32 or not alibi_slopes.is_contiguous() or not alibi_slopes.is_cuda:
+            raise ValueError(f"slopes are contiguous float32 on the device, got {alibi_slopes.dtype} on {alibi_slopes.device}")
         sc.alibi_slopes = alibi_slopes.data_ptr()
         sc._keep = alibi_slopes
     return sc
@@ -496,7 +497,8 @@ def make_score(logit_cap: float = 0.0, window: int = 0, alibi_slopes: Optional[t
 
 def make_rope(inv_freq: torch.Tensor, interleaved: bool = False, sections=None, scale: float = 1.0) -> Rope:
     """Rotation of spd_append_kv_rope; inv_freq: float32 [rotary_dim / 2] on the device; sections: pairs per position axis."""
-    assert inv_freq.dtype == torch.float32 and inv_freq.is_contiguous() and inv_freq.is_cuda and inv_freq.dim() == 1
+    if inv_freq.dtype is not torch.float32 or not inv_freq.is_contiguous() or not inv_freq.is_cuda or inv_freq.dim() != 1:
+        raise ValueError(f"inv_freq is contiguous float32 [rotary_dim / 2] on the device, got {inv_freq.dtype} {list(inv_freq.shape)} on {inv_freq.device}")
     rope = Rope(2 * inv_freq.numel(), 1 if interleaved else 0, len(sections) if sections else 1, _Sections(*(sections or ())),
                 float(scale), inv_freq.data_ptr())
     rope._keep = inv_freq
@@ -505,30 +507,39 @@ def make_rope(inv_freq: torch.Tensor, interleaved: bool = False, sections=None, 
 
 _TORCH_DTYPES = {SPD_F32: torch.float32, SPD_BF16: torch.bfloat16}
 
-
-def _here(t: torch.Tensor) -> None:
-    """The tensors of a call live on the current device, whose stream and context the call uses."""
-    if not t.is_cuda or t.get_device() != torch._C._cuda_getDevice():
-        raise ValueError(f"tensor on {t.device}, which is not the current CUDA device")
+# Checks of the tensors whose addresses a call hands over.  `dev` is the device that the call runs on; an address on another device or
+# on the host, or a tensor smaller than the kernels read or write, would fault there.
 
 
-def _host(t: torch.Tensor) -> ValueError:
+def _elsewhere(t: torch.Tensor) -> ValueError:
     return ValueError(f"expected a tensor on the current CUDA device, got one on {t.device}")
 
 
-def _slopes(shape, score) -> None:
+def _here(t: torch.Tensor) -> int:
+    """The tensors of a call live on the current device, whose stream and context the call uses; its index."""
+    if not t.is_cuda or t.get_device() != torch._C._cuda_getDevice():
+        raise _elsewhere(t)
+    return t.get_device()
+
+
+def _slopes(shape, score, dev) -> None:
     keep = getattr(score, "_keep", None)
-    assert keep is None or keep.numel() == shape.num_q_heads, "one slope per query head"
+    if keep is None:
+        return
+    if keep.numel() != shape.num_q_heads:
+        raise ValueError(f"one slope per query head: expected {shape.num_q_heads}, got {keep.numel()}")
+    if keep.get_device() != dev:
+        raise _elsewhere(keep)
 
 
-def _rows(t: torch.Tensor, heads: int, d: int, n: int, dtype):
+def _rows(t: torch.Tensor, heads: int, d: int, n: int, dtype, dev=None):
     """(pointer, token stride in elements) of [n, heads, d] rows that may be part of a wider row per token."""
     if t.dtype is not dtype or t.shape != (n, heads, d):
         raise ValueError(f"expected {dtype} [{n}, {heads}, {d}], got {t.dtype} {list(t.shape)}")
     if n == 0:
         return None, 0
-    if not t.is_cuda:
-        raise _host(t)
+    if t.get_device() != dev:
+        raise _elsewhere(t)
     if t.is_contiguous():
         return t.data_ptr(), 0
     s0, s1, s2 = t.stride()
@@ -539,81 +550,109 @@ def _rows(t: torch.Tensor, heads: int, d: int, n: int, dtype):
     return t.data_ptr(), s0 if n > 1 else 0
 
 
-def _i32(t: Optional[torch.Tensor], *size) -> Optional[int]:
+def _i32(t: Optional[torch.Tensor], *size, dev=None) -> Optional[int]:
     """Pointer of a contiguous int32 tensor of the given shape, or None."""
     if t is None:
         return None
     if t.dtype is not torch.int32 or t.shape != size or not t.is_contiguous():
         raise ValueError(f"expected contiguous int32 {list(size)}, got {t.dtype} {list(t.shape)}")
-    if not t.is_cuda:
-        raise _host(t)
+    if t.get_device() != dev:
+        raise _elsewhere(t)
     return t.data_ptr()
 
 
-def _packed(t: Optional[torch.Tensor], numel: int, dtype=None) -> Optional[int]:
+def _packed(t: Optional[torch.Tensor], numel: int, dtype=None, dev=None) -> Optional[int]:
     """Pointer of a contiguous tensor of `numel` elements, or None."""
     if t is None:
         return None
     if t.numel() != numel or not t.is_contiguous() or (dtype is not None and t.dtype is not dtype):
         raise ValueError(f"expected a contiguous tensor of {numel} elements, got {t.dtype} {list(t.shape)}")
-    if not t.is_cuda:
-        raise _host(t)
+    if t.get_device() != dev:
+        raise _elsewhere(t)
     return t.data_ptr() if numel else None
 
 
-def _query(shape, q, *parts) -> None:
-    """One packed query row per user and head; the partitions where it is."""
-    _here(q)
-    _packed(q, shape.batch * shape.num_q_heads * shape.head_dim, _TORCH_DTYPES[shape.dtype])
-    for part in parts:
-        if not part.seq_lens.is_cuda:
-            raise _host(part.seq_lens)
+def _workspace(ws: torch.Tensor, dev):
+    """(pointer, bytes) of a workspace."""
+    if ws.dtype is not torch.uint8 or not ws.is_contiguous():
+        raise ValueError(f"a workspace is a contiguous uint8 tensor, got {ws.dtype}")
+    if ws.get_device() != dev:
+        raise _elsewhere(ws)
+    return ws.data_ptr(), ws.numel()
+
+
+def _partition(shape, part, dev):
+    """The fields of PagedKV, in order: pools as the shape says, a table and a length per user."""
+    kp, vp, indptr, indices, lens = part.k_pool, part.v_pool, part.page_indptr, part.page_indices, part.seq_lens
+    pages, dtype, B = kp.shape[0], _TORCH_DTYPES[shape.dtype], shape.batch
+    n = pages * shape.num_kv_heads * shape.page_size * shape.head_dim
+    if not (kp.dtype is dtype and vp.dtype is dtype and kp.numel() == n and vp.numel() == n and kp.is_contiguous() and vp.is_contiguous()):
+        raise ValueError(f"expected contiguous {dtype} pools [{pages}, {shape.num_kv_heads}, {shape.page_size}, {shape.head_dim}], got "
+                         f"{kp.dtype} {list(kp.shape)} and {vp.dtype} {list(vp.shape)}")
+    if not (indptr.dtype is _I32 and indices.dtype is _I32 and lens.dtype is _I32 and indptr.numel() == B + 1 and lens.numel() == B and
+            indptr.is_contiguous() and indices.is_contiguous() and lens.is_contiguous()):
+        raise ValueError(f"expected contiguous int32 page_indptr [{B + 1}], page_indices and seq_lens [{B}], got {indptr.dtype} "
+                         f"{list(indptr.shape)}, {indices.dtype} and {lens.dtype} {list(lens.shape)}")
+    for t in (kp, vp, indptr, indices, lens):
+        if t.get_device() != dev:
+            raise _elsewhere(t)
+    return (kp.data_ptr() if pages else None, vp.data_ptr() if pages else None, pages, indptr.data_ptr(),
+            indices.data_ptr() if indices.numel() else None, lens.data_ptr())
+
+
+def _query(shape, q) -> int:
+    """One packed query row per user and head; the device of the call."""
+    dev = _here(q)
+    _packed(q, shape.batch * shape.num_q_heads * shape.head_dim, _TORCH_DTYPES[shape.dtype], dev)
+    return dev
+
+
+def _partial(shape, part, dev) -> Partial:
+    rows = shape.batch * shape.num_q_heads
+    return Partial(_packed(part[0], rows * shape.head_dim, torch.float32, dev), _packed(part[1], rows, torch.float32, dev),
+                   _packed(part[2], rows, torch.float32, dev))
 
 
 def spd_partial_attn_scored(shape, score, q, priv, pub_lens, out, ws, plan=SPD_PLAN_PER_CALL, stream=None) -> None:
     """spd_partial_attn with score options; pub_lens: int32 [batch], tokens in the public partition."""
-    _slopes(shape, score)
-    _query(shape, q, priv)
-    kv = paged_kv(priv)
-    part = Partial(out[0].data_ptr(), out[1].data_ptr(), out[2].data_ptr())
-    _check(lib().spd_partial_attn_scored(shape, score, q.data_ptr(), kv, _i32(pub_lens, shape.batch), part, plan, ws.data_ptr(), ws.numel(),
+    dev = _query(shape, q)
+    _slopes(shape, score, dev)
+    kv, part = PagedKV(*_partition(shape, priv, dev)), _partial(shape, out, dev)
+    _check(lib().spd_partial_attn_scored(shape, score, q.data_ptr(), kv, _i32(pub_lens, shape.batch, dev=dev), part, plan, *_workspace(ws, dev),
                                          _stream_ptr(stream)), "spd_partial_attn_scored")
 
 
 def spd_service_attn_merge_scored(shape, score, q, pub, priv_lens, partial_in, out, ws, plan=SPD_PLAN_PER_CALL, stream=None) -> None:
     """spd_service_attn_merge with score options; priv_lens: int32 [batch], tokens in the private partition."""
-    _slopes(shape, score)
-    _query(shape, q, pub)
-    _packed(out, q.numel())
-    kv = paged_kv(pub)
-    part = Partial(partial_in[0].data_ptr(), partial_in[1].data_ptr(), partial_in[2].data_ptr())
-    _check(lib().spd_service_attn_merge_scored(shape, score, q.data_ptr(), kv, _i32(priv_lens, shape.batch), part, out.data_ptr(),
-                                               _dtype_code(out.dtype), plan, ws.data_ptr(), ws.numel(), _stream_ptr(stream)),
-           "spd_service_attn_merge_scored")
+    dev = _query(shape, q)
+    _slopes(shape, score, dev)
+    kv, part = PagedKV(*_partition(shape, pub, dev)), _partial(shape, partial_in, dev)
+    _check(lib().spd_service_attn_merge_scored(shape, score, q.data_ptr(), kv, _i32(priv_lens, shape.batch, dev=dev), part,
+                                               _packed(out, q.numel(), dev=dev), _dtype_code(out.dtype), plan, *_workspace(ws, dev),
+                                               _stream_ptr(stream)), "spd_service_attn_merge_scored")
 
 
 def spd_decode_step_scored(shape, score, q, priv, pub, out, ws, plan=SPD_PLAN_PER_CALL, stream=None) -> None:
     """The fused decode step with score options (make_score) over both partitions."""
-    _slopes(shape, score)
-    _query(shape, q, priv, pub)
-    _packed(out, q.numel())
-    a, b = paged_kv(priv), paged_kv(pub)
-    _check(lib().spd_decode_step_scored(shape, score, q.data_ptr(), a, b, out.data_ptr(), _dtype_code(out.dtype), plan, ws.data_ptr(),
-                                        ws.numel(), _stream_ptr(stream)), "spd_decode_step_scored")
+    dev = _query(shape, q)
+    _slopes(shape, score, dev)
+    a, b = PagedKV(*_partition(shape, priv, dev)), PagedKV(*_partition(shape, pub, dev))
+    _check(lib().spd_decode_step_scored(shape, score, q.data_ptr(), a, b, _packed(out, q.numel(), dev=dev), _dtype_code(out.dtype), plan,
+                                        *_workspace(ws, dev), _stream_ptr(stream)), "spd_decode_step_scored")
 
 
 def spd_prefill_attn_scored(shape, score, q, k, v, tok_indptr, out, ws, prefix_lens=None, doc_start=None, stream=None) -> None:
     """Prompt attention with score options and interval masks: q [T,Hq,D], k, v [T,Hkv,D] (rows may be parts of a wider row per
     token), tok_indptr int32 [B+1], prefix_lens int32 [B], doc_start int32 [T], out [T,Hq,D] packed."""
-    _slopes(shape, score)
-    _here(q)
+    dev = _here(q)
+    _slopes(shape, score, dev)
     T, B, hq, hkv, d, dtype = q.shape[0], shape.batch, shape.num_q_heads, shape.num_kv_heads, shape.head_dim, _TORCH_DTYPES[shape.dtype]
-    qp, qs = _rows(q, hq, d, T, dtype)
-    kp, ks = _rows(k, hkv, d, T, dtype)
-    vp, vs = _rows(v, hkv, d, T, dtype)
-    _check(lib().spd_prefill_attn_scored(shape, score, T, Tokens(qp, kp, vp, qs, ks, vs), _i32(tok_indptr, B + 1), _i32(prefix_lens, B),
-                                         _i32(doc_start, T), _packed(out, T * hq * d), _dtype_code(out.dtype), ws.data_ptr(), ws.numel(),
-                                         _stream_ptr(stream)), "spd_prefill_attn_scored")
+    qp, qs = _rows(q, hq, d, T, dtype, dev)
+    kp, ks = _rows(k, hkv, d, T, dtype, dev)
+    vp, vs = _rows(v, hkv, d, T, dtype, dev)
+    _check(lib().spd_prefill_attn_scored(shape, score, T, Tokens(qp, kp, vp, qs, ks, vs), _i32(tok_indptr, B + 1, dev=dev),
+                                         _i32(prefix_lens, B, dev=dev), _i32(doc_start, T, dev=dev), _packed(out, T * hq * d, dev=dev),
+                                         _dtype_code(out.dtype), *_workspace(ws, dev), _stream_ptr(stream)), "spd_prefill_attn_scored")
 
 
 def spd_append_kv_rope(shape, rope, q, k, v, part, ws, q_out=None, k_out=None, tok_indptr=None, positions=None, pos_base=None,
@@ -623,24 +662,22 @@ def spd_append_kv_rope(shape, rope, q, k, v, part, ws, q_out=None, k_out=None, t
     rope: make_rope(...) or None (no rotation; q and q_out are not used).  tok_indptr int32 [B+1]: tokens per user; None: one
     token per user.  positions int32 [axes, T] or [T]; pos_base int32 [B].  new_lens: an int32 [B] tensor, None, or by default
     part.seq_lens itself."""
-    _here(k)
+    dev = _here(k)
     T, B, hq, hkv, d, dtype = k.shape[0], shape.batch, shape.num_q_heads, shape.num_kv_heads, shape.head_dim, _TORCH_DTYPES[shape.dtype]
-    kp, ks = _rows(k, hkv, d, T, dtype)
-    vp, vs = _rows(v, hkv, d, T, dtype)
-    qp, qs = _rows(q, hq, d, T, dtype) if rope is not None else (None, 0)
+    kp, ks = _rows(k, hkv, d, T, dtype, dev)
+    vp, vs = _rows(v, hkv, d, T, dtype, dev)
+    qp, qs = _rows(q, hq, d, T, dtype, dev) if rope is not None else (None, 0)
+    if rope is not None:
+        keep = getattr(rope, "_keep", None)
+        if keep is not None and keep.get_device() != dev:
+            raise _elsewhere(keep)
     if positions is not None:
         if rope is None:
             raise ValueError("positions are for a rotation")
-        positions = _i32(positions, T) if positions.dim() == 1 and rope.num_axes == 1 else _i32(positions, rope.num_axes, T)
-    pages, indices = part.k_pool.shape[0], part.page_indices
-    for pool in (part.k_pool, part.v_pool):
-        if pool.dtype is not dtype or pool.numel() != pages * hkv * 16 * d or not pool.is_contiguous() or not pool.is_cuda:
-            raise ValueError(f"expected contiguous {dtype} pools [{pages}, {hkv}, 16, {d}] on the device, got {pool.dtype} {list(pool.shape)} on {pool.device}")
-    if indices.dtype is not torch.int32 or not indices.is_contiguous() or not indices.is_cuda:
-        raise ValueError("page indices are contiguous int32 on the device")
-    lens = _i32(part.seq_lens, B)
-    _check(lib().spd_append_kv_rope(shape, rope, T, Tokens(qp, kp, vp, qs, ks, vs), _i32(tok_indptr, B + 1), positions, _i32(pos_base, B),
-                                    _packed(q_out, T * hq * d, dtype), _packed(k_out, T * hkv * d, dtype), part.k_pool.data_ptr(),
-                                    part.v_pool.data_ptr(), pages, _i32(part.page_indptr, B + 1), _ptr(indices),
-                                    lens, lens if isinstance(new_lens, str) else _i32(new_lens, B), ws.data_ptr(), ws.numel(),
+        positions = _i32(positions, T, dev=dev) if positions.dim() == 1 and rope.num_axes == 1 else _i32(positions, rope.num_axes, T, dev=dev)
+    pool_k, pool_v, pages, indptr, indices, lens = _partition(shape, part, dev)
+    _check(lib().spd_append_kv_rope(shape, rope, T, Tokens(qp, kp, vp, qs, ks, vs), _i32(tok_indptr, B + 1, dev=dev), positions,
+                                    _i32(pos_base, B, dev=dev), _packed(q_out, T * hq * d, dtype, dev), _packed(k_out, T * hkv * d, dtype, dev),
+                                    pool_k, pool_v, pages, indptr, indices, lens,
+                                    lens if isinstance(new_lens, str) else _i32(new_lens, B, dev=dev), *_workspace(ws, dev),
                                     _stream_ptr(stream)), "spd_append_kv_rope")
