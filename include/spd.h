@@ -31,7 +31,8 @@
  *     stream is still finishing; q, an incoming partial, the workspace and the outputs are touched only after
  *     that kernel has completed.  If a kernel of yours on the same stream writes lengths, page tables or KV rows
  *     immediately before a call, launch in plain stream order: spd_set_programmatic_launch(0), or SPD_NO_PDL=1
- *     in the environment.  Where the library's own calls write such inputs (the appends), they order themselves.
+ *     in the environment.  Where the library's own calls write such inputs (the appends), they order themselves: an
+ *     attention call behind an appending launch on its stream starts in plain stream order, whatever their workspaces.
  *   - Threads.  Calls may come from several host threads, also from threads that have made no CUDA call of their
  *     own yet (the library makes the current device's context current on such a thread at its first call); calls
  *     that share a workspace must be ordered by the caller (one stream at a time per workspace).  Each workspace keeps a small table of streaming rates that
@@ -294,8 +295,7 @@ spd_status spd_service_attn_merge_append(const spd_shape *shape, const void *q, 
  * spd_service_attn_merge_scored are its two halves: each sees one partition and is told how many tokens the other one holds
  * (pub_lens, priv_lens: device [batch]; a negative entry, or a sum beyond 2^31 - 1, raises SPD_ERR_BAD_PAGE for the user).
  * A partition wholly in front of the window gives the empty partial.  `plan` as for the *_planned calls; a plan also fits
- * only calls with the same window and, under a window, the same lengths of the other half.  A scored call that follows an
- * appending launch on its workspace starts in plain stream order.  spd_set_bf16_math does not concern these calls (tensor
+ * only calls with the same window and, under a window, the same lengths of the other half.  spd_set_bf16_math does not concern these calls (tensor
  * cores always).  Stream order (the other half's lengths are read ahead of the previous kernel like one's own), errors and workspace as for the plain calls.
  * A visible key whose row of k is NaN makes the outputs concerned NaN (the plain calls give zeros there).  Calls with few and
  * short sequences -- by the window, or by the pools' pages -- take a kernel of their own (a cluster of CTAs per sequence) unless

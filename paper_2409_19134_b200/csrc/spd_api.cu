@@ -7,6 +7,8 @@
 #include <cstdlib>
 #include <cstring>
 #include <mutex>
+#include <set>
+#include <tuple>
 #include <unordered_map>
 #include <vector>
 
@@ -48,25 +50,42 @@ std::atomic<int> g_pdl{-1};                       // programmatic launch: -1 = n
 struct WsHostState {
     uint64_t launches = 0;
     uint64_t stored_at[3] = {~0ull, ~0ull, ~0ull};
-    bool appended = false;          // the last of them grew its lengths as its last act
 };
 
 // Registers one attention launch.  *early_plan: a launch that loads a stored plan may read it before the
 // previous kernel on the stream has finished when that kernel is not the one that stored it (the launch before
-// the previous one has left every SM by the time this one starts, since each CTA takes a whole SM).  *after_append: the
-// launch before this one on the workspace wrote lengths.
-uint32_t register_launch(const void *ws, int slot, int plan_mode, bool appends, bool *early_plan, bool *after_append) {
+// the previous one has left every SM by the time this one starts, since each CTA takes a whole SM).
+uint32_t register_launch(const void *ws, int slot, int plan_mode, bool *early_plan) {
     static std::mutex mu;
     static std::unordered_map<const void *, WsHostState> table;
     std::lock_guard<std::mutex> lock(mu);
     WsHostState &st = table[ws];
     const uint64_t n = st.launches++;
-    *after_append = st.appended;
-    st.appended = appends;
     *early_plan = plan_mode == PLAN_LOAD && st.stored_at[slot] != ~0ull && n >= st.stored_at[slot] + 2;
     if (plan_mode == PLAN_DERIVE_STORE) st.stored_at[slot] = n;
     if (plan_mode == PLAN_DERIVE) st.stored_at[slot] = ~0ull;
     return static_cast<uint32_t>(n % 3u);
+}
+
+// Whether the last attention launch on the stream was one that appends (it lets the next kernel in early, but grows its lengths as
+// its last act, so a launch that may read them must not start ahead of its end), and notes whether this one is.  A stream is
+// known by its handle (one that is handed out again costs its first call the overlap), the default streams by device, the
+// per-thread one by thread too; asking the runtime for a stream's id would end a capture.
+bool behind_append(cudaStream_t st, bool appends) {
+    static std::mutex mu;
+    static std::set<std::tuple<int, uintptr_t, uint64_t>> behind;
+    static std::atomic<bool> any{false};            // no launch has ever appended: nothing to look up
+    static std::atomic<uint64_t> threads{0};
+    static thread_local const uint64_t thread = ++threads;
+    if (!appends && !any.load()) return false;
+    int dev = 0;
+    cudaGetDevice(&dev);
+    const bool own = st == cudaStreamPerThread;
+    const auto key = std::make_tuple(dev, reinterpret_cast<uintptr_t>(st == cudaStreamLegacy ? nullptr : st), own ? thread : 0);
+    std::lock_guard<std::mutex> lock(mu);
+    if (!appends) return behind.erase(key) != 0;
+    any.store(true);
+    return !behind.insert(key).second;
 }
 
 bool programmatic_launch() {
@@ -323,8 +342,8 @@ spd_status run_job(const Job &job, void *ws, size_t ws_bytes, void *stream) {
     p.rates = reinterpret_cast<float2 *>(w + L.rates);
     const int slot = (job.part[0] ? 1 : 0) + (job.part[1] ? 2 : 0) - 1;   // one stored plan per kind of call
     if (slot < 0) return SPD_ERR_INVALID_ARG;
-    bool early_plan = false, after_append = false;
-    p.rate_sel = static_cast<int32_t>(register_launch(ws, slot, job.plan_mode, job.k_new != nullptr, &early_plan, &after_append));   // rotates through the thirds
+    bool early_plan = false;
+    p.rate_sel = static_cast<int32_t>(register_launch(ws, slot, job.plan_mode, &early_plan));   // rotates through the thirds
     p.plan_early = early_plan && !job.wait_first ? 1 : 0;
     p.min_tiles = g_min_tiles.load();
     p.uniform = g_uniform_shares.load();
@@ -392,7 +411,10 @@ spd_status run_job(const Job &job, void *ws, size_t ws_bytes, void *stream) {
     }
     prof_mark(pj, 0, st);
     const int D = s.head_dim;
-    const bool pdl = programmatic_launch() && !job.plain_order && !(job.score && after_append);
+    // A launch that appends says itself whether it may overlap the one before (the layers of a token step may: each has lengths of
+    // its own); any other one waits for an append to end.
+    const bool behind = behind_append(st, job.k_new != nullptr);
+    const bool pdl = programmatic_launch() && !job.plain_order && (job.k_new || !behind);
     if (job.score) {
         rc = launch_attn_scored(p, maps, di.sms, st, pdl, bf, D);
     } else if (bf && g_bf16_math.load() == 1) {
