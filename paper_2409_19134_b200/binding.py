@@ -194,7 +194,17 @@ def paged_kv(part) -> PagedKV:
 def _stream_ptr(stream: Optional[torch.cuda.Stream]) -> int:
     if stream is not None:
         return stream.cuda_stream
-    return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())    # torch.cuda.current_stream() without the wrapper object
+    try:                        # torch.cuda.current_stream() without the wrapper object: 3 us less per call, but not a documented function
+        return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
+    except AttributeError:
+        return torch.cuda.current_stream().cuda_stream
+
+
+def _current_device() -> int:
+    try:
+        return torch._C._cuda_getDevice()
+    except AttributeError:
+        return torch.cuda.current_device()
 
 
 def spd_workspace_size(shape: Shape) -> int:
@@ -517,7 +527,7 @@ def _elsewhere(t: torch.Tensor) -> ValueError:
 
 def _here(t: torch.Tensor) -> int:
     """The tensors of a call live on the current device, whose stream and context the call uses; its index."""
-    if not t.is_cuda or t.get_device() != torch._C._cuda_getDevice():
+    if not t.is_cuda or t.get_device() != _current_device():
         raise _elsewhere(t)
     return t.get_device()
 
@@ -581,30 +591,29 @@ def _workspace(ws: torch.Tensor, dev):
     return ws.data_ptr(), ws.numel()
 
 
-def _partition(shape, part, dev):
-    """The fields of PagedKV, in order: pools as the shape says, a table and a length per user."""
+def _partition(part, B, page, dtype, dev):
+    """The fields of PagedKV, in order: pools of pages of `page` elements, a table and a length per user."""
     kp, vp, indptr, indices, lens = part.k_pool, part.v_pool, part.page_indptr, part.page_indices, part.seq_lens
-    pages, dtype, B = kp.shape[0], _TORCH_DTYPES[shape.dtype], shape.batch
-    n = pages * shape.num_kv_heads * shape.page_size * shape.head_dim
-    if not (kp.dtype is dtype and vp.dtype is dtype and kp.numel() == n and vp.numel() == n and kp.is_contiguous() and vp.is_contiguous()):
-        raise ValueError(f"expected contiguous {dtype} pools [{pages}, {shape.num_kv_heads}, {shape.page_size}, {shape.head_dim}], got "
+    pages = kp.shape[0]
+    if not (kp.dtype is dtype and vp.dtype is dtype and kp.numel() == pages * page == vp.numel() and kp.is_contiguous() and vp.is_contiguous()):
+        raise ValueError(f"expected contiguous {dtype} pools of {pages} pages of {page} elements (KV heads x page size x head_dim), got "
                          f"{kp.dtype} {list(kp.shape)} and {vp.dtype} {list(vp.shape)}")
+    listed = indices.numel()
     if not (indptr.dtype is _I32 and indices.dtype is _I32 and lens.dtype is _I32 and indptr.numel() == B + 1 and lens.numel() == B and
             indptr.is_contiguous() and indices.is_contiguous() and lens.is_contiguous()):
         raise ValueError(f"expected contiguous int32 page_indptr [{B + 1}], page_indices and seq_lens [{B}], got {indptr.dtype} "
                          f"{list(indptr.shape)}, {indices.dtype} and {lens.dtype} {list(lens.shape)}")
-    for t in (kp, vp, indptr, indices, lens):
-        if t.get_device() != dev:
-            raise _elsewhere(t)
+    if not (kp.get_device() == dev == vp.get_device() and indptr.get_device() == dev == indices.get_device() and lens.get_device() == dev):
+        raise _elsewhere(next(t for t in (kp, vp, indptr, indices, lens) if t.get_device() != dev))
     return (kp.data_ptr() if pages else None, vp.data_ptr() if pages else None, pages, indptr.data_ptr(),
-            indices.data_ptr() if indices.numel() else None, lens.data_ptr())
+            indices.data_ptr() if listed else None, lens.data_ptr())
 
 
-def _query(shape, q) -> int:
-    """One packed query row per user and head; the device of the call."""
-    dev = _here(q)
-    _packed(q, shape.batch * shape.num_q_heads * shape.head_dim, _TORCH_DTYPES[shape.dtype], dev)
-    return dev
+def _query(shape, q):
+    """One packed query row per user and head.  The device of the call, and what its partitions are held against."""
+    dev, B, d, dtype = _here(q), shape.batch, shape.head_dim, _TORCH_DTYPES[shape.dtype]
+    _packed(q, B * shape.num_q_heads * d, dtype, dev)
+    return dev, (B, shape.num_kv_heads * shape.page_size * d, dtype, dev)
 
 
 def _partial(shape, part, dev) -> Partial:
@@ -615,18 +624,18 @@ def _partial(shape, part, dev) -> Partial:
 
 def spd_partial_attn_scored(shape, score, q, priv, pub_lens, out, ws, plan=SPD_PLAN_PER_CALL, stream=None) -> None:
     """spd_partial_attn with score options; pub_lens: int32 [batch], tokens in the public partition."""
-    dev = _query(shape, q)
+    dev, fit = _query(shape, q)
     _slopes(shape, score, dev)
-    kv, part = PagedKV(*_partition(shape, priv, dev)), _partial(shape, out, dev)
+    kv, part = PagedKV(*_partition(priv, *fit)), _partial(shape, out, dev)
     _check(lib().spd_partial_attn_scored(shape, score, q.data_ptr(), kv, _i32(pub_lens, shape.batch, dev=dev), part, plan, *_workspace(ws, dev),
                                          _stream_ptr(stream)), "spd_partial_attn_scored")
 
 
 def spd_service_attn_merge_scored(shape, score, q, pub, priv_lens, partial_in, out, ws, plan=SPD_PLAN_PER_CALL, stream=None) -> None:
     """spd_service_attn_merge with score options; priv_lens: int32 [batch], tokens in the private partition."""
-    dev = _query(shape, q)
+    dev, fit = _query(shape, q)
     _slopes(shape, score, dev)
-    kv, part = PagedKV(*_partition(shape, pub, dev)), _partial(shape, partial_in, dev)
+    kv, part = PagedKV(*_partition(pub, *fit)), _partial(shape, partial_in, dev)
     _check(lib().spd_service_attn_merge_scored(shape, score, q.data_ptr(), kv, _i32(priv_lens, shape.batch, dev=dev), part,
                                                _packed(out, q.numel(), dev=dev), _dtype_code(out.dtype), plan, *_workspace(ws, dev),
                                                _stream_ptr(stream)), "spd_service_attn_merge_scored")
@@ -634,9 +643,9 @@ def spd_service_attn_merge_scored(shape, score, q, pub, priv_lens, partial_in, o
 
 def spd_decode_step_scored(shape, score, q, priv, pub, out, ws, plan=SPD_PLAN_PER_CALL, stream=None) -> None:
     """The fused decode step with score options (make_score) over both partitions."""
-    dev = _query(shape, q)
+    dev, fit = _query(shape, q)
     _slopes(shape, score, dev)
-    a, b = PagedKV(*_partition(shape, priv, dev)), PagedKV(*_partition(shape, pub, dev))
+    a, b = PagedKV(*_partition(priv, *fit)), PagedKV(*_partition(pub, *fit))
     _check(lib().spd_decode_step_scored(shape, score, q.data_ptr(), a, b, _packed(out, q.numel(), dev=dev), _dtype_code(out.dtype), plan,
                                         *_workspace(ws, dev), _stream_ptr(stream)), "spd_decode_step_scored")
 
@@ -675,7 +684,7 @@ def spd_append_kv_rope(shape, rope, q, k, v, part, ws, q_out=None, k_out=None, t
         if rope is None:
             raise ValueError("positions are for a rotation")
         positions = _i32(positions, T, dev=dev) if positions.dim() == 1 and rope.num_axes == 1 else _i32(positions, rope.num_axes, T, dev=dev)
-    pool_k, pool_v, pages, indptr, indices, lens = _partition(shape, part, dev)
+    pool_k, pool_v, pages, indptr, indices, lens = _partition(part, B, hkv * shape.page_size * d, dtype, dev)
     _check(lib().spd_append_kv_rope(shape, rope, T, Tokens(qp, kp, vp, qs, ks, vs), _i32(tok_indptr, B + 1, dev=dev), positions,
                                     _i32(pos_base, B, dev=dev), _packed(q_out, T * hq * d, dtype, dev), _packed(k_out, T * hkv * d, dtype, dev),
                                     pool_k, pool_v, pages, indptr, indices, lens,
