@@ -527,9 +527,10 @@ def _elsewhere(t: torch.Tensor) -> ValueError:
 
 def _here(t: torch.Tensor) -> int:
     """The tensors of a call live on the current device, whose stream and context the call uses; its index."""
-    if not t.is_cuda or t.get_device() != _current_device():
+    dev = t.get_device()
+    if dev < 0 or dev != _current_device():
         raise _elsewhere(t)
-    return t.get_device()
+    return dev
 
 
 def _slopes(shape, score, dev) -> None:
@@ -584,10 +585,8 @@ def _packed(t: Optional[torch.Tensor], numel: int, dtype=None, dev=None) -> Opti
 
 def _workspace(ws: torch.Tensor, dev):
     """(pointer, bytes) of a workspace."""
-    if ws.dtype is not torch.uint8 or not ws.is_contiguous():
-        raise ValueError(f"a workspace is a contiguous uint8 tensor, got {ws.dtype}")
-    if ws.get_device() != dev:
-        raise _elsewhere(ws)
+    if ws.get_device() != dev or ws.dtype is not torch.uint8 or not ws.is_contiguous():
+        raise ValueError(f"a workspace is a contiguous uint8 tensor on the current CUDA device, got {ws.dtype} on {ws.device}")
     return ws.data_ptr(), ws.numel()
 
 
@@ -598,15 +597,13 @@ def _partition(part, B, page, dtype, dev):
     if not (kp.dtype is dtype and vp.dtype is dtype and kp.numel() == pages * page == vp.numel() and kp.is_contiguous() and vp.is_contiguous()):
         raise ValueError(f"expected contiguous {dtype} pools of {pages} pages of {page} elements (KV heads x page size x head_dim), got "
                          f"{kp.dtype} {list(kp.shape)} and {vp.dtype} {list(vp.shape)}")
-    listed = indices.numel()
     if not (indptr.dtype is _I32 and indices.dtype is _I32 and lens.dtype is _I32 and indptr.numel() == B + 1 and lens.numel() == B and
             indptr.is_contiguous() and indices.is_contiguous() and lens.is_contiguous()):
         raise ValueError(f"expected contiguous int32 page_indptr [{B + 1}], page_indices and seq_lens [{B}], got {indptr.dtype} "
                          f"{list(indptr.shape)}, {indices.dtype} and {lens.dtype} {list(lens.shape)}")
     if not (kp.get_device() == dev == vp.get_device() and indptr.get_device() == dev == indices.get_device() and lens.get_device() == dev):
         raise _elsewhere(next(t for t in (kp, vp, indptr, indices, lens) if t.get_device() != dev))
-    return (kp.data_ptr() if pages else None, vp.data_ptr() if pages else None, pages, indptr.data_ptr(),
-            indices.data_ptr() if listed else None, lens.data_ptr())
+    return kp.data_ptr(), vp.data_ptr(), pages, indptr.data_ptr(), indices.data_ptr(), lens.data_ptr()      # an empty tensor's is 0
 
 
 def _query(shape, q):
