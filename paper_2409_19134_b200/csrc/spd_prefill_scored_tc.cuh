@@ -189,8 +189,8 @@ __device__ __noinline__ void st_slow_row(const ScoredTcParams &p, int64_t first,
         s *= p.s.sm_scale;
         if (p.s.cap > 0.f) s = p.s.cap * tanhf(s / p.s.cap);
         s = fmaf(-slope, fabsf(static_cast<float>(row - j)), s);
-        const float m_new = fmaxf(m, s);
-        const float alpha = m == -INFINITY ? 0.f : expf(m - m_new), w = expf(s - m_new);
+        const float m_new = fmaxf(m, s), ref = m_new == -INFINITY ? 0.f : m_new;      // a score of -inf weighs nothing, a first one too
+        const float alpha = m == -INFINITY ? 0.f : expf(m - ref), w = expf(s - ref);
         l = l * alpha + w;
 #pragma unroll
         for (int i = 0; i < V; ++i) o[i] = fmaf(w, __bfloat162float(v[lane + 32 * i]), o[i] * alpha);
