@@ -297,7 +297,8 @@ spd_status spd_service_attn_merge_append(const spd_shape *shape, const void *q, 
  * A partition wholly in front of the window gives the empty partial.  `plan` as for the *_planned calls; a plan also fits
  * only calls with the same window and, under a window, the same lengths of the other half.  spd_set_bf16_math does not concern these calls (tensor
  * cores always).  Stream order (the other half's lengths are read ahead of the previous kernel like one's own), errors and workspace as for the plain calls.
- * A visible key whose row of k is NaN makes the outputs concerned NaN (the plain calls give zeros there).  Calls with few and
+ * A visible key whose row of k is NaN makes the outputs concerned NaN (the plain calls give zeros there); one whose score is
+ * -inf weighs nothing, and where all of them do, the output is zeros.  Calls with few and
  * short sequences -- by the window, or by the pools' pages -- take a kernel of their own (a cluster of CTAs per sequence) unless
  * spd_set_split asks for a cut or `plan` is not SPD_PLAN_PER_CALL.
  */

@@ -357,6 +357,11 @@ __device__ __forceinline__ float scored_value(const Params &p, float s, float sl
     return (p.window > 0 && d >= p.window) ? -INFINITY : s;
 }
 
+// What weights are taken relative to: the maximum, or 0 while nothing but scores of -inf has been seen (they weigh nothing; the plain
+// calls give NaN to such a tile and zeros to its row in the end).
+template <bool Scored>
+__device__ __forceinline__ float softmax_reference(float m) { return Scored && m == -INFINITY ? 0.f : m; }
+
 // ------------------------------------------------------------------------------------------------
 // bf16 tile math on the tensor cores (mma.sync m16n8k16, fp32 accumulate).
 //   S  = Q K^T   : M = 16 query-head rows (8 used), N = 8 tokens (x2), K = head_dim
@@ -479,9 +484,10 @@ struct MathBF16 {
         tmax = fmaxf(tmax, __shfl_xor_sync(0xffffffffu, tmax, 1));
         tmax = fmaxf(tmax, __shfl_xor_sync(0xffffffffu, tmax, 2));
         const float m_new = fmaxf(st.m, tmax);
-        const float alpha = ex2_approx((st.m - m_new) * kLog2e);
-        const float p0 = ex2_approx((v0 - m_new) * kLog2e), p1 = ex2_approx((v1 - m_new) * kLog2e);
-        const float p2 = ex2_approx((v2 - m_new) * kLog2e), p3 = ex2_approx((v3 - m_new) * kLog2e);
+        const float ref = softmax_reference<kScored>(m_new);
+        const float alpha = ex2_approx((st.m - ref) * kLog2e);
+        const float p0 = ex2_approx((v0 - ref) * kLog2e), p1 = ex2_approx((v1 - ref) * kLog2e);
+        const float p2 = ex2_approx((v2 - ref) * kLog2e), p3 = ex2_approx((v3 - ref) * kLog2e);
         st.l = st.l * alpha + ((p0 + p1) + (p2 + p3));
         st.m = m_new;
         if (!kScored && st.whi > st.wlo) {   // warp-uniform
@@ -756,8 +762,9 @@ struct MathF32 {
 #pragma unroll
             for (int d = 8; d >= 1; d >>= 1) tmax = fmaxf(tmax, __shfl_xor_sync(0xffffffffu, tmax, d));
             const float m_new = fmaxf(st.m[hh], tmax);
-            const float alpha = exp2f((st.m[hh] - m_new) * kLog2e);
-            const float pr = exp2f((v - m_new) * kLog2e);
+            const float ref = softmax_reference<kScored>(m_new);
+            const float alpha = exp2f((st.m[hh] - ref) * kLog2e);
+            const float pr = exp2f((v - ref) * kLog2e);
             st.l[hh] = st.l[hh] * alpha + (hf == 0 ? pr : 0.f);
             if constexpr (!kScored)
                 st.lw[hh] = st.lw[hh] * alpha + ((hf == 0 && watch_base + t >= st.wlo && watch_base + t < st.whi) ? pr : 0.f);

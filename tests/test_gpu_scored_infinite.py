@@ -4,7 +4,8 @@ import torch
 
 from paper_2409_19134_b200 import binding as spd
 from tests import scored_reference as ref
-from tests.test_gpu_decode_scored import close
+from tests.test_gpu_decode_scored import close, setup, workload
+from tests.test_gpu_decode_scored import kernel  # noqa: F401
 from tests.test_gpu_prefill_scored import P_WEIGHT, prompts, run
 
 pytestmark = pytest.mark.gpu
@@ -33,3 +34,37 @@ def test_prompt_keys_that_score_minus_infinity_weigh_nothing(dtype, d, hq, hkv, 
     good = 150 if spoiled else n
     close(out[:good], want[:good], tol[:good], "keys of no weight")
     assert bool((out[0] == 0).all()) and bool(out[good:].isnan().all())
+
+
+def decode_job(dtype, d, hq, hkv):
+    """Two users of 320 tokens whose first 40 score minus infinity: 40 of 300 private ones; all 20 private and 20 of 300 public ones."""
+    w = workload([300, 20], [20, 300], hq, hkv, d, dtype, seed=91)
+    w.q[..., 0] = -w.q[..., 0].abs() - 0.125
+    for u in range(2):
+        for part, base, m in ((w.priv, 0, (300, 20)[u]), (w.pub, (300, 20)[u], (20, 300)[u])):
+            for t in range(m):
+                if base + t < 40:
+                    page = int(part.page_indices[int(part.page_indptr[u]) + t // 16])
+                    part.k_pool[page, :, t % 16] = 0
+                    part.k_pool[page, :, t % 16, 0] = float("inf")
+    want, O, m, l, tol = ref.decode(w, window=280)          # as if the 40 were out of sight
+    return setup(w, 0.0, 0, False), want, tol
+
+
+@pytest.mark.parametrize("dtype,d,hq,hkv", [("bf16", 128, 8, 2), ("bf16", 64, 2, 2), ("f32", 128, 2, 1), ("f32", 64, 8, 1)])
+def test_decode_keys_that_score_minus_infinity_weigh_nothing(kernel, dtype, d, hq, hkv):  # noqa: F811
+    """Whole tiles, pieces and a whole partition of such keys, in front of others that count."""
+    (g, shape, score, _, ws), want, tol = decode_job(dtype, d, hq, hkv)
+    for share in ((0,) if kernel == "short" else (3, 1)):
+        spd.spd_set_split(share, False)
+        out = torch.full((2, hq, d), float("nan"), device="cuda")
+        spd.spd_decode_step_scored(shape, score, g.q, g.priv, g.pub, out, ws)
+        assert spd.spd_query_device_status(ws) == (spd.SPD_OK, -1)
+        close(out, want, tol, ("fused", share))
+        part = spd.alloc_partial(shape)
+        spd.spd_partial_attn_scored(shape, score, g.q, g.priv, g.pub.seq_lens, part, ws)
+        assert bool((part[0][1] == 0).all()) and bool((part[1][1] == -float("inf")).all()) and bool((part[2][1] == 0).all())
+        out = torch.full((2, hq, d), float("nan"), device="cuda")
+        spd.spd_service_attn_merge_scored(shape, score, g.q, g.pub, g.priv.seq_lens, part, out, ws)
+        assert spd.spd_query_device_status(ws) == (spd.SPD_OK, -1)
+        close(out, want, 2 * tol, ("halves", share))
