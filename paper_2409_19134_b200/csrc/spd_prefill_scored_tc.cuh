@@ -168,40 +168,91 @@ __device__ __forceinline__ float st_cap(const ScoredTcParams &p, float x) {
     return p.cap2 - __fdividef(2.f * p.cap2, ex2_approx(x * (2.f * kLog2e) * p.y1) + 1.f);
 }
 
-// One row the slow way, run by a whole warp: keys outside [lo, hi] are not touched.
+// Waits like mbar_wait, but does not give up while rows are being done one by one (st_slow_row counts `beat` on): how long that
+// takes goes by the length of the prompt.
+__device__ __forceinline__ bool st_mbar_wait(uint32_t bar, uint32_t parity, const volatile int32_t *beat) {
+    int32_t seen = 0;
+    for (uint32_t i = 0; i < kWaitLimit; ++i) {
+        if (mbar_try_wait(bar, parity)) return true;
+        if ((i & 0xffffu) == 0xffffu) {
+            const int32_t now = *beat;
+            if (now != seen) { seen = now; i = 0; }
+        }
+    }
+    return false;
+}
+
+// One row the slow way, run by a whole warp: keys outside [lo, hi] are not touched.  32 keys at a time, a score per lane, then the
+// lanes' channels of O: 4 us per 32 keys with eight warps at it (reads of K, a row per lane, past an L1 that the tiles have taken).
+// It is for broken inputs: one NaN among the V rows of 8192 tokens x 32/8 heads makes 0.46 ms 33; 700 k tokens of one head, 77 ms, 2.5 s.
 template <int D>
-__device__ __noinline__ void st_slow_row(const ScoredTcParams &p, int64_t first, int row, int h, int lo, int hi, int lane) {
+__device__ __noinline__ void st_slow_row(const ScoredTcParams &p, int64_t first, int row, int h, int lo, int hi, int lane, int32_t *beat) {
     constexpr int V = D / 32;
     const __nv_bfloat16 *q = static_cast<const __nv_bfloat16 *>(p.s.q) + (first + row) * p.s.q_stride + h * D;
     const int kvh = h / (p.s.Hq / p.s.Hkv);
+    const __nv_bfloat16 *k = static_cast<const __nv_bfloat16 *>(p.s.k) + first * p.s.k_stride + kvh * D;
+    const __nv_bfloat16 *v = static_cast<const __nv_bfloat16 *>(p.s.v) + first * p.s.v_stride + kvh * D + lane * V;
     const float slope = p.s.slopes ? p.s.slopes[h] : 0.f;
-    float qv[V], o[V], m = -INFINITY, l = 0.f;
+    auto wide = [](uint32_t x) { return __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162 *>(&x)); };
+    float o[V], m = -INFINITY, l = 0.f;
 #pragma unroll
-    for (int i = 0; i < V; ++i) { qv[i] = __bfloat162float(q[lane + 32 * i]); o[i] = 0.f; }
-    for (int j = lo; j <= hi; ++j) {
-        const __nv_bfloat16 *k = static_cast<const __nv_bfloat16 *>(p.s.k) + (first + j) * p.s.k_stride + kvh * D;
-        const __nv_bfloat16 *v = static_cast<const __nv_bfloat16 *>(p.s.v) + (first + j) * p.s.v_stride + kvh * D;
+    for (int i = 0; i < V; ++i) o[i] = 0.f;
+    for (int64_t j0 = lo; j0 <= hi; j0 += 32) {
+        if (((j0 - lo) & 0x1fff) == 0 && lane == 0) atomicAdd(beat, 1);
+        const int64_t j = j0 + lane;
         float s = 0.f;
-#pragma unroll
-        for (int i = 0; i < V; ++i) s = fmaf(qv[i], __bfloat162float(k[lane + 32 * i]), s);
-#pragma unroll
-        for (int d = 16; d >= 1; d >>= 1) s += __shfl_xor_sync(0xffffffffu, s, d);
+        if (j <= hi) {
+            const uint4 *kj = reinterpret_cast<const uint4 *>(k + j * p.s.k_stride), *qj = reinterpret_cast<const uint4 *>(q);
+#pragma unroll 4
+            for (int c = 0; c < D / 8; ++c) {
+                const uint4 a = qj[c], b = kj[c];
+                float2 x = wide(a.x), y = wide(b.x);
+                s = fmaf(x.x, y.x, s); s = fmaf(x.y, y.y, s);
+                x = wide(a.y); y = wide(b.y);
+                s = fmaf(x.x, y.x, s); s = fmaf(x.y, y.y, s);
+                x = wide(a.z); y = wide(b.z);
+                s = fmaf(x.x, y.x, s); s = fmaf(x.y, y.y, s);
+                x = wide(a.w); y = wide(b.w);
+                s = fmaf(x.x, y.x, s); s = fmaf(x.y, y.y, s);
+            }
+        }
         s *= p.s.sm_scale;
         if (p.s.cap > 0.f) s = p.s.cap * tanhf(s / p.s.cap);
         s = fmaf(-slope, fabsf(static_cast<float>(row - j)), s);
-        const float m_new = fmaxf(m, s), ref = m_new == -INFINITY ? 0.f : m_new;      // a score of -inf weighs nothing, a first one too
+        if (j > hi) s = -INFINITY;
+        float mx = s;
+#pragma unroll
+        for (int d = 16; d >= 1; d >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, d));
+        const float m_new = fmaxf(m, mx), ref = m_new == -INFINITY ? 0.f : m_new;      // a score of -inf weighs nothing, a first one too
         const float alpha = m == -INFINITY ? 0.f : expf(m - ref), w = expf(s - ref);
-        l = l * alpha + w;
+        float sum = w;
 #pragma unroll
-        for (int i = 0; i < V; ++i) o[i] = fmaf(w, __bfloat162float(v[lane + 32 * i]), o[i] * alpha);
+        for (int d = 16; d >= 1; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
+        l = l != l ? l : l * alpha + sum;              // NaN scores leave no maximum, but a sum that is NaN
+#pragma unroll
+        for (int i = 0; i < V; ++i) o[i] *= alpha;
         m = m_new;
+        const int n = static_cast<int>(min(static_cast<int64_t>(32), hi - j0 + 1));
+#pragma unroll 8
+        for (int t = 0; t < n; ++t) {
+            const float wt = __shfl_sync(0xffffffffu, w, t);
+            const __nv_bfloat16 *vt = v + (j0 + t) * p.s.v_stride;
+            if constexpr (V == 4) {
+                const uint2 x = *reinterpret_cast<const uint2 *>(vt);
+                const float2 a = wide(x.x), b = wide(x.y);
+                o[0] = fmaf(wt, a.x, o[0]); o[1] = fmaf(wt, a.y, o[1]); o[2] = fmaf(wt, b.x, o[2]); o[3] = fmaf(wt, b.y, o[3]);
+            } else {
+                const float2 a = wide(*reinterpret_cast<const uint32_t *>(vt));
+                o[0] = fmaf(wt, a.x, o[0]); o[1] = fmaf(wt, a.y, o[1]);
+            }
+        }
     }
-    const int64_t dst = ((first + row) * p.s.Hq + h) * D;
+    const int64_t dst = ((first + row) * p.s.Hq + h) * D + lane * V;
 #pragma unroll
-    for (int i = 0; i < V; ++i) {
-        const float y = l == 0.f ? 0.f : o[i] / l;
-        if (p.s.out_bf16) reinterpret_cast<__nv_bfloat16 *>(p.s.out)[dst + lane + 32 * i] = __float2bfloat16_rn(y);
-        else reinterpret_cast<float *>(p.s.out)[dst + lane + 32 * i] = y;
+    for (int i = 0; i < V; i += 2) {
+        const float y0 = l == 0.f ? 0.f : o[i] / l, y1 = l == 0.f ? 0.f : o[i + 1] / l;
+        if (p.s.out_bf16) *reinterpret_cast<__nv_bfloat162 *>(reinterpret_cast<__nv_bfloat16 *>(p.s.out) + dst + i) = __floats2bfloat162_rn(y0, y1);
+        else *reinterpret_cast<float2 *>(reinterpret_cast<float *>(p.s.out) + dst + i) = make_float2(y0, y1);
     }
 }
 
@@ -223,8 +274,9 @@ prefill_scored_tc_kernel(const __grid_constant__ ScoredTcParams p, const __grid_
     uint64_t *bar_k = bars + 14, *bar_v = bar_k + NS, *bar_kfree = bar_v + NS, *bar_vfree = bar_kfree + NS;
     uint64_t *bar_guard = bar_vfree + NS;                          // per V slot: the guards are done with the block
     constexpr int NBARS = 14 + 5 * NS;
-    static_assert(NBARS * 8 + 4 <= kStBarBytes, "barrier block");
+    static_assert(NBARS * 8 + 8 <= kStBarBytes, "barrier block");
     uint32_t &tmem_slot = *reinterpret_cast<uint32_t *>(bars + NBARS);
+    int32_t *beat = reinterpret_cast<int32_t *>(bars + NBARS) + 1;      // counted on while rows are done one by one
     StPlan *plans = reinterpret_cast<StPlan *>(stage_all + 8 * kStStage + kStBarBytes);
     const int tid = threadIdx.x, wid = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31;
     const int hpc = p.heads_per_cta, hgroups = p.s.Hq / hpc, gq = p.s.Hq / p.s.Hkv;
@@ -232,6 +284,7 @@ prefill_scored_tc_kernel(const __grid_constant__ ScoredTcParams p, const __grid_
 
     if (blockIdx.x == 0) scored_check_offsets(p.s);
     if (tid == 320) {
+        *beat = 0;
         prefetch_tensormap(&mq); prefetch_tensormap(&mk); prefetch_tensormap(&mv); prefetch_tensormap(&mo);
         for (int b = 0; b < NBARS; ++b) {
             // Q and ring slots free: one per tile; S in registers, P written: one per softmax warp of the tile;
@@ -251,11 +304,11 @@ prefill_scored_tc_kernel(const __grid_constant__ ScoredTcParams p, const __grid_
     tc_fence_after();
     const uint32_t tmem = __shfl_sync(0xffffffffu, tmem_slot, 0);
 
-    // Every wait is bounded.  A wait that runs out clears `ok`, and the warp leaves its loops at the next turn; nothing in the
+    // Every wait is bounded (st_slow_row by the length of its rows).  A wait that runs out clears `ok`, and the warp leaves its loops at the next turn; nothing in the
     // loops waits for all threads, so everybody comes to the common end.
     bool ok = true;
-    auto wait = [&](uint64_t *bar, uint32_t parity) { if (ok) ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(bar), parity & 1)); };   // whole warps
-    auto wait1 = [&](uint64_t *bar, uint32_t parity) { ok = ok && mbar_wait(smem_u32(bar), parity & 1); };                             // the loading thread
+    auto wait = [&](uint64_t *bar, uint32_t parity) { if (ok) ok = __all_sync(0xffffffffu, st_mbar_wait(smem_u32(bar), parity & 1, beat)); };   // whole warps
+    auto wait1 = [&](uint64_t *bar, uint32_t parity) { ok = ok && st_mbar_wait(smem_u32(bar), parity & 1, beat); };                             // the loading thread
     // item r of this CTA: plan buffer r & 1, in its (r / 2)-th use
     auto plan_of = [&](int r) -> StPlan & { wait(&bar_plan[r & 1], r >> 1); __syncwarp(); return plans[r & 1]; };
     auto plan_done = [&](int r) { __syncwarp(); if (lane == 0) mbar_arrive(smem_u32(&bar_planfree[r & 1])); };
@@ -482,7 +535,7 @@ prefill_scored_tc_kernel(const __grid_constant__ ScoredTcParams p, const __grid_
                 for (int x = 0; x < 32; ++x) {               // the warp's own rows, one by one
                     const int rr = trow0 + (wid & 3) * 32 + x;
                     const int2 s2 = pl.span[(wid << 5) + x];
-                    if (rr < len) st_slow_row<D>(p, first, rr, h, s2.x, s2.y, lane);
+                    if (rr < len) st_slow_row<D>(p, first, rr, h, s2.x, s2.y, lane, beat);
                 }
             } else if (ok && have) {
                 // ---- normalise this thread's row, 128 bytes of output at a time, into the warp's staging area (128-byte rows, 16-byte

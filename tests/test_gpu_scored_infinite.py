@@ -68,3 +68,18 @@ def test_decode_keys_that_score_minus_infinity_weigh_nothing(kernel, dtype, d, h
         spd.spd_service_attn_merge_scored(shape, score, g.q, g.pub, g.priv.seq_lens, part, out, ws)
         assert spd.spd_query_device_status(ws) == (spd.SPD_OK, -1)
         close(out, want, 2 * tol, ("halves", share))
+
+
+@pytest.mark.parametrize("n,d,hq", [(9000, 128, 2), (700001, 64, 1)])
+def test_a_spoiled_row_at_the_end_of_a_long_prompt(n, d, hq):
+    """The rows of the last tile are done again one by one over all their keys; everybody else waits for them as long as it takes."""
+    q, k, v, ip = prompts([n], hq, 1, d, "bf16", seed=92)
+    bad = n - 70                                          # the last tile's rows in front of it do not see it
+    v[bad] = float("nan")
+    out, status = run(q, k, v, ip, d)
+    assert status == (spd.SPD_OK, -1)
+    rows = {0, 1, 4095, n // 2, n - 300, bad - 20, bad - 1}
+    want, tol = ref.prefill(q, k, v, [n], d ** -0.5, weight=P_WEIGHT["bf16"], rows=rows)
+    at = sorted(rows)
+    close(out[at], want[at], tol[at], "rows in front of the spoiled one")
+    assert bool(out[bad:].isnan().all()) and bool(torch.isfinite(out[:bad]).all())
