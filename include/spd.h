@@ -341,9 +341,10 @@ typedef struct {
  * is not consistent as for spd_prefill_attn; out [total_tokens][num_q_heads][head_dim] in out_dtype, packed.  The prompts'
  * rows do not go to a cache here: spd_append_kv_rope does that, with or without rotation.  sm_scale > 0, else
  * SPD_ERR_UNSUPPORTED.  One kernel in plain stream order; it counts its work in words of `ws`, so calls that share a
- * workspace must be ordered.  BF16 runs on the tensor cores (weights rounded to bf16 once, as in spd_prefill_attn; with a cap
- * of at most 50 and no bias they are taken relative to a score of 0 and reach e^50 = 5e21, so that rows of v beyond 1e11 in
- * magnitude may overflow fp32 in prompts of 10^5 tokens), FP32 on the FMA pipes in fp32 throughout.
+ * workspace must be ordered.  BF16 runs on the tensor cores (weights rounded to bf16 once, as in spd_prefill_attn; rows that see only
+ * a part of a V row that is not finite, and rows whose weighted sums leave fp32's range though the output does not -- with a cap
+ * of at most 50 and no bias weights reach e^50, so from |v| of about 1e11 on -- are done again one key after another, which is slow),
+ * FP32 on the FMA pipes in fp32 throughout.
  */
 spd_status spd_prefill_attn_scored(const spd_shape *shape, const spd_score *score, int64_t total_tokens,
                                    const spd_tokens *tok, const int32_t *tok_indptr, const int32_t *prefix_lens,

@@ -182,11 +182,11 @@ __device__ __forceinline__ bool st_mbar_wait(uint32_t bar, uint32_t parity, cons
     return false;
 }
 
-// One row the slow way, run by a whole warp: keys outside [lo, hi] are not touched.  32 keys at a time, a score per lane, then the
+// One row the slow way, run by a whole warp: keys outside [lo, hi] are not touched; O is summed in units of 1 / unit.  32 keys at a time, a score per lane, then the
 // lanes' channels of O: 4 us per 32 keys with eight warps at it (reads of K, a row per lane, past an L1 that the tiles have taken).
 // It is for broken inputs: one NaN among the V rows of 8192 tokens x 32/8 heads makes 0.46 ms 33; 700 k tokens of one head, 77 ms, 2.5 s.
 template <int D>
-__device__ __noinline__ void st_slow_row(const ScoredTcParams &p, int64_t first, int row, int h, int lo, int hi, int lane, int32_t *beat) {
+__device__ __noinline__ void st_slow_row(const ScoredTcParams &p, int64_t first, int row, int h, int lo, int hi, int lane, int32_t *beat, float unit) {
     constexpr int V = D / 32;
     const __nv_bfloat16 *q = static_cast<const __nv_bfloat16 *>(p.s.q) + (first + row) * p.s.q_stride + h * D;
     const int kvh = h / (p.s.Hq / p.s.Hkv);
@@ -235,7 +235,7 @@ __device__ __noinline__ void st_slow_row(const ScoredTcParams &p, int64_t first,
         const int n = static_cast<int>(min(static_cast<int64_t>(32), hi - j0 + 1));
 #pragma unroll 8
         for (int t = 0; t < n; ++t) {
-            const float wt = __shfl_sync(0xffffffffu, w, t);
+            const float wt = __shfl_sync(0xffffffffu, w, t) * unit;
             const __nv_bfloat16 *vt = v + (j0 + t) * p.s.v_stride;
             if constexpr (V == 4) {
                 const uint2 x = *reinterpret_cast<const uint2 *>(vt);
@@ -250,7 +250,7 @@ __device__ __noinline__ void st_slow_row(const ScoredTcParams &p, int64_t first,
     const int64_t dst = ((first + row) * p.s.Hq + h) * D + lane * V;
 #pragma unroll
     for (int i = 0; i < V; i += 2) {
-        const float y0 = l == 0.f ? 0.f : o[i] / l, y1 = l == 0.f ? 0.f : o[i + 1] / l;
+        const float y0 = l == 0.f ? 0.f : o[i] / l / unit, y1 = l == 0.f ? 0.f : o[i + 1] / l / unit;
         if (p.s.out_bf16) *reinterpret_cast<__nv_bfloat162 *>(reinterpret_cast<__nv_bfloat16 *>(p.s.out) + dst + i) = __floats2bfloat162_rn(y0, y1);
         else *reinterpret_cast<float2 *>(reinterpret_cast<float *>(p.s.out) + dst + i) = make_float2(y0, y1);
     }
@@ -466,8 +466,8 @@ prefill_scored_tc_kernel(const __grid_constant__ ScoredTcParams p, const __grid_
                 };
                 auto nothing = [](float &, float, float) {};
                 if constexpr (CAP == 1) {
-                    // Capped scores lie within +-cap2 <= 72 log2 units: relative to 0, weights, sums over 2^24 keys and O (|v| < 2^31)
-                    // stay within fp32, so no maximum is needed.  The form that suits the block before is tried first; whether it holds here
+                    // Capped scores lie within +-cap2 <= 72 log2 units: relative to 0, weights and sums over 2^31 keys stay within fp32 (and
+                    // O for |v| < 2^31 and 2^24 keys; rows that leave it are done again), so no maximum is needed.  The form that suits the block before is tried first; whether it holds here
                     // is found out alongside.
                     if (masked) {
                         weights([&](int x) { return pack_f32x2(sv[x], sv[x + 1]); }, nothing);
@@ -535,7 +535,7 @@ prefill_scored_tc_kernel(const __grid_constant__ ScoredTcParams p, const __grid_
                 for (int x = 0; x < 32; ++x) {               // the warp's own rows, one by one
                     const int rr = trow0 + (wid & 3) * 32 + x;
                     const int2 s2 = pl.span[(wid << 5) + x];
-                    if (rr < len) st_slow_row<D>(p, first, rr, h, s2.x, s2.y, lane, beat);
+                    if (rr < len) st_slow_row<D>(p, first, rr, h, s2.x, s2.y, lane, beat, 1.f);
                 }
             } else if (ok && have) {
                 // ---- normalise this thread's row, 128 bytes of output at a time, into the warp's staging area (128-byte rows, 16-byte
@@ -548,6 +548,15 @@ prefill_scored_tc_kernel(const __grid_constant__ ScoredTcParams p, const __grid_
                 const int64_t tok0 = first + trow0 + (wid & 3) * 32;
                 const bool b16 = p.s.out_bf16 != 0;
                 const int width = b16 ? 64 : 32;                                 // channels in 128 bytes
+                float strange = 0.f, big = 0.f;                                  // NaN where some channel of O is not finite; greatest channel
+                auto scaled = [&](float (&ov)[32]) {
+#pragma unroll
+                    for (int x = 0; x < 32; ++x) {
+                        strange = fmaf(ov[x], 0.f, strange);
+                        if constexpr (CAP == 1) big = fmaxf(big, fabsf(ov[x]));
+                        ov[x] = inv == 0.f ? 0.f : ov[x] * inv;
+                    }
+                };
 #pragma unroll 1
                 for (int c = 0; c < D && rows_live > 0; c += width) {
                     if (lane == 0) tma_store_wait_read();                        // the box before has left the staging area
@@ -555,8 +564,7 @@ prefill_scored_tc_kernel(const __grid_constant__ ScoredTcParams p, const __grid_
                     uint8_t *mine = stage + lane * 128;
                     float ov[32];
                     tmem_ld32(t_o + c, ov);
-#pragma unroll
-                    for (int x = 0; x < 32; ++x) ov[x] = inv == 0.f ? 0.f : ov[x] * inv;
+                    scaled(ov);
                     if (b16) {
 #pragma unroll
                         for (int q4 = 0; q4 < 4; ++q4)
@@ -564,8 +572,7 @@ prefill_scored_tc_kernel(const __grid_constant__ ScoredTcParams p, const __grid_
                                 make_uint4(pack_bf16(ov[8 * q4], ov[8 * q4 + 1]), pack_bf16(ov[8 * q4 + 2], ov[8 * q4 + 3]),
                                            pack_bf16(ov[8 * q4 + 4], ov[8 * q4 + 5]), pack_bf16(ov[8 * q4 + 6], ov[8 * q4 + 7]));
                         tmem_ld32(t_o + c + 32, ov);
-#pragma unroll
-                        for (int x = 0; x < 32; ++x) ov[x] = inv == 0.f ? 0.f : ov[x] * inv;
+                        scaled(ov);
 #pragma unroll
                         for (int q4 = 0; q4 < 4; ++q4)
                             *reinterpret_cast<uint4 *>(mine + (((q4 + 4) ^ (lane & 7)) << 4)) =
@@ -589,6 +596,20 @@ prefill_scored_tc_kernel(const __grid_constant__ ScoredTcParams p, const __grid_
                             *reinterpret_cast<uint4 *>(dst + (((tok0 + (x >> 3)) * p.s.Hq + h) * D + c) * es + (x & 7) * 16) =
                                 *reinterpret_cast<const uint4 *>(stage + (x >> 3) * 128 + (((x & 7) ^ ((x >> 3) & 7)) << 4));
                         __syncwarp();
+                    }
+                }
+                // Weights relative to something else than the row's greatest score (0, or a reference that lags behind it) may have taken O
+                // out of fp32's range, up or (scores deep below 0, tiny v) down, though the quotient lies within: such rows are done again.
+                const bool over = strange != strange, under = CAP == 1 && l < 0x1p-32f && big < 0x1p-100f;
+                uint32_t again = __ballot_sync(0xffffffffu, lane < rows_live && l > 0.f && l < INFINITY && (over || under));
+                if (again != 0) {
+                    if (lane == 0) tma_store_wait();         // what is there already is overwritten
+                    __syncwarp();
+                    const uint32_t overs = __ballot_sync(0xffffffffu, over);
+                    for (; again != 0; again &= again - 1) {
+                        const int x = __ffs(again) - 1;
+                        const int2 s2 = pl.span[(wid << 5) + x];
+                        st_slow_row<D>(p, first, trow0 + (wid & 3) * 32 + x, h, s2.x, s2.y, lane, beat, (overs >> x) & 1 ? 0x1p-32f : 1.f);
                     }
                 }
             }

@@ -83,3 +83,22 @@ def test_a_spoiled_row_at_the_end_of_a_long_prompt(n, d, hq):
     at = sorted(rows)
     close(out[at], want[at], tol[at], "rows in front of the spoiled one")
     assert bool(out[bad:].isnan().all()) and bool(torch.isfinite(out[:bad]).all())
+
+
+@pytest.mark.parametrize("out_dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("d,hq", [(128, 2), (64, 1)])
+@pytest.mark.parametrize("cap,side,size", [(50.0, 1, 1e17), (50.0, 1, 1e36), (20.0, 1, 1e32), (50.0, -1, 1e-30), (0.0, 0, 1e37), (60.0, 1, 1e37)])
+def test_rows_of_v_far_from_one(cap, side, size, d, hq, out_dtype):
+    """Finite rows of v whose products with the weights, taken relative to another score than the row's greatest, leave fp32's range: the
+    output is an average of them all the same.  side: all scores deep in the cap's upper or lower end, or spread over some units."""
+    lens = [300, 33]
+    q, k, v, ip = prompts(lens, hq, 1, d, "bf16", seed=93, qscale=4.0 if side == 0 else 1.0)
+    if side:
+        q.copy_(q.abs() + 1)
+        k.copy_(side * (k.abs() + 1))
+    v.mul_(size)
+    assert bool(torch.isfinite(v).all())
+    want, tol = ref.prefill(q, k, v, lens, d ** -0.5 * (8 if side else 1), cap, weight=P_WEIGHT["bf16"])
+    out, status = run(q, k, v, ip, d, cap=cap, scale=d ** -0.5 * (8 if side else 1), out_dtype=out_dtype)
+    assert status == (spd.SPD_OK, -1)
+    close(out, want, tol, (cap, size))
