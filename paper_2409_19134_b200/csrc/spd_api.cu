@@ -43,19 +43,19 @@ std::atomic<int> g_min_tiles{kMinTilesPerWarp};   // fewest page tiles a share o
 std::atomic<int> g_uniform_shares{0};             // 1 = equal shares, the measured rates are ignored
 std::atomic<int> g_pdl{-1};                       // programmatic launch: -1 = not decided yet (environment), 0 off, 1 on
 
-// What the host remembers about a workspace (keyed by its address): the attention launches made on it so far, and
-// at which of them each kind of call last stored its plan.  The kernel rotates through the three thirds of the
-// workspace's rate table by the launch count, so it must advance by exactly one per attention launch on that
-// workspace whatever else the process launches in between.
+// What the host remembers about a workspace (keyed by its address): the attention launches made on it so far, how many of
+// them were the persistent kernel's, and at which of them each kind of call last stored its plan.  The persistent kernel
+// rotates through the three thirds of the workspace's rate table by its own count, so it must advance by exactly one
+// per launch of it on that workspace whatever else the process launches in between.
 struct WsHostState {
-    uint64_t launches = 0;
+    uint64_t launches = 0, turns = 0;
     uint64_t stored_at[3] = {~0ull, ~0ull, ~0ull};
 };
 
 // Registers one attention launch.  *early_plan: a launch that loads a stored plan may read it before the
 // previous kernel on the stream has finished when that kernel is not the one that stored it (the launch before
 // the previous one has left every SM by the time this one starts, since each CTA takes a whole SM).
-uint32_t register_launch(const void *ws, int slot, int plan_mode, bool *early_plan) {
+uint32_t register_launch(const void *ws, int slot, int plan_mode, bool persistent, bool *early_plan) {
     static std::mutex mu;
     static std::unordered_map<const void *, WsHostState> table;
     std::lock_guard<std::mutex> lock(mu);
@@ -64,7 +64,7 @@ uint32_t register_launch(const void *ws, int slot, int plan_mode, bool *early_pl
     *early_plan = plan_mode == PLAN_LOAD && st.stored_at[slot] != ~0ull && n >= st.stored_at[slot] + 2;
     if (plan_mode == PLAN_DERIVE_STORE) st.stored_at[slot] = n;
     if (plan_mode == PLAN_DERIVE) st.stored_at[slot] = ~0ull;
-    return static_cast<uint32_t>(n % 3u);
+    return static_cast<uint32_t>((persistent ? st.turns++ : 0) % 3u);
 }
 
 // Whether the last attention launch on the stream was one that appends (it lets the next kernel in early, but grows its lengths as
@@ -342,9 +342,6 @@ spd_status run_job(const Job &job, void *ws, size_t ws_bytes, void *stream) {
     p.rates = reinterpret_cast<float2 *>(w + L.rates);
     const int slot = (job.part[0] ? 1 : 0) + (job.part[1] ? 2 : 0) - 1;   // one stored plan per kind of call
     if (slot < 0) return SPD_ERR_INVALID_ARG;
-    bool early_plan = false;
-    p.rate_sel = static_cast<int32_t>(register_launch(ws, slot, job.plan_mode, &early_plan));   // rotates through the thirds
-    p.plan_early = early_plan && !job.wait_first ? 1 : 0;
     p.min_tiles = g_min_tiles.load();
     p.uniform = g_uniform_shares.load();
     p.plan = reinterpret_cast<int32_t *>(w + L.plan + slot * kPlanBytes);
@@ -404,19 +401,23 @@ spd_status run_job(const Job &job, void *ws, size_t ws_bytes, void *stream) {
         // descriptors it never uses
         memset(maps, 0, sizeof maps);
     }
+    // Calls with few and short sequences take a kernel of their own (a cluster of CTAs per sequence), which leaves the rates alone.
+    const int D = s.head_dim, cluster = job.score ? scored_cluster(p, di.sms, bf, D) : 0;
+    bool early_plan = false;
+    p.rate_sel = static_cast<int32_t>(register_launch(ws, slot, job.plan_mode, cluster == 0, &early_plan));   // rotates through the thirds
+    p.plan_early = early_plan && !job.wait_first ? 1 : 0;
     int pj = -1;
     {
         std::lock_guard<std::mutex> lock(g_prof.mu);
         if (g_prof.on && g_prof.jobs < g_prof.cap) pj = g_prof.jobs++;
     }
     prof_mark(pj, 0, st);
-    const int D = s.head_dim;
     // A launch that appends says itself whether it may overlap the one before (the layers of a token step may: each has lengths of
     // its own); any other one waits for an append to end.
     const bool behind = behind_append(st, job.k_new != nullptr);
     const bool pdl = programmatic_launch() && !job.plain_order && (job.k_new || !behind);
     if (job.score) {
-        rc = launch_attn_scored(p, maps, di.sms, st, pdl, bf, D);
+        rc = launch_attn_scored(p, maps, di.sms, st, pdl, bf, D, cluster);
     } else if (bf && g_bf16_math.load() == 1) {
 #define SPD_SIMT_CASE(DD, GG) if (D == DD && p.geff == GG) rc = launch_attn<MathBF16Simt<DD, GG>>(p, maps, di.sms, st, pdl);
         SPD_SIMT_CASE(64, 1) SPD_SIMT_CASE(64, 2) SPD_SIMT_CASE(64, 4) SPD_SIMT_CASE(64, 8)

@@ -79,7 +79,7 @@ struct Params {
     int32_t *tickets;       // [B * S] pieces delivered so far per sequence; zero between calls
     int32_t epoch;          // non-zero id of this call
     float2 *rates;          // [3][kMaxGrid] per-CTA (share weight, cycles) of earlier launches
-    int32_t rate_sel;       // attention launches on this workspace so far: this launch writes third rate_sel % 3,
+    int32_t rate_sel;       // launches of the persistent kernel on this workspace so far: this launch writes third rate_sel % 3,
                             // reads (rate_sel + 1) % 3
     int32_t *plan;          // [PLAN_WORDS] the stored plan
     int32_t plan_mode;      // PlanMode

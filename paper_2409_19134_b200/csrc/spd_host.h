@@ -27,7 +27,6 @@ size_t cleared_end(int batch, int seqs);       // first byte behind what a statu
 
 inline bool misaligned(const void *p, size_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) != 0; }
 
-
 inline int elem_size(const spd_shape &s) { return s.dtype == SPD_BF16 ? 2 : 4; }
 
 // Strides of a token's rows in elements (0 = packed); false if they do not fit the rows or their alignment.
@@ -39,7 +38,9 @@ inline bool row_stride(const spd_shape &s, int heads, int64_t given, int64_t *st
 
 }  // namespace host
 
-// Launch of the scored attention kernels (spd_scored.cu): bf16 or fp32, by head_dim and group.
-spd_status launch_attn_scored(const Params &p, const CUtensorMap *maps, int sms, cudaStream_t st, bool pdl, bool bf16, int head_dim);
+// The scored attention kernels (spd_scored.cu), bf16 or fp32, by head_dim and group.  scored_cluster: CTAs that share a sequence where
+// the call takes the cluster kernel, 0 where it takes the persistent one.
+int scored_cluster(const Params &p, int sms, bool bf16, int head_dim);
+spd_status launch_attn_scored(const Params &p, const CUtensorMap *maps, int sms, cudaStream_t st, bool pdl, bool bf16, int head_dim, int cluster);
 
 }  // namespace spd

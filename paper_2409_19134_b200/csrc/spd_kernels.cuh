@@ -955,7 +955,8 @@ attn_kernel(const __grid_constant__ Params p, const __grid_constant__ CUtensorMa
 
     const int C = (p.B + NT - 1) / NT;
     const int G = gridDim.x;
-    // launch N on a workspace writes third N % 3 and reads the one launch N-2 wrote: launch N-1 may still be running
+    // launch N of this kernel on a workspace writes third N % 3 and reads the one launch N-2 wrote: launch N-1 may still be running
+    // (where a launch of the cluster kernel lies in between, it has let this one in only after its own predecessor had gone)
     const float2 *rate_rd = p.rates + ((p.rate_sel + 1) % 3) * kMaxGrid;
     float2 *rate_wr = p.rates + (p.rate_sel % 3) * kMaxGrid;
     int32_t *bnd = reinterpret_cast<int32_t *>(tail + attn_bnd_offset<Math>());

@@ -1,4 +1,6 @@
 // Append with rotation, and the launch of the scored decode kernels.
+#include <type_traits>
+
 #include "spd_host.h"
 #include "spd_launch.cuh"
 #include "spd_rope.cuh"
@@ -51,8 +53,7 @@ static int short_cluster(const Params &p, int sms) {
 }
 
 template <class Math>
-static spd_status launch_scored(const Params &p, const CUtensorMap *maps, int sms, cudaStream_t st, bool pdl) {
-    const int cluster = short_cluster<Math>(p, sms);
+static spd_status launch_scored(const Params &p, const CUtensorMap *maps, int sms, cudaStream_t st, bool pdl, int cluster) {
     if (cluster == 0) return launch_attn<Math>(p, maps, sms, st, pdl);
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(static_cast<unsigned>(p.B * p.S * cluster));
@@ -73,29 +74,31 @@ static spd_status launch_scored(const Params &p, const CUtensorMap *maps, int sm
     return err == cudaSuccess ? SPD_OK : SPD_ERR_CUDA;
 }
 
-spd_status launch_attn_scored(const Params &p, const CUtensorMap *maps, int sms, cudaStream_t st, bool pdl, bool bf16, int head_dim) {
-    spd_status rc = SPD_ERR_UNSUPPORTED;
-    if (bf16) {
-        rc = head_dim == 128 ? launch_scored<MathBF16<128, true>>(p, maps, sms, st, pdl) : launch_scored<MathBF16<64, true>>(p, maps, sms, st, pdl);
-    } else {
-#define SPD_F32_CASE(DD, GG) if (head_dim == DD && p.geff == GG) rc = launch_scored<MathF32<DD, GG, true>>(p, maps, sms, st, pdl);
-        SPD_F32_CASE(64, 1) SPD_F32_CASE(64, 2) SPD_F32_CASE(64, 4) SPD_F32_CASE(64, 8)
-        SPD_F32_CASE(128, 1) SPD_F32_CASE(128, 2) SPD_F32_CASE(128, 4) SPD_F32_CASE(128, 8)
+// f(m) with m a (null) pointer to the arithmetic of the call.
+template <class F>
+static auto with_math(const Params &p, bool bf16, int head_dim, F &&f) -> decltype(f(static_cast<MathBF16<128, true> *>(nullptr))) {
+    if (bf16) return head_dim == 128 ? f(static_cast<MathBF16<128, true> *>(nullptr)) : f(static_cast<MathBF16<64, true> *>(nullptr));
+#define SPD_F32_CASE(DD, GG) if (head_dim == DD && p.geff == GG) return f(static_cast<MathF32<DD, GG, true> *>(nullptr));
+    SPD_F32_CASE(64, 1) SPD_F32_CASE(64, 2) SPD_F32_CASE(64, 4) SPD_F32_CASE(64, 8)
+    SPD_F32_CASE(128, 1) SPD_F32_CASE(128, 2) SPD_F32_CASE(128, 4)
 #undef SPD_F32_CASE
-    }
-    return rc;
+    return f(static_cast<MathF32<128, 8, true> *>(nullptr));      // check_shape lets no other through
+}
+
+int scored_cluster(const Params &p, int sms, bool bf16, int head_dim) {
+    return with_math(p, bf16, head_dim, [&](auto *m) { return short_cluster<std::remove_pointer_t<decltype(m)>>(p, sms); });
+}
+
+spd_status launch_attn_scored(const Params &p, const CUtensorMap *maps, int sms, cudaStream_t st, bool pdl, bool bf16, int head_dim, int cluster) {
+    return with_math(p, bf16, head_dim, [&](auto *m) { return launch_scored<std::remove_pointer_t<decltype(m)>>(p, maps, sms, st, pdl, cluster); });
 }
 
 }  // namespace spd
-
-namespace {
 
 using namespace spd;
 using host::elem_size;
 using host::misaligned;
 using host::row_stride;
-
-}  // namespace
 
 extern "C" {
 
