@@ -61,6 +61,7 @@ spd_status prefill_tc(const spd_shape &s, const ScoredPrefillParams &sp, cudaStr
     p.heads_per_cta = g % 2 == 0 ? 2 : 1;
     p.c2 = s.sm_scale * kLog2e;
     p.half_at = p.one_at = -1.f;
+    p.wait_limit = st_wait_limit(sp.T);
     const bool bias = sp.slopes != nullptr;
     const int cap = sp.cap == 0.f ? 0 : (sp.cap <= kStFixedCap && !bias) ? 1 : 2;
     if (sp.cap > 0.f) {

@@ -72,11 +72,20 @@ constexpr size_t st_smem_bytes(int D) {
 }
 static_assert(st_smem_bytes(128) <= 232448, "shared memory of an SM");
 
+// Polls before a wait gives up.  Beyond the usual limit 512 per token of the call: a tile whose rows are done one by one takes its warps
+// 4 us per key (in L2; more where K and V are not), and a poll takes 0.1 us beside such warps (1.5 us where nothing moves), by
+// measurement.  (A limit that starts anew while such rows make progress costs the ordinary call 2 to 4 %.)
+inline uint32_t st_wait_limit(int64_t tokens) {
+    const int64_t polls = static_cast<int64_t>(kWaitLimit) + 512 * tokens;
+    return polls > 0xffffffffll ? 0xffffffffu : static_cast<uint32_t>(polls);
+}
+
 struct ScoredTcParams {
     ScoredPrefillParams s;
     int32_t heads_per_cta;      // 2: tiles are two heads over the same rows; 1: two row blocks of one head
     float c2;                   // sm_scale log2(e)
     float cap2;                 // cap log2(e)
+    uint32_t wait_limit;        // polls before a wait gives up
     float y1;                   // sm_scale / cap: what is inside the tanh per unit of q.k
     float half_at, one_at;      // where the two polynomials below end (1/2 and 1; -1 = not to be used)
     uint64_t p1[4], p2[6];      // coefficients for |y1 x| <= 1/2 and <= 1, each in both halves.  CAP 1: of cap2 tanh(y1 x) = x P(x^2);
@@ -138,6 +147,13 @@ __device__ __forceinline__ float fmax3_abs(float a, float b, float c) {
     return r;
 }
 
+// The same, but NaN where one of them is.
+__device__ __forceinline__ float fmax3_abs_nan(float a, float b, float c) {
+    float r;
+    asm("max.NaN.abs.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+    return r;
+}
+
 // One box from shared memory to the output (every row of it belongs to the prompt), and the waits for such stores: until the
 // staging area has been read, and until they are done.
 __device__ __forceinline__ void tma_store_3d(const CUtensorMap *map, uint32_t src, int x, int y, int z) {
@@ -168,25 +184,20 @@ __device__ __forceinline__ float st_cap(const ScoredTcParams &p, float x) {
     return p.cap2 - __fdividef(2.f * p.cap2, ex2_approx(x * (2.f * kLog2e) * p.y1) + 1.f);
 }
 
-// Waits like mbar_wait, but does not give up while rows are being done one by one (st_slow_row counts `beat` on): how long that
-// takes goes by the length of the prompt.
-__device__ __forceinline__ bool st_mbar_wait(uint32_t bar, uint32_t parity, const volatile int32_t *beat) {
-    int32_t seen = 0;
-    for (uint32_t i = 0; i < kWaitLimit; ++i) {
+// mbar_wait with a limit of the call's own.
+__device__ __forceinline__ bool st_mbar_wait(uint32_t bar, uint32_t parity, uint32_t limit) {
+    if (mbar_try_wait(bar, parity)) return true;       // no look at the limit on the way that counts
+    for (uint32_t i = 1; i < limit; ++i)
         if (mbar_try_wait(bar, parity)) return true;
-        if ((i & 0xffffu) == 0xffffu) {
-            const int32_t now = *beat;
-            if (now != seen) { seen = now; i = 0; }
-        }
-    }
     return false;
 }
 
-// One row the slow way, run by a whole warp: keys outside [lo, hi] are not touched; O is summed in units of 1 / unit.  32 keys at a time, a score per lane, then the
-// lanes' channels of O: 4 us per 32 keys with eight warps at it (reads of K, a row per lane, past an L1 that the tiles have taken).
+// One row the slow way, run by a whole warp: keys outside [lo, hi] are not touched; O is summed in units of 1 / unit.  32 keys at
+// a time, a score per lane, then the lanes' channels of O: 4 us per 32 keys with eight warps at it (reads of K, a row per lane,
+// past an L1 that the tiles have taken).
 // It is for broken inputs: one NaN among the V rows of 8192 tokens x 32/8 heads makes 0.46 ms 33; 700 k tokens of one head, 77 ms, 2.5 s.
 template <int D>
-__device__ __noinline__ void st_slow_row(const ScoredTcParams &p, int64_t first, int row, int h, int lo, int hi, int lane, int32_t *beat, float unit) {
+__device__ __noinline__ void st_slow_row(const ScoredTcParams &p, int64_t first, int row, int h, int lo, int hi, int lane, float unit) {
     constexpr int V = D / 32;
     const __nv_bfloat16 *q = static_cast<const __nv_bfloat16 *>(p.s.q) + (first + row) * p.s.q_stride + h * D;
     const int kvh = h / (p.s.Hq / p.s.Hkv);
@@ -198,7 +209,6 @@ __device__ __noinline__ void st_slow_row(const ScoredTcParams &p, int64_t first,
 #pragma unroll
     for (int i = 0; i < V; ++i) o[i] = 0.f;
     for (int64_t j0 = lo; j0 <= hi; j0 += 32) {
-        if (((j0 - lo) & 0x1fff) == 0 && lane == 0) atomicAdd(beat, 1);
         const int64_t j = j0 + lane;
         float s = 0.f;
         if (j <= hi) {
@@ -256,6 +266,29 @@ __device__ __noinline__ void st_slow_row(const ScoredTcParams &p, int64_t first,
     }
 }
 
+// In the sign bits of the result's halves: a 16-bit half with all exponent bits set carries into its sign bit.
+__device__ __forceinline__ uint32_t st_not_finite(const uint4 &w) {
+    return (((w.x & 0x7f807f80u) + 0x00800080u) | ((w.y & 0x7f807f80u) + 0x00800080u) | ((w.z & 0x7f807f80u) + 0x00800080u) |
+            ((w.w & 0x7f807f80u) + 0x00800080u)) & 0x80008000u;
+}
+
+// Whether some V row of keys [lo, hi] is not finite; run by a whole warp.
+template <int D>
+__device__ __noinline__ bool st_spoiled(const ScoredTcParams &p, int64_t first, int h, int lo, int hi, int lane) {
+    constexpr int CH = D / 8, KW = 32 / CH;             // 16-byte chunks of a row, keys per load of the warp
+    const __nv_bfloat16 *v = static_cast<const __nv_bfloat16 *>(p.s.v) + first * p.s.v_stride + h / (p.s.Hq / p.s.Hkv) * D + lane % CH * 8;
+    for (int64_t j0 = lo; j0 <= hi; j0 += 8 * KW) {
+        uint32_t any = 0;
+#pragma unroll
+        for (int x = 0; x < 8; ++x) {
+            const int64_t j = j0 + x * KW + lane / CH;
+            if (j <= hi) any |= st_not_finite(*reinterpret_cast<const uint4 *>(v + j * p.s.v_stride));
+        }
+        if (__any_sync(0xffffffffu, any != 0)) return true;
+    }
+    return false;
+}
+
 // CAP: 0 = scores are not capped; 1 = capped, with a cap that lets every weight be taken relative to 0; 2 = any cap.
 template <int D, int CAP, bool BIAS>
 __global__ void __launch_bounds__(kStThreads, 1)
@@ -274,9 +307,8 @@ prefill_scored_tc_kernel(const __grid_constant__ ScoredTcParams p, const __grid_
     uint64_t *bar_k = bars + 14, *bar_v = bar_k + NS, *bar_kfree = bar_v + NS, *bar_vfree = bar_kfree + NS;
     uint64_t *bar_guard = bar_vfree + NS;                          // per V slot: the guards are done with the block
     constexpr int NBARS = 14 + 5 * NS;
-    static_assert(NBARS * 8 + 8 <= kStBarBytes, "barrier block");
+    static_assert(NBARS * 8 + 4 <= kStBarBytes, "barrier block");
     uint32_t &tmem_slot = *reinterpret_cast<uint32_t *>(bars + NBARS);
-    int32_t *beat = reinterpret_cast<int32_t *>(bars + NBARS) + 1;      // counted on while rows are done one by one
     StPlan *plans = reinterpret_cast<StPlan *>(stage_all + 8 * kStStage + kStBarBytes);
     const int tid = threadIdx.x, wid = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31;
     const int hpc = p.heads_per_cta, hgroups = p.s.Hq / hpc, gq = p.s.Hq / p.s.Hkv;
@@ -284,7 +316,6 @@ prefill_scored_tc_kernel(const __grid_constant__ ScoredTcParams p, const __grid_
 
     if (blockIdx.x == 0) scored_check_offsets(p.s);
     if (tid == 320) {
-        *beat = 0;
         prefetch_tensormap(&mq); prefetch_tensormap(&mk); prefetch_tensormap(&mv); prefetch_tensormap(&mo);
         for (int b = 0; b < NBARS; ++b) {
             // Q and ring slots free: one per tile; S in registers, P written: one per softmax warp of the tile;
@@ -304,11 +335,11 @@ prefill_scored_tc_kernel(const __grid_constant__ ScoredTcParams p, const __grid_
     tc_fence_after();
     const uint32_t tmem = __shfl_sync(0xffffffffu, tmem_slot, 0);
 
-    // Every wait is bounded (st_slow_row by the length of its rows).  A wait that runs out clears `ok`, and the warp leaves its loops at the next turn; nothing in the
+    // Every wait is bounded, by more than rows that are done one by one take the warps that are waited for.  A wait that runs out clears `ok`, and the warp leaves its loops at the next turn; nothing in the
     // loops waits for all threads, so everybody comes to the common end.
     bool ok = true;
-    auto wait = [&](uint64_t *bar, uint32_t parity) { if (ok) ok = __all_sync(0xffffffffu, st_mbar_wait(smem_u32(bar), parity & 1, beat)); };   // whole warps
-    auto wait1 = [&](uint64_t *bar, uint32_t parity) { ok = ok && st_mbar_wait(smem_u32(bar), parity & 1, beat); };                             // the loading thread
+    auto wait = [&](uint64_t *bar, uint32_t parity) { if (ok) ok = __all_sync(0xffffffffu, st_mbar_wait(smem_u32(bar), parity & 1, p.wait_limit)); };   // whole warps
+    auto wait1 = [&](uint64_t *bar, uint32_t parity) { ok = ok && st_mbar_wait(smem_u32(bar), parity & 1, p.wait_limit); };                             // the loading thread
     // item r of this CTA: plan buffer r & 1, in its (r / 2)-th use
     auto plan_of = [&](int r) -> StPlan & { wait(&bar_plan[r & 1], r >> 1); __syncwarp(); return plans[r & 1]; };
     auto plan_done = [&](int r) { __syncwarp(); if (lane == 0) mbar_arrive(smem_u32(&bar_planfree[r & 1])); };
@@ -535,7 +566,7 @@ prefill_scored_tc_kernel(const __grid_constant__ ScoredTcParams p, const __grid_
                 for (int x = 0; x < 32; ++x) {               // the warp's own rows, one by one
                     const int rr = trow0 + (wid & 3) * 32 + x;
                     const int2 s2 = pl.span[(wid << 5) + x];
-                    if (rr < len) st_slow_row<D>(p, first, rr, h, s2.x, s2.y, lane, beat, 1.f);
+                    if (rr < len) st_slow_row<D>(p, first, rr, h, s2.x, s2.y, lane, 1.f);
                 }
             } else if (ok && have) {
                 // ---- normalise this thread's row, 128 bytes of output at a time, into the warp's staging area (128-byte rows, 16-byte
@@ -548,14 +579,12 @@ prefill_scored_tc_kernel(const __grid_constant__ ScoredTcParams p, const __grid_
                 const int64_t tok0 = first + trow0 + (wid & 3) * 32;
                 const bool b16 = p.s.out_bf16 != 0;
                 const int width = b16 ? 64 : 32;                                 // channels in 128 bytes
-                float strange = 0.f, big = 0.f;                                  // NaN where some channel of O is not finite; greatest channel
+                float big[4] = {0.f, 0.f, 0.f, 0.f};                            // greatest channel of O, NaN among them included
                 auto scaled = [&](float (&ov)[32]) {
 #pragma unroll
-                    for (int x = 0; x < 32; ++x) {
-                        strange = fmaf(ov[x], 0.f, strange);
-                        if constexpr (CAP == 1) big = fmaxf(big, fabsf(ov[x]));
-                        ov[x] = inv == 0.f ? 0.f : ov[x] * inv;
-                    }
+                    for (int x = 0; x < 32; x += 2) big[(x >> 1) & 3] = fmax3_abs_nan(big[(x >> 1) & 3], ov[x], ov[x + 1]);
+#pragma unroll
+                    for (int x = 0; x < 32; ++x) ov[x] = inv == 0.f ? 0.f : ov[x] * inv;
                 };
 #pragma unroll 1
                 for (int c = 0; c < D && rows_live > 0; c += width) {
@@ -599,17 +628,23 @@ prefill_scored_tc_kernel(const __grid_constant__ ScoredTcParams p, const __grid_
                     }
                 }
                 // Weights relative to something else than the row's greatest score (0, or a reference that lags behind it) may have taken O
-                // out of fp32's range, up or (scores deep below 0, tiny v) down, though the quotient lies within: such rows are done again.
-                const bool over = strange != strange, under = CAP == 1 && l < 0x1p-32f && big < 0x1p-100f;
-                uint32_t again = __ballot_sync(0xffffffffu, lane < rows_live && l > 0.f && l < INFINITY && (over || under));
+                // out of fp32's range, up or (scores deep below 0, tiny v) down, though the quotient lies within: such rows are done again,
+                // unless V itself is not finite among the keys that they all see (were it so among others, all rows would be done so).
+                const float top = fmax3_abs_nan(fmax3_abs_nan(big[0], big[1], big[2]), big[3], 0.f);
+                const bool over = !(top < INFINITY), under = CAP == 1 && l < 0x1p-32f && top < 0x1p-100f;
+                const bool sound = lane < rows_live && l > 0.f && l < INFINITY;
+                uint32_t again = __ballot_sync(0xffffffffu, sound && (over || under)), overs = __ballot_sync(0xffffffffu, sound && over);
+                if (overs != 0) {
+                    const int a = __reduce_max_sync(0xffffffffu, sound && over ? lo : 0), b = __reduce_min_sync(0xffffffffu, sound && over ? hi : 0x7fffffff);
+                    if (st_spoiled<D>(p, first, h, a, b, lane)) again &= ~overs;
+                }
                 if (again != 0) {
                     if (lane == 0) tma_store_wait();         // what is there already is overwritten
                     __syncwarp();
-                    const uint32_t overs = __ballot_sync(0xffffffffu, over);
                     for (; again != 0; again &= again - 1) {
                         const int x = __ffs(again) - 1;
                         const int2 s2 = pl.span[(wid << 5) + x];
-                        st_slow_row<D>(p, first, trow0 + (wid & 3) * 32 + x, h, s2.x, s2.y, lane, beat, (overs >> x) & 1 ? 0x1p-32f : 1.f);
+                        st_slow_row<D>(p, first, trow0 + (wid & 3) * 32 + x, h, s2.x, s2.y, lane, (overs >> x) & 1 ? 0x1p-32f : 1.f);
                     }
                 }
             }
@@ -785,19 +820,15 @@ prefill_scored_tc_kernel(const __grid_constant__ ScoredTcParams p, const __grid_
                     continue;
                 }
                 uint8_t *vt = base + 2 * QTILE + (NS + slot) * TILE;
-                auto odd = [](const uint4 &w) {           // a 16-bit half with all exponent bits set carries into its sign bit
-                    return ((w.x & 0x7f807f80u) + 0x00800080u) | ((w.y & 0x7f807f80u) + 0x00800080u) | ((w.z & 0x7f807f80u) + 0x00800080u) |
-                           ((w.w & 0x7f807f80u) + 0x00800080u);
-                };
                 uint32_t any = 0;
 #pragma unroll
                 for (int x = lane; x < BOXES * GR * 8; x += 32)
-                    any |= odd(*reinterpret_cast<const uint4 *>(vt + (x / (GR * 8)) * kStBox + g0 * 128 + (x % (GR * 8)) * 16));
-                if (__any_sync(0xffffffffu, (any & 0x80008000u) != 0)) {
+                    any |= st_not_finite(*reinterpret_cast<const uint4 *>(vt + (x / (GR * 8)) * kStBox + g0 * 128 + (x % (GR * 8)) * 16));
+                if (__any_sync(0xffffffffu, any != 0)) {
                     for (int row = g0; row < g0 + GR; ++row) {        // rare: row by row
                         uint4 *chunk = reinterpret_cast<uint4 *>(vt + (lane >> 3) * kStBox + row * 128 + (lane & 7) * 16);
                         const bool mine = lane < 8 * BOXES;
-                        if (!__any_sync(0xffffffffu, mine && (odd(*(mine ? chunk : reinterpret_cast<uint4 *>(vt + row * 128))) & 0x80008000u) != 0)) continue;
+                        if (!__any_sync(0xffffffffu, mine && st_not_finite(*(mine ? chunk : reinterpret_cast<uint4 *>(vt + row * 128))) != 0)) continue;
                         const int key = kb + row;
                         bool seen = false, hidden = false;
                         for (int x = lane; x < 256; x += 32) {

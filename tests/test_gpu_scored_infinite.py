@@ -102,3 +102,17 @@ def test_rows_of_v_far_from_one(cap, side, size, d, hq, out_dtype):
     out, status = run(q, k, v, ip, d, cap=cap, scale=d ** -0.5 * (8 if side else 1), out_dtype=out_dtype)
     assert status == (spd.SPD_OK, -1)
     close(out, want, tol, (cap, size))
+
+
+@pytest.mark.parametrize("cap", [0.0, 30.0])
+@pytest.mark.parametrize("n,d,hq", [(512, 128, 2), (300, 64, 1), (70001, 64, 1)])
+def test_one_channel_of_a_key_that_everybody_sees_is_nan(n, d, hq, cap):
+    """That channel is NaN for every row, the others are as without it; nothing is to be gained by doing rows again."""
+    q, k, v, ip = prompts([n], hq, 1, d, "bf16", seed=94)
+    rows = set(range(n)) if n < 1000 else {0, 1, 255, 256, n // 2, n - 1}
+    want, tol = ref.prefill(q, k, v, [n], d ** -0.5, cap, weight=P_WEIGHT["bf16"], rows=rows)
+    v[0, 0, 3] = float("nan")
+    out, status = run(q, k, v, ip, d, cap=cap)
+    assert status == (spd.SPD_OK, -1) and bool(out[:, :, 3].isnan().all())
+    at, rest = sorted(rows), [c for c in range(d) if c != 3]
+    close(out[at][..., rest], want[at][..., rest], tol[at], "other channels")
