@@ -299,7 +299,7 @@ spd_status spd_service_attn_merge_append(const spd_shape *shape, const void *q, 
  * cores always).  Stream order (the other half's lengths are read ahead of the previous kernel like one's own), errors and workspace as for the plain calls.
  * A visible key whose row of k is NaN makes the outputs concerned NaN (the plain calls give zeros there); one whose score is
  * -inf weighs nothing, and where all of them do, the output is zeros.  Calls with few and
- * short sequences -- by the window, or by the pools' pages -- take a kernel of their own (a cluster of CTAs per sequence) unless
+ * short sequences -- by the window, or by the pools' pages, since the host does not see the lengths -- take a kernel of their own (a cluster of CTAs per sequence) unless
  * spd_set_split asks for a cut or `plan` is not SPD_PLAN_PER_CALL.
  */
 typedef struct {
@@ -333,12 +333,13 @@ typedef struct {
  * Prompt attention with the scores of the scored calls and interval masks (no counterpart in the paper): row i of a prompt
  * sees its keys j with lo_i <= j <= hi_i, positions counted within the prompt,
  *     lo_i = max(0, doc_start_i, i - window + 1),     hi_i = i, or min(prefix_lens[u], length) - 1 where i lies below that.
- *   prefix_lens : device [batch] or NULL; the first prefix_lens[u] tokens see one another in both directions.
+ *   prefix_lens : device [batch] or NULL; the first prefix_lens[u] tokens see forward to the prefix's end (and so one another in
+ *                 both directions, as far as doc_start and window let a row look back: across documents only the forward look is there).
  *   doc_start   : device [total_tokens] or NULL; the first token that the row may see (packed documents: its document's
  *                 first token; padding: anything above i).
- * d is |i - j|.  A row that sees nothing gives zeros.  Keys that a row does not see never enter its result, whatever
+ * d is |i - j|.  A row that sees nothing, or only scores of -inf, gives zeros.  Keys that a row does not see never enter its result, whatever
  * their rows of k and v hold.  `tok` as above; tok_indptr [batch+1] (device), its consistency and what happens where it
- * is not consistent as for spd_prefill_attn; out [total_tokens][num_q_heads][head_dim] in out_dtype, packed.  The prompts'
+ * is not consistent as for spd_prefill_attn; out [total_tokens][num_q_heads][head_dim] in out_dtype, packed, overlapping none of the inputs.  The prompts'
  * rows do not go to a cache here: spd_append_kv_rope does that, with or without rotation.  sm_scale > 0, else
  * SPD_ERR_UNSUPPORTED.  One kernel in plain stream order; it counts its work in words of `ws`, so calls that share a
  * workspace must be ordered.  BF16 runs on the tensor cores (weights rounded to bf16 once, as in spd_prefill_attn; rows that see only

@@ -117,7 +117,8 @@ spd_status launch_prefill_f32(const spd_shape &s, const ScoredPrefillParams &p, 
     return cudaGetLastError() == cudaSuccess ? SPD_OK : SPD_ERR_CUDA;
 }
 
-// fp32 prompts on the FMA pipes: four rows per thread, two where that leaves SMs without work or prompts do not fill 64 rows; two
+// fp32 prompts on the FMA pipes: four rows per thread, two where that leaves SMs without work or prompts fill half of 64 rows at most
+// (by the mean over all users, those without a prompt among them: the host knows no lengths, and any choice is right); two
 // groups of threads per tile where the keys of a row, not the number of tiles, are what an SM's work consists of.  us, two rows / four /
 // four and two groups, 8 heads of 64: 2 x 256 tokens 19.1 / 26.2 / 24.4, 200 x 20 53 / 70 / 107, 4 x 256 30.2 / 41.2 / 25.1, 2 x 1000
 // 149 / 152 / 129, 4 x 1000 255 / 217 / 205, 16 x 1000 846 / 634 / 683, 64 x 256 271 / 208 / 256.

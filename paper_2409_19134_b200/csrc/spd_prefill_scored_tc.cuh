@@ -22,10 +22,12 @@
 // visible to others, the CTA's rows are done again one by one, hidden keys left out.
 //
 // Bound: the exponential unit (2 x 128 x 80 exponentials a block of two tiles at 16 a cycle: 1280 cycles) and the tensor core
-// (about 1470) alike, of about 2000 that a block takes; with capped scores the FMA pipe too (2700), and over seconds the power
-// limit (8192 tokens, 32/8 heads: 446 us in the first 100 calls, 514 at 1590 MHz and 990 W after three seconds).  Measured in bursts,
-// head_dim 128, bf16: 8192 tokens x 32/8 heads plain 447 us (1230 TFLOP/s of visible pairs), capped 580 (948), distance bias 545
-// (1008); 8 prompts of 2 to 8 k tokens 1.85 ms (1260); 3 prompts with prefix and window 124 us (915).
+// (about 1470) alike, of about 2000 that a block takes (each pipe two thirds busy).  With a cap a block takes about 2700, with a distance bias
+// 2400, and no pipe is busy for more than half of it: what they add stands in a row's chain between a score's arrival and its
+// weight, on top of the exponentials instead of beside them.  Over seconds the power limit (8192 tokens, 32/8 heads: 446 us in the
+// first 100 calls, 514 at 1590 MHz and 990 W after three seconds).  Measured on one GPU, back to back, head_dim 128, bf16: 8192 tokens
+// x 32/8 heads plain 445 us (1236 TFLOP/s of visible pairs), distance bias 539 (1020), cap of 50 640 (859; 580 in a first burst), of
+// 64 744; 8 prompts of 2 to 8 k tokens (50 572 in all) 2.24 ms (1220); 3 prompts with prefix and window 126 us (900).
 // Slower here: the tiles' exponentials in turns by named barriers (20 %), two threads per row (instruction issue, 15 %), the next
 // block's scores prepared in registers under this block's exponentials (60 %; the compiler serialises them), barriers of its own for
 // each tile's Q, which lets the tiles drift apart (4 % with caps).

@@ -7,7 +7,7 @@
 // anybody, and keeps the sines and cosines of its unit in registers while it walks the token's heads.  Angles: the turns
 // pos * inv_freq / 2 pi are formed in 64 bits and reduced to [-1/2, 1/2] there (a position of 10^5 leaves 32 bits no
 // fraction to speak of), then sincospif; once per token and pair, shared by all heads.
-// Measured: 8 prompts, 38 k tokens of 32/8 heads, head_dim 128, bf16 (1.42 GB) 258 us, 5.5 TB/s; rows in flight per thread 2 / 3 / 4:
+// Measured: 8 prompts, 53 k tokens of 32/8 heads, head_dim 128, bf16 (1.42 GB) 258 us, 5.5 TB/s; rows in flight per thread 2 / 3 / 4:
 // 269 / 258 / 259 us, tokens per CTA 2 / 4 / 8: 306 / 258 / 255, and 7.0 / 7.4 / 9.2 us for 1800 tokens; without loading rows ahead of
 // the search 327.  One token for each of 512 users (22 MB, L2) 6.2 us, of 8 users 3.6 us.
 #pragma once

@@ -6,7 +6,8 @@
 // cut of the whole batch) and on handing pieces over through global memory (fence, ticket, round trips of the merge).  Here
 // the chain is: lengths and table bounds, page indices, tiles, join.  Tiles, arithmetic and ring are the persistent kernel's.
 // Used where every warp has at most kShortTiles tiles and all clusters fit the machine at once (one CTA per SM).  Measured, this
-// kernel / the persistent one, us per call back to back, 32/8 heads, head_dim 128, bf16: 1 user x 288 tokens 5.9 / 18.2, 8 users
+// kernel / the persistent one, us per call back to back, 32/8 heads, head_dim 128, bf16: 1 user x 288 tokens (in pools that hold
+// little more: without a window the pools' pages are all that the host knows of the lengths) 5.9 / 18.2, 8 users
 // through a window of 1024 tokens 10.3 / 26.2, of 4096 25.2 / 42.1, of 8192 (32 tiles a warp) 45.3 / 61.0; beyond that the gap
 // closes (16 users, 16384: 171 / 180) and uneven lengths are what the persistent kernel's cut is for.
 #pragma once
