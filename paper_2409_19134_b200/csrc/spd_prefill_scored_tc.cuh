@@ -274,9 +274,9 @@ __device__ __forceinline__ uint32_t st_not_finite(const uint4 &w) {
             ((w.w & 0x7f807f80u) + 0x00800080u)) & 0x80008000u;
 }
 
-// Whether some V row of keys [lo, hi] is not finite; run by a whole warp.
+// Whether some V row of keys [lo, hi] holds a number that is not finite, or (nonzero) one that is not 0; run by a whole warp.
 template <int D>
-__device__ __noinline__ bool st_spoiled(const ScoredTcParams &p, int64_t first, int h, int lo, int hi, int lane) {
+__device__ __noinline__ bool st_found(const ScoredTcParams &p, int64_t first, int h, int lo, int hi, int lane, bool nonzero) {
     constexpr int CH = D / 8, KW = 32 / CH;             // 16-byte chunks of a row, keys per load of the warp
     const __nv_bfloat16 *v = static_cast<const __nv_bfloat16 *>(p.s.v) + first * p.s.v_stride + h / (p.s.Hq / p.s.Hkv) * D + lane % CH * 8;
     for (int64_t j0 = lo; j0 <= hi; j0 += 8 * KW) {
@@ -284,7 +284,10 @@ __device__ __noinline__ bool st_spoiled(const ScoredTcParams &p, int64_t first, 
 #pragma unroll
         for (int x = 0; x < 8; ++x) {
             const int64_t j = j0 + x * KW + lane / CH;
-            if (j <= hi) any |= st_not_finite(*reinterpret_cast<const uint4 *>(v + j * p.s.v_stride));
+            if (j <= hi) {
+                const uint4 w = *reinterpret_cast<const uint4 *>(v + j * p.s.v_stride);
+                any |= nonzero ? (w.x | w.y | w.z | w.w) & 0x7fff7fffu : st_not_finite(w);
+            }
         }
         if (__any_sync(0xffffffffu, any != 0)) return true;
     }
@@ -630,15 +633,22 @@ prefill_scored_tc_kernel(const __grid_constant__ ScoredTcParams p, const __grid_
                     }
                 }
                 // Weights relative to something else than the row's greatest score (0, or a reference that lags behind it) may have taken O
-                // out of fp32's range, up or (scores deep below 0, tiny v) down, though the quotient lies within: such rows are done again,
-                // unless V itself is not finite among the keys that they all see (were it so among others, all rows would be done so).
+                // out of fp32's range, though the quotient lies within: up, or down (all weights below 1 and tiny v; the tensor core
+                // knows no denormal sums).  Such rows are done again, unless V itself is not finite among the keys that they all see
+                // (were it so among others, all rows would be done again) or 0 wherever they look.
                 const float top = fmax3_abs_nan(fmax3_abs_nan(big[0], big[1], big[2]), big[3], 0.f);
-                const bool over = !(top < INFINITY), under = CAP == 1 && l < 0x1p-32f && top < 0x1p-100f;
-                const bool sound = lane < rows_live && l > 0.f && l < INFINITY;
-                uint32_t again = __ballot_sync(0xffffffffu, sound && (over || under)), overs = __ballot_sync(0xffffffffu, sound && over);
+                const bool sound = lane < rows_live && l > 0.f && l < INFINITY, over = sound && !(top < INFINITY);
+                const bool under = CAP == 1 && sound && top < 0x1p-100f && l < static_cast<float>(hi - lo + 1);
+                const uint32_t overs = __ballot_sync(0xffffffffu, over);
+                uint32_t again = overs;
                 if (overs != 0) {
-                    const int a = __reduce_max_sync(0xffffffffu, sound && over ? lo : 0), b = __reduce_min_sync(0xffffffffu, sound && over ? hi : 0x7fffffff);
-                    if (st_spoiled<D>(p, first, h, a, b, lane)) again &= ~overs;
+                    const int a = __reduce_max_sync(0xffffffffu, over ? lo : 0), b = __reduce_min_sync(0xffffffffu, over ? hi : 0x7fffffff);
+                    if (st_found<D>(p, first, h, a, b, lane, false)) again = 0;
+                }
+                if (CAP == 1 && __any_sync(0xffffffffu, under)) {
+                    const int a = __reduce_min_sync(0xffffffffu, under ? lo : 0x7fffffff), b = __reduce_max_sync(0xffffffffu, under ? hi : -1);
+                    const uint32_t unders = __ballot_sync(0xffffffffu, under);
+                    if (st_found<D>(p, first, h, a, b, lane, true)) again |= unders;
                 }
                 if (again != 0) {
                     if (lane == 0) tma_store_wait();         // what is there already is overwritten

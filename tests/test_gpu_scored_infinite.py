@@ -116,3 +116,17 @@ def test_one_channel_of_a_key_that_everybody_sees_is_nan(n, d, hq, cap):
     assert status == (spd.SPD_OK, -1) and bool(out[:, :, 3].isnan().all())
     at, rest = sorted(rows), [c for c in range(d) if c != 3]
     close(out[at][..., rest], want[at][..., rest], tol[at], "other channels")
+
+
+@pytest.mark.parametrize("d,hq", [(128, 2), (64, 1)])
+def test_tiny_rows_of_v_under_moderately_low_scores(d, hq):
+    """All scores near -20, v near the smallest normal numbers: sums relative to a score of 0 would be left with a few bits."""
+    lens = [300, 33]
+    q, k, v, ip = prompts(lens, hq, 1, d, "bf16", seed=95)
+    q.copy_(q.abs() + 1)
+    k.copy_(-k.abs() - 1)
+    v.mul_(1e-37)
+    want, tol = ref.prefill(q, k, v, lens, d ** -0.5 * 8, 20.0, weight=P_WEIGHT["bf16"])
+    out, status = run(q, k, v, ip, d, cap=20.0, scale=d ** -0.5 * 8)
+    assert status == (spd.SPD_OK, -1)
+    close(out, want, tol, "tiny")
