@@ -32,7 +32,8 @@
  *     that kernel has completed.  If a kernel of yours on the same stream writes lengths, page tables or KV rows
  *     immediately before a call, launch in plain stream order: spd_set_programmatic_launch(0), or SPD_NO_PDL=1
  *     in the environment.  Where the library's own calls write such inputs (the appends), they order themselves: an
- *     attention call behind an appending launch on its stream starts in plain stream order, whatever their workspaces.
+ *     attention call behind an appending launch on its stream starts in plain stream order, whatever their workspaces (the
+ *     layers of one token step, which share no lengths, overlap).
  *   - Threads.  Calls may come from several host threads, also from threads that have made no CUDA call of their
  *     own yet (the library makes the current device's context current on such a thread at its first call); calls
  *     that share a workspace must be ordered by the caller (one stream at a time per workspace).  Each workspace keeps a small table of streaming rates that
