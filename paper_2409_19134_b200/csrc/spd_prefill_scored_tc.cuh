@@ -496,8 +496,11 @@ prefill_scored_tc_kernel(const __grid_constant__ ScoredTcParams p, const __grid_
                         extremum(r4[y & 3], sv[2 * y], sv[2 * y + 1]);
                         unpack_f32x2(arg(2 * y), a0, a1);
                         const float p0 = ex2_approx(a0), p1 = ex2_approx(a1);
-                        lsum2 = add_f32x2(lsum2, pack_f32x2(p0, p1));
                         pk[y] = pack_bf16(p0, p1);
+                        // With a cap the rounded weights are summed, so that where few keys carry a row, numerator and sum are off
+                        // alike: errors against 64 bits 0.0023 -> 0.0018 of the output, which its own rounding to bf16 makes 0.0016.  Without one
+                        // (weights are flatter, errors stay) it would cost 7 %; here it is 2 % faster.
+                        lsum2 = add_f32x2(lsum2, CAP ? pack_f32x2(__uint_as_float(pk[y] << 16), __uint_as_float(pk[y] & 0xffff0000u)) : pack_f32x2(p0, p1));
                     }
                 };
                 auto nothing = [](float &, float, float) {};
