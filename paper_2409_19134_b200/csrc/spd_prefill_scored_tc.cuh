@@ -26,8 +26,8 @@
 // 2400, and no pipe is busy for more than half of it: what they add stands in a row's chain between a score's arrival and its
 // weight, on top of the exponentials instead of beside them.  Over seconds the power limit (8192 tokens, 32/8 heads: 446 us in the
 // first 100 calls, 514 at 1590 MHz and 990 W after three seconds).  Measured on one GPU, back to back, head_dim 128, bf16: 8192 tokens
-// x 32/8 heads plain 445 us (1236 TFLOP/s of visible pairs), distance bias 539 (1020), cap of 50 640 (859; 580 in a first burst), of
-// 64 744; 8 prompts of 2 to 8 k tokens (50 572 in all) 2.24 ms (1220); 3 prompts with prefix and window 126 us (900).
+// x 32/8 heads plain 445 us (1236 TFLOP/s of visible pairs), distance bias 539 (1020), cap of 50 610 (900; 552 in a first burst), of
+// 64 700; 8 prompts of 2 to 8 k tokens (50 572 in all) 2.24 ms (1220); 3 prompts with prefix and window 126 us (900).
 // Slower here: the tiles' exponentials in turns by named barriers (20 %), two threads per row (instruction issue, 15 %), the next
 // block's scores prepared in registers under this block's exponentials (60 %; the compiler serialises them), barriers of its own for
 // each tile's Q, which lets the tiles drift apart (4 % with caps).
@@ -497,10 +497,10 @@ prefill_scored_tc_kernel(const __grid_constant__ ScoredTcParams p, const __grid_
                         unpack_f32x2(arg(2 * y), a0, a1);
                         const float p0 = ex2_approx(a0), p1 = ex2_approx(a1);
                         pk[y] = pack_bf16(p0, p1);
-                        // With a cap the rounded weights are summed, so that where few keys carry a row, numerator and sum are off
-                        // alike: errors against 64 bits 0.0023 -> 0.0018 of the output, which its own rounding to bf16 makes 0.0016.  Without one
-                        // (weights are flatter, errors stay) it would cost 7 %; here it is 2 % faster.
-                        lsum2 = add_f32x2(lsum2, CAP ? pack_f32x2(__uint_as_float(pk[y] << 16), __uint_as_float(pk[y] & 0xffff0000u)) : pack_f32x2(p0, p1));
+                        // CAP 1: the rounded weights are summed, so that where few keys carry a row, numerator and sum are off alike: errors
+                        // against 64 bits 0.0023 -> 0.0018 of the output, whose own rounding to bf16 makes 0.0016; and 2 % faster.  Elsewhere that
+                        // would cost 5 to 17 % (the instructions stand in the chain of a score there) and sums of the weights as computed do.
+                        lsum2 = add_f32x2(lsum2, CAP == 1 ? pack_f32x2(__uint_as_float(pk[y] << 16), __uint_as_float(pk[y] & 0xffff0000u)) : pack_f32x2(p0, p1));
                     }
                 };
                 auto nothing = [](float &, float, float) {};
