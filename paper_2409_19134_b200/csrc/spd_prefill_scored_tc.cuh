@@ -340,8 +340,9 @@ prefill_scored_tc_kernel(const __grid_constant__ ScoredTcParams p, const __grid_
     tc_fence_after();
     const uint32_t tmem = __shfl_sync(0xffffffffu, tmem_slot, 0);
 
-    // Every wait is bounded, by more than rows that are done one by one take the warps that are waited for.  A wait that runs out clears `ok`, and the warp leaves its loops at the next turn; nothing in the
-    // loops waits for all threads, so everybody comes to the common end.
+    // Every wait is bounded, by more than rows that are done one by one take the warps that are waited for.  A wait that runs out
+    // clears `ok`, and the warp leaves its loops at the next turn; nothing in the loops waits for all threads, so everybody comes to
+    // the common end.
     bool ok = true;
     auto wait = [&](uint64_t *bar, uint32_t parity) { if (ok) ok = __all_sync(0xffffffffu, st_mbar_wait(smem_u32(bar), parity & 1, p.wait_limit)); };   // whole warps
     auto wait1 = [&](uint64_t *bar, uint32_t parity) { ok = ok && st_mbar_wait(smem_u32(bar), parity & 1, p.wait_limit); };                             // the loading thread
@@ -506,8 +507,8 @@ prefill_scored_tc_kernel(const __grid_constant__ ScoredTcParams p, const __grid_
                 auto nothing = [](float &, float, float) {};
                 if constexpr (CAP == 1) {
                     // Capped scores lie within +-cap2 <= 72 log2 units: relative to 0, weights and sums over 2^31 keys stay within fp32 (and
-                    // O for |v| < 2^31 and 2^24 keys; rows that leave it are done again), so no maximum is needed.  The form that suits the block before is tried first; whether it holds here
-                    // is found out alongside.
+                    // O for |v| < 2^31 and 2^24 keys; rows that leave it are done again), so no maximum is needed.  The form that suits
+                    // the block before is tried first; whether it holds here is found out alongside.
                     if (masked) {
                         weights([&](int x) { return pack_f32x2(sv[x], sv[x + 1]); }, nothing);
                     } else {
