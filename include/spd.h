@@ -321,6 +321,48 @@ spd_status spd_decode_step_scored(const spd_shape *shape, const spd_score *score
                                   void *cuda_stream);
 
 /*
+ * Several tokens per user in one decode step: drafted tokens that a model is to verify, one token with sinks, or a part of a prompt
+ * behind what the cache holds.  (The paper's prototype decodes one token at a time; this is its protocol's step 3, b and c, for several.)
+ * The drafted tokens of user u are the LAST tokens of its public partition: their k and v rows are appended first
+ * (spd_append_kv_rope), seq_lens counts them.  Row tok_indptr[u] + i of q is token i of the user's n.
+ *   tok_indptr [batch+1] (device): as for spd_append_kv_rope; NULL = one token per user.  Where it is not consistent, the users from the
+ *     first such one on are not served, their rows stay as they are, and SPD_ERR_BAD_PAGE is raised.
+ *   parents [total_tokens] (device) or NULL: the token of the same user, with a lower number, that token i comes after; -1 = it comes right
+ *     after the context.  NULL: every token comes after the one before it (a run).  A tree has at most 256 tokens per user, a run any number.
+ * Token i lies d_i steps below the context and has position ctx + d_i, with ctx = private tokens + public tokens - n.  It sees itself and the
+ * tokens that it comes after, directly or through others, and the context (positions 0 .. ctx - 1, private tokens first), each where
+ *     (its position) - (the other's position) < score->window, or (the other's position) < sinks      (window 0: everything)
+ * with scores as for the scored calls, d = the difference of the positions.
+ *   sinks: tokens at the start of the sequence that stay visible behind a window; 0 = none.  Pages between the sinks and the widest
+ *     window are neither listed nor read.
+ * spd_decode_step_drafted is the whole step; spd_partial_attn_drafted and spd_service_attn_merge_drafted are its halves, over one partition
+ * each, told the lengths of the other (pub_lens counts the drafted tokens too).  Partials have total_tokens rows: [total_tokens][num_q_heads]
+ * [head_dim] and [total_tokens][num_q_heads]; spd_merge_partials joins them given a shape whose batch is total_tokens.  q and out are
+ * [total_tokens][num_q_heads][head_dim], packed.
+ * Keys that a row does not see never enter its result, whatever their rows of k and v hold; a row that sees nothing, or only scores of -inf, gives
+ * zeros (the empty partial).  A user with an inconsistent table, length or tree (a parent out of range, more drafted tokens than public ones)
+ * raises SPD_ERR_BAD_PAGE and gets zeros; one with a page out of range raises it too, and gets zeros wherever that page was needed.
+ * The workspace is one of spd_drafted_workspace_size (which serves all other calls of the shape too).  Two kernels in plain stream order (the
+ * second starts early and waits for the first); results do not depend on timing.  sm_scale > 0, else SPD_ERR_UNSUPPORTED.
+ */
+typedef struct {
+    int64_t        total_tokens;
+    const int32_t *tok_indptr;
+    const int32_t *parents;
+    int32_t        sinks;
+} spd_drafts;
+spd_status spd_drafted_workspace_size(const spd_shape *shape, size_t *bytes);
+spd_status spd_decode_step_drafted(const spd_shape *shape, const spd_score *score, const spd_drafts *drafts, const void *q,
+                                   const spd_paged_kv *priv, const spd_paged_kv *pub, void *out, spd_dtype out_dtype,
+                                   void *ws, size_t ws_bytes, void *cuda_stream);
+spd_status spd_partial_attn_drafted(const spd_shape *shape, const spd_score *score, const spd_drafts *drafts, const void *q,
+                                    const spd_paged_kv *priv, const int32_t *pub_lens, spd_partial out, void *ws,
+                                    size_t ws_bytes, void *cuda_stream);
+spd_status spd_service_attn_merge_drafted(const spd_shape *shape, const spd_score *score, const spd_drafts *drafts, const void *q,
+                                          const spd_paged_kv *pub, const int32_t *priv_lens, spd_partial in, void *out,
+                                          spd_dtype out_dtype, void *ws, size_t ws_bytes, void *cuda_stream);
+
+/*
  * Rows of new tokens, as a projection leaves them: [total_tokens][heads][head_dim] in the shape's dtype, consecutive
  * tokens *_stride elements apart (0 = packed, i.e. heads * head_dim; q, k and v may be parts of one wider row).  Strides
  * and pointers are multiples of 16 bytes.

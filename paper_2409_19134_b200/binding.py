@@ -29,7 +29,8 @@ EXPORTS = ["spd_workspace_size", "spd_partial_attn", "spd_service_attn_merge", "
            "spd_decode_step_planned", "spd_set_split", "spd_set_programmatic_launch", "spd_debug_read_plan",
            "spd_debug_sm_moves", "spd_decode_step_append", "spd_watch_alarm", "spd_service_attn_merge_append",
            "spd_partial_attn_scored", "spd_service_attn_merge_scored", "spd_decode_step_scored", "spd_prefill_attn_scored",
-           "spd_append_kv_rope"]
+           "spd_append_kv_rope", "spd_drafted_workspace_size", "spd_decode_step_drafted", "spd_partial_attn_drafted",
+           "spd_service_attn_merge_drafted"]
 
 
 class SpdError(RuntimeError):
@@ -79,6 +80,10 @@ _Sections = C.c_int32 * 4
 class Rope(C.Structure):
     _fields_ = [("rotary_dim", C.c_int32), ("interleaved", C.c_int32), ("num_axes", C.c_int32), ("sections", _Sections),
                 ("scale", C.c_float), ("inv_freq", C.c_void_p)]
+
+
+class Drafts(C.Structure):
+    _fields_ = [("total_tokens", C.c_int64), ("tok_indptr", C.c_void_p), ("parents", C.c_void_p), ("sinks", C.c_int32)]
 
 
 class Partial(C.Structure):
@@ -137,6 +142,13 @@ def lib() -> C.CDLL:
                                               C.c_int, vp, sz, vp]
         L.spd_append_kv_rope.argtypes = [C.POINTER(Shape), C.POINTER(Rope), C.c_int64, C.POINTER(Tokens), vp, vp, vp, vp, vp, vp,
                                          vp, C.c_int32, vp, vp, vp, vp, vp, sz, vp]
+        L.spd_drafted_workspace_size.argtypes = [C.POINTER(Shape), C.POINTER(sz)]
+        L.spd_decode_step_drafted.argtypes = [C.POINTER(Shape), C.POINTER(Score), C.POINTER(Drafts), vp, C.POINTER(PagedKV), C.POINTER(PagedKV),
+                                              vp, C.c_int, vp, sz, vp]
+        L.spd_partial_attn_drafted.argtypes = [C.POINTER(Shape), C.POINTER(Score), C.POINTER(Drafts), vp, C.POINTER(PagedKV), vp, Partial,
+                                               vp, sz, vp]
+        L.spd_service_attn_merge_drafted.argtypes = [C.POINTER(Shape), C.POINTER(Score), C.POINTER(Drafts), vp, C.POINTER(PagedKV), vp,
+                                                     Partial, vp, C.c_int, vp, sz, vp]
         L.spd_watch_alarm.argtypes = [vp, C.c_int32, C.c_int32, vp, C.c_float, vp, vp]
         L.spd_set_split.argtypes = [C.c_int32, C.c_int32]
         L.spd_set_programmatic_launch.argtypes = [C.c_int32]
@@ -687,3 +699,59 @@ def spd_append_kv_rope(shape, rope, q, k, v, part, ws, q_out=None, k_out=None, t
                                     pool_k, pool_v, pages, indptr, indices, lens,
                                     lens if isinstance(new_lens, str) else _i32(new_lens, B, dev=dev), *_workspace(ws, dev),
                                     _stream_ptr(stream)), "spd_append_kv_rope")
+
+
+def spd_drafted_workspace_size(shape: Shape) -> int:
+    n = C.c_size_t(0)
+    _check(lib().spd_drafted_workspace_size(C.byref(shape), C.byref(n)), "spd_drafted_workspace_size")
+    return int(n.value)
+
+
+def alloc_drafted_workspace(shape: Shape, device="cuda") -> torch.Tensor:
+    """A zeroed workspace for the *_drafted calls, and for every other call of the shape."""
+    return torch.zeros(spd_drafted_workspace_size(shape), dtype=torch.uint8, device=device)
+
+
+def _drafted(shape, score, q, tok_indptr, parents, sinks):
+    """What the *_drafted calls have in common: the drafts, the rows' count, the device, and what partitions are held against."""
+    dev, T, B, hq, d, dtype = _here(q), q.shape[0], shape.batch, shape.num_q_heads, shape.head_dim, _TORCH_DTYPES[shape.dtype]
+    if q.dtype is not dtype or q.shape != (T, hq, d) or not q.is_contiguous():
+        raise ValueError(f"expected contiguous {dtype} [tokens, {hq}, {d}], got {q.dtype} {list(q.shape)}")
+    if not 0 <= sinks < 2**31:
+        raise ValueError("the number of sinks is a 32-bit number, not negative")
+    if tok_indptr is None and T != B:
+        raise ValueError(f"{T} tokens of {B} users need a tok_indptr")
+    _slopes(shape, score, dev)
+    return Drafts(T, _i32(tok_indptr, B + 1, dev=dev), _i32(parents, T, dev=dev), sinks), T, dev, (B, shape.num_kv_heads * shape.page_size * d, dtype, dev)
+
+
+def _drafted_partial(shape, part, T, dev) -> Partial:
+    rows = T * shape.num_q_heads
+    return Partial(_packed(part[0], rows * shape.head_dim, torch.float32, dev), _packed(part[1], rows, torch.float32, dev),
+                   _packed(part[2], rows, torch.float32, dev))
+
+
+def spd_decode_step_drafted(shape, score, q, priv, pub, out, ws, tok_indptr=None, parents=None, sinks=0, stream=None) -> None:
+    """One decode step for several tokens per user, the last ones of the public partition: q, out [T,Hq,D]; tok_indptr int32 [B+1] (None: one
+    token per user); parents int32 [T], a tree (None: runs); sinks: first tokens that stay visible behind the window."""
+    drafts, T, dev, fit = _drafted(shape, score, q, tok_indptr, parents, sinks)
+    a, b = PagedKV(*_partition(priv, *fit)), PagedKV(*_partition(pub, *fit))
+    _check(lib().spd_decode_step_drafted(shape, score, drafts, _ptr(q), a, b, _packed(out, q.numel(), dev=dev), _dtype_code(out.dtype),
+                                         *_workspace(ws, dev), _stream_ptr(stream)), "spd_decode_step_drafted")
+
+
+def spd_partial_attn_drafted(shape, score, q, priv, pub_lens, out, ws, tok_indptr=None, parents=None, sinks=0, stream=None) -> None:
+    """The private half of spd_decode_step_drafted: out = (o [T,Hq,D], m [T,Hq], l [T,Hq]); pub_lens int32 [B] counts the drafted tokens."""
+    drafts, T, dev, fit = _drafted(shape, score, q, tok_indptr, parents, sinks)
+    kv, part = PagedKV(*_partition(priv, *fit)), _drafted_partial(shape, out, T, dev)
+    _check(lib().spd_partial_attn_drafted(shape, score, drafts, _ptr(q), kv, _i32(pub_lens, shape.batch, dev=dev), part, *_workspace(ws, dev),
+                                          _stream_ptr(stream)), "spd_partial_attn_drafted")
+
+
+def spd_service_attn_merge_drafted(shape, score, q, pub, priv_lens, partial_in, out, ws, tok_indptr=None, parents=None, sinks=0, stream=None) -> None:
+    """The public half of spd_decode_step_drafted, merged with the private partial and normalised; priv_lens int32 [B]."""
+    drafts, T, dev, fit = _drafted(shape, score, q, tok_indptr, parents, sinks)
+    kv, part = PagedKV(*_partition(pub, *fit)), _drafted_partial(shape, partial_in, T, dev)
+    _check(lib().spd_service_attn_merge_drafted(shape, score, drafts, _ptr(q), kv, _i32(priv_lens, shape.batch, dev=dev), part,
+                                                _packed(out, q.numel(), dev=dev), _dtype_code(out.dtype), *_workspace(ws, dev),
+                                                _stream_ptr(stream)), "spd_service_attn_merge_drafted")

@@ -1,0 +1,189 @@
+// Attention of drafted tokens: argument checks, choice of the kernel, launches.
+#include <cstdio>
+#include <mutex>
+
+#include "spd_drafted.cuh"
+#include "spd_drafted_fma.cuh"
+#include "spd_host.h"
+
+namespace {
+
+using namespace spd;
+using host::misaligned;
+
+// Query heads that a tile of RT rows takes of one token: all of a KV head's where they fit.
+int heads_per_tile(int g, int RT) { return g <= RT ? g : kHeadsPerItem; }
+
+constexpr int kFmaPerSm = 2;        // CTAs of the largest FMA variant that share an SM; the others fit more
+constexpr int kMostRows = 128;      // rows of the largest tile
+
+// Behind the workspace's head: records and slots of the pieces.
+struct DraftedLayout { size_t records, scratch, total; };
+DraftedLayout drafted_layout(const spd_shape &s, int sms) {
+    const int g = s.num_q_heads / s.num_kv_heads;
+    const int seqs = s.batch * s.num_kv_heads * (g > kHeadsPerItem ? g / kHeadsPerItem : 1);
+    const size_t slots = 2 * static_cast<size_t>(kFmaPerSm) * sms;
+    DraftedLayout L;
+    L.records = host::cleared_end(s.batch, seqs);
+    L.scratch = L.records + (slots * 2 * sizeof(int4) + 255) / 256 * 256;
+    L.total = L.scratch + slots * drafted_slot_floats(s.head_dim, kMostRows) * sizeof(float);
+    return L;
+}
+
+// The join may be set up while the attention's last CTAs are still at work; it waits for them before it reads anything.
+template <int D, int RT, bool LOG2>
+spd_status launch_join(const DraftedParams &p, cudaStream_t st) {
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(static_cast<unsigned>(p.grid));
+    cfg.blockDim = dim3(256);
+    cfg.stream = st;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    const cudaError_t err = cudaLaunchKernelEx(&cfg, drafted_join_kernel<D, RT, LOG2>, p);
+    host::count_launch();
+    return err == cudaSuccess ? SPD_OK : SPD_ERR_CUDA;
+}
+
+template <typename E, int D, int RT>
+spd_status launch_fma(DraftedParams p, int sms, cudaStream_t st) {
+    using C = DraftedFma<D, RT>;
+    static std::once_flag once[64];
+    int dev = 0;
+    cudaGetDevice(&dev);
+    cudaError_t err = cudaSuccess;
+    std::call_once(once[dev & 63], [&] {
+        err = cudaFuncSetAttribute(drafted_fma_kernel<E, D, RT>, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(C::smem_bytes()));
+    });
+    if (err != cudaSuccess) return SPD_ERR_CUDA;
+    p.hs = heads_per_tile(p.g, RT);
+    p.hgroups = p.g / p.hs;
+    p.tt = RT / p.hs;
+    p.SQ = p.Hkv * p.hgroups;
+    p.grid = kFmaPerSm * sms;
+    drafted_fma_kernel<E, D, RT><<<p.grid, C::kThreads, C::smem_bytes(), st>>>(p);
+    host::count_launch();
+    if (cudaGetLastError() != cudaSuccess) return SPD_ERR_CUDA;
+    return launch_join<D, RT, false>(p, st);
+}
+
+template <typename E>
+spd_status run_fma(const DraftedParams &p, int D, int sms, cudaStream_t st) {
+    const bool few = p.T * p.g <= 16ll * p.B;          // 16 rows of a KV head or fewer, by the mean over the users
+    if (D == 128) return few ? launch_fma<E, 128, 16>(p, sms, st) : launch_fma<E, 128, 64>(p, sms, st);
+    return few ? launch_fma<E, 64, 16>(p, sms, st) : launch_fma<E, 64, 64>(p, sms, st);
+}
+
+spd_status check_part(const spd_shape &s, const spd_paged_kv *kv) {
+    if (!kv || kv->num_pages < 0 || !kv->page_indptr || !kv->seq_lens) return SPD_ERR_INVALID_ARG;
+    if (kv->num_pages > 0 && (!kv->k_pool || !kv->v_pool)) return SPD_ERR_INVALID_ARG;
+    if (misaligned(kv->k_pool, 128) || misaligned(kv->v_pool, 128)) return SPD_ERR_INVALID_ARG;
+    if (static_cast<int64_t>(kv->num_pages) * s.num_kv_heads * kPage >= (1ll << 31)) return SPD_ERR_UNSUPPORTED;
+    return SPD_OK;
+}
+
+// One call: partitions absent from it are null, then peer holds their lengths.
+struct DraftedCall {
+    const spd_paged_kv *part[2];
+    const int32_t *peer[2];
+    const spd_partial *pin, *pout;
+    void *out;
+    spd_dtype out_dtype;
+};
+
+spd_status run(const spd_shape *shape, const spd_score *score, const spd_drafts *drafts, const void *q, const DraftedCall &c, void *ws,
+               size_t ws_bytes, void *cuda_stream) {
+    spd_status rc = host::check_shape(shape);
+    if (rc != SPD_OK) return rc;
+    if ((rc = host::check_score(score)) != SPD_OK) return rc;
+    const spd_shape &s = *shape;
+    if (!drafts) return SPD_ERR_INVALID_ARG;
+    const int64_t T = drafts->total_tokens;
+    for (int x = 0; x < 2; ++x)
+        if (c.part[x] && (rc = check_part(s, c.part[x])) != SPD_OK) return rc;
+    if (!(s.sm_scale > 0.f && s.sm_scale <= 1e30f)) return SPD_ERR_UNSUPPORTED;
+    if (T < 0 || T >= (1ll << 31) - 1024 || drafts->sinks < 0 || (!drafts->tok_indptr && T != s.batch)) return SPD_ERR_INVALID_ARG;
+    if (T > 0 && !q) return SPD_ERR_INVALID_ARG;
+    if (misaligned(q, 16) || !ws || misaligned(ws, 256)) return SPD_ERR_INVALID_ARG;
+    for (const spd_partial *x : {c.pin, c.pout})
+        if (x && ((T > 0 && (!x->o || !x->m || !x->l)) || misaligned(x->o, 16) || misaligned(x->m, 4) || misaligned(x->l, 4))) return SPD_ERR_INVALID_ARG;
+    if (!c.pout) {
+        if ((T > 0 && !c.out) || misaligned(c.out, 16)) return SPD_ERR_INVALID_ARG;
+        if (c.out_dtype != SPD_F32 && c.out_dtype != SPD_BF16) return SPD_ERR_UNSUPPORTED;
+    }
+    int sms = 0;
+    if ((rc = host::device_sms(&sms)) != SPD_OK) return rc;
+    const DraftedLayout L = drafted_layout(s, sms);
+    if (ws_bytes < L.total) return SPD_ERR_WORKSPACE;
+    if (T == 0) return SPD_OK;
+    const int g = s.num_q_heads / s.num_kv_heads;
+    DraftedParams p{};
+    p.B = s.batch; p.Hq = s.num_q_heads; p.Hkv = s.num_kv_heads; p.g = g;
+    p.T = T; p.sm_scale = s.sm_scale; p.q = q;
+    for (int x = 0; x < 2; ++x) {
+        if (const spd_paged_kv *kv = c.part[x]) {
+            p.part[x] = PartDev{kv->page_indptr, kv->page_indices, kv->seq_lens, kv->num_pages, 1};
+            p.k_pool[x] = kv->k_pool;
+            p.v_pool[x] = kv->v_pool;
+        }
+        p.peer_lens[x] = c.peer[x];
+    }
+    p.tok_indptr = drafts->tok_indptr; p.parents = drafts->parents; p.sinks = drafts->sinks;
+    p.cap = score->logit_cap; p.window = score->window; p.slopes = score->alibi_slopes;
+    p.mode = c.pout ? OUT_PARTIAL : OUT_FINAL;
+    if (c.pout) { p.po = c.pout->o; p.pm = c.pout->m; p.pl = c.pout->l; }
+    if (c.pin) { p.in_o = c.pin->o; p.in_m = c.pin->m; p.in_l = c.pin->l; }
+    p.out = c.out; p.out_bf16 = c.out_dtype == SPD_BF16;
+    uint8_t *w = static_cast<uint8_t *>(ws);
+    p.hdr = reinterpret_cast<int32_t *>(w);
+    p.bad = reinterpret_cast<int32_t *>(w + host::flags_offset(s.batch));
+    p.epoch = host::next_call_id();
+    p.seqs = s.batch * s.num_kv_heads * (g > kHeadsPerItem ? g / kHeadsPerItem : 1);
+    p.records = reinterpret_cast<int4 *>(w + L.records);
+    p.scratch = reinterpret_cast<float *>(w + L.scratch);
+    cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+    return s.dtype == SPD_BF16 ? run_fma<__nv_bfloat16>(p, s.head_dim, sms, st) : run_fma<float>(p, s.head_dim, sms, st);
+}
+
+}  // namespace
+
+extern "C" {
+
+spd_status spd_drafted_workspace_size(const spd_shape *shape, size_t *bytes) {
+    if (!bytes) return SPD_ERR_INVALID_ARG;
+    spd_status rc = spd_workspace_size(shape, bytes);
+    if (rc != SPD_OK) return rc;
+    int sms = 0;
+    if ((rc = host::device_sms(&sms)) != SPD_OK) return rc;
+    const size_t own = drafted_layout(*shape, sms).total;
+    if (own > *bytes) *bytes = own;
+    return SPD_OK;
+}
+
+spd_status spd_decode_step_drafted(const spd_shape *shape, const spd_score *score, const spd_drafts *drafts, const void *q,
+                                   const spd_paged_kv *priv, const spd_paged_kv *pub, void *out, spd_dtype out_dtype, void *ws,
+                                   size_t ws_bytes, void *cuda_stream) {
+    if (!priv || !pub) return SPD_ERR_INVALID_ARG;
+    const DraftedCall c{{priv, pub}, {nullptr, nullptr}, nullptr, nullptr, out, out_dtype};
+    return run(shape, score, drafts, q, c, ws, ws_bytes, cuda_stream);
+}
+
+spd_status spd_partial_attn_drafted(const spd_shape *shape, const spd_score *score, const spd_drafts *drafts, const void *q,
+                                    const spd_paged_kv *priv, const int32_t *pub_lens, spd_partial out, void *ws, size_t ws_bytes,
+                                    void *cuda_stream) {
+    if (!priv || !pub_lens) return SPD_ERR_INVALID_ARG;
+    const DraftedCall c{{priv, nullptr}, {nullptr, pub_lens}, nullptr, &out, nullptr, SPD_F32};
+    return run(shape, score, drafts, q, c, ws, ws_bytes, cuda_stream);
+}
+
+spd_status spd_service_attn_merge_drafted(const spd_shape *shape, const spd_score *score, const spd_drafts *drafts, const void *q,
+                                          const spd_paged_kv *pub, const int32_t *priv_lens, spd_partial in, void *out,
+                                          spd_dtype out_dtype, void *ws, size_t ws_bytes, void *cuda_stream) {
+    if (!pub || !priv_lens) return SPD_ERR_INVALID_ARG;
+    const DraftedCall c{{nullptr, pub}, {priv_lens, nullptr}, &in, nullptr, out, out_dtype};
+    return run(shape, score, drafts, q, c, ws, ws_bytes, cuda_stream);
+}
+
+}  // extern "C"

@@ -1,0 +1,358 @@
+// Attention of drafted tokens over the two paged partitions: what the kernels share.
+//
+// A user's drafted tokens are the last n tokens of its public partition; they hang together as a tree (parents) or a run.  Token i at
+// depth d_i has position ctx + d_i, ctx = cached tokens in front of the drafted ones, and sees
+//     the context and, among the drafted tokens, itself and its ancestors, each where pos_i - pos_j < window or pos_j < sinks;
+//     s = sm_scale q.k;  s <- cap tanh(s / cap);  s <- s - slope_h (pos_i - pos_j).
+// Rows that read the same keys are computed together: an item is (user, tile of tokens x heads of one group, KV head), its keys the page
+// tiles that some row of it may see (those that hold sinks, then from the widest window on), kDrBlock keys at a time.  All items' blocks
+// laid end to end are cut into equal shares, one per CTA, whatever the batch looks like: an item inside a share is finished there, one that
+// is cut leaves (O, m, l) per piece in scratch, and a second kernel joins the pieces (Theorem 1) in order, so that results do not
+// depend on who came first.  No CTA waits for another.
+#pragma once
+
+#include "spd_kernels.cuh"
+
+namespace spd {
+
+constexpr int kDrBlock = 64;              // keys per block: four page tiles
+constexpr int kDrTiles = kDrBlock / kPage;
+constexpr int kDrTree = 256;              // most drafted tokens of a user that come as a tree
+constexpr int kDrWords = kDrTree / 32;
+constexpr int kDrMinBlocks = 2;           // do not cut the work into shares of fewer blocks
+
+struct DraftedParams {
+    int32_t B, Hq, Hkv, g;
+    int32_t hs, hgroups;                  // query heads that a tile takes of a token, and how many such groups a KV head has
+    int32_t tt;                           // tokens per tile
+    int32_t SQ;                           // Hkv * hgroups
+    int64_t T;
+    float sm_scale;
+    const void *q;                        // [T][Hq][D]
+    PartDev part[2];                      // 0 = private, 1 = public
+    const void *k_pool[2], *v_pool[2];
+    const int32_t *peer_lens[2];          // lengths of a partition that the call does not read
+    const int32_t *tok_indptr;            // [B+1]; null = one token per user
+    const int32_t *parents;               // [T]; null = runs
+    float cap;
+    int32_t window, sinks;
+    const float *slopes;
+    int32_t mode;                         // OutMode
+    float *po, *pm, *pl;                  // OUT_PARTIAL: [T][Hq][D], [T][Hq], [T][Hq]
+    const float *in_o, *in_m, *in_l;      // OUT_FINAL: optional partial to merge in
+    void *out;                            // OUT_FINAL: [T][Hq][D]
+    int32_t out_bf16;
+    int32_t *hdr, *bad;
+    int32_t epoch, seqs;                  // seqs: what HDR_NSEQ is to hold
+    int32_t grid;                         // CTAs of the launch
+    int4 *records;                        // [2 * grid][2]: what the join has to know of the pieces in a CTA's two slots
+    float *scratch;                       // [2 * grid] slots
+};
+
+// A slot holds one piece: O as [D / 4][RT] float4 (threads of consecutive rows write consecutive chunks), then m [RT] and l [RT].
+__host__ __device__ constexpr size_t drafted_slot_floats(int D, int RT) { return static_cast<size_t>(RT) * (D + 2); }
+
+struct DraftedUser {
+    int first, n;                          // rows of q
+    int lp, lq, ctx;                       // private and public tokens; those in front of the drafted ones
+    int np, nt;                            // page tiles: private ones, all that the call reads
+    int64_t base0, base1;                  // first page-table entries
+    bool good;
+};
+
+// Tokens of user u, without a look at the cache; false where the offsets are inconsistent.
+__device__ __forceinline__ bool drafted_tokens(const DraftedParams &p, int u, int &first, int &n) {
+    if (p.tok_indptr == nullptr) { first = u; n = 1; return true; }
+    const int64_t a = p.tok_indptr[u], b = p.tok_indptr[u + 1];
+    first = static_cast<int>(a);
+    n = static_cast<int>(b - a);
+    return a >= 0 && b >= a && b <= p.T && (u != 0 || a == 0) && (u != p.B - 1 || b == p.T);
+}
+
+// A user whose tables, lengths or counts are inconsistent is not good: it has no keys, and its rows become zeros.
+__device__ __forceinline__ void drafted_user(const DraftedParams &p, int u, DraftedUser &s) {
+    drafted_tokens(p, u, s.first, s.n);
+    int64_t len[2], base[2] = {0, 0};
+    bool good = true;
+#pragma unroll
+    for (int x = 0; x < 2; ++x) {
+        const PartDev &a = p.part[x];
+        if (a.present) {
+            const int64_t lo = a.indptr[u], hi = a.indptr[u + 1], end = a.indptr[p.B];
+            len[x] = a.lens[u];
+            base[x] = lo;
+            good = good && lo >= 0 && hi >= lo && hi <= end && len[x] >= 0 && len[x] <= (hi - lo) * kPage && (len[x] == 0 || a.indices != nullptr);
+        } else {
+            len[x] = p.peer_lens[x] ? p.peer_lens[x][u] : 0;
+            good = good && len[x] >= 0;
+        }
+    }
+    good = good && len[0] + len[1] <= 0x7fffffff && len[1] >= s.n && (p.parents == nullptr || s.n <= kDrTree);
+    s.good = good;
+    s.lp = good ? static_cast<int>(len[0]) : 0;
+    s.lq = good ? static_cast<int>(len[1]) : s.n;
+    s.ctx = s.lp + s.lq - s.n;
+    s.base0 = base[0]; s.base1 = base[1];
+    s.np = p.part[0].present && good ? (s.lp + kPage - 1) / kPage : 0;
+    s.nt = s.np + (p.part[1].present && good ? (s.lq + kPage - 1) / kPage : 0);
+}
+
+// Keys of a tile of rows: page tiles [0, ns) and [a, e) of the user's, ceil((ns + e - a) / 4) blocks (at least one, so that rows that
+// see nothing are written too).
+struct DraftedKeys { int ns, a, e, nb; };
+__device__ __forceinline__ DraftedKeys drafted_keys(const DraftedParams &p, const DraftedUser &s, int i0, int i1) {
+    const int64_t P0 = p.part[0].present ? 0 : s.lp, P1 = s.nt == 0 ? P0 : (p.part[1].present ? static_cast<int64_t>(s.lp) + s.lq : s.lp);
+    const int64_t hi = p.parents ? P1 : min(P1, static_cast<int64_t>(s.ctx) + i1);
+    int64_t lo = P0;
+    if (p.window > 0) lo = max(lo, static_cast<int64_t>(s.ctx) + (p.parents ? 0 : i0) - p.window + 1);
+    // tiles in front of position x, with the one that x lies in
+    auto upto = [&](int64_t x) { return static_cast<int>(x < s.lp ? x / kPage : s.np + (x - s.lp) / kPage) + 1; };
+    DraftedKeys k;
+    k.a = lo < hi ? upto(lo) - 1 : s.nt;
+    k.e = lo < hi ? upto(hi - 1) : s.nt;
+    const int64_t se = min(static_cast<int64_t>(p.sinks), hi);
+    k.ns = p.window > 0 && se > P0 && lo > P0 ? upto(se - 1) : 0;
+    if (k.ns >= k.a) { k.a = 0; k.ns = 0; }
+    k.nb = max(1, (k.ns + k.e - k.a + kDrTiles - 1) / kDrTiles);
+    return k;
+}
+
+// Tile x of a user's list: first position, tokens, and where its page stands.
+struct DraftedTile { int base, cnt, part; int64_t entry; };
+__device__ __forceinline__ DraftedTile drafted_tile(const DraftedParams &p, const DraftedUser &s, const DraftedKeys &k, int v) {
+    DraftedTile t{0, 0, 0, 0};
+    if (v >= k.ns + k.e - k.a) return t;
+    const int x = v < k.ns ? v : k.a + v - k.ns;
+    if (x < s.np) {
+        t.base = x * kPage; t.cnt = min(kPage, s.lp - t.base); t.entry = s.base0 + x;
+    } else {
+        const int y = x - s.np;
+        t.base = s.lp + y * kPage; t.cnt = min(kPage, s.lq - y * kPage); t.part = 1; t.entry = s.base1 + y;
+    }
+    return t;
+}
+
+// ---------------------------------------------------------------------------------------------------------------------
+// The cut.  Blocks in the order user, row tile, (KV head, head group), block; W of them in `shares` shares.
+struct DraftedWalk {
+    int u, rt, sq;             // the item
+    DraftedUser s;
+    DraftedKeys k;
+    int64_t x0;                // its first block among all
+};
+
+__device__ __forceinline__ int64_t drafted_bound(int64_t W, int shares, int c) { return W * c / shares; }
+__device__ __forceinline__ int drafted_share_of(int64_t W, int shares, int64_t x) { return static_cast<int>(((x + 1) * shares - 1) / W); }
+
+__device__ __forceinline__ void drafted_item_keys(const DraftedParams &p, DraftedWalk &w) {
+    w.k = drafted_keys(p, w.s, w.rt * p.tt, min(w.s.n, (w.rt + 1) * p.tt));
+}
+
+// Blocks of one KV head and head group over tiles [rt0, rt1), every `step`-th.
+__device__ __forceinline__ int64_t drafted_user_blocks(const DraftedParams &p, const DraftedUser &s, int rt0, int step) {
+    int64_t sum = 0;
+    for (int rt = rt0; rt * p.tt < s.n; rt += step) sum += drafted_keys(p, s, rt * p.tt, min(s.n, (rt + 1) * p.tt)).nb;
+    return sum;
+}
+
+// The sums of the users' blocks, by all NT threads of a CTA: chunk c of C users (a user per warp where there are few of them, so that the
+// lanes share a long run's tiles) ends at sums[c].  *first_bad: the first user whose offsets are inconsistent; it and all behind it have no rows.
+template <int NT>
+__device__ __forceinline__ int64_t drafted_sums(const DraftedParams &p, int64_t *sums, int *first_bad, int &C, int &chunks) {
+    const int tid = threadIdx.x, lane = tid & 31;
+    const bool warps = p.B <= NT / 32;
+    C = warps ? 1 : (p.B + NT - 1) / NT;
+    chunks = (p.B + C - 1) / C;
+    if (tid == 0) *first_bad = p.B;
+    __syncthreads();
+    for (int u = tid; u < p.B; u += NT) {
+        int a, n;
+        if (!drafted_tokens(p, u, a, n)) atomicMin(first_bad, u);
+    }
+    __syncthreads();
+    const int users = *first_bad;
+    int64_t sum = 0;
+    DraftedUser s;
+    if (warps) {
+        const int u = tid >> 5;
+        if (u < users) { drafted_user(p, u, s); sum = drafted_user_blocks(p, s, lane, 32); }
+#pragma unroll
+        for (int d = 16; d >= 1; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
+    } else {
+        for (int u = tid * C; u < min(users, (tid + 1) * C); ++u) { drafted_user(p, u, s); sum += drafted_user_blocks(p, s, 0, 1); }
+    }
+    sum *= p.SQ;
+    // inclusive sums over the chunks
+    __shared__ int64_t warp_sums[32];
+    if (warps) {
+        if (lane == 0) warp_sums[tid >> 5] = sum;
+        __syncthreads();
+        if (tid < chunks) {
+            int64_t t = 0;
+            for (int w = 0; w <= tid; ++w) t += warp_sums[w];
+            sums[tid] = t;
+        }
+    } else {
+        int64_t inc = sum;
+#pragma unroll
+        for (int d = 1; d < 32; d <<= 1) {
+            const int64_t up = __shfl_up_sync(0xffffffffu, inc, d);
+            if (lane >= d) inc += up;
+        }
+        if (lane == 31) warp_sums[tid >> 5] = inc;
+        __syncthreads();
+        for (int w = 0; w < (tid >> 5); ++w) inc += warp_sums[w];
+        if (tid < chunks) sums[tid] = inc;
+    }
+    __syncthreads();
+    return sums[chunks - 1];
+}
+
+// The item that holds block x, by one warp.
+__device__ __forceinline__ void drafted_locate(const DraftedParams &p, const int64_t *sums, int C, int chunks, int64_t x, int lane, DraftedWalk &w) {
+    int c = 0;
+    for (int c0 = 0; c0 < chunks; c0 += 32) {
+        const unsigned hit = __ballot_sync(0xffffffffu, c0 + lane < chunks && x < sums[c0 + lane]);
+        if (hit) { c = c0 + __ffs(hit) - 1; break; }
+    }
+    int64_t at = c == 0 ? 0 : sums[c - 1];
+    for (w.u = c * C;; ++w.u) {
+        drafted_user(p, w.u, w.s);
+        for (int rt0 = 0; rt0 * p.tt < w.s.n; rt0 += 32) {
+            const int rt = rt0 + lane;
+            const int64_t mine = rt * p.tt < w.s.n ? static_cast<int64_t>(drafted_keys(p, w.s, rt * p.tt, min(w.s.n, (rt + 1) * p.tt)).nb) * p.SQ : 0;
+            int64_t inc = mine;
+#pragma unroll
+            for (int d = 1; d < 32; d <<= 1) {
+                const int64_t up = __shfl_up_sync(0xffffffffu, inc, d);
+                if (lane >= d) inc += up;
+            }
+            const unsigned hit = __ballot_sync(0xffffffffu, x < at + inc);
+            if (hit) {
+                const int src = __ffs(hit) - 1;
+                w.rt = rt0 + src;
+                at += __shfl_sync(0xffffffffu, inc - mine, src);
+                drafted_item_keys(p, w);
+                w.sq = static_cast<int>((x - at) / w.k.nb);
+                w.x0 = at + static_cast<int64_t>(w.sq) * w.k.nb;
+                return;
+            }
+            at += __shfl_sync(0xffffffffu, inc, 31);
+        }
+    }
+}
+
+// The next item; the caller knows that there is one.
+__device__ __forceinline__ void drafted_next(const DraftedParams &p, DraftedWalk &w) {
+    w.x0 += w.k.nb;
+    if (++w.sq < p.SQ) return;
+    w.sq = 0;
+    if (++w.rt * p.tt >= w.s.n) {
+        w.rt = 0;
+        do { ++w.u; drafted_user(p, w.u, w.s); } while (w.s.n == 0);
+    }
+    drafted_item_keys(p, w);
+}
+
+// What the join has to know of a piece: valid, user, first token of q and first token of the tile; (KV head, head group), tokens of the tile,
+// first and last CTA that hold a piece of the item.
+__device__ __forceinline__ void drafted_record(const DraftedParams &p, const DraftedWalk &w, int slot, int64_t W, int shares) {
+    const int i0 = w.rt * p.tt;
+    p.records[2 * slot] = make_int4(1, w.u, w.s.first + i0, w.sq);
+    p.records[2 * slot + 1] = make_int4(min(p.tt, w.s.n - i0), drafted_share_of(W, shares, w.x0), drafted_share_of(W, shares, w.x0 + w.k.nb - 1), 0);
+}
+
+// Raises the status of a user.
+__device__ __forceinline__ void drafted_flag(const DraftedParams &p, int u) {
+    p.bad[u] = p.epoch;
+    flag_error(p.hdr, 4 /* SPD_ERR_BAD_PAGE */, u);
+}
+
+// CTA 0 leaves in the header what the status query needs, and raises the first inconsistent offsets.
+__device__ __forceinline__ void drafted_header(const DraftedParams &p, int first_bad) {
+    p.hdr[HDR_BATCH] = p.B;
+    p.hdr[HDR_NSEQ] = p.seqs;
+    if (first_bad < p.B) flag_error(p.hdr, 4 /* SPD_ERR_BAD_PAGE */, first_bad);
+}
+
+// Four channels of one row, unnormalised with maximum m (natural units) and sum l, to their place: the partial, or merged with the partial
+// that came in and normalised.
+template <int D>
+__device__ __forceinline__ void drafted_store4(const DraftedParams &p, int64_t row, int c4, float4 o, float m, float l, bool bad) {
+    if (p.mode == OUT_PARTIAL) {
+        reinterpret_cast<float4 *>(p.po)[row * (D / 4) + c4] = bad ? make_float4(0.f, 0.f, 0.f, 0.f) : o;
+        if (c4 == 0) { p.pm[row] = bad ? -INFINITY : m; p.pl[row] = bad ? 0.f : l; }
+        return;
+    }
+    if (p.in_o != nullptr && !bad) {
+        const float mi = p.in_m[row], li = p.in_l[row], M = fmaxf(m, mi);
+        const float4 v = reinterpret_cast<const float4 *>(p.in_o)[row * (D / 4) + c4];
+        const float a = m == -INFINITY ? 0.f : expf(m - M), b = mi == -INFINITY ? 0.f : expf(mi - M);
+        // an empty part weighs nothing, whatever stands in its O; a sum that is NaN stays
+        l = (a != 0.f || l != l ? l * (l != l ? 1.f : a) : 0.f) + (b != 0.f || li != li ? li * (li != li ? 1.f : b) : 0.f);
+        o.x = (a != 0.f ? o.x * a : 0.f) + (b != 0.f ? v.x * b : 0.f);
+        o.y = (a != 0.f ? o.y * a : 0.f) + (b != 0.f ? v.y * b : 0.f);
+        o.z = (a != 0.f ? o.z * a : 0.f) + (b != 0.f ? v.z * b : 0.f);
+        o.w = (a != 0.f ? o.w * a : 0.f) + (b != 0.f ? v.w * b : 0.f);
+    }
+    const bool none = bad || l == 0.f;
+    const float4 y = none ? make_float4(0.f, 0.f, 0.f, 0.f) : make_float4(o.x / l, o.y / l, o.z / l, o.w / l);
+    if (p.out_bf16) reinterpret_cast<uint2 *>(p.out)[row * (D / 4) + c4] = make_uint2(pack_bf16(y.x, y.y), pack_bf16(y.z, y.w));
+    else reinterpret_cast<float4 *>(p.out)[row * (D / 4) + c4] = y;
+}
+
+// The trees.  parent: the user's parents, -1 = the context.  Tokens above a token are found by walking up; `words` gets the bits of
+// those (and of the token itself) that the window and the sinks let it see.  Depths are how many steps the walk takes.
+__device__ __forceinline__ int drafted_depth(const int16_t *parent, int i) {
+    int d = 0;
+    for (int j = parent[i]; j >= 0; j = parent[j]) ++d;
+    return d;
+}
+__device__ __forceinline__ void drafted_line(const DraftedParams &p, const DraftedUser &s, const int16_t *parent, int i, int depth, uint32_t *words) {
+#pragma unroll
+    for (int x = 0; x < kDrWords; ++x) words[x] = 0u;
+    int d = depth;
+    for (int j = i; j >= 0; j = parent[j], --d)
+        if (p.window == 0 || depth - d < p.window || static_cast<int64_t>(s.ctx) + d < p.sinks) words[j >> 5] |= 1u << (j & 31);
+}
+
+// ---------------------------------------------------------------------------------------------------------------------
+// The join: CTA j takes a part of the items that the attention's CTA j left a piece of, in proportion to their pieces.
+template <int D, int RT, bool LOG2>
+__global__ void __launch_bounds__(256) drafted_join_kernel(const __grid_constant__ DraftedParams p) {
+    constexpr float kUnit = LOG2 ? 0.69314718055994531f : 1.f;
+    griddep_wait();
+    for (int x = 0; x < 2; ++x) {
+        const int slot = 2 * blockIdx.x + x;
+        const int4 a = p.records[2 * slot], b = p.records[2 * slot + 1];
+        if (a.x == 0) continue;
+        const int u = a.y, tok0 = a.z, sq = a.w, toks = b.x, c0 = b.y, c1 = b.z, pieces = c1 - c0 + 1, rows = toks * p.hs;
+        const int h0 = sq / p.hgroups * p.g + sq % p.hgroups * p.hs;
+        const bool bad = p.bad[u] == p.epoch;
+        const int E = rows * (D / 4), mine = blockIdx.x - c0;
+        const int e0 = static_cast<int>(static_cast<int64_t>(E) * mine / pieces), e1 = static_cast<int>(static_cast<int64_t>(E) * (mine + 1) / pieces);
+        for (int e = e0 + threadIdx.x; e < e1; e += 256) {
+            const int r = e % rows, c = e / rows;
+            float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+            float m = -INFINITY, l = 0.f;
+#pragma unroll 4
+            for (int k = 0; k < pieces; ++k) {
+                const float *s = p.scratch + static_cast<size_t>(2 * (c0 + k) + (k == 0 ? 1 : 0)) * drafted_slot_floats(D, RT);
+                const float mk = s[RT * D + r], lk = s[RT * (D + 1) + r];
+                const float4 v = reinterpret_cast<const float4 *>(s)[c * RT + r];
+                const float M = fmaxf(m, mk);
+                const float wa = m == -INFINITY ? 0.f : (LOG2 ? exp2f(m - M) : expf(m - M));
+                const float wb = mk == -INFINITY ? 0.f : (LOG2 ? exp2f(mk - M) : expf(mk - M));
+                l = (l != l ? l : l * wa) + (lk != lk ? lk : wb != 0.f ? lk * wb : 0.f);
+                o.x = o.x * wa + (wb != 0.f ? v.x * wb : 0.f);
+                o.y = o.y * wa + (wb != 0.f ? v.y * wb : 0.f);
+                o.z = o.z * wa + (wb != 0.f ? v.z * wb : 0.f);
+                o.w = o.w * wa + (wb != 0.f ? v.w * wb : 0.f);
+                m = M;
+            }
+            drafted_store4<D>(p, (static_cast<int64_t>(tok0) + r / p.hs) * p.Hq + h0 + r % p.hs, c, o, m * kUnit, l, bad);
+        }
+    }
+}
+
+}  // namespace spd

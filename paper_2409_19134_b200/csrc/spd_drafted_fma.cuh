@@ -1,0 +1,228 @@
+// Drafted tokens on the FMA pipes: fp32 arithmetic throughout.
+//
+// RT rows (64, or 16 where users bring few) x 64 keys a block, 4 x 4 scores per thread; the 16 threads of a row keep its maximum and sum in
+// registers, weights go through shared memory to the threads that hold the row's channels (the same 16).  A hidden key's weight is the
+// mark -1, which the product with V skips: whatever its rows of k and v hold never enters.
+#pragma once
+
+#include "spd_drafted.cuh"
+
+namespace spd {
+
+template <int D, int RT>
+struct DraftedFma {
+    static constexpr int kThreads = RT * 4, kPitch = D + 4;       // rows of Q, K and V: 16-byte reads of 8 lanes fall in 32 banks
+    static constexpr size_t smem_bytes() { return (static_cast<size_t>(RT + 2 * kDrBlock) * kPitch + RT * kDrBlock) * 4; }
+};
+
+template <typename E> __device__ __forceinline__ float4 drafted_load4(const E *p);
+template <> __device__ __forceinline__ float4 drafted_load4<float>(const float *p) { return *reinterpret_cast<const float4 *>(p); }
+template <> __device__ __forceinline__ float4 drafted_load4<__nv_bfloat16>(const __nv_bfloat16 *p) {
+    const uint2 w = *reinterpret_cast<const uint2 *>(p);
+    const float2 a = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162 *>(&w.x)), b = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162 *>(&w.y));
+    return make_float4(a.x, a.y, b.x, b.y);
+}
+
+template <typename E, int D, int RT>
+__global__ void __launch_bounds__(DraftedFma<D, RT>::kThreads) drafted_fma_kernel(const __grid_constant__ DraftedParams p) {
+    using C = DraftedFma<D, RT>;
+    constexpr int NT = C::kThreads, PITCH = C::kPitch, KB = kDrBlock, CH = D / 64;      // CH chunks of four channels per thread
+    extern __shared__ __align__(16) float sm[];
+    float *Qs = sm, *Ks = Qs + RT * PITCH, *Vs = Ks + KB * PITCH, *Ps = Vs + KB * PITCH;
+    __shared__ int64_t sums[NT];
+    __shared__ int first_bad;
+    __shared__ DraftedTile tiles[kDrTiles];
+    __shared__ int tile_page[kDrTiles];
+    __shared__ int16_t parent[kDrTree];
+    __shared__ int16_t depths[kDrTree];
+    __shared__ uint32_t lines[RT][kDrWords];
+    const int tid = threadIdx.x, lane = tid & 31, tx = tid & 15, ty = tid >> 4;
+    int Cu, chunks;
+    const int64_t W = drafted_sums<NT>(p, sums, &first_bad, Cu, chunks);
+    if (blockIdx.x == 0 && tid == 0) drafted_header(p, first_bad);
+    if (tid < 4) p.records[4 * blockIdx.x + tid] = make_int4(0, 0, 0, 0);
+    __syncthreads();
+    const int shares = static_cast<int>(min(static_cast<int64_t>(p.grid), (W + kDrMinBlocks - 1) / kDrMinBlocks));
+    if (static_cast<int>(blockIdx.x) >= shares) return;
+    int64_t x = drafted_bound(W, shares, blockIdx.x);
+    const int64_t x1 = drafted_bound(W, shares, blockIdx.x + 1);
+    DraftedWalk w;
+    drafted_locate(p, sums, Cu, chunks, x, lane, w);
+    while (true) {
+        const int b0 = static_cast<int>(x - w.x0), b1 = static_cast<int>(min(static_cast<int64_t>(w.k.nb), x1 - w.x0));
+        const DraftedUser s = w.s;
+        const int i0 = w.rt * p.tt, toks = min(p.tt, s.n - i0), rows = toks * p.hs;
+        const int kvh = w.sq / p.hgroups, h0 = kvh * p.g + w.sq % p.hgroups * p.hs;
+        bool bad = !s.good;
+        // ---- Q, and the tree
+        __syncthreads();
+        for (int e = tid; e < RT * (D / 4); e += NT) {
+            const int r = e / (D / 4), c = e % (D / 4);
+            float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+            if (r < rows) v = drafted_load4(static_cast<const E *>(p.q) + ((static_cast<int64_t>(s.first) + i0 + r / p.hs) * p.Hq + h0 + r % p.hs) * D + 4 * c);
+            *reinterpret_cast<float4 *>(Qs + r * PITCH + 4 * c) = v;
+        }
+        if (p.parents != nullptr && s.good) {
+            bool wrong = false;
+            for (int i = tid; i < s.n; i += NT) {
+                const int up = p.parents[s.first + i];
+                wrong = wrong || up < -1 || up >= i;
+                parent[i] = static_cast<int16_t>(up < -1 || up >= i ? -1 : up);
+            }
+            if (__syncthreads_or(wrong)) { bad = true; }
+            for (int i = tid; i < s.n; i += NT) depths[i] = static_cast<int16_t>(drafted_depth(parent, i));
+            __syncthreads();
+            for (int i = tid; i < toks; i += NT) drafted_line(p, s, parent, i0 + i, depths[i0 + i], lines[i]);
+        }
+        __syncthreads();
+        int pos[4], tok[4];              // positions and tokens (within the tile) of the thread's rows
+        float slope[4], m[4], l[4], o[4][4 * CH];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int r = min(4 * ty + i, rows - 1);
+            tok[i] = r / p.hs;
+            pos[i] = s.ctx + (p.parents ? (s.good ? depths[i0 + tok[i]] : 0) : i0 + tok[i]);
+            slope[i] = p.slopes ? p.slopes[h0 + r % p.hs] : 0.f;
+            m[i] = -INFINITY; l[i] = 0.f;
+#pragma unroll
+            for (int c = 0; c < 4 * CH; ++c) o[i][c] = 0.f;
+        }
+        for (int b = b0; b < b1; ++b) {
+            if (tid < kDrTiles) {
+                const DraftedTile t = drafted_tile(p, s, w.k, b * kDrTiles + tid);
+                int page = 0;
+                if (t.cnt > 0) page = p.part[t.part].indices[t.entry];
+                const bool ok = t.cnt > 0 && page >= 0 && page < p.part[t.part].num_pages;
+                tiles[tid] = t;
+                tile_page[tid] = ok ? page : (t.cnt > 0 ? -1 : -2);
+            }
+            __syncthreads();
+            for (int e = tid; e < KB * (D / 4); e += NT) {
+                const int key = e / (D / 4), c = e % (D / 4), t = key / kPage, slot = key % kPage;
+                float4 kv = make_float4(0.f, 0.f, 0.f, 0.f), vv = kv;
+                if (tile_page[t] >= 0 && slot < tiles[t].cnt) {
+                    const int64_t at = ((static_cast<int64_t>(tile_page[t]) * p.Hkv + kvh) * kPage + slot) * D + 4 * c;
+                    kv = drafted_load4(static_cast<const E *>(p.k_pool[tiles[t].part]) + at);
+                    vv = drafted_load4(static_cast<const E *>(p.v_pool[tiles[t].part]) + at);
+                }
+                *reinterpret_cast<float4 *>(Ks + key * PITCH + 4 * c) = kv;
+                *reinterpret_cast<float4 *>(Vs + key * PITCH + 4 * c) = vv;
+            }
+#pragma unroll
+            for (int t = 0; t < kDrTiles; ++t) bad = bad || tile_page[t] == -1;
+            __syncthreads();
+            if ((tid & ~31) / 16 * 4 < rows) {            // warps without a row have nothing to do
+                float sc[4][4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) sc[i][j] = 0.f;
+#pragma unroll 4
+                for (int c = 0; c < D; c += 4) {
+                    float4 a[4], k4[4];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) a[i] = *reinterpret_cast<const float4 *>(Qs + (4 * ty + i) * PITCH + c);
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) k4[j] = *reinterpret_cast<const float4 *>(Ks + (tx + 16 * j) * PITCH + c);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) {
+                            sc[i][j] = fmaf(a[i].x, k4[j].x, sc[i][j]); sc[i][j] = fmaf(a[i].y, k4[j].y, sc[i][j]);
+                            sc[i][j] = fmaf(a[i].z, k4[j].z, sc[i][j]); sc[i][j] = fmaf(a[i].w, k4[j].w, sc[i][j]);
+                        }
+                }
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    bool seen[4];
+                    float mx = -INFINITY;
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {          // key tx of tile j
+                        const int at = tiles[j].base + tx;
+                        const bool drafted = at >= s.ctx;
+                        int far = pos[i] - at;             // distance
+                        bool see = tx < tiles[j].cnt && tile_page[j] >= 0;
+                        if (drafted && p.parents != nullptr) {
+                            const int d = see ? at - s.ctx : 0;
+                            far = see ? pos[i] - s.ctx - depths[d] : 0;
+                            see = see && ((lines[tok[i]][d >> 5] >> (d & 31)) & 1u);
+                        } else {
+                            see = see && far >= 0 && (p.window == 0 || far < p.window || at < p.sinks);
+                        }
+                        seen[j] = see;
+                        float v = sc[i][j] * p.sm_scale;
+                        if (p.cap > 0.f) v = p.cap * tanhf(v / p.cap);
+                        if (p.slopes != nullptr) v = fmaf(-slope[i], static_cast<float>(far), v);
+                        sc[i][j] = see ? v : -INFINITY;
+                        mx = fmaxf(mx, sc[i][j]);
+                    }
+#pragma unroll
+                    for (int d = 8; d >= 1; d >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, d));
+                    const float mn = fmaxf(m[i], mx), ref = mn == -INFINITY ? 0.f : mn;
+                    const float alpha = m[i] == -INFINITY ? 1.f : expf(m[i] - ref);        // nothing seen yet: O is 0, and l 0 or NaN
+                    float sum = 0.f;
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        const float wt = seen[j] ? expf(sc[i][j] - ref) : -1.f;
+                        Ps[(4 * ty + i) * KB + tx + 16 * j] = wt;
+                        sum += seen[j] ? wt : 0.f;
+                    }
+#pragma unroll
+                    for (int d = 8; d >= 1; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
+                    l[i] = l[i] * alpha + sum;
+                    m[i] = mn;
+#pragma unroll
+                    for (int c = 0; c < 4 * CH; ++c) o[i][c] *= alpha;
+                }
+                __syncwarp();
+#pragma unroll 2
+                for (int k4 = 0; k4 < KB; k4 += 4) {
+                    float4 wt[4];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) wt[i] = *reinterpret_cast<const float4 *>(Ps + (4 * ty + i) * KB + k4);
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {
+                        float4 v[CH];
+#pragma unroll
+                        for (int c = 0; c < CH; ++c) v[c] = *reinterpret_cast<const float4 *>(Vs + (k4 + k) * PITCH + 4 * (tx + 16 * c));
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            const float q = k == 0 ? wt[i].x : k == 1 ? wt[i].y : k == 2 ? wt[i].z : wt[i].w;
+                            if (q < 0.f) continue;
+#pragma unroll
+                            for (int c = 0; c < CH; ++c) {
+                                o[i][4 * c] = fmaf(q, v[c].x, o[i][4 * c]); o[i][4 * c + 1] = fmaf(q, v[c].y, o[i][4 * c + 1]);
+                                o[i][4 * c + 2] = fmaf(q, v[c].z, o[i][4 * c + 2]); o[i][4 * c + 3] = fmaf(q, v[c].w, o[i][4 * c + 3]);
+                            }
+                        }
+                    }
+                }
+            }
+            __syncthreads();
+        }
+        // ---- the piece: the whole item, or a slot
+        if (bad && tid == 0) drafted_flag(p, w.u);
+        const bool whole = b0 == 0 && b1 == w.k.nb;
+        const int slot = 2 * blockIdx.x + (b0 == 0 ? 1 : 0);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int r = 4 * ty + i;
+            if (r >= rows) continue;
+            const int64_t row = (static_cast<int64_t>(s.first) + i0 + tok[i]) * p.Hq + h0 + r % p.hs;
+            float *dst = p.scratch + static_cast<size_t>(slot) * drafted_slot_floats(D, RT);
+#pragma unroll
+            for (int c = 0; c < CH; ++c) {
+                const float4 v = make_float4(o[i][4 * c], o[i][4 * c + 1], o[i][4 * c + 2], o[i][4 * c + 3]);
+                if (whole) drafted_store4<D>(p, row, tx + 16 * c, v, m[i], l[i], bad);
+                else reinterpret_cast<float4 *>(dst)[(tx + 16 * c) * RT + r] = v;
+            }
+            if (!whole && tx == 0) { dst[RT * D + r] = m[i]; dst[RT * (D + 1) + r] = l[i]; }
+        }
+        if (!whole && tid == 0) drafted_record(p, w, slot, W, shares);
+        x = w.x0 + b1;
+        if (x >= x1) break;
+        drafted_next(p, w);
+    }
+}
+
+}  // namespace spd
