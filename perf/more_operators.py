@@ -428,14 +428,16 @@ def _run_own(st):
         else:
             spd.spd_decode_step_drafted(shape, score, st["q"], st["priv"], st["pub"], st["out"], ws, **drafts)
         return st["out"]
+    if case["op"] != "turn" and "handle" not in st:        # kept as long as the cache's pools, like the pools themselves
+        st["handle"] = spd.make_pools(shape, st["pools"] if case["op"] == "fork" else st["part"].pools)
     if case["op"] == "keep":
-        spd.spd_keep_drafted(shape, st["part"].pools, st["part"], st["indptr"], st["last"], ws, parents=st["parents"], new_lens=st["new_lens"],
+        spd.spd_keep_drafted(shape, st["handle"], st["part"], st["indptr"], st["last"], ws, parents=st["parents"], new_lens=st["new_lens"],
                              kept=st["kept"])
         return {"pools": st["part"].pools, "new_lens": st["new_lens"], "kept": st["kept"]}
     spd.spd_pages_release(shape, st["refs"], st["page_indptr"], st["page_indices"], st["gone_from"], ws)
     if case["op"] == "fork":
         spd.spd_pages_fork(shape, st["refs"], st["page_indptr"], st["page_indices"], st["seq_lens"], st["source"], st["copies"], ws)
-        spd.spd_pages_copy(shape, st["pools"], st["copies"], ws)
+        spd.spd_pages_copy(shape, st["handle"], st["copies"], ws)
         return {"pools": st["pools"], "table": st["page_indices"], "refs": st["refs"], "lens": st["seq_lens"], "copies": st["copies"]}
     spd.spd_pages_take(shape, st["refs"], st["page_indptr"], st["page_indices"], st["have"], st["want"], ws)
     return {"table": st["page_indices"], "refs": st["refs"]}
