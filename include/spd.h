@@ -63,7 +63,8 @@ typedef enum {
     SPD_ERR_BAD_PAGE = 4,      /* device saw a page index or length out of range (sticky flag) */
     SPD_ERR_CUDA = 5,          /* a CUDA runtime or driver call failed                         */
     SPD_ERR_TIMEOUT = 6,       /* a bounded wait inside a kernel ran out (sticky flag)         */
-    SPD_ERR_PLAN = 7           /* a call told to reuse a stored plan found none that fits (sticky flag) */
+    SPD_ERR_PLAN = 7,          /* a call told to reuse a stored plan found none that fits (sticky flag) */
+    SPD_ERR_NO_PAGE = 8        /* fewer free pages than asked for (sticky flag) */
 } spd_status;
 
 typedef enum { SPD_F32 = 0, SPD_BF16 = 1 } spd_dtype;
@@ -363,6 +364,61 @@ spd_status spd_service_attn_merge_drafted(const spd_shape *shape, const spd_scor
                                           spd_dtype out_dtype, void *ws, size_t ws_bytes, void *cuda_stream);
 
 /*
+ * Accepted drafted tokens: what the model has verified stays, the rest of the draft goes (no counterpart in the paper).  For user u with drafted
+ * tokens as above (the last n of the partition), last[u] (device [batch]) is the last accepted token: it and the tokens that it comes after
+ * stay, -1 = none.  Their k and v rows move, root first, to the front of the drafted ones in every pool, so that the partition's length is
+ * ctx + (tokens that stay).
+ *   pools: HOST array of num_pools device pointers, K and V pools of all layers that share the partition's tables, each
+ *     [num_pages][num_kv_heads][page_size][head_dim] in the shape's dtype, 128-byte aligned.
+ *   tok_indptr, parents as for spd_drafts (parents NULL: tokens 0 .. last[u] stay, and nothing has to move).
+ *   new_lens [batch]: the lengths afterwards; seq_lens itself (in place), another array, or NULL.
+ *   kept [total_tokens] or NULL: kept[tok_indptr[u] + i] = the token that is now the i-th, -1 behind the last one.
+ * A user with an inconsistent table, length, tree or `last`, or a page out of range among the rows that stay, keeps its rows and its length (kept: -1)
+ * and raises SPD_ERR_BAD_PAGE.  The pages that hold drafted tokens must not be shared with another user.  new_lens and kept overlap no other argument.
+ * One kernel per 128 pools, in plain stream order; the workspace is one of spd_workspace_size.
+ */
+spd_status spd_keep_drafted(const spd_shape *shape, int64_t total_tokens, const int32_t *tok_indptr, const int32_t *parents,
+                            const int32_t *last, int32_t num_pools, void *const *pools, int32_t num_pages,
+                            const int32_t *page_indptr, const int32_t *page_indices, const int32_t *seq_lens,
+                            int32_t *new_lens, int32_t *kept, void *ws, size_t ws_bytes, void *cuda_stream);
+
+/*
+ * Pages handed out, shared, copied and released on the device (no counterpart in the paper, whose caches grow and go with their process).
+ *   refs [num_pages] (device, 16-byte aligned): how many table entries list each page; 0 = the page is free.  All zeros at the start.
+ *   page_indptr, page_indices: the tables of all other calls; user u has room for page_indptr[u+1] - page_indptr[u] entries, and an entry
+ *     that lists no page holds -1.  A page shared by several users (or caches) counts once per entry.
+ * spd_pages_take lists a fresh page in every entry that holds -1 among those for tokens [from_tokens[u], to_tokens[u]) -- from a multiple of
+ *   page_size on: entry ceil(from / page_size) is the first one, entry ceil(to / page_size) - 1 the last.  Fresh pages are the free ones with
+ *   the lowest numbers, in the order of users and entries.  Users are served in order as long as there are pages for all that a user wants; one that
+ *   there are not enough for gets none, like all behind it that want any, and raises SPD_ERR_NO_PAGE.
+ * spd_pages_release takes out the entries that hold nothing but tokens [from_tokens[u], to_tokens[u]) (to_tokens NULL: to the end of the
+ *   table): refs of their pages go down by one, the entries become -1; entries of -1 are passed over.  Releasing [0, end) ends a user;
+ *   [new length, end) gives back what a shorter sequence no longer needs; [sinks, first visible token) what lies hidden behind a window
+ *   (calls with that window never look at those entries).
+ * spd_pages_fork: where source[u] >= 0, user u, whose entries for as many tokens must hold -1, becomes a copy of user source[u] != u (which is not
+ *   one itself in this call): full pages are shared, the page that is being filled is replaced by a fresh one, seq_lens[u] is set;
+ *   copies[u] = (that page, the fresh one) tells spd_pages_copy what to copy in every layer's pools.  (-1, -1) where nothing is to copy.
+ *   source[u] = -1: the user stays as it is.  Entries of -1 in full pages (released behind a window) stay -1.
+ * spd_pages_copy copies page copies[i][0] to page copies[i][1] (device [num_copies][2], (-1, -1) = nothing) in every pool (HOST array, as for
+ *   spd_keep_drafted).  No page may be the target of two pairs, nor the source of one and the target of another.
+ * A user with an inconsistent table or request (ranges behind the table's end, negative numbers, a fork into entries in use, pages out of range or
+ * with refs that say nobody lists them) raises SPD_ERR_BAD_PAGE; take and fork leave it as it is, release takes out the entries that are
+ * in order.  A pair with a page out of range is left out and raises SPD_ERR_BAD_PAGE (for the pair's number in place of a user's).
+ * Plain stream order; take and fork are two kernels, release is one, copy one per 128 pools.  The workspace is one of spd_workspace_size;
+ * take and fork keep 4 bytes per page in it, and pools of more than a million pages may need a larger one (SPD_ERR_WORKSPACE).
+ */
+spd_status spd_pages_take(const spd_shape *shape, int32_t num_pages, int32_t *refs, const int32_t *page_indptr, int32_t *page_indices,
+                          const int32_t *from_tokens, const int32_t *to_tokens, void *ws, size_t ws_bytes, void *cuda_stream);
+spd_status spd_pages_release(const spd_shape *shape, int32_t num_pages, int32_t *refs, const int32_t *page_indptr,
+                             int32_t *page_indices, const int32_t *from_tokens, const int32_t *to_tokens, void *ws,
+                             size_t ws_bytes, void *cuda_stream);
+spd_status spd_pages_fork(const spd_shape *shape, int32_t num_pages, int32_t *refs, const int32_t *page_indptr, int32_t *page_indices,
+                          int32_t *seq_lens, const int32_t *source, int32_t *copies, void *ws, size_t ws_bytes,
+                          void *cuda_stream);
+spd_status spd_pages_copy(const spd_shape *shape, int32_t num_pools, void *const *pools, int32_t num_pages, int32_t num_copies,
+                          const int32_t *copies, void *ws, size_t ws_bytes, void *cuda_stream);
+
+/*
  * Rows of new tokens, as a projection leaves them: [total_tokens][heads][head_dim] in the shape's dtype, consecutive
  * tokens *_stride elements apart (0 = packed, i.e. heads * head_dim; q, k and v may be parts of one wider row).  Strides
  * and pointers are multiples of 16 bytes.
@@ -501,7 +557,7 @@ spd_status spd_decode_step_host(const spd_shape *shape, const spd_step_blob *lay
 
 /*
  * Waits for `cuda_stream`, then reads and clears the workspace's sticky status.  Returns SPD_OK,
- * SPD_ERR_BAD_PAGE, SPD_ERR_TIMEOUT or SPD_ERR_PLAN; *first_bad_user (may be NULL) receives the lowest user
+ * SPD_ERR_BAD_PAGE, SPD_ERR_TIMEOUT, SPD_ERR_PLAN or SPD_ERR_NO_PAGE; *first_bad_user (may be NULL) receives the lowest user
  * index that was flagged, or -1.  After a status other than SPD_OK the per-user flags and the merge tickets of
  * the workspace are cleared too, so the next call starts clean.
  */

@@ -17,7 +17,7 @@ SPD_OK = 0
 SPD_F32, SPD_BF16 = 0, 1
 SPD_PLAN_PER_CALL, SPD_PLAN_STORE, SPD_PLAN_REUSE = 0, 1, 2
 _STATUS_NAMES = {0: "SPD_OK", 1: "SPD_ERR_INVALID_ARG", 2: "SPD_ERR_UNSUPPORTED", 3: "SPD_ERR_WORKSPACE",
-                 4: "SPD_ERR_BAD_PAGE", 5: "SPD_ERR_CUDA", 6: "SPD_ERR_TIMEOUT", 7: "SPD_ERR_PLAN"}
+                 4: "SPD_ERR_BAD_PAGE", 5: "SPD_ERR_CUDA", 6: "SPD_ERR_TIMEOUT", 7: "SPD_ERR_PLAN", 8: "SPD_ERR_NO_PAGE"}
 _DEVICE_CODES = (SPD_OK, 4, 6, 7)     # what a call that waits for the device may report without raising
 
 EXPORTS = ["spd_workspace_size", "spd_partial_attn", "spd_service_attn_merge", "spd_decode_step",
@@ -30,7 +30,7 @@ EXPORTS = ["spd_workspace_size", "spd_partial_attn", "spd_service_attn_merge", "
            "spd_debug_sm_moves", "spd_decode_step_append", "spd_watch_alarm", "spd_service_attn_merge_append",
            "spd_partial_attn_scored", "spd_service_attn_merge_scored", "spd_decode_step_scored", "spd_prefill_attn_scored",
            "spd_append_kv_rope", "spd_drafted_workspace_size", "spd_decode_step_drafted", "spd_partial_attn_drafted",
-           "spd_service_attn_merge_drafted"]
+           "spd_service_attn_merge_drafted", "spd_keep_drafted", "spd_pages_take", "spd_pages_release", "spd_pages_fork", "spd_pages_copy"]
 
 
 class SpdError(RuntimeError):
@@ -149,6 +149,11 @@ def lib() -> C.CDLL:
                                                vp, sz, vp]
         L.spd_service_attn_merge_drafted.argtypes = [C.POINTER(Shape), C.POINTER(Score), C.POINTER(Drafts), vp, C.POINTER(PagedKV), vp,
                                                      Partial, vp, C.c_int, vp, sz, vp]
+        L.spd_keep_drafted.argtypes = [C.POINTER(Shape), C.c_int64, vp, vp, vp, C.c_int32, vp, C.c_int32, vp, vp, vp, vp, vp, vp, sz, vp]
+        for name in ("take", "release"):
+            getattr(L, "spd_pages_" + name).argtypes = [C.POINTER(Shape), C.c_int32, vp, vp, vp, vp, vp, vp, sz, vp]
+        L.spd_pages_fork.argtypes = [C.POINTER(Shape), C.c_int32, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+        L.spd_pages_copy.argtypes = [C.POINTER(Shape), C.c_int32, vp, C.c_int32, C.c_int32, vp, vp, sz, vp]
         L.spd_watch_alarm.argtypes = [vp, C.c_int32, C.c_int32, vp, C.c_float, vp, vp]
         L.spd_set_split.argtypes = [C.c_int32, C.c_int32]
         L.spd_set_programmatic_launch.argtypes = [C.c_int32]
@@ -755,3 +760,97 @@ def spd_service_attn_merge_drafted(shape, score, q, pub, priv_lens, partial_in, 
     _check(lib().spd_service_attn_merge_drafted(shape, score, drafts, _ptr(q), kv, _i32(priv_lens, shape.batch, dev=dev), part,
                                                 _packed(out, q.numel(), dev=dev), _dtype_code(out.dtype), *_workspace(ws, dev),
                                                 _stream_ptr(stream)), "spd_service_attn_merge_drafted")
+
+
+class Pools:
+    """Pools that share their pages' tables, K and V of any number of layers, as the calls take them; it keeps them alive."""
+
+    def __init__(self, shape, pools):
+        pools = list(pools)
+        self.dev = _here(pools[0]) if pools else -1
+        self.pages, self.page, self.dtype = (pools[0].shape[0] if pools else 0), shape.num_kv_heads * shape.page_size * shape.head_dim, _TORCH_DTYPES[shape.dtype]
+        for t in pools:
+            if t.dtype is not self.dtype or t.shape[0] != self.pages or t.numel() != self.pages * self.page or not t.is_contiguous():
+                raise ValueError(f"expected contiguous {self.dtype} pools of {self.pages} pages of {self.page} elements (KV heads x page size x "
+                                 f"head_dim), got {t.dtype} {list(t.shape)}")
+            if t.get_device() != self.dev:
+                raise _elsewhere(t)
+        self.count, self.array, self._keep = len(pools), (C.c_void_p * max(1, len(pools)))(*[t.data_ptr() for t in pools]), pools
+
+
+def make_pools(shape, pools) -> Pools:
+    """A handle for spd_keep_drafted and spd_pages_copy, for a program that keeps its pools: the list is looked over once."""
+    return Pools(shape, pools)
+
+
+def _pools(shape, pools, dev) -> Pools:
+    if not isinstance(pools, Pools):
+        pools = Pools(shape, pools)
+    if pools.page != shape.num_kv_heads * shape.page_size * shape.head_dim or pools.dtype is not _TORCH_DTYPES[shape.dtype]:
+        raise ValueError("the pools were made for another shape")
+    if pools.count and pools.dev != dev:
+        raise _elsewhere(pools._keep[0])
+    return pools
+
+
+def spd_keep_drafted(shape, pools, part, tok_indptr, last, ws, parents=None, new_lens="in place", kept=None, total_tokens=None, stream=None) -> None:
+    """Keep token last[u] (int32 [B], -1 = none) of each user's drafted tokens and those that it comes after: their rows move to the front in
+    all `pools` (make_pools, or a list of tensors), whose tables and lengths `part` has; tok_indptr int32 [B+1] or None (one token per user);
+    parents int32 [T] or None (runs); new_lens: an int32 [B] tensor, None, or by default part.seq_lens itself; kept int32 [T] or None;
+    total_tokens: T, where neither parents nor kept tells it."""
+    dev, B = _here(last), shape.batch
+    T = B if tok_indptr is None else next((t.numel() for t in (parents, kept) if t is not None), total_tokens)
+    if T is None:
+        raise ValueError("total_tokens is needed")
+    pools = _pools(shape, pools, dev)
+    lens = _i32(part.seq_lens, B, dev=dev)
+    indices = part.page_indices
+    if indices.dtype is not _I32 or not indices.is_contiguous():
+        raise ValueError(f"expected contiguous int32 page_indices, got {indices.dtype}")
+    if indices.get_device() != dev:
+        raise _elsewhere(indices)
+    _check(lib().spd_keep_drafted(shape, T, _i32(tok_indptr, B + 1, dev=dev), _i32(parents, T, dev=dev), _i32(last, B, dev=dev), pools.count,
+                                  pools.array, pools.pages, _i32(part.page_indptr, B + 1, dev=dev), _ptr(indices), lens,
+                                  lens if isinstance(new_lens, str) else _i32(new_lens, B, dev=dev), _i32(kept, T, dev=dev),
+                                  *_workspace(ws, dev), _stream_ptr(stream)), "spd_keep_drafted")
+
+
+def _page_table(shape, refs, page_indptr, page_indices):
+    """(num_pages, refs, page_indptr, page_indices) of a table whose pages are counted, and the device."""
+    dev = _here(refs)
+    for t in (refs, page_indices):
+        if t.dtype is not _I32 or t.dim() != 1 or not t.is_contiguous():
+            raise ValueError(f"expected contiguous one-dimensional int32 refs and page_indices, got {t.dtype} {list(t.shape)}")
+    if page_indices.get_device() != dev:
+        raise _elsewhere(page_indices)
+    return (refs.numel(), _ptr(refs), _i32(page_indptr, shape.batch + 1, dev=dev), _ptr(page_indices)), dev
+
+
+def spd_pages_take(shape, refs, page_indptr, page_indices, from_tokens, to_tokens, ws, stream=None) -> None:
+    """Fresh pages for the entries of tokens [from_tokens[u], to_tokens[u]) that hold -1 (int32 [B] each)."""
+    table, dev = _page_table(shape, refs, page_indptr, page_indices)
+    _check(lib().spd_pages_take(shape, *table, _i32(from_tokens, shape.batch, dev=dev), _i32(to_tokens, shape.batch, dev=dev), *_workspace(ws, dev),
+                                _stream_ptr(stream)), "spd_pages_take")
+
+
+def spd_pages_release(shape, refs, page_indptr, page_indices, from_tokens, ws, to_tokens=None, stream=None) -> None:
+    """Take the entries that hold nothing but tokens [from_tokens[u], to_tokens[u]) out of the tables; to_tokens None: to the tables' end."""
+    table, dev = _page_table(shape, refs, page_indptr, page_indices)
+    _check(lib().spd_pages_release(shape, *table, _i32(from_tokens, shape.batch, dev=dev), _i32(to_tokens, shape.batch, dev=dev), *_workspace(ws, dev),
+                                   _stream_ptr(stream)), "spd_pages_release")
+
+
+def spd_pages_fork(shape, refs, page_indptr, page_indices, seq_lens, source, copies, ws, stream=None) -> None:
+    """User u becomes a copy of user source[u] (int32 [B], -1: it stays); copies int32 [B, 2] receives the pages to copy (spd_pages_copy)."""
+    table, dev = _page_table(shape, refs, page_indptr, page_indices)
+    B = shape.batch
+    _check(lib().spd_pages_fork(shape, *table, _i32(seq_lens, B, dev=dev), _i32(source, B, dev=dev), _i32(copies, B, 2, dev=dev), *_workspace(ws, dev),
+                                _stream_ptr(stream)), "spd_pages_fork")
+
+
+def spd_pages_copy(shape, pools, copies, ws, stream=None) -> None:
+    """Copy page copies[i, 0] to page copies[i, 1] (int32 [n, 2]) in all pools (make_pools, or a list of tensors)."""
+    dev = _here(copies)
+    pools, n = _pools(shape, pools, dev), copies.shape[0]
+    _check(lib().spd_pages_copy(shape, pools.count, pools.array, pools.pages, n, _i32(copies, n, 2, dev=dev), *_workspace(ws, dev),
+                                _stream_ptr(stream)), "spd_pages_copy")

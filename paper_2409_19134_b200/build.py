@@ -8,7 +8,8 @@ import sys
 _PKG = os.path.dirname(os.path.abspath(__file__))
 _ROOT = os.path.dirname(_PKG)
 LIB_PATH = os.path.join(_PKG, "libspd.so")
-SOURCES = [os.path.join(_PKG, "csrc", f) for f in ("spd_api.cu", "spd_scored.cu", "spd_prefill_scored.cu", "spd_drafted.cu")]
+SOURCES = [os.path.join(_PKG, "csrc", f) for f in ("spd_api.cu", "spd_scored.cu", "spd_prefill_scored.cu", "spd_drafted.cu",
+                                                  "spd_pages.cu")]
 HEADERS = sorted(os.path.join(_PKG, "csrc", f) for f in os.listdir(os.path.join(_PKG, "csrc")) if f.endswith((".cuh", ".h"))) + \
           [os.path.join(_ROOT, "include", "spd.h")]
 

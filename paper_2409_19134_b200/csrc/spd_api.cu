@@ -1138,6 +1138,7 @@ const char *spd_status_string(spd_status status) {
         case SPD_ERR_BAD_PAGE: return "page index or sequence length out of range (seen on the device)";
         case SPD_ERR_CUDA: return "CUDA call failed";
         case SPD_ERR_TIMEOUT: return "a bounded wait inside a kernel ran out";
+        case SPD_ERR_NO_PAGE: return "fewer free pages than asked for";
         case SPD_ERR_PLAN: return "no stored plan fits this call (never stored, or stored for another shape or grid)";
     }
     return "unknown status";
