@@ -1,9 +1,11 @@
 // Attention of drafted tokens: argument checks, choice of the kernel, launches.
+#include <cmath>
 #include <cstdio>
 #include <mutex>
 
 #include "spd_drafted.cuh"
 #include "spd_drafted_fma.cuh"
+#include "spd_drafted_tc.cuh"
 #include "spd_host.h"
 
 namespace {
@@ -15,18 +17,19 @@ using host::misaligned;
 int heads_per_tile(int g, int RT) { return g <= RT ? g : kHeadsPerItem; }
 
 constexpr int kFmaPerSm = 2;        // CTAs of the largest FMA variant that share an SM; the others fit more
-constexpr int kMostRows = 128;      // rows of the largest tile
+constexpr int kMostFmaRows = 64;
 
 // Behind the workspace's head: records and slots of the pieces.
 struct DraftedLayout { size_t records, scratch, total; };
 DraftedLayout drafted_layout(const spd_shape &s, int sms) {
     const int g = s.num_q_heads / s.num_kv_heads;
     const int seqs = s.batch * s.num_kv_heads * (g > kHeadsPerItem ? g / kHeadsPerItem : 1);
-    const size_t slots = 2 * static_cast<size_t>(kFmaPerSm) * sms;
+    const bool tc = s.dtype == SPD_BF16;
+    const size_t slots = 2 * static_cast<size_t>(tc ? 1 : kFmaPerSm) * sms;
     DraftedLayout L;
     L.records = host::cleared_end(s.batch, seqs);
     L.scratch = L.records + (slots * 2 * sizeof(int4) + 255) / 256 * 256;
-    L.total = L.scratch + slots * drafted_slot_floats(s.head_dim, kMostRows) * sizeof(float);
+    L.total = L.scratch + slots * drafted_slot_floats(s.head_dim, tc ? kDtRows : kMostFmaRows) * sizeof(float);
     return L;
 }
 
@@ -47,6 +50,88 @@ spd_status launch_join(const DraftedParams &p, cudaStream_t st) {
     return err == cudaSuccess ? SPD_OK : SPD_ERR_CUDA;
 }
 
+// [T][Hq][D] bf16 as a 3-D map: a box is `tokens` tokens x `heads` heads x 128 bytes, 128-byte swizzle.
+spd_status make_q_map(CUtensorMap *map, const DraftedParams &p, int D, int tokens) {
+    EncodeTiledFn fn = host::tensor_map_encoder();
+    if (!fn) return SPD_ERR_CUDA;
+    cuuint64_t dims[3] = {static_cast<cuuint64_t>(D), static_cast<cuuint64_t>(p.Hq), static_cast<cuuint64_t>(p.T)};
+    cuuint64_t strides[2] = {static_cast<cuuint64_t>(D) * 2, static_cast<cuuint64_t>(p.Hq) * D * 2};
+    cuuint32_t box[3] = {64u, static_cast<cuuint32_t>(p.hs), static_cast<cuuint32_t>(tokens)};
+    cuuint32_t estr[3] = {1, 1, 1};
+    const CUresult r = fn(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void *>(p.q), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                          CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    if (r != CUDA_SUCCESS) fprintf(stderr, "libspd: cuTensorMapEncodeTiled failed with CUresult %d\n", static_cast<int>(r));
+    return r == CUDA_SUCCESS ? SPD_OK : SPD_ERR_CUDA;
+}
+
+// A pool's rows of one page and head: 16 x 128 bytes, 128-byte swizzle.
+spd_status make_pool_map(CUtensorMap *map, const DraftedParams &p, const void *pool, int64_t num_pages, int D) {
+    EncodeTiledFn fn = host::tensor_map_encoder();
+    if (!fn) return SPD_ERR_CUDA;
+    cuuint64_t dims[2] = {static_cast<cuuint64_t>(D), static_cast<cuuint64_t>(num_pages) * p.Hkv * kPage};
+    cuuint64_t strides[1] = {static_cast<cuuint64_t>(D) * 2};
+    cuuint32_t box[2] = {64u, static_cast<cuuint32_t>(kPage)};
+    cuuint32_t estr[2] = {1, 1};
+    const CUresult r = fn(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void *>(pool), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                          CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    if (r != CUDA_SUCCESS) fprintf(stderr, "libspd: cuTensorMapEncodeTiled failed with CUresult %d\n", static_cast<int>(r));
+    return r == CUDA_SUCCESS ? SPD_OK : SPD_ERR_CUDA;
+}
+
+template <int D, bool CAP, bool BIAS>
+spd_status launch_tc(const DraftedTcParams &p, const CUtensorMap *maps, cudaStream_t st) {
+    static std::once_flag once[64];
+    int dev = 0;
+    cudaGetDevice(&dev);
+    cudaError_t err = cudaSuccess;
+    std::call_once(once[dev & 63], [&] {
+        err = cudaFuncSetAttribute(drafted_tc_kernel<D, CAP, BIAS>, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(dt_smem_bytes(D)));
+    });
+    if (err != cudaSuccess) return SPD_ERR_CUDA;
+    drafted_tc_kernel<D, CAP, BIAS><<<p.d.grid, kDtThreads, dt_smem_bytes(D), st>>>(p, maps[0], maps[1], maps[2], maps[3], maps[4]);
+    host::count_launch();
+    if (cudaGetLastError() != cudaSuccess) return SPD_ERR_CUDA;
+    return launch_join<D, kDtRows, true>(p.d, st);
+}
+
+spd_status run_tc(const DraftedParams &call, int D, int sms, cudaStream_t st) {
+    DraftedTcParams p{};
+    p.d = call;
+    DraftedParams &d = p.d;
+    d.hs = heads_per_tile(d.g, kDtRows / 2);
+    d.hgroups = d.g / d.hs;
+    p.tpt = kDtRows / 2 / d.hs;
+    d.tt = 2 * p.tpt;
+    d.SQ = d.Hkv * d.hgroups;
+    d.bt = kDtPages;
+    d.grid = sms;
+    p.c2 = d.sm_scale * kLog2e;
+    if (d.cap > 0.f) {
+        p.cap2 = d.cap * kLog2e;
+        p.y1 = static_cast<float>(fmin(static_cast<double>(d.sm_scale) / d.cap, 1e30));
+    }
+    // A tile whose rows are done one by one takes its warps about 4 us per key: 64 polls or so, beyond the usual limit.
+    const int64_t keys = (static_cast<int64_t>(d.part[0].num_pages) + d.part[1].num_pages) * kPage, polls = static_cast<int64_t>(kWaitLimit) + 64 * keys;
+    p.wait_limit = static_cast<uint32_t>(polls < (1ll << 31) ? polls : 1ll << 31);
+    CUtensorMap maps[5];
+    spd_status rc;
+    if ((rc = make_q_map(&maps[0], d, D, p.tpt)) != SPD_OK) return rc;
+    for (int x = 0; x < 2; ++x) {
+        if (d.part[x].num_pages > 0) {
+            if ((rc = make_pool_map(&maps[1 + 2 * x], d, d.k_pool[x], d.part[x].num_pages, D)) != SPD_OK) return rc;
+            if ((rc = make_pool_map(&maps[2 + 2 * x], d, d.v_pool[x], d.part[x].num_pages, D)) != SPD_OK) return rc;
+        } else {
+            maps[1 + 2 * x] = maps[2 + 2 * x] = maps[0];   // never loaded from
+        }
+    }
+    const bool cap = d.cap > 0.f, bias = d.slopes != nullptr;
+#define SPD_DT_CASE(DD, CC, BB) if (D == DD && cap == CC && bias == BB) return launch_tc<DD, CC, BB>(p, maps, st);
+    SPD_DT_CASE(128, false, false) SPD_DT_CASE(128, true, false) SPD_DT_CASE(128, false, true) SPD_DT_CASE(128, true, true)
+    SPD_DT_CASE(64, false, false) SPD_DT_CASE(64, true, false) SPD_DT_CASE(64, false, true) SPD_DT_CASE(64, true, true)
+#undef SPD_DT_CASE
+    return SPD_ERR_UNSUPPORTED;
+}
+
 template <typename E, int D, int RT>
 spd_status launch_fma(DraftedParams p, int sms, cudaStream_t st) {
     using C = DraftedFma<D, RT>;
@@ -62,6 +147,7 @@ spd_status launch_fma(DraftedParams p, int sms, cudaStream_t st) {
     p.hgroups = p.g / p.hs;
     p.tt = RT / p.hs;
     p.SQ = p.Hkv * p.hgroups;
+    p.bt = kDrTiles;
     p.grid = kFmaPerSm * sms;
     drafted_fma_kernel<E, D, RT><<<p.grid, C::kThreads, C::smem_bytes(), st>>>(p);
     host::count_launch();
@@ -144,7 +230,7 @@ spd_status run(const spd_shape *shape, const spd_score *score, const spd_drafts 
     p.records = reinterpret_cast<int4 *>(w + L.records);
     p.scratch = reinterpret_cast<float *>(w + L.scratch);
     cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
-    return s.dtype == SPD_BF16 ? run_fma<__nv_bfloat16>(p, s.head_dim, sms, st) : run_fma<float>(p, s.head_dim, sms, st);
+    return s.dtype == SPD_BF16 ? run_tc(p, s.head_dim, sms, st) : run_fma<float>(p, s.head_dim, sms, st);
 }
 
 }  // namespace

@@ -15,8 +15,6 @@
 
 namespace spd {
 
-constexpr int kDrBlock = 64;              // keys per block: four page tiles
-constexpr int kDrTiles = kDrBlock / kPage;
 constexpr int kDrTree = 256;              // most drafted tokens of a user that come as a tree
 constexpr int kDrWords = kDrTree / 32;
 constexpr int kDrMinBlocks = 2;           // do not cut the work into shares of fewer blocks
@@ -26,6 +24,7 @@ struct DraftedParams {
     int32_t hs, hgroups;                  // query heads that a tile takes of a token, and how many such groups a KV head has
     int32_t tt;                           // tokens per tile
     int32_t SQ;                           // Hkv * hgroups
+    int32_t bt;                           // page tiles per block
     int64_t T;
     float sm_scale;
     const void *q;                        // [T][Hq][D]
@@ -97,7 +96,7 @@ __device__ __forceinline__ void drafted_user(const DraftedParams &p, int u, Draf
     s.nt = s.np + (p.part[1].present && good ? (s.lq + kPage - 1) / kPage : 0);
 }
 
-// Keys of a tile of rows: page tiles [0, ns) and [a, e) of the user's, ceil((ns + e - a) / 4) blocks (at least one, so that rows that
+// Keys of a tile of rows: page tiles [0, ns) and [a, e) of the user's, ceil((ns + e - a) / bt) blocks (at least one, so that rows that
 // see nothing are written too).
 struct DraftedKeys { int ns, a, e, nb; };
 __device__ __forceinline__ DraftedKeys drafted_keys(const DraftedParams &p, const DraftedUser &s, int i0, int i1) {
@@ -113,7 +112,7 @@ __device__ __forceinline__ DraftedKeys drafted_keys(const DraftedParams &p, cons
     const int64_t se = min(static_cast<int64_t>(p.sinks), hi);
     k.ns = p.window > 0 && se > P0 && lo > P0 ? upto(se - 1) : 0;
     if (k.ns >= k.a) { k.a = 0; k.ns = 0; }
-    k.nb = max(1, (k.ns + k.e - k.a + kDrTiles - 1) / kDrTiles);
+    k.nb = max(1, (k.ns + k.e - k.a + p.bt - 1) / p.bt);
     return k;
 }
 

@@ -9,6 +9,9 @@
 
 namespace spd {
 
+constexpr int kDrBlock = 64;              // keys per block
+constexpr int kDrTiles = kDrBlock / kPage;
+
 template <int D, int RT>
 struct DraftedFma {
     static constexpr int kThreads = RT * 4, kPitch = D + 4;       // rows of Q, K and V: 16-byte reads of 8 lanes fall in 32 banks

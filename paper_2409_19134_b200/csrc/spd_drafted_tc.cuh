@@ -1,0 +1,660 @@
+// Drafted tokens on the fifth-generation tensor cores (bf16).
+//
+// One CTA per SM works through its share of blocks (spd_drafted.cuh).  An item has up to two 128-row tiles over shared K/V blocks of 80 keys = five
+// pages, each page a pair of TMA boxes per operand.  Per tile and block:
+//     S = Q K^T     128 x 80 x D, fp32 in TMEM;   softmax: one row per thread, S into registers, options, mask, exponentials, P as bf16 pairs into
+//     TMEM columns of its own, so that the next S is computed under the exponentials;   O += P V     128 x D x 80, P read from TMEM.
+// 8 softmax warps, one warp per tile that issues its MMAs, one that loads, one that plans the next item (and walks its tree) while this one
+// runs, four that guard V.  Everything is handed over through mbarriers with bounded waits; a wait that runs out ends the CTA with
+// SPD_ERR_TIMEOUT once all its threads have come to the common end.
+//
+// Masks: a row sees one or two intervals of the context (window, sinks) and a set of drafted tokens (bits per token).  A warp builds them,
+// 16 bits per page, only in blocks that some of its rows do not see whole.  A hidden key's weight is 0, but 0 * NaN is NaN: the guards look
+// through the V rows of such blocks, clear slots that hold no token and rows that nobody sees, and where a row that is not finite is hidden from
+// some rows and visible to others, the rows of the piece are done again one by one.  So are rows whose weighted sums left fp32's range
+// (weights are relative to a reference that may lag 2^8 behind the maximum).
+#pragma once
+
+#include "spd_drafted.cuh"
+#include "spd_prefill_scored_tc.cuh"
+
+namespace spd {
+
+constexpr int kDtThreads = 512;
+constexpr int kDtConsumers = 15;                    // warps that read a plan
+constexpr int kDtRows = 256;                        // rows of an item: two tiles
+constexpr int kDtPages = kStKeys / kPage;           // page tiles per block
+constexpr int kDtPageBox = kPage * 128;             // one swizzled box: 16 rows x 64 channels
+
+struct DrPlan {
+    int32_t valid;                                   // 0: the share is done
+    int32_t u, first, i0, toks, h0, kvh;             // user; first token of q, of the tile; tokens; first head; KV head
+    int32_t tiles;                                   // tiles with rows
+    int32_t b0, b1, whole, slot;                     // blocks of the piece; whether it is the whole item; else where it goes
+    int32_t deepest;                                 // greatest depth of the tree (0 for runs)
+    int32_t bad, poisoned;
+    DraftedUser s;
+    DraftedKeys k;
+    int16_t parent[kDrTree], depth[kDrTree];         // of all the user's drafted tokens
+    uint32_t line[kDrTree][kDrWords];                // of the item's tokens
+};
+constexpr int kDtBarBytes = 320;
+constexpr size_t dt_smem_bytes(int D) {
+    return 2 * static_cast<size_t>(st_qtile(D)) + 2 * st_slots(D) * static_cast<size_t>(st_tile(D)) + kDtBarBytes + 2 * sizeof(DrPlan);
+}
+static_assert(dt_smem_bytes(128) + 1024 <= 232448, "shared memory of an SM");
+
+struct DraftedTcParams {
+    DraftedParams d;
+    int32_t tpt;                // tokens per tile
+    float c2;                   // sm_scale log2(e)
+    float cap2, y1;             // cap log2(e); sm_scale / cap
+    uint32_t wait_limit;
+};
+
+__device__ __forceinline__ uint32_t dt_low(int n) { return (1u << min(max(n, 0), 16)) - 1u; }       // bits 0 .. n - 1 of 16
+
+template <int K>
+__device__ __forceinline__ uint64_t dt_tanh() {                 // coefficient K of tanh(y) / y for |y| <= 1, in both halves
+    constexpr float f = static_cast<float>(kTanhOne[K]);
+    return pack_f32x2(f, f);
+}
+
+// First position and tokens of page tile v of an item's list.
+__device__ __forceinline__ int2 dt_tile(const DrPlan &pl, int v) {
+    if (v >= pl.k.ns + pl.k.e - pl.k.a) return make_int2(0, 0);
+    const int x = v < pl.k.ns ? v : pl.k.a + v - pl.k.ns;
+    if (x < pl.s.np) return make_int2(x * kPage, min(kPage, pl.s.lp - x * kPage));
+    const int y = (x - pl.s.np) * kPage;
+    return make_int2(pl.s.lp + y, min(kPage, pl.s.lq - y));
+}
+
+// Which of the 16 keys of a page tile a row sees: token `it` of the item at position pos.
+__device__ __forceinline__ uint32_t dt_sees(const DraftedParams &p, const DrPlan &pl, int2 tile, int it, int pos) {
+    const bool tree = p.parents != nullptr;
+    const int base = tile.x, cnt = tile.y;
+    uint32_t m = dt_low(min(cnt, (tree ? pl.s.ctx : pos + 1) - base));
+    if (p.window > 0) m &= ~dt_low(max(pos - p.window, -1) + 1 - base) | dt_low(p.sinks - base);
+    if (tree && base + cnt > pl.s.ctx) {
+        const int off = base - pl.s.ctx;
+        const uint32_t *w = pl.line[it];
+        uint32_t d;
+        if (off < 0) d = w[0] << -off;
+        else d = (off & 31) == 0 ? w[off >> 5] : __funnelshift_r(w[off >> 5], (off >> 5) + 1 < kDrWords ? w[(off >> 5) + 1] : 0u, off & 31);
+        m |= d & dt_low(cnt);
+    }
+    return m;
+}
+
+// One row of a piece the slow way, by a whole warp: 32 keys at a time, a score per lane, then four channels of O per lane.  Keys that the row
+// does not see are not touched.
+template <int D>
+__device__ __noinline__ void dt_slow_row(const DraftedTcParams &q, const DrPlan &pl, int it, int hh, int lane) {
+    const DraftedParams &p = q.d;
+    const int pos = pl.s.ctx + (p.parents ? pl.depth[pl.i0 + it] : pl.i0 + it), h = pl.h0 + hh;
+    const int64_t row = (static_cast<int64_t>(pl.first) + pl.i0 + it) * p.Hq + h;
+    const __nv_bfloat16 *qr = static_cast<const __nv_bfloat16 *>(p.q) + row * D;
+    const float slope = p.slopes ? p.slopes[h] : 0.f;
+    float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+    float m = -INFINITY, l = 0.f;
+    const int v1 = min(pl.b1 * kDtPages, pl.k.ns + pl.k.e - pl.k.a);
+    for (int v0 = pl.b0 * kDtPages; v0 < v1; v0 += 2) {
+        const int v = v0 + (lane >> 4), slot = lane & 15;
+        const int2 t = v < v1 ? dt_tile(pl, v) : make_int2(0, 0);
+        const bool see = v < v1 && ((dt_sees(p, pl, t, it, pos) >> slot) & 1u);
+        int64_t at = 0;
+        int part = 0;
+        float s = -INFINITY;
+        if (see) {
+            const DraftedTile d = drafted_tile(p, pl.s, pl.k, v);
+            part = d.part;
+            at = ((static_cast<int64_t>(p.part[part].indices[d.entry]) * p.Hkv + pl.kvh) * kPage + slot) * D;
+            const __nv_bfloat16 *k = static_cast<const __nv_bfloat16 *>(p.k_pool[part]) + at;
+            s = 0.f;
+#pragma unroll 4
+            for (int c = 0; c < D; c += 4) {
+                const float4 a = drafted_load4(qr + c), b = drafted_load4(k + c);
+                s = fmaf(a.x, b.x, s); s = fmaf(a.y, b.y, s); s = fmaf(a.z, b.z, s); s = fmaf(a.w, b.w, s);
+            }
+            s *= p.sm_scale;
+            if (p.cap > 0.f) s = p.cap * tanhf(s / p.cap);
+            const int far = p.parents && t.x + slot >= pl.s.ctx ? pos - pl.s.ctx - pl.depth[t.x + slot - pl.s.ctx] : pos - (t.x + slot);
+            if (p.slopes) s = fmaf(-slope, static_cast<float>(far), s);
+        }
+        float mx = s;
+#pragma unroll
+        for (int d = 16; d >= 1; d >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, d));
+        const float mn = fmaxf(m, mx), ref = mn == -INFINITY ? 0.f : mn;
+        const float alpha = m == -INFINITY ? 1.f : expf(m - ref), w = see ? expf(s - ref) : 0.f;
+        float sum = w;
+#pragma unroll
+        for (int d = 16; d >= 1; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
+        l = l * alpha + sum;
+        m = mn;
+        o.x *= alpha; o.y *= alpha; o.z *= alpha; o.w *= alpha;
+        const uint32_t seen = __ballot_sync(0xffffffffu, see);
+        for (uint32_t left = seen; left != 0; left &= left - 1) {
+            const int x = __ffs(left) - 1;
+            const float wt = __shfl_sync(0xffffffffu, w, x);
+            const int64_t a = __shfl_sync(0xffffffffu, at, x);
+            const int pt = __shfl_sync(0xffffffffu, part, x);
+            if (lane < D / 4) {
+                const float4 b = drafted_load4(static_cast<const __nv_bfloat16 *>(p.v_pool[pt]) + a + 4 * lane);
+                o.x = fmaf(wt, b.x, o.x); o.y = fmaf(wt, b.y, o.y); o.z = fmaf(wt, b.z, o.z); o.w = fmaf(wt, b.w, o.w);
+            }
+        }
+    }
+    if (pl.whole) {
+        if (lane < D / 4) drafted_store4<D>(p, row, lane, o, m, l, false);
+    } else {
+        float *dst = p.scratch + static_cast<size_t>(pl.slot) * drafted_slot_floats(D, kDtRows);
+        const int r = it * p.hs + hh;
+        if (lane < D / 4) reinterpret_cast<float4 *>(dst)[lane * kDtRows + r] = o;
+        if (lane == 0) { dst[kDtRows * D + r] = m * kLog2e; dst[kDtRows * (D + 1) + r] = l; }
+    }
+}
+
+template <int D, bool CAP, bool BIAS>
+__global__ void __launch_bounds__(kDtThreads, 1)
+drafted_tc_kernel(const __grid_constant__ DraftedTcParams q, const __grid_constant__ CUtensorMap mq, const __grid_constant__ CUtensorMap mk0,
+                  const __grid_constant__ CUtensorMap mv0, const __grid_constant__ CUtensorMap mk1, const __grid_constant__ CUtensorMap mv1) {
+    constexpr int QTILE = st_qtile(D), TILE = st_tile(D), NS = st_slots(D), BOXES = D / 64, KB = kStKeys;
+    const DraftedParams &p = q.d;
+    extern __shared__ __align__(1024) uint8_t base[];
+    const uint32_t Qs = smem_u32(base), Ks = Qs + 2 * QTILE, Vs = Ks + NS * TILE;
+    uint64_t *bars = reinterpret_cast<uint64_t *>(base + 2 * QTILE + 2 * NS * TILE);
+    uint64_t *bar_q = bars, *bar_qfree = bars + 1;                 // Q loaded; Q read by both tiles
+    uint64_t *bar_s = bars + 2, *bar_sf = bars + 4;                // per tile: S ready; S in registers
+    uint64_t *bar_p = bars + 6, *bar_o = bars + 8;                 // per tile: P written; O has taken the block in (P is free)
+    uint64_t *bar_plan = bars + 10, *bar_planfree = bars + 12;     // per plan buffer
+    uint64_t *bar_k = bars + 14, *bar_v = bar_k + NS, *bar_kfree = bar_v + NS, *bar_vfree = bar_kfree + NS;
+    uint64_t *bar_guard = bar_vfree + NS;                          // per V slot: the guards are done with the block
+    constexpr int NBARS = 14 + 5 * NS;
+    static_assert(NBARS * 8 + 8 <= kDtBarBytes, "barrier block");
+    uint32_t &tmem_slot = *reinterpret_cast<uint32_t *>(bars + NBARS);
+    int &first_bad = *reinterpret_cast<int *>(&tmem_slot + 1);
+    DrPlan *plans = reinterpret_cast<DrPlan *>(base + 2 * QTILE + 2 * NS * TILE + kDtBarBytes);
+    const int tid = threadIdx.x, wid = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31;
+
+    // ---- the cut: sums over the users in what becomes the K ring, the share's first item by the planning warp
+    int64_t *sums = reinterpret_cast<int64_t *>(base + 2 * QTILE);
+    int Cu, chunks;
+    const int64_t W = drafted_sums<kDtThreads>(p, sums, &first_bad, Cu, chunks);
+    if (blockIdx.x == 0 && tid == 0) drafted_header(p, first_bad);
+    if (tid < 4) p.records[4 * blockIdx.x + tid] = make_int4(0, 0, 0, 0);
+    const int shares = static_cast<int>(min(static_cast<int64_t>(p.grid), (W + kDrMinBlocks - 1) / kDrMinBlocks));
+    if (static_cast<int>(blockIdx.x) >= shares) return;
+    const int64_t x1 = drafted_bound(W, shares, blockIdx.x + 1);
+    int64_t x = drafted_bound(W, shares, blockIdx.x);
+    DraftedWalk w;
+    if (wid == 12) drafted_locate(p, sums, Cu, chunks, x, lane, w);
+    if (tid == 320) {
+        prefetch_tensormap(&mq); prefetch_tensormap(&mk0); prefetch_tensormap(&mv0); prefetch_tensormap(&mk1); prefetch_tensormap(&mv1);
+        for (int b = 0; b < NBARS; ++b) {
+            // Q and ring slots free: one per tile; S in registers, P written: one per softmax warp of the tile;
+            // V looked through: one per guard; plan read: one per warp
+            const int n = b == 1 || (b >= 14 + 2 * NS && b < 14 + 4 * NS) ? 2 : ((b >= 4 && b < 8) || b >= 14 + 4 * NS) ? 4 : (b >= 12 && b < 14) ? kDtConsumers : 1;
+            mbar_init(smem_u32(&bars[b]), n);
+        }
+        fence_mbar_init();
+    }
+    if (wid == 8) {       // one warp allocates all of tensor memory for the CTA (it has the SM to itself)
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tmem_slot)), "r"(kStTmemCols) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    }
+    fence_proxy_async();  // the sums were written where TMA and tensor core will work
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = __shfl_sync(0xffffffffu, tmem_slot, 0);
+
+    bool ok = true;       // cleared by a wait that runs out; the warp then leaves its loops and comes to the common end
+    auto wait = [&](uint64_t *bar, uint32_t parity) { if (ok) ok = __all_sync(0xffffffffu, st_mbar_wait(smem_u32(bar), parity & 1, q.wait_limit)); };
+    auto plan_of = [&](int r) -> DrPlan & { wait(&bar_plan[r & 1], r >> 1); __syncwarp(); return plans[r & 1]; };
+    auto plan_done = [&](int r) { __syncwarp(); if (lane == 0) mbar_arrive(smem_u32(&bar_planfree[r & 1])); };
+
+    // the launch's 512 x 128 registers, shared out by warpgroup: 256 x 192 + 256 x 64 = 65536
+    if (wid < 8) {
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 192;");
+        // ---------------- softmax warps: one row per thread; n counts the tile's blocks
+        const int t = wid >> 2, rr = tid & 127, in_tile = rr / p.hs, hh = rr - in_tile * p.hs, it = t * q.tpt + in_tile;
+        const int w0 = t * q.tpt + ((rr & ~31) / p.hs), w1 = t * q.tpt + min(q.tpt - 1, (rr | 31) / p.hs);       // the warp's tokens
+        const bool tree = p.parents != nullptr;
+        const uint32_t lanes = static_cast<uint32_t>((wid & 3) * 32) << 16;
+        const uint32_t t_s = tmem + lanes + (t ? kStS1 : kStS0), t_p = tmem + lanes + (t ? kStP1 : kStP0);
+        const uint32_t t_o = tmem + lanes + (t ? kStO1 : kStO0);
+        int n = 0;
+        for (int r = 0; ok; ++r) {
+            DrPlan &pl = plan_of(r);
+            if (!ok || !pl.valid) break;
+            const int nblk = t < pl.tiles ? pl.b1 - pl.b0 : 0, toks = pl.toks, ctx = pl.s.ctx, i0 = pl.i0;
+            const bool mine = (rr & ~31) / p.hs < q.tpt && w0 < toks, live = in_tile < q.tpt && it < toks;      // of the warp, of the thread
+            const int tok = live ? it : 0;
+            const int pos = ctx + (!tree ? i0 + tok : pl.s.good ? pl.depth[i0 + tok] : 0);      // no tree where the user is refused
+            // what every row of the warp sees: whole tiles of context in [full_lo, full_hi], or in front of the sinks' end
+            const int full_hi = tree ? ctx - 1 : ctx + i0 + w0;
+            const int full_lo = p.window > 0 ? ctx + (tree ? pl.deepest : i0 + min(w1, toks - 1)) - p.window + 1 : 0;
+            const int last_pos = tree ? 0x7fffffff : ctx + i0 + min(w1, toks - 1);
+            const float slope2 = BIAS ? p.slopes[pl.h0 + hh] * kLog2e : 0.f;
+            float l = 0.f, m = -INFINITY, top = -INFINITY;          // reference point and greatest score, log2 units
+            for (int i = 0; i < nblk && ok; ++i) {
+                const int v = (pl.b1 - 1 - i) * kDtPages;
+                int2 tl[kDtPages];
+                bool whole = true, none = true;
+#pragma unroll
+                for (int y = 0; y < kDtPages; ++y) {
+                    tl[y] = dt_tile(pl, v + y);
+                    const int e = tl[y].x + kPage - 1;
+                    whole = whole && tl[y].y == kPage && e <= full_hi && (tl[y].x >= full_lo || e < p.sinks);
+                    none = none && (tl[y].y == 0 || tl[y].x > last_pos);
+                }
+                none = none || !mine;
+                wait(&bar_s[t], n + i);
+                __syncwarp();
+                tc_fence_after();
+                if (none) {                                   // nobody in this warp sees any of it: weights 0
+                    if (lane == 0) mbar_arrive(smem_u32(&bar_sf[t]));
+                    if (n + i > 0) wait(&bar_o[t], n + i - 1);
+                    tc_fence_after();
+                    uint32_t z[32];
+#pragma unroll
+                    for (int y = 0; y < 32; ++y) z[y] = 0u;
+                    tmem_st32p(t_p, z);
+                    tmem_st8(t_p + 32, z);
+                    tmem_wait_st();
+                    tc_fence_before();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(smem_u32(&bar_p[t]));
+                    continue;
+                }
+                uint32_t raw[KB];
+                tmem_ld64_nowait(t_s, raw);
+                tmem_ld16_nowait(t_s + 64, raw + 64);
+                tmem_wait_ld();
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(smem_u32(&bar_sf[t]));       // the next block's S may be computed
+                float sv[KB];
+#pragma unroll
+                for (int y = 0; y < KB; ++y) sv[y] = __uint_as_float(raw[y]);
+                uint32_t see[3] = {0xffffffffu, 0xffffffffu, 0xffffu};
+                if (!whole) {
+                    uint32_t m16[kDtPages];
+#pragma unroll
+                    for (int y = 0; y < kDtPages; ++y) m16[y] = live ? dt_sees(p, pl, tl[y], it, pos) : 0u;
+                    see[0] = m16[0] | m16[1] << 16; see[1] = m16[2] | m16[3] << 16; see[2] = m16[4];
+                }
+                auto seen = [&](int y) { return (see[y >> 5] >> (y & 31)) & 1u; };
+                constexpr bool kLog2 = CAP || BIAS;             // sv holds scores in log2 units from here on; q.k else
+                if constexpr (CAP) {
+                    // tanh by a polynomial where the whole warp's scores allow it (error 2.4e-7), else by the special-function unit
+                    float big[4] = {0.f, 0.f, 0.f, 0.f};
+                    if (!whole) {                               // hidden scores may be anything
+#pragma unroll
+                        for (int y = 0; y < KB; ++y) sv[y] = seen(y) ? sv[y] : 0.f;
+                    }
+#pragma unroll
+                    for (int y = 0; y < KB; y += 2) big[(y >> 1) & 3] = fmax3_abs_nan(big[(y >> 1) & 3], sv[y], sv[y + 1]);
+                    const float most = fmax3_abs_nan(fmax3_abs_nan(big[0], big[1], big[2]), big[3], 0.f) * q.y1;
+                    if (__all_sync(0xffffffffu, most <= 1.f)) {
+                        const uint64_t y12 = pack_f32x2(q.y1, q.y1), cap22 = pack_f32x2(q.cap2, q.cap2);
+#pragma unroll
+                        for (int y = 0; y < KB; y += 2) {
+                            const uint64_t a = mul_f32x2(pack_f32x2(sv[y], sv[y + 1]), y12), a2 = mul_f32x2(a, a);
+                            uint64_t f = fma_f32x2(a2, dt_tanh<5>(), dt_tanh<4>());
+                            f = fma_f32x2(f, a2, dt_tanh<3>());
+                            f = fma_f32x2(f, a2, dt_tanh<2>());
+                            f = fma_f32x2(f, a2, dt_tanh<1>());
+                            f = fma_f32x2(f, a2, dt_tanh<0>());
+                            unpack_f32x2(mul_f32x2(mul_f32x2(f, a), cap22), sv[y], sv[y + 1]);
+                        }
+                    } else {
+#pragma unroll
+                        for (int y = 0; y < KB; ++y) sv[y] = q.cap2 - __fdividef(2.f * q.cap2, ex2_approx(sv[y] * (2.f * kLog2e) * q.y1) + 1.f);
+                    }
+                }
+                if constexpr (BIAS) {
+                    const float scale = CAP ? 1.f : q.c2;
+#pragma unroll
+                    for (int y = 0; y < kDtPages; ++y) {
+                        const float off = static_cast<float>(tl[y].x - pos);
+                        if (tree && tl[y].x + tl[y].y > ctx) {          // drafted tokens count by depth
+#pragma unroll
+                            for (int z = 0; z < kPage; ++z) {
+                                const int d = tl[y].x + z - ctx;
+                                const float far = d >= 0 ? static_cast<float>(ctx - pos + pl.depth[min(d, kDrTree - 1)]) : off + static_cast<float>(z);
+                                sv[16 * y + z] = fmaf(slope2, far, sv[16 * y + z] * scale);
+                            }
+                        } else {
+#pragma unroll
+                            for (int z = 0; z < kPage; ++z) sv[16 * y + z] = fmaf(slope2, off + static_cast<float>(z), sv[16 * y + z] * scale);
+                        }
+                    }
+                }
+                if (!whole) {
+#pragma unroll
+                    for (int y = 0; y < KB; ++y) sv[y] = seen(y) ? sv[y] : -INFINITY;
+                }
+                // ---- the reference is the greatest score so far, or less by up to kPfSlack, so that O is hardly ever rescaled
+                bool o_ready = n + i == 0;                       // O has taken the block before in
+                float r4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+                for (int y = 0; y < KB; y += 2) r4[(y >> 1) & 3] = fmax3(r4[(y >> 1) & 3], sv[y], sv[y + 1]);
+                const float mx = fmaxf(fmaxf(r4[0], r4[1]), fmaxf(r4[2], r4[3])), xmax = kLog2 ? mx : mx * q.c2;
+                top = fmaxf(top, xmax);
+                if (__any_sync(0xffffffffu, xmax > m + kPfSlack)) {
+                    const float m_new = (xmax > m + kPfSlack) ? xmax : m;
+                    const float alpha = m == -INFINITY ? 1.f : ex2_approx(m - m_new);
+                    l *= alpha;
+                    m = m_new;
+                    if (i > 0 && !__all_sync(0xffffffffu, alpha == 1.f)) {
+                        wait(&bar_o[t], n + i - 1);
+                        o_ready = true;
+                        tc_fence_after();
+#pragma unroll 1
+                        for (int c = 0; c < D / 32; ++c) {
+                            float ov[32];
+                            tmem_ld32(t_o + c * 32, ov);
+#pragma unroll
+                            for (int y = 0; y < 32; ++y) ov[y] *= alpha;
+                            tmem_st32(t_o + c * 32, ov);
+                        }
+                    }
+                }
+                const float ref = m == -INFINITY ? 0.f : m;
+                const uint64_t mx2 = pack_f32x2(-ref, -ref), c22 = pack_f32x2(q.c2, q.c2);
+                // ---- weights 2^(score - reference), P, and their sum as they are rounded for the product with V: numerator and sum are off alike
+                uint64_t lsum2 = 0;                              // (+0, +0)
+                uint32_t pk[KB / 2];
+#pragma unroll
+                for (int y = 0; y < KB / 2; ++y) {
+                    float a0, a1;
+                    const uint64_t s2 = pack_f32x2(sv[2 * y], sv[2 * y + 1]);
+                    unpack_f32x2(kLog2 ? add_f32x2(s2, mx2) : fma_f32x2(s2, c22, mx2), a0, a1);
+                    pk[y] = pack_bf16(ex2_approx(a0), ex2_approx(a1));
+                    lsum2 = add_f32x2(lsum2, pack_f32x2(__uint_as_float(pk[y] << 16), __uint_as_float(pk[y] & 0xffff0000u)));
+                }
+                if (!o_ready) wait(&bar_o[t], n + i - 1);        // P of the block before has been read
+                tc_fence_after();
+                tmem_st32p(t_p, pk);
+                tmem_st8(t_p + 32, pk + 32);
+                tmem_wait_st();
+                tc_fence_before();
+                __syncwarp();                                    // one arrival per warp
+                if (lane == 0) mbar_arrive(smem_u32(&bar_p[t]));
+                float s0, s1;
+                unpack_f32x2(lsum2, s0, s1);
+                l += s0 + s1;
+            }
+            n += nblk;
+            if (nblk > 0) wait(&bar_o[t], n - 1);
+            __syncwarp();
+            tc_fence_after();
+            if (ok && nblk > 0 && mine) {
+                const bool poisoned = *const_cast<volatile int32_t *>(&pl.poisoned) != 0, bad = *const_cast<volatile int32_t *>(&pl.bad) != 0;
+                const int64_t row = (static_cast<int64_t>(pl.first) + i0 + tok) * p.Hq + pl.h0 + hh;
+                const float back = m == -INFINITY ? 1.f : ex2_approx(m - top);       // from the reference to the maximum
+                const float ls = l * back, mn = top * 0.69314718055994531f;
+                float *dst = p.scratch + static_cast<size_t>(pl.slot) * drafted_slot_floats(D, kDtRows);
+                const int slot_row = it * p.hs + hh;
+                bool over = false;
+                if (!poisoned || bad) {
+                    float big = 0.f;
+#pragma unroll 1
+                    for (int c = 0; c < D; c += 32) {
+                        float ov[32];
+                        tmem_ld32(t_o + c, ov);
+                        if (live) {
+#pragma unroll
+                            for (int y = 0; y < 32; y += 4) {
+                                big = fmax3_abs_nan(fmax3_abs_nan(big, ov[y], ov[y + 1]), ov[y + 2], ov[y + 3]);
+                                const float4 o4 = make_float4(ov[y] * back, ov[y + 1] * back, ov[y + 2] * back, ov[y + 3] * back);
+                                if (pl.whole) drafted_store4<D>(p, row, (c + y) / 4, o4, mn, ls, bad);
+                                else reinterpret_cast<float4 *>(dst)[(c + y) / 4 * kDtRows + slot_row] = o4;
+                            }
+                        }
+                        __syncwarp();
+                    }
+                    if (live && !pl.whole) { dst[kDtRows * D + slot_row] = top; dst[kDtRows * (D + 1) + slot_row] = ls; }
+                    over = live && !bad && l > 0.f && l < INFINITY && !(big < INFINITY);
+                }
+                uint32_t again = __ballot_sync(0xffffffffu, poisoned && !bad ? live : over);
+                for (; again != 0; again &= again - 1) {
+                    const int src = __ffs(again) - 1;
+                    dt_slow_row<D>(q, pl, __shfl_sync(0xffffffffu, it, src), __shfl_sync(0xffffffffu, hh, src), lane);
+                }
+                if (bad && lane == 0 && (wid & 3) == 0) drafted_flag(p, pl.u);
+            }
+            tc_fence_before();                               // O is read: ordered before this warp's next arrival
+            plan_done(r);
+        }
+    } else {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
+    if (wid == 12) {
+        // ---------------- the planning warp
+        for (int r = 0;; ++r) {
+            DrPlan &pl = plans[r & 1];
+            if (r >= 2) wait(&bar_planfree[r & 1], (r >> 1) - 1);
+            __syncwarp();
+            if (!ok || x >= x1) {
+                if (lane == 0) { pl.valid = 0; mbar_arrive(smem_u32(&bar_plan[r & 1])); }
+                break;
+            }
+            if (r > 0) drafted_next(p, w);
+            const int b0 = static_cast<int>(x - w.x0), b1 = static_cast<int>(min(static_cast<int64_t>(w.k.nb), x1 - w.x0));
+            const int i0 = w.rt * p.tt, toks = min(p.tt, w.s.n - i0), kvh = w.sq / p.hgroups;
+            const bool whole = b0 == 0 && b1 == w.k.nb;
+            const int slot = 2 * blockIdx.x + (b0 == 0 ? 1 : 0);
+            bool wrong = false;
+            int deepest = 0;
+            if (p.parents != nullptr && w.s.good) {
+                for (int i = lane; i < w.s.n; i += 32) {
+                    const int up = p.parents[w.s.first + i];
+                    const bool off = up < -1 || up >= i;
+                    wrong = wrong || off;
+                    pl.parent[i] = static_cast<int16_t>(off ? -1 : up);
+                }
+                wrong = __any_sync(0xffffffffu, wrong);
+                __syncwarp();
+                for (int i = lane; i < w.s.n; i += 32) {
+                    const int d = drafted_depth(pl.parent, i);
+                    pl.depth[i] = static_cast<int16_t>(d);
+                    deepest = max(deepest, d);
+                    if (i >= i0 && i < i0 + toks) drafted_line(p, w.s, pl.parent, i, d, pl.line[i - i0]);
+                }
+                deepest = __reduce_max_sync(0xffffffffu, deepest);
+            } else if (p.parents != nullptr) {              // no keys: depths are looked at all the same
+                for (int i = lane; i < min(w.s.n, kDrTree); i += 32) pl.depth[i] = 0;
+            }
+            if (lane == 0) {
+                pl.valid = 1; pl.u = w.u; pl.first = w.s.first; pl.i0 = i0; pl.toks = toks; pl.kvh = kvh;
+                pl.h0 = kvh * p.g + w.sq % p.hgroups * p.hs;
+                pl.tiles = toks > q.tpt ? 2 : 1;
+                pl.b0 = b0; pl.b1 = b1; pl.whole = whole; pl.slot = slot; pl.deepest = deepest;
+                pl.bad = !w.s.good || wrong; pl.poisoned = 0;
+                pl.s = w.s; pl.k = w.k;
+                if (!whole) drafted_record(p, w, slot, W, shares);
+            }
+            __syncwarp();
+            if (lane == 0) mbar_arrive(smem_u32(&bar_plan[r & 1]));
+            x = w.x0 + b1;
+        }
+    } else if (wid == 10) {
+        // ---------------- the loading warp; c counts blocks over all items
+        const uint64_t once = l2_evict_first_policy();
+        uint64_t often;
+        asm volatile("createpolicy.fractional.L2::evict_normal.b64 %0, 1.0;" : "=l"(often));
+        int c = 0, nq = 0;
+        for (int r = 0; ok; ++r) {
+            DrPlan &pl = plan_of(r);
+            if (!ok || !pl.valid) break;
+            if (nq > 0) wait(bar_qfree, nq - 1);
+            if (ok && lane == 0) {
+                const int rows = p.hs * q.tpt;
+                mbar_expect_tx(smem_u32(bar_q), pl.tiles * BOXES * rows * 128);
+                for (int t = 0; t < pl.tiles; ++t)
+                    for (int y = 0; y < BOXES; ++y)
+                        tma_load_3d(Qs + t * QTILE + y * kStQBox, &mq, 64 * y, pl.h0, pl.first + pl.i0 + t * q.tpt, smem_u32(bar_q));
+            }
+            if (ok) ++nq;
+            const uint64_t policy = pl.s.n > p.tt ? often : once;      // other items read these keys too
+            const int list = pl.k.ns + pl.k.e - pl.k.a;
+            const int v1 = min(pl.b1 * kDtPages, list);
+            int page = -1, part = 0, have = v1;                 // lane k holds the page of tile have + k; tiles are worked through downwards
+            for (int i = 0, b = pl.b1 - 1; b >= pl.b0 && ok; --b, ++i, ++c) {
+                const int v0 = b * kDtPages, slot = c % NS, use = c / NS;
+                if (v0 < have) {                                // 30 tiles at a time: six blocks
+                    have = max(pl.b0 * kDtPages, v0 - 5 * kDtPages);
+                    page = -1;
+                    if (lane < 6 * kDtPages && have + lane < v1) {
+                        const DraftedTile d = drafted_tile(p, pl.s, pl.k, have + lane);
+                        part = d.part;
+                        page = p.part[part].indices[d.entry];
+                        if (page < 0 || page >= p.part[part].num_pages) { page = -1; pl.bad = 1; }
+                    }
+                }
+                // lanes 0 .. 9 load: tile lane / 2, box lane % 2
+                const int y = lane / BOXES, my_page = __shfl_sync(0xffffffffu, page, min(31, v0 - have + min(y, kDtPages - 1)));
+                const int my_part = __shfl_sync(0xffffffffu, part, min(31, v0 - have + min(y, kDtPages - 1)));
+                const bool loads = lane < kDtPages * BOXES && v0 + y < v1 && my_page >= 0;
+                const uint32_t bytes = __popc(__ballot_sync(0xffffffffu, loads)) * kDtPageBox;
+                const uint32_t off = slot * TILE + lane % BOXES * kStBox + y * kDtPageBox;
+                const int at = (my_page * p.Hkv + pl.kvh) * kPage;
+                if (use > 0) wait(&bar_kfree[slot], use - 1);
+                if (!ok) break;
+                __syncwarp();
+                if (lane == 0) mbar_expect_tx(smem_u32(&bar_k[slot]), bytes);
+                __syncwarp();
+                if (loads) tma_load_2d(Ks + off, my_part ? &mk1 : &mk0, lane % BOXES * 64, at, smem_u32(&bar_k[slot]), policy);
+                if (use > 0) wait(&bar_vfree[slot], use - 1);
+                if (!ok) break;
+                if (lane == 0) mbar_expect_tx(smem_u32(&bar_v[slot]), bytes);
+                __syncwarp();
+                if (loads) tma_load_2d(Vs + off, my_part ? &mv1 : &mv0, lane % BOXES * 64, at, smem_u32(&bar_v[slot]), policy);
+            }
+            plan_done(r);
+        }
+        if (!ok && lane == 0) {              // leave nothing in flight behind: a bounded chance for what was asked for last
+            if (nq > 0) mbar_wait(smem_u32(bar_q), (nq - 1) & 1);
+            for (int y = 0; y < NS; ++y) {
+                const int uses = (c - y + NS) / NS;          // blocks that went to slot y, the one that was cut off included
+                if (c >= y && uses > 0) { mbar_wait(smem_u32(&bar_k[y]), (uses - 1) & 1); mbar_wait(smem_u32(&bar_v[y]), (uses - 1) & 1); }
+            }
+        }
+    } else if (wid == 11 || wid >= 13) {
+        // ---------------- the guards: V rows of blocks with hidden keys, a quarter of the rows each
+        constexpr int GR = KB / 4;
+        const int g0 = (wid == 11 ? 0 : wid - 12) * GR;
+        const bool tree = p.parents != nullptr;
+        int c = 0;
+        for (int r = 0; ok; ++r) {
+            DrPlan &pl = plan_of(r);
+            if (!ok || !pl.valid) break;
+            const int ctx = pl.s.ctx, full_hi = tree ? ctx - 1 : ctx + pl.i0;
+            const int full_lo = p.window > 0 ? ctx + (tree ? pl.deepest : pl.i0 + pl.toks - 1) - p.window + 1 : 0;
+            for (int b = pl.b1 - 1; b >= pl.b0 && ok; --b, ++c) {
+                // every block passes through here, so that no guard is ever a whole ring ahead of or behind the others
+                const int slot = c % NS, v = b * kDtPages;
+                wait(&bar_v[slot], c / NS);
+                __syncwarp();
+                bool whole = true;
+#pragma unroll
+                for (int y = 0; y < kDtPages; ++y) {
+                    const int2 tl = dt_tile(pl, v + y);
+                    const int e = tl.x + kPage - 1;
+                    whole = whole && tl.y == kPage && e <= full_hi && (tl.x >= full_lo || e < p.sinks);
+                }
+                if (!whole) {
+                    uint8_t *vt = base + 2 * QTILE + (NS + slot) * TILE;
+                    for (int row = g0; row < g0 + GR; ++row) {
+                        uint4 *chunk = reinterpret_cast<uint4 *>(vt + (lane >> 3) * kStBox + row * 128 + (lane & 7) * 16);
+                        const bool has = lane < 8 * BOXES;
+                        const int2 tl = dt_tile(pl, v + row / kPage);
+                        const int key = row % kPage;
+                        if (key >= tl.y) {                       // holds no token
+                            if (has) *chunk = make_uint4(0, 0, 0, 0);
+                            continue;
+                        }
+                        if (!__any_sync(0xffffffffu, has && st_not_finite(*(has ? chunk : reinterpret_cast<uint4 *>(vt + row * 128))) != 0)) continue;
+                        bool sees = false, not_all = false;      // rare
+                        for (int y = lane; y < pl.toks; y += 32) {
+                            const bool s1 = (dt_sees(p, pl, tl, y, ctx + (tree ? pl.depth[pl.i0 + y] : pl.i0 + y)) >> key) & 1u;
+                            sees = sees || s1;
+                            not_all = not_all || !s1;
+                        }
+                        if (!__any_sync(0xffffffffu, sees)) {
+                            if (has) *chunk = make_uint4(0, 0, 0, 0);
+                        } else if (__any_sync(0xffffffffu, not_all)) {
+                            pl.poisoned = 1;
+                        }
+                    }
+                    fence_proxy_async();
+                    __syncwarp();
+                }
+                if (lane == 0) mbar_arrive(smem_u32(&bar_guard[slot]));
+            }
+            plan_done(r);
+        }
+    } else if (wid < 10) {
+        // ---------------- the warp that issues tile t's MMAs: S of block j, then P V of block j - 1; n counts the tile's blocks
+        const int t = wid - 8;
+        const uint32_t ts = tmem + (t ? kStS1 : kStS0), tp = tmem + (t ? kStP1 : kStP0), to = tmem + (t ? kStO1 : kStO0);
+        int c = 0, n = 0, nq = 0;
+        for (int r = 0; ok; ++r) {
+            const DrPlan &pl = plan_of(r);
+            if (!ok || !pl.valid) break;
+            const int NB = pl.b1 - pl.b0;
+            const bool mine = t < pl.tiles;
+            wait(bar_q, nq++);
+            for (int j = 0; j <= NB && ok; ++j) {
+                if (j < NB) {
+                    const int slot = (c + j) % NS;
+                    // a tile that has no use for a block gives it back all the same, once it is there: never a ring ahead
+                    wait(&bar_k[slot], (c + j) / NS);
+                    if (mine) {
+                        if (n + j > 0) wait(&bar_sf[t], n + j - 1);
+                        __syncwarp();
+                        tc_fence_after();
+#pragma unroll
+                        for (int kk = 0; kk < D / 16; ++kk)       // 16 channels per MMA
+                            st_mma_ss(ts, umma_desc(Qs + t * QTILE + (kk >> 2) * kStQBox + (kk & 3) * 32, 16, 1024),
+                                      umma_desc(Ks + slot * TILE + (kk >> 2) * kStBox + (kk & 3) * 32, 16, 1024), umma_idesc(false, KB), kk > 0 ? 1u : 0u);
+                        st_commit(smem_u32(&bar_s[t]));
+                        st_commit(smem_u32(&bar_kfree[slot]));
+                    } else if (lane == 0) {
+                        mbar_arrive(smem_u32(&bar_kfree[slot]));
+                    }
+                    if (j == NB - 1) st_commit(smem_u32(bar_qfree));      // behind the item's last use of Q (at once where nothing is under way)
+                }
+                if (j > 0) {
+                    const int jj = j - 1, slot = (c + jj) % NS;
+                    wait(&bar_v[slot], (c + jj) / NS);
+                    wait(&bar_guard[slot], (c + jj) / NS);
+                    if (mine) {
+                        wait(&bar_p[t], n + jj);          // also: this tile's softmax has read the O of the item before
+                        __syncwarp();
+                        tc_fence_after();
+#pragma unroll
+                        for (int kk = 0; kk < KB / 16; ++kk)      // 16 keys per MMA: 8 columns of P, 2 KB of each 64-channel box of V
+                            st_mma_ts(to, tp + kk * 8, umma_desc(Vs + slot * TILE + kk * 2048, kStBox, 1024), umma_idesc(true, D), (jj > 0 || kk > 0) ? 1u : 0u);
+                        st_commit(smem_u32(&bar_o[t]));
+                        st_commit(smem_u32(&bar_vfree[slot]));
+                    } else if (lane == 0) {
+                        mbar_arrive(smem_u32(&bar_vfree[slot]));
+                    }
+                }
+            }
+            c += NB;
+            if (mine) n += NB;
+            plan_done(r);
+        }
+    }
+    }
+    tc_fence_before();
+    const bool gave_up = !__syncthreads_and(ok);
+    tc_fence_after();
+    if (gave_up && tid == 0) flag_error(p.hdr, 6 /* SPD_ERR_TIMEOUT */, -1);
+    if (wid == 8) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(kStTmemCols) : "memory");
+}
+
+}  // namespace spd
