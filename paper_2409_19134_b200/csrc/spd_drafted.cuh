@@ -274,28 +274,39 @@ __device__ __forceinline__ void drafted_header(const DraftedParams &p, int first
     if (first_bad < p.B) flag_error(p.hdr, 4 /* SPD_ERR_BAD_PAGE */, first_bad);
 }
 
-// Four channels of one row, unnormalised with maximum m (natural units) and sum l, to their place: the partial, or merged with the partial
-// that came in and normalised.
+// What becomes of a row with maximum m (natural units) and sum l: its O times `a`, plus the O that came in times `b` (0: not looked at).
+// For a final result both carry 1 / l of the whole; a partial keeps O as it is, and m and l go with its first channels.
+struct DraftedRow { float a, b, m, l; };
+__device__ __forceinline__ DraftedRow drafted_row(const DraftedParams &p, int64_t row, float m, float l, bool bad) {
+    if (bad) return DraftedRow{0.f, 0.f, -INFINITY, 0.f};
+    DraftedRow f{1.f, 0.f, m, l};
+    if (p.mode == OUT_PARTIAL) return f;
+    if (p.in_o != nullptr) {
+        const float mi = p.in_m[row], li = p.in_l[row], M = fmaxf(m, mi);
+        f.a = m == -INFINITY ? 0.f : expf(m - M);
+        f.b = mi == -INFINITY ? 0.f : expf(mi - M);
+        // an empty part weighs nothing; a sum that is NaN (scores that are) stays
+        l = (l != l ? l : f.a != 0.f ? l * f.a : 0.f) + (li != li ? li : f.b != 0.f ? li * f.b : 0.f);
+    }
+    const float inv = l == 0.f ? 0.f : 1.f / l;
+    f.a = f.a == 0.f && l == l ? 0.f : f.a * inv;
+    f.b = f.b == 0.f ? 0.f : f.b * inv;
+    return f;
+}
+
+// Four channels of the row.
 template <int D>
-__device__ __forceinline__ void drafted_store4(const DraftedParams &p, int64_t row, int c4, float4 o, float m, float l, bool bad) {
+__device__ __forceinline__ void drafted_put4(const DraftedParams &p, int64_t row, int c4, float4 o, const DraftedRow &f) {
+    float4 y = f.a == 0.f ? make_float4(0.f, 0.f, 0.f, 0.f) : make_float4(o.x * f.a, o.y * f.a, o.z * f.a, o.w * f.a);
     if (p.mode == OUT_PARTIAL) {
-        reinterpret_cast<float4 *>(p.po)[row * (D / 4) + c4] = bad ? make_float4(0.f, 0.f, 0.f, 0.f) : o;
-        if (c4 == 0) { p.pm[row] = bad ? -INFINITY : m; p.pl[row] = bad ? 0.f : l; }
+        reinterpret_cast<float4 *>(p.po)[row * (D / 4) + c4] = y;
+        if (c4 == 0) { p.pm[row] = f.m; p.pl[row] = f.l; }
         return;
     }
-    if (p.in_o != nullptr && !bad) {
-        const float mi = p.in_m[row], li = p.in_l[row], M = fmaxf(m, mi);
+    if (f.b != 0.f) {
         const float4 v = reinterpret_cast<const float4 *>(p.in_o)[row * (D / 4) + c4];
-        const float a = m == -INFINITY ? 0.f : expf(m - M), b = mi == -INFINITY ? 0.f : expf(mi - M);
-        // an empty part weighs nothing, whatever stands in its O; a sum that is NaN stays
-        l = (a != 0.f || l != l ? l * (l != l ? 1.f : a) : 0.f) + (b != 0.f || li != li ? li * (li != li ? 1.f : b) : 0.f);
-        o.x = (a != 0.f ? o.x * a : 0.f) + (b != 0.f ? v.x * b : 0.f);
-        o.y = (a != 0.f ? o.y * a : 0.f) + (b != 0.f ? v.y * b : 0.f);
-        o.z = (a != 0.f ? o.z * a : 0.f) + (b != 0.f ? v.z * b : 0.f);
-        o.w = (a != 0.f ? o.w * a : 0.f) + (b != 0.f ? v.w * b : 0.f);
+        y.x = fmaf(v.x, f.b, y.x); y.y = fmaf(v.y, f.b, y.y); y.z = fmaf(v.z, f.b, y.z); y.w = fmaf(v.w, f.b, y.w);
     }
-    const bool none = bad || l == 0.f;
-    const float4 y = none ? make_float4(0.f, 0.f, 0.f, 0.f) : make_float4(o.x / l, o.y / l, o.z / l, o.w / l);
     if (p.out_bf16) reinterpret_cast<uint2 *>(p.out)[row * (D / 4) + c4] = make_uint2(pack_bf16(y.x, y.y), pack_bf16(y.z, y.w));
     else reinterpret_cast<float4 *>(p.out)[row * (D / 4) + c4] = y;
 }
@@ -349,7 +360,8 @@ __global__ void __launch_bounds__(256) drafted_join_kernel(const __grid_constant
                 o.w = o.w * wa + (wb != 0.f ? v.w * wb : 0.f);
                 m = M;
             }
-            drafted_store4<D>(p, (static_cast<int64_t>(tok0) + r / p.hs) * p.Hq + h0 + r % p.hs, c, o, m * kUnit, l, bad);
+            const int64_t row = (static_cast<int64_t>(tok0) + r / p.hs) * p.Hq + h0 + r % p.hs;
+            drafted_put4<D>(p, row, c, o, drafted_row(p, row, m * kUnit, l, bad));
         }
     }
 }

@@ -213,10 +213,12 @@ __global__ void __launch_bounds__(DraftedFma<D, RT>::kThreads) drafted_fma_kerne
             if (r >= rows) continue;
             const int64_t row = (static_cast<int64_t>(s.first) + i0 + tok[i]) * p.Hq + h0 + r % p.hs;
             float *dst = p.scratch + static_cast<size_t>(slot) * drafted_slot_floats(D, RT);
+            DraftedRow f{};
+            if (whole) f = drafted_row(p, row, m[i], l[i], bad);
 #pragma unroll
             for (int c = 0; c < CH; ++c) {
                 const float4 v = make_float4(o[i][4 * c], o[i][4 * c + 1], o[i][4 * c + 2], o[i][4 * c + 3]);
-                if (whole) drafted_store4<D>(p, row, tx + 16 * c, v, m[i], l[i], bad);
+                if (whole) drafted_put4<D>(p, row, tx + 16 * c, v, f);
                 else reinterpret_cast<float4 *>(dst)[(tx + 16 * c) * RT + r] = v;
             }
             if (!whole && tx == 0) { dst[RT * D + r] = m[i]; dst[RT * (D + 1) + r] = l[i]; }

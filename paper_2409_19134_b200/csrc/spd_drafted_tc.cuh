@@ -4,8 +4,10 @@
 // pages, each page a pair of TMA boxes per operand.  Per tile and block:
 //     S = Q K^T     128 x 80 x D, fp32 in TMEM;   softmax: one row per thread, S into registers, options, mask, exponentials, P as bf16 pairs into
 //     TMEM columns of its own, so that the next S is computed under the exponentials;   O += P V     128 x D x 80, P read from TMEM.
-// 8 softmax warps, one warp per tile that issues its MMAs, one that loads, one that plans the next item (and walks its tree) while this one
-// runs, four that guard V.  Everything is handed over through mbarriers with bounded waits; a wait that runs out ends the CTA with
+// An item with rows for one tile only is worked on by both: each takes every other block, and their (O, m, l) are joined at the end, O straight from
+// TMEM (a row has the same lane in both tiles).  With one tile at work the chain of its softmax, not HBM, bounds the loop.
+// 8 softmax warps, one warp per tile that issues its MMAs, one that loads K and one that loads V, one that plans the next item (and walks its tree)
+// while this one runs, three that guard V.  Everything is handed over through mbarriers with bounded waits; a wait that runs out ends the CTA with
 // SPD_ERR_TIMEOUT once all its threads have come to the common end.
 //
 // Masks: a row sees one or two intervals of the context (window, sinks) and a set of drafted tokens (bits per token).  A warp builds them,
@@ -38,9 +40,14 @@ struct DrPlan {
     int16_t parent[kDrTree], depth[kDrTree];         // of all the user's drafted tokens
     uint32_t line[kDrTree][kDrWords];                // of the item's tokens
 };
-constexpr int kDtBarBytes = 320;
+__host__ __device__ constexpr int dt_kslots(int D) { return D == 128 ? 3 : 5; }
+__host__ __device__ constexpr int dt_vslots(int D) { return D == 128 ? 4 : 6; }
+constexpr int kDtGuards = 3;
+constexpr int kDtBarBytes = 384;
+struct DtExchange { float m[2][128], top[2][128], l[2][128]; uint32_t again[2][4]; };      // of both tiles' rows, where they share an item
 constexpr size_t dt_smem_bytes(int D) {
-    return 2 * static_cast<size_t>(st_qtile(D)) + 2 * st_slots(D) * static_cast<size_t>(st_tile(D)) + kDtBarBytes + 2 * sizeof(DrPlan);
+    return 2 * static_cast<size_t>(st_qtile(D)) + (dt_kslots(D) + dt_vslots(D)) * static_cast<size_t>(st_tile(D)) + kDtBarBytes + sizeof(DtExchange) +
+           2 * sizeof(DrPlan);
 }
 static_assert(dt_smem_bytes(128) + 1024 <= 232448, "shared memory of an SM");
 
@@ -67,6 +74,28 @@ __device__ __forceinline__ int2 dt_tile(const DrPlan &pl, int v) {
     if (x < pl.s.np) return make_int2(x * kPage, min(kPage, pl.s.lp - x * kPage));
     const int y = (x - pl.s.np) * kPage;
     return make_int2(pl.s.lp + y, min(kPage, pl.s.lq - y));
+}
+
+// Where the list's tiles hold nothing but keys that rows with these bounds see whole (context in [lo, hi]): tiles [a0, a1) and [b0, b1).
+struct DtWhole {
+    int a0, a1, b0, b1;
+    __device__ __forceinline__ bool holds(int v) const { return (v >= a0 && v + kDtPages <= a1) || (v >= b0 && v + kDtPages <= b1); }
+};
+__device__ __forceinline__ DtWhole dt_whole(const DrPlan &pl, int lo, int hi) {
+    const int shift = pl.k.ns - pl.k.a, lp = pl.s.lp, np = pl.s.np;
+    const int64_t end = static_cast<int64_t>(hi) + 1;
+    auto up = [](int x) { return x / kPage + (x % kPage != 0 ? 1 : 0); };
+    DtWhole w{0, 0, 0, 0};
+    if (np > 0) {
+        w.a0 = max(pl.k.ns, up(max(lo, 0)) + shift);
+        w.a1 = static_cast<int>(min(static_cast<int64_t>(lp), end) / kPage) + shift;
+    }
+    if (pl.s.nt > np && end > lp) {
+        w.b0 = max(pl.k.ns, np + up(max(lo, lp) - lp) + shift);
+        w.b1 = np + static_cast<int>(min(static_cast<int64_t>(pl.s.lq), end - lp) / kPage) + shift;
+    }
+    if (np > 0 && lp % kPage == 0 && w.a1 == w.b0) { w.a1 = w.b1; w.b0 = w.a0; }        // one page follows upon the other
+    return w;
 }
 
 // Which of the 16 keys of a page tile a row sees: token `it` of the item at position pos.
@@ -145,7 +174,7 @@ __device__ __noinline__ void dt_slow_row(const DraftedTcParams &q, const DrPlan 
         }
     }
     if (pl.whole) {
-        if (lane < D / 4) drafted_store4<D>(p, row, lane, o, m, l, false);
+        if (lane < D / 4) drafted_put4<D>(p, row, lane, o, drafted_row(p, row, m, l, false));
     } else {
         float *dst = p.scratch + static_cast<size_t>(pl.slot) * drafted_slot_floats(D, kDtRows);
         const int r = it * p.hs + hh;
@@ -158,22 +187,25 @@ template <int D, bool CAP, bool BIAS>
 __global__ void __launch_bounds__(kDtThreads, 1)
 drafted_tc_kernel(const __grid_constant__ DraftedTcParams q, const __grid_constant__ CUtensorMap mq, const __grid_constant__ CUtensorMap mk0,
                   const __grid_constant__ CUtensorMap mv0, const __grid_constant__ CUtensorMap mk1, const __grid_constant__ CUtensorMap mv1) {
-    constexpr int QTILE = st_qtile(D), TILE = st_tile(D), NS = st_slots(D), BOXES = D / 64, KB = kStKeys;
+    constexpr int QTILE = st_qtile(D), TILE = st_tile(D), NSK = dt_kslots(D), NSV = dt_vslots(D), BOXES = D / 64, KB = kStKeys;
     const DraftedParams &p = q.d;
     extern __shared__ __align__(1024) uint8_t base[];
-    const uint32_t Qs = smem_u32(base), Ks = Qs + 2 * QTILE, Vs = Ks + NS * TILE;
-    uint64_t *bars = reinterpret_cast<uint64_t *>(base + 2 * QTILE + 2 * NS * TILE);
+    const uint32_t Qs = smem_u32(base), Ks = Qs + 2 * QTILE, Vs = Ks + NSK * TILE;
+    uint8_t *behind = base + 2 * QTILE + (NSK + NSV) * TILE;
+    uint64_t *bars = reinterpret_cast<uint64_t *>(behind);
     uint64_t *bar_q = bars, *bar_qfree = bars + 1;                 // Q loaded; Q read by both tiles
     uint64_t *bar_s = bars + 2, *bar_sf = bars + 4;                // per tile: S ready; S in registers
     uint64_t *bar_p = bars + 6, *bar_o = bars + 8;                 // per tile: P written; O has taken the block in (P is free)
     uint64_t *bar_plan = bars + 10, *bar_planfree = bars + 12;     // per plan buffer
-    uint64_t *bar_k = bars + 14, *bar_v = bar_k + NS, *bar_kfree = bar_v + NS, *bar_vfree = bar_kfree + NS;
-    uint64_t *bar_guard = bar_vfree + NS;                          // per V slot: the guards are done with the block
-    constexpr int NBARS = 14 + 5 * NS;
+    uint64_t *bar_x = bars + 14, *bar_y = bars + 15;               // a shared item's rows are exchanged; their O's are read
+    uint64_t *bar_k = bars + 16, *bar_kfree = bar_k + NSK, *bar_v = bar_kfree + NSK, *bar_vfree = bar_v + NSV;
+    uint64_t *bar_guard = bar_vfree + NSV;                         // per V slot: the guards are done with the block
+    constexpr int NBARS = 16 + 2 * NSK + 3 * NSV;
     static_assert(NBARS * 8 + 8 <= kDtBarBytes, "barrier block");
     uint32_t &tmem_slot = *reinterpret_cast<uint32_t *>(bars + NBARS);
     int &first_bad = *reinterpret_cast<int *>(&tmem_slot + 1);
-    DrPlan *plans = reinterpret_cast<DrPlan *>(base + 2 * QTILE + 2 * NS * TILE + kDtBarBytes);
+    DtExchange &ex = *reinterpret_cast<DtExchange *>(behind + kDtBarBytes);
+    DrPlan *plans = reinterpret_cast<DrPlan *>(behind + kDtBarBytes + sizeof(DtExchange));
     const int tid = threadIdx.x, wid = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31;
 
     // ---- the cut: sums over the users in what becomes the K ring, the share's first item by the planning warp
@@ -191,9 +223,10 @@ drafted_tc_kernel(const __grid_constant__ DraftedTcParams q, const __grid_consta
     if (tid == 320) {
         prefetch_tensormap(&mq); prefetch_tensormap(&mk0); prefetch_tensormap(&mv0); prefetch_tensormap(&mk1); prefetch_tensormap(&mv1);
         for (int b = 0; b < NBARS; ++b) {
-            // Q and ring slots free: one per tile; S in registers, P written: one per softmax warp of the tile;
-            // V looked through: one per guard; plan read: one per warp
-            const int n = b == 1 || (b >= 14 + 2 * NS && b < 14 + 4 * NS) ? 2 : ((b >= 4 && b < 8) || b >= 14 + 4 * NS) ? 4 : (b >= 12 && b < 14) ? kDtConsumers : 1;
+            // Q and ring slots free: one per tile; S in registers, P written: one per softmax warp of the tile; rows exchanged, O's
+            // read: one per softmax warp; V looked through: one per guard; plan read: one per warp
+            const int k = b - 16, n = b == 1 || (k >= NSK && k < 2 * NSK) || (k >= 2 * NSK + NSV && k < 2 * NSK + 2 * NSV) ? 2 : b >= 4 && b < 8 ? 4
+                                      : b == 14 || b == 15 ? 8 : k >= 2 * NSK + 2 * NSV ? kDtGuards : b >= 12 && b < 14 ? kDtConsumers : 1;
             mbar_init(smem_u32(&bars[b]), n);
         }
         fence_mbar_init();
@@ -217,38 +250,45 @@ drafted_tc_kernel(const __grid_constant__ DraftedTcParams q, const __grid_consta
     if (wid < 8) {
         asm volatile("setmaxnreg.inc.sync.aligned.u32 192;");
         // ---------------- softmax warps: one row per thread; n counts the tile's blocks
-        const int t = wid >> 2, rr = tid & 127, in_tile = rr / p.hs, hh = rr - in_tile * p.hs, it = t * q.tpt + in_tile;
-        const int w0 = t * q.tpt + ((rr & ~31) / p.hs), w1 = t * q.tpt + min(q.tpt - 1, (rr | 31) / p.hs);       // the warp's tokens
+        const int t = wid >> 2, rr = tid & 127, in_tile = rr / p.hs, hh = rr - in_tile * p.hs;
+        const int wt0 = (rr & ~31) / p.hs, wt1 = min(q.tpt - 1, (rr | 31) / p.hs);       // the warp's tokens within the tile
         const bool tree = p.parents != nullptr;
         const uint32_t lanes = static_cast<uint32_t>((wid & 3) * 32) << 16;
         const uint32_t t_s = tmem + lanes + (t ? kStS1 : kStS0), t_p = tmem + lanes + (t ? kStP1 : kStP0);
         const uint32_t t_o = tmem + lanes + (t ? kStO1 : kStO0);
-        int n = 0;
+        int n = 0, nx = 0;                                    // blocks of the tile; items that both tiles shared
         for (int r = 0; ok; ++r) {
             DrPlan &pl = plan_of(r);
             if (!ok || !pl.valid) break;
-            const int nblk = t < pl.tiles ? pl.b1 - pl.b0 : 0, toks = pl.toks, ctx = pl.s.ctx, i0 = pl.i0;
-            const bool mine = (rr & ~31) / p.hs < q.tpt && w0 < toks, live = in_tile < q.tpt && it < toks;      // of the warp, of the thread
+            const bool shared = pl.tiles == 1;                // both tiles work for the first one's rows, every other block each
+            const int nb = pl.b1 - pl.b0, nblk = shared ? (nb - t + 1) / 2 : nb, toks = pl.toks, ctx = pl.s.ctx, i0 = pl.i0;
+            const int it = in_tile + (shared ? 0 : t * q.tpt), w0 = wt0 + (shared ? 0 : t * q.tpt), w1 = wt1 + (shared ? 0 : t * q.tpt);
+            const bool mine = wt0 < q.tpt && w0 < toks, live = in_tile < q.tpt && it < toks;      // of the warp, of the thread
             const int tok = live ? it : 0;
             const int pos = ctx + (!tree ? i0 + tok : pl.s.good ? pl.depth[i0 + tok] : 0);      // no tree where the user is refused
-            // what every row of the warp sees: whole tiles of context in [full_lo, full_hi], or in front of the sinks' end
+            // what every row of the warp sees: whole tiles of context in [full_lo, full_hi]
             const int full_hi = tree ? ctx - 1 : ctx + i0 + w0;
             const int full_lo = p.window > 0 ? ctx + (tree ? pl.deepest : i0 + min(w1, toks - 1)) - p.window + 1 : 0;
             const int last_pos = tree ? 0x7fffffff : ctx + i0 + min(w1, toks - 1);
+            const DtWhole dw = dt_whole(pl, full_lo, full_hi);
+            const int vtop = (pl.b1 - 1 - (shared ? t : 0)) * kDtPages, vstep = (shared ? 2 : 1) * kDtPages;      // tiles of the first block; between blocks
+            const int prv = pl.k.ns - pl.k.a, pub = prv + pl.s.np, lp = pl.s.lp;      // list index of the first private and public tile
             const float slope2 = BIAS ? p.slopes[pl.h0 + hh] * kLog2e : 0.f;
             float l = 0.f, m = -INFINITY, top = -INFINITY;          // reference point and greatest score, log2 units
             for (int i = 0; i < nblk && ok; ++i) {
-                const int v = (pl.b1 - 1 - i) * kDtPages;
+                const int v = vtop - i * vstep;
+                const bool whole = mine && dw.holds(v);
+                bool none = !mine;
                 int2 tl[kDtPages];
-                bool whole = true, none = true;
+                if (!whole) {
+                    none = true;
 #pragma unroll
-                for (int y = 0; y < kDtPages; ++y) {
-                    tl[y] = dt_tile(pl, v + y);
-                    const int e = tl[y].x + kPage - 1;
-                    whole = whole && tl[y].y == kPage && e <= full_hi && (tl[y].x >= full_lo || e < p.sinks);
-                    none = none && (tl[y].y == 0 || tl[y].x > last_pos);
+                    for (int y = 0; y < kDtPages; ++y) {
+                        tl[y] = dt_tile(pl, v + y);
+                        none = none && (tl[y].y == 0 || tl[y].x > last_pos);
+                    }
+                    none = none || !mine;
                 }
-                none = none || !mine;
                 wait(&bar_s[t], n + i);
                 __syncwarp();
                 tc_fence_after();
@@ -315,19 +355,25 @@ drafted_tc_kernel(const __grid_constant__ DraftedTcParams q, const __grid_consta
                 }
                 if constexpr (BIAS) {
                     const float scale = CAP ? 1.f : q.c2;
+                    if (whole) {                                       // the block's positions follow upon one another
+                        const float off = static_cast<float>((v >= pub ? lp + (v - pub) * kPage : (v - prv) * kPage) - pos);
 #pragma unroll
-                    for (int y = 0; y < kDtPages; ++y) {
-                        const float off = static_cast<float>(tl[y].x - pos);
-                        if (tree && tl[y].x + tl[y].y > ctx) {          // drafted tokens count by depth
+                        for (int y = 0; y < KB; ++y) sv[y] = fmaf(slope2, off + static_cast<float>(y), sv[y] * scale);
+                    } else {
 #pragma unroll
-                            for (int z = 0; z < kPage; ++z) {
-                                const int d = tl[y].x + z - ctx;
-                                const float far = d >= 0 ? static_cast<float>(ctx - pos + pl.depth[min(d, kDrTree - 1)]) : off + static_cast<float>(z);
-                                sv[16 * y + z] = fmaf(slope2, far, sv[16 * y + z] * scale);
+                        for (int y = 0; y < kDtPages; ++y) {
+                            const float off = static_cast<float>(tl[y].x - pos);
+                            if (tree && tl[y].x + tl[y].y > ctx) {     // drafted tokens count by depth
+#pragma unroll
+                                for (int z = 0; z < kPage; ++z) {
+                                    const int d = tl[y].x + z - ctx;
+                                    const float far = d >= 0 ? static_cast<float>(ctx - pos + pl.depth[min(d, kDrTree - 1)]) : off + static_cast<float>(z);
+                                    sv[16 * y + z] = fmaf(slope2, far, sv[16 * y + z] * scale);
+                                }
+                            } else {
+#pragma unroll
+                                for (int z = 0; z < kPage; ++z) sv[16 * y + z] = fmaf(slope2, off + static_cast<float>(z), sv[16 * y + z] * scale);
                             }
-                        } else {
-#pragma unroll
-                            for (int z = 0; z < kPage; ++z) sv[16 * y + z] = fmaf(slope2, off + static_cast<float>(z), sv[16 * y + z] * scale);
                         }
                     }
                 }
@@ -390,41 +436,82 @@ drafted_tc_kernel(const __grid_constant__ DraftedTcParams q, const __grid_consta
             if (nblk > 0) wait(&bar_o[t], n - 1);
             __syncwarp();
             tc_fence_after();
-            if (ok && nblk > 0 && mine) {
-                const bool poisoned = *const_cast<volatile int32_t *>(&pl.poisoned) != 0, bad = *const_cast<volatile int32_t *>(&pl.bad) != 0;
-                const int64_t row = (static_cast<int64_t>(pl.first) + i0 + tok) * p.Hq + pl.h0 + hh;
-                const float back = m == -INFINITY ? 1.f : ex2_approx(m - top);       // from the reference to the maximum
-                const float ls = l * back, mn = top * 0.69314718055994531f;
-                float *dst = p.scratch + static_cast<size_t>(pl.slot) * drafted_slot_floats(D, kDtRows);
-                const int slot_row = it * p.hs + hh;
-                bool over = false;
-                if (!poisoned || bad) {
-                    float big = 0.f;
-#pragma unroll 1
-                    for (int c = 0; c < D; c += 32) {
-                        float ov[32];
-                        tmem_ld32(t_o + c, ov);
-                        if (live) {
-#pragma unroll
-                            for (int y = 0; y < 32; y += 4) {
-                                big = fmax3_abs_nan(fmax3_abs_nan(big, ov[y], ov[y + 1]), ov[y + 2], ov[y + 3]);
-                                const float4 o4 = make_float4(ov[y] * back, ov[y + 1] * back, ov[y + 2] * back, ov[y + 3] * back);
-                                if (pl.whole) drafted_store4<D>(p, row, (c + y) / 4, o4, mn, ls, bad);
-                                else reinterpret_cast<float4 *>(dst)[(c + y) / 4 * kDtRows + slot_row] = o4;
-                            }
-                        }
-                        __syncwarp();
-                    }
-                    if (live && !pl.whole) { dst[kDtRows * D + slot_row] = top; dst[kDtRows * (D + 1) + slot_row] = ls; }
-                    over = live && !bad && l > 0.f && l < INFINITY && !(big < INFINITY);
-                }
-                uint32_t again = __ballot_sync(0xffffffffu, poisoned && !bad ? live : over);
-                for (; again != 0; again &= again - 1) {
-                    const int src = __ffs(again) - 1;
-                    dt_slow_row<D>(q, pl, __shfl_sync(0xffffffffu, it, src), __shfl_sync(0xffffffffu, hh, src), lane);
-                }
-                if (bad && lane == 0 && (wid & 3) == 0) drafted_flag(p, pl.u);
+            // ---- the rows' way out
+            const int64_t row = (static_cast<int64_t>(pl.first) + i0 + tok) * p.Hq + pl.h0 + hh;
+            float *dst = p.scratch + static_cast<size_t>(pl.slot) * drafted_slot_floats(D, kDtRows);
+            const int slot_row = it * p.hs + hh;
+            float a0 = 1.f, a1 = 0.f;                        // weights of the tiles' O
+            if (shared) {
+                ex.m[t][rr] = m; ex.top[t][rr] = top; ex.l[t][rr] = l;
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(smem_u32(bar_x));
+                wait(bar_x, nx);
+                __syncwarp();
+                tc_fence_after();
+                const float m0 = ex.m[0][rr], m1 = ex.m[1][rr];
+                top = fmaxf(ex.top[0][rr], ex.top[1][rr]);
+                a0 = m0 == -INFINITY ? 0.f : ex2_approx(m0 - top);
+                a1 = m1 == -INFINITY ? 0.f : ex2_approx(m1 - top);
+                l = ex.l[0][rr] * (a0 == 0.f && ex.l[0][rr] == 0.f ? 0.f : a0) + ex.l[1][rr] * a1;
+            } else if (m != -INFINITY) {
+                a0 = ex2_approx(m - top);                    // from the reference to the maximum
+                l *= a0;
             }
+            // read only now: a tile without blocks of its own has waited for nobody before the exchange
+            const bool poisoned = *const_cast<volatile int32_t *>(&pl.poisoned) != 0, bad = *const_cast<volatile int32_t *>(&pl.bad) != 0;
+            bool over = false;
+            if (ok && mine && (!poisoned || bad)) {
+                DraftedRow f{};
+                if (live && pl.whole) f = drafted_row(p, row, top * 0.69314718055994531f, l, bad);
+                float big = 0.f;
+                // a shared row's channels go half by either tile's thread
+                const int c_end = shared ? (t + 1) * (D / 2) : D;
+#pragma unroll 1
+                for (int c = shared ? t * (D / 2) : 0; c < c_end; c += 32) {
+                    float ov[32];
+                    tmem_ld32((shared ? tmem + lanes + kStO0 : t_o) + c, ov);
+                    if (shared) {
+                        float o1[32];
+                        tmem_ld32(tmem + lanes + kStO1 + c, o1);
+#pragma unroll
+                        for (int y = 0; y < 32; ++y) ov[y] = (a0 == 0.f ? 0.f : ov[y] * a0) + (a1 == 0.f ? 0.f : o1[y] * a1);
+                    } else {
+#pragma unroll
+                        for (int y = 0; y < 32; ++y) ov[y] *= a0;
+                    }
+                    if (live) {
+#pragma unroll
+                        for (int y = 0; y < 32; y += 4) {
+                            big = fmax3_abs_nan(fmax3_abs_nan(big, ov[y], ov[y + 1]), ov[y + 2], ov[y + 3]);
+                            const float4 o4 = make_float4(ov[y], ov[y + 1], ov[y + 2], ov[y + 3]);
+                            if (pl.whole) drafted_put4<D>(p, row, (c + y) / 4, o4, f);
+                            else reinterpret_cast<float4 *>(dst)[(c + y) / 4 * kDtRows + slot_row] = o4;
+                        }
+                    }
+                    __syncwarp();
+                }
+                if (live && !pl.whole && (!shared || t == 0)) { dst[kDtRows * D + slot_row] = top; dst[kDtRows * (D + 1) + slot_row] = l; }
+                over = live && !bad && l > 0.f && l < INFINITY && !(big < INFINITY);
+            }
+            uint32_t again = __ballot_sync(0xffffffffu, ok && mine && (poisoned && !bad ? live : over));
+            if (shared) {
+                // the other tile may not write its next O before this one's is read; rows that are done again wait for both halves
+                if (lane == 0) ex.again[t][wid & 3] = again;
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(smem_u32(bar_y));
+                wait(bar_y, nx);
+                __syncwarp();
+                tc_fence_after();
+                ++nx;
+                again = ok ? (ex.again[0][wid & 3] | ex.again[1][wid & 3]) & (t ? 0xaaaaaaaau : 0x55555555u) : 0u;
+            }
+            for (; again != 0; again &= again - 1) {
+                const int src = __ffs(again) - 1;
+                dt_slow_row<D>(q, pl, __shfl_sync(0xffffffffu, it, src), __shfl_sync(0xffffffffu, hh, src), lane);
+            }
+            if (ok && bad && lane == 0 && wid == 0) drafted_flag(p, pl.u);
             tc_fence_before();                               // O is read: ordered before this warp's next arrival
             plan_done(r);
         }
@@ -479,8 +566,13 @@ drafted_tc_kernel(const __grid_constant__ DraftedTcParams q, const __grid_consta
             if (lane == 0) mbar_arrive(smem_u32(&bar_plan[r & 1]));
             x = w.x0 + b1;
         }
-    } else if (wid == 10) {
-        // ---------------- the loading warp; c counts blocks over all items
+    } else if (wid == 10 || wid == 11) {
+        // ---------------- the loading warps: K (and Q), V; c counts blocks over all items
+        const bool is_k = wid == 10;
+        const int ring = is_k ? NSK : NSV;
+        const uint32_t slots = is_k ? Ks : Vs;
+        uint64_t *bar_full = is_k ? bar_k : bar_v, *bar_free = is_k ? bar_kfree : bar_vfree;
+        const CUtensorMap *m0 = is_k ? &mk0 : &mv0, *m1 = is_k ? &mk1 : &mv1;
         const uint64_t once = l2_evict_first_policy();
         uint64_t often;
         asm volatile("createpolicy.fractional.L2::evict_normal.b64 %0, 1.0;" : "=l"(often));
@@ -488,104 +580,110 @@ drafted_tc_kernel(const __grid_constant__ DraftedTcParams q, const __grid_consta
         for (int r = 0; ok; ++r) {
             DrPlan &pl = plan_of(r);
             if (!ok || !pl.valid) break;
-            if (nq > 0) wait(bar_qfree, nq - 1);
-            if (ok && lane == 0) {
-                const int rows = p.hs * q.tpt;
-                mbar_expect_tx(smem_u32(bar_q), pl.tiles * BOXES * rows * 128);
-                for (int t = 0; t < pl.tiles; ++t)
-                    for (int y = 0; y < BOXES; ++y)
-                        tma_load_3d(Qs + t * QTILE + y * kStQBox, &mq, 64 * y, pl.h0, pl.first + pl.i0 + t * q.tpt, smem_u32(bar_q));
+            if (is_k) {
+                if (nq > 0) wait(bar_qfree, nq - 1);
+                if (ok && lane == 0) {
+                    const int rows = p.hs * q.tpt;
+                    mbar_expect_tx(smem_u32(bar_q), pl.tiles * BOXES * rows * 128);
+                    for (int t = 0; t < pl.tiles; ++t)
+                        for (int y = 0; y < BOXES; ++y)
+                            tma_load_3d(Qs + t * QTILE + y * kStQBox, &mq, 64 * y, pl.h0, pl.first + pl.i0 + t * q.tpt, smem_u32(bar_q));
+                }
+                if (ok) ++nq;
             }
-            if (ok) ++nq;
             const uint64_t policy = pl.s.n > p.tt ? often : once;      // other items read these keys too
-            const int list = pl.k.ns + pl.k.e - pl.k.a;
-            const int v1 = min(pl.b1 * kDtPages, list);
-            int page = -1, part = 0, have = v1;                 // lane k holds the page of tile have + k; tiles are worked through downwards
-            for (int i = 0, b = pl.b1 - 1; b >= pl.b0 && ok; --b, ++i, ++c) {
-                const int v0 = b * kDtPages, slot = c % NS, use = c / NS;
+            const int b0 = pl.b0, list = pl.k.ns + pl.k.e - pl.k.a, v1 = min(pl.b1 * kDtPages, list), kvh = pl.kvh;
+            int at = -1, part = 0, have = v1;                   // lane k holds where tile have + k starts; tiles are worked through downwards
+            for (int b = pl.b1 - 1; b >= b0 && ok; --b, ++c) {
+                const int v0 = b * kDtPages, slot = c % ring, use = c / ring;
                 if (v0 < have) {                                // 30 tiles at a time: six blocks
-                    have = max(pl.b0 * kDtPages, v0 - 5 * kDtPages);
-                    page = -1;
+                    have = max(b0 * kDtPages, v0 - 5 * kDtPages);
+                    at = -1;
                     if (lane < 6 * kDtPages && have + lane < v1) {
                         const DraftedTile d = drafted_tile(p, pl.s, pl.k, have + lane);
                         part = d.part;
-                        page = p.part[part].indices[d.entry];
-                        if (page < 0 || page >= p.part[part].num_pages) { page = -1; pl.bad = 1; }
+                        const int page = p.part[part].indices[d.entry];
+                        if (page < 0 || page >= p.part[part].num_pages) pl.bad = 1;
+                        else at = (page * p.Hkv + kvh) * kPage;
                     }
                 }
                 // lanes 0 .. 9 load: tile lane / 2, box lane % 2
-                const int y = lane / BOXES, my_page = __shfl_sync(0xffffffffu, page, min(31, v0 - have + min(y, kDtPages - 1)));
-                const int my_part = __shfl_sync(0xffffffffu, part, min(31, v0 - have + min(y, kDtPages - 1)));
-                const bool loads = lane < kDtPages * BOXES && v0 + y < v1 && my_page >= 0;
+                const int y = lane / BOXES, from = min(31, v0 - have + min(y, kDtPages - 1));
+                const int my_at = __shfl_sync(0xffffffffu, at, from), my_part = __shfl_sync(0xffffffffu, part, from);
+                const bool loads = lane < kDtPages * BOXES && v0 + y < v1 && my_at >= 0;
                 const uint32_t bytes = __popc(__ballot_sync(0xffffffffu, loads)) * kDtPageBox;
-                const uint32_t off = slot * TILE + lane % BOXES * kStBox + y * kDtPageBox;
-                const int at = (my_page * p.Hkv + pl.kvh) * kPage;
-                if (use > 0) wait(&bar_kfree[slot], use - 1);
+                if (use > 0) wait(&bar_free[slot], use - 1);
                 if (!ok) break;
                 __syncwarp();
-                if (lane == 0) mbar_expect_tx(smem_u32(&bar_k[slot]), bytes);
+                if (lane == 0) mbar_expect_tx(smem_u32(&bar_full[slot]), bytes);
                 __syncwarp();
-                if (loads) tma_load_2d(Ks + off, my_part ? &mk1 : &mk0, lane % BOXES * 64, at, smem_u32(&bar_k[slot]), policy);
-                if (use > 0) wait(&bar_vfree[slot], use - 1);
-                if (!ok) break;
-                if (lane == 0) mbar_expect_tx(smem_u32(&bar_v[slot]), bytes);
-                __syncwarp();
-                if (loads) tma_load_2d(Vs + off, my_part ? &mv1 : &mv0, lane % BOXES * 64, at, smem_u32(&bar_v[slot]), policy);
+                if (loads)
+                    tma_load_2d(slots + slot * TILE + lane % BOXES * kStBox + y * kDtPageBox, my_part ? m1 : m0, lane % BOXES * 64, my_at,
+                                smem_u32(&bar_full[slot]), policy);
             }
             plan_done(r);
         }
         if (!ok && lane == 0) {              // leave nothing in flight behind: a bounded chance for what was asked for last
             if (nq > 0) mbar_wait(smem_u32(bar_q), (nq - 1) & 1);
-            for (int y = 0; y < NS; ++y) {
-                const int uses = (c - y + NS) / NS;          // blocks that went to slot y, the one that was cut off included
-                if (c >= y && uses > 0) { mbar_wait(smem_u32(&bar_k[y]), (uses - 1) & 1); mbar_wait(smem_u32(&bar_v[y]), (uses - 1) & 1); }
+            for (int y = 0; y < ring; ++y) {
+                const int uses = (c - y + ring) / ring;         // blocks that went to slot y, the one that was cut off included
+                if (c >= y && uses > 0) mbar_wait(smem_u32(&bar_full[y]), (uses - 1) & 1);
             }
         }
-    } else if (wid == 11 || wid >= 13) {
-        // ---------------- the guards: V rows of blocks with hidden keys, a quarter of the rows each
-        constexpr int GR = KB / 4;
-        const int g0 = (wid == 11 ? 0 : wid - 12) * GR;
+    } else if (wid >= 13) {
+        // ---------------- the guards: V rows of blocks with hidden keys, 16-byte chunks in turns
+        constexpr int CHUNKS = KB * 8 * BOXES, PER = (CHUNKS + 32 * kDtGuards - 1) / (32 * kDtGuards);
         const bool tree = p.parents != nullptr;
         int c = 0;
         for (int r = 0; ok; ++r) {
             DrPlan &pl = plan_of(r);
             if (!ok || !pl.valid) break;
-            const int ctx = pl.s.ctx, full_hi = tree ? ctx - 1 : ctx + pl.i0;
-            const int full_lo = p.window > 0 ? ctx + (tree ? pl.deepest : pl.i0 + pl.toks - 1) - p.window + 1 : 0;
-            for (int b = pl.b1 - 1; b >= pl.b0 && ok; --b, ++c) {
+            const int ctx = pl.s.ctx, b0 = pl.b0;
+            const DtWhole dw = dt_whole(pl, p.window > 0 ? ctx + (tree ? pl.deepest : pl.i0 + pl.toks - 1) - p.window + 1 : 0, tree ? ctx - 1 : ctx + pl.i0);
+            for (int b = pl.b1 - 1; b >= b0 && ok; --b, ++c) {
                 // every block passes through here, so that no guard is ever a whole ring ahead of or behind the others
-                const int slot = c % NS, v = b * kDtPages;
-                wait(&bar_v[slot], c / NS);
+                const int slot = c % NSV, v = b * kDtPages;
+                wait(&bar_v[slot], c / NSV);
                 __syncwarp();
-                bool whole = true;
+                if (!dw.holds(v)) {
+                    uint8_t *vt = base + 2 * QTILE + (NSK + slot) * TILE;
+                    int cnt[kDtPages];
 #pragma unroll
-                for (int y = 0; y < kDtPages; ++y) {
-                    const int2 tl = dt_tile(pl, v + y);
-                    const int e = tl.x + kPage - 1;
-                    whole = whole && tl.y == kPage && e <= full_hi && (tl.x >= full_lo || e < p.sinks);
-                }
-                if (!whole) {
-                    uint8_t *vt = base + 2 * QTILE + (NS + slot) * TILE;
-                    for (int row = g0; row < g0 + GR; ++row) {
-                        uint4 *chunk = reinterpret_cast<uint4 *>(vt + (lane >> 3) * kStBox + row * 128 + (lane & 7) * 16);
-                        const bool has = lane < 8 * BOXES;
-                        const int2 tl = dt_tile(pl, v + row / kPage);
-                        const int key = row % kPage;
-                        if (key >= tl.y) {                       // holds no token
-                            if (has) *chunk = make_uint4(0, 0, 0, 0);
-                            continue;
-                        }
-                        if (!__any_sync(0xffffffffu, has && st_not_finite(*(has ? chunk : reinterpret_cast<uint4 *>(vt + row * 128))) != 0)) continue;
-                        bool sees = false, not_all = false;      // rare
-                        for (int y = lane; y < pl.toks; y += 32) {
-                            const bool s1 = (dt_sees(p, pl, tl, y, ctx + (tree ? pl.depth[pl.i0 + y] : pl.i0 + y)) >> key) & 1u;
-                            sees = sees || s1;
-                            not_all = not_all || !s1;
-                        }
-                        if (!__any_sync(0xffffffffu, sees)) {
-                            if (has) *chunk = make_uint4(0, 0, 0, 0);
-                        } else if (__any_sync(0xffffffffu, not_all)) {
-                            pl.poisoned = 1;
+                    for (int y = 0; y < kDtPages; ++y) cnt[y] = dt_tile(pl, v + y).y;
+                    uint32_t any = 0;
+#pragma unroll
+                    for (int z = 0; z < PER; ++z) {
+                        const int e = (z * kDtGuards + wid - 13) * 32 + lane, key = e >> 3;       // chunk e & 7 of row `key`, box after box
+                        if (e >= CHUNKS) continue;
+                        const int box = BOXES > 1 && key >= KB ? 1 : 0, k = key - box * KB, y = k >> 4;
+                        uint4 *chunk = reinterpret_cast<uint4 *>(vt + box * kStBox + k * 128 + (e & 7) * 16);
+                        const int n = y == 0 ? cnt[0] : y == 1 ? cnt[1] : y == 2 ? cnt[2] : y == 3 ? cnt[3] : cnt[4];
+                        if ((k & 15) >= n) *chunk = make_uint4(0, 0, 0, 0);      // holds no token
+                        else any |= st_not_finite(*chunk);
+                    }
+                    if (__any_sync(0xffffffffu, any != 0)) {                     // rare: row by row, each guard those where it found something
+#pragma unroll 1
+                        for (int z = 0; z < PER; ++z) {
+                            const int e = (z * kDtGuards + wid - 13) * 32 + lane, key = e >> 3;
+                            const int box = BOXES > 1 && key >= KB ? 1 : 0, k = key - box * KB;
+                            uint4 *chunk = reinterpret_cast<uint4 *>(vt + box * kStBox + k * 128 + (e & 7) * 16);
+                            uint32_t found = __ballot_sync(0xffffffffu, e < CHUNKS && st_not_finite(*(e < CHUNKS ? chunk : reinterpret_cast<uint4 *>(vt))) != 0);
+                            while (found != 0) {
+                                const int row = __shfl_sync(0xffffffffu, k, __ffs(found) - 1);
+                                const int2 tl = dt_tile(pl, v + row / kPage);
+                                bool sees = false, not_all = false;
+                                for (int y = lane; y < pl.toks; y += 32) {
+                                    const bool s1 = (dt_sees(p, pl, tl, y, ctx + (tree ? pl.depth[pl.i0 + y] : pl.i0 + y)) >> (row % kPage)) & 1u;
+                                    sees = sees || s1;
+                                    not_all = not_all || !s1;
+                                }
+                                if (!__any_sync(0xffffffffu, sees)) {
+                                    if (e < CHUNKS && k == row) *chunk = make_uint4(0, 0, 0, 0);
+                                } else if (__any_sync(0xffffffffu, not_all)) {
+                                    pl.poisoned = 1;
+                                }
+                                found &= ~__ballot_sync(0xffffffffu, k == row);
+                            }
                         }
                     }
                     fence_proxy_async();
@@ -604,20 +702,23 @@ drafted_tc_kernel(const __grid_constant__ DraftedTcParams q, const __grid_consta
             const DrPlan &pl = plan_of(r);
             if (!ok || !pl.valid) break;
             const int NB = pl.b1 - pl.b0;
-            const bool mine = t < pl.tiles;
+            const bool shared = pl.tiles == 1;
+            const int lag = shared ? 2 : 1;                      // the tile's next S goes before its P V
+            const uint32_t qa = Qs + (shared ? 0 : t * QTILE);
             wait(bar_q, nq++);
-            for (int j = 0; j <= NB && ok; ++j) {
+            for (int j = 0; j < NB + lag && ok; ++j) {
                 if (j < NB) {
-                    const int slot = (c + j) % NS;
+                    const int slot = (c + j) % NSK;
                     // a tile that has no use for a block gives it back all the same, once it is there: never a ring ahead
-                    wait(&bar_k[slot], (c + j) / NS);
-                    if (mine) {
-                        if (n + j > 0) wait(&bar_sf[t], n + j - 1);
+                    wait(&bar_k[slot], (c + j) / NSK);
+                    if (!shared || (j & 1) == t) {
+                        const int k = n + (shared ? j >> 1 : j);
+                        if (k > 0) wait(&bar_sf[t], k - 1);
                         __syncwarp();
                         tc_fence_after();
 #pragma unroll
                         for (int kk = 0; kk < D / 16; ++kk)       // 16 channels per MMA
-                            st_mma_ss(ts, umma_desc(Qs + t * QTILE + (kk >> 2) * kStQBox + (kk & 3) * 32, 16, 1024),
+                            st_mma_ss(ts, umma_desc(qa + (kk >> 2) * kStQBox + (kk & 3) * 32, 16, 1024),
                                       umma_desc(Ks + slot * TILE + (kk >> 2) * kStBox + (kk & 3) * 32, 16, 1024), umma_idesc(false, KB), kk > 0 ? 1u : 0u);
                         st_commit(smem_u32(&bar_s[t]));
                         st_commit(smem_u32(&bar_kfree[slot]));
@@ -626,17 +727,17 @@ drafted_tc_kernel(const __grid_constant__ DraftedTcParams q, const __grid_consta
                     }
                     if (j == NB - 1) st_commit(smem_u32(bar_qfree));      // behind the item's last use of Q (at once where nothing is under way)
                 }
-                if (j > 0) {
-                    const int jj = j - 1, slot = (c + jj) % NS;
-                    wait(&bar_v[slot], (c + jj) / NS);
-                    wait(&bar_guard[slot], (c + jj) / NS);
-                    if (mine) {
-                        wait(&bar_p[t], n + jj);          // also: this tile's softmax has read the O of the item before
+                if (j >= lag) {
+                    const int jj = j - lag, slot = (c + jj) % NSV;
+                    wait(&bar_v[slot], (c + jj) / NSV);
+                    wait(&bar_guard[slot], (c + jj) / NSV);
+                    if (!shared || (jj & 1) == t) {
+                        wait(&bar_p[t], n + (shared ? jj >> 1 : jj));     // also: this tile's softmax has read the O of the item before
                         __syncwarp();
                         tc_fence_after();
 #pragma unroll
                         for (int kk = 0; kk < KB / 16; ++kk)      // 16 keys per MMA: 8 columns of P, 2 KB of each 64-channel box of V
-                            st_mma_ts(to, tp + kk * 8, umma_desc(Vs + slot * TILE + kk * 2048, kStBox, 1024), umma_idesc(true, D), (jj > 0 || kk > 0) ? 1u : 0u);
+                            st_mma_ts(to, tp + kk * 8, umma_desc(Vs + slot * TILE + kk * 2048, kStBox, 1024), umma_idesc(true, D), (jj >= lag || kk > 0) ? 1u : 0u);
                         st_commit(smem_u32(&bar_o[t]));
                         st_commit(smem_u32(&bar_vfree[slot]));
                     } else if (lane == 0) {
@@ -645,7 +746,7 @@ drafted_tc_kernel(const __grid_constant__ DraftedTcParams q, const __grid_consta
                 }
             }
             c += NB;
-            if (mine) n += NB;
+            n += shared ? (NB - t + 1) / 2 : NB;
             plan_done(r);
         }
     }
