@@ -33,21 +33,28 @@ DraftedLayout drafted_layout(const spd_shape &s, int sms) {
     return L;
 }
 
-// The join may be set up while the attention's last CTAs are still at work; it waits for them before it reads anything.
-template <int D, int RT, bool LOG2>
-spd_status launch_join(const DraftedParams &p, cudaStream_t st) {
+// A launch that may be set up while the kernel before it is still at work; both kernels wait for that one's end before they read anything.
+template <class... Args>
+spd_status launch_early(void (*kernel)(Args...), dim3 grid, int threads, size_t smem, cudaStream_t st, const Args &...args) {
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(static_cast<unsigned>(p.grid));
-    cfg.blockDim = dim3(256);
+    cfg.gridDim = grid;
+    cfg.blockDim = dim3(static_cast<unsigned>(threads));
+    cfg.dynamicSmemBytes = smem;
     cfg.stream = st;
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[0].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr;
     cfg.numAttrs = 1;
-    const cudaError_t err = cudaLaunchKernelEx(&cfg, drafted_join_kernel<D, RT, LOG2>, p);
+    const cudaError_t err = cudaLaunchKernelEx(&cfg, kernel, args...);
     host::count_launch();
+    if (err != cudaSuccess) fprintf(stderr, "libspd: launch of a kernel for drafted tokens: %s\n", cudaGetErrorString(err));
     return err == cudaSuccess ? SPD_OK : SPD_ERR_CUDA;
+}
+
+template <int D, int RT, bool LOG2>
+spd_status launch_join(const DraftedParams &p, cudaStream_t st) {
+    return launch_early(drafted_join_kernel<D, RT, LOG2>, dim3(static_cast<unsigned>(p.grid), 2, kDrJoin), 256, 0, st, p);
 }
 
 // [T][Hq][D] bf16 as a 3-D map: a box is `tokens` tokens x `heads` heads x 128 bytes, 128-byte swizzle.
@@ -88,10 +95,9 @@ spd_status launch_tc(const DraftedTcParams &p, const CUtensorMap *maps, cudaStre
         err = cudaFuncSetAttribute(drafted_tc_kernel<D, CAP, BIAS>, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(dt_smem_bytes(D)));
     });
     if (err != cudaSuccess) return SPD_ERR_CUDA;
-    drafted_tc_kernel<D, CAP, BIAS><<<p.d.grid, kDtThreads, dt_smem_bytes(D), st>>>(p, maps[0], maps[1], maps[2], maps[3], maps[4]);
-    host::count_launch();
-    if (cudaGetLastError() != cudaSuccess) return SPD_ERR_CUDA;
-    return launch_join<D, kDtRows, true>(p.d, st);
+    const spd_status rc = launch_early(drafted_tc_kernel<D, CAP, BIAS>, dim3(static_cast<unsigned>(p.d.grid)), kDtThreads, dt_smem_bytes(D), st, p, maps[0],
+                                       maps[1], maps[2], maps[3], maps[4]);
+    return rc != SPD_OK ? rc : launch_join<D, kDtRows, true>(p.d, st);
 }
 
 spd_status run_tc(const DraftedParams &call, int D, int sms, cudaStream_t st) {
@@ -149,10 +155,8 @@ spd_status launch_fma(DraftedParams p, int sms, cudaStream_t st) {
     p.SQ = p.Hkv * p.hgroups;
     p.bt = kDrTiles;
     p.grid = kFmaPerSm * sms;
-    drafted_fma_kernel<E, D, RT><<<p.grid, C::kThreads, C::smem_bytes(), st>>>(p);
-    host::count_launch();
-    if (cudaGetLastError() != cudaSuccess) return SPD_ERR_CUDA;
-    return launch_join<D, RT, false>(p, st);
+    const spd_status rc = launch_early(drafted_fma_kernel<E, D, RT>, dim3(static_cast<unsigned>(p.grid)), C::kThreads, C::smem_bytes(), st, p);
+    return rc != SPD_OK ? rc : launch_join<D, RT, false>(p, st);
 }
 
 template <typename E>
@@ -222,6 +226,7 @@ spd_status run(const spd_shape *shape, const spd_score *score, const spd_drafts 
     if (c.pout) { p.po = c.pout->o; p.pm = c.pout->m; p.pl = c.pout->l; }
     if (c.pin) { p.in_o = c.pin->o; p.in_m = c.pin->m; p.in_l = c.pin->l; }
     p.out = c.out; p.out_bf16 = c.out_dtype == SPD_BF16;
+    p.wide = !misaligned(c.pout ? static_cast<const void *>(p.po) : c.out, 32);
     uint8_t *w = static_cast<uint8_t *>(ws);
     p.hdr = reinterpret_cast<int32_t *>(w);
     p.bad = reinterpret_cast<int32_t *>(w + host::flags_offset(s.batch));

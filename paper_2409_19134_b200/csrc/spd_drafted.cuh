@@ -40,7 +40,7 @@ struct DraftedParams {
     float *po, *pm, *pl;                  // OUT_PARTIAL: [T][Hq][D], [T][Hq], [T][Hq]
     const float *in_o, *in_m, *in_l;      // OUT_FINAL: optional partial to merge in
     void *out;                            // OUT_FINAL: [T][Hq][D]
-    int32_t out_bf16;
+    int32_t out_bf16, wide;               // wide: the output is aligned to 32 bytes
     int32_t *hdr, *bad;
     int32_t epoch, seqs;                  // seqs: what HDR_NSEQ is to hold
     int32_t grid;                         // CTAs of the launch
@@ -69,8 +69,9 @@ __device__ __forceinline__ bool drafted_tokens(const DraftedParams &p, int u, in
 }
 
 // A user whose tables, lengths or counts are inconsistent is not good: it has no keys, and its rows become zeros.
-__device__ __forceinline__ void drafted_user(const DraftedParams &p, int u, DraftedUser &s) {
-    drafted_tokens(p, u, s.first, s.n);
+// False where its offsets are inconsistent.
+__device__ __forceinline__ bool drafted_user(const DraftedParams &p, int u, DraftedUser &s) {
+    const bool consistent = drafted_tokens(p, u, s.first, s.n);
     int64_t len[2], base[2] = {0, 0};
     bool good = true;
 #pragma unroll
@@ -94,6 +95,7 @@ __device__ __forceinline__ void drafted_user(const DraftedParams &p, int u, Draf
     s.base0 = base[0]; s.base1 = base[1];
     s.np = p.part[0].present && good ? (s.lp + kPage - 1) / kPage : 0;
     s.nt = s.np + (p.part[1].present && good ? (s.lq + kPage - 1) / kPage : 0);
+    return consistent;
 }
 
 // Keys of a tile of rows: page tiles [0, ns) and [a, e) of the user's, ceil((ns + e - a) / bt) blocks (at least one, so that rows that
@@ -164,21 +166,21 @@ __device__ __forceinline__ int64_t drafted_sums(const DraftedParams &p, int64_t 
     chunks = (p.B + C - 1) / C;
     if (tid == 0) *first_bad = p.B;
     __syncthreads();
-    for (int u = tid; u < p.B; u += NT) {
-        int a, n;
-        if (!drafted_tokens(p, u, a, n)) atomicMin(first_bad, u);
-    }
-    __syncthreads();
-    const int users = *first_bad;
+    // a user's blocks count unless its offsets, or those of somebody in front of it, turn out to be inconsistent
     int64_t sum = 0;
     DraftedUser s;
+    const int u0 = warps ? tid >> 5 : tid * C, u1 = min(p.B, warps ? u0 + 1 : u0 + C);
+    int bad = 0x7fffffff;
+    for (int u = u0; u < u1 && bad == 0x7fffffff; ++u) {
+        if (!drafted_user(p, u, s)) bad = u;
+        else sum += warps ? drafted_user_blocks(p, s, lane, 32) : drafted_user_blocks(p, s, 0, 1);
+    }
+    if (bad != 0x7fffffff) atomicMin(first_bad, bad);
+    __syncthreads();
+    if (u0 > *first_bad) sum = 0;
     if (warps) {
-        const int u = tid >> 5;
-        if (u < users) { drafted_user(p, u, s); sum = drafted_user_blocks(p, s, lane, 32); }
 #pragma unroll
         for (int d = 16; d >= 1; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
-    } else {
-        for (int u = tid * C; u < min(users, (tid + 1) * C); ++u) { drafted_user(p, u, s); sum += drafted_user_blocks(p, s, 0, 1); }
     }
     sum *= p.SQ;
     // inclusive sums over the chunks
@@ -280,7 +282,10 @@ struct DraftedRow { float a, b, m, l; };
 __device__ __forceinline__ DraftedRow drafted_row(const DraftedParams &p, int64_t row, float m, float l, bool bad) {
     if (bad) return DraftedRow{0.f, 0.f, -INFINITY, 0.f};
     DraftedRow f{1.f, 0.f, m, l};
-    if (p.mode == OUT_PARTIAL) return f;
+    if (p.mode == OUT_PARTIAL) {
+        if (l == 0.f) f.a = 0.f;              // nothing seen: whatever O holds comes from keys that are hidden
+        return f;
+    }
     if (p.in_o != nullptr) {
         const float mi = p.in_m[row], li = p.in_l[row], M = fmaxf(m, mi);
         f.a = m == -INFINITY ? 0.f : expf(m - M);
@@ -311,6 +316,42 @@ __device__ __forceinline__ void drafted_put4(const DraftedParams &p, int64_t row
     else reinterpret_cast<float4 *>(p.out)[row * (D / 4) + c4] = y;
 }
 
+// 32 consecutive channels from c on of the row, 32 bytes at a time (a thread's neighbours write other rows: whole sectors).
+__device__ __forceinline__ void drafted_st32(bool wide, void *p, uint32_t a, uint32_t b, uint32_t c, uint32_t d, uint32_t e, uint32_t f, uint32_t g, uint32_t h) {
+    if (!wide) {                              // the output starts at an odd multiple of 16 bytes
+        static_cast<uint4 *>(p)[0] = make_uint4(a, b, c, d);
+        static_cast<uint4 *>(p)[1] = make_uint4(e, f, g, h);
+        return;
+    }
+    asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "r"(a), "r"(b), "r"(c), "r"(d), "r"(e), "r"(f), "r"(g), "r"(h) : "memory");
+}
+template <int D>
+__device__ __forceinline__ void drafted_put32(const DraftedParams &p, int64_t row, int c, float (&o)[32], const DraftedRow &f) {
+#pragma unroll
+    for (int i = 0; i < 32; ++i) o[i] = f.a == 0.f ? 0.f : o[i] * f.a;
+    if (f.b != 0.f) {
+#pragma unroll
+        for (int i = 0; i < 32; i += 4) {
+            const float4 v = *reinterpret_cast<const float4 *>(p.in_o + row * D + c + i);
+            o[i] = fmaf(v.x, f.b, o[i]); o[i + 1] = fmaf(v.y, f.b, o[i + 1]); o[i + 2] = fmaf(v.z, f.b, o[i + 2]); o[i + 3] = fmaf(v.w, f.b, o[i + 3]);
+        }
+    }
+    if (p.mode == OUT_PARTIAL && c == 0) { p.pm[row] = f.m; p.pl[row] = f.l; }
+    if (p.mode == OUT_FINAL && p.out_bf16) {
+        __nv_bfloat16 *dst = static_cast<__nv_bfloat16 *>(p.out) + row * D + c;
+#pragma unroll
+        for (int i = 0; i < 32; i += 16)
+            drafted_st32(p.wide != 0, dst + i, pack_bf16(o[i], o[i + 1]), pack_bf16(o[i + 2], o[i + 3]), pack_bf16(o[i + 4], o[i + 5]), pack_bf16(o[i + 6], o[i + 7]),
+                         pack_bf16(o[i + 8], o[i + 9]), pack_bf16(o[i + 10], o[i + 11]), pack_bf16(o[i + 12], o[i + 13]), pack_bf16(o[i + 14], o[i + 15]));
+    } else {
+        float *dst = (p.mode == OUT_PARTIAL ? p.po : static_cast<float *>(p.out)) + row * D + c;
+#pragma unroll
+        for (int i = 0; i < 32; i += 8)
+            drafted_st32(p.wide != 0, dst + i, __float_as_uint(o[i]), __float_as_uint(o[i + 1]), __float_as_uint(o[i + 2]), __float_as_uint(o[i + 3]),
+                         __float_as_uint(o[i + 4]), __float_as_uint(o[i + 5]), __float_as_uint(o[i + 6]), __float_as_uint(o[i + 7]));
+    }
+}
+
 // The trees.  parent: the user's parents, -1 = the context.  Tokens above a token are found by walking up; `words` gets the bits of
 // those (and of the token itself) that the window and the sinks let it see.  Depths are how many steps the walk takes.
 __device__ __forceinline__ int drafted_depth(const int16_t *parent, int i) {
@@ -327,42 +368,54 @@ __device__ __forceinline__ void drafted_line(const DraftedParams &p, const Draft
 }
 
 // ---------------------------------------------------------------------------------------------------------------------
-// The join: CTA j takes a part of the items that the attention's CTA j left a piece of, in proportion to their pieces.
+// The join: CTAs (j, x, .) take a part of the item that the attention's CTA j left a piece of in its slot x, in proportion to the pieces; kDrJoin of
+// them share that part.
+constexpr int kDrJoin = 4;
 template <int D, int RT, bool LOG2>
 __global__ void __launch_bounds__(256) drafted_join_kernel(const __grid_constant__ DraftedParams p) {
     constexpr float kUnit = LOG2 ? 0.69314718055994531f : 1.f;
+    griddep_launch_dependents();        // what comes next may set itself up; it waits for this kernel's end before it looks at anything of this call
     griddep_wait();
-    for (int x = 0; x < 2; ++x) {
-        const int slot = 2 * blockIdx.x + x;
-        const int4 a = p.records[2 * slot], b = p.records[2 * slot + 1];
-        if (a.x == 0) continue;
-        const int u = a.y, tok0 = a.z, sq = a.w, toks = b.x, c0 = b.y, c1 = b.z, pieces = c1 - c0 + 1, rows = toks * p.hs;
-        const int h0 = sq / p.hgroups * p.g + sq % p.hgroups * p.hs;
-        const bool bad = p.bad[u] == p.epoch;
-        const int E = rows * (D / 4), mine = blockIdx.x - c0;
-        const int e0 = static_cast<int>(static_cast<int64_t>(E) * mine / pieces), e1 = static_cast<int>(static_cast<int64_t>(E) * (mine + 1) / pieces);
-        for (int e = e0 + threadIdx.x; e < e1; e += 256) {
-            const int r = e % rows, c = e / rows;
-            float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-            float m = -INFINITY, l = 0.f;
-#pragma unroll 4
-            for (int k = 0; k < pieces; ++k) {
-                const float *s = p.scratch + static_cast<size_t>(2 * (c0 + k) + (k == 0 ? 1 : 0)) * drafted_slot_floats(D, RT);
-                const float mk = s[RT * D + r], lk = s[RT * (D + 1) + r];
-                const float4 v = reinterpret_cast<const float4 *>(s)[c * RT + r];
-                const float M = fmaxf(m, mk);
-                const float wa = m == -INFINITY ? 0.f : (LOG2 ? exp2f(m - M) : expf(m - M));
-                const float wb = mk == -INFINITY ? 0.f : (LOG2 ? exp2f(mk - M) : expf(mk - M));
-                l = (l != l ? l : l * wa) + (lk != lk ? lk : wb != 0.f ? lk * wb : 0.f);
-                o.x = o.x * wa + (wb != 0.f ? v.x * wb : 0.f);
-                o.y = o.y * wa + (wb != 0.f ? v.y * wb : 0.f);
-                o.z = o.z * wa + (wb != 0.f ? v.z * wb : 0.f);
-                o.w = o.w * wa + (wb != 0.f ? v.w * wb : 0.f);
-                m = M;
+    const int slot = 2 * blockIdx.x + blockIdx.y;
+    const int4 a = p.records[2 * slot], b = p.records[2 * slot + 1];
+    if (a.x == 0) return;
+    const int u = a.y, tok0 = a.z, sq = a.w, toks = b.x, c0 = b.y, c1 = b.z, pieces = c1 - c0 + 1, rows = toks * p.hs;
+    const int h0 = sq / p.hgroups * p.g + sq % p.hgroups * p.hs;
+    const bool bad = p.bad[u] == p.epoch;
+    const int E = rows * (D / 4), parts = pieces * kDrJoin, mine = (static_cast<int>(blockIdx.x) - c0) * kDrJoin + blockIdx.z;
+    const int e0 = static_cast<int>(static_cast<int64_t>(E) * mine / parts), e1 = static_cast<int>(static_cast<int64_t>(E) * (mine + 1) / parts);
+    for (int e = e0 + threadIdx.x; e < e1; e += 256) {
+        const int r = e % rows, c = e / rows;
+        float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+        float m = -INFINITY, l = 0.f;
+        for (int k0 = 0; k0 < pieces; k0 += 8) {              // eight pieces under way at a time
+            float mk[8], lk[8];
+            float4 v[8];
+#pragma unroll
+            for (int y = 0; y < 8; ++y) {
+                mk[y] = -INFINITY; lk[y] = 0.f;
+                if (k0 + y < pieces) {
+                    const float *s = p.scratch + static_cast<size_t>(2 * (c0 + k0 + y) + (k0 + y == 0 ? 1 : 0)) * drafted_slot_floats(D, RT);
+                    mk[y] = s[RT * D + r]; lk[y] = s[RT * (D + 1) + r];
+                    v[y] = reinterpret_cast<const float4 *>(s)[c * RT + r];
+                }
             }
-            const int64_t row = (static_cast<int64_t>(tok0) + r / p.hs) * p.Hq + h0 + r % p.hs;
-            drafted_put4<D>(p, row, c, o, drafted_row(p, row, m * kUnit, l, bad));
+            float M = m;
+#pragma unroll
+            for (int y = 0; y < 8; ++y) M = fmaxf(M, mk[y]);
+            const float wa = m == -INFINITY ? 0.f : (LOG2 ? exp2f(m - M) : expf(m - M));
+            l = l != l ? l : l * wa;
+            o.x *= wa; o.y *= wa; o.z *= wa; o.w *= wa;
+#pragma unroll
+            for (int y = 0; y < 8; ++y) {
+                const float wb = mk[y] == -INFINITY ? 0.f : (LOG2 ? exp2f(mk[y] - M) : expf(mk[y] - M));
+                l += lk[y] != lk[y] ? lk[y] : wb != 0.f ? lk[y] * wb : 0.f;
+                if (wb != 0.f) { o.x = fmaf(v[y].x, wb, o.x); o.y = fmaf(v[y].y, wb, o.y); o.z = fmaf(v[y].z, wb, o.z); o.w = fmaf(v[y].w, wb, o.w); }
+            }
+            m = M;
         }
+        const int64_t row = (static_cast<int64_t>(tok0) + r / p.hs) * p.Hq + h0 + r % p.hs;
+        drafted_put4<D>(p, row, c, o, drafted_row(p, row, m * kUnit, l, bad));
     }
 }
 

@@ -41,6 +41,7 @@ __global__ void __launch_bounds__(DraftedFma<D, RT>::kThreads) drafted_fma_kerne
     __shared__ uint32_t lines[RT][kDrWords];
     const int tid = threadIdx.x, lane = tid & 31, tx = tid & 15, ty = tid >> 4;
     int Cu, chunks;
+    griddep_wait();
     const int64_t W = drafted_sums<NT>(p, sums, &first_bad, Cu, chunks);
     if (blockIdx.x == 0 && tid == 0) drafted_header(p, first_bad);
     if (tid < 4) p.records[4 * blockIdx.x + tid] = make_int4(0, 0, 0, 0);

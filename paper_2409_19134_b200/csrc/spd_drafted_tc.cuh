@@ -11,10 +11,10 @@
 // SPD_ERR_TIMEOUT once all its threads have come to the common end.
 //
 // Masks: a row sees one or two intervals of the context (window, sinks) and a set of drafted tokens (bits per token).  A warp builds them,
-// 16 bits per page, only in blocks that some of its rows do not see whole.  A hidden key's weight is 0, but 0 * NaN is NaN: the guards look
-// through the V rows of such blocks, clear slots that hold no token and rows that nobody sees, and where a row that is not finite is hidden from
-// some rows and visible to others, the rows of the piece are done again one by one.  So are rows whose weighted sums left fp32's range
-// (weights are relative to a reference that may lag 2^8 behind the maximum).
+// 16 bits per page, only in blocks that some of its rows do not see whole.  A hidden key's weight is 0, but 0 * NaN is NaN: the guards clear the
+// slots of V that hold no token; where a token's V row is not finite, the sums of all rows are not either, and such rows are done again one by one,
+// without a look at what they do not see.  So are rows whose sums left fp32's range by themselves (weights are relative to a reference
+// that may lag 2^8 behind the maximum).
 #pragma once
 
 #include "spd_drafted.cuh"
@@ -34,7 +34,7 @@ struct DrPlan {
     int32_t tiles;                                   // tiles with rows
     int32_t b0, b1, whole, slot;                     // blocks of the piece; whether it is the whole item; else where it goes
     int32_t deepest;                                 // greatest depth of the tree (0 for runs)
-    int32_t bad, poisoned;
+    int32_t bad;
     DraftedUser s;
     DraftedKeys k;
     int16_t parent[kDrTree], depth[kDrTree];         // of all the user's drafted tokens
@@ -94,6 +94,9 @@ __device__ __forceinline__ DtWhole dt_whole(const DrPlan &pl, int lo, int hi) {
         w.b0 = max(pl.k.ns, np + up(max(lo, lp) - lp) + shift);
         w.b1 = np + static_cast<int>(min(static_cast<int64_t>(pl.s.lq), end - lp) / kPage) + shift;
     }
+    const int list = pl.k.ns + pl.k.e - pl.k.a;          // a run's tile may end in front of the partition's
+    w.a1 = min(w.a1, list);
+    w.b1 = min(w.b1, list);
     if (np > 0 && lp % kPage == 0 && w.a1 == w.b0) { w.a1 = w.b1; w.b0 = w.a0; }        // one page follows upon the other
     return w;
 }
@@ -208,6 +211,8 @@ drafted_tc_kernel(const __grid_constant__ DraftedTcParams q, const __grid_consta
     DrPlan *plans = reinterpret_cast<DrPlan *>(behind + kDtBarBytes + sizeof(DtExchange));
     const int tid = threadIdx.x, wid = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31;
 
+    if (tid == 320) { prefetch_tensormap(&mq); prefetch_tensormap(&mk0); prefetch_tensormap(&mv0); prefetch_tensormap(&mk1); prefetch_tensormap(&mv1); }
+    griddep_wait();
     // ---- the cut: sums over the users in what becomes the K ring, the share's first item by the planning warp
     int64_t *sums = reinterpret_cast<int64_t *>(base + 2 * QTILE);
     int Cu, chunks;
@@ -221,7 +226,6 @@ drafted_tc_kernel(const __grid_constant__ DraftedTcParams q, const __grid_consta
     DraftedWalk w;
     if (wid == 12) drafted_locate(p, sums, Cu, chunks, x, lane, w);
     if (tid == 320) {
-        prefetch_tensormap(&mq); prefetch_tensormap(&mk0); prefetch_tensormap(&mv0); prefetch_tensormap(&mk1); prefetch_tensormap(&mv1);
         for (int b = 0; b < NBARS; ++b) {
             // Q and ring slots free: one per tile; S in registers, P written: one per softmax warp of the tile; rows exchanged, O's
             // read: one per softmax warp; V looked through: one per guard; plan read: one per warp
@@ -321,7 +325,10 @@ drafted_tc_kernel(const __grid_constant__ DraftedTcParams q, const __grid_consta
                 if (!whole) {
                     uint32_t m16[kDtPages];
 #pragma unroll
-                    for (int y = 0; y < kDtPages; ++y) m16[y] = live ? dt_sees(p, pl, tl[y], it, pos) : 0u;
+                    for (int y = 0; y < kDtPages; ++y) {
+                        const int e = tl[y].x + kPage - 1;
+                        m16[y] = tl[y].y == kPage && e <= full_hi && (tl[y].x >= full_lo || e < p.sinks) ? 0xffffu : dt_sees(p, pl, tl[y], tok, pos);
+                    }
                     see[0] = m16[0] | m16[1] << 16; see[1] = m16[2] | m16[3] << 16; see[2] = m16[4];
                 }
                 auto seen = [&](int y) { return (see[y >> 5] >> (y & 31)) & 1u; };
@@ -459,11 +466,12 @@ drafted_tc_kernel(const __grid_constant__ DraftedTcParams q, const __grid_consta
                 l *= a0;
             }
             // read only now: a tile without blocks of its own has waited for nobody before the exchange
-            const bool poisoned = *const_cast<volatile int32_t *>(&pl.poisoned) != 0, bad = *const_cast<volatile int32_t *>(&pl.bad) != 0;
+            const bool bad = *const_cast<volatile int32_t *>(&pl.bad) != 0;
             bool over = false;
-            if (ok && mine && (!poisoned || bad)) {
+            if (ok && mine) {
                 DraftedRow f{};
-                if (live && pl.whole) f = drafted_row(p, row, top * 0.69314718055994531f, l, bad);
+                const bool whole_item = pl.whole != 0;
+                if (live && whole_item) f = drafted_row(p, row, top * 0.69314718055994531f, l, bad);
                 float big = 0.f;
                 // a shared row's channels go half by either tile's thread
                 const int c_end = shared ? (t + 1) * (D / 2) : D;
@@ -482,19 +490,21 @@ drafted_tc_kernel(const __grid_constant__ DraftedTcParams q, const __grid_consta
                     }
                     if (live) {
 #pragma unroll
-                        for (int y = 0; y < 32; y += 4) {
-                            big = fmax3_abs_nan(fmax3_abs_nan(big, ov[y], ov[y + 1]), ov[y + 2], ov[y + 3]);
-                            const float4 o4 = make_float4(ov[y], ov[y + 1], ov[y + 2], ov[y + 3]);
-                            if (pl.whole) drafted_put4<D>(p, row, (c + y) / 4, o4, f);
-                            else reinterpret_cast<float4 *>(dst)[(c + y) / 4 * kDtRows + slot_row] = o4;
+                        for (int y = 0; y < 32; y += 4) big = fmax3_abs_nan(fmax3_abs_nan(big, ov[y], ov[y + 1]), ov[y + 2], ov[y + 3]);
+                        if (whole_item) {
+                            drafted_put32<D>(p, row, c, ov, f);
+                        } else {
+#pragma unroll
+                            for (int y = 0; y < 32; y += 4)
+                                reinterpret_cast<float4 *>(dst)[(c + y) / 4 * kDtRows + slot_row] = make_float4(ov[y], ov[y + 1], ov[y + 2], ov[y + 3]);
                         }
                     }
                     __syncwarp();
                 }
-                if (live && !pl.whole && (!shared || t == 0)) { dst[kDtRows * D + slot_row] = top; dst[kDtRows * (D + 1) + slot_row] = l; }
+                if (live && !whole_item && (!shared || t == 0)) { dst[kDtRows * D + slot_row] = top; dst[kDtRows * (D + 1) + slot_row] = l; }
                 over = live && !bad && l > 0.f && l < INFINITY && !(big < INFINITY);
             }
-            uint32_t again = __ballot_sync(0xffffffffu, ok && mine && (poisoned && !bad ? live : over));
+            uint32_t again = __ballot_sync(0xffffffffu, over);
             if (shared) {
                 // the other tile may not write its next O before this one's is read; rows that are done again wait for both halves
                 if (lane == 0) ex.again[t][wid & 3] = again;
@@ -558,7 +568,7 @@ drafted_tc_kernel(const __grid_constant__ DraftedTcParams q, const __grid_consta
                 pl.h0 = kvh * p.g + w.sq % p.hgroups * p.hs;
                 pl.tiles = toks > q.tpt ? 2 : 1;
                 pl.b0 = b0; pl.b1 = b1; pl.whole = whole; pl.slot = slot; pl.deepest = deepest;
-                pl.bad = !w.s.good || wrong; pl.poisoned = 0;
+                pl.bad = !w.s.good || wrong;
                 pl.s = w.s; pl.k = w.k;
                 if (!whole) drafted_record(p, w, slot, W, shares);
             }
@@ -631,15 +641,13 @@ drafted_tc_kernel(const __grid_constant__ DraftedTcParams q, const __grid_consta
             }
         }
     } else if (wid >= 13) {
-        // ---------------- the guards: V rows of blocks with hidden keys, 16-byte chunks in turns
-        constexpr int CHUNKS = KB * 8 * BOXES, PER = (CHUNKS + 32 * kDtGuards - 1) / (32 * kDtGuards);
-        const bool tree = p.parents != nullptr;
+        // ---------------- the guards: slots of V that hold no token, in the last pages of a partition and behind the list's end
         int c = 0;
         for (int r = 0; ok; ++r) {
-            DrPlan &pl = plan_of(r);
+            const DrPlan &pl = plan_of(r);
             if (!ok || !pl.valid) break;
-            const int ctx = pl.s.ctx, b0 = pl.b0;
-            const DtWhole dw = dt_whole(pl, p.window > 0 ? ctx + (tree ? pl.deepest : pl.i0 + pl.toks - 1) - p.window + 1 : 0, tree ? ctx - 1 : ctx + pl.i0);
+            const int b0 = pl.b0;
+            const DtWhole dw = dt_whole(pl, 0, 0x7ffffffe);     // full pages
             for (int b = pl.b1 - 1; b >= b0 && ok; --b, ++c) {
                 // every block passes through here, so that no guard is ever a whole ring ahead of or behind the others
                 const int slot = c % NSV, v = b * kDtPages;
@@ -647,43 +655,13 @@ drafted_tc_kernel(const __grid_constant__ DraftedTcParams q, const __grid_consta
                 __syncwarp();
                 if (!dw.holds(v)) {
                     uint8_t *vt = base + 2 * QTILE + (NSK + slot) * TILE;
-                    int cnt[kDtPages];
-#pragma unroll
-                    for (int y = 0; y < kDtPages; ++y) cnt[y] = dt_tile(pl, v + y).y;
-                    uint32_t any = 0;
-#pragma unroll
-                    for (int z = 0; z < PER; ++z) {
-                        const int e = (z * kDtGuards + wid - 13) * 32 + lane, key = e >> 3;       // chunk e & 7 of row `key`, box after box
-                        if (e >= CHUNKS) continue;
-                        const int box = BOXES > 1 && key >= KB ? 1 : 0, k = key - box * KB, y = k >> 4;
-                        uint4 *chunk = reinterpret_cast<uint4 *>(vt + box * kStBox + k * 128 + (e & 7) * 16);
-                        const int n = y == 0 ? cnt[0] : y == 1 ? cnt[1] : y == 2 ? cnt[2] : y == 3 ? cnt[3] : cnt[4];
-                        if ((k & 15) >= n) *chunk = make_uint4(0, 0, 0, 0);      // holds no token
-                        else any |= st_not_finite(*chunk);
-                    }
-                    if (__any_sync(0xffffffffu, any != 0)) {                     // rare: row by row, each guard those where it found something
 #pragma unroll 1
-                        for (int z = 0; z < PER; ++z) {
-                            const int e = (z * kDtGuards + wid - 13) * 32 + lane, key = e >> 3;
-                            const int box = BOXES > 1 && key >= KB ? 1 : 0, k = key - box * KB;
-                            uint4 *chunk = reinterpret_cast<uint4 *>(vt + box * kStBox + k * 128 + (e & 7) * 16);
-                            uint32_t found = __ballot_sync(0xffffffffu, e < CHUNKS && st_not_finite(*(e < CHUNKS ? chunk : reinterpret_cast<uint4 *>(vt))) != 0);
-                            while (found != 0) {
-                                const int row = __shfl_sync(0xffffffffu, k, __ffs(found) - 1);
-                                const int2 tl = dt_tile(pl, v + row / kPage);
-                                bool sees = false, not_all = false;
-                                for (int y = lane; y < pl.toks; y += 32) {
-                                    const bool s1 = (dt_sees(p, pl, tl, y, ctx + (tree ? pl.depth[pl.i0 + y] : pl.i0 + y)) >> (row % kPage)) & 1u;
-                                    sees = sees || s1;
-                                    not_all = not_all || !s1;
-                                }
-                                if (!__any_sync(0xffffffffu, sees)) {
-                                    if (e < CHUNKS && k == row) *chunk = make_uint4(0, 0, 0, 0);
-                                } else if (__any_sync(0xffffffffu, not_all)) {
-                                    pl.poisoned = 1;
-                                }
-                                found &= ~__ballot_sync(0xffffffffu, k == row);
-                            }
+                    for (int y = 0; y < kDtPages; ++y) {
+                        const int n = dt_tile(pl, v + y).y, chunks = (kPage - n) * 8;      // 16-byte chunks of each box from row n on
+#pragma unroll 1
+                        for (int e = (wid - 13) * 32 + lane; e < chunks * BOXES; e += 32 * kDtGuards) {
+                            const int box = BOXES > 1 && e >= chunks ? 1 : 0;
+                            *reinterpret_cast<uint4 *>(vt + box * kStBox + (y * kPage + n) * 128 + (e - box * chunks) * 16) = make_uint4(0, 0, 0, 0);
                         }
                     }
                     fence_proxy_async();

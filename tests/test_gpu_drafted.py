@@ -237,3 +237,38 @@ def test_nothing_drafted():
     g = dr.OnDevice(w)
     assert g.fused().numel() == 0
     ok(g)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_outputs_at_odd_multiples_of_16_bytes(dtype):
+    w = dr.batch([3, 9], [40, 600], [5, 0], 8, 2, 128, "bf16", seed=93)
+    g = dr.OnDevice(w)
+    want, _, _, _, tol = dr.expected(w)
+    es = torch.finfo(dtype).bits // 8
+    room = torch.full((12 * 8 * 128 + 64,), float("nan"), dtype=dtype, device="cuda")
+    out = room[16 // es:16 // es + 12 * 8 * 128].view(12, 8, 128)
+    assert out.data_ptr() % 32 == 16
+    dr.close(g.fused(out=out), want, tol)
+    assert bool(torch.isnan(room[:16 // es]).all()) and bool(torch.isnan(room[16 // es + out.numel():]).all())
+    ok(g)
+
+
+@pytest.mark.parametrize("window,sinks", [(0, 0), (200, 20)])
+def test_what_shared_memory_held_before(window, sinks):
+    """Runs whose tiles of rows end in front of the partition's end leave parts of their last block unloaded: nothing of what an earlier
+    call left there (here: rows that are not finite) may enter."""
+    spoil = dr.batch([40, 40], [500, 300], [0, 0], 4, 2, 128, "bf16", seed=95, kind="run")
+    for part in (spoil.priv, spoil.pub):
+        part.v_pool.fill_(float("nan"))
+    s = dr.OnDevice(spoil)
+    w = dr.batch([500, 300, 77], [333, 70, 9], [0, 3, 0], 4, 2, 128, "bf16", seed=96, kind="run")
+    g = dr.OnDevice(w, window=window, sinks=sinks)
+    first = g.fused()
+    rows = set(range(0, 877, 23))
+    want, _, _, _, tol = dr.expected(w, window=window, sinks=sinks, rows=rows)
+    at = torch.tensor(sorted(rows))
+    dr.close(first[at.cuda()], want[at], tol[at])
+    for _ in range(3):
+        s.fused()
+        assert torch.equal(g.fused(), first)
+    ok(g)
