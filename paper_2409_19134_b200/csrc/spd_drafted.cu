@@ -1,6 +1,7 @@
 // Attention of drafted tokens: argument checks, choice of the kernel, launches.
 #include <cmath>
 #include <cstdio>
+#include <cstring>
 #include <mutex>
 
 #include "spd_drafted.cuh"
@@ -18,6 +19,8 @@ int heads_per_tile(int g, int RT) { return g <= RT ? g : kHeadsPerItem; }
 
 constexpr int kFmaPerSm = 2;        // CTAs of the largest FMA variant that share an SM; the others fit more
 constexpr int kMostFmaRows = 64;
+constexpr int kTcOverhead = 2;      // what an item costs beside its blocks, in blocks
+constexpr int kFmaOverhead = 0;
 
 // Behind the workspace's head: records and slots of the pieces.
 struct DraftedLayout { size_t records, scratch, total; };
@@ -85,6 +88,13 @@ spd_status make_pool_map(CUtensorMap *map, const DraftedParams &p, const void *p
     return r == CUDA_SUCCESS ? SPD_OK : SPD_ERR_CUDA;
 }
 
+uint64_t twice(double x) {              // an fp32 value in both halves of a two-lane operand
+    const float f = static_cast<float>(x);
+    uint32_t u;
+    memcpy(&u, &f, 4);
+    return (static_cast<uint64_t>(u) << 32) | u;
+}
+
 template <int D, bool CAP, bool BIAS>
 spd_status launch_tc(const DraftedTcParams &p, const CUtensorMap *maps, cudaStream_t st) {
     static std::once_flag once[64];
@@ -112,9 +122,22 @@ spd_status run_tc(const DraftedParams &call, int D, int sms, cudaStream_t st) {
     d.bt = kDtPages;
     d.grid = sms;
     p.c2 = d.sm_scale * kLog2e;
+    d.ov = kTcOverhead;
+    p.half_at = p.one_at = -1.f;
     if (d.cap > 0.f) {
+        const double y1 = static_cast<double>(d.sm_scale) / d.cap;
         p.cap2 = d.cap * kLog2e;
-        p.y1 = static_cast<float>(fmin(static_cast<double>(d.sm_scale) / d.cap, 1e30));
+        p.y1 = static_cast<float>(fmin(y1, 1e30));
+        bool fits1 = true, fits2 = true;                  // coefficients that leave fp32's normal range: the exact form does it
+        auto normal = [](double c) { return fabs(c) > 1e-37 && fabs(c) < 1e37; };
+        for (int i = 0; i < 6; ++i) {
+            const double c = d.cap * 1.4426950408889634 * pow(y1, 2 * i + 1);
+            if (i < 4) { p.p1[i] = twice(c * kTanhHalf[i]); fits1 = fits1 && normal(c * kTanhHalf[i]); }
+            p.p2[i] = twice(c * kTanhOne[i]);
+            fits2 = fits2 && normal(c * kTanhOne[i]);
+        }
+        if (fits2) p.one_at = 1.f;
+        if (fits1 && fits2) p.half_at = 0.5f;             // where a mask comes on top of the cap, the longer one serves both ranges
     }
     // A tile whose rows are done one by one takes its warps about 4 us per key: 64 polls or so, beyond the usual limit.
     const int64_t keys = (static_cast<int64_t>(d.part[0].num_pages) + d.part[1].num_pages) * kPage, polls = static_cast<int64_t>(kWaitLimit) + 64 * keys;
@@ -154,6 +177,7 @@ spd_status launch_fma(DraftedParams p, int sms, cudaStream_t st) {
     p.tt = RT / p.hs;
     p.SQ = p.Hkv * p.hgroups;
     p.bt = kDrTiles;
+    p.ov = kFmaOverhead;
     p.grid = kFmaPerSm * sms;
     const spd_status rc = launch_early(drafted_fma_kernel<E, D, RT>, dim3(static_cast<unsigned>(p.grid)), C::kThreads, C::smem_bytes(), st, p);
     return rc != SPD_OK ? rc : launch_join<D, RT, false>(p, st);

@@ -17,7 +17,7 @@ namespace spd {
 
 constexpr int kDrTree = 256;              // most drafted tokens of a user that come as a tree
 constexpr int kDrWords = kDrTree / 32;
-constexpr int kDrMinBlocks = 2;           // do not cut the work into shares of fewer blocks
+constexpr int kDrMinBlocks = 1;           // do not cut the work into shares of less than that, and an item's own cost
 
 struct DraftedParams {
     int32_t B, Hq, Hkv, g;
@@ -25,6 +25,7 @@ struct DraftedParams {
     int32_t tt;                           // tokens per tile
     int32_t SQ;                           // Hkv * hgroups
     int32_t bt;                           // page tiles per block
+    int32_t ov;                           // what an item costs beside its blocks, in blocks: where the cut is made, it counts in front of them
     int64_t T;
     float sm_scale;
     const void *q;                        // [T][Hq][D]
@@ -59,42 +60,29 @@ struct DraftedUser {
     bool good;
 };
 
-// Tokens of user u, without a look at the cache; false where the offsets are inconsistent.
-__device__ __forceinline__ bool drafted_tokens(const DraftedParams &p, int u, int &first, int &n) {
-    if (p.tok_indptr == nullptr) { first = u; n = 1; return true; }
-    const int64_t a = p.tok_indptr[u], b = p.tok_indptr[u + 1];
-    first = static_cast<int>(a);
-    n = static_cast<int>(b - a);
-    return a >= 0 && b >= a && b <= p.T && (u != 0 || a == 0) && (u != p.B - 1 || b == p.T);
-}
-
-// A user whose tables, lengths or counts are inconsistent is not good: it has no keys, and its rows become zeros.
-// False where its offsets are inconsistent.
+// A user whose tables, lengths or counts are inconsistent is not good: it has no keys, and its rows become zeros.  False where its offsets
+// are inconsistent.  All loads are asked for before anything is decided.
 __device__ __forceinline__ bool drafted_user(const DraftedParams &p, int u, DraftedUser &s) {
-    const bool consistent = drafted_tokens(p, u, s.first, s.n);
-    int64_t len[2], base[2] = {0, 0};
-    bool good = true;
-#pragma unroll
-    for (int x = 0; x < 2; ++x) {
-        const PartDev &a = p.part[x];
-        if (a.present) {
-            const int64_t lo = a.indptr[u], hi = a.indptr[u + 1], end = a.indptr[p.B];
-            len[x] = a.lens[u];
-            base[x] = lo;
-            good = good && lo >= 0 && hi >= lo && hi <= end && len[x] >= 0 && len[x] <= (hi - lo) * kPage && (len[x] == 0 || a.indices != nullptr);
-        } else {
-            len[x] = p.peer_lens[x] ? p.peer_lens[x][u] : 0;
-            good = good && len[x] >= 0;
-        }
-    }
-    good = good && len[0] + len[1] <= 0x7fffffff && len[1] >= s.n && (p.parents == nullptr || s.n <= kDrTree);
+    const PartDev &A = p.part[0], &B = p.part[1];
+    const bool pa = A.present != 0, pb = B.present != 0, offsets = p.tok_indptr != nullptr;
+    const int64_t t0 = offsets ? p.tok_indptr[u] : u, t1 = offsets ? p.tok_indptr[u + 1] : u + 1;
+    const int64_t alo = pa ? A.indptr[u] : 0, ahi = pa ? A.indptr[u + 1] : 0, aend = pa ? A.indptr[p.B] : 0;
+    const int64_t blo = pb ? B.indptr[u] : 0, bhi = pb ? B.indptr[u + 1] : 0, bend = pb ? B.indptr[p.B] : 0;
+    const int32_t *la = pa ? A.lens : p.peer_lens[0], *lb = pb ? B.lens : p.peer_lens[1];
+    const int64_t alen = la ? la[u] : 0, blen = lb ? lb[u] : 0;
+    s.first = static_cast<int>(t0);
+    s.n = static_cast<int>(t1 - t0);
+    const bool consistent = t0 >= 0 && t1 >= t0 && t1 <= p.T && (u != 0 || t0 == 0) && (u != p.B - 1 || t1 == p.T);
+    bool good = alen >= 0 && blen >= s.n && alen + blen <= 0x7fffffff && (p.parents == nullptr || s.n <= kDrTree);
+    good = good && alo >= 0 && ahi >= alo && ahi <= aend && (!pa || alen <= (ahi - alo) * kPage) && (alen == 0 || !pa || A.indices != nullptr);
+    good = good && blo >= 0 && bhi >= blo && bhi <= bend && (!pb || blen <= (bhi - blo) * kPage) && (blen == 0 || !pb || B.indices != nullptr);
     s.good = good;
-    s.lp = good ? static_cast<int>(len[0]) : 0;
-    s.lq = good ? static_cast<int>(len[1]) : s.n;
+    s.lp = good ? static_cast<int>(alen) : 0;
+    s.lq = good ? static_cast<int>(blen) : s.n;
     s.ctx = s.lp + s.lq - s.n;
-    s.base0 = base[0]; s.base1 = base[1];
-    s.np = p.part[0].present && good ? (s.lp + kPage - 1) / kPage : 0;
-    s.nt = s.np + (p.part[1].present && good ? (s.lq + kPage - 1) / kPage : 0);
+    s.base0 = alo; s.base1 = blo;
+    s.np = pa && good ? (s.lp + kPage - 1) / kPage : 0;
+    s.nt = s.np + (pb && good ? (s.lq + kPage - 1) / kPage : 0);
     return consistent;
 }
 
@@ -134,25 +122,31 @@ __device__ __forceinline__ DraftedTile drafted_tile(const DraftedParams &p, cons
 }
 
 // ---------------------------------------------------------------------------------------------------------------------
-// The cut.  Blocks in the order user, row tile, (KV head, head group), block; W of them in `shares` shares.
+// The cut.  Units (an item's own cost, then its blocks) in the order user, row tile, (KV head, head group); W of them in `shares` shares.
+// A share that ends inside an item's own cost has none of its blocks.
 struct DraftedWalk {
     int u, rt, sq;             // the item
     DraftedUser s;
     DraftedKeys k;
-    int64_t x0;                // its first block among all
+    int64_t x0;                // its first unit among all
 };
 
-__device__ __forceinline__ int64_t drafted_bound(int64_t W, int shares, int c) { return W * c / shares; }
-__device__ __forceinline__ int drafted_share_of(int64_t W, int shares, int64_t x) { return static_cast<int>(((x + 1) * shares - 1) / W); }
+// Quotient of numbers that are not negative, in 32 bits where they fit (a division in 64 bits is some 100 instructions, one behind the other).
+__device__ __forceinline__ int64_t drafted_div(int64_t a, int64_t b) {
+    if (((a | b) >> 32) == 0) return static_cast<uint32_t>(a) / static_cast<uint32_t>(b);
+    return a / b;
+}
+__device__ __forceinline__ int64_t drafted_bound(int64_t W, int shares, int c) { return drafted_div(W * c, shares); }
+__device__ __forceinline__ int drafted_share_of(int64_t W, int shares, int64_t x) { return static_cast<int>(drafted_div((x + 1) * shares - 1, W)); }
 
 __device__ __forceinline__ void drafted_item_keys(const DraftedParams &p, DraftedWalk &w) {
     w.k = drafted_keys(p, w.s, w.rt * p.tt, min(w.s.n, (w.rt + 1) * p.tt));
 }
 
-// Blocks of one KV head and head group over tiles [rt0, rt1), every `step`-th.
+// Units of one KV head and head group over tiles from rt0 on, every `step`-th.
 __device__ __forceinline__ int64_t drafted_user_blocks(const DraftedParams &p, const DraftedUser &s, int rt0, int step) {
     int64_t sum = 0;
-    for (int rt = rt0; rt * p.tt < s.n; rt += step) sum += drafted_keys(p, s, rt * p.tt, min(s.n, (rt + 1) * p.tt)).nb;
+    for (int rt = rt0; rt * p.tt < s.n; rt += step) sum += drafted_keys(p, s, rt * p.tt, min(s.n, (rt + 1) * p.tt)).nb + p.ov;
     return sum;
 }
 
@@ -209,7 +203,7 @@ __device__ __forceinline__ int64_t drafted_sums(const DraftedParams &p, int64_t 
     return sums[chunks - 1];
 }
 
-// The item that holds block x, by one warp.
+// The item that holds unit x, by one warp.
 __device__ __forceinline__ void drafted_locate(const DraftedParams &p, const int64_t *sums, int C, int chunks, int64_t x, int lane, DraftedWalk &w) {
     int c = 0;
     for (int c0 = 0; c0 < chunks; c0 += 32) {
@@ -221,7 +215,7 @@ __device__ __forceinline__ void drafted_locate(const DraftedParams &p, const int
         drafted_user(p, w.u, w.s);
         for (int rt0 = 0; rt0 * p.tt < w.s.n; rt0 += 32) {
             const int rt = rt0 + lane;
-            const int64_t mine = rt * p.tt < w.s.n ? static_cast<int64_t>(drafted_keys(p, w.s, rt * p.tt, min(w.s.n, (rt + 1) * p.tt)).nb) * p.SQ : 0;
+            const int64_t mine = rt * p.tt < w.s.n ? static_cast<int64_t>(drafted_keys(p, w.s, rt * p.tt, min(w.s.n, (rt + 1) * p.tt)).nb + p.ov) * p.SQ : 0;
             int64_t inc = mine;
 #pragma unroll
             for (int d = 1; d < 32; d <<= 1) {
@@ -234,8 +228,8 @@ __device__ __forceinline__ void drafted_locate(const DraftedParams &p, const int
                 w.rt = rt0 + src;
                 at += __shfl_sync(0xffffffffu, inc - mine, src);
                 drafted_item_keys(p, w);
-                w.sq = static_cast<int>((x - at) / w.k.nb);
-                w.x0 = at + static_cast<int64_t>(w.sq) * w.k.nb;
+                w.sq = static_cast<int>(drafted_div(x - at, w.k.nb + p.ov));
+                w.x0 = at + static_cast<int64_t>(w.sq) * (w.k.nb + p.ov);
                 return;
             }
             at += __shfl_sync(0xffffffffu, inc, 31);
@@ -245,7 +239,7 @@ __device__ __forceinline__ void drafted_locate(const DraftedParams &p, const int
 
 // The next item; the caller knows that there is one.
 __device__ __forceinline__ void drafted_next(const DraftedParams &p, DraftedWalk &w) {
-    w.x0 += w.k.nb;
+    w.x0 += w.k.nb + p.ov;
     if (++w.sq < p.SQ) return;
     w.sq = 0;
     if (++w.rt * p.tt >= w.s.n) {
@@ -260,7 +254,16 @@ __device__ __forceinline__ void drafted_next(const DraftedParams &p, DraftedWalk
 __device__ __forceinline__ void drafted_record(const DraftedParams &p, const DraftedWalk &w, int slot, int64_t W, int shares) {
     const int i0 = w.rt * p.tt;
     p.records[2 * slot] = make_int4(1, w.u, w.s.first + i0, w.sq);
-    p.records[2 * slot + 1] = make_int4(min(p.tt, w.s.n - i0), drafted_share_of(W, shares, w.x0), drafted_share_of(W, shares, w.x0 + w.k.nb - 1), 0);
+    p.records[2 * slot + 1] = make_int4(min(p.tt, w.s.n - i0), drafted_share_of(W, shares, w.x0 + p.ov), drafted_share_of(W, shares, w.x0 + p.ov + w.k.nb - 1), 0);
+}
+
+// The blocks [b0, b1) of the item that units [x, x1) hold; none where b0 == b1.
+__device__ __forceinline__ void drafted_blocks(const DraftedParams &p, const DraftedWalk &w, int64_t x, int64_t x1, int &b0, int &b1) {
+    b0 = static_cast<int>(max(x - w.x0 - p.ov, static_cast<int64_t>(0)));
+    b1 = static_cast<int>(max(min(static_cast<int64_t>(w.k.nb), x1 - w.x0 - p.ov), static_cast<int64_t>(0)));
+}
+__device__ __forceinline__ int drafted_shares(const DraftedParams &p, int64_t W) {
+    return static_cast<int>(min(static_cast<int64_t>(p.grid), drafted_div(W + p.ov + kDrMinBlocks - 1, p.ov + kDrMinBlocks)));
 }
 
 // Raises the status of a user.
@@ -316,39 +319,39 @@ __device__ __forceinline__ void drafted_put4(const DraftedParams &p, int64_t row
     else reinterpret_cast<float4 *>(p.out)[row * (D / 4) + c4] = y;
 }
 
-// 32 consecutive channels from c on of the row, 32 bytes at a time (a thread's neighbours write other rows: whole sectors).
-__device__ __forceinline__ void drafted_st32(bool wide, void *p, uint32_t a, uint32_t b, uint32_t c, uint32_t d, uint32_t e, uint32_t f, uint32_t g, uint32_t h) {
-    if (!wide) {                              // the output starts at an odd multiple of 16 bytes
-        static_cast<uint4 *>(p)[0] = make_uint4(a, b, c, d);
-        static_cast<uint4 *>(p)[1] = make_uint4(e, f, g, h);
-        return;
+// 16 consecutive channels from c on of the row, 32 bytes at a time (a thread's neighbours write other rows: whole sectors).
+__device__ __forceinline__ void drafted_st32(bool wide, void *p, const uint32_t *w) {
+    if (wide) {
+        asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};"
+                     ::"l"(p), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]), "r"(w[4]), "r"(w[5]), "r"(w[6]), "r"(w[7]) : "memory");
+    } else {                                  // the output starts at an odd multiple of 16 bytes
+        static_cast<uint4 *>(p)[0] = make_uint4(w[0], w[1], w[2], w[3]);
+        static_cast<uint4 *>(p)[1] = make_uint4(w[4], w[5], w[6], w[7]);
     }
-    asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "r"(a), "r"(b), "r"(c), "r"(d), "r"(e), "r"(f), "r"(g), "r"(h) : "memory");
 }
 template <int D>
-__device__ __forceinline__ void drafted_put32(const DraftedParams &p, int64_t row, int c, float (&o)[32], const DraftedRow &f) {
+__device__ __forceinline__ void drafted_put16(const DraftedParams &p, int64_t row, int c, float (&o)[16], const DraftedRow &f) {
 #pragma unroll
-    for (int i = 0; i < 32; ++i) o[i] = f.a == 0.f ? 0.f : o[i] * f.a;
+    for (int i = 0; i < 16; ++i) o[i] = f.a == 0.f ? 0.f : o[i] * f.a;
     if (f.b != 0.f) {
 #pragma unroll
-        for (int i = 0; i < 32; i += 4) {
+        for (int i = 0; i < 16; i += 4) {
             const float4 v = *reinterpret_cast<const float4 *>(p.in_o + row * D + c + i);
             o[i] = fmaf(v.x, f.b, o[i]); o[i + 1] = fmaf(v.y, f.b, o[i + 1]); o[i + 2] = fmaf(v.z, f.b, o[i + 2]); o[i + 3] = fmaf(v.w, f.b, o[i + 3]);
         }
     }
     if (p.mode == OUT_PARTIAL && c == 0) { p.pm[row] = f.m; p.pl[row] = f.l; }
+    uint32_t w[16];
     if (p.mode == OUT_FINAL && p.out_bf16) {
-        __nv_bfloat16 *dst = static_cast<__nv_bfloat16 *>(p.out) + row * D + c;
 #pragma unroll
-        for (int i = 0; i < 32; i += 16)
-            drafted_st32(p.wide != 0, dst + i, pack_bf16(o[i], o[i + 1]), pack_bf16(o[i + 2], o[i + 3]), pack_bf16(o[i + 4], o[i + 5]), pack_bf16(o[i + 6], o[i + 7]),
-                         pack_bf16(o[i + 8], o[i + 9]), pack_bf16(o[i + 10], o[i + 11]), pack_bf16(o[i + 12], o[i + 13]), pack_bf16(o[i + 14], o[i + 15]));
+        for (int i = 0; i < 8; ++i) w[i] = pack_bf16(o[2 * i], o[2 * i + 1]);
+        drafted_st32(p.wide != 0, static_cast<__nv_bfloat16 *>(p.out) + row * D + c, w);
     } else {
-        float *dst = (p.mode == OUT_PARTIAL ? p.po : static_cast<float *>(p.out)) + row * D + c;
 #pragma unroll
-        for (int i = 0; i < 32; i += 8)
-            drafted_st32(p.wide != 0, dst + i, __float_as_uint(o[i]), __float_as_uint(o[i + 1]), __float_as_uint(o[i + 2]), __float_as_uint(o[i + 3]),
-                         __float_as_uint(o[i + 4]), __float_as_uint(o[i + 5]), __float_as_uint(o[i + 6]), __float_as_uint(o[i + 7]));
+        for (int i = 0; i < 16; ++i) w[i] = __float_as_uint(o[i]);
+        float *dst = (p.mode == OUT_PARTIAL ? p.po : static_cast<float *>(p.out)) + row * D + c;
+        drafted_st32(p.wide != 0, dst, w);
+        drafted_st32(p.wide != 0, dst + 8, w + 8);
     }
 }
 

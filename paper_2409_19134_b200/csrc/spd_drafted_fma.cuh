@@ -1,6 +1,6 @@
 // Drafted tokens on the FMA pipes: fp32 arithmetic throughout.
 //
-// RT rows (64, or 16 where users bring few) x 64 keys a block, 4 x 4 scores per thread; the 16 threads of a row keep its maximum and sum in
+// RT rows (64, or 16 where users bring few) x 64 keys a block, RPT x 4 scores per thread; the 16 threads of a row keep its maximum and sum in
 // registers, weights go through shared memory to the threads that hold the row's channels (the same 16).  A hidden key's weight is the
 // mark -1, which the product with V skips: whatever its rows of k and v hold never enters.
 #pragma once
@@ -14,7 +14,8 @@ constexpr int kDrTiles = kDrBlock / kPage;
 
 template <int D, int RT>
 struct DraftedFma {
-    static constexpr int kThreads = RT * 4, kPitch = D + 4;       // rows of Q, K and V: 16-byte reads of 8 lanes fall in 32 banks
+    static constexpr int RPT = RT == 16 ? 2 : 4;                  // rows per thread
+    static constexpr int kThreads = RT / RPT * 16, kPitch = D + 4;       // rows of Q, K and V: 16-byte reads of 8 lanes fall in 32 banks
     static constexpr size_t smem_bytes() { return (static_cast<size_t>(RT + 2 * kDrBlock) * kPitch + RT * kDrBlock) * 4; }
 };
 
@@ -29,7 +30,7 @@ template <> __device__ __forceinline__ float4 drafted_load4<__nv_bfloat16>(const
 template <typename E, int D, int RT>
 __global__ void __launch_bounds__(DraftedFma<D, RT>::kThreads) drafted_fma_kernel(const __grid_constant__ DraftedParams p) {
     using C = DraftedFma<D, RT>;
-    constexpr int NT = C::kThreads, PITCH = C::kPitch, KB = kDrBlock, CH = D / 64;      // CH chunks of four channels per thread
+    constexpr int NT = C::kThreads, RPT = C::RPT, PITCH = C::kPitch, KB = kDrBlock, CH = D / 64;      // CH chunks of four channels per thread
     extern __shared__ __align__(16) float sm[];
     float *Qs = sm, *Ks = Qs + RT * PITCH, *Vs = Ks + KB * PITCH, *Ps = Vs + KB * PITCH;
     __shared__ int64_t sums[NT];
@@ -46,14 +47,17 @@ __global__ void __launch_bounds__(DraftedFma<D, RT>::kThreads) drafted_fma_kerne
     if (blockIdx.x == 0 && tid == 0) drafted_header(p, first_bad);
     if (tid < 4) p.records[4 * blockIdx.x + tid] = make_int4(0, 0, 0, 0);
     __syncthreads();
-    const int shares = static_cast<int>(min(static_cast<int64_t>(p.grid), (W + kDrMinBlocks - 1) / kDrMinBlocks));
+    const int shares = drafted_shares(p, W);
     if (static_cast<int>(blockIdx.x) >= shares) return;
     int64_t x = drafted_bound(W, shares, blockIdx.x);
     const int64_t x1 = drafted_bound(W, shares, blockIdx.x + 1);
     DraftedWalk w;
     drafted_locate(p, sums, Cu, chunks, x, lane, w);
-    while (true) {
-        const int b0 = static_cast<int>(x - w.x0), b1 = static_cast<int>(min(static_cast<int64_t>(w.k.nb), x1 - w.x0));
+    for (;; drafted_next(p, w)) {
+        int b0, b1;
+        drafted_blocks(p, w, x, x1, b0, b1);
+        x = w.x0 + p.ov + w.k.nb;                 // the next item, if it is this share's
+        if (b0 == b1) break;
         const DraftedUser s = w.s;
         const int i0 = w.rt * p.tt, toks = min(p.tt, s.n - i0), rows = toks * p.hs;
         const int kvh = w.sq / p.hgroups, h0 = kvh * p.g + w.sq % p.hgroups * p.hs;
@@ -79,11 +83,11 @@ __global__ void __launch_bounds__(DraftedFma<D, RT>::kThreads) drafted_fma_kerne
             for (int i = tid; i < toks; i += NT) drafted_line(p, s, parent, i0 + i, depths[i0 + i], lines[i]);
         }
         __syncthreads();
-        int pos[4], tok[4];              // positions and tokens (within the tile) of the thread's rows
-        float slope[4], m[4], l[4], o[4][4 * CH];
+        int pos[RPT], tok[RPT];              // positions and tokens (within the tile) of the thread's rows
+        float slope[RPT], m[RPT], l[RPT], o[RPT][4 * CH];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int r = min(4 * ty + i, rows - 1);
+        for (int i = 0; i < RPT; ++i) {
+            const int r = min(RPT * ty + i, rows - 1);
             tok[i] = r / p.hs;
             pos[i] = s.ctx + (p.parents ? (s.good ? depths[i0 + tok[i]] : 0) : i0 + tok[i]);
             slope[i] = p.slopes ? p.slopes[h0 + r % p.hs] : 0.f;
@@ -115,21 +119,21 @@ __global__ void __launch_bounds__(DraftedFma<D, RT>::kThreads) drafted_fma_kerne
 #pragma unroll
             for (int t = 0; t < kDrTiles; ++t) bad = bad || tile_page[t] == -1;
             __syncthreads();
-            if ((tid & ~31) / 16 * 4 < rows) {            // warps without a row have nothing to do
-                float sc[4][4];
+            if ((tid & ~31) / 16 * RPT < rows) {            // warps without a row have nothing to do
+                float sc[RPT][4];
 #pragma unroll
-                for (int i = 0; i < 4; ++i)
+                for (int i = 0; i < RPT; ++i)
 #pragma unroll
                     for (int j = 0; j < 4; ++j) sc[i][j] = 0.f;
 #pragma unroll 4
                 for (int c = 0; c < D; c += 4) {
-                    float4 a[4], k4[4];
+                    float4 a[RPT], k4[4];
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) a[i] = *reinterpret_cast<const float4 *>(Qs + (4 * ty + i) * PITCH + c);
+                    for (int i = 0; i < RPT; ++i) a[i] = *reinterpret_cast<const float4 *>(Qs + (RPT * ty + i) * PITCH + c);
 #pragma unroll
                     for (int j = 0; j < 4; ++j) k4[j] = *reinterpret_cast<const float4 *>(Ks + (tx + 16 * j) * PITCH + c);
 #pragma unroll
-                    for (int i = 0; i < 4; ++i)
+                    for (int i = 0; i < RPT; ++i)
 #pragma unroll
                         for (int j = 0; j < 4; ++j) {
                             sc[i][j] = fmaf(a[i].x, k4[j].x, sc[i][j]); sc[i][j] = fmaf(a[i].y, k4[j].y, sc[i][j]);
@@ -137,7 +141,7 @@ __global__ void __launch_bounds__(DraftedFma<D, RT>::kThreads) drafted_fma_kerne
                         }
                 }
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
+                for (int i = 0; i < RPT; ++i) {
                     bool seen[4];
                     float mx = -INFINITY;
 #pragma unroll
@@ -168,7 +172,7 @@ __global__ void __launch_bounds__(DraftedFma<D, RT>::kThreads) drafted_fma_kerne
 #pragma unroll
                     for (int j = 0; j < 4; ++j) {
                         const float wt = seen[j] ? expf(sc[i][j] - ref) : -1.f;
-                        Ps[(4 * ty + i) * KB + tx + 16 * j] = wt;
+                        Ps[(RPT * ty + i) * KB + tx + 16 * j] = wt;
                         sum += seen[j] ? wt : 0.f;
                     }
 #pragma unroll
@@ -181,16 +185,16 @@ __global__ void __launch_bounds__(DraftedFma<D, RT>::kThreads) drafted_fma_kerne
                 __syncwarp();
 #pragma unroll 2
                 for (int k4 = 0; k4 < KB; k4 += 4) {
-                    float4 wt[4];
+                    float4 wt[RPT];
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) wt[i] = *reinterpret_cast<const float4 *>(Ps + (4 * ty + i) * KB + k4);
+                    for (int i = 0; i < RPT; ++i) wt[i] = *reinterpret_cast<const float4 *>(Ps + (RPT * ty + i) * KB + k4);
 #pragma unroll
                     for (int k = 0; k < 4; ++k) {
                         float4 v[CH];
 #pragma unroll
                         for (int c = 0; c < CH; ++c) v[c] = *reinterpret_cast<const float4 *>(Vs + (k4 + k) * PITCH + 4 * (tx + 16 * c));
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) {
+                        for (int i = 0; i < RPT; ++i) {
                             const float q = k == 0 ? wt[i].x : k == 1 ? wt[i].y : k == 2 ? wt[i].z : wt[i].w;
                             if (q < 0.f) continue;
 #pragma unroll
@@ -209,8 +213,8 @@ __global__ void __launch_bounds__(DraftedFma<D, RT>::kThreads) drafted_fma_kerne
         const bool whole = b0 == 0 && b1 == w.k.nb;
         const int slot = 2 * blockIdx.x + (b0 == 0 ? 1 : 0);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int r = 4 * ty + i;
+        for (int i = 0; i < RPT; ++i) {
+            const int r = RPT * ty + i;
             if (r >= rows) continue;
             const int64_t row = (static_cast<int64_t>(s.first) + i0 + tok[i]) * p.Hq + h0 + r % p.hs;
             float *dst = p.scratch + static_cast<size_t>(slot) * drafted_slot_floats(D, RT);
@@ -225,9 +229,7 @@ __global__ void __launch_bounds__(DraftedFma<D, RT>::kThreads) drafted_fma_kerne
             if (!whole && tx == 0) { dst[RT * D + r] = m[i]; dst[RT * (D + 1) + r] = l[i]; }
         }
         if (!whole && tid == 0) drafted_record(p, w, slot, W, shares);
-        x = w.x0 + b1;
         if (x >= x1) break;
-        drafted_next(p, w);
     }
 }
 

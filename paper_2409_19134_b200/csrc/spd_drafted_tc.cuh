@@ -56,15 +56,27 @@ struct DraftedTcParams {
     int32_t tpt;                // tokens per tile
     float c2;                   // sm_scale log2(e)
     float cap2, y1;             // cap log2(e); sm_scale / cap
+    float half_at, one_at;      // where the two polynomials end (1/2 and 1; -1 = not to be used)
+    uint64_t p1[4], p2[6];      // of cap2 tanh(y1 x) = x P(x^2) for |y1 x| <= 1/2 and <= 1, each in both halves
     uint32_t wait_limit;
 };
 
 __device__ __forceinline__ uint32_t dt_low(int n) { return (1u << min(max(n, 0), 16)) - 1u; }       // bits 0 .. n - 1 of 16
 
-template <int K>
-__device__ __forceinline__ uint64_t dt_tanh() {                 // coefficient K of tanh(y) / y for |y| <= 1, in both halves
-    constexpr float f = static_cast<float>(kTanhOne[K]);
-    return pack_f32x2(f, f);
+// 16 consecutive fp32 columns of this thread's TMEM lane.
+__device__ __forceinline__ void dt_ld16(uint32_t taddr, float (&o)[16]) {
+    uint32_t r[16];
+    tmem_ld16_nowait(taddr, r);
+    tmem_wait_ld();
+#pragma unroll
+    for (int i = 0; i < 16; ++i) o[i] = __uint_as_float(r[i]);
+}
+__device__ __forceinline__ void dt_st16(uint32_t taddr, const float (&v)[16]) {
+    uint32_t r[16];
+#pragma unroll
+    for (int i = 0; i < 16; ++i) r[i] = __float_as_uint(v[i]);
+    tmem_st8(taddr, r);
+    tmem_st8(taddr + 8, r + 8);
 }
 
 // First position and tokens of page tile v of an item's list.
@@ -201,9 +213,10 @@ drafted_tc_kernel(const __grid_constant__ DraftedTcParams q, const __grid_consta
     uint64_t *bar_p = bars + 6, *bar_o = bars + 8;                 // per tile: P written; O has taken the block in (P is free)
     uint64_t *bar_plan = bars + 10, *bar_planfree = bars + 12;     // per plan buffer
     uint64_t *bar_x = bars + 14, *bar_y = bars + 15;               // a shared item's rows are exchanged; their O's are read
-    uint64_t *bar_k = bars + 16, *bar_kfree = bar_k + NSK, *bar_v = bar_kfree + NSK, *bar_vfree = bar_v + NSV;
+    uint64_t *bar_tree = bars + 16;                                // per plan buffer: the tree's part of the plan is there too
+    uint64_t *bar_k = bars + 18, *bar_kfree = bar_k + NSK, *bar_v = bar_kfree + NSK, *bar_vfree = bar_v + NSV;
     uint64_t *bar_guard = bar_vfree + NSV;                         // per V slot: the guards are done with the block
-    constexpr int NBARS = 16 + 2 * NSK + 3 * NSV;
+    constexpr int NBARS = 18 + 2 * NSK + 3 * NSV;
     static_assert(NBARS * 8 + 8 <= kDtBarBytes, "barrier block");
     uint32_t &tmem_slot = *reinterpret_cast<uint32_t *>(bars + NBARS);
     int &first_bad = *reinterpret_cast<int *>(&tmem_slot + 1);
@@ -219,7 +232,7 @@ drafted_tc_kernel(const __grid_constant__ DraftedTcParams q, const __grid_consta
     const int64_t W = drafted_sums<kDtThreads>(p, sums, &first_bad, Cu, chunks);
     if (blockIdx.x == 0 && tid == 0) drafted_header(p, first_bad);
     if (tid < 4) p.records[4 * blockIdx.x + tid] = make_int4(0, 0, 0, 0);
-    const int shares = static_cast<int>(min(static_cast<int64_t>(p.grid), (W + kDrMinBlocks - 1) / kDrMinBlocks));
+    const int shares = drafted_shares(p, W);
     if (static_cast<int>(blockIdx.x) >= shares) return;
     const int64_t x1 = drafted_bound(W, shares, blockIdx.x + 1);
     int64_t x = drafted_bound(W, shares, blockIdx.x);
@@ -229,7 +242,7 @@ drafted_tc_kernel(const __grid_constant__ DraftedTcParams q, const __grid_consta
         for (int b = 0; b < NBARS; ++b) {
             // Q and ring slots free: one per tile; S in registers, P written: one per softmax warp of the tile; rows exchanged, O's
             // read: one per softmax warp; V looked through: one per guard; plan read: one per warp
-            const int k = b - 16, n = b == 1 || (k >= NSK && k < 2 * NSK) || (k >= 2 * NSK + NSV && k < 2 * NSK + 2 * NSV) ? 2 : b >= 4 && b < 8 ? 4
+            const int k = b - 18, n = b == 1 || (k >= NSK && k < 2 * NSK) || (k >= 2 * NSK + NSV && k < 2 * NSK + 2 * NSV) ? 2 : b >= 4 && b < 8 ? 4
                                       : b == 14 || b == 15 ? 8 : k >= 2 * NSK + 2 * NSV ? kDtGuards : b >= 12 && b < 14 ? kDtConsumers : 1;
             mbar_init(smem_u32(&bars[b]), n);
         }
@@ -264,6 +277,8 @@ drafted_tc_kernel(const __grid_constant__ DraftedTcParams q, const __grid_consta
         for (int r = 0; ok; ++r) {
             DrPlan &pl = plan_of(r);
             if (!ok || !pl.valid) break;
+            wait(&bar_tree[r & 1], r >> 1);
+            __syncwarp();
             const bool shared = pl.tiles == 1;                // both tiles work for the first one's rows, every other block each
             const int nb = pl.b1 - pl.b0, nblk = shared ? (nb - t + 1) / 2 : nb, toks = pl.toks, ctx = pl.s.ctx, i0 = pl.i0;
             const int it = in_tile + (shared ? 0 : t * q.tpt), w0 = wt0 + (shared ? 0 : t * q.tpt), w1 = wt1 + (shared ? 0 : t * q.tpt);
@@ -276,124 +291,12 @@ drafted_tc_kernel(const __grid_constant__ DraftedTcParams q, const __grid_consta
             const int last_pos = tree ? 0x7fffffff : ctx + i0 + min(w1, toks - 1);
             const DtWhole dw = dt_whole(pl, full_lo, full_hi);
             const int vtop = (pl.b1 - 1 - (shared ? t : 0)) * kDtPages, vstep = (shared ? 2 : 1) * kDtPages;      // tiles of the first block; between blocks
-            const int prv = pl.k.ns - pl.k.a, pub = prv + pl.s.np, lp = pl.s.lp;      // list index of the first private and public tile
+            const int ns = pl.k.ns, prv = ns - pl.k.a, np = pl.s.np, pub = prv + np, lp = pl.s.lp, lpq = lp + pl.s.lq, list = prv + pl.k.e;
             const float slope2 = BIAS ? p.slopes[pl.h0 + hh] * kLog2e : 0.f;
             float l = 0.f, m = -INFINITY, top = -INFINITY;          // reference point and greatest score, log2 units
-            for (int i = 0; i < nblk && ok; ++i) {
-                const int v = vtop - i * vstep;
-                const bool whole = mine && dw.holds(v);
-                bool none = !mine;
-                int2 tl[kDtPages];
-                if (!whole) {
-                    none = true;
-#pragma unroll
-                    for (int y = 0; y < kDtPages; ++y) {
-                        tl[y] = dt_tile(pl, v + y);
-                        none = none && (tl[y].y == 0 || tl[y].x > last_pos);
-                    }
-                    none = none || !mine;
-                }
-                wait(&bar_s[t], n + i);
-                __syncwarp();
-                tc_fence_after();
-                if (none) {                                   // nobody in this warp sees any of it: weights 0
-                    if (lane == 0) mbar_arrive(smem_u32(&bar_sf[t]));
-                    if (n + i > 0) wait(&bar_o[t], n + i - 1);
-                    tc_fence_after();
-                    uint32_t z[32];
-#pragma unroll
-                    for (int y = 0; y < 32; ++y) z[y] = 0u;
-                    tmem_st32p(t_p, z);
-                    tmem_st8(t_p + 32, z);
-                    tmem_wait_st();
-                    tc_fence_before();
-                    __syncwarp();
-                    if (lane == 0) mbar_arrive(smem_u32(&bar_p[t]));
-                    continue;
-                }
-                uint32_t raw[KB];
-                tmem_ld64_nowait(t_s, raw);
-                tmem_ld16_nowait(t_s + 64, raw + 64);
-                tmem_wait_ld();
-                tc_fence_before();
-                __syncwarp();
-                if (lane == 0) mbar_arrive(smem_u32(&bar_sf[t]));       // the next block's S may be computed
-                float sv[KB];
-#pragma unroll
-                for (int y = 0; y < KB; ++y) sv[y] = __uint_as_float(raw[y]);
-                uint32_t see[3] = {0xffffffffu, 0xffffffffu, 0xffffu};
-                if (!whole) {
-                    uint32_t m16[kDtPages];
-#pragma unroll
-                    for (int y = 0; y < kDtPages; ++y) {
-                        const int e = tl[y].x + kPage - 1;
-                        m16[y] = tl[y].y == kPage && e <= full_hi && (tl[y].x >= full_lo || e < p.sinks) ? 0xffffu : dt_sees(p, pl, tl[y], tok, pos);
-                    }
-                    see[0] = m16[0] | m16[1] << 16; see[1] = m16[2] | m16[3] << 16; see[2] = m16[4];
-                }
-                auto seen = [&](int y) { return (see[y >> 5] >> (y & 31)) & 1u; };
-                constexpr bool kLog2 = CAP || BIAS;             // sv holds scores in log2 units from here on; q.k else
-                if constexpr (CAP) {
-                    // tanh by a polynomial where the whole warp's scores allow it (error 2.4e-7), else by the special-function unit
-                    float big[4] = {0.f, 0.f, 0.f, 0.f};
-                    if (!whole) {                               // hidden scores may be anything
-#pragma unroll
-                        for (int y = 0; y < KB; ++y) sv[y] = seen(y) ? sv[y] : 0.f;
-                    }
-#pragma unroll
-                    for (int y = 0; y < KB; y += 2) big[(y >> 1) & 3] = fmax3_abs_nan(big[(y >> 1) & 3], sv[y], sv[y + 1]);
-                    const float most = fmax3_abs_nan(fmax3_abs_nan(big[0], big[1], big[2]), big[3], 0.f) * q.y1;
-                    if (__all_sync(0xffffffffu, most <= 1.f)) {
-                        const uint64_t y12 = pack_f32x2(q.y1, q.y1), cap22 = pack_f32x2(q.cap2, q.cap2);
-#pragma unroll
-                        for (int y = 0; y < KB; y += 2) {
-                            const uint64_t a = mul_f32x2(pack_f32x2(sv[y], sv[y + 1]), y12), a2 = mul_f32x2(a, a);
-                            uint64_t f = fma_f32x2(a2, dt_tanh<5>(), dt_tanh<4>());
-                            f = fma_f32x2(f, a2, dt_tanh<3>());
-                            f = fma_f32x2(f, a2, dt_tanh<2>());
-                            f = fma_f32x2(f, a2, dt_tanh<1>());
-                            f = fma_f32x2(f, a2, dt_tanh<0>());
-                            unpack_f32x2(mul_f32x2(mul_f32x2(f, a), cap22), sv[y], sv[y + 1]);
-                        }
-                    } else {
-#pragma unroll
-                        for (int y = 0; y < KB; ++y) sv[y] = q.cap2 - __fdividef(2.f * q.cap2, ex2_approx(sv[y] * (2.f * kLog2e) * q.y1) + 1.f);
-                    }
-                }
-                if constexpr (BIAS) {
-                    const float scale = CAP ? 1.f : q.c2;
-                    if (whole) {                                       // the block's positions follow upon one another
-                        const float off = static_cast<float>((v >= pub ? lp + (v - pub) * kPage : (v - prv) * kPage) - pos);
-#pragma unroll
-                        for (int y = 0; y < KB; ++y) sv[y] = fmaf(slope2, off + static_cast<float>(y), sv[y] * scale);
-                    } else {
-#pragma unroll
-                        for (int y = 0; y < kDtPages; ++y) {
-                            const float off = static_cast<float>(tl[y].x - pos);
-                            if (tree && tl[y].x + tl[y].y > ctx) {     // drafted tokens count by depth
-#pragma unroll
-                                for (int z = 0; z < kPage; ++z) {
-                                    const int d = tl[y].x + z - ctx;
-                                    const float far = d >= 0 ? static_cast<float>(ctx - pos + pl.depth[min(d, kDrTree - 1)]) : off + static_cast<float>(z);
-                                    sv[16 * y + z] = fmaf(slope2, far, sv[16 * y + z] * scale);
-                                }
-                            } else {
-#pragma unroll
-                                for (int z = 0; z < kPage; ++z) sv[16 * y + z] = fmaf(slope2, off + static_cast<float>(z), sv[16 * y + z] * scale);
-                            }
-                        }
-                    }
-                }
-                if (!whole) {
-#pragma unroll
-                    for (int y = 0; y < KB; ++y) sv[y] = seen(y) ? sv[y] : -INFINITY;
-                }
-                // ---- the reference is the greatest score so far, or less by up to kPfSlack, so that O is hardly ever rescaled
-                bool o_ready = n + i == 0;                       // O has taken the block before in
-                float r4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-#pragma unroll
-                for (int y = 0; y < KB; y += 2) r4[(y >> 1) & 3] = fmax3(r4[(y >> 1) & 3], sv[y], sv[y + 1]);
-                const float mx = fmaxf(fmaxf(r4[0], r4[1]), fmaxf(r4[2], r4[3])), xmax = kLog2 ? mx : mx * q.c2;
+            // The reference is the greatest score so far, or less by up to kPfSlack, so that O is hardly ever rescaled.  o_ready: O has taken the
+            // block before in.
+            auto refer = [&](int i, float xmax, bool &o_ready) {
                 top = fmaxf(top, xmax);
                 if (__any_sync(0xffffffffu, xmax > m + kPfSlack)) {
                     const float m_new = (xmax > m + kPfSlack) ? xmax : m;
@@ -414,26 +317,164 @@ drafted_tc_kernel(const __grid_constant__ DraftedTcParams q, const __grid_consta
                         }
                     }
                 }
-                const float ref = m == -INFINITY ? 0.f : m;
-                const uint64_t mx2 = pack_f32x2(-ref, -ref), c22 = pack_f32x2(q.c2, q.c2);
-                // ---- weights 2^(score - reference), P, and their sum as they are rounded for the product with V: numerator and sum are off alike
-                uint64_t lsum2 = 0;                              // (+0, +0)
-                uint32_t pk[KB / 2];
-#pragma unroll
-                for (int y = 0; y < KB / 2; ++y) {
-                    float a0, a1;
-                    const uint64_t s2 = pack_f32x2(sv[2 * y], sv[2 * y + 1]);
-                    unpack_f32x2(kLog2 ? add_f32x2(s2, mx2) : fma_f32x2(s2, c22, mx2), a0, a1);
-                    pk[y] = pack_bf16(ex2_approx(a0), ex2_approx(a1));
-                    lsum2 = add_f32x2(lsum2, pack_f32x2(__uint_as_float(pk[y] << 16), __uint_as_float(pk[y] & 0xffff0000u)));
-                }
-                if (!o_ready) wait(&bar_o[t], n + i - 1);        // P of the block before has been read
+                return m == -INFINITY ? 0.f : m;
+            };
+            // Scores that the cap applies to, by the special-function unit, or by polynomials in x^2 that are multiplied by x.
+            auto capped = [&](float s) { return q.cap2 - __fdividef(2.f * q.cap2, ex2_approx(s * (2.f * kLog2e) * q.y1) + 1.f); };
+            auto poly1 = [&](uint64_t y) { return fma_f32x2(fma_f32x2(fma_f32x2(y, q.p1[3], q.p1[2]), y, q.p1[1]), y, q.p1[0]); };
+            auto poly2 = [&](uint64_t y) {
+                const uint64_t f = fma_f32x2(fma_f32x2(fma_f32x2(y, q.p2[5], q.p2[4]), y, q.p2[3]), y, q.p2[2]);
+                return fma_f32x2(fma_f32x2(f, y, q.p2[1]), y, q.p2[0]);
+            };
+            // Weights are summed as they are rounded for the product with V: numerator and sum are off alike.
+            uint64_t lsum2 = 0;
+            auto weigh = [&](uint64_t arg2) {
+                float x0, x1;
+                unpack_f32x2(arg2, x0, x1);
+                const uint32_t w = pack_bf16(ex2_approx(x0), ex2_approx(x1));
+                lsum2 = add_f32x2(lsum2, pack_f32x2(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u)));
+                return w;
+            };
+            for (int i = 0; i < nblk && ok; ++i) {
+                const int v = vtop - i * vstep;
+                bool o_ready = n + i == 0;
+                lsum2 = 0;                                        // (+0, +0)
+                wait(&bar_s[t], n + i);
+                __syncwarp();
                 tc_fence_after();
-                tmem_st32p(t_p, pk);
-                tmem_st8(t_p + 32, pk + 32);
+                if (!mine) {                                      // rows of nobody: what becomes of them does not matter
+                    if (lane == 0) mbar_arrive(smem_u32(&bar_sf[t]));
+                    if (n + i > 0) wait(&bar_o[t], n + i - 1);    // never a phase of P ahead of the others
+                    if (lane == 0) mbar_arrive(smem_u32(&bar_p[t]));
+                    continue;
+                }
+                if (dw.holds(v)) {
+                    // ---- all of the block's keys are seen by all rows of the warp
+                    uint32_t raw[KB];
+                    tmem_ld64_nowait(t_s, raw);
+                    tmem_ld16_nowait(t_s + 64, raw + 64);
+                    tmem_wait_ld();
+                    tc_fence_before();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(smem_u32(&bar_sf[t]));   // the next block's S may be computed
+                    float sv[KB];
+#pragma unroll
+                    for (int y = 0; y < KB; ++y) sv[y] = __uint_as_float(raw[y]);
+                    auto pair = [&](int y) { return pack_f32x2(sv[y], sv[y + 1]); };
+                    int form = 0;                                 // 1, 2: the polynomial that holds for the whole warp; 0: the special-function unit
+                    if constexpr (CAP) {
+                        float big[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                        for (int y = 0; y < KB; y += 2) big[(y >> 1) & 3] = fmax3_abs_nan(big[(y >> 1) & 3], sv[y], sv[y + 1]);
+                        const float most = fmax3_abs_nan(fmax3_abs_nan(big[0], big[1], big[2]), big[3], 0.f) * q.y1;
+                        form = __all_sync(0xffffffffu, most <= q.half_at) ? 1 : __all_sync(0xffffffffu, most <= q.one_at) ? 2 : 0;
+                    }
+                    if constexpr (CAP && BIAS) {                  // the bias comes on top of capped scores
+                        if (form != 0) {
+#pragma unroll
+                            for (int y = 0; y < KB; y += 2) { const uint64_t s2 = pair(y); unpack_f32x2(mul_f32x2(poly2(mul_f32x2(s2, s2)), s2), sv[y], sv[y + 1]); }
+                        } else {
+#pragma unroll
+                            for (int y = 0; y < KB; ++y) sv[y] = capped(sv[y]);
+                        }
+                    }
+                    if constexpr (BIAS) {                         // the block's positions follow upon one another
+                        const float scale = CAP ? 1.f : q.c2, off = static_cast<float>((v >= pub ? lp + (v - pub) * kPage : (v - prv) * kPage) - pos);
+#pragma unroll
+                        for (int y = 0; y < KB; ++y) sv[y] = fmaf(slope2, off + static_cast<float>(y), sv[y] * scale);
+                    }
+                    float r4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+                    for (int y = 0; y < KB; y += 2) r4[(y >> 1) & 3] = fmax3(r4[(y >> 1) & 3], sv[y], sv[y + 1]);
+                    const float mx = fmaxf(fmaxf(r4[0], r4[1]), fmaxf(r4[2], r4[3]));
+                    const float ref = refer(i, BIAS ? mx : CAP ? capped(mx) : mx * q.c2, o_ready);
+                    const uint64_t mx2 = pack_f32x2(-ref, -ref), c22 = pack_f32x2(q.c2, q.c2);
+                    uint32_t pk[KB / 2];
+                    auto weights = [&](auto &&arg) {
+#pragma unroll
+                        for (int y = 0; y < KB / 2; ++y) pk[y] = weigh(arg(2 * y));
+                    };
+                    if constexpr (BIAS) {
+                        weights([&](int y) { return add_f32x2(pair(y), mx2); });
+                    } else if constexpr (CAP) {
+                        if (form == 1) weights([&](int y) { const uint64_t s2 = pair(y); return fma_f32x2(poly1(mul_f32x2(s2, s2)), s2, mx2); });
+                        else if (form == 2) weights([&](int y) { const uint64_t s2 = pair(y); return fma_f32x2(poly2(mul_f32x2(s2, s2)), s2, mx2); });
+                        else weights([&](int y) { return add_f32x2(pack_f32x2(capped(sv[y]), capped(sv[y + 1])), mx2); });
+                    } else {
+                        weights([&](int y) { return fma_f32x2(pair(y), c22, mx2); });
+                    }
+                    if (!o_ready) wait(&bar_o[t], n + i - 1);     // P of the block before has been read
+                    tc_fence_after();
+                    tmem_st32p(t_p, pk);
+                    tmem_st8(t_p + 32, pk + 32);
+                } else {
+                    // ---- masks: page by page, twice, scores going back to TMEM in log2 units in between.  Few blocks of an item come here, and
+                    // code that is run seldom costs by its length (every line of it comes from L2: 5000 cycles unrolled).
+                    float mx = -INFINITY;
+#pragma unroll 1
+                    for (int y = 0; y < kDtPages; ++y) {
+                        const int vv = v + y, z = vv < ns ? vv : vv - prv, tb = z < np ? z * kPage : lp + (z - np) * kPage;
+                        const int cnt = vv < list ? min(kPage, (z < np ? lp : lpq) - tb) : 0;
+                        uint32_t sees = 0u;
+                        if (cnt > 0 && tb <= last_pos) sees = dt_sees(p, pl, make_int2(tb, cnt), tok, pos);
+                        float s[kPage];
+                        dt_ld16(t_s + y * kPage, s);
+                        if constexpr (CAP) {
+                            float most = 0.f;
+#pragma unroll
+                            for (int x = 0; x < kPage; ++x) {
+                                s[x] = (sees >> x) & 1u ? s[x] : 0.f;      // hidden scores may be anything
+                                most = fmax3_abs_nan(most, s[x], 0.f);
+                            }
+                            if (__all_sync(0xffffffffu, most * q.y1 <= q.one_at)) {
+#pragma unroll
+                                for (int x = 0; x < kPage; x += 2) {
+                                    const uint64_t s2 = pack_f32x2(s[x], s[x + 1]);
+                                    unpack_f32x2(mul_f32x2(poly2(mul_f32x2(s2, s2)), s2), s[x], s[x + 1]);
+                                }
+                            } else {
+#pragma unroll
+                                for (int x = 0; x < kPage; ++x) s[x] = capped(s[x]);
+                            }
+                        } else {
+#pragma unroll
+                            for (int x = 0; x < kPage; ++x) s[x] *= q.c2;
+                        }
+                        if constexpr (BIAS) {
+#pragma unroll
+                            for (int x = 0; x < kPage; ++x) {
+                                const int d = tb + x - ctx;                // drafted tokens of a tree count by depth
+                                const int far = tree && d >= 0 ? ctx - pos + pl.depth[min(d, kDrTree - 1)] : tb + x - pos;
+                                s[x] = fmaf(slope2, static_cast<float>(far), s[x]);
+                            }
+                        }
+#pragma unroll
+                        for (int x = 0; x < kPage; ++x) {
+                            s[x] = (sees >> x) & 1u ? s[x] : -INFINITY;
+                            mx = fmaxf(mx, s[x]);
+                        }
+                        dt_st16(t_s + y * kPage, s);
+                    }
+                    tmem_wait_st();
+                    const float ref = refer(i, mx, o_ready);
+                    if (!o_ready) wait(&bar_o[t], n + i - 1);
+                    tc_fence_after();
+#pragma unroll 1
+                    for (int y = 0; y < kDtPages; ++y) {
+                        float s[kPage];
+                        dt_ld16(t_s + y * kPage, s);
+                        uint32_t pk[kPage / 2];
+#pragma unroll
+                        for (int x = 0; x < kPage; x += 2) pk[x / 2] = weigh(pack_f32x2(s[x] - ref, s[x + 1] - ref));
+                        tmem_st8(t_p + y * (kPage / 2), pk);
+                    }
+                    tc_fence_before();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(smem_u32(&bar_sf[t]));
+                }
                 tmem_wait_st();
                 tc_fence_before();
-                __syncwarp();                                    // one arrival per warp
+                __syncwarp();                                     // one arrival per warp
                 if (lane == 0) mbar_arrive(smem_u32(&bar_p[t]));
                 float s0, s1;
                 unpack_f32x2(lsum2, s0, s1);
@@ -467,43 +508,39 @@ drafted_tc_kernel(const __grid_constant__ DraftedTcParams q, const __grid_consta
             }
             // read only now: a tile without blocks of its own has waited for nobody before the exchange
             const bool bad = *const_cast<volatile int32_t *>(&pl.bad) != 0;
-            bool over = false;
-            if (ok && mine) {
-                DraftedRow f{};
-                const bool whole_item = pl.whole != 0;
-                if (live && whole_item) f = drafted_row(p, row, top * 0.69314718055994531f, l, bad);
-                float big = 0.f;
-                // a shared row's channels go half by either tile's thread
-                const int c_end = shared ? (t + 1) * (D / 2) : D;
+            const bool whole_item = pl.whole != 0;
+            DraftedRow f{};
+            if (ok && live && whole_item) f = drafted_row(p, row, top * 0.69314718055994531f, l, bad);
+            float big = 0.f;
+            // 16 channels at a time, in a loop (see the masks); a shared row's go half by either tile's thread, from both tiles' O
+            const int c_end = shared ? (t + 1) * (D / 2) : D;
 #pragma unroll 1
-                for (int c = shared ? t * (D / 2) : 0; c < c_end; c += 32) {
-                    float ov[32];
-                    tmem_ld32((shared ? tmem + lanes + kStO0 : t_o) + c, ov);
-                    if (shared) {
-                        float o1[32];
-                        tmem_ld32(tmem + lanes + kStO1 + c, o1);
+            for (int c = shared ? t * (D / 2) : 0; c < c_end; c += 16) {
+                float ov[16];
+                dt_ld16((shared ? tmem + lanes + kStO0 : t_o) + c, ov);
 #pragma unroll
-                        for (int y = 0; y < 32; ++y) ov[y] = (a0 == 0.f ? 0.f : ov[y] * a0) + (a1 == 0.f ? 0.f : o1[y] * a1);
+                for (int y = 0; y < 16; ++y) ov[y] = a0 == 0.f ? 0.f : ov[y] * a0;
+                if (shared) {
+                    float o1[16];
+                    dt_ld16(tmem + lanes + kStO1 + c, o1);
+#pragma unroll
+                    for (int y = 0; y < 16; ++y) ov[y] = a1 == 0.f ? ov[y] : fmaf(o1[y], a1, ov[y]);
+                }
+#pragma unroll
+                for (int y = 0; y < 16; y += 2) big = fmax3_abs_nan(big, ov[y], ov[y + 1]);
+                if (ok && live) {
+                    if (whole_item) {
+                        drafted_put16<D>(p, row, c, ov, f);
                     } else {
 #pragma unroll
-                        for (int y = 0; y < 32; ++y) ov[y] *= a0;
+                        for (int y = 0; y < 16; y += 4)
+                            reinterpret_cast<float4 *>(dst)[(c + y) / 4 * kDtRows + slot_row] = make_float4(ov[y], ov[y + 1], ov[y + 2], ov[y + 3]);
                     }
-                    if (live) {
-#pragma unroll
-                        for (int y = 0; y < 32; y += 4) big = fmax3_abs_nan(fmax3_abs_nan(big, ov[y], ov[y + 1]), ov[y + 2], ov[y + 3]);
-                        if (whole_item) {
-                            drafted_put32<D>(p, row, c, ov, f);
-                        } else {
-#pragma unroll
-                            for (int y = 0; y < 32; y += 4)
-                                reinterpret_cast<float4 *>(dst)[(c + y) / 4 * kDtRows + slot_row] = make_float4(ov[y], ov[y + 1], ov[y + 2], ov[y + 3]);
-                        }
-                    }
-                    __syncwarp();
                 }
-                if (live && !whole_item && (!shared || t == 0)) { dst[kDtRows * D + slot_row] = top; dst[kDtRows * (D + 1) + slot_row] = l; }
-                over = live && !bad && l > 0.f && l < INFINITY && !(big < INFINITY);
+                __syncwarp();
             }
+            if (ok && live && !whole_item && (!shared || t == 0)) { dst[kDtRows * D + slot_row] = top; dst[kDtRows * (D + 1) + slot_row] = l; }
+            const bool over = ok && live && !bad && l > 0.f && l < INFINITY && !(big < INFINITY);
             uint32_t again = __ballot_sync(0xffffffffu, over);
             if (shared) {
                 // the other tile may not write its next O before this one's is read; rows that are done again wait for both halves
@@ -533,25 +570,37 @@ drafted_tc_kernel(const __grid_constant__ DraftedTcParams q, const __grid_consta
             DrPlan &pl = plans[r & 1];
             if (r >= 2) wait(&bar_planfree[r & 1], (r >> 1) - 1);
             __syncwarp();
-            if (!ok || x >= x1) {
+            int b0 = 0, b1 = 0;
+            if (ok && x < x1) {
+                if (r > 0) drafted_next(p, w);
+                drafted_blocks(p, w, x, x1, b0, b1);
+            }
+            if (b0 == b1) {                             // the share is done, or ends inside the item's own cost
                 if (lane == 0) { pl.valid = 0; mbar_arrive(smem_u32(&bar_plan[r & 1])); }
                 break;
             }
-            if (r > 0) drafted_next(p, w);
-            const int b0 = static_cast<int>(x - w.x0), b1 = static_cast<int>(min(static_cast<int64_t>(w.k.nb), x1 - w.x0));
             const int i0 = w.rt * p.tt, toks = min(p.tt, w.s.n - i0), kvh = w.sq / p.hgroups;
             const bool whole = b0 == 0 && b1 == w.k.nb;
             const int slot = 2 * blockIdx.x + (b0 == 0 ? 1 : 0);
-            bool wrong = false;
-            int deepest = 0;
+            if (lane == 0) {
+                pl.valid = 1; pl.u = w.u; pl.first = w.s.first; pl.i0 = i0; pl.toks = toks; pl.kvh = kvh;
+                pl.h0 = kvh * p.g + w.sq % p.hgroups * p.hs;
+                pl.tiles = toks > q.tpt ? 2 : 1;
+                pl.b0 = b0; pl.b1 = b1; pl.whole = whole; pl.slot = slot; pl.deepest = 0;
+                pl.bad = !w.s.good;
+                pl.s = w.s; pl.k = w.k;
+            }
+            __syncwarp();
+            if (lane == 0) mbar_arrive(smem_u32(&bar_plan[r & 1]));      // loads and products may begin; the masks need the tree
             if (p.parents != nullptr && w.s.good) {
+                bool wrong = false;
+                int deepest = 0;
                 for (int i = lane; i < w.s.n; i += 32) {
                     const int up = p.parents[w.s.first + i];
                     const bool off = up < -1 || up >= i;
                     wrong = wrong || off;
                     pl.parent[i] = static_cast<int16_t>(off ? -1 : up);
                 }
-                wrong = __any_sync(0xffffffffu, wrong);
                 __syncwarp();
                 for (int i = lane; i < w.s.n; i += 32) {
                     const int d = drafted_depth(pl.parent, i);
@@ -560,21 +609,15 @@ drafted_tc_kernel(const __grid_constant__ DraftedTcParams q, const __grid_consta
                     if (i >= i0 && i < i0 + toks) drafted_line(p, w.s, pl.parent, i, d, pl.line[i - i0]);
                 }
                 deepest = __reduce_max_sync(0xffffffffu, deepest);
-            } else if (p.parents != nullptr) {              // no keys: depths are looked at all the same
-                for (int i = lane; i < min(w.s.n, kDrTree); i += 32) pl.depth[i] = 0;
-            }
-            if (lane == 0) {
-                pl.valid = 1; pl.u = w.u; pl.first = w.s.first; pl.i0 = i0; pl.toks = toks; pl.kvh = kvh;
-                pl.h0 = kvh * p.g + w.sq % p.hgroups * p.hs;
-                pl.tiles = toks > q.tpt ? 2 : 1;
-                pl.b0 = b0; pl.b1 = b1; pl.whole = whole; pl.slot = slot; pl.deepest = deepest;
-                pl.bad = !w.s.good || wrong;
-                pl.s = w.s; pl.k = w.k;
-                if (!whole) drafted_record(p, w, slot, W, shares);
+                if (lane == 0) pl.deepest = deepest;
+                if (wrong) pl.bad = 1;
             }
             __syncwarp();
-            if (lane == 0) mbar_arrive(smem_u32(&bar_plan[r & 1]));
-            x = w.x0 + b1;
+            if (lane == 0) {
+                mbar_arrive(smem_u32(&bar_tree[r & 1]));
+                if (!whole) drafted_record(p, w, slot, W, shares);
+            }
+            x = w.x0 + p.ov + w.k.nb;
         }
     } else if (wid == 10 || wid == 11) {
         // ---------------- the loading warps: K (and Q), V; c counts blocks over all items
