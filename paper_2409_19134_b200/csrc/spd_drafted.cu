@@ -19,7 +19,7 @@ int heads_per_tile(int g, int RT) { return g <= RT ? g : kHeadsPerItem; }
 
 constexpr int kFmaPerSm = 2;        // CTAs of the largest FMA variant that share an SM; the others fit more
 constexpr int kMostFmaRows = 64;
-constexpr int kTcOverhead = 2;      // what an item costs beside its blocks, in blocks
+constexpr int kTcOverhead = 6;      // what an item costs beside its blocks, in blocks
 constexpr int kFmaOverhead = 0;
 
 // Behind the workspace's head: records and slots of the pieces.

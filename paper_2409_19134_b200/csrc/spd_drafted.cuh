@@ -25,7 +25,7 @@ struct DraftedParams {
     int32_t tt;                           // tokens per tile
     int32_t SQ;                           // Hkv * hgroups
     int32_t bt;                           // page tiles per block
-    int32_t ov;                           // what an item costs beside its blocks, in blocks: where the cut is made, it counts in front of them
+    int32_t ov;                           // what an item costs beside its blocks, in blocks
     int64_t T;
     float sm_scale;
     const void *q;                        // [T][Hq][D]
@@ -125,6 +125,7 @@ __device__ __forceinline__ DraftedTile drafted_tile(const DraftedParams &p, cons
 // The cut.  Units (an item's own cost, then its blocks) in the order user, row tile, (KV head, head group); W of them in `shares` shares.
 // A share that ends inside an item's own cost has none of its blocks.
 struct DraftedWalk {
+    int ov;                    // units of an item's own cost
     int u, rt, sq;             // the item
     DraftedUser s;
     DraftedKeys k;
@@ -143,68 +144,69 @@ __device__ __forceinline__ void drafted_item_keys(const DraftedParams &p, Drafte
     w.k = drafted_keys(p, w.s, w.rt * p.tt, min(w.s.n, (w.rt + 1) * p.tt));
 }
 
-// Units of one KV head and head group over tiles from rt0 on, every `step`-th.
+// Blocks of one KV head and head group over tiles from rt0 on, every `step`-th.
 __device__ __forceinline__ int64_t drafted_user_blocks(const DraftedParams &p, const DraftedUser &s, int rt0, int step) {
     int64_t sum = 0;
-    for (int rt = rt0; rt * p.tt < s.n; rt += step) sum += drafted_keys(p, s, rt * p.tt, min(s.n, (rt + 1) * p.tt)).nb + p.ov;
+    for (int rt = rt0; rt * p.tt < s.n; rt += step) sum += drafted_keys(p, s, rt * p.tt, min(s.n, (rt + 1) * p.tt)).nb;
     return sum;
 }
 
-// The sums of the users' blocks, by all NT threads of a CTA: chunk c of C users (a user per warp where there are few of them, so that the
+// Shares of many blocks go by what items cost beside their blocks too; where there are few, finishing together matters less than starting early.
+// us on one GPU, ov 2 / 6: 64 users x 26-token trees over 1-9 k tokens 239 / 233, a part of a prompt 184 / 179; 8 users x 5-16 tokens
+// over 300-800 tokens in two halves 40 / 45.
+constexpr int kDrManyBlocks = 16;
+
+// The sums of the users' units, by all NT threads of a CTA: chunk c of C users (a user per warp where there are few of them, so that the
 // lanes share a long run's tiles) ends at sums[c].  *first_bad: the first user whose offsets are inconsistent; it and all behind it have no rows.
 template <int NT>
-__device__ __forceinline__ int64_t drafted_sums(const DraftedParams &p, int64_t *sums, int *first_bad, int &C, int &chunks) {
-    const int tid = threadIdx.x, lane = tid & 31;
+__device__ __forceinline__ int64_t drafted_sums(const DraftedParams &p, int64_t *sums, int *first_bad, int &C, int &chunks, int &ov) {
+    __shared__ int64_t warp_blocks[NT / 32];
+    __shared__ int warp_tiles[NT / 32];
+    const int tid = threadIdx.x, lane = tid & 31, wid = tid >> 5;
     const bool warps = p.B <= NT / 32;
     C = warps ? 1 : (p.B + NT - 1) / NT;
     chunks = (p.B + C - 1) / C;
     if (tid == 0) *first_bad = p.B;
     __syncthreads();
     // a user's blocks count unless its offsets, or those of somebody in front of it, turn out to be inconsistent
-    int64_t sum = 0;
+    int64_t blocks = 0;
+    int tiles = 0;
     DraftedUser s;
-    const int u0 = warps ? tid >> 5 : tid * C, u1 = min(p.B, warps ? u0 + 1 : u0 + C);
+    const int u0 = warps ? wid : tid * C, u1 = min(p.B, warps ? u0 + 1 : u0 + C);
     int bad = 0x7fffffff;
     for (int u = u0; u < u1 && bad == 0x7fffffff; ++u) {
-        if (!drafted_user(p, u, s)) bad = u;
-        else sum += warps ? drafted_user_blocks(p, s, lane, 32) : drafted_user_blocks(p, s, 0, 1);
+        if (!drafted_user(p, u, s)) { bad = u; break; }
+        blocks += warps ? drafted_user_blocks(p, s, lane, 32) : drafted_user_blocks(p, s, 0, 1);
+        if (!warps || lane == 0) tiles += s.n / p.tt + (s.n % p.tt != 0 ? 1 : 0);
     }
     if (bad != 0x7fffffff) atomicMin(first_bad, bad);
     __syncthreads();
-    if (u0 > *first_bad) sum = 0;
-    if (warps) {
+    if (u0 > *first_bad) { blocks = 0; tiles = 0; }
+    // inclusive sums over the warp's threads, then over the warps
 #pragma unroll
-        for (int d = 16; d >= 1; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
+    for (int d = 1; d < 32; d <<= 1) {
+        const int64_t ub = __shfl_up_sync(0xffffffffu, blocks, d);
+        const int ut = __shfl_up_sync(0xffffffffu, tiles, d);
+        if (lane >= d) { blocks += ub; tiles += ut; }
     }
-    sum *= p.SQ;
-    // inclusive sums over the chunks
-    __shared__ int64_t warp_sums[32];
-    if (warps) {
-        if (lane == 0) warp_sums[tid >> 5] = sum;
-        __syncthreads();
-        if (tid < chunks) {
-            int64_t t = 0;
-            for (int w = 0; w <= tid; ++w) t += warp_sums[w];
-            sums[tid] = t;
-        }
-    } else {
-        int64_t inc = sum;
-#pragma unroll
-        for (int d = 1; d < 32; d <<= 1) {
-            const int64_t up = __shfl_up_sync(0xffffffffu, inc, d);
-            if (lane >= d) inc += up;
-        }
-        if (lane == 31) warp_sums[tid >> 5] = inc;
-        __syncthreads();
-        for (int w = 0; w < (tid >> 5); ++w) inc += warp_sums[w];
-        if (tid < chunks) sums[tid] = inc;
-    }
+    if (lane == 31) { warp_blocks[wid] = blocks; warp_tiles[wid] = tiles; }
     __syncthreads();
-    return sums[chunks - 1];
+    int64_t before = 0, all = 0;
+    int tiles_before = 0, tiles_all = 0;
+    for (int w = 0; w < NT / 32; ++w) {
+        if (w < wid) { before += warp_blocks[w]; tiles_before += warp_tiles[w]; }
+        all += warp_blocks[w]; tiles_all += warp_tiles[w];
+    }
+    ov = all * p.SQ >= static_cast<int64_t>(kDrManyBlocks) * p.grid ? p.ov : min(p.ov, 2);
+    const int64_t mine = (before + blocks + static_cast<int64_t>(tiles_before + tiles) * ov) * p.SQ;
+    if (warps ? lane == 31 && wid < chunks : tid < chunks) sums[warps ? wid : tid] = mine;
+    __syncthreads();
+    return (all + static_cast<int64_t>(tiles_all) * ov) * p.SQ;
 }
 
 // The item that holds unit x, by one warp.
-__device__ __forceinline__ void drafted_locate(const DraftedParams &p, const int64_t *sums, int C, int chunks, int64_t x, int lane, DraftedWalk &w) {
+__device__ __forceinline__ void drafted_locate(const DraftedParams &p, const int64_t *sums, int C, int chunks, int ov, int64_t x, int lane, DraftedWalk &w) {
+    w.ov = ov;
     int c = 0;
     for (int c0 = 0; c0 < chunks; c0 += 32) {
         const unsigned hit = __ballot_sync(0xffffffffu, c0 + lane < chunks && x < sums[c0 + lane]);
@@ -215,7 +217,7 @@ __device__ __forceinline__ void drafted_locate(const DraftedParams &p, const int
         drafted_user(p, w.u, w.s);
         for (int rt0 = 0; rt0 * p.tt < w.s.n; rt0 += 32) {
             const int rt = rt0 + lane;
-            const int64_t mine = rt * p.tt < w.s.n ? static_cast<int64_t>(drafted_keys(p, w.s, rt * p.tt, min(w.s.n, (rt + 1) * p.tt)).nb + p.ov) * p.SQ : 0;
+            const int64_t mine = rt * p.tt < w.s.n ? static_cast<int64_t>(drafted_keys(p, w.s, rt * p.tt, min(w.s.n, (rt + 1) * p.tt)).nb + ov) * p.SQ : 0;
             int64_t inc = mine;
 #pragma unroll
             for (int d = 1; d < 32; d <<= 1) {
@@ -228,8 +230,8 @@ __device__ __forceinline__ void drafted_locate(const DraftedParams &p, const int
                 w.rt = rt0 + src;
                 at += __shfl_sync(0xffffffffu, inc - mine, src);
                 drafted_item_keys(p, w);
-                w.sq = static_cast<int>(drafted_div(x - at, w.k.nb + p.ov));
-                w.x0 = at + static_cast<int64_t>(w.sq) * (w.k.nb + p.ov);
+                w.sq = static_cast<int>(drafted_div(x - at, w.k.nb + ov));
+                w.x0 = at + static_cast<int64_t>(w.sq) * (w.k.nb + ov);
                 return;
             }
             at += __shfl_sync(0xffffffffu, inc, 31);
@@ -239,7 +241,7 @@ __device__ __forceinline__ void drafted_locate(const DraftedParams &p, const int
 
 // The next item; the caller knows that there is one.
 __device__ __forceinline__ void drafted_next(const DraftedParams &p, DraftedWalk &w) {
-    w.x0 += w.k.nb + p.ov;
+    w.x0 += w.k.nb + w.ov;
     if (++w.sq < p.SQ) return;
     w.sq = 0;
     if (++w.rt * p.tt >= w.s.n) {
@@ -254,16 +256,16 @@ __device__ __forceinline__ void drafted_next(const DraftedParams &p, DraftedWalk
 __device__ __forceinline__ void drafted_record(const DraftedParams &p, const DraftedWalk &w, int slot, int64_t W, int shares) {
     const int i0 = w.rt * p.tt;
     p.records[2 * slot] = make_int4(1, w.u, w.s.first + i0, w.sq);
-    p.records[2 * slot + 1] = make_int4(min(p.tt, w.s.n - i0), drafted_share_of(W, shares, w.x0 + p.ov), drafted_share_of(W, shares, w.x0 + p.ov + w.k.nb - 1), 0);
+    p.records[2 * slot + 1] = make_int4(min(p.tt, w.s.n - i0), drafted_share_of(W, shares, w.x0 + w.ov), drafted_share_of(W, shares, w.x0 + w.ov + w.k.nb - 1), 0);
 }
 
 // The blocks [b0, b1) of the item that units [x, x1) hold; none where b0 == b1.
-__device__ __forceinline__ void drafted_blocks(const DraftedParams &p, const DraftedWalk &w, int64_t x, int64_t x1, int &b0, int &b1) {
-    b0 = static_cast<int>(max(x - w.x0 - p.ov, static_cast<int64_t>(0)));
-    b1 = static_cast<int>(max(min(static_cast<int64_t>(w.k.nb), x1 - w.x0 - p.ov), static_cast<int64_t>(0)));
+__device__ __forceinline__ void drafted_blocks(const DraftedWalk &w, int64_t x, int64_t x1, int &b0, int &b1) {
+    b0 = static_cast<int>(max(x - w.x0 - w.ov, static_cast<int64_t>(0)));
+    b1 = static_cast<int>(max(min(static_cast<int64_t>(w.k.nb), x1 - w.x0 - w.ov), static_cast<int64_t>(0)));
 }
-__device__ __forceinline__ int drafted_shares(const DraftedParams &p, int64_t W) {
-    return static_cast<int>(min(static_cast<int64_t>(p.grid), drafted_div(W + p.ov + kDrMinBlocks - 1, p.ov + kDrMinBlocks)));
+__device__ __forceinline__ int drafted_shares(const DraftedParams &p, int64_t W, int ov) {
+    return static_cast<int>(min(static_cast<int64_t>(p.grid), drafted_div(W + ov + kDrMinBlocks - 1, ov + kDrMinBlocks)));
 }
 
 // Raises the status of a user.

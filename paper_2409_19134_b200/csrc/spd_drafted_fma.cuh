@@ -41,22 +41,22 @@ __global__ void __launch_bounds__(DraftedFma<D, RT>::kThreads) drafted_fma_kerne
     __shared__ int16_t depths[kDrTree];
     __shared__ uint32_t lines[RT][kDrWords];
     const int tid = threadIdx.x, lane = tid & 31, tx = tid & 15, ty = tid >> 4;
-    int Cu, chunks;
+    int Cu, chunks, ov;
     griddep_wait();
-    const int64_t W = drafted_sums<NT>(p, sums, &first_bad, Cu, chunks);
+    const int64_t W = drafted_sums<NT>(p, sums, &first_bad, Cu, chunks, ov);
     if (blockIdx.x == 0 && tid == 0) drafted_header(p, first_bad);
     if (tid < 4) p.records[4 * blockIdx.x + tid] = make_int4(0, 0, 0, 0);
     __syncthreads();
-    const int shares = drafted_shares(p, W);
+    const int shares = drafted_shares(p, W, ov);
     if (static_cast<int>(blockIdx.x) >= shares) return;
     int64_t x = drafted_bound(W, shares, blockIdx.x);
     const int64_t x1 = drafted_bound(W, shares, blockIdx.x + 1);
     DraftedWalk w;
-    drafted_locate(p, sums, Cu, chunks, x, lane, w);
+    drafted_locate(p, sums, Cu, chunks, ov, x, lane, w);
     for (;; drafted_next(p, w)) {
         int b0, b1;
-        drafted_blocks(p, w, x, x1, b0, b1);
-        x = w.x0 + p.ov + w.k.nb;                 // the next item, if it is this share's
+        drafted_blocks(w, x, x1, b0, b1);
+        x = w.x0 + w.ov + w.k.nb;                 // the next item, if it is this share's
         if (b0 == b1) break;
         const DraftedUser s = w.s;
         const int i0 = w.rt * p.tt, toks = min(p.tt, s.n - i0), rows = toks * p.hs;

@@ -228,16 +228,16 @@ drafted_tc_kernel(const __grid_constant__ DraftedTcParams q, const __grid_consta
     griddep_wait();
     // ---- the cut: sums over the users in what becomes the K ring, the share's first item by the planning warp
     int64_t *sums = reinterpret_cast<int64_t *>(base + 2 * QTILE);
-    int Cu, chunks;
-    const int64_t W = drafted_sums<kDtThreads>(p, sums, &first_bad, Cu, chunks);
+    int Cu, chunks, ov;
+    const int64_t W = drafted_sums<kDtThreads>(p, sums, &first_bad, Cu, chunks, ov);
     if (blockIdx.x == 0 && tid == 0) drafted_header(p, first_bad);
     if (tid < 4) p.records[4 * blockIdx.x + tid] = make_int4(0, 0, 0, 0);
-    const int shares = drafted_shares(p, W);
+    const int shares = drafted_shares(p, W, ov);
     if (static_cast<int>(blockIdx.x) >= shares) return;
     const int64_t x1 = drafted_bound(W, shares, blockIdx.x + 1);
     int64_t x = drafted_bound(W, shares, blockIdx.x);
     DraftedWalk w;
-    if (wid == 12) drafted_locate(p, sums, Cu, chunks, x, lane, w);
+    if (wid == 12) drafted_locate(p, sums, Cu, chunks, ov, x, lane, w);
     if (tid == 320) {
         for (int b = 0; b < NBARS; ++b) {
             // Q and ring slots free: one per tile; S in registers, P written: one per softmax warp of the tile; rows exchanged, O's
@@ -573,7 +573,7 @@ drafted_tc_kernel(const __grid_constant__ DraftedTcParams q, const __grid_consta
             int b0 = 0, b1 = 0;
             if (ok && x < x1) {
                 if (r > 0) drafted_next(p, w);
-                drafted_blocks(p, w, x, x1, b0, b1);
+                drafted_blocks(w, x, x1, b0, b1);
             }
             if (b0 == b1) {                             // the share is done, or ends inside the item's own cost
                 if (lane == 0) { pl.valid = 0; mbar_arrive(smem_u32(&bar_plan[r & 1])); }
@@ -617,7 +617,7 @@ drafted_tc_kernel(const __grid_constant__ DraftedTcParams q, const __grid_consta
                 mbar_arrive(smem_u32(&bar_tree[r & 1]));
                 if (!whole) drafted_record(p, w, slot, W, shares);
             }
-            x = w.x0 + p.ov + w.k.nb;
+            x = w.x0 + w.ov + w.k.nb;
         }
     } else if (wid == 10 || wid == 11) {
         // ---------------- the loading warps: K (and Q), V; c counts blocks over all items
