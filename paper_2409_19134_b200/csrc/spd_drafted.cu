@@ -57,7 +57,7 @@ spd_status launch_early(void (*kernel)(Args...), dim3 grid, int threads, size_t 
 
 template <int D, int RT, bool LOG2>
 spd_status launch_join(const DraftedParams &p, cudaStream_t st) {
-    return launch_early(drafted_join_kernel<D, RT, LOG2>, dim3(static_cast<unsigned>(p.grid), 2, kDrJoin), 256, 0, st, p);
+    return launch_early(drafted_join_kernel<D, RT, LOG2>, dim3(static_cast<unsigned>(p.grid), 2, kDrJoin), kDrJoinThreads, 0, st, p);
 }
 
 // [T][Hq][D] bf16 as a 3-D map: a box is `tokens` tokens x `heads` heads x 128 bytes, 128-byte swizzle.

@@ -374,11 +374,13 @@ __device__ __forceinline__ void drafted_line(const DraftedParams &p, const Draft
 
 // ---------------------------------------------------------------------------------------------------------------------
 // The join: CTAs (j, x, .) take a part of the item that the attention's CTA j left a piece of in its slot x, in proportion to the pieces; kDrJoin of
-// them share that part.
-constexpr int kDrJoin = 4;
+// them share that part.  A thread joins 16 channels of a row: its neighbours' are the next rows', side by side in the slots, and it writes
+// whole sectors.
+constexpr int kDrJoin = 4, kDrJoinThreads = 128;
 template <int D, int RT, bool LOG2>
-__global__ void __launch_bounds__(256) drafted_join_kernel(const __grid_constant__ DraftedParams p) {
+__global__ void __launch_bounds__(kDrJoinThreads) drafted_join_kernel(const __grid_constant__ DraftedParams p) {
     constexpr float kUnit = LOG2 ? 0.69314718055994531f : 1.f;
+    constexpr int AHEAD = 3;            // pieces under way at a time
     griddep_launch_dependents();        // what comes next may set itself up; it waits for this kernel's end before it looks at anything of this call
     griddep_wait();
     const int slot = 2 * blockIdx.x + blockIdx.y;
@@ -387,40 +389,50 @@ __global__ void __launch_bounds__(256) drafted_join_kernel(const __grid_constant
     const int u = a.y, tok0 = a.z, sq = a.w, toks = b.x, c0 = b.y, c1 = b.z, pieces = c1 - c0 + 1, rows = toks * p.hs;
     const int h0 = sq / p.hgroups * p.g + sq % p.hgroups * p.hs;
     const bool bad = p.bad[u] == p.epoch;
-    const int E = rows * (D / 4), parts = pieces * kDrJoin, mine = (static_cast<int>(blockIdx.x) - c0) * kDrJoin + blockIdx.z;
-    const int e0 = static_cast<int>(static_cast<int64_t>(E) * mine / parts), e1 = static_cast<int>(static_cast<int64_t>(E) * (mine + 1) / parts);
-    for (int e = e0 + threadIdx.x; e < e1; e += 256) {
-        const int r = e % rows, c = e / rows;
-        float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-        float m = -INFINITY, l = 0.f;
-        for (int k0 = 0; k0 < pieces; k0 += 8) {              // eight pieces under way at a time
-            float mk[8], lk[8];
-            float4 v[8];
+    const int E = rows * (D / 16), parts = pieces * kDrJoin, mine = (static_cast<int>(blockIdx.x) - c0) * kDrJoin + blockIdx.z;
+    const int e0 = static_cast<int>(drafted_div(static_cast<int64_t>(E) * mine, parts)), e1 = static_cast<int>(drafted_div(static_cast<int64_t>(E) * (mine + 1), parts));
+    auto exp_of = [](float x) { return LOG2 ? exp2f(x) : expf(x); };
+    for (int e = e0 + threadIdx.x; e < e1; e += kDrJoinThreads) {
+        const int c = e / rows, r = e - c * rows;
+        float o[16], m = -INFINITY, l = 0.f;
 #pragma unroll
-            for (int y = 0; y < 8; ++y) {
+        for (int i = 0; i < 16; ++i) o[i] = 0.f;
+        for (int k0 = 0; k0 < pieces; k0 += AHEAD) {
+            float mk[AHEAD], lk[AHEAD];
+            float4 v[AHEAD][4];
+#pragma unroll
+            for (int y = 0; y < AHEAD; ++y) {
                 mk[y] = -INFINITY; lk[y] = 0.f;
                 if (k0 + y < pieces) {
                     const float *s = p.scratch + static_cast<size_t>(2 * (c0 + k0 + y) + (k0 + y == 0 ? 1 : 0)) * drafted_slot_floats(D, RT);
                     mk[y] = s[RT * D + r]; lk[y] = s[RT * (D + 1) + r];
-                    v[y] = reinterpret_cast<const float4 *>(s)[c * RT + r];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) v[y][i] = reinterpret_cast<const float4 *>(s)[(4 * c + i) * RT + r];
                 }
             }
             float M = m;
 #pragma unroll
-            for (int y = 0; y < 8; ++y) M = fmaxf(M, mk[y]);
-            const float wa = m == -INFINITY ? 0.f : (LOG2 ? exp2f(m - M) : expf(m - M));
+            for (int y = 0; y < AHEAD; ++y) M = fmaxf(M, mk[y]);
+            const float wa = m == -INFINITY ? 0.f : exp_of(m - M);
             l = l != l ? l : l * wa;
-            o.x *= wa; o.y *= wa; o.z *= wa; o.w *= wa;
 #pragma unroll
-            for (int y = 0; y < 8; ++y) {
-                const float wb = mk[y] == -INFINITY ? 0.f : (LOG2 ? exp2f(mk[y] - M) : expf(mk[y] - M));
+            for (int i = 0; i < 16; ++i) o[i] *= wa;
+#pragma unroll
+            for (int y = 0; y < AHEAD; ++y) {
+                const float wb = mk[y] == -INFINITY ? 0.f : exp_of(mk[y] - M);
                 l += lk[y] != lk[y] ? lk[y] : wb != 0.f ? lk[y] * wb : 0.f;
-                if (wb != 0.f) { o.x = fmaf(v[y].x, wb, o.x); o.y = fmaf(v[y].y, wb, o.y); o.z = fmaf(v[y].z, wb, o.z); o.w = fmaf(v[y].w, wb, o.w); }
+                if (wb != 0.f) {
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        o[4 * i] = fmaf(v[y][i].x, wb, o[4 * i]); o[4 * i + 1] = fmaf(v[y][i].y, wb, o[4 * i + 1]);
+                        o[4 * i + 2] = fmaf(v[y][i].z, wb, o[4 * i + 2]); o[4 * i + 3] = fmaf(v[y][i].w, wb, o[4 * i + 3]);
+                    }
+                }
             }
             m = M;
         }
         const int64_t row = (static_cast<int64_t>(tok0) + r / p.hs) * p.Hq + h0 + r % p.hs;
-        drafted_put4<D>(p, row, c, o, drafted_row(p, row, m * kUnit, l, bad));
+        drafted_put16<D>(p, row, 16 * c, o, drafted_row(p, row, m * kUnit, l, bad));
     }
 }
 

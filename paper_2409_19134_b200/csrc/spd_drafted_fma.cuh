@@ -43,6 +43,7 @@ __global__ void __launch_bounds__(DraftedFma<D, RT>::kThreads) drafted_fma_kerne
     const int tid = threadIdx.x, lane = tid & 31, tx = tid & 15, ty = tid >> 4;
     int Cu, chunks, ov;
     griddep_wait();
+    griddep_launch_dependents();          // the join's CTAs take the places of those that are done here, and wait for the last
     const int64_t W = drafted_sums<NT>(p, sums, &first_bad, Cu, chunks, ov);
     if (blockIdx.x == 0 && tid == 0) drafted_header(p, first_bad);
     if (tid < 4) p.records[4 * blockIdx.x + tid] = make_int4(0, 0, 0, 0);

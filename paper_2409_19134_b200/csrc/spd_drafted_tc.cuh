@@ -226,6 +226,7 @@ drafted_tc_kernel(const __grid_constant__ DraftedTcParams q, const __grid_consta
 
     if (tid == 320) { prefetch_tensormap(&mq); prefetch_tensormap(&mk0); prefetch_tensormap(&mv0); prefetch_tensormap(&mk1); prefetch_tensormap(&mv1); }
     griddep_wait();
+    griddep_launch_dependents();          // the join's CTAs take the places of those that are done here, and wait for the last
     // ---- the cut: sums over the users in what becomes the K ring, the share's first item by the planning warp
     int64_t *sums = reinterpret_cast<int64_t *>(base + 2 * QTILE);
     int Cu, chunks, ov;
