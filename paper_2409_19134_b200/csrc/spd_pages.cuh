@@ -20,6 +20,13 @@ constexpr int kPgPools = 128;             // pools per launch
 constexpr int kPgPiece = 16384;           // bytes that a CTA copies
 constexpr int kPgTree = 256;              // most drafted tokens of a user that come as a tree
 
+// What a kernel here has written is there, for TMA reads too, once all its CTAs have left: an attention call behind it may read tables, lengths and
+// rows before the kernel counts as finished for its stream.
+__device__ __forceinline__ void pages_written() {
+    __threadfence();
+    asm volatile("fence.proxy.async.global;" ::: "memory");
+}
+
 enum PagesState { PG_REFUSED = -1, PG_NONE = -2 };      // in place of a user's demand
 
 struct PagesParams {
@@ -85,6 +92,7 @@ static __global__ void __launch_bounds__(kPgThreads) pages_release_kernel(const 
         }
     }
     if (bad) flag_error(p.hdr, 4 /* SPD_ERR_BAD_PAGE */, u);
+    pages_written();
 }
 
 // CTAs [0, chunks): the free pages of a chunk; CTAs behind them: the demand of a user.
@@ -230,6 +238,7 @@ static __global__ void __launch_bounds__(kPgThreads) pages_give_kernel(const __g
             p.lens[u] = len;
         }
     }
+    pages_written();
 }
 
 struct PagesPools { void *pool[kPgPools]; };
@@ -255,6 +264,7 @@ pages_copy_kernel(const __grid_constant__ PagesPools pools, const int32_t *copie
 #pragma unroll
     for (int x = 0; x < PER; ++x)
         if (threadIdx.x + x * kPgThreads < n) b[threadIdx.x + x * kPgThreads] = v[x];
+    pages_written();
 }
 
 struct KeepParams {
@@ -337,9 +347,9 @@ static __global__ void __launch_bounds__(kPgThreads) keep_kernel(const __grid_co
         if (p.kept != nullptr && rows_ok)
             for (int64_t i = tid; i < n; i += kPgThreads) p.kept[a + i] = i < kept ? (p.parents ? path[i] : static_cast<int>(i)) : -1;
     }
+    pages_written();
     if (p.new_lens != p.lens) return;
     // in place: the lengths change once nobody reads them any more, so the last CTA out does it
-    __threadfence();
     __syncthreads();
     if (tid == 0) last_cta = atomicAdd(&p.hdr[HDR_GRID_EXITS], 1) == static_cast<int32_t>(gridDim.x * gridDim.y) - 1;
     __syncthreads();
@@ -347,6 +357,7 @@ static __global__ void __launch_bounds__(kPgThreads) keep_kernel(const __grid_co
     __threadfence();
     if (tid == 0) p.hdr[HDR_GRID_EXITS] = 0;
     for (int x = tid; x < p.B; x += kPgThreads) p.new_lens[x] = __ldcg(p.result + x);
+    __threadfence();
 }
 
 }  // namespace spd

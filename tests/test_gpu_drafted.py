@@ -272,3 +272,46 @@ def test_what_shared_memory_held_before(window, sinks):
         s.fused()
         assert torch.equal(g.fused(), first)
     ok(g)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("hq,hkv", [(136, 1), (128, 1), (40, 1), (48, 2)])
+def test_wide_groups(dtype, hq, hkv):
+    """Groups that fill a tile of rows, leave some of it empty, or are cut."""
+    w = dr.batch([3, 1, 9], [20, 90, 0], [4, 0, 7], hq, hkv, 64, dtype, seed=hq)
+    g = dr.OnDevice(w, window=40, sinks=2)
+    want, _, _, _, tol = dr.expected(w, window=40, sinks=2)
+    dr.close(g.fused(), want, tol)
+    ok(g)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_pools_without_pages(dtype):
+    w = dr.batch([4, 2], [0, 0], [9, 30], 4, 2, 64, dtype, seed=97)
+    w.priv.k_pool, w.priv.v_pool = w.priv.k_pool[:0].contiguous(), w.priv.v_pool[:0].contiguous()
+    w.priv.page_indptr, w.priv.page_indices = torch.zeros(3, dtype=torch.int32), torch.zeros(0, dtype=torch.int32)
+    g = dr.OnDevice(w)
+    want, _, _, _, tol = dr.expected(w)
+    dr.close(g.fused(), want, tol)
+    dr.close(g.halves()[0], want, tol)
+    ok(g)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_many_users_many_heads_drawn(dtype):
+    rng = np.random.default_rng(98)
+    for seed in range(12):
+        B, hkv, g = int(rng.integers(1, 9)), int(rng.choice([1, 2, 3])), int(rng.choice([1, 2, 4, 8, 16]))
+        d, kind = int(rng.choice([64, 128])), str(rng.choice(["tree", "run", "star", "chain"]))
+        counts = rng.integers(0, int(rng.choice([2, 20, 70])), B)
+        if counts.sum() == 0:
+            counts[0] = 1
+        w = dr.batch(counts, rng.integers(0, int(rng.choice([5, 200, 900])), B), rng.integers(0, 90, B), hkv * g, hkv, d, dtype, seed=seed, kind=kind, qscale=2.0)
+        args = float(rng.choice([0.0, 20.0, 1e-3, 1e6])), int(rng.choice([0, 5, 70, 2**31 - 1])), int(rng.choice([0, 3, 50, 2**31 - 1]))
+        h = dr.OnDevice(w, *args, alibi=bool(rng.integers(0, 2)))
+        rows = set(rng.integers(0, h.T, 12).tolist())
+        want, _, _, _, tol = dr.expected(w, *args, h.slopes, rows=rows)
+        at = torch.tensor(sorted(rows))
+        dr.close(h.fused(torch.bfloat16)[at.cuda()], want[at], tol[at], seed)
+        dr.close(h.halves()[0][at.cuda()], want[at], tol[at], seed)
+        ok(h)
