@@ -717,17 +717,29 @@ def alloc_drafted_workspace(shape: Shape, device="cuda") -> torch.Tensor:
     return torch.zeros(spd_drafted_workspace_size(shape), dtype=torch.uint8, device=device)
 
 
+def _ints(t, n, dev):
+    """Pointer of n int32 numbers one after the other on the call's device, or None.  (_i32 without the shape: half its time.)"""
+    if t is None:
+        return None
+    if t.dtype is _I32 and t.numel() == n and t.is_contiguous() and t.get_device() == dev:
+        return t.data_ptr()
+    if t.dtype is _I32 and t.numel() == n and t.is_contiguous():
+        raise _elsewhere(t)
+    raise ValueError(f"expected contiguous int32 of {n} elements, got {t.dtype} {list(t.shape)}")
+
+
 def _drafted(shape, score, q, tok_indptr, parents, sinks):
     """What the *_drafted calls have in common: the drafts, the rows' count, the device, and what partitions are held against."""
     dev, T, B, hq, d, dtype = _here(q), q.shape[0], shape.batch, shape.num_q_heads, shape.head_dim, _TORCH_DTYPES[shape.dtype]
-    if q.dtype is not dtype or q.shape != (T, hq, d) or not q.is_contiguous():
+    if q.dtype is not dtype or q.numel() != T * hq * d or not q.is_contiguous():
         raise ValueError(f"expected contiguous {dtype} [tokens, {hq}, {d}], got {q.dtype} {list(q.shape)}")
     if not 0 <= sinks < 2**31:
         raise ValueError("the number of sinks is a 32-bit number, not negative")
     if tok_indptr is None and T != B:
         raise ValueError(f"{T} tokens of {B} users need a tok_indptr")
-    _slopes(shape, score, dev)
-    return Drafts(T, _i32(tok_indptr, B + 1, dev=dev), _i32(parents, T, dev=dev), sinks), T, dev, (B, shape.num_kv_heads * shape.page_size * d, dtype, dev)
+    if score.alibi_slopes is not None:
+        _slopes(shape, score, dev)
+    return Drafts(T, _ints(tok_indptr, B + 1, dev), _ints(parents, T, dev), sinks), T, dev, (B, shape.num_kv_heads * shape.page_size * d, dtype, dev)
 
 
 def _drafted_partial(shape, part, T, dev) -> Partial:
@@ -749,7 +761,7 @@ def spd_partial_attn_drafted(shape, score, q, priv, pub_lens, out, ws, tok_indpt
     """The private half of spd_decode_step_drafted: out = (o [T,Hq,D], m [T,Hq], l [T,Hq]); pub_lens int32 [B] counts the drafted tokens."""
     drafts, T, dev, fit = _drafted(shape, score, q, tok_indptr, parents, sinks)
     kv, part = PagedKV(*_partition(priv, *fit)), _drafted_partial(shape, out, T, dev)
-    _check(lib().spd_partial_attn_drafted(shape, score, drafts, _ptr(q), kv, _i32(pub_lens, shape.batch, dev=dev), part, *_workspace(ws, dev),
+    _check(lib().spd_partial_attn_drafted(shape, score, drafts, _ptr(q), kv, _ints(pub_lens, shape.batch, dev), part, *_workspace(ws, dev),
                                           _stream_ptr(stream)), "spd_partial_attn_drafted")
 
 
@@ -757,7 +769,7 @@ def spd_service_attn_merge_drafted(shape, score, q, pub, priv_lens, partial_in, 
     """The public half of spd_decode_step_drafted, merged with the private partial and normalised; priv_lens int32 [B]."""
     drafts, T, dev, fit = _drafted(shape, score, q, tok_indptr, parents, sinks)
     kv, part = PagedKV(*_partition(pub, *fit)), _drafted_partial(shape, partial_in, T, dev)
-    _check(lib().spd_service_attn_merge_drafted(shape, score, drafts, _ptr(q), kv, _i32(priv_lens, shape.batch, dev=dev), part,
+    _check(lib().spd_service_attn_merge_drafted(shape, score, drafts, _ptr(q), kv, _ints(priv_lens, shape.batch, dev), part,
                                                 _packed(out, q.numel(), dev=dev), _dtype_code(out.dtype), *_workspace(ws, dev),
                                                 _stream_ptr(stream)), "spd_service_attn_merge_drafted")
 
@@ -786,7 +798,7 @@ def make_pools(shape, pools) -> Pools:
 def _pools(shape, pools, dev) -> Pools:
     if not isinstance(pools, Pools):
         pools = Pools(shape, pools)
-    if pools.page != shape.num_kv_heads * shape.page_size * shape.head_dim or pools.dtype is not _TORCH_DTYPES[shape.dtype]:
+    elif pools.page != shape.num_kv_heads * shape.page_size * shape.head_dim or pools.dtype is not _TORCH_DTYPES[shape.dtype]:
         raise ValueError("the pools were made for another shape")
     if pools.count and pools.dev != dev:
         raise _elsewhere(pools._keep[0])
@@ -803,48 +815,32 @@ def spd_keep_drafted(shape, pools, part, tok_indptr, last, ws, parents=None, new
     if T is None:
         raise ValueError("total_tokens is needed")
     pools = _pools(shape, pools, dev)
-    lens = _i32(part.seq_lens, B, dev=dev)
-    indices = part.page_indices
-    if indices.dtype is not _I32 or not indices.is_contiguous():
-        raise ValueError(f"expected contiguous int32 page_indices, got {indices.dtype}")
-    if indices.get_device() != dev:
-        raise _elsewhere(indices)
-    _check(lib().spd_keep_drafted(shape, T, _i32(tok_indptr, B + 1, dev=dev), _i32(parents, T, dev=dev), _i32(last, B, dev=dev), pools.count,
-                                  pools.array, pools.pages, _i32(part.page_indptr, B + 1, dev=dev), _ptr(indices), lens,
-                                  lens if isinstance(new_lens, str) else _i32(new_lens, B, dev=dev), _i32(kept, T, dev=dev),
+    lens, indices = _ints(part.seq_lens, B, dev), part.page_indices
+    new_lens = lens if isinstance(new_lens, str) else _ints(new_lens, B, dev)
+    _check(lib().spd_keep_drafted(shape, T, _ints(tok_indptr, B + 1, dev), _ints(parents, T, dev), _ints(last, B, dev), pools.count, pools.array, pools.pages,
+                                  _ints(part.page_indptr, B + 1, dev), _ints(indices, indices.numel(), dev), lens, new_lens, _ints(kept, T, dev),
                                   *_workspace(ws, dev), _stream_ptr(stream)), "spd_keep_drafted")
-
-
-def _page_table(shape, refs, page_indptr, page_indices):
-    """(num_pages, refs, page_indptr, page_indices) of a table whose pages are counted, and the device."""
-    dev = _here(refs)
-    for t in (refs, page_indices):
-        if t.dtype is not _I32 or t.dim() != 1 or not t.is_contiguous():
-            raise ValueError(f"expected contiguous one-dimensional int32 refs and page_indices, got {t.dtype} {list(t.shape)}")
-    if page_indices.get_device() != dev:
-        raise _elsewhere(page_indices)
-    return (refs.numel(), _ptr(refs), _i32(page_indptr, shape.batch + 1, dev=dev), _ptr(page_indices)), dev
 
 
 def spd_pages_take(shape, refs, page_indptr, page_indices, from_tokens, to_tokens, ws, stream=None) -> None:
     """Fresh pages for the entries of tokens [from_tokens[u], to_tokens[u]) that hold -1 (int32 [B] each)."""
-    table, dev = _page_table(shape, refs, page_indptr, page_indices)
-    _check(lib().spd_pages_take(shape, *table, _i32(from_tokens, shape.batch, dev=dev), _i32(to_tokens, shape.batch, dev=dev), *_workspace(ws, dev),
-                                _stream_ptr(stream)), "spd_pages_take")
+    dev, n, B = _here(refs), refs.numel(), shape.batch
+    _check(lib().spd_pages_take(shape, n, _ints(refs, n, dev), _ints(page_indptr, B + 1, dev), _ints(page_indices, page_indices.numel(), dev),
+                                _ints(from_tokens, B, dev), _ints(to_tokens, B, dev), *_workspace(ws, dev), _stream_ptr(stream)), "spd_pages_take")
 
 
 def spd_pages_release(shape, refs, page_indptr, page_indices, from_tokens, ws, to_tokens=None, stream=None) -> None:
     """Take the entries that hold nothing but tokens [from_tokens[u], to_tokens[u]) out of the tables; to_tokens None: to the tables' end."""
-    table, dev = _page_table(shape, refs, page_indptr, page_indices)
-    _check(lib().spd_pages_release(shape, *table, _i32(from_tokens, shape.batch, dev=dev), _i32(to_tokens, shape.batch, dev=dev), *_workspace(ws, dev),
-                                   _stream_ptr(stream)), "spd_pages_release")
+    dev, n, B = _here(refs), refs.numel(), shape.batch
+    _check(lib().spd_pages_release(shape, n, _ints(refs, n, dev), _ints(page_indptr, B + 1, dev), _ints(page_indices, page_indices.numel(), dev),
+                                   _ints(from_tokens, B, dev), _ints(to_tokens, B, dev), *_workspace(ws, dev), _stream_ptr(stream)), "spd_pages_release")
 
 
 def spd_pages_fork(shape, refs, page_indptr, page_indices, seq_lens, source, copies, ws, stream=None) -> None:
     """User u becomes a copy of user source[u] (int32 [B], -1: it stays); copies int32 [B, 2] receives the pages to copy (spd_pages_copy)."""
-    table, dev = _page_table(shape, refs, page_indptr, page_indices)
-    B = shape.batch
-    _check(lib().spd_pages_fork(shape, *table, _i32(seq_lens, B, dev=dev), _i32(source, B, dev=dev), _i32(copies, B, 2, dev=dev), *_workspace(ws, dev),
+    dev, n, B = _here(refs), refs.numel(), shape.batch
+    _check(lib().spd_pages_fork(shape, n, _ints(refs, n, dev), _ints(page_indptr, B + 1, dev), _ints(page_indices, page_indices.numel(), dev),
+                                _ints(seq_lens, B, dev), _ints(source, B, dev), _ints(copies, 2 * B, dev), *_workspace(ws, dev),
                                 _stream_ptr(stream)), "spd_pages_fork")
 
 
@@ -852,5 +848,5 @@ def spd_pages_copy(shape, pools, copies, ws, stream=None) -> None:
     """Copy page copies[i, 0] to page copies[i, 1] (int32 [n, 2]) in all pools (make_pools, or a list of tensors)."""
     dev = _here(copies)
     pools, n = _pools(shape, pools, dev), copies.shape[0]
-    _check(lib().spd_pages_copy(shape, pools.count, pools.array, pools.pages, n, _i32(copies, n, 2, dev=dev), *_workspace(ws, dev),
+    _check(lib().spd_pages_copy(shape, pools.count, pools.array, pools.pages, n, _ints(copies, 2 * n, dev), *_workspace(ws, dev),
                                 _stream_ptr(stream)), "spd_pages_copy")

@@ -412,21 +412,28 @@ drafted_tc_kernel(const __grid_constant__ DraftedTcParams q, const __grid_consta
                     // ---- masks: page by page, twice, scores going back to TMEM in log2 units in between.  Few blocks of an item come here, and
                     // code that is run seldom costs by its length (every line of it comes from L2: 5000 cycles unrolled).
                     float mx = -INFINITY;
+                    uint32_t hidden = 0u;                              // pages that no row of the warp sees anything of
 #pragma unroll 1
                     for (int y = 0; y < kDtPages; ++y) {
                         const int vv = v + y, z = vv < ns ? vv : vv - prv, tb = z < np ? z * kPage : lp + (z - np) * kPage;
                         const int cnt = vv < list ? min(kPage, (z < np ? lp : lpq) - tb) : 0;
                         uint32_t sees = 0u;
                         if (cnt > 0 && tb <= last_pos) sees = dt_sees(p, pl, make_int2(tb, cnt), tok, pos);
+                        if (!__any_sync(0xffffffffu, sees != 0u)) {
+                            hidden |= 1u << y;
+                            continue;
+                        }
+                        const bool all = __all_sync(0xffffffffu, sees == 0xffffu);
                         float s[kPage];
                         dt_ld16(t_s + y * kPage, s);
                         if constexpr (CAP) {
+                            if (!all) {                                    // hidden scores may be anything
+#pragma unroll
+                                for (int x = 0; x < kPage; ++x) s[x] = (sees >> x) & 1u ? s[x] : 0.f;
+                            }
                             float most = 0.f;
 #pragma unroll
-                            for (int x = 0; x < kPage; ++x) {
-                                s[x] = (sees >> x) & 1u ? s[x] : 0.f;      // hidden scores may be anything
-                                most = fmax3_abs_nan(most, s[x], 0.f);
-                            }
+                            for (int x = 0; x < kPage; x += 2) most = fmax3_abs_nan(most, s[x], s[x + 1]);
                             if (__all_sync(0xffffffffu, most * q.y1 <= q.one_at)) {
 #pragma unroll
                                 for (int x = 0; x < kPage; x += 2) {
@@ -449,11 +456,12 @@ drafted_tc_kernel(const __grid_constant__ DraftedTcParams q, const __grid_consta
                                 s[x] = fmaf(slope2, static_cast<float>(far), s[x]);
                             }
                         }
+                        if (!all) {
 #pragma unroll
-                        for (int x = 0; x < kPage; ++x) {
-                            s[x] = (sees >> x) & 1u ? s[x] : -INFINITY;
-                            mx = fmaxf(mx, s[x]);
+                            for (int x = 0; x < kPage; ++x) s[x] = (sees >> x) & 1u ? s[x] : -INFINITY;
                         }
+#pragma unroll
+                        for (int x = 0; x < kPage; x += 2) mx = fmax3(mx, s[x], s[x + 1]);
                         dt_st16(t_s + y * kPage, s);
                     }
                     tmem_wait_st();
@@ -462,9 +470,15 @@ drafted_tc_kernel(const __grid_constant__ DraftedTcParams q, const __grid_consta
                     tc_fence_after();
 #pragma unroll 1
                     for (int y = 0; y < kDtPages; ++y) {
+                        uint32_t pk[kPage / 2];
+                        if ((hidden >> y) & 1u) {
+#pragma unroll
+                            for (int x = 0; x < kPage / 2; ++x) pk[x] = 0u;
+                            tmem_st8(t_p + y * (kPage / 2), pk);
+                            continue;
+                        }
                         float s[kPage];
                         dt_ld16(t_s + y * kPage, s);
-                        uint32_t pk[kPage / 2];
 #pragma unroll
                         for (int x = 0; x < kPage; x += 2) pk[x / 2] = weigh(pack_f32x2(s[x] - ref, s[x + 1] - ref));
                         tmem_st8(t_p + y * (kPage / 2), pk);

@@ -169,7 +169,10 @@ spd_status spd_keep_drafted(const spd_shape *shape, int64_t total_tokens, const 
         p.new_lens = end ? new_lens : nullptr;
         p.kept = end ? kept : nullptr;
         const int64_t heads = static_cast<int64_t>(p.num_pools) * s.num_kv_heads;
-        const unsigned y = parents ? static_cast<unsigned>(std::min<int64_t>(1024, std::max<int64_t>(1, (heads + per - 1) / per))) : 1u;
+        // A CTA finds its user's branch by a chain of loads before it moves anything: about two rounds of CTAs, each over several heads, where there
+        // are many users (512 users, 16 layers: 47 us with a CTA for every 16 heads).
+        const int64_t most = (heads + per - 1) / per, some_of = std::max<int64_t>(1, 16ll * sms / s.batch);
+        const unsigned y = parents ? static_cast<unsigned>(std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(1024, most), some_of))) : 1u;
         keep_kernel<<<dim3(static_cast<unsigned>(s.batch), y), kPgThreads, 0, static_cast<cudaStream_t>(cuda_stream)>>>(p, some);
         host::count_launch();
         if (cudaGetLastError() != cudaSuccess) return SPD_ERR_CUDA;
