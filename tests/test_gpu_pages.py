@@ -305,3 +305,54 @@ def test_captured():
     t.same()
     for a, b in copies.tolist()[1:]:
         assert all(torch.equal(p[a], p[b]) for p in pools)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_pages_beyond_32_bits(dtype):
+    """Pools of more than 2^32 bytes: attention, kept rows and copies at their far end."""
+    hkv, d = 8, 128
+    page = hkv * PAGE * d * (2 if dtype == torch.bfloat16 else 4)
+    n = 2**32 // page + 40
+    w = dr.batch([6, 3], [70, 0], [20, 33], 16, hkv, d, "bf16" if dtype == torch.bfloat16 else "f32", seed=13)
+    want, _, _, _, tol = dr.expected(w)
+    g = dr.OnDevice(w)
+    far = {}
+    for name, part in (("priv", g.priv), ("pub", g.pub)):
+        pools = [torch.empty((n, hkv, PAGE, d), dtype=dtype, device="cuda") for _ in range(2)]
+        shift = n - part.k_pool.shape[0]
+        for pool, small in zip(pools, (part.k_pool, part.v_pool)):
+            pool[shift:] = small
+        part.k_pool, part.v_pool = pools
+        part.page_indices += shift
+        far[name] = shift
+    dr.close(g.fused(), want, tol)
+    dr.close(g.halves()[0], want, tol)
+    pools = [g.pub.k_pool, g.pub.v_pool]
+    small = [p[far["pub"]:].cpu() for p in pools]
+    w.pub.page_indices = g.pub.page_indices.cpu() - far["pub"]
+    lens, names = keep_by_loops(w, [5, 1], small)
+    spd.spd_keep_drafted(g.shape, pools, g.pub, g.drafts["tok_indptr"], i32([5, 1]), g.ws, parents=g.drafts["parents"])
+    assert spd.spd_query_device_status(g.ws) == (spd.SPD_OK, -1) and g.pub.seq_lens.tolist() == lens
+    used = torch.cat([(p[far["pub"]:].cpu() == s) | (torch.isnan(s) & torch.isnan(p[far["pub"]:].cpu())) for p, s in zip(pools, small)])
+    assert bool(used.all())
+    spd.spd_pages_copy(g.shape, pools, i32([[n - 1, 1], [int(g.pub.page_indices[0]), n - 30]]), g.ws)
+    assert spd.spd_query_device_status(g.ws) == (spd.SPD_OK, -1)
+    for p in pools:
+        for a, b in ((n - 1, 1), (int(g.pub.page_indices[0]), n - 30)):
+            assert bool(((p[a] == p[b]) | (torch.isnan(p[a]) & torch.isnan(p[b]))).all())
+
+
+def test_take_from_a_large_pool_in_rounds():
+    """Pages are given out and come back until every page of a pool of many chunks has been used, by users of very different sizes."""
+    rng = np.random.default_rng(14)
+    t = Table(rng.integers(1, 4000, 40), 40001, seed=14)
+    for _ in range(6):
+        first = np.zeros(40)
+        last = np.minimum(np.diff(t.indptr) * PAGE, rng.integers(0, 64000, 40))
+        spd.spd_pages_take(*t.args(), i32(first), i32(last), t.ws)
+        short = t.take(first, last)
+        t.same((8, short[0]) if short else (spd.SPD_OK, -1))
+        gone = np.where(rng.random(40) < 0.4, 0, 1 << 30)
+        spd.spd_pages_release(*t.args(), i32(gone), t.ws)
+        t.release(gone)
+        t.same()
