@@ -17,7 +17,7 @@ using host::misaligned;
 // Query heads that a tile of RT rows takes of one token: all of a KV head's where they fit.
 int heads_per_tile(int g, int RT) { return g <= RT ? g : kHeadsPerItem; }
 
-constexpr int kFmaPerSm = 2;        // CTAs of the largest FMA variant that share an SM; the others fit more
+constexpr int kFmaMostPerSm = 4;    // CTAs of an FMA variant that may share an SM
 constexpr int kMostFmaRows = 64;
 constexpr int kTcOverhead = 6;      // what an item costs beside its blocks, in blocks
 constexpr int kFmaOverhead = 0;
@@ -28,7 +28,7 @@ DraftedLayout drafted_layout(const spd_shape &s, int sms) {
     const int g = s.num_q_heads / s.num_kv_heads;
     const int seqs = s.batch * s.num_kv_heads * (g > kHeadsPerItem ? g / kHeadsPerItem : 1);
     const bool tc = s.dtype == SPD_BF16;
-    const size_t slots = 2 * static_cast<size_t>(tc ? 1 : kFmaPerSm) * sms;
+    const size_t slots = 2 * static_cast<size_t>(tc ? 1 : kFmaMostPerSm) * sms;
     DraftedLayout L;
     L.records = host::cleared_end(s.batch, seqs);
     L.scratch = L.records + (slots * 2 * sizeof(int4) + 255) / 256 * 256;
@@ -57,7 +57,7 @@ spd_status launch_early(void (*kernel)(Args...), dim3 grid, int threads, size_t 
 
 template <int D, int RT, bool LOG2>
 spd_status launch_join(const DraftedParams &p, cudaStream_t st) {
-    return launch_early(drafted_join_kernel<D, RT, LOG2>, dim3(static_cast<unsigned>(p.grid), 2, kDrJoin), kDrJoinThreads, 0, st, p);
+    return launch_early(drafted_join_kernel<D, RT, LOG2>, dim3(static_cast<unsigned>(p.grid), 2, drafted_join_split(RT)), kDrJoinThreads, 0, st, p);
 }
 
 // [T][Hq][D] bf16 as a 3-D map: a box is `tokens` tokens x `heads` heads x 128 bytes, 128-byte swizzle.
@@ -161,33 +161,35 @@ spd_status run_tc(const DraftedParams &call, int D, int sms, cudaStream_t st) {
     return SPD_ERR_UNSUPPORTED;
 }
 
-template <typename E, int D, int RT>
+template <int D, int RT>
 spd_status launch_fma(DraftedParams p, int sms, cudaStream_t st) {
     using C = DraftedFma<D, RT>;
     static std::once_flag once[64];
+    static int fit[64];                 // CTAs that an SM holds at once
     int dev = 0;
     cudaGetDevice(&dev);
+    dev &= 63;
     cudaError_t err = cudaSuccess;
-    std::call_once(once[dev & 63], [&] {
-        err = cudaFuncSetAttribute(drafted_fma_kernel<E, D, RT>, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(C::smem_bytes()));
+    std::call_once(once[dev], [&] {
+        err = cudaFuncSetAttribute(drafted_fma_kernel<D, RT>, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(C::smem_bytes()));
+        if (err == cudaSuccess) err = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&fit[dev], drafted_fma_kernel<D, RT>, C::kThreads, C::smem_bytes());
     });
-    if (err != cudaSuccess) return SPD_ERR_CUDA;
+    if (err != cudaSuccess || fit[dev] < 1) return SPD_ERR_CUDA;
     p.hs = heads_per_tile(p.g, RT);
     p.hgroups = p.g / p.hs;
     p.tt = RT / p.hs;
     p.SQ = p.Hkv * p.hgroups;
     p.bt = kDrTiles;
     p.ov = kFmaOverhead;
-    p.grid = kFmaPerSm * sms;
-    const spd_status rc = launch_early(drafted_fma_kernel<E, D, RT>, dim3(static_cast<unsigned>(p.grid)), C::kThreads, C::smem_bytes(), st, p);
+    p.grid = (fit[dev] < kFmaMostPerSm ? fit[dev] : kFmaMostPerSm) * sms;
+    const spd_status rc = launch_early(drafted_fma_kernel<D, RT>, dim3(static_cast<unsigned>(p.grid)), C::kThreads, C::smem_bytes(), st, p);
     return rc != SPD_OK ? rc : launch_join<D, RT, false>(p, st);
 }
 
-template <typename E>
 spd_status run_fma(const DraftedParams &p, int D, int sms, cudaStream_t st) {
     const bool few = p.T * p.g <= 16ll * p.B;          // 16 rows of a KV head or fewer, by the mean over the users
-    if (D == 128) return few ? launch_fma<E, 128, 16>(p, sms, st) : launch_fma<E, 128, 64>(p, sms, st);
-    return few ? launch_fma<E, 64, 16>(p, sms, st) : launch_fma<E, 64, 64>(p, sms, st);
+    if (D == 128) return few ? launch_fma<128, 16>(p, sms, st) : launch_fma<128, 64>(p, sms, st);
+    return few ? launch_fma<64, 16>(p, sms, st) : launch_fma<64, 64>(p, sms, st);
 }
 
 spd_status check_part(const spd_shape &s, const spd_paged_kv *kv) {
@@ -259,7 +261,7 @@ spd_status run(const spd_shape *shape, const spd_score *score, const spd_drafts 
     p.records = reinterpret_cast<int4 *>(w + L.records);
     p.scratch = reinterpret_cast<float *>(w + L.scratch);
     cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
-    return s.dtype == SPD_BF16 ? run_tc(p, s.head_dim, sms, st) : run_fma<float>(p, s.head_dim, sms, st);
+    return s.dtype == SPD_BF16 ? run_tc(p, s.head_dim, sms, st) : run_fma(p, s.head_dim, sms, st);
 }
 
 }  // namespace

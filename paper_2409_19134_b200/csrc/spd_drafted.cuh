@@ -373,14 +373,15 @@ __device__ __forceinline__ void drafted_line(const DraftedParams &p, const Draft
 }
 
 // ---------------------------------------------------------------------------------------------------------------------
-// The join: CTAs (j, x, .) take a part of the item that the attention's CTA j left a piece of in its slot x, in proportion to the pieces; kDrJoin of
-// them share that part.  A thread joins 16 channels of a row: its neighbours' are the next rows', side by side in the slots, and it writes
+// The join: CTAs (j, x, .) take a part of the item that the attention's CTA j left a piece of in its slot x, in proportion to the pieces; up to
+// four of them share that part, one where a tile has few rows.  A thread joins 16 channels of a row: its neighbours' are the next rows', side by side in the slots, and it writes
 // whole sectors.
-constexpr int kDrJoin = 4, kDrJoinThreads = 128;
+constexpr int kDrJoinThreads = 128;
+__host__ __device__ constexpr int drafted_join_split(int RT) { return RT >= 256 ? 4 : RT >= 64 ? 2 : 1; }
 template <int D, int RT, bool LOG2>
 __global__ void __launch_bounds__(kDrJoinThreads) drafted_join_kernel(const __grid_constant__ DraftedParams p) {
     constexpr float kUnit = LOG2 ? 0.69314718055994531f : 1.f;
-    constexpr int AHEAD = 3;            // pieces under way at a time
+    constexpr int AHEAD = 3, SPLIT = drafted_join_split(RT);      // pieces under way at a time
     griddep_launch_dependents();        // what comes next may set itself up; it waits for this kernel's end before it looks at anything of this call
     griddep_wait();
     const int slot = 2 * blockIdx.x + blockIdx.y;
@@ -389,7 +390,7 @@ __global__ void __launch_bounds__(kDrJoinThreads) drafted_join_kernel(const __gr
     const int u = a.y, tok0 = a.z, sq = a.w, toks = b.x, c0 = b.y, c1 = b.z, pieces = c1 - c0 + 1, rows = toks * p.hs;
     const int h0 = sq / p.hgroups * p.g + sq % p.hgroups * p.hs;
     const bool bad = p.bad[u] == p.epoch;
-    const int E = rows * (D / 16), parts = pieces * kDrJoin, mine = (static_cast<int>(blockIdx.x) - c0) * kDrJoin + blockIdx.z;
+    const int E = rows * (D / 16), parts = pieces * SPLIT, mine = (static_cast<int>(blockIdx.x) - c0) * SPLIT + blockIdx.z;
     const int e0 = static_cast<int>(drafted_div(static_cast<int64_t>(E) * mine, parts)), e1 = static_cast<int>(drafted_div(static_cast<int64_t>(E) * (mine + 1), parts));
     auto exp_of = [](float x) { return LOG2 ? exp2f(x) : expf(x); };
     for (int e = e0 + threadIdx.x; e < e1; e += kDrJoinThreads) {

@@ -2,7 +2,11 @@
 //
 // RT rows (64, or 16 where users bring few) x 64 keys a block, RPT x 4 scores per thread; the 16 threads of a row keep its maximum and sum in
 // registers, weights go through shared memory to the threads that hold the row's channels (the same 16).  A hidden key's weight is the
-// mark -1, which the product with V skips: whatever its rows of k and v hold never enters.
+// mark -1, which the product with V skips: whatever its rows of k and v hold never enters.  V comes (cp.async) under the scores, the next block's K under
+// the weights and the product with V, so that a CTA has loads under way all the time.  Bound by shared-memory reads (RPT x 4 register tiles) and, where
+// rows are few, by what a CTA has under way.  Measured, fp32: 32 users x 4-token trees over 4 k tokens, 8 heads of 64: 264 us (2.0 TB/s; 512 without the
+// copies ahead and with two CTAs per SM), 32/8 heads of 128: 651 us (1.7); 8 users x 64 tokens over 4 k tokens, 32/8 heads of 128: 1.64 ms (21
+// TFLOP/s); 4 users x 12 tokens over 270-290 tokens, 8 heads of 64: 19 us with the join (44 with four rows per thread and blocks in pairs).
 #pragma once
 
 #include "spd_drafted.cuh"
@@ -27,7 +31,13 @@ template <> __device__ __forceinline__ float4 drafted_load4<__nv_bfloat16>(const
     return make_float4(a.x, a.y, b.x, b.y);
 }
 
-template <typename E, int D, int RT>
+__device__ __forceinline__ void drafted_copy16(uint32_t dst, const void *src, bool there) {       // zeros where there is nothing
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(there ? 16 : 0) : "memory");
+}
+__device__ __forceinline__ void drafted_copies_end() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+__device__ __forceinline__ void drafted_copies_wait1() { asm volatile("cp.async.wait_group 1;" ::: "memory"); }      // all but the last group
+
+template <int D, int RT>
 __global__ void __launch_bounds__(DraftedFma<D, RT>::kThreads) drafted_fma_kernel(const __grid_constant__ DraftedParams p) {
     using C = DraftedFma<D, RT>;
     constexpr int NT = C::kThreads, RPT = C::RPT, PITCH = C::kPitch, KB = kDrBlock, CH = D / 64;      // CH chunks of four channels per thread
@@ -35,8 +45,8 @@ __global__ void __launch_bounds__(DraftedFma<D, RT>::kThreads) drafted_fma_kerne
     float *Qs = sm, *Ks = Qs + RT * PITCH, *Vs = Ks + KB * PITCH, *Ps = Vs + KB * PITCH;
     __shared__ int64_t sums[NT];
     __shared__ int first_bad;
-    __shared__ DraftedTile tiles[kDrTiles];
-    __shared__ int tile_page[kDrTiles];
+    __shared__ DraftedTile tile_of[2][kDrTiles];
+    __shared__ int page_of[2][kDrTiles];
     __shared__ int16_t parent[kDrTree];
     __shared__ int16_t depths[kDrTree];
     __shared__ uint32_t lines[RT][kDrWords];
@@ -68,7 +78,7 @@ __global__ void __launch_bounds__(DraftedFma<D, RT>::kThreads) drafted_fma_kerne
         for (int e = tid; e < RT * (D / 4); e += NT) {
             const int r = e / (D / 4), c = e % (D / 4);
             float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-            if (r < rows) v = drafted_load4(static_cast<const E *>(p.q) + ((static_cast<int64_t>(s.first) + i0 + r / p.hs) * p.Hq + h0 + r % p.hs) * D + 4 * c);
+            if (r < rows) v = drafted_load4(static_cast<const float *>(p.q) + ((static_cast<int64_t>(s.first) + i0 + r / p.hs) * p.Hq + h0 + r % p.hs) * D + 4 * c);
             *reinterpret_cast<float4 *>(Qs + r * PITCH + 4 * c) = v;
         }
         if (p.parents != nullptr && s.good) {
@@ -96,32 +106,44 @@ __global__ void __launch_bounds__(DraftedFma<D, RT>::kThreads) drafted_fma_kerne
 #pragma unroll
             for (int c = 0; c < 4 * CH; ++c) o[i][c] = 0.f;
         }
-        for (int b = b0; b < b1; ++b) {
+        // pages of block b, by the first threads; a page that is out of range counts as one without tokens, and the user is flagged
+        auto look = [&](int b) {
             if (tid < kDrTiles) {
                 const DraftedTile t = drafted_tile(p, s, w.k, b * kDrTiles + tid);
                 int page = 0;
                 if (t.cnt > 0) page = p.part[t.part].indices[t.entry];
                 const bool ok = t.cnt > 0 && page >= 0 && page < p.part[t.part].num_pages;
-                tiles[tid] = t;
-                tile_page[tid] = ok ? page : (t.cnt > 0 ? -1 : -2);
+                tile_of[b & 1][tid] = t;
+                page_of[b & 1][tid] = ok ? page : (t.cnt > 0 ? -1 : -2);
             }
-            __syncthreads();
+        };
+        auto fetch = [&](int b, const void *const *pools, float *to) {
             for (int e = tid; e < KB * (D / 4); e += NT) {
-                const int key = e / (D / 4), c = e % (D / 4), t = key / kPage, slot = key % kPage;
-                float4 kv = make_float4(0.f, 0.f, 0.f, 0.f), vv = kv;
-                if (tile_page[t] >= 0 && slot < tiles[t].cnt) {
-                    const int64_t at = ((static_cast<int64_t>(tile_page[t]) * p.Hkv + kvh) * kPage + slot) * D + 4 * c;
-                    kv = drafted_load4(static_cast<const E *>(p.k_pool[tiles[t].part]) + at);
-                    vv = drafted_load4(static_cast<const E *>(p.v_pool[tiles[t].part]) + at);
-                }
-                *reinterpret_cast<float4 *>(Ks + key * PITCH + 4 * c) = kv;
-                *reinterpret_cast<float4 *>(Vs + key * PITCH + 4 * c) = vv;
+                const int key = e / (D / 4), c = e % (D / 4), t = key / kPage, slot = key % kPage, page = page_of[b & 1][t];
+                const DraftedTile &tile = tile_of[b & 1][t];
+                const bool there = page >= 0 && slot < tile.cnt;
+                const float *src = there ? static_cast<const float *>(pools[tile.part]) + ((static_cast<int64_t>(page) * p.Hkv + kvh) * kPage + slot) * D + 4 * c
+                                         : static_cast<const float *>(p.q);
+                drafted_copy16(smem_u32(to + key * PITCH + 4 * c), src, there);
             }
+        };
+        look(b0);
+        __syncthreads();
+        fetch(b0, p.k_pool, Ks);
+        drafted_copies_end();
+        for (int b = b0; b < b1; ++b) {
+            const DraftedTile *tiles = tile_of[b & 1];
+            const int *tile_page = page_of[b & 1];
+            if (b + 1 < b1) look(b + 1);
+            fetch(b, p.v_pool, Vs);
+            drafted_copies_end();
 #pragma unroll
             for (int t = 0; t < kDrTiles; ++t) bad = bad || tile_page[t] == -1;
-            __syncthreads();
-            if ((tid & ~31) / 16 * RPT < rows) {            // warps without a row have nothing to do
-                float sc[RPT][4];
+            drafted_copies_wait1();
+            __syncthreads();                              // K is there
+            float sc[RPT][4];
+            const bool work = (tid & ~31) / 16 * RPT < rows;      // warps without a row have nothing to do
+            if (work) {
 #pragma unroll
                 for (int i = 0; i < RPT; ++i)
 #pragma unroll
@@ -141,6 +163,11 @@ __global__ void __launch_bounds__(DraftedFma<D, RT>::kThreads) drafted_fma_kerne
                             sc[i][j] = fmaf(a[i].z, k4[j].z, sc[i][j]); sc[i][j] = fmaf(a[i].w, k4[j].w, sc[i][j]);
                         }
                 }
+            }
+            __syncthreads();                              // K is read
+            if (b + 1 < b1) fetch(b + 1, p.k_pool, Ks);
+            drafted_copies_end();
+            if (work) {
 #pragma unroll
                 for (int i = 0; i < RPT; ++i) {
                     bool seen[4];
@@ -183,7 +210,10 @@ __global__ void __launch_bounds__(DraftedFma<D, RT>::kThreads) drafted_fma_kerne
 #pragma unroll
                     for (int c = 0; c < 4 * CH; ++c) o[i][c] *= alpha;
                 }
-                __syncwarp();
+            }
+            drafted_copies_wait1();
+            __syncthreads();                              // V is there, and the weights
+            if (work) {
 #pragma unroll 2
                 for (int k4 = 0; k4 < KB; k4 += 4) {
                     float4 wt[RPT];
