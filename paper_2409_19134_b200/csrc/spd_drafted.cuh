@@ -204,8 +204,8 @@ __device__ __forceinline__ int64_t drafted_sums(const DraftedParams &p, int64_t 
     return (all + static_cast<int64_t>(tiles_all) * ov) * p.SQ;
 }
 
-// The item that holds unit x, by one warp.
-__device__ __forceinline__ void drafted_locate(const DraftedParams &p, const int64_t *sums, int C, int chunks, int ov, int64_t x, int lane, DraftedWalk &w) {
+// The item that holds unit x, by one warp.  False (here and below) where there is none: lengths that changed under the call.
+__device__ __forceinline__ bool drafted_locate(const DraftedParams &p, const int64_t *sums, int C, int chunks, int ov, int64_t x, int lane, DraftedWalk &w) {
     w.ov = ov;
     int c = 0;
     for (int c0 = 0; c0 < chunks; c0 += 32) {
@@ -213,7 +213,7 @@ __device__ __forceinline__ void drafted_locate(const DraftedParams &p, const int
         if (hit) { c = c0 + __ffs(hit) - 1; break; }
     }
     int64_t at = c == 0 ? 0 : sums[c - 1];
-    for (w.u = c * C;; ++w.u) {
+    for (w.u = c * C; w.u < p.B; ++w.u) {
         drafted_user(p, w.u, w.s);
         for (int rt0 = 0; rt0 * p.tt < w.s.n; rt0 += 32) {
             const int rt = rt0 + lane;
@@ -232,23 +232,27 @@ __device__ __forceinline__ void drafted_locate(const DraftedParams &p, const int
                 drafted_item_keys(p, w);
                 w.sq = static_cast<int>(drafted_div(x - at, w.k.nb + ov));
                 w.x0 = at + static_cast<int64_t>(w.sq) * (w.k.nb + ov);
-                return;
+                return true;
             }
             at += __shfl_sync(0xffffffffu, inc, 31);
         }
     }
+    return false;
 }
 
-// The next item; the caller knows that there is one.
-__device__ __forceinline__ void drafted_next(const DraftedParams &p, DraftedWalk &w) {
+// The next item.
+__device__ __forceinline__ bool drafted_next(const DraftedParams &p, DraftedWalk &w) {
     w.x0 += w.k.nb + w.ov;
-    if (++w.sq < p.SQ) return;
+    if (++w.sq < p.SQ) return true;
     w.sq = 0;
     if (++w.rt * p.tt >= w.s.n) {
         w.rt = 0;
-        do { ++w.u; drafted_user(p, w.u, w.s); } while (w.s.n == 0);
+        do {
+            if (++w.u >= p.B || !drafted_user(p, w.u, w.s)) return false;
+        } while (w.s.n == 0);
     }
     drafted_item_keys(p, w);
+    return true;
 }
 
 // What the join has to know of a piece: valid, user, first token of q and first token of the tile; (KV head, head group), tokens of the tile,

@@ -62,11 +62,20 @@ __global__ void __launch_bounds__(DraftedFma<D, RT>::kThreads) drafted_fma_kerne
     if (static_cast<int>(blockIdx.x) >= shares) return;
     int64_t x = drafted_bound(W, shares, blockIdx.x);
     const int64_t x1 = drafted_bound(W, shares, blockIdx.x + 1);
-    DraftedWalk w;
-    drafted_locate(p, sums, Cu, chunks, ov, x, lane, w);
-    for (;; drafted_next(p, w)) {
-        int b0, b1;
-        drafted_blocks(w, x, x1, b0, b1);
+    __shared__ DraftedWalk walk;                  // one warp's: all threads must go by the same item
+    __shared__ int found;
+    for (bool start = true;; start = false) {
+        if (tid < 32) {
+            DraftedWalk next;
+            if (!start) next = walk;
+            __syncwarp();
+            const bool is = start ? drafted_locate(p, sums, Cu, chunks, ov, x, lane, next) : drafted_next(p, next);
+            if (lane == 0) { walk = next; found = is; }
+        }
+        __syncthreads();
+        const DraftedWalk w = walk;
+        int b0 = 0, b1 = 0;
+        if (found) drafted_blocks(w, x, x1, b0, b1);
         x = w.x0 + w.ov + w.k.nb;                 // the next item, if it is this share's
         if (b0 == b1) break;
         const DraftedUser s = w.s;

@@ -152,7 +152,9 @@ __device__ __noinline__ void dt_slow_row(const DraftedTcParams &q, const DrPlan 
         if (see) {
             const DraftedTile d = drafted_tile(p, pl.s, pl.k, v);
             part = d.part;
-            at = ((static_cast<int64_t>(p.part[part].indices[d.entry]) * p.Hkv + pl.kvh) * kPage + slot) * D;
+            int page = p.part[part].indices[d.entry];
+            if (page < 0 || page >= p.part[part].num_pages) page = 0;        // it was in range a moment ago
+            at = ((static_cast<int64_t>(page) * p.Hkv + pl.kvh) * kPage + slot) * D;
             const __nv_bfloat16 *k = static_cast<const __nv_bfloat16 *>(p.k_pool[part]) + at;
             s = 0.f;
 #pragma unroll 4
@@ -238,7 +240,7 @@ drafted_tc_kernel(const __grid_constant__ DraftedTcParams q, const __grid_consta
     const int64_t x1 = drafted_bound(W, shares, blockIdx.x + 1);
     int64_t x = drafted_bound(W, shares, blockIdx.x);
     DraftedWalk w;
-    if (wid == 12) drafted_locate(p, sums, Cu, chunks, ov, x, lane, w);
+    if (wid == 12 && !drafted_locate(p, sums, Cu, chunks, ov, x, lane, w)) x = x1;
     if (tid == 320) {
         for (int b = 0; b < NBARS; ++b) {
             // Q and ring slots free: one per tile; S in registers, P written: one per softmax warp of the tile; rows exchanged, O's
@@ -586,10 +588,7 @@ drafted_tc_kernel(const __grid_constant__ DraftedTcParams q, const __grid_consta
             if (r >= 2) wait(&bar_planfree[r & 1], (r >> 1) - 1);
             __syncwarp();
             int b0 = 0, b1 = 0;
-            if (ok && x < x1) {
-                if (r > 0) drafted_next(p, w);
-                drafted_blocks(w, x, x1, b0, b1);
-            }
+            if (ok && x < x1 && (r == 0 || drafted_next(p, w))) drafted_blocks(w, x, x1, b0, b1);
             if (b0 == b1) {                             // the share is done, or ends inside the item's own cost
                 if (lane == 0) { pl.valid = 0; mbar_arrive(smem_u32(&bar_plan[r & 1])); }
                 break;

@@ -148,7 +148,7 @@ spd_status spd_keep_drafted(const spd_shape *shape, int64_t total_tokens, const 
     if (total_tokens < 0 || total_tokens >= (1ll << 31) || (!tok_indptr && total_tokens != s.batch)) return SPD_ERR_INVALID_ARG;
     if (!last || !page_indptr || !seq_lens || !ws || misaligned(ws, 256)) return SPD_ERR_INVALID_ARG;
     if (kept && (kept == tok_indptr || kept == parents || kept == last || kept == seq_lens)) return SPD_ERR_INVALID_ARG;
-    if (new_lens && (new_lens == tok_indptr || new_lens == last || new_lens == kept)) return SPD_ERR_INVALID_ARG;
+    if (new_lens && (new_lens == tok_indptr || new_lens == parents || new_lens == last || new_lens == kept)) return SPD_ERR_INVALID_ARG;
     const PagesLayout L = pages_layout(host::cleared_end(s.batch, seqs_of(s)), s.batch, 0);
     if (ws_bytes < L.total) return SPD_ERR_WORKSPACE;
     int sms = 0;

@@ -199,7 +199,8 @@ static __global__ void __launch_bounds__(kPgThreads) pages_give_kernel(const __g
         if (tid == 0) flag_error(p.hdr, 8 /* SPD_ERR_NO_PAGE */, u);
         return;
     }
-    auto fresh = [&](int r) {                      // the free page of rank r
+    auto fresh = [&](int r) {                      // the free page of rank r; -1 where tables changed under the call
+        if (p.chunks == 0 || r >= ends[p.chunks - 1]) return -1;
         int a = 0, b = p.chunks - 1;
         while (a < b) {
             const int mid = (a + b) / 2;
@@ -209,9 +210,10 @@ static __global__ void __launch_bounds__(kPgThreads) pages_give_kernel(const __g
         p.refs[page] = 1;
         return page;
     };
-    const int64_t lo = p.indptr[u];
+    int64_t lo, cap;
+    if (!pages_entries(p, u, lo, cap)) return;
     if (p.source == nullptr) {
-        const int64_t e0 = (p.from[u] + static_cast<int64_t>(kPage) - 1) / kPage, e1 = (p.to[u] + static_cast<int64_t>(kPage) - 1) / kPage;
+        const int64_t e0 = (max(p.from[u], 0) + static_cast<int64_t>(kPage) - 1) / kPage, e1 = min(cap, (p.to[u] + static_cast<int64_t>(kPage) - 1) / kPage);
         for (int64_t at = e0; at < e1; at += kPgThreads) {
             const int64_t e = at + tid;
             const bool wants = e < e1 && p.indices[lo + e] == -1;
@@ -222,14 +224,15 @@ static __global__ void __launch_bounds__(kPgThreads) pages_give_kernel(const __g
         }
     } else {
         const int s = p.source[u], len = p.lens[s];
-        const int64_t slo = p.indptr[s];
+        int64_t slo, scap;
+        if (!pages_entries(p, s, slo, scap) || len < 0 || (len + kPage - 1ll) / kPage > min(scap, cap)) return;
         for (int e = tid; e < len / kPage; e += kPgThreads) {
             const int page = p.indices[slo + e];
             p.indices[lo + e] = page;
             if (page >= 0) atomicAdd(&p.refs[page], 1);
         }
         if (tid == 0) {
-            if (len % kPage != 0) {
+            if (len % kPage != 0 && need > 0) {
                 const int page = fresh(rank);
                 p.copies[2 * u] = p.indices[slo + len / kPage];
                 p.copies[2 * u + 1] = page;
