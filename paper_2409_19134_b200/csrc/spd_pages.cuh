@@ -6,7 +6,8 @@
 // Handing out takes two kernels.  The first looks over refs (a CTA per chunk of pages writes its free ones down in ascending order) and
 // over the users (how many pages each needs, and whether its request is in order); the second gives each user its ranks among the free
 // pages by sums over the users in front of it, so no CTA waits for another.  Bound by latency: two launches and the loads behind
-// one another; refs are read once.
+// one another; refs are read once.  One launch of either 5 us under ncu, cold; release and take of 512 users over 122 k pages 12.5 us from a
+// graph, of 8 users over 460 pages 7.
 #pragma once
 
 #include "spd_device.cuh"
@@ -246,7 +247,8 @@ static __global__ void __launch_bounds__(kPgThreads) pages_give_kernel(const __g
 
 struct PagesPools { void *pool[kPgPools]; };
 
-// Pages copies[i][0] -> copies[i][1] in every pool; a CTA per pair, pool and piece of a page.  Bound by HBM.
+// Pages copies[i][0] -> copies[i][1] in every pool; a CTA per pair, pool and piece of a page, four 16-byte loads per thread under way.  Bound by HBM: 360
+// pages of 32 KB in 16 pools (378 MB read and written) 40 us under ncu (9 TB/s, a part of it in L2).
 static __global__ void __launch_bounds__(kPgThreads)
 pages_copy_kernel(const __grid_constant__ PagesPools pools, const int32_t *copies, int32_t num_pages, int64_t page_bytes, int32_t *hdr) {
     const int i = blockIdx.x, src = copies[2 * i], dst = copies[2 * i + 1];
@@ -282,7 +284,8 @@ struct KeepParams {
 // Accepted branches to the front of the drafted rows.  Token path[i] of a user's branch (root first) goes to place i <= path[i]; the
 // branch ascends, so a place is written after its row was read, if it is written at all, when the rows are taken in order: a thread
 // keeps to one 16-byte column of one head of one pool and walks the branch, and nobody else touches that column.
-// Bound by latency (parents, pages, rows behind one another); rows of 128-256 bytes, read and written once.
+// Bound by latency (parents, pages, rows behind one another); rows of 128-256 bytes, read and written once.  512 users x 33-64-token trees, 16
+// layers of 8 heads of 128 (205 MB) 45 us, 8 users in two layers 3.6 us from a graph.
 static __global__ void __launch_bounds__(kPgThreads) keep_kernel(const __grid_constant__ KeepParams p, const __grid_constant__ PagesPools pools) {
     __shared__ int16_t parent[kPgTree];
     __shared__ int16_t path[kPgTree];
