@@ -4,8 +4,8 @@
 // registers, weights go through shared memory to the threads that hold the row's channels (the same 16).  A hidden key's weight is the
 // mark -1, which the product with V skips: whatever its rows of k and v hold never enters.  V comes (cp.async) under the scores, the next block's K under
 // the weights and the product with V, so that a CTA has loads under way all the time.  Bound by shared-memory reads (RPT x 4 register tiles) and, where
-// rows are few, by what a CTA has under way.  Measured, fp32: 32 users x 4-token trees over 4 k tokens, 8 heads of 64: 264 us (2.0 TB/s; 512 without the
-// copies ahead and with two CTAs per SM), 32/8 heads of 128: 651 us (1.7); 8 users x 64 tokens over 4 k tokens, 32/8 heads of 128: 1.64 ms (21
+// rows are few, by what a CTA has under way.  Measured, fp32: 32 users x 4-token trees over 4 k tokens, 8 heads of 64: 264-276 us (2.0 TB/s; 512 without
+// the copies ahead and with two CTAs per SM), 32/8 heads of 128: 642 us (1.7); 8 users x 64 tokens over 4 k tokens, 32/8 heads of 128: 1.53 ms (22.5
 // TFLOP/s); 4 users x 12 tokens over 270-290 tokens, 8 heads of 64: 19 us with the join (44 with four rows per thread and blocks in pairs).
 #pragma once
 
@@ -19,17 +19,10 @@ constexpr int kDrTiles = kDrBlock / kPage;
 template <int D, int RT>
 struct DraftedFma {
     static constexpr int RPT = RT == 16 ? 2 : 4;                  // rows per thread
+    static constexpr int kPerSm = RT == 16 && D == 64 ? 4 : 1;   // CTAs of it that registers have to leave room for (shared memory allows so many)
     static constexpr int kThreads = RT / RPT * 16, kPitch = D + 4;       // rows of Q, K and V: 16-byte reads of 8 lanes fall in 32 banks
     static constexpr size_t smem_bytes() { return (static_cast<size_t>(RT + 2 * kDrBlock) * kPitch + RT * kDrBlock) * 4; }
 };
-
-template <typename E> __device__ __forceinline__ float4 drafted_load4(const E *p);
-template <> __device__ __forceinline__ float4 drafted_load4<float>(const float *p) { return *reinterpret_cast<const float4 *>(p); }
-template <> __device__ __forceinline__ float4 drafted_load4<__nv_bfloat16>(const __nv_bfloat16 *p) {
-    const uint2 w = *reinterpret_cast<const uint2 *>(p);
-    const float2 a = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162 *>(&w.x)), b = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162 *>(&w.y));
-    return make_float4(a.x, a.y, b.x, b.y);
-}
 
 __device__ __forceinline__ void drafted_copy16(uint32_t dst, const void *src, bool there) {       // zeros where there is nothing
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(there ? 16 : 0) : "memory");
@@ -38,7 +31,7 @@ __device__ __forceinline__ void drafted_copies_end() { asm volatile("cp.async.co
 __device__ __forceinline__ void drafted_copies_wait1() { asm volatile("cp.async.wait_group 1;" ::: "memory"); }      // all but the last group
 
 template <int D, int RT>
-__global__ void __launch_bounds__(DraftedFma<D, RT>::kThreads) drafted_fma_kernel(const __grid_constant__ DraftedParams p) {
+__global__ void __launch_bounds__(DraftedFma<D, RT>::kThreads, DraftedFma<D, RT>::kPerSm) drafted_fma_kernel(const __grid_constant__ DraftedParams p) {
     using C = DraftedFma<D, RT>;
     constexpr int NT = C::kThreads, RPT = C::RPT, PITCH = C::kPitch, KB = kDrBlock, CH = D / 64;      // CH chunks of four channels per thread
     extern __shared__ __align__(16) float sm[];
@@ -82,39 +75,6 @@ __global__ void __launch_bounds__(DraftedFma<D, RT>::kThreads) drafted_fma_kerne
         const int i0 = w.rt * p.tt, toks = min(p.tt, s.n - i0), rows = toks * p.hs;
         const int kvh = w.sq / p.hgroups, h0 = kvh * p.g + w.sq % p.hgroups * p.hs;
         bool bad = !s.good;
-        // ---- Q, and the tree
-        __syncthreads();
-        for (int e = tid; e < RT * (D / 4); e += NT) {
-            const int r = e / (D / 4), c = e % (D / 4);
-            float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-            if (r < rows) v = drafted_load4(static_cast<const float *>(p.q) + ((static_cast<int64_t>(s.first) + i0 + r / p.hs) * p.Hq + h0 + r % p.hs) * D + 4 * c);
-            *reinterpret_cast<float4 *>(Qs + r * PITCH + 4 * c) = v;
-        }
-        if (p.parents != nullptr && s.good) {
-            bool wrong = false;
-            for (int i = tid; i < s.n; i += NT) {
-                const int up = p.parents[s.first + i];
-                wrong = wrong || up < -1 || up >= i;
-                parent[i] = static_cast<int16_t>(up < -1 || up >= i ? -1 : up);
-            }
-            if (__syncthreads_or(wrong)) { bad = true; }
-            for (int i = tid; i < s.n; i += NT) depths[i] = static_cast<int16_t>(drafted_depth(parent, i));
-            __syncthreads();
-            for (int i = tid; i < toks; i += NT) drafted_line(p, s, parent, i0 + i, depths[i0 + i], lines[i]);
-        }
-        __syncthreads();
-        int pos[RPT], tok[RPT];              // positions and tokens (within the tile) of the thread's rows
-        float slope[RPT], m[RPT], l[RPT], o[RPT][4 * CH];
-#pragma unroll
-        for (int i = 0; i < RPT; ++i) {
-            const int r = min(RPT * ty + i, rows - 1);
-            tok[i] = r / p.hs;
-            pos[i] = s.ctx + (p.parents ? (s.good ? depths[i0 + tok[i]] : 0) : i0 + tok[i]);
-            slope[i] = p.slopes ? p.slopes[h0 + r % p.hs] : 0.f;
-            m[i] = -INFINITY; l[i] = 0.f;
-#pragma unroll
-            for (int c = 0; c < 4 * CH; ++c) o[i][c] = 0.f;
-        }
         // pages of block b, by the first threads; a page that is out of range counts as one without tokens, and the user is flagged
         auto look = [&](int b) {
             if (tid < kDrTiles) {
@@ -136,10 +96,42 @@ __global__ void __launch_bounds__(DraftedFma<D, RT>::kThreads) drafted_fma_kerne
                 drafted_copy16(smem_u32(to + key * PITCH + 4 * c), src, there);
             }
         };
-        look(b0);
+        // ---- the first pages, Q and K on their way while the tree is walked
         __syncthreads();
+        look(b0);
+        for (int e = tid; e < RT * (D / 4); e += NT) {
+            const int r = e / (D / 4), c = e % (D / 4);
+            const int64_t row = r < rows ? (static_cast<int64_t>(s.first) + i0 + r / p.hs) * p.Hq + h0 + r % p.hs : 0;
+            drafted_copy16(smem_u32(Qs + r * PITCH + 4 * c), static_cast<const float *>(p.q) + row * D + 4 * c, r < rows);
+        }
+        bool wrong = false;
+        const bool tree = p.parents != nullptr && s.good;
+        for (int i = tid; tree && i < s.n; i += NT) {
+            const int up = p.parents[s.first + i];
+            wrong = wrong || up < -1 || up >= i;
+            parent[i] = static_cast<int16_t>(up < -1 || up >= i ? -1 : up);
+        }
+        bad = __syncthreads_or(wrong) || bad;
         fetch(b0, p.k_pool, Ks);
         drafted_copies_end();
+        if (tree) {
+            for (int i = tid; i < s.n; i += NT) depths[i] = static_cast<int16_t>(drafted_depth(parent, i));
+            __syncthreads();
+            for (int i = tid; i < toks; i += NT) drafted_line(p, s, parent, i0 + i, depths[i0 + i], lines[i]);
+            __syncthreads();
+        }
+        int pos[RPT], tok[RPT];              // positions and tokens (within the tile) of the thread's rows
+        float slope[RPT], m[RPT], l[RPT], o[RPT][4 * CH];
+#pragma unroll
+        for (int i = 0; i < RPT; ++i) {
+            const int r = min(RPT * ty + i, rows - 1);
+            tok[i] = r / p.hs;
+            pos[i] = s.ctx + (p.parents ? (s.good ? depths[i0 + tok[i]] : 0) : i0 + tok[i]);
+            slope[i] = p.slopes ? p.slopes[h0 + r % p.hs] : 0.f;
+            m[i] = -INFINITY; l[i] = 0.f;
+#pragma unroll
+            for (int c = 0; c < 4 * CH; ++c) o[i][c] = 0.f;
+        }
         for (int b = b0; b < b1; ++b) {
             const DraftedTile *tiles = tile_of[b & 1];
             const int *tile_page = page_of[b & 1];

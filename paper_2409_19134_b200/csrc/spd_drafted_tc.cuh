@@ -139,6 +139,12 @@ __device__ __forceinline__ uint32_t dt_sees(const DraftedParams &p, const DrPlan
     return m;
 }
 
+__device__ __forceinline__ float4 dt_load4(const __nv_bfloat16 *p) {
+    const uint2 w = *reinterpret_cast<const uint2 *>(p);
+    const float2 a = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162 *>(&w.x)), b = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162 *>(&w.y));
+    return make_float4(a.x, a.y, b.x, b.y);
+}
+
 // One row of a piece the slow way, by a whole warp: 32 keys at a time, a score per lane, then four channels of O per lane.  Keys that the row
 // does not see are not touched.
 template <int D>
@@ -168,7 +174,7 @@ __device__ __noinline__ void dt_slow_row(const DraftedTcParams &q, const DrPlan 
             s = 0.f;
 #pragma unroll 4
             for (int c = 0; c < D; c += 4) {
-                const float4 a = drafted_load4(qr + c), b = drafted_load4(k + c);
+                const float4 a = dt_load4(qr + c), b = dt_load4(k + c);
                 s = fmaf(a.x, b.x, s); s = fmaf(a.y, b.y, s); s = fmaf(a.z, b.z, s); s = fmaf(a.w, b.w, s);
             }
             s *= p.sm_scale;
@@ -194,7 +200,7 @@ __device__ __noinline__ void dt_slow_row(const DraftedTcParams &q, const DrPlan 
             const int64_t a = __shfl_sync(0xffffffffu, at, x);
             const int pt = __shfl_sync(0xffffffffu, part, x);
             if (lane < D / 4) {
-                const float4 b = drafted_load4(static_cast<const __nv_bfloat16 *>(p.v_pool[pt]) + a + 4 * lane);
+                const float4 b = dt_load4(static_cast<const __nv_bfloat16 *>(p.v_pool[pt]) + a + 4 * lane);
                 o.x = fmaf(wt, b.x, o.x); o.y = fmaf(wt, b.y, o.y); o.z = fmaf(wt, b.z, o.z); o.w = fmaf(wt, b.w, o.w);
             }
         }
