@@ -5,7 +5,7 @@
 //     the context and, among the drafted tokens, itself and its ancestors, each where pos_i - pos_j < window or pos_j < sinks;
 //     s = sm_scale q.k;  s <- cap tanh(s / cap);  s <- s - slope_h (pos_i - pos_j).
 // Rows that read the same keys are computed together: an item is (user, tile of tokens x heads of one group, KV head), its keys the page
-// tiles that some row of it may see (those that hold sinks, then from the widest window on), kDrBlock keys at a time.  All items' blocks
+// tiles that some row of it may see (those that hold sinks, then from the widest window on), a block of `bt` page tiles at a time.  All items' blocks
 // laid end to end are cut into equal shares, one per CTA, whatever the batch looks like: an item inside a share is finished there, one that
 // is cut leaves (O, m, l) per piece in scratch, and a second kernel joins the pieces (Theorem 1) in order, so that results do not
 // depend on who came first.  No CTA waits for another.
