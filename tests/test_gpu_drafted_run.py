@@ -199,3 +199,32 @@ def test_two_streams():
     for o, x in zip(outs, want):
         dr.close(o[0], x[0], x[4])
         assert all(torch.equal(o[0], y) for y in o)
+
+
+def test_two_graphs_on_one_workspace():
+    """Two captured calls of one shape that share a workspace, replayed in turns on one stream, with eager calls in between."""
+    ws = [dr.batch([5, 17, 1], [700, 30, 64], [3, 0, 16], 8, 2, 128, "bf16", seed=73), dr.batch([33, 2, 9], [90, 1500, 0], [0, 40, 7], 8, 2, 128, "bf16", seed=74)]
+    gs = [dr.OnDevice(w) for w in ws]
+    gs[1].ws = gs[0].ws
+    want, outs, graphs = [dr.expected(w) for w in ws], [g.out() for g in gs], []
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        for g, o in zip(gs, outs):
+            g.fused(out=o)
+    torch.cuda.current_stream().wait_stream(side)
+    for g, o in zip(gs, outs):
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[-1]):
+            g.fused(out=o)
+    for i in range(20):
+        for o in outs:
+            o.fill_(float("nan"))
+        graphs[i % 2].replay()
+        eager = gs[0].fused()
+        graphs[1 - i % 2].replay()
+        torch.cuda.synchronize()
+        assert torch.equal(eager, outs[0])
+    for o, x in zip(outs, want):
+        dr.close(o, x[0], x[4])
+    assert spd.spd_query_device_status(gs[0].ws) == (spd.SPD_OK, -1)
