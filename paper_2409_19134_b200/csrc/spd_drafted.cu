@@ -95,7 +95,7 @@ uint64_t twice(double x) {              // an fp32 value in both halves of a two
     return (static_cast<uint64_t>(u) << 32) | u;
 }
 
-template <int D, bool CAP, bool BIAS>
+template <int D, int CAP, bool BIAS>
 spd_status launch_tc(const DraftedTcParams &p, const CUtensorMap *maps, cudaStream_t st) {
     static std::once_flag once[64];
     int dev = 0;
@@ -123,21 +123,21 @@ spd_status run_tc(const DraftedParams &call, int D, int sms, cudaStream_t st) {
     d.grid = sms;
     p.c2 = d.sm_scale * kLog2e;
     d.ov = kTcOverhead;
-    p.half_at = p.one_at = -1.f;
+    int cap = 0;
     if (d.cap > 0.f) {
         const double y1 = static_cast<double>(d.sm_scale) / d.cap;
         p.cap2 = d.cap * kLog2e;
-        p.y1 = static_cast<float>(fmin(y1, 1e30));
-        bool fits1 = true, fits2 = true;                  // coefficients that leave fp32's normal range: the exact form does it
+        p.y1 = static_cast<float>(fmax(fmin(y1, 1e30), 1.5e-45));      // not 0: infinite scores stay infinite
+        bool fits = true;                                 // the coefficients carry the cap
         auto normal = [](double c) { return fabs(c) > 1e-37 && fabs(c) < 1e37; };
         for (int i = 0; i < 6; ++i) {
             const double c = d.cap * 1.4426950408889634 * pow(y1, 2 * i + 1);
-            if (i < 4) { p.p1[i] = twice(c * kTanhHalf[i]); fits1 = fits1 && normal(c * kTanhHalf[i]); }
-            p.p2[i] = twice(c * kTanhOne[i]);
-            fits2 = fits2 && normal(c * kTanhOne[i]);
+            if (i < 4) { p.p1[i] = twice(c * kTanhHalf[i]); fits = fits && normal(c * kTanhHalf[i]); }
+            p.p2[i] = twice(c * kTanhOne[i]);             // where a mask comes on top of the cap, this longer one serves both ranges
+            fits = fits && normal(c * kTanhOne[i]);
         }
-        if (fits2) p.one_at = 1.f;
-        if (fits1 && fits2) p.half_at = 0.5f;             // where a mask comes on top of the cap, the longer one serves both ranges
+        cap = fits ? 1 : 2;
+        for (int i = 0; i < 6 && !fits; ++i) p.p2[i] = twice(kTanhOne[i]);
     }
     // A tile whose rows are done one by one takes its warps about 4 us per key: 64 polls or so, beyond the usual limit.
     const int64_t keys = (static_cast<int64_t>(d.part[0].num_pages) + d.part[1].num_pages) * kPage, polls = static_cast<int64_t>(kWaitLimit) + 64 * keys;
@@ -153,10 +153,11 @@ spd_status run_tc(const DraftedParams &call, int D, int sms, cudaStream_t st) {
             maps[1 + 2 * x] = maps[2 + 2 * x] = maps[0];   // never loaded from
         }
     }
-    const bool cap = d.cap > 0.f, bias = d.slopes != nullptr;
+    const bool bias = d.slopes != nullptr;
 #define SPD_DT_CASE(DD, CC, BB) if (D == DD && cap == CC && bias == BB) return launch_tc<DD, CC, BB>(p, maps, st);
-    SPD_DT_CASE(128, false, false) SPD_DT_CASE(128, true, false) SPD_DT_CASE(128, false, true) SPD_DT_CASE(128, true, true)
-    SPD_DT_CASE(64, false, false) SPD_DT_CASE(64, true, false) SPD_DT_CASE(64, false, true) SPD_DT_CASE(64, true, true)
+    SPD_DT_CASE(128, 0, false) SPD_DT_CASE(128, 1, false) SPD_DT_CASE(128, 2, false) SPD_DT_CASE(128, 0, true) SPD_DT_CASE(128, 1, true)
+    SPD_DT_CASE(128, 2, true) SPD_DT_CASE(64, 0, false) SPD_DT_CASE(64, 1, false) SPD_DT_CASE(64, 2, false) SPD_DT_CASE(64, 0, true)
+    SPD_DT_CASE(64, 1, true) SPD_DT_CASE(64, 2, true)
 #undef SPD_DT_CASE
     return SPD_ERR_UNSUPPORTED;
 }

@@ -65,8 +65,8 @@ struct DraftedTcParams {
     int32_t tpt;                // tokens per tile
     float c2;                   // sm_scale log2(e)
     float cap2, y1;             // cap log2(e); sm_scale / cap
-    float half_at, one_at;      // where the two polynomials end (1/2 and 1; -1 = not to be used)
-    uint64_t p1[4], p2[6];      // of cap2 tanh(y1 x) = x P(x^2) for |y1 x| <= 1/2 and <= 1, each in both halves
+    uint64_t p1[4], p2[6];      // coefficients for |y1 x| <= 1/2 and <= 1, each in both halves.  CAP 1: of cap2 tanh(y1 x) = x P(x^2); CAP 2: of
+                                // tanh(y) = y P(y^2), p2 alone
     uint32_t wait_limit;
 };
 
@@ -215,7 +215,9 @@ __device__ __noinline__ void dt_slow_row(const DraftedTcParams &q, const DrPlan 
     }
 }
 
-template <int D, bool CAP, bool BIAS>
+// CAP: 0 none, 1 one that the polynomials' coefficients carry, 2 a cap for which those would leave fp32's normal range (tiny ones, and large ones: from 202 on at
+// head_dim 128, 295 at 64, with a scale of 1 / sqrt(head_dim)).
+template <int D, int CAP, bool BIAS>
 __global__ void __launch_bounds__(kDtThreads, 1)
 drafted_tc_kernel(const __grid_constant__ DraftedTcParams q, const __grid_constant__ CUtensorMap mq, const __grid_constant__ CUtensorMap mk0,
                   const __grid_constant__ CUtensorMap mv0, const __grid_constant__ CUtensorMap mk1, const __grid_constant__ CUtensorMap mv1) {
@@ -344,6 +346,17 @@ drafted_tc_kernel(const __grid_constant__ DraftedTcParams q, const __grid_consta
                 const uint64_t f = fma_f32x2(fma_f32x2(fma_f32x2(y, q.p2[5], q.p2[4]), y, q.p2[3]), y, q.p2[2]);
                 return fma_f32x2(fma_f32x2(f, y, q.p2[1]), y, q.p2[0]);
             };
+            // CAP 2.  Large caps lie far above most scores, and the special-function unit's error is 2^-22 of the cap: each score up to the cap goes by the
+            // polynomial, cap2 tanh(y1 x) = c2 x P((y1 x)^2), whatever its neighbours are.  all: none is beyond the cap.
+            auto far_capped = [&](uint64_t s2, bool all, float &x0, float &x1) {
+                float s0, s1, u0, u1, c0, c1;
+                const uint64_t y2 = mul_f32x2(s2, pack_f32x2(q.y1, q.y1));
+                unpack_f32x2(mul_f32x2(poly2(mul_f32x2(y2, y2)), mul_f32x2(s2, pack_f32x2(q.c2, q.c2))), c0, c1);
+                unpack_f32x2(s2, s0, s1);
+                unpack_f32x2(y2, u0, u1);
+                x0 = all || fabsf(u0) <= 1.f ? c0 : capped(s0);
+                x1 = all || fabsf(u1) <= 1.f ? c1 : capped(s1);
+            };
             // Weights are summed as they are rounded for the product with V: numerator and sum are off alike.
             uint64_t lsum2 = 0;
             auto weigh = [&](uint64_t arg2) {
@@ -385,9 +398,18 @@ drafted_tc_kernel(const __grid_constant__ DraftedTcParams q, const __grid_consta
 #pragma unroll
                         for (int y = 0; y < KB; y += 2) big[(y >> 1) & 3] = fmax3_abs_nan(big[(y >> 1) & 3], sv[y], sv[y + 1]);
                         const float most = fmax3_abs_nan(fmax3_abs_nan(big[0], big[1], big[2]), big[3], 0.f) * q.y1;
-                        form = __all_sync(0xffffffffu, most <= q.half_at) ? 1 : __all_sync(0xffffffffu, most <= q.one_at) ? 2 : 0;
+                        form = CAP == 1 && __all_sync(0xffffffffu, most <= 0.5f) ? 1 : __all_sync(0xffffffffu, most <= 1.f) ? 2 : 0;
                     }
-                    if constexpr (CAP && BIAS) {                  // the bias comes on top of capped scores
+                    if constexpr (CAP == 2) {
+                        if (form != 0) {
+#pragma unroll
+                            for (int y = 0; y < KB; y += 2) far_capped(pair(y), true, sv[y], sv[y + 1]);
+                        } else {
+#pragma unroll
+                            for (int y = 0; y < KB; y += 2) far_capped(pair(y), false, sv[y], sv[y + 1]);
+                        }
+                    }
+                    if constexpr (CAP == 1 && BIAS) {             // the bias comes on top of capped scores
                         if (form != 0) {
 #pragma unroll
                             for (int y = 0; y < KB; y += 2) { const uint64_t s2 = pair(y); unpack_f32x2(mul_f32x2(poly2(mul_f32x2(s2, s2)), s2), sv[y], sv[y + 1]); }
@@ -405,14 +427,14 @@ drafted_tc_kernel(const __grid_constant__ DraftedTcParams q, const __grid_consta
 #pragma unroll
                     for (int y = 0; y < KB; y += 2) r4[(y >> 1) & 3] = fmax3(r4[(y >> 1) & 3], sv[y], sv[y + 1]);
                     const float mx = fmaxf(fmaxf(r4[0], r4[1]), fmaxf(r4[2], r4[3]));
-                    const float ref = refer(i, BIAS ? mx : CAP ? capped(mx) : mx * q.c2, o_ready);
+                    const float ref = refer(i, BIAS || CAP == 2 ? mx : CAP ? capped(mx) : mx * q.c2, o_ready);
                     const uint64_t mx2 = pack_f32x2(-ref, -ref), c22 = pack_f32x2(q.c2, q.c2);
                     uint32_t pk[KB / 2];
                     auto weights = [&](auto &&arg) {
 #pragma unroll
                         for (int y = 0; y < KB / 2; ++y) pk[y] = weigh(arg(2 * y));
                     };
-                    if constexpr (BIAS) {
+                    if constexpr (BIAS || CAP == 2) {
                         weights([&](int y) { return add_f32x2(pair(y), mx2); });
                     } else if constexpr (CAP) {
                         if (form == 1) weights([&](int y) { const uint64_t s2 = pair(y); return fma_f32x2(poly1(mul_f32x2(s2, s2)), s2, mx2); });
@@ -451,7 +473,11 @@ drafted_tc_kernel(const __grid_constant__ DraftedTcParams q, const __grid_consta
                             float most = 0.f;
 #pragma unroll
                             for (int x = 0; x < kPage; x += 2) most = fmax3_abs_nan(most, s[x], s[x + 1]);
-                            if (__all_sync(0xffffffffu, most * q.y1 <= q.one_at)) {
+                            const bool small = __all_sync(0xffffffffu, most * q.y1 <= 1.f);
+                            if constexpr (CAP == 2) {
+#pragma unroll
+                                for (int x = 0; x < kPage; x += 2) far_capped(pack_f32x2(s[x], s[x + 1]), small, s[x], s[x + 1]);
+                            } else if (small) {
 #pragma unroll
                                 for (int x = 0; x < kPage; x += 2) {
                                     const uint64_t s2 = pack_f32x2(s[x], s[x + 1]);

@@ -1,0 +1,65 @@
+"""Capped scores of drafted tokens over the whole range of caps, with error bounds relative to the scores where the cap is far above them."""
+import pytest
+import torch
+
+from paper_2409_19134_b200 import binding as spd
+from tests import drafted_reference as dr
+from tests import scored_reference as ref
+
+pytestmark = pytest.mark.gpu
+
+
+def ok(d):
+    assert spd.spd_query_device_status(d.ws) == (spd.SPD_OK, -1)
+
+
+# The cap's own error.  Caps that the polynomials' coefficients carry (up to about 200 at head_dim 128 and 300 at 64, with the scale of these batches): 2^-21 of the
+# cap, as a maximum or a block with greater scores goes by the special-function unit.  Larger ones: an odd polynomial that is off by 3.2e-6 of
+# the score, and five roundings of 2^-24, below 2^-18 of the score; beyond the cap itself 2^-21 of it.
+def cap_error(cap, S):
+    return 2.0 ** -21 * cap if cap < 300 else min(2.0 ** -21 * cap, 2.0 ** -18 * S)
+
+
+def score_error(D, S, cap, bias):
+    return D * 2.0 ** -24 * S + cap_error(cap, S) + 2.0 ** -23 * bias
+
+
+def bound(vmax, D, S, n, cap, bias, weight):
+    return (2.0 * (score_error(D, S, cap, bias) + 2.0 ** -21 + n * 2.0 ** -24) + weight) * vmax
+
+
+@pytest.mark.parametrize("cap", [0.01, 20.0, 150.0, 210.0, 300.0, 1e3, 1e4, 1e5, 1e6, 1e8, 1e30])
+@pytest.mark.parametrize("d,kind,window", [(64, "tree", 0), (64, "run", 130), (128, "tree", 100), (128, "run", 0)])
+@pytest.mark.parametrize("alibi", [False, True])
+def test_caps_over_their_range(cap, d, kind, window, alibi, monkeypatch):
+    """Scores from far below every cap to far above the small ones, side by side in a tile; blocks seen whole and blocks with masks."""
+    w = dr.batch([9, 40, 3], [400, 170, 90], [37, 20, 0], 4, 2, d, "bf16", seed=d, kind=kind)
+    w.q *= torch.logspace(-2, 1.5, 52)[torch.randperm(52, generator=torch.Generator().manual_seed(1))][:, None, None].bfloat16()
+    g = dr.OnDevice(w, cap, window, 5 if window else 0, alibi)
+    args = cap, window, 5 if window else 0, g.slopes
+
+    monkeypatch.setattr(ref, "bound", bound)
+    want, _, _, _, tol = dr.expected(w, *args)
+    dr.close(g.fused(), want, tol, "fused")
+    out, part = g.halves()
+    dr.close(out, want, tol, "halves")
+    ok(g)
+    # the private half's maxima say how exact the scores are, without the rounding of the weights; 2^-22: there and back between natural and log2 units
+    monkeypatch.setattr(ref, "bound", lambda vmax, D, S, n, cap, bias, weight: score_error(D, S, cap, bias))
+    _, _, m, l, err = dr.expected(w, *args, parts=(True, False))
+    seen = l > 0
+    assert bool(((part[1].cpu().double() - m).abs()[seen] <= (err + 2.0 ** -22 * m.abs())[seen]).all())
+
+
+@pytest.mark.parametrize("alibi", [False, True])
+def test_huge_caps_change_nothing(alibi, monkeypatch):
+    """At 1e8 a score is capped by less than its own rounding."""
+    w = dr.batch([9, 40], [400, 170], [37, 20], 4, 2, 128, "bf16", seed=3)
+    monkeypatch.setattr(ref, "bound", bound)
+    outs, tols = [], []
+    for cap in (0.0, 1e8):
+        g = dr.OnDevice(w, cap, 0, 0, alibi)
+        outs.append(g.fused())
+        tols.append(dr.expected(w, cap, 0, 0, g.slopes)[4])
+        ok(g)
+    dr.close(outs[1], outs[0].cpu().double(), tols[0] + tols[1])
