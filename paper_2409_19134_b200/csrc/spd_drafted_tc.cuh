@@ -397,7 +397,8 @@ drafted_tc_kernel(const __grid_constant__ DraftedTcParams q, const __grid_consta
                         float big[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
                         for (int y = 0; y < KB; y += 2) big[(y >> 1) & 3] = fmax3_abs_nan(big[(y >> 1) & 3], sv[y], sv[y + 1]);
-                        const float most = fmax3_abs_nan(fmax3_abs_nan(big[0], big[1], big[2]), big[3], 0.f) * q.y1;
+                        // rows of nobody hold another user's q, or what was there before: they have no vote
+                        const float most = live ? fmax3_abs_nan(fmax3_abs_nan(big[0], big[1], big[2]), big[3], 0.f) * q.y1 : 0.f;
                         form = CAP == 1 && __all_sync(0xffffffffu, most <= 0.5f) ? 1 : __all_sync(0xffffffffu, most <= 1.f) ? 2 : 0;
                     }
                     if constexpr (CAP == 2) {
@@ -473,7 +474,7 @@ drafted_tc_kernel(const __grid_constant__ DraftedTcParams q, const __grid_consta
                             float most = 0.f;
 #pragma unroll
                             for (int x = 0; x < kPage; x += 2) most = fmax3_abs_nan(most, s[x], s[x + 1]);
-                            const bool small = __all_sync(0xffffffffu, most * q.y1 <= 1.f);
+                            const bool small = __all_sync(0xffffffffu, !live || most * q.y1 <= 1.f);
                             if constexpr (CAP == 2) {
 #pragma unroll
                                 for (int x = 0; x < kPage; x += 2) far_capped(pack_f32x2(s[x], s[x + 1]), small, s[x], s[x + 1]);

@@ -1,4 +1,5 @@
-"""Capped scores of drafted tokens over the whole range of caps, with error bounds relative to the scores where the cap is far above them."""
+"""Capped scores of drafted tokens over the whole range of caps, with error bounds relative to the scores where the cap is far above them, and
+rows whose bits must not depend on what lies beside them."""
 import pytest
 import torch
 
@@ -63,3 +64,34 @@ def test_huge_caps_change_nothing(alibi, monkeypatch):
         tols.append(dr.expected(w, cap, 0, 0, g.slopes)[4])
         ok(g)
     dr.close(outs[1], outs[0].cpu().double(), tols[0] + tols[1])
+
+
+def capped(w, cap=20.0, window=0):
+    g = dr.OnDevice(w, cap, window)
+    out = g.fused()
+    ok(g)
+    return out
+
+
+@pytest.mark.parametrize("kind,window", [("tree", 0), ("run", 0), ("run", 60)])
+@pytest.mark.parametrize("cap", [20.0, 1e4])
+def test_a_neighbour_does_not_choose_the_arithmetic(kind, window, cap):
+    """A tile's rows behind a user's last token hold the next user's q: whatever it is, the first user's bits stay."""
+    outs = []
+    for scale in (0.01, 1.0, 1e3, float("nan")):
+        w = dr.batch([5, 30], [400, 200], [9, 3], 8, 2, 128, "bf16", seed=17, kind=kind)
+        w.q[5:] *= scale
+        outs.append(capped(w, cap, window)[:5])
+    assert all(torch.equal(outs[0], x) for x in outs[1:])
+
+
+def test_what_shared_memory_held_chooses_no_arithmetic():
+    """Groups of 24 leave 8 rows of a tile without a query: whatever an earlier call left there, the bits stay."""
+    w = dr.batch([5, 3], [400, 200], [9, 3], 24, 1, 64, "bf16", seed=18)
+    outs = []
+    for scale in (0.01, 1e3, float("nan")):
+        other = dr.batch([64, 64], [9000, 9000], [0, 0], 4, 1, 64, "bf16", seed=19, kind="run")      # all rows of both tiles, on every SM
+        other.q *= scale
+        dr.OnDevice(other).fused()
+        outs.append(capped(w))
+    assert all(torch.equal(outs[0], x) for x in outs[1:])
