@@ -259,8 +259,6 @@ spd_status run(const spd_shape *shape, const spd_score *score, const spd_drafts 
     p.wide = !misaligned(c.pout ? static_cast<const void *>(p.po) : c.out, 32);
     uint8_t *w = static_cast<uint8_t *>(ws);
     p.hdr = reinterpret_cast<int32_t *>(w);
-    p.bad = reinterpret_cast<int32_t *>(w + host::flags_offset(s.batch));
-    p.epoch = host::next_call_id();
     p.seqs = s.batch * s.num_kv_heads * (g > kHeadsPerItem ? g / kHeadsPerItem : 1);
     p.records = reinterpret_cast<int4 *>(w + L.records);
     p.scratch = reinterpret_cast<float *>(w + L.scratch);

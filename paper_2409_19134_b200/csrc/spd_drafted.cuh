@@ -17,6 +17,7 @@ namespace spd {
 
 constexpr int kDrTree = 256;              // most drafted tokens of a user that come as a tree
 constexpr int kDrWords = kDrTree / 32;
+constexpr float kDrBad = -1.f;            // in place of a piece's sum of weights
 constexpr int kDrMinBlocks = 1;           // do not cut the work into shares of less than that, and an item's own cost
 
 struct DraftedParams {
@@ -42,14 +43,15 @@ struct DraftedParams {
     const float *in_o, *in_m, *in_l;      // OUT_FINAL: optional partial to merge in
     void *out;                            // OUT_FINAL: [T][Hq][D]
     int32_t out_bf16, wide;               // wide: the output is aligned to 32 bytes
-    int32_t *hdr, *bad;
-    int32_t epoch, seqs;                  // seqs: what HDR_NSEQ is to hold
+    int32_t *hdr;
+    int32_t seqs;                         // what HDR_NSEQ is to hold
     int32_t grid;                         // CTAs of the launch
     int4 *records;                        // [2 * grid][2]: what the join has to know of the pieces in a CTA's two slots
     float *scratch;                       // [2 * grid] slots
 };
 
-// A slot holds one piece: O as [D / 4][RT] float4 (threads of consecutive rows write consecutive chunks), then m [RT] and l [RT].
+// A slot holds one piece: O as [D / 4][RT] float4 (threads of consecutive rows write consecutive chunks), then m [RT] and l [RT].  A sum of
+// kDrBad says that the piece met something out of order: an item that is cut becomes what a whole one does, zeros, and the join needs no other word.
 __host__ __device__ constexpr size_t drafted_slot_floats(int D, int RT) { return static_cast<size_t>(RT) * (D + 2); }
 
 struct DraftedUser {
@@ -255,8 +257,8 @@ __device__ __forceinline__ bool drafted_next(const DraftedParams &p, DraftedWalk
     return true;
 }
 
-// What the join has to know of a piece: valid, user, first token of q and first token of the tile; (KV head, head group), tokens of the tile,
-// first and last CTA that hold a piece of the item.
+// What the join has to know of a piece: valid, user, first token of q that is the tile's, (KV head, head group); tokens of the tile, first and last
+// CTA that hold a piece of the item.
 __device__ __forceinline__ void drafted_record(const DraftedParams &p, const DraftedWalk &w, int slot, int64_t W, int shares) {
     const int i0 = w.rt * p.tt;
     p.records[2 * slot] = make_int4(1, w.u, w.s.first + i0, w.sq);
@@ -273,10 +275,7 @@ __device__ __forceinline__ int drafted_shares(const DraftedParams &p, int64_t W,
 }
 
 // Raises the status of a user.
-__device__ __forceinline__ void drafted_flag(const DraftedParams &p, int u) {
-    p.bad[u] = p.epoch;
-    flag_error(p.hdr, 4 /* SPD_ERR_BAD_PAGE */, u);
-}
+__device__ __forceinline__ void drafted_flag(const DraftedParams &p, int u) { flag_error(p.hdr, 4 /* SPD_ERR_BAD_PAGE */, u); }
 
 // CTA 0 leaves in the header what the status query needs, and raises the first inconsistent offsets.
 __device__ __forceinline__ void drafted_header(const DraftedParams &p, int first_bad) {
@@ -392,15 +391,15 @@ __global__ void __launch_bounds__(kDrJoinThreads) drafted_join_kernel(const __gr
     const int slot = 2 * blockIdx.x + blockIdx.y;
     const int4 a = p.records[2 * slot], b = p.records[2 * slot + 1];
     if (a.x == 0) return;
-    const int u = a.y, tok0 = a.z, sq = a.w, toks = b.x, c0 = b.y, c1 = b.z, pieces = c1 - c0 + 1, rows = toks * p.hs;
+    const int tok0 = a.z, sq = a.w, toks = b.x, c0 = b.y, c1 = b.z, pieces = c1 - c0 + 1, rows = toks * p.hs;
     const int h0 = sq / p.hgroups * p.g + sq % p.hgroups * p.hs;
-    const bool bad = p.bad[u] == p.epoch;
     const int E = rows * (D / 16), parts = pieces * SPLIT, mine = (static_cast<int>(blockIdx.x) - c0) * SPLIT + blockIdx.z;
     const int e0 = static_cast<int>(drafted_div(static_cast<int64_t>(E) * mine, parts)), e1 = static_cast<int>(drafted_div(static_cast<int64_t>(E) * (mine + 1), parts));
     auto exp_of = [](float x) { return LOG2 ? exp2f(x) : expf(x); };
     for (int e = e0 + threadIdx.x; e < e1; e += kDrJoinThreads) {
         const int c = e / rows, r = e - c * rows;
         float o[16], m = -INFINITY, l = 0.f;
+        bool bad = false;
 #pragma unroll
         for (int i = 0; i < 16; ++i) o[i] = 0.f;
         for (int k0 = 0; k0 < pieces; k0 += AHEAD) {
@@ -418,7 +417,7 @@ __global__ void __launch_bounds__(kDrJoinThreads) drafted_join_kernel(const __gr
             }
             float M = m;
 #pragma unroll
-            for (int y = 0; y < AHEAD; ++y) M = fmaxf(M, mk[y]);
+            for (int y = 0; y < AHEAD; ++y) { M = fmaxf(M, mk[y]); bad = bad || lk[y] == kDrBad; }
             const float wa = m == -INFINITY ? 0.f : exp_of(m - M);
             l = l != l ? l : l * wa;
 #pragma unroll

@@ -258,7 +258,7 @@ __global__ void __launch_bounds__(DraftedFma<D, RT>::kThreads, DraftedFma<D, RT>
                 if (whole) drafted_put4<D>(p, row, tx + 16 * c, v, f);
                 else reinterpret_cast<float4 *>(dst)[(tx + 16 * c) * RT + r] = v;
             }
-            if (!whole && tx == 0) { dst[RT * D + r] = m[i]; dst[RT * (D + 1) + r] = l[i]; }
+            if (!whole && tx == 0) { dst[RT * D + r] = m[i]; dst[RT * (D + 1) + r] = bad ? kDrBad : l[i]; }
         }
         if (!whole && tid == 0) drafted_record(p, w, slot, W, shares);
         if (x >= x1) break;

@@ -598,7 +598,7 @@ drafted_tc_kernel(const __grid_constant__ DraftedTcParams q, const __grid_consta
                 }
                 __syncwarp();
             }
-            if (ok && live && !whole_item && (!shared || t == 0)) { dst[kDtRows * D + slot_row] = top; dst[kDtRows * (D + 1) + slot_row] = l; }
+            if (ok && live && !whole_item && (!shared || t == 0)) { dst[kDtRows * D + slot_row] = top; dst[kDtRows * (D + 1) + slot_row] = bad ? kDrBad : l; }
             const bool over = ok && live && !bad && l > 0.f && l < INFINITY && !(big < INFINITY);
             uint32_t again = __ballot_sync(0xffffffffu, over);
             if (shared) {
