@@ -386,7 +386,10 @@ template <int D, int RT, bool LOG2>
 __global__ void __launch_bounds__(kDrJoinThreads) drafted_join_kernel(const __grid_constant__ DraftedParams p) {
     constexpr float kUnit = LOG2 ? 0.69314718055994531f : 1.f;
     constexpr int AHEAD = 3, SPLIT = drafted_join_split(RT);      // pieces under way at a time
-    griddep_launch_dependents();        // what comes next may set itself up; it waits for this kernel's end before it looks at anything of this call
+    // What comes next may set itself up; it waits for this kernel's end before it looks at anything of this call.  Not behind the FMA kernel, whose CTAs share
+    // SMs: the next call's would be laid down unevenly around the join's (fp32, 8 heads of 64, call after call, early / not: 32 users x 4 tokens over 4 k
+    // tokens 265-305 us / 193, 8 x 5 over 1.5 k 51 / 38, 4 x 12 over 280 18.6 / 17.4).
+    if (LOG2) griddep_launch_dependents();
     griddep_wait();
     const int slot = 2 * blockIdx.x + blockIdx.y;
     const int4 a = p.records[2 * slot], b = p.records[2 * slot + 1];
