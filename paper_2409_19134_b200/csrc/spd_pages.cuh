@@ -342,6 +342,13 @@ static __global__ void __launch_bounds__(kPgThreads) keep_kernel(const __grid_co
             }
         }
     }
+    if (p.parents == nullptr && p.num_pools > 0 && kept > 0) {      // a run's rows stay where they are, but their pages have to be there
+        for (int64_t e = base / kPage + tid; e <= (base + kept - 1) / kPage; e += kPgThreads) {
+            const int page = p.indices[lo + e];
+            bad = bad || page < 0 || page >= p.num_pages;
+        }
+        bad = __syncthreads_or(bad);
+    }
     if (bad) kept = 0;
     if (blockIdx.y == 0) {
         if (bad && tid == 0) flag_error(p.hdr, 4 /* SPD_ERR_BAD_PAGE */, u);

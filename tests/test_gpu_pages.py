@@ -356,3 +356,28 @@ def test_take_from_a_large_pool_in_rounds():
         spd.spd_pages_release(*t.args(), i32(gone), t.ws)
         t.release(gone)
         t.same()
+
+
+def test_keep_looks_at_the_pages_of_runs():
+    """Tokens of a run stay where they are, but not on a page that is not there."""
+    counts, lout = [40, 40, 40, 20, 5, 30], [10, 10, 10, 16, 3, 0]
+    w = dr.batch(counts, [0] * 6, lout, 2, 2, 64, "bf16", seed=15, kind="run")
+    on = [p.cuda() for p in (w.pub.k_pool, w.pub.v_pool)]
+    shape = spd.make_shape(6, 2, 2, 64, torch.bfloat16, 1.0)
+    ws, g = spd.alloc_workspace(shape), w.pub.to("cuda")
+    first = w.pub.page_indptr.tolist()
+    g.page_indices[first[0] + 2] = -1                       # tokens 32 .. 47 of user 0, of which 10 .. 30 stay
+    g.page_indices[first[1] + 1] = -1                       # tokens 16 .. 31 of user 1, of which 10 .. 16 stay
+    g.page_indices[first[2] + 1] = on[0].shape[0]           # user 2: the same, behind the pool's end
+    g.page_indices[first[3]] = -1                           # user 3: in front of the drafted tokens
+    last = [20, 6, 39, 19, -1, 29]
+    g.page_indices[first[4]] = -1                           # user 4: nothing stays
+    g.seq_lens[5] = 9                                       # user 5: shorter than its draft
+    kept = torch.full((175,), 9, dtype=torch.int32, device="cuda")
+    spd.spd_keep_drafted(shape, on, g, w.indptr.cuda(), i32(last), ws, kept=kept)
+    assert spd.spd_query_device_status(ws) == (4, 1)           # and users 2 and 5
+    assert g.seq_lens.tolist() == [31, 50, 50, 36, 3, 9]
+    names = [list(range(x + 1)) + [-1] * (n - x - 1) for n, x in zip(counts, [20, -1, -1, 19, -1, -1])]
+    assert kept.tolist() == sum(names, [])
+    for a, b in zip(on, (w.pub.k_pool, w.pub.v_pool)):
+        assert torch.equal(a.cpu().nan_to_num(7.0), b.nan_to_num(7.0))
