@@ -86,7 +86,6 @@ spd_status spd_pages_release(const spd_shape *shape, int32_t num_pages, int32_t 
     if (!from_tokens) return SPD_ERR_INVALID_ARG;
     const spd_status rc = fill(shape, num_pages, refs, page_indptr, page_indices, ws, ws_bytes, p, &sms);
     if (rc != SPD_OK) return rc;
-    if (num_pages == 0) return SPD_OK;
     p.from = from_tokens; p.to = to_tokens;
     const int per_user = std::max(1, std::min(32, 2 * sms / p.B));      // a few users may have long tables
     pages_release_kernel<<<dim3(static_cast<unsigned>(p.B), static_cast<unsigned>(per_user)), kPgThreads, 0, static_cast<cudaStream_t>(cuda_stream)>>>(p);

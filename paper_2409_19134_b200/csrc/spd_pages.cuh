@@ -47,11 +47,12 @@ __device__ __forceinline__ void pages_header(int32_t *hdr, int B, int seqs) {
     hdr[HDR_NSEQ] = seqs;
 }
 
+// A user's entries; false where its table is inconsistent, or has entries and is not there.
 __device__ __forceinline__ bool pages_entries(const PagesParams &p, int u, int64_t &lo, int64_t &cap) {
     const int64_t hi = p.indptr[u + 1], end = p.indptr[p.B];
     lo = p.indptr[u];
     cap = hi - lo;
-    return lo >= 0 && cap >= 0 && hi <= end;
+    return lo >= 0 && cap >= 0 && hi <= end && (cap == 0 || p.indices != nullptr);
 }
 
 // Block-wide: exclusive prefix of v over the threads, and the total.

@@ -381,3 +381,27 @@ def test_keep_looks_at_the_pages_of_runs():
     assert kept.tolist() == sum(names, [])
     for a, b in zip(on, (w.pub.k_pool, w.pub.v_pool)):
         assert torch.equal(a.cpu().nan_to_num(7.0), b.nan_to_num(7.0))
+
+
+def test_tables_that_are_not_there():
+    """No pages and no entries, though the offsets list some: users that have any are refused, nothing is read."""
+    shape = spd.make_shape(3, 2, 2, 64, torch.bfloat16, 1.0)
+    ws, none, indptr = spd.alloc_workspace(shape), torch.zeros(0, dtype=torch.int32, device="cuda"), i32([0, 0, 2, 5])
+    lens, copies = i32([0, 20, 0]), i32(np.zeros((3, 2)))
+    spd.spd_pages_take(shape, none, indptr, none, i32([0, 0, 0]), i32([0, 0, 20]), ws)
+    assert spd.spd_query_device_status(ws) == (4, 1)
+    spd.spd_pages_release(shape, none, indptr, none, i32([0, 0, 0]), ws)
+    assert spd.spd_query_device_status(ws) == (4, 1)
+    spd.spd_pages_fork(shape, none, indptr, none, lens, i32([-1, -1, 1]), copies, ws)
+    assert spd.spd_query_device_status(ws) == (4, 2)
+    assert lens.tolist() == [0, 20, 0] and copies.tolist() == [[-1, -1]] * 3
+    spd.spd_pages_fork(shape, none, indptr, none, lens, i32([-1, 0, 0]), copies, ws)      # of a user without tokens, into entries that are not there
+    assert spd.spd_query_device_status(ws) == (4, 1)
+    empty = i32([0, 0, 0, 0])                                                             # nobody lists anything: nothing to do
+    spd.spd_pages_take(shape, none, empty, none, i32([0, 0, 0]), i32([0, 0, 0]), ws)
+    spd.spd_pages_release(shape, none, empty, none, i32([0, 0, 0]), ws)
+    spd.spd_pages_fork(shape, none, empty, none, i32([0, 0, 0]), i32([-1, 0, -1]), copies, ws)
+    assert spd.spd_query_device_status(ws) == (spd.SPD_OK, -1)
+    held = i32([3, -1, -1, -1, -1])                                                       # entries, but no pool: a page that is listed is out of range
+    spd.spd_pages_release(shape, none, indptr, held, i32([0, 0, 0]), ws)
+    assert spd.spd_query_device_status(ws) == (4, 1) and held.tolist() == [3, -1, -1, -1, -1]
