@@ -774,16 +774,22 @@ def spd_service_attn_merge_drafted(shape, score, q, pub, priv_lens, partial_in, 
                                                 _stream_ptr(stream)), "spd_service_attn_merge_drafted")
 
 
+def _layout(shape):
+    """What the rows of a pool's pages go by."""
+    return shape.num_kv_heads, shape.page_size, shape.head_dim, shape.dtype
+
+
 class Pools:
     """Pools that share their pages' tables, K and V of any number of layers, as the calls take them; it keeps them alive."""
 
     def __init__(self, shape, pools):
         pools = list(pools)
         self.dev = _here(pools[0]) if pools else -1
-        self.pages, self.page, self.dtype = (pools[0].shape[0] if pools else 0), shape.num_kv_heads * shape.page_size * shape.head_dim, _TORCH_DTYPES[shape.dtype]
+        self.pages, self.layout = (pools[0].shape[0] if pools else 0), _layout(shape)
+        page, dtype = shape.num_kv_heads * shape.page_size * shape.head_dim, _TORCH_DTYPES[shape.dtype]
         for t in pools:
-            if t.dtype is not self.dtype or t.shape[0] != self.pages or t.numel() != self.pages * self.page or not t.is_contiguous():
-                raise ValueError(f"expected contiguous {self.dtype} pools of {self.pages} pages of {self.page} elements (KV heads x page size x "
+            if t.dtype is not dtype or t.shape[0] != self.pages or t.numel() != self.pages * page or not t.is_contiguous():
+                raise ValueError(f"expected contiguous {dtype} pools of {self.pages} pages of {page} elements (KV heads x page size x "
                                  f"head_dim), got {t.dtype} {list(t.shape)}")
             if t.get_device() != self.dev:
                 raise _elsewhere(t)
@@ -798,7 +804,7 @@ def make_pools(shape, pools) -> Pools:
 def _pools(shape, pools, dev) -> Pools:
     if not isinstance(pools, Pools):
         pools = Pools(shape, pools)
-    elif pools.page != shape.num_kv_heads * shape.page_size * shape.head_dim or pools.dtype is not _TORCH_DTYPES[shape.dtype]:
+    elif pools.layout != _layout(shape):
         raise ValueError("the pools were made for another shape")
     if pools.count and pools.dev != dev:
         raise _elsewhere(pools._keep[0])

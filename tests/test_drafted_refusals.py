@@ -190,3 +190,18 @@ def test_python_page_calls_check_their_tensors(calls):  # noqa: F811
         with pytest.raises(ValueError):
             spd.spd_keep_drafted(FAKE, [pool], a["part"], a["ip"], a["last"], ws, parents=a["parents"], kept=a["kept"], new_lens=a["new"], stream=FakeStream)
     assert calls == []
+
+
+@pytest.mark.parametrize("other", [spd.make_shape(B, HQ, HKV // 2, 2 * D, BF16, 1.0), spd.make_shape(B, HQ, 2 * HKV, D, BF16, 1.0),
+                                   spd.make_shape(B, HQ, HKV, D, torch.float32, 1.0)])
+def test_pools_made_for_other_rows_are_refused(calls, other):  # noqa: F811
+    """Pages of as many elements, cut into other heads."""
+    handle, u = spd.make_pools(FAKE, [FakeTensor(7, HKV, 16, D, dtype=BF16)]), FakeTensor(B, **I32)
+    ws, pairs = FakeTensor(1 << 20, dtype=torch.uint8), FakeTensor(4, 2, **I32)
+    spd.spd_pages_copy(FAKE, handle, pairs, ws, stream=FakeStream)
+    assert calls == ["spd_pages_copy"]
+    with pytest.raises(ValueError):
+        spd.spd_pages_copy(other, handle, pairs, ws, stream=FakeStream)
+    with pytest.raises(ValueError):
+        spd.spd_keep_drafted(other, handle, FakePart(B, 7, HKV, D, BF16), FakeTensor(B + 1, **I32), u, ws, parents=FakeTensor(T, **I32), stream=FakeStream)
+    assert calls == ["spd_pages_copy"]
