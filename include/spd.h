@@ -404,9 +404,11 @@ spd_status spd_keep_drafted(const spd_shape *shape, int64_t total_tokens, const 
  * A user with an inconsistent table or request (ranges behind the table's end, negative numbers, a fork into entries in use, pages out of range or
  * with refs that say nobody lists them) raises SPD_ERR_BAD_PAGE; take and fork leave it as it is, release takes out the entries that are
  * in order.  A pair with a page out of range is left out and raises SPD_ERR_BAD_PAGE (for the pair's number in place of a user's).
- * Plain stream order; take and fork are two kernels, release is one, copy one per 128 pools.  The workspace is one of spd_workspace_size;
- * take and fork keep 4 bytes per page in it, and pools of more than a million pages may need a larger one (SPD_ERR_WORKSPACE).
+ * Plain stream order; take and fork are two kernels, release is one, copy one per 128 pools.  The workspace is one of spd_pages_workspace_size
+ * (which serves all other calls of the shape but the drafted ones too): take and fork keep 4 bytes per page in it, and pools of more than about a million pages
+ * need more than spd_workspace_size or spd_drafted_workspace_size say (SPD_ERR_WORKSPACE).
  */
+spd_status spd_pages_workspace_size(const spd_shape *shape, int32_t num_pages, size_t *bytes);
 spd_status spd_pages_take(const spd_shape *shape, int32_t num_pages, int32_t *refs, const int32_t *page_indptr, int32_t *page_indices,
                           const int32_t *from_tokens, const int32_t *to_tokens, void *ws, size_t ws_bytes, void *cuda_stream);
 spd_status spd_pages_release(const spd_shape *shape, int32_t num_pages, int32_t *refs, const int32_t *page_indptr,

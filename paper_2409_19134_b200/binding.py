@@ -30,7 +30,7 @@ EXPORTS = ["spd_workspace_size", "spd_partial_attn", "spd_service_attn_merge", "
            "spd_debug_sm_moves", "spd_decode_step_append", "spd_watch_alarm", "spd_service_attn_merge_append",
            "spd_partial_attn_scored", "spd_service_attn_merge_scored", "spd_decode_step_scored", "spd_prefill_attn_scored",
            "spd_append_kv_rope", "spd_drafted_workspace_size", "spd_decode_step_drafted", "spd_partial_attn_drafted",
-           "spd_service_attn_merge_drafted", "spd_keep_drafted", "spd_pages_take", "spd_pages_release", "spd_pages_fork", "spd_pages_copy"]
+           "spd_service_attn_merge_drafted", "spd_keep_drafted", "spd_pages_workspace_size", "spd_pages_take", "spd_pages_release", "spd_pages_fork", "spd_pages_copy"]
 
 
 class SpdError(RuntimeError):
@@ -150,6 +150,7 @@ def lib() -> C.CDLL:
         L.spd_service_attn_merge_drafted.argtypes = [C.POINTER(Shape), C.POINTER(Score), C.POINTER(Drafts), vp, C.POINTER(PagedKV), vp,
                                                      Partial, vp, C.c_int, vp, sz, vp]
         L.spd_keep_drafted.argtypes = [C.POINTER(Shape), C.c_int64, vp, vp, vp, C.c_int32, vp, C.c_int32, vp, vp, vp, vp, vp, vp, sz, vp]
+        L.spd_pages_workspace_size.argtypes = [C.POINTER(Shape), C.c_int32, C.POINTER(sz)]
         for name in ("take", "release"):
             getattr(L, "spd_pages_" + name).argtypes = [C.POINTER(Shape), C.c_int32, vp, vp, vp, vp, vp, vp, sz, vp]
         L.spd_pages_fork.argtypes = [C.POINTER(Shape), C.c_int32, vp, vp, vp, vp, vp, vp, vp, sz, vp]
@@ -826,6 +827,17 @@ def spd_keep_drafted(shape, pools, part, tok_indptr, last, ws, parents=None, new
     _check(lib().spd_keep_drafted(shape, T, _ints(tok_indptr, B + 1, dev), _ints(parents, T, dev), _ints(last, B, dev), pools.count, pools.array, pools.pages,
                                   _ints(part.page_indptr, B + 1, dev), _ints(indices, indices.numel(), dev), lens, new_lens, _ints(kept, T, dev),
                                   *_workspace(ws, dev), _stream_ptr(stream)), "spd_keep_drafted")
+
+
+def spd_pages_workspace_size(shape: Shape, num_pages: int) -> int:
+    n = C.c_size_t(0)
+    _check(lib().spd_pages_workspace_size(shape, num_pages, C.byref(n)), "spd_pages_workspace_size")
+    return int(n.value)
+
+
+def alloc_pages_workspace(shape: Shape, num_pages: int, device="cuda") -> torch.Tensor:
+    """A zeroed workspace for the spd_pages_* calls over pools of num_pages pages, and for every other call of the shape but the *_drafted ones."""
+    return torch.zeros(spd_pages_workspace_size(shape, num_pages), dtype=torch.uint8, device=device)
 
 
 def spd_pages_take(shape, refs, page_indptr, page_indices, from_tokens, to_tokens, ws, stream=None) -> None:

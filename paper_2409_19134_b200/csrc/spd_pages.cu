@@ -79,6 +79,14 @@ spd_status check_pools(const spd_shape *shape, int32_t num_pools, void *const *p
 
 extern "C" {
 
+spd_status spd_pages_workspace_size(const spd_shape *shape, int32_t num_pages, size_t *bytes) {
+    if (!bytes || num_pages < 0 || num_pages > (1 << 30)) return SPD_ERR_INVALID_ARG;
+    const spd_status rc = spd_workspace_size(shape, bytes);
+    if (rc != SPD_OK) return rc;
+    *bytes = std::max(*bytes, pages_layout(host::cleared_end(shape->batch, seqs_of(*shape)), shape->batch, num_pages).total);
+    return SPD_OK;
+}
+
 spd_status spd_pages_release(const spd_shape *shape, int32_t num_pages, int32_t *refs, const int32_t *page_indptr, int32_t *page_indices,
                              const int32_t *from_tokens, const int32_t *to_tokens, void *ws, size_t ws_bytes, void *cuda_stream) {
     PagesParams p{};

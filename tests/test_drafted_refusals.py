@@ -205,3 +205,11 @@ def test_pools_made_for_other_rows_are_refused(calls, other):  # noqa: F811
     with pytest.raises(ValueError):
         spd.spd_keep_drafted(other, handle, FakePart(B, 7, HKV, D, BF16), FakeTensor(B + 1, **I32), u, ws, parents=FakeTensor(T, **I32), stream=FakeStream)
     assert calls == ["spd_pages_copy"]
+
+
+def test_pages_workspace_size_checks_its_arguments(lib):
+    n = C.c_size_t(0)
+    assert "spd_pages_workspace_size" in spd.EXPORTS
+    assert lib.spd_pages_workspace_size(SHAPE, 8, None) == INVALID and lib.spd_pages_workspace_size(None, 8, C.byref(n)) == INVALID
+    assert lib.spd_pages_workspace_size(SHAPE, -1, C.byref(n)) == INVALID and lib.spd_pages_workspace_size(SHAPE, (1 << 30) + 1, C.byref(n)) == INVALID
+    assert lib.spd_pages_workspace_size(spd.make_shape(2, 8, 3, 64, torch.bfloat16, 1.0), 8, C.byref(n)) == UNSUPPORTED

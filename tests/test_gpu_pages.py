@@ -405,3 +405,20 @@ def test_tables_that_are_not_there():
     held = i32([3, -1, -1, -1, -1])                                                       # entries, but no pool: a page that is listed is out of range
     spd.spd_pages_release(shape, none, indptr, held, i32([0, 0, 0]), ws)
     assert spd.spd_query_device_status(ws) == (4, 1) and held.tolist() == [3, -1, -1, -1, -1]
+
+
+def test_workspace_for_a_pool_of_many_pages():
+    """Four bytes per page do not fit every shape's workspace: the size call says what does."""
+    shape, pages = spd.make_shape(2, 1, 1, 64, torch.bfloat16, 1.0), 6_000_001
+    assert spd.spd_pages_workspace_size(shape, 0) == spd.spd_workspace_size(shape)
+    refs, indptr, indices = torch.ones(pages, dtype=torch.int32, device="cuda"), i32([0, 3, 5]), i32([-1] * 5)
+    refs[[5, 4_000_000, pages - 2, pages - 1]] = 0
+    size = spd.spd_pages_workspace_size(shape, pages)
+    assert size > spd.spd_workspace_size(shape)
+    with pytest.raises(spd.SpdError, match="SPD_ERR_WORKSPACE"):
+        spd.spd_pages_take(shape, refs, indptr, indices, i32([0, 0]), i32([40, 16]), torch.zeros(size - 1, dtype=torch.uint8, device="cuda"))
+    ws = spd.alloc_pages_workspace(shape, pages)
+    assert ws.numel() == size
+    spd.spd_pages_take(shape, refs, indptr, indices, i32([0, 0]), i32([40, 16]), ws)
+    assert spd.spd_query_device_status(ws) == (spd.SPD_OK, -1)
+    assert indices.tolist() == [5, 4_000_000, pages - 2, pages - 1, -1] and int(refs.sum()) == pages
