@@ -342,7 +342,9 @@ spd_status spd_decode_step_scored(const spd_shape *shape, const spd_score *score
  * [total_tokens][num_q_heads][head_dim], packed.
  * Keys that a row does not see never enter its result, whatever their rows of k and v hold; a row that sees nothing, or only scores of -inf, gives
  * zeros (the empty partial).  A user with an inconsistent table, length or tree (a parent out of range, more drafted tokens than public ones)
- * raises SPD_ERR_BAD_PAGE and gets zeros; one with a page out of range raises it too, and gets zeros wherever that page was needed.
+ * raises SPD_ERR_BAD_PAGE and gets zeros; one with a page out of range raises it too, and gets zeros in every tile of tokens (256 rows of a KV head at
+ * most) of which some row may see a token of that page, whatever the other users are.  A call judges its users afresh, a replayed one too.  Users
+ * without drafted tokens are not looked at.  In halves each one knows only what it reads itself.
  * The workspace is one of spd_drafted_workspace_size (which serves all other calls of the shape too).  Two kernels in plain stream order (the
  * second starts early and waits for the first); results do not depend on timing.  sm_scale > 0, else SPD_ERR_UNSUPPORTED.
  */
@@ -373,8 +375,8 @@ spd_status spd_service_attn_merge_drafted(const spd_shape *shape, const spd_scor
  *   tok_indptr, parents as for spd_drafts (parents NULL: tokens 0 .. last[u] stay, and nothing has to move).
  *   new_lens [batch]: the lengths afterwards; seq_lens itself (in place), another array, or NULL.
  *   kept [total_tokens] or NULL: kept[tok_indptr[u] + i] = the token that is now the i-th, -1 behind the last one.
- * A user with an inconsistent table, length, tree or `last`, or a page out of range among the rows that stay, keeps its rows and its length (kept: -1)
- * and raises SPD_ERR_BAD_PAGE.  The pages that hold drafted tokens must not be shared with another user.  new_lens and kept overlap no other argument.
+ * A user with an inconsistent table, length, tree or `last`, or a page out of range among the rows that stay (of a run too; not looked at where num_pools is
+ * 0), keeps its rows and its length (kept: -1) and raises SPD_ERR_BAD_PAGE.  The pages that hold drafted tokens must not be shared with another user.  new_lens and kept overlap no other argument.
  * One kernel per 128 pools, in plain stream order; the workspace is one of spd_workspace_size.
  */
 spd_status spd_keep_drafted(const spd_shape *shape, int64_t total_tokens, const int32_t *tok_indptr, const int32_t *parents,
@@ -401,9 +403,9 @@ spd_status spd_keep_drafted(const spd_shape *shape, int64_t total_tokens, const 
  *   source[u] = -1: the user stays as it is.  Entries of -1 in full pages (released behind a window) stay -1.
  * spd_pages_copy copies page copies[i][0] to page copies[i][1] (device [num_copies][2], (-1, -1) = nothing) in every pool (HOST array, as for
  *   spd_keep_drafted).  No page may be the target of two pairs, nor the source of one and the target of another.
- * A user with an inconsistent table or request (ranges behind the table's end, negative numbers, a fork into entries in use, pages out of range or
- * with refs that say nobody lists them) raises SPD_ERR_BAD_PAGE; take and fork leave it as it is, release takes out the entries that are
- * in order.  A pair with a page out of range is left out and raises SPD_ERR_BAD_PAGE (for the pair's number in place of a user's).
+ * A user with an inconsistent table or request (a table that is not there, negative numbers, to_tokens of a take behind the table's end, a fork into entries in
+ * use or from a table too short, pages out of range or with refs that say nobody lists them) raises SPD_ERR_BAD_PAGE.  Take and fork leave it as it is; release
+ * takes out the other entries, and that of a page that nobody lists, whose refs stay 0.  Ranges of a release may reach behind the table's end.  A pair with a page out of range is left out and raises SPD_ERR_BAD_PAGE (for the pair's number in place of a user's).
  * Plain stream order; take and fork are two kernels, release is one, copy one per 128 pools.  The workspace is one of spd_pages_workspace_size
  * (which serves all other calls of the shape but the drafted ones too): take and fork keep 4 bytes per page in it, and pools of more than about a million pages
  * need more than spd_workspace_size or spd_drafted_workspace_size say (SPD_ERR_WORKSPACE).

@@ -188,8 +188,8 @@ spd_status launch_fma(DraftedParams p, int sms, cudaStream_t st) {
 }
 
 // Tiles of 16 rows (several CTAs per SM, each with its own keys) or of 64, by the rows of a KV head, on average over the users.  us, 16 / 64 rows,
-// 32 users, 4 k tokens: 8 heads of 64, 4 rows 266 / 839, 16 rows 302 / 840, 20 to 32 rows (two tiles of 16) 548 / 868, so three tiles about even;
-// 32/8 heads of 128, 16 rows 640 / 1162, 24 rows 1248 / 1168, 40 rows 1868 / 1431.
+// 32 users, 4 k tokens: 8 heads of 64, 4 rows 193 / 814, 16 rows 280 / 820, 20 rows (two tiles of 16) 531 / 825, 32 rows 540 / 854, 33 to 48 rows (three
+// tiles) 791-796 / 950-960, which the rule leaves to tiles of 64; 32/8 heads of 128, 16 rows 624 / 1140, 20 to 32 rows 1220 / 1150-1169, 40 rows 1828 / 1395.
 spd_status run_fma(const DraftedParams &p, int D, int sms, cudaStream_t st) {
     const bool few = p.T * p.g <= (D == 128 ? 16ll : 32ll) * p.B;
     if (D == 128) return few ? launch_fma<128, 16>(p, sms, st) : launch_fma<128, 64>(p, sms, st);

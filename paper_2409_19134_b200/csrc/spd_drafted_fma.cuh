@@ -4,9 +4,9 @@
 // registers, weights go through shared memory to the threads that hold the row's channels (the same 16).  A hidden key's weight is the
 // mark -1, which the product with V skips: whatever its rows of k and v hold never enters.  V comes (cp.async) under the scores, the next block's K under
 // the weights and the product with V, so that a CTA has loads under way all the time.  Bound by shared-memory reads (RPT x 4 register tiles) and, where
-// rows are few, by what a CTA has under way.  Measured, fp32: 32 users x 4-token trees over 4 k tokens, 8 heads of 64: 232-276 us (2.0-2.3 TB/s; 512 without
-// the copies ahead and with two CTAs per SM), 32/8 heads of 128: 642 us (1.7); 8 users x 64 tokens over 4 k tokens, 32/8 heads of 128: 1.53 ms (22.5
-// TFLOP/s); 4 users x 12 tokens over 270-290 tokens, 8 heads of 64: 19 us with the join (44 with four rows per thread and blocks in pairs).
+// rows are few, by what a CTA has under way.  Measured, fp32, call after call: 32 users x 4-token trees over 4 k tokens, 8 heads of 64: 193 us (2.7 TB/s; with 4 rows one warp of a CTA's four
+// computes), 32/8 heads of 128: 621 us (1.7); 8 users x 64 tokens over 4 k tokens, 32/8 heads of 128: 1.48 ms (23 TFLOP/s); 4 users x 12 tokens over
+// 270-290 tokens, 8 heads of 64: 17.4 us with the join.
 #pragma once
 
 #include "spd_drafted.cuh"

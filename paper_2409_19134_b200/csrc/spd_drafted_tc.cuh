@@ -16,8 +16,9 @@
 // without a look at what they do not see.  So are rows whose sums left fp32's range by themselves (weights are relative to a reference
 // that may lag 2^8 behind the maximum).
 //
-// Bound: HBM where tiles hold one user's few rows; the chain of a block's softmax where two tiles share long caches (2200 cycles a block of 2 x 128 x
-// 80 scores, 3200 with a cap; tensor and exponential pipes are at half then); over seconds the power limit.  Measured back to back in a first burst,
+// Bound: HBM where tiles hold one user's few rows.  Where two tiles share long caches a block's softmax is a chain of 2200 cycles per 2 x 128 x 80 scores
+// (3200 with a cap; tensor and exponential pipes are at half then), which explains three quarters of such a call; the rest has not been
+// accounted for.  Over seconds the power limit.  Measured back to back in a first burst,
 // head_dim 128, 32/8 heads: 64 users x 26-token trees over 1-9 k tokens 221 us (1.31 GB, 5.9 TB/s with the join; 250 over seconds), 64 users x one
 // token through a window of 2048 behind 4 sinks 104 us (5.2 TB/s), 4 users x 64-token trees over 33-80 k tokens 296 us (980 TFLOP/s), 1.5-2.1 k new
 // tokens of 2 users through a window of 1500 behind 16 sinks, cap 50, 168 us (530 TFLOP/s of visible pairs).
