@@ -66,6 +66,18 @@ def test_huge_caps_change_nothing(alibi, monkeypatch):
     dr.close(outs[1], outs[0].cpu().double(), tols[0] + tols[1])
 
 
+@pytest.mark.parametrize("kind,window", [("tree", 0), ("run", 90)])
+def test_scales_that_leave_nothing_of_the_quotient(kind, window, monkeypatch):
+    """sm_scale / cap below fp32's range: scores of ordinary size stay what they are without a cap."""
+    w = dr.batch([9, 40], [400, 170], [37, 20], 4, 2, 64, "bf16", seed=4, kind=kind)
+    w.sm_scale, w.q = 1e-20, (w.q.float() * 1e19).bfloat16()
+    g = dr.OnDevice(w, 1e30, window)
+    monkeypatch.setattr(ref, "bound", bound)
+    want, _, _, _, tol = dr.expected(w, 1e30, window)
+    dr.close(g.fused(), want, tol)
+    ok(g)
+
+
 def capped(w, cap=20.0, window=0):
     g = dr.OnDevice(w, cap, window)
     out = g.fused()
